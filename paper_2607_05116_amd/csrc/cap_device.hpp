@@ -16,6 +16,7 @@ constexpr int kMaxDevices = 64;                       // per-device caches of ho
 constexpr size_t kLayoutScratchBytes = size_t(4) << 20;   // cap_dispatch_layout_static's workspace
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 // 16- and 8-byte raw vectors (native clang vector: stay in registers, unlike HIP's uint4 struct)
