@@ -11,7 +11,8 @@
  *   combine (Sec. II-C, Eq. 1), also folded into the FFN for tokens with one
  *   kept expert on the rank; expert co-activation counts (Sec. IV-B); the
  *   expert-level pruning baseline (Sec. II-D); the Adjustment Approach's
- *   placement spectrum (Sec. V).
+ *   placement spectrum (Sec. V).  For training: the load-balance loss of the
+ *   routing with its gradient, and the orthogonalised update of weights.
  * Expert-parallel ranks are virtual: all of them live on the one GPU.
  *
  * Conventions for every call
@@ -80,7 +81,9 @@ typedef enum {
     CAP_OP_COMBINE = 4,
     CAP_OP_COACTIVATION = 5,
     CAP_OP_ADJUSTMENT = 6,
-    CAP_OP_ROUTE_LAYOUT = 7
+    CAP_OP_ROUTE_LAYOUT = 7,
+    CAP_OP_BALANCE_LOSS = 8,
+    CAP_OP_ORTHOGONALISE = 9
 } cap_op;
 
 /*
@@ -164,6 +167,11 @@ int32_t cap_version(void);
  *   CAP_OP_ADJUSTMENT: the E x E fp64 co-activation ratios (uses topo->E).
  *   CAP_OP_ROUTE_LAYOUT: per-32-token column counts, column totals, volume
  *                      sums and co-activation partials (uses topo only).
+ *   CAP_OP_BALANCE_LOSS: partial sums of cap_balance_loss (uses topo->T and
+ *                      topo->E; max_rows is the number of sequences).
+ *   CAP_OP_ORTHOGONALISE: the products of cap_orthogonalise and cap_muon_update
+ *                      (inter is rows, d is cols, max_rows is the batch; topo
+ *                      unused, may be NULL).
  *   Other ops need none.
  * Returns 0 for invalid arguments as well.
  */
@@ -506,6 +514,85 @@ cap_status cap_adjustment_spectrum(const uint32_t *coact, int32_t E, int32_t R, 
                                    float inter_node_cost, int32_t *expert_rank, int32_t *expert_local,
                                    int32_t max_swaps, int32_t *swaps, double *deltas, int32_t *n_swaps,
                                    void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Load-balance loss of a batch's routing, with its counts (training of the
+ * router; the device loads that Sec. V balances are sums of these counts).
+ *   logits[T][E]  fp32 router logits; idx, keep [T][k] as cap_route_prune gives
+ *                 them (keep NULL: every slot is kept).
+ *   token_mask[T] (nullable) 0 for padding tokens: they count nowhere, whatever
+ *                 their rows hold.
+ *   seq_offsets[n_seq+1] (device; NULL needs n_seq == 1: all T tokens are one
+ *                 sequence) non-decreasing offsets of the sequences, which may be
+ *                 empty; tokens outside all of them count nowhere.
+ * A token is valid if it belongs to a sequence, its mask is not 0 and it has a
+ * logit above -inf (single logits may be -inf: experts that are switched off;
+ * +inf and NaN in a valid token's row are a precondition violation).  With
+ * P_te the softmax of token t's logits, lse_t their log-sum-exp, n_s the valid
+ * tokens of sequence s, present the sequences that have one, N their sum:
+ *   counts[n_seq][E] c_se = kept slots of valid tokens of s whose expert is e
+ *   probs[n_seq][E]  p_se = (sum of P_te over valid tokens of s) / n_s, 0 if n_s = 0
+ *   tokens[n_seq+2]  n_s of each sequence, then present, then N
+ *   loss[3]          balance_coef * balance + z_coef * z, then
+ *     balance = (sum over s of E / (k n_s) * sum over e of c_se p_se) / present,
+ *     z       = (sum over valid t of lse_t^2) / N;  all 0 without a valid token.
+ * Sums are fp32, in an order fixed by T and the offsets.  1 <= k <= 8, k <= E <=
+ * 256, T >= 0, n_seq * E < 2^31.  Workspace: cap_workspace_size(
+ * CAP_OP_BALANCE_LOSS, topo with this T and E, 0, 0, n_seq, ...), 256-byte aligned.
+ */
+cap_status cap_balance_loss(int32_t T, int32_t k, int32_t E, const float *logits, const int32_t *idx,
+                            const uint8_t *keep, const uint8_t *token_mask, const int32_t *seq_offsets,
+                            int32_t n_seq, float balance_coef, float z_coef, int32_t *counts, float *probs,
+                            int32_t *tokens, float *loss, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Gradient of the router logits: of cap_balance_loss's total and of the gates
+ * w' that the combine weighs with (Eq. 1; cap_route_prune).
+ *   counts, tokens  as cap_balance_loss wrote them for the same arguments;
+ *   d_loss  (device, nullable: 1) the gradient that arrives at the total loss;
+ *   w[T][k] the gates; d_w[T][k] (nullable: none) the gradient at them.
+ * d_logits[T][E] (fp32 or bf16, rounded to nearest even once) =
+ *   d_loss * (P_te (C_se - sum over f of P_tf C_sf) + 2 z_coef lse_t P_te / N)
+ *     with C_se = balance_coef E c_se / (k n_s^2 present) (counts have no gradient),
+ *   + for each kept slot s of t whose expert is e: w_ts (d_w_ts - sum over t's
+ *     kept slots of w d_w);
+ *   0 for tokens that are not valid.
+ * A token's experts are distinct.  Limits as cap_balance_loss.  No workspace.
+ */
+cap_status cap_router_grad(int32_t T, int32_t k, int32_t E, const float *logits, const int32_t *idx,
+                           const uint8_t *keep, const float *w, const float *d_w, const uint8_t *token_mask,
+                           const int32_t *seq_offsets, int32_t n_seq, const int32_t *counts, const int32_t *tokens,
+                           float balance_coef, float z_coef, const float *d_loss, cap_dtype dtype, void *d_logits,
+                           void *stream);
+
+/*
+ * Orthogonalised form of a batch of matrices (an optimizer's update for the
+ * experts' or the router's weights): `steps` Newton-Schulz steps
+ *   X <- a X + b (X X^T) X + c (X X^T)^2 X   from   X = G / (|G|_F + eps),
+ * each matrix by itself, which bring its singular values to about 1.
+ *   g[batch][rows][cols]   fp32 or bf16;  out[batch][rows][cols] bf16.
+ *   coef (HOST, [steps][3], nullable) a, b, c of each step; NULL: the quintic
+ *     3.4445, -4.7750, 2.0315 for all of them.
+ * Products take fp16 operands and fp32 sums, X is carried to 22 bits between the
+ * steps; steps should keep its singular values below about 100 (with the default
+ * they stay below 1.3).  A non-finite value in a matrix gives NaN in that matrix
+ * alone; a matrix of zeros gives zeros.  0 <= rows, cols <= 65536, batch <= 65535,
+ * 1 <= steps <= 16; nothing is done if one of the sizes is 0.  Workspace:
+ * cap_workspace_size(CAP_OP_ORTHOGONALISE, NULL, cols, rows, batch, ...), 256-byte
+ * aligned; its contents need no initialisation.
+ */
+cap_status cap_orthogonalise(cap_dtype dtype, int32_t batch, int32_t rows, int32_t cols, const void *g, int32_t steps,
+                             const float *coef, float eps, void *out, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * cap_orthogonalise of the momentum: M <- mu M + G (fp32, in place), then of
+ * G + mu M (nesterov != 0) or of M.  0 <= mu < 1.
+ *   momentum[batch][rows][cols]  fp32, zeros before the first step.
+ * Other arguments, limits and workspace as cap_orthogonalise.
+ */
+cap_status cap_muon_update(cap_dtype dtype, int32_t batch, int32_t rows, int32_t cols, const void *g, float *momentum,
+                           float mu, int32_t nesterov, int32_t steps, const float *coef, float eps, void *out, void *ws,
+                           size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

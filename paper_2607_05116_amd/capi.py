@@ -8,7 +8,8 @@ call raises CapError on a non-zero status.
 Function names follow the C ABI: cap_route_prune, cap_route_prune_naive, cap_router_route_prune,
 cap_dispatch_layout,
 cap_permute, cap_row_plan, cap_expert_ffn, cap_expert_ffn_gather, cap_expert_ffn_ex, cap_expert_ffn_combine,
-cap_combine, cap_coactivation, cap_workspace_size, cap_status_string, cap_version.
+cap_combine, cap_coactivation, cap_balance_loss, cap_router_grad, cap_orthogonalise, cap_muon_update,
+cap_workspace_size, cap_status_string, cap_version.
 """
 from __future__ import annotations
 
@@ -25,14 +26,16 @@ CAP_DTYPE_F32, CAP_DTYPE_BF16 = 0, 1
 CAP_PERMUTE_EXPERT_GATHER, CAP_PERMUTE_SEND_PACK, CAP_PERMUTE_ROW_SOURCE = 0, 1, 2
 CAP_COMBINE_DEST_REDUCE, CAP_COMBINE_SRC_REDUCE, CAP_COMBINE_DEST_REDUCE_MULTI = 0, 1, 2
 (CAP_OP_ROUTE_PRUNE, CAP_OP_DISPATCH_LAYOUT, CAP_OP_PERMUTE, CAP_OP_EXPERT_FFN,
- CAP_OP_COMBINE, CAP_OP_COACTIVATION, CAP_OP_ADJUSTMENT, CAP_OP_ROUTE_LAYOUT) = range(8)
+ CAP_OP_COMBINE, CAP_OP_COACTIVATION, CAP_OP_ADJUSTMENT, CAP_OP_ROUTE_LAYOUT, CAP_OP_BALANCE_LOSS,
+ CAP_OP_ORTHOGONALISE) = range(10)
 
 EXPORTS = ["cap_status_string", "cap_version", "cap_workspace_size", "cap_route_prune", "cap_route_prune_naive",
            "cap_router_route_prune",
            "cap_dispatch_layout", "cap_permute", "cap_expert_ffn", "cap_expert_ffn_gather", "cap_expert_ffn_ex",
            "cap_combine", "cap_coactivation", "cap_dispatch_layout_static",
            "cap_dispatch_layout_static_max_bytes", "cap_adjustment_spectrum", "cap_route_layout",
-           "cap_row_plan", "cap_expert_ffn_combine"]
+           "cap_row_plan", "cap_expert_ffn_combine", "cap_balance_loss", "cap_router_grad", "cap_orthogonalise",
+           "cap_muon_update"]
 
 
 class CapError(RuntimeError):
@@ -92,6 +95,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                          P(Layout), vp, vp, i32, vp], ctypes.c_int),
         "cap_coactivation": ([i32, i32, i32, vp, vp, vp, i32, vp, sz, vp], ctypes.c_int),
         "cap_route_layout": ([P(Topology), vp, f32, vp, vp, vp, vp, P(Layout), vp, vp, sz, vp], ctypes.c_int),
+        "cap_balance_loss": ([i32, i32, i32, vp, vp, vp, vp, vp, i32, f32, f32, vp, vp, vp, vp, vp, sz, vp],
+                             ctypes.c_int),
+        "cap_router_grad": ([i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, f32, f32, vp, ctypes.c_int, vp,
+                             vp], ctypes.c_int),
+        "cap_orthogonalise": ([ctypes.c_int, i32, i32, i32, vp, i32, vp, f32, vp, vp, sz, vp], ctypes.c_int),
+        "cap_muon_update": ([ctypes.c_int, i32, i32, i32, vp, vp, f32, i32, i32, vp, f32, vp, vp, sz, vp],
+                            ctypes.c_int),
         "cap_adjustment_spectrum": ([vp, i32, i32, i32, f32, vp, vp, i32, vp, vp, vp, vp, sz, vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
@@ -264,3 +274,48 @@ def cap_adjustment_spectrum(coact, E, R, ranks_per_node, inter_node_cost, expert
         _ptr(coact), int(E), int(R), int(ranks_per_node), float(inter_node_cost), _ptr(expert_rank),
         _ptr(expert_local), int(max_swaps), _ptr(swaps), _ptr(deltas), _ptr(n_swaps), _ptr(ws), nbytes,
         _stream(stream)))
+
+
+def cap_balance_loss(T, k, E, logits, idx, keep, token_mask, seq_offsets, n_seq, balance_coef, z_coef, counts, probs,
+                     tokens, loss, ws, ws_bytes=None, stream=None):
+    nbytes = ws_bytes if ws_bytes is not None else ws.numel() * ws.element_size()
+    _check("cap_balance_loss", _lib.cap_balance_loss(
+        T, k, E, _ptr(logits), _ptr(idx), _ptr(keep), _ptr(token_mask), _ptr(seq_offsets), n_seq, balance_coef, z_coef,
+        _ptr(counts), _ptr(probs), _ptr(tokens), _ptr(loss), _ptr(ws), nbytes, _stream(stream)))
+
+
+def cap_router_grad(T, k, E, logits, idx, keep, w, d_w, token_mask, seq_offsets, n_seq, counts, tokens, balance_coef,
+                    z_coef, d_loss, dtype, d_logits, stream=None):
+    _check("cap_router_grad", _lib.cap_router_grad(
+        T, k, E, _ptr(logits), _ptr(idx), _ptr(keep), _ptr(w), _ptr(d_w), _ptr(token_mask), _ptr(seq_offsets), n_seq,
+        _ptr(counts), _ptr(tokens), balance_coef, z_coef, _ptr(d_loss), dtype, _ptr(d_logits), _stream(stream)))
+
+
+def make_coefficients(coef):
+    """Host array of the (a, b, c) of each Newton-Schulz step, or None for the default."""
+    if coef is None or isinstance(coef, ctypes.Array):
+        return coef
+    flat = [float(v) for step in coef for v in step]
+    return (ctypes.c_float * len(flat))(*flat)
+
+
+def _coefficients(coef, steps):
+    c = make_coefficients(coef)
+    if c is not None and len(c) != 3 * steps:
+        raise ValueError(f"{steps} steps take {3 * steps} coefficients, got {len(c)}")
+    return c
+
+
+def cap_orthogonalise(dtype, batch, rows, cols, g, steps, coef, eps, out, ws, ws_bytes=None, stream=None):
+    nbytes = ws_bytes if ws_bytes is not None else ws.numel() * ws.element_size()
+    _check("cap_orthogonalise", _lib.cap_orthogonalise(
+        dtype, batch, rows, cols, _ptr(g), steps, _coefficients(coef, steps), eps, _ptr(out), _ptr(ws), nbytes,
+        _stream(stream)))
+
+
+def cap_muon_update(dtype, batch, rows, cols, g, momentum, mu, nesterov, steps, coef, eps, out, ws, ws_bytes=None,
+                    stream=None):
+    nbytes = ws_bytes if ws_bytes is not None else ws.numel() * ws.element_size()
+    _check("cap_muon_update", _lib.cap_muon_update(
+        dtype, batch, rows, cols, _ptr(g), _ptr(momentum), mu, int(bool(nesterov)), steps, _coefficients(coef, steps),
+        eps, _ptr(out), _ptr(ws), nbytes, _stream(stream)))

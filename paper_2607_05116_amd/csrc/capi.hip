@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <atomic>
+#include <cmath>
 
 #include "cap_device.hpp"
 
@@ -35,6 +36,16 @@ cap_status front_end_launch(const cap_topology*, const float*, float, int32_t*, 
                             const cap_layout*, uint32_t*, void*, hipStream_t);
 cap_status adjustment_launch(const uint32_t*, int, int, int, float, int32_t*, int32_t*, int, int32_t*, double*,
                              int32_t*, void*, hipStream_t);
+size_t balance_workspace_bytes(int, int, int);
+cap_status balance_loss_launch(int, int, int, const float*, const int32_t*, const uint8_t*, const uint8_t*,
+                               const int32_t*, int, float, float, int32_t*, float*, int32_t*, float*, void*,
+                               hipStream_t);
+cap_status router_grad_launch(int, int, int, const float*, const int32_t*, const uint8_t*, const float*, const float*,
+                              const uint8_t*, const int32_t*, int, const int32_t*, const int32_t*, float, float,
+                              const float*, cap_dtype, void*, hipStream_t);
+size_t orthogonalise_workspace_bytes(int, int, int);
+cap_status orthogonalise_launch(cap_dtype, int, int, int, const void*, float*, float, int, int, const float*, float,
+                                void*, void*, hipStream_t);
 cap_status coactivation_launch(int, int, int, const int32_t*, const uint8_t*, uint32_t*, int, void*,
                                hipStream_t);
 
@@ -91,6 +102,13 @@ bool row_dtype_ok(cap_dtype dt, int d) {
     return false;
 }
 
+// Matrices of the orthogonalisation: sides that the products' 32-bit row offsets
+// and the launch's grid hold.
+bool orth_shape_ok(int batch, int rows, int cols) {
+    return batch >= 1 && batch <= kMaxOrthBatch && rows >= 1 && rows <= kMaxOrthSide && cols >= 1 &&
+           cols <= kMaxOrthSide;
+}
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
@@ -128,6 +146,11 @@ size_t cap_workspace_size(cap_op op, const cap_topology* topo, int32_t d, int32_
             return coact_workspace_bytes(topo->T, topo->E);
         case CAP_OP_ROUTE_LAYOUT:
             return topo_ok(topo) ? front_end_workspace_bytes(topo) : 0;
+        case CAP_OP_BALANCE_LOSS:
+            if (!topo || topo->T < 0 || topo->E < 1 || topo->E > kMaxE || max_rows < 1) return 0;
+            return balance_workspace_bytes(topo->T, topo->E, max_rows);
+        case CAP_OP_ORTHOGONALISE:
+            return orth_shape_ok(max_rows, inter, d) ? orthogonalise_workspace_bytes(max_rows, inter, d) : 0;
         case CAP_OP_ADJUSTMENT:
             if (!topo || topo->E < 1 || topo->E > kMaxE) return 0;
             return adjustment_workspace_bytes(topo->E);
@@ -343,6 +366,97 @@ cap_status cap_adjustment_spectrum(const uint32_t* coact, int32_t E, int32_t R, 
         return CAP_ERR_WORKSPACE;
     return adjustment_launch(coact, E, R, ranks_per_node, inter_node_cost, expert_rank, expert_local, max_swaps,
                              swaps, deltas, n_swaps, ws, as_stream(stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+bool loss_shape_ok(int32_t T, int32_t k, int32_t E, int32_t n_seq) {
+    return T >= 0 && k >= 1 && k <= kMaxK && E >= 1 && E <= kMaxE && k <= E &&
+           static_cast<long long>(T) * k < (1ll << 31) && n_seq >= 1 &&
+           static_cast<long long>(n_seq) * E < (1ll << 31);
+}
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+
+cap_status orth_check(cap_dtype dtype, int32_t batch, int32_t rows, int32_t cols, const void* g, int32_t steps,
+                      const float* coef, float eps, const void* out, const void* ws, size_t ws_bytes) {
+    if (batch < 0 || rows < 0 || cols < 0 || steps < 1 || steps > kMaxOrthSteps) return CAP_ERR_INVALID_ARG;
+    if (!(eps >= 0.0f) || !(eps < INFINITY)) return CAP_ERR_INVALID_ARG;
+    if (coef)
+        for (int i = 0; i < 3 * steps; ++i)
+            if (!(coef[i] > -INFINITY && coef[i] < INFINITY)) return CAP_ERR_INVALID_ARG;
+    if (dtype != CAP_DTYPE_BF16 && dtype != CAP_DTYPE_F32) return CAP_ERR_UNSUPPORTED;
+    if (batch == 0 || rows == 0 || cols == 0) return CAP_OK;
+    if (!g || !out) return CAP_ERR_INVALID_ARG;
+    if (!orth_shape_ok(batch, rows, cols)) return CAP_ERR_UNSUPPORTED;
+    if ((reinterpret_cast<uintptr_t>(g) & (dtype == CAP_DTYPE_BF16 ? 1 : 3)) != 0 ||
+        (reinterpret_cast<uintptr_t>(out) & 1) != 0)
+        return CAP_ERR_INVALID_ARG;
+    if (!ws || ws_bytes < orthogonalise_workspace_bytes(batch, rows, cols) ||
+        (reinterpret_cast<uintptr_t>(ws) & 255) != 0)
+        return CAP_ERR_WORKSPACE;
+    return CAP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cap_status cap_balance_loss(int32_t T, int32_t k, int32_t E, const float* logits, const int32_t* idx,
+                            const uint8_t* keep, const uint8_t* token_mask, const int32_t* seq_offsets, int32_t n_seq,
+                            float balance_coef, float z_coef, int32_t* counts, float* probs, int32_t* tokens,
+                            float* loss, void* ws, size_t ws_bytes, void* stream) {
+    if (!loss_shape_ok(T, k, E, n_seq) || (!seq_offsets && n_seq != 1)) return CAP_ERR_INVALID_ARG;
+    if ((T > 0 && (!logits || !idx)) || !counts || !probs || !tokens || !loss) return CAP_ERR_INVALID_ARG;
+    if (!(fabsf(balance_coef) < INFINITY) || !(fabsf(z_coef) < INFINITY)) return CAP_ERR_INVALID_ARG;
+    if (!aligned4(logits) || !aligned4(idx) || !aligned4(seq_offsets) || !aligned4(counts) || !aligned4(probs) ||
+        !aligned4(tokens) || !aligned4(loss))
+        return CAP_ERR_INVALID_ARG;
+    if (!ws || ws_bytes < balance_workspace_bytes(T, E, n_seq) || (reinterpret_cast<uintptr_t>(ws) & 255) != 0)
+        return CAP_ERR_WORKSPACE;
+    return balance_loss_launch(T, k, E, logits, idx, keep, token_mask, seq_offsets, n_seq, balance_coef, z_coef, counts,
+                               probs, tokens, loss, ws, as_stream(stream));
+}
+
+cap_status cap_router_grad(int32_t T, int32_t k, int32_t E, const float* logits, const int32_t* idx,
+                           const uint8_t* keep, const float* w, const float* d_w, const uint8_t* token_mask,
+                           const int32_t* seq_offsets, int32_t n_seq, const int32_t* counts, const int32_t* tokens,
+                           float balance_coef, float z_coef, const float* d_loss, cap_dtype dtype, void* d_logits,
+                           void* stream) {
+    if (!loss_shape_ok(T, k, E, n_seq) || (!seq_offsets && n_seq != 1)) return CAP_ERR_INVALID_ARG;
+    if (dtype != CAP_DTYPE_BF16 && dtype != CAP_DTYPE_F32) return CAP_ERR_UNSUPPORTED;
+    if (!counts || !tokens) return CAP_ERR_INVALID_ARG;
+    if (T > 0 && (!logits || !d_logits || (d_w && (!idx || !w)))) return CAP_ERR_INVALID_ARG;
+    if (!(fabsf(balance_coef) < INFINITY) || !(fabsf(z_coef) < INFINITY)) return CAP_ERR_INVALID_ARG;
+    if (!aligned4(logits) || !aligned4(idx) || !aligned4(w) || !aligned4(d_w) || !aligned4(seq_offsets) ||
+        !aligned4(counts) || !aligned4(tokens) || !aligned4(d_loss))
+        return CAP_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(d_logits) & (dtype == CAP_DTYPE_BF16 ? 1 : 3)) != 0) return CAP_ERR_INVALID_ARG;
+    if (T == 0) return CAP_OK;
+    return router_grad_launch(T, k, E, logits, idx, keep, w, d_w, token_mask, seq_offsets, n_seq, counts, tokens,
+                              balance_coef, z_coef, d_loss, dtype, d_logits, as_stream(stream));
+}
+
+cap_status cap_orthogonalise(cap_dtype dtype, int32_t batch, int32_t rows, int32_t cols, const void* g, int32_t steps,
+                             const float* coef, float eps, void* out, void* ws, size_t ws_bytes, void* stream) {
+    const cap_status st = orth_check(dtype, batch, rows, cols, g, steps, coef, eps, out, ws, ws_bytes);
+    if (st != CAP_OK || batch == 0 || rows == 0 || cols == 0) return st;
+    return orthogonalise_launch(dtype, batch, rows, cols, g, nullptr, 0.0f, 0, steps, coef, eps, out, ws,
+                                as_stream(stream));
+}
+
+cap_status cap_muon_update(cap_dtype dtype, int32_t batch, int32_t rows, int32_t cols, const void* g, float* momentum,
+                           float mu, int32_t nesterov, int32_t steps, const float* coef, float eps, void* out, void* ws,
+                           size_t ws_bytes, void* stream) {
+    const cap_status st = orth_check(dtype, batch, rows, cols, g, steps, coef, eps, out, ws, ws_bytes);
+    if (st != CAP_OK) return st;
+    if (!(mu >= 0.0f) || !(mu < 1.0f)) return CAP_ERR_INVALID_ARG;
+    if (batch == 0 || rows == 0 || cols == 0) return CAP_OK;
+    if (!momentum || !aligned4(momentum)) return CAP_ERR_INVALID_ARG;
+    return orthogonalise_launch(dtype, batch, rows, cols, g, momentum, mu, nesterov != 0, steps, coef, eps, out, ws,
+                                as_stream(stream));
 }
 
 }  // extern "C"
