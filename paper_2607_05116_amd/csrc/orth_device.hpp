@@ -1,0 +1,120 @@
+// What the two forms of the orthogonalisation share (gfx950): loading U, values
+// split over two fp16, and the transpose that mirrors a symmetric product.
+#pragma once
+
+#include "mfma_tile.hpp"
+
+namespace cap {
+namespace {
+
+// A value as fp16 plus its rounding error in a second fp16, scaled so that the
+// error of the smallest normal values is normal too: 22 bits together.
+constexpr float kLoScale = 2048.0f;
+
+__device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    const h2 v = {static_cast<_Float16>(a), static_cast<_Float16>(b)};
+    return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ float f16_to_f32(uint16_t b) { return static_cast<float>(__builtin_bit_cast(_Float16, b)); }
+// value e = 0..3 of four packed fp16
+__device__ __forceinline__ float f16_at(const u32x2& v, int e) {
+    return f16_to_f32(static_cast<uint16_t>(v[e >> 1] >> (16 * (e & 1))));
+}
+__device__ __forceinline__ void split4(const float (&v)[4], u32x2& hi, u32x2& lo) {
+    hi = u32x2{pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3])};
+    float d[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) d[e] = (v[e] - f16_at(hi, e)) * kLoScale;
+    lo = u32x2{pack_f16x2(d[0], d[1]), pack_f16x2(d[2], d[3])};
+}
+
+// 4 x 4 transpose of 16-bit values within each quad of lanes: lane r holds four
+// columns of row r; afterwards lane r holds four rows of column r % 4.
+__device__ __forceinline__ u32x2 quad_transpose(const u32x2& v, int lane) {
+    const uint32_t p0 = __builtin_amdgcn_update_dpp(0, v[0], 0xB1, 0xF, 0xF, false);       // lane ^ 1
+    const uint32_t p1 = __builtin_amdgcn_update_dpp(0, v[1], 0xB1, 0xF, 0xF, false);
+    const bool odd = lane & 1;
+    const uint32_t x0 = odd ? (p0 >> 16) | (v[0] & 0xFFFF0000u) : (v[0] & 0xFFFFu) | (p0 << 16);
+    const uint32_t x1 = odd ? (p1 >> 16) | (v[1] & 0xFFFF0000u) : (v[1] & 0xFFFFu) | (p1 << 16);
+    const bool up = lane & 2;
+    const uint32_t y = __builtin_amdgcn_update_dpp(0, up ? x0 : x1, 0x4E, 0xF, 0xF, false);   // lane ^ 2
+    return up ? u32x2{y, x1} : u32x2{x0, y};
+}
+
+// Block (i, j), j <= i, of the t-th block on or below the diagonal.
+__device__ __forceinline__ void triangle(int t, int& i, int& j) {
+    i = static_cast<int>((sqrtf(8.0f * static_cast<float>(t) + 1.0f) - 1.0f) * 0.5f);
+    while (i * (i + 1) / 2 > t) --i;
+    while ((i + 1) * (i + 2) / 2 <= t) ++i;
+    j = t - i * (i + 1) / 2;
+}
+
+// The matrix to orthogonalise: U = G, or G + mu M / M with M the new momentum
+// (which the first pass writes: M <- mu M + G).
+struct Source {
+    const void* g;
+    float* mom;
+    float mu;
+    int nesterov;
+    int bf16;
+};
+template <bool BF16>
+__device__ __forceinline__ float load_g(const void* g, size_t i) {
+    if constexpr (BF16) return bf16_to_f32(static_cast<const uint16_t*>(g)[i]);
+    else return static_cast<const float*>(g)[i];
+}
+template <bool BF16, bool MOM, bool FIRST>
+__device__ __forceinline__ float load_u(const Source& s, size_t i) {
+    const float g = load_g<BF16>(s.g, i);
+    if constexpr (!MOM) return g;
+    float m = s.mom[i];
+    if constexpr (FIRST) {
+        m = __builtin_fmaf(s.mu, m, g);
+        s.mom[i] = m;
+    }
+    return s.nesterov ? __builtin_fmaf(s.mu, m, g) : m;
+}
+// Four consecutive values, 16-byte (fp32) and 8-byte (bf16) aligned.
+template <bool BF16, bool MOM, bool FIRST>
+__device__ __forceinline__ f32x4 load_u4(const Source& s, size_t i) {
+    f32x4 g;
+    if constexpr (BF16) {
+        const u32x2 v = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(s.g) + i);
+        g = f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u), __uint_as_float(v[1] << 16),
+                  __uint_as_float(v[1] & 0xFFFF0000u)};
+    } else {
+        g = *reinterpret_cast<const f32x4*>(static_cast<const float*>(s.g) + i);
+    }
+    if constexpr (!MOM) return g;
+    f32x4 m = *reinterpret_cast<const f32x4*>(s.mom + i);
+    if constexpr (FIRST) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[e] = __builtin_fmaf(s.mu, m[e], g[e]);
+        *reinterpret_cast<f32x4*>(s.mom + i) = m;
+    }
+    if (s.nesterov) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[e] = __builtin_fmaf(s.mu, m[e], g[e]);
+    }
+    return m;
+}
+
+// Whether every run of four columns may be loaded as one vector.
+inline bool vector_rows(const Source& s, int cols) {
+    return cols % 4 == 0 && (reinterpret_cast<uintptr_t>(s.g) & (s.bf16 ? 7 : 15)) == 0 &&
+           (reinterpret_cast<uintptr_t>(s.mom) & 15) == 0;
+}
+
+}  // namespace
+
+struct StepCoef {
+    float v[kMaxOrthSteps][3];
+};
+
+size_t gram_form_bytes(int batch, int rows, int cols);
+cap_status gram_form_launch(int batch, int rows, int cols, const void* g, bool bf16, float* momentum, float mu,
+                            int nesterov, int steps, const StepCoef& coef, float eps, void* out, void* workspace,
+                            hipStream_t stream);
+
+}  // namespace cap

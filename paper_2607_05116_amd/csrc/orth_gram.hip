@@ -1,0 +1,498 @@
+// Orthogonalised gradients of few rows (or columns): the steps in the space of
+// the Gram matrix.
+//
+// Every step multiplies X by a polynomial of S = X X^T, and polynomials of one
+// symmetric matrix commute, so with S_0 = U U^T / |U|^2 (n x n, n the shorter side)
+//   P = a I + b S + c S S;   Q <- Q P  (Q_0 = I);   S <- P S P
+// for each step, and the result is Q X_0.  U is read twice whatever the number of
+// steps, and the trace of U U^T is the norm.  What the short form costs is
+// precision: S has the squares of the singular values, so its rounding reaches
+// directions of sqrt(2^-p) of the largest one.  S_0 is summed in fp32 and the n x n
+// products are taken on values of 22 bits (fp16 pairs, three MFMAs a product), which
+// leaves 1e-6 to 7e-4 of the result's norm over spectra that fall by e^-12; with plain
+// fp16 it would be 1e-3 to 2e-1.
+//
+//   1. gram_partial_kernel   lower blocks of U U^T over a run of the longer side, fp32
+//                            MFMAs straight from global memory; the momentum update
+//   2. gram_reduce_kernel    (128 rows, many runs) sums the runs
+//   3. gram_steps_kernel     one workgroup per matrix: the sum, the norm, all the steps
+//   4. gram_apply_kernel     Q X_0, rounded to bf16 once
+// Three or four launches, against two or more for every step of the general form.
+// Bound by the latency of the steps' chain of n x n products (four a step) for few
+// matrices, by U's way from HBM for many.
+#include "orth_device.hpp"
+
+namespace cap {
+namespace {
+
+constexpr int kGramWaves = 4;
+constexpr int kGramThreads = kGramWaves * kWave;
+constexpr int kStepThreads = 1024;
+constexpr int kMaxSplits = 64;
+
+constexpr int blocks_of(int NB) { return NB * (NB + 1) / 2; }
+
+// Sum over the runs' parts: block t of the lower triangle, lane l: rows 16 i + 4 (l /
+// 16) + 0..3, column 16 j + l % 16.
+template <int NB, bool BF16, bool MOM>
+__global__ __launch_bounds__(kGramThreads) void gram_partial_kernel(Source src, int n, int m, int tall, int vec,
+                                                                    int run, f32x4* __restrict__ part) {
+    constexpr int NT = blocks_of(NB);
+    __shared__ f32x4 sums[NT][kWave];
+    const int lane = threadIdx.x % kWave;
+    const int wave = static_cast<int>(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
+    const int r = lane & 15, kq = lane >> 4;
+    const size_t base = static_cast<size_t>(blockIdx.y) * n * m;
+    const int k_end = min(m, static_cast<int>(blockIdx.x + 1) * run);
+    f32x4 acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k0 = blockIdx.x * run + wave * 16; k0 < k_end; k0 += kGramWaves * 16) {
+        const int k = k0 + 4 * kq;                           // this lane's four positions along the longer side
+        f32x4 u[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int row = 16 * i + r;
+            u[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (row >= n) continue;
+            if (!tall && vec) {
+                if (k < k_end) u[i] = load_u4<BF16, MOM, true>(src, base + static_cast<size_t>(row) * m + k);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (k + e < k_end)
+                        u[i][e] = load_u<BF16, MOM, true>(
+                            src, base + (tall ? static_cast<size_t>(k + e) * n + row : static_cast<size_t>(row) * m + k + e));
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+                for (int j = 0; j <= i; ++j)
+                    acc[i * (i + 1) / 2 + j] =
+                        __builtin_amdgcn_mfma_f32_16x16x4f32(u[i][e], u[j][e], acc[i * (i + 1) / 2 + j], 0, 0, 0);
+    }
+    // the waves add their sums in turn
+    for (int w = 0; w < kGramWaves; ++w) {
+        if (wave == w) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) sums[t][lane] = w ? sums[t][lane] + acc[t] : acc[t];
+        }
+        __syncthreads();
+    }
+    f32x4* out = part + (static_cast<size_t>(blockIdx.y) * gridDim.x + blockIdx.x) * NT * kWave;
+    for (int i = threadIdx.x; i < NT * kWave; i += kGramThreads) out[i] = sums[i / kWave][i % kWave];
+}
+
+__global__ __launch_bounds__(kGramThreads) void gram_reduce_kernel(int items, int splits, const f32x4* __restrict__ part,
+                                                                   f32x4* __restrict__ sum) {
+    const int i = blockIdx.x * kGramThreads + threadIdx.x;
+    if (i >= items) return;
+    const f32x4* p = part + static_cast<size_t>(blockIdx.y) * splits * items + i;
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+    for (int k = 0; k < splits; ++k) s += p[static_cast<size_t>(k) * items];
+    sum[static_cast<size_t>(blockIdx.y) * items + i] = s;
+}
+
+// An n x n matrix of value pairs, rows of NP fp16 padded by 16 bytes (fragment reads,
+// 16 rows at one chunk, then hit distinct banks).
+template <int NP>
+struct Pair {
+    static constexpr int kPitch = NP * 2 + 16;
+    uint8_t hi[NP * kPitch];
+    uint8_t lo[NP * kPitch];
+};
+
+template <int NP>
+__device__ __forceinline__ f16x8 pair_frag(const uint8_t* p, int row, int chunk) {
+    return *reinterpret_cast<const f16x8*>(p + row * Pair<NP>::kPitch + chunk * 16);
+}
+
+// Q between the steps: in LDS with S and P up to 64 rows; at 128 rows those two take
+// 139 of the 160 KB, and Q, read once a step, stays in the workspace.
+template <int NP, int NB>
+__global__ __launch_bounds__(kStepThreads) void gram_steps_kernel(int n, int splits, int steps, StepCoef coef, float eps,
+                                                                  const f32x4* __restrict__ part,
+                                                                  uint16_t* __restrict__ q_hi, uint16_t* __restrict__ q_lo,
+                                                                  float* __restrict__ scale_out) {
+    constexpr int NT = blocks_of(NB);
+    constexpr int WB = NP == 128 ? 2 : 1;                    // 16 x 16 blocks of a wave, each way
+    constexpr int SB = NP / (16 * WB);                       // waves' super-blocks a side
+    constexpr int KS = NP / 32;
+    constexpr bool kQLds = NP <= 64;
+    static_assert(blocks_of(SB) <= kStepThreads / kWave, "a wave for each lower super-block");
+    __shared__ __attribute__((aligned(16))) Pair<NP> S, P;
+    __shared__ __attribute__((aligned(16))) Pair<kQLds ? NP : 32> Ql;
+    __shared__ float red[kStepThreads / kWave];
+    const int lane = threadIdx.x % kWave;
+    const int wave = static_cast<int>(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
+    const int r = lane & 15, g = lane >> 4;
+    uint16_t* const qh = q_hi + static_cast<size_t>(blockIdx.x) * NP * NP;
+    uint16_t* const ql = q_lo + static_cast<size_t>(blockIdx.x) * NP * NP;
+
+    // S_0 = U U^T / |U|^2, with |U|^2 its trace
+    constexpr int ITEMS = NT * kWave, PER = (ITEMS + kStepThreads - 1) / kStepThreads;
+    f32x4 s[PER];
+    float trace = 0.0f;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+        const int it = x * kStepThreads + threadIdx.x;
+        s[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (it < ITEMS) {
+            const f32x4* p = part + static_cast<size_t>(blockIdx.x) * splits * ITEMS + it;
+#pragma unroll 8
+            for (int k = 0; k < splits; ++k) s[x] += p[static_cast<size_t>(k) * ITEMS];
+            int bi, bj;
+            triangle(it / kWave, bi, bj);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (bi == bj && 4 * g + e == r) trace += s[x][e];
+        }
+    }
+    for (int i = threadIdx.x; i < static_cast<int>(sizeof(Pair<NP>)) / 16; i += kStepThreads) {
+        reinterpret_cast<u32x4*>(&S)[i] = u32x4{0, 0, 0, 0};
+        reinterpret_cast<u32x4*>(&P)[i] = u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) trace += __shfl_xor(trace, o);
+    if (lane == 0) red[wave] = trace;
+    __syncthreads();
+    trace = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kStepThreads / kWave; ++w) trace += red[w];
+    const float scale = 1.0f / (sqrtf(trace) + eps);
+    if (threadIdx.x == 0) scale_out[blockIdx.x] = scale;
+
+    // four values of one column (rows 4 g ..) of block (i, j), mirrored too
+    auto put = [&](Pair<NP>& M, int row, int col, const float (&v)[4]) __attribute__((always_inline)) {
+        u32x2 hi, lo;
+        split4(v, hi, lo);
+        *reinterpret_cast<u32x2*>(M.hi + row * Pair<NP>::kPitch + col * 2) = hi;
+        *reinterpret_cast<u32x2*>(M.lo + row * Pair<NP>::kPitch + col * 2) = lo;
+    };
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+        const int it = x * kStepThreads + threadIdx.x;
+        if (it >= ITEMS) continue;
+        int bi, bj;
+        triangle(it / kWave, bi, bj);
+        // D rows 4 g + e, column r: symmetric, so row 16 j + r holds columns 16 i + 4 g ..
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = s[x][e] * scale * scale;
+        put(S, 16 * bj + r, 16 * bi + 4 * g, v);
+        if (bi != bj) {
+            u32x2 hi, lo;
+            split4(v, hi, lo);
+            hi = quad_transpose(hi, lane);
+            lo = quad_transpose(lo, lane);
+            const int row = 16 * bi + 4 * g + (r & 3), col = 16 * bj + 4 * (r >> 2);
+            *reinterpret_cast<u32x2*>(S.hi + row * Pair<NP>::kPitch + col * 2) = hi;
+            *reinterpret_cast<u32x2*>(S.lo + row * Pair<NP>::kPitch + col * 2) = lo;
+        }
+    }
+    __syncthreads();
+
+    int si = 0, sj = 0;
+    const bool mine = wave < blocks_of(SB);
+    if (mine) triangle(wave, si, sj);
+    si = __builtin_amdgcn_readfirstlane(si);
+    sj = __builtin_amdgcn_readfirstlane(sj);
+
+    // lower super-block of A B: lane (r, g) holds columns 4 g .. of row r of each block
+    float v[WB][WB][4];
+    auto product = [&](auto&& frag_a, const Pair<NP>& B) __attribute__((always_inline)) {
+        f32x4 main[WB][WB], corr[WB][WB];
+#pragma unroll
+        for (int i = 0; i < WB; ++i)
+#pragma unroll
+            for (int j = 0; j < WB; ++j) main[i][j] = corr[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            f16x8 ah[WB], al[WB], bh[WB], bl[WB];
+#pragma unroll
+            for (int i = 0; i < WB; ++i) {
+                frag_a((si * WB + i) * 16 + r, ks * 4 + g, ah[i], al[i]);
+                bh[i] = pair_frag<NP>(B.hi, (sj * WB + i) * 16 + r, ks * 4 + g);
+                bl[i] = pair_frag<NP>(B.lo, (sj * WB + i) * 16 + r, ks * 4 + g);
+            }
+#pragma unroll
+            for (int i = 0; i < WB; ++i)
+#pragma unroll
+                for (int j = 0; j < WB; ++j) {
+                    main[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bh[j], ah[i], main[i][j], 0, 0, 0);
+                    corr[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bl[j], ah[i], corr[i][j], 0, 0, 0);
+                    corr[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bh[j], al[i], corr[i][j], 0, 0, 0);
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < WB; ++i)
+#pragma unroll
+            for (int j = 0; j < WB; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[i][j][e] = __builtin_fmaf(corr[i][j][e], 1.0f / kLoScale, main[i][j][e]);
+    };
+    auto from = [&](const Pair<NP>& M) {
+        return [&M](int row, int chunk, f16x8& hi, f16x8& lo) __attribute__((always_inline)) {
+            hi = pair_frag<NP>(M.hi, row, chunk);
+            lo = pair_frag<NP>(M.lo, row, chunk);
+        };
+    };
+    auto from_ws = [&](int row, int chunk, f16x8& hi, f16x8& lo) __attribute__((always_inline)) {
+        hi = *reinterpret_cast<const f16x8*>(qh + row * NP + chunk * 8);
+        lo = *reinterpret_cast<const f16x8*>(ql + row * NP + chunk * 8);
+    };
+    // store(row, col, hi, lo) of the wave's blocks and their mirror images
+    auto each = [&](auto&& store) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < WB; ++i)
+#pragma unroll
+            for (int j = 0; j < WB; ++j) {
+                const int bi = si * WB + i, bj = sj * WB + j;
+                u32x2 hi, lo;
+                split4(v[i][j], hi, lo);
+                store(16 * bi + r, 16 * bj + 4 * g, hi, lo);
+                if (si != sj) store(16 * bj + 4 * g + (r & 3), 16 * bi + 4 * (r >> 2), quad_transpose(hi, lane), quad_transpose(lo, lane));
+            }
+    };
+    auto to_lds = [](auto& M) {
+        return [&M](int row, int col, const u32x2& hi, const u32x2& lo) __attribute__((always_inline)) {
+            *reinterpret_cast<u32x2*>(M.hi + row * Pair<NP>::kPitch + col * 2) = hi;
+            *reinterpret_cast<u32x2*>(M.lo + row * Pair<NP>::kPitch + col * 2) = lo;
+        };
+    };
+    auto to_ws = [&](int row, int col, const u32x2& hi, const u32x2& lo) __attribute__((always_inline)) {
+        *reinterpret_cast<u32x2*>(qh + row * NP + col) = hi;
+        *reinterpret_cast<u32x2*>(ql + row * NP + col) = lo;
+    };
+
+    for (int it = 0; it < steps; ++it) {
+        const float a = coef.v[it][0], b = coef.v[it][1], c = coef.v[it][2];
+        const bool last = it + 1 == steps;
+        if (mine) {
+            product(from(S), S);
+#pragma unroll
+            for (int i = 0; i < WB; ++i)
+#pragma unroll
+                for (int j = 0; j < WB; ++j) {
+                    const int row = (si * WB + i) * 16 + r, col = (sj * WB + j) * 16 + 4 * g;
+                    const u32x2 hi = *reinterpret_cast<const u32x2*>(S.hi + row * Pair<NP>::kPitch + col * 2);
+                    const u32x2 lo = *reinterpret_cast<const u32x2*>(S.lo + row * Pair<NP>::kPitch + col * 2);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float sv = __builtin_fmaf(f16_at(lo, e), 1.0f / kLoScale, f16_at(hi, e));
+                        const float d = row == col + e && row < n ? a : 0.0f;
+                        v[i][j][e] = __builtin_fmaf(c, v[i][j][e], __builtin_fmaf(b, sv, d));
+                    }
+                }
+            each(to_lds(P));
+            if (it == 0) {
+                if constexpr (kQLds) each(to_lds(Ql));
+                if (!kQLds || last) each(to_ws);
+            }
+        }
+        __syncthreads();
+        if (it > 0) {                                        // Q <- Q P
+            if (mine) {
+                if constexpr (kQLds) product(from(Ql), P);
+                else product(from_ws, P);
+            }
+            __syncthreads();
+            if (mine) {
+                if constexpr (kQLds) each(to_lds(Ql));
+                if (!kQLds || last) each(to_ws);
+            }
+        }
+        if (last) break;
+        if (mine) product(from(P), S);                       // S <- P S P
+        __syncthreads();
+        if (mine) each(to_lds(S));
+        __syncthreads();
+        if (mine) product(from(S), P);
+        __syncthreads();
+        if (mine) each(to_lds(S));
+        __syncthreads();
+    }
+}
+
+// Q X_0: a wave takes 16 positions of the longer side at a time.
+template <int NP, bool BF16, bool MOM>
+__global__ __launch_bounds__(kGramThreads) void gram_apply_kernel(Source src, int n, int m, int tall, int vec, int run,
+                                                                  const uint16_t* __restrict__ q_hi,
+                                                                  const uint16_t* __restrict__ q_lo,
+                                                                  const float* __restrict__ scales,
+                                                                  uint16_t* __restrict__ out) {
+    constexpr int KS = NP / 32;
+    __shared__ __attribute__((aligned(16))) Pair<NP> Q;
+    const int lane = threadIdx.x % kWave;
+    const int wave = static_cast<int>(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
+    const int r = lane & 15, g = lane >> 4;
+    const uint16_t* qh = q_hi + static_cast<size_t>(blockIdx.y) * NP * NP;
+    const uint16_t* ql = q_lo + static_cast<size_t>(blockIdx.y) * NP * NP;
+    for (int i = threadIdx.x; i < NP * NP / 8; i += kGramThreads) {
+        const int row = i / (NP / 8), c = i % (NP / 8);
+        *reinterpret_cast<u32x4*>(Q.hi + row * Pair<NP>::kPitch + c * 16) = *reinterpret_cast<const u32x4*>(qh + i * 8);
+        *reinterpret_cast<u32x4*>(Q.lo + row * Pair<NP>::kPitch + c * 16) = *reinterpret_cast<const u32x4*>(ql + i * 8);
+    }
+    const float scale = scales[blockIdx.y];
+    const size_t base = static_cast<size_t>(blockIdx.y) * n * m;
+    const int end = min(m, static_cast<int>(blockIdx.x + 1) * run);
+    __syncthreads();
+    for (int c0 = blockIdx.x * run + wave * 16; c0 < end; c0 += kGramWaves * 16) {
+        f16x8 vh[KS], vl[KS];
+        const int c = c0 + r;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            float u[8];
+            const int k0 = ks * 32 + g * 8;
+            if (tall && vec) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    f32x4 q = {0.0f, 0.0f, 0.0f, 0.0f};
+                    if (c < end && k0 + 4 * h < n) q = load_u4<BF16, MOM, false>(src, base + static_cast<size_t>(c) * n + k0 + 4 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) u[4 * h + e] = q[e];
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    u[e] = 0.0f;
+                    if (c < end && k0 + e < n)
+                        u[e] = load_u<BF16, MOM, false>(
+                            src, base + (tall ? static_cast<size_t>(c) * n + k0 + e : static_cast<size_t>(k0 + e) * m + c));
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = u[e] * scale;
+                const _Float16 hi = static_cast<_Float16>(x);
+                vh[ks][e] = hi;
+                vl[ks][e] = static_cast<_Float16>((x - static_cast<float>(hi)) * kLoScale);
+            }
+        }
+#pragma unroll 2
+        for (int i = 0; i < NP / 16; ++i) {
+            if (i * 16 >= n) break;
+            f32x4 main = {0.0f, 0.0f, 0.0f, 0.0f}, corr = main;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const f16x8 h = pair_frag<NP>(Q.hi, i * 16 + r, ks * 4 + g), l = pair_frag<NP>(Q.lo, i * 16 + r, ks * 4 + g);
+                if (tall) {
+                    main = __builtin_amdgcn_mfma_f32_16x16x32_f16(h, vh[ks], main, 0, 0, 0);
+                    corr = __builtin_amdgcn_mfma_f32_16x16x32_f16(l, vh[ks], corr, 0, 0, 0);
+                    corr = __builtin_amdgcn_mfma_f32_16x16x32_f16(h, vl[ks], corr, 0, 0, 0);
+                } else {
+                    main = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh[ks], h, main, 0, 0, 0);
+                    corr = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh[ks], l, corr, 0, 0, 0);
+                    corr = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl[ks], h, corr, 0, 0, 0);
+                }
+            }
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(corr[e], 1.0f / kLoScale, main[e]);
+            const u32x2 o = {pack_bf16x2_rne(v[0], v[1]), pack_bf16x2_rne(v[2], v[3])};
+            // tall: row c, columns 16 i + 4 g ..; wide: row 16 i + r, columns c0 + 4 g ..
+            const int row = tall ? c : i * 16 + r, col = tall ? i * 16 + 4 * g : c0 + 4 * g;
+            const int rows_end = tall ? end : n, cols_end = tall ? n : end, pitch = tall ? n : m;
+            if (row >= rows_end) continue;
+            uint16_t* dst = out + base + static_cast<size_t>(row) * pitch + col;
+            if (col + 3 < cols_end && (reinterpret_cast<uintptr_t>(dst) & 7) == 0) {
+                *reinterpret_cast<u32x2*>(dst) = o;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col + e < cols_end) dst[e] = static_cast<uint16_t>(o[e >> 1] >> (16 * (e & 1)));
+            }
+        }
+    }
+}
+
+struct GramPlan {
+    int n, m, NB, NP, splits, run, items;
+    bool reduce;
+};
+
+GramPlan gram_plan(int batch, int rows, int cols) {
+    GramPlan p;
+    p.n = rows < cols ? rows : cols;
+    p.m = rows < cols ? cols : rows;
+    p.NB = p.n <= 16 ? 1 : p.n <= 32 ? 2 : p.n <= 64 ? 4 : 8;
+    p.NP = p.NB < 2 ? 32 : 16 * p.NB;
+    p.items = blocks_of(p.NB) * kWave;
+    // runs of at least 64 positions (one step of the four waves); about two
+    // workgroups a CU over the batch, and no more parts than one workgroup sums soon
+    int splits = (512 + batch - 1) / batch;
+    if (splits > kMaxSplits) splits = kMaxSplits;
+    const int most = (p.m + 63) / 64;
+    if (splits > most) splits = most;
+    p.run = ((p.m + splits - 1) / splits + 63) / 64 * 64;
+    p.splits = (p.m + p.run - 1) / p.run;
+    p.reduce = p.NB == 8 && p.splits > 8;
+    return p;
+}
+
+size_t align_up(size_t v) { return (v + 255) & ~size_t(255); }
+
+}  // namespace
+
+size_t gram_form_bytes(int batch, int rows, int cols) {
+    const GramPlan p = gram_plan(batch, rows, cols);
+    const size_t b = batch;
+    return align_up(b * p.splits * p.items * 16) + align_up(p.reduce ? b * p.items * 16 : 0) +
+           2 * align_up(b * p.NP * p.NP * 2) + align_up(b * 4);
+}
+
+cap_status gram_form_launch(int batch, int rows, int cols, const void* g, bool bf16, float* momentum, float mu,
+                            int nesterov, int steps, const StepCoef& coef, float eps, void* out, void* workspace,
+                            hipStream_t stream) {
+    const GramPlan p = gram_plan(batch, rows, cols);
+    const size_t b = batch;
+    char* at = static_cast<char*>(workspace);
+    f32x4* part = reinterpret_cast<f32x4*>(at);
+    at += align_up(b * p.splits * p.items * 16);
+    f32x4* sum = reinterpret_cast<f32x4*>(at);
+    at += align_up(p.reduce ? b * p.items * 16 : 0);
+    uint16_t* qh = reinterpret_cast<uint16_t*>(at);
+    at += align_up(b * p.NP * p.NP * 2);
+    uint16_t* ql = reinterpret_cast<uint16_t*>(at);
+    at += align_up(b * p.NP * p.NP * 2);
+    float* scale = reinterpret_cast<float*>(at);
+    const Source src{g, momentum, mu, nesterov, bf16 ? 1 : 0};
+    const int tall = rows > cols, vec = vector_rows(src, cols);
+    uint16_t* o = static_cast<uint16_t*>(out);
+    // the applying kernel: a workgroup loads Q once for its run
+    int arun = 64;
+    while (arun < p.m && static_cast<size_t>((p.m + arun - 1) / arun) * batch > 1024) arun += 64;
+    const dim3 agrid((p.m + arun - 1) / arun, batch);
+
+    auto go = [&](auto NBc, auto NPc, auto BF, auto MO) {
+        constexpr int NB = decltype(NBc)::value, NP = decltype(NPc)::value;
+        constexpr bool bf = decltype(BF)::value, mo = decltype(MO)::value;
+        gram_partial_kernel<NB, bf, mo><<<dim3(p.splits, batch), kGramThreads, 0, stream>>>(src, p.n, p.m, tall, vec, p.run, part);
+        if (p.reduce)
+            gram_reduce_kernel<<<dim3((p.items + kGramThreads - 1) / kGramThreads, batch), kGramThreads, 0, stream>>>(
+                p.items, p.splits, part, sum);
+        gram_steps_kernel<NP, NB><<<batch, kStepThreads, 0, stream>>>(p.n, p.reduce ? 1 : p.splits, steps, coef, eps,
+                                                                   p.reduce ? sum : part, qh, ql, scale);
+        gram_apply_kernel<NP, bf, mo><<<agrid, kGramThreads, 0, stream>>>(src, p.n, p.m, tall, vec, arun, qh, ql, scale, o);
+    };
+    auto by_type = [&](auto NBc, auto NPc) {
+        if (bf16 && momentum) go(NBc, NPc, std::true_type{}, std::true_type{});
+        else if (bf16) go(NBc, NPc, std::true_type{}, std::false_type{});
+        else if (momentum) go(NBc, NPc, std::false_type{}, std::true_type{});
+        else go(NBc, NPc, std::false_type{}, std::false_type{});
+    };
+    using std::integral_constant;
+    if (p.NB == 1) by_type(integral_constant<int, 1>{}, integral_constant<int, 32>{});
+    else if (p.NB == 2) by_type(integral_constant<int, 2>{}, integral_constant<int, 32>{});
+    else if (p.NB == 4) by_type(integral_constant<int, 4>{}, integral_constant<int, 64>{});
+    else by_type(integral_constant<int, 8>{}, integral_constant<int, 128>{});
+    CAP_LAUNCH_CHECK();
+    return CAP_OK;
+}
+
+}  // namespace cap

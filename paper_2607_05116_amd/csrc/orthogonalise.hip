@@ -20,7 +20,7 @@
 // X itself is carried to 22 bits (a second fp16 with the rounding error, scaled by
 // 2^11), because a X passes its rounding on undamped: rounding X to fp16 at each
 // step doubles the error on square or decaying spectra.
-#include "mfma_tile.hpp"
+#include "orth_device.hpp"
 
 namespace cap {
 namespace {
@@ -31,9 +31,9 @@ constexpr int kThreads = 256;              // four waves of 64 x 64
 constexpr int kTileStageB = 2 * kT * kRowB;
 constexpr int kNormThreads = 256;
 constexpr int kMaxNormParts = 256;
-constexpr float kLoScale = 2048.0f;
-
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+// Up to this many rows (or columns) the Gram form (orth_gram.hip) is taken.
+constexpr int kGramRows = 128;
+constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
 
 struct OrthWs {
     uint16_t *xh, *xl, *xt[2], *s, *p;
@@ -82,24 +82,10 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
     return at;
 }
 
-__device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
-    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-    const h2 v = {static_cast<_Float16>(a), static_cast<_Float16>(b)};
-    return __builtin_bit_cast(uint32_t, v);
-}
-__device__ __forceinline__ float f16_to_f32(uint16_t b) { return static_cast<float>(__builtin_bit_cast(_Float16, b)); }
-
 // ------------------------------------------------------------------ norm and momentum
-template <bool BF16>
-__device__ __forceinline__ float load_g(const void* g, size_t i) {
-    if constexpr (BF16) return bf16_to_f32(static_cast<const uint16_t*>(g)[i]);
-    else return static_cast<const float*>(g)[i];
-}
-
 // Sum of squares of U over this block's part of its matrix; writes the momentum.
 template <bool BF16, bool MOM>
-__global__ __launch_bounds__(kNormThreads) void norm_kernel(const void* __restrict__ g, float* __restrict__ mom,
-                                                            float mu, int nesterov, size_t size, int parts,
+__global__ __launch_bounds__(kNormThreads) void norm_kernel(Source src, size_t size, int parts,
                                                             float* __restrict__ norm) {
     __shared__ float red[kNormThreads / kWave];
     const size_t base = blockIdx.y * size;
@@ -107,12 +93,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(const void* __restri
     const size_t a = blockIdx.x * per, b = a + per < size ? a + per : size;
     float sum = 0.0f;
     for (size_t i = a + threadIdx.x; i < b; i += kNormThreads) {
-        float u = load_g<BF16>(g, base + i);
-        if constexpr (MOM) {
-            const float m = __builtin_fmaf(mu, mom[base + i], u);
-            mom[base + i] = m;
-            u = nesterov ? __builtin_fmaf(mu, m, u) : m;
-        }
+        const float u = load_u<BF16, MOM, true>(src, base + i);
         sum = __builtin_fmaf(u, u, sum);
     }
 #pragma unroll
@@ -128,8 +109,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(const void* __restri
 
 // X0 in both orientations, padded with zeros: 64 x 64 tiles of U through LDS.
 template <bool BF16, bool MOM>
-__global__ __launch_bounds__(256) void start_kernel(const void* __restrict__ g, const float* __restrict__ mom, float mu,
-                                                    int nesterov, int rows, int cols, float eps, OrthWs w) {
+__global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int cols, float eps, OrthWs w) {
     __shared__ float tile[64][65];
     __shared__ float scale_s;
     const bool tall = rows > cols;
@@ -150,11 +130,7 @@ __global__ __launch_bounds__(256) void start_kernel(const void* __restrict__ g, 
         float u = 0.0f;
         if (r0 + r < rows && c0 + tx < cols) {
             const size_t i = base + static_cast<size_t>(r0 + r) * cols + c0 + tx;
-            u = load_g<BF16>(g, i);
-            if constexpr (MOM) {
-                const float m = mom[i];
-                u = nesterov ? __builtin_fmaf(mu, m, u) : m;
-            }
+            u = load_u<BF16, MOM, false>(src, i);
         }
         tile[r][tx] = u * scale;
     }
@@ -188,28 +164,6 @@ struct ProductArgs {
     uint16_t* out;
     int rows, cols;
 };
-
-// 4 x 4 transpose of 16-bit values within each quad of lanes: lane r holds four
-// columns of row r (packed in lo, hi); afterwards four rows of column r % 4.
-__device__ __forceinline__ void quad_transpose(uint32_t& lo, uint32_t& hi, int lane) {
-    const uint32_t plo = __builtin_amdgcn_update_dpp(0, lo, 0xB1, 0xF, 0xF, false);       // lane ^ 1
-    const uint32_t phi = __builtin_amdgcn_update_dpp(0, hi, 0xB1, 0xF, 0xF, false);
-    const bool odd = lane & 1;
-    const uint32_t x0 = odd ? (plo >> 16) | (lo & 0xFFFF0000u) : (lo & 0xFFFFu) | (plo << 16);
-    const uint32_t x1 = odd ? (phi >> 16) | (hi & 0xFFFF0000u) : (hi & 0xFFFFu) | (phi << 16);
-    const bool up = lane & 2;
-    const uint32_t y = __builtin_amdgcn_update_dpp(0, up ? x0 : x1, 0x4E, 0xF, 0xF, false);   // lane ^ 2
-    lo = up ? y : x0;
-    hi = up ? x1 : y;
-}
-
-// Row and column tile of the t-th tile on or below the diagonal.
-__device__ __forceinline__ void triangle(int t, int& i, int& j) {
-    i = static_cast<int>((sqrtf(8.0f * static_cast<float>(t) + 1.0f) - 1.0f) * 0.5f);
-    while (i * (i + 1) / 2 > t) --i;
-    while ((i + 1) * (i + 2) / 2 <= t) ++i;
-    j = t - i * (i + 1) / 2;
-}
 
 template <Product MODE>
 __global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs q) {
@@ -294,52 +248,45 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs q) {
                     const u32x2 s = *reinterpret_cast<const u32x2*>(w.s + sb + static_cast<size_t>(row) * w.np + col);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        v[e] = __builtin_fmaf(q.c, v[e], q.b * f16_to_f32(static_cast<uint16_t>(s[e >> 1] >> (16 * (e & 1)))));
+                        v[e] = __builtin_fmaf(q.c, v[e], q.b * f16_at(s, e));
                 }
                 uint16_t* out = MODE == kGram ? w.s : w.p;
-                uint32_t lo = pack_f16x2(v[0], v[1]), hi = pack_f16x2(v[2], v[3]);
-                *reinterpret_cast<u32x2*>(out + sb + static_cast<size_t>(row) * w.np + col) = u32x2{lo, hi};
-                if (ti != tj) {
-                    quad_transpose(lo, hi, lane);
-                    *reinterpret_cast<u32x2*>(out + sb + static_cast<size_t>(tcol) * w.np + trow) = u32x2{lo, hi};
-                }
+                const u32x2 h = {pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3])};
+                *reinterpret_cast<u32x2*>(out + sb + static_cast<size_t>(row) * w.np + col) = h;
+                if (ti != tj)
+                    *reinterpret_cast<u32x2*>(out + sb + static_cast<size_t>(tcol) * w.np + trow) = quad_transpose(h, lane);
             } else {
                 const size_t at = xb + static_cast<size_t>(row) * w.mp + col;
                 const u32x2 h = *reinterpret_cast<const u32x2*>(w.xh + at), l = *reinterpret_cast<const u32x2*>(w.xl + at);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float x = __builtin_fmaf(f16_to_f32(static_cast<uint16_t>(l[e >> 1] >> (16 * (e & 1)))),
-                                                   1.0f / kLoScale,
-                                                   f16_to_f32(static_cast<uint16_t>(h[e >> 1] >> (16 * (e & 1)))));
+                    const float x = __builtin_fmaf(f16_at(l, e), 1.0f / kLoScale, f16_at(h, e));
                     v[e] = __builtin_fmaf(q.a, x, v[e]);
                 }
                 if constexpr (MODE == kApply) {
-                    uint32_t lo = pack_f16x2(v[0], v[1]), hi = pack_f16x2(v[2], v[3]);
-                    *reinterpret_cast<u32x2*>(w.xh + at) = u32x2{lo, hi};
-                    float d[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        d[e] = (v[e] - f16_to_f32(static_cast<uint16_t>((e >> 1 ? hi : lo) >> (16 * (e & 1))))) * kLoScale;
-                    *reinterpret_cast<u32x2*>(w.xl + at) = u32x2{pack_f16x2(d[0], d[1]), pack_f16x2(d[2], d[3])};
-                    quad_transpose(lo, hi, lane);
-                    *reinterpret_cast<u32x2*>(w.xt[q.from ^ 1] + xb + static_cast<size_t>(tcol) * w.np + trow) = u32x2{lo, hi};
+                    u32x2 hi, lo;
+                    split4(v, hi, lo);
+                    *reinterpret_cast<u32x2*>(w.xh + at) = hi;
+                    *reinterpret_cast<u32x2*>(w.xl + at) = lo;
+                    *reinterpret_cast<u32x2*>(w.xt[q.from ^ 1] + xb + static_cast<size_t>(tcol) * w.np + trow) =
+                        quad_transpose(hi, lane);
                 } else {
-                    uint32_t lo = pack_bf16x2_rne(v[0], v[1]), hi = pack_bf16x2_rne(v[2], v[3]);
+                    u32x2 y = {pack_bf16x2_rne(v[0], v[1]), pack_bf16x2_rne(v[2], v[3])};
                     uint16_t* out = q.out + static_cast<size_t>(blockIdx.y) * q.rows * q.cols;
                     int orow = row, ocol = col;
                     if (q.rows > q.cols) {
-                        quad_transpose(lo, hi, lane);
+                        y = quad_transpose(y, lane);
                         orow = tcol;
                         ocol = trow;
                     }
                     if (orow < q.rows) {
                         uint16_t* o = out + static_cast<size_t>(orow) * q.cols + ocol;
                         if (ocol + 3 < q.cols && (reinterpret_cast<uintptr_t>(o) & 7) == 0) {
-                            *reinterpret_cast<u32x2*>(o) = u32x2{lo, hi};
+                            *reinterpret_cast<u32x2*>(o) = y;
                         } else {
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                if (ocol + e < q.cols) o[e] = static_cast<uint16_t>((e >> 1 ? hi : lo) >> (16 * (e & 1)));
+                                if (ocol + e < q.cols) o[e] = static_cast<uint16_t>(y[e >> 1] >> (16 * (e & 1)));
                         }
                     }
                 }
@@ -350,12 +297,20 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs q) {
 }  // namespace
 
 size_t orthogonalise_workspace_bytes(int batch, int rows, int cols) {
+    if ((rows < cols ? rows : cols) <= kGramRows) return gram_form_bytes(batch, rows, cols);
     return orth_layout(batch, rows, cols, nullptr, nullptr);
 }
 
 cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, const void* g, float* momentum, float mu,
                                 int nesterov, int steps, const float* coef, float eps, void* out, void* workspace,
                                 hipStream_t stream) {
+    StepCoef sc;
+    for (int i = 0; i < kMaxOrthSteps; ++i)
+        for (int j = 0; j < 3; ++j) sc.v[i][j] = coef && i < steps ? coef[3 * i + j] : kQuintic[j];
+    const bool bf16 = dtype == CAP_DTYPE_BF16;
+    if ((rows < cols ? rows : cols) <= kGramRows)
+        return gram_form_launch(batch, rows, cols, g, bf16, momentum, mu, nesterov, steps, sc, eps, out, workspace, stream);
+    const Source src{g, momentum, mu, nesterov, bf16 ? 1 : 0};
     ProductArgs q{};
     orth_layout(batch, rows, cols, workspace, &q.w);
     const OrthWs& w = q.w;
@@ -368,10 +323,9 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
     const dim3 sgrid((tall ? w.np : w.mp) / 64, (tall ? w.mp : w.np) / 64, batch);
     auto begin = [&](auto BF, auto MOM) {
         constexpr bool bf = decltype(BF)::value, mo = decltype(MOM)::value;
-        norm_kernel<bf, mo><<<ngrid, kNormThreads, 0, stream>>>(g, momentum, mu, nesterov, size, w.parts, w.norm);
-        start_kernel<bf, mo><<<sgrid, 256, 0, stream>>>(g, momentum, mu, nesterov, rows, cols, eps, w);
+        norm_kernel<bf, mo><<<ngrid, kNormThreads, 0, stream>>>(src, size, w.parts, w.norm);
+        start_kernel<bf, mo><<<sgrid, 256, 0, stream>>>(src, rows, cols, eps, w);
     };
-    const bool bf16 = dtype == CAP_DTYPE_BF16;
     if (bf16 && momentum) begin(std::true_type{}, std::true_type{});
     else if (bf16) begin(std::true_type{}, std::false_type{});
     else if (momentum) begin(std::false_type{}, std::true_type{});
@@ -381,9 +335,9 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
     const dim3 tri(tn * (tn + 1) / 2, batch), all(tn * tm, batch);
     for (int i = 0; i < steps; ++i) {
         q.from = i & 1;
-        q.a = coef ? coef[3 * i] : 3.4445f;
-        q.b = coef ? coef[3 * i + 1] : -4.7750f;
-        q.c = coef ? coef[3 * i + 2] : 2.0315f;
+        q.a = sc.v[i][0];
+        q.b = sc.v[i][1];
+        q.c = sc.v[i][2];
         product_kernel<kGram><<<tri, kThreads, 0, stream>>>(q);
         product_kernel<kPoly><<<tri, kThreads, 0, stream>>>(q);
         if (i + 1 < steps) product_kernel<kApply><<<all, kThreads, 0, stream>>>(q);
