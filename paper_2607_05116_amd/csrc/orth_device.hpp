@@ -29,6 +29,19 @@ __device__ __forceinline__ void split4(const float (&v)[4], u32x2& hi, u32x2& lo
     lo = u32x2{pack_f16x2(d[0], d[1]), pack_f16x2(d[2], d[3])};
 }
 
+// The same rounding toward zero (one instruction for two values): where both halves
+// are always used, the second takes up what the first leaves, and 21 bits remain.
+__device__ __forceinline__ uint32_t pack_f16x2_rtz(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
+}
+__device__ __forceinline__ void split4_rtz(const float (&v)[4], u32x2& hi, u32x2& lo) {
+    hi = u32x2{pack_f16x2_rtz(v[0], v[1]), pack_f16x2_rtz(v[2], v[3])};
+    float d[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) d[e] = __builtin_fmaf(f16_at(hi, e), -kLoScale, v[e] * kLoScale);
+    lo = u32x2{pack_f16x2_rtz(d[0], d[1]), pack_f16x2_rtz(d[2], d[3])};
+}
+
 // 4 x 4 transpose of 16-bit values within each quad of lanes: lane r holds four
 // columns of row r; afterwards lane r holds four rows of column r % 4.
 __device__ __forceinline__ u32x2 quad_transpose(const u32x2& v, int lane) {

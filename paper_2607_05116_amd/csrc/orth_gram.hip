@@ -27,7 +27,6 @@ namespace {
 
 constexpr int kGramWaves = 4;
 constexpr int kGramThreads = kGramWaves * kWave;
-constexpr int kStepThreads = 1024;
 constexpr int kMaxSplits = 64;
 
 constexpr int blocks_of(int NB) { return NB * (NB + 1) / 2; }
@@ -111,35 +110,43 @@ __device__ __forceinline__ f16x8 pair_frag(const uint8_t* p, int row, int chunk)
     return *reinterpret_cast<const f16x8*>(p + row * Pair<NP>::kPitch + chunk * 16);
 }
 
-// Q between the steps: in LDS with S and P up to 64 rows; at 128 rows those two take
-// 139 of the 160 KB, and Q, read once a step, stays in the workspace.
+// The steps of one matrix, in one workgroup: a wave for each lower block (pair of
+// blocks a side at 128 rows) of the products.  Q P and P S of a step are one phase.  Up
+// to 64 rows S, P S, P and two Q are in LDS and a phase ends in one barrier; at 128
+// rows S and P take 139 of the 160 KB: P S replaces S behind a second barrier, and Q,
+// read once a step, is in the workspace.
+template <int NP>
+constexpr int step_waves() { return blocks_of(NP == 128 ? 4 : NP / 16); }
+template <int NP>
+constexpr int step_threads() { return kWave * (step_waves<NP>() < 4 ? 4 : step_waves<NP>()); }
+
 template <int NP, int NB>
-__global__ __launch_bounds__(kStepThreads) void gram_steps_kernel(int n, int splits, int steps, StepCoef coef, float eps,
-                                                                  const f32x4* __restrict__ part,
-                                                                  uint16_t* __restrict__ q_hi, uint16_t* __restrict__ q_lo,
-                                                                  float* __restrict__ scale_out) {
+__global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, int splits, int steps, StepCoef coef, float eps,
+                                                                       const f32x4* __restrict__ part,
+                                                                       uint16_t* __restrict__ q_ws,
+                                                                       float* __restrict__ scale_out) {
     constexpr int NT = blocks_of(NB);
     constexpr int WB = NP == 128 ? 2 : 1;                    // 16 x 16 blocks of a wave, each way
-    constexpr int SB = NP / (16 * WB);                       // waves' super-blocks a side
     constexpr int KS = NP / 32;
-    constexpr bool kQLds = NP <= 64;
-    static_assert(blocks_of(SB) <= kStepThreads / kWave, "a wave for each lower super-block");
-    __shared__ __attribute__((aligned(16))) Pair<NP> S, P;
-    __shared__ __attribute__((aligned(16))) Pair<kQLds ? NP : 32> Ql;
-    __shared__ float red[kStepThreads / kWave];
+    constexpr bool kSmall = NP <= 64;
+    constexpr int THREADS = step_threads<NP>();
+    __shared__ __attribute__((aligned(16))) Pair<NP> M[kSmall ? 5 : 2];
+    __shared__ float red[THREADS / kWave];
+    Pair<NP>&S = M[0], &P = M[1];
+    Pair<NP>& T = M[kSmall ? 2 : 0];
     const int lane = threadIdx.x % kWave;
     const int wave = static_cast<int>(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
     const int r = lane & 15, g = lane >> 4;
-    uint16_t* const qh = q_hi + static_cast<size_t>(blockIdx.x) * NP * NP;
-    uint16_t* const ql = q_lo + static_cast<size_t>(blockIdx.x) * NP * NP;
+    // the workspace's Q: two of them in turn, high and low halves; the result is the first
+    uint16_t* const qw = q_ws + static_cast<size_t>(blockIdx.x) * (kSmall ? 2 : 4) * NP * NP;
 
     // S_0 = U U^T / |U|^2, with |U|^2 its trace
-    constexpr int ITEMS = NT * kWave, PER = (ITEMS + kStepThreads - 1) / kStepThreads;
+    constexpr int ITEMS = NT * kWave, PER = (ITEMS + THREADS - 1) / THREADS;
     f32x4 s[PER];
     float trace = 0.0f;
 #pragma unroll
     for (int x = 0; x < PER; ++x) {
-        const int it = x * kStepThreads + threadIdx.x;
+        const int it = x * THREADS + threadIdx.x;
         s[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         if (it < ITEMS) {
             const f32x4* p = part + static_cast<size_t>(blockIdx.x) * splits * ITEMS + it;
@@ -152,59 +159,63 @@ __global__ __launch_bounds__(kStepThreads) void gram_steps_kernel(int n, int spl
                 if (bi == bj && 4 * g + e == r) trace += s[x][e];
         }
     }
-    for (int i = threadIdx.x; i < static_cast<int>(sizeof(Pair<NP>)) / 16; i += kStepThreads) {
-        reinterpret_cast<u32x4*>(&S)[i] = u32x4{0, 0, 0, 0};
-        reinterpret_cast<u32x4*>(&P)[i] = u32x4{0, 0, 0, 0};
-    }
+    if constexpr (16 * NB < NP)
+        for (int i = threadIdx.x; i < static_cast<int>(sizeof(Pair<NP>)) / 16; i += THREADS)
+            reinterpret_cast<u32x4*>(&S)[i] = u32x4{0, 0, 0, 0};
 #pragma unroll
     for (int o = 32; o; o >>= 1) trace += __shfl_xor(trace, o);
     if (lane == 0) red[wave] = trace;
     __syncthreads();
     trace = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kStepThreads / kWave; ++w) trace += red[w];
+    for (int w = 0; w < THREADS / kWave; ++w) trace += red[w];
     const float scale = 1.0f / (sqrtf(trace) + eps);
     if (threadIdx.x == 0) scale_out[blockIdx.x] = scale;
 
-    // four values of one column (rows 4 g ..) of block (i, j), mirrored too
-    auto put = [&](Pair<NP>& M, int row, int col, const float (&v)[4]) __attribute__((always_inline)) {
+    auto to_lds = [](Pair<NP>& D) {
+        return [&D](int row, int col, const u32x2& hi, const u32x2& lo) __attribute__((always_inline)) {
+            *reinterpret_cast<u32x2*>(D.hi + row * Pair<NP>::kPitch + col * 2) = hi;
+            *reinterpret_cast<u32x2*>(D.lo + row * Pair<NP>::kPitch + col * 2) = lo;
+        };
+    };
+    auto to_ws = [&](int which) {
+        uint16_t* const q = qw + which * 2 * NP * NP;
+        return [q](int row, int col, const u32x2& hi, const u32x2& lo) __attribute__((always_inline)) {
+            *reinterpret_cast<u32x2*>(q + row * NP + col) = hi;
+            *reinterpret_cast<u32x2*>(q + NP * NP + row * NP + col) = lo;
+        };
+    };
+    // four values of row 16 bi + r, columns 16 bj + 4 g .., and their mirror image
+    auto put = [&](int bi, int bj, bool mirror, const float (&v)[4], auto&& store) __attribute__((always_inline)) {
         u32x2 hi, lo;
-        split4(v, hi, lo);
-        *reinterpret_cast<u32x2*>(M.hi + row * Pair<NP>::kPitch + col * 2) = hi;
-        *reinterpret_cast<u32x2*>(M.lo + row * Pair<NP>::kPitch + col * 2) = lo;
+        split4_rtz(v, hi, lo);
+        store(16 * bi + r, 16 * bj + 4 * g, hi, lo);
+        if (mirror)
+            store(16 * bj + 4 * g + (r & 3), 16 * bi + 4 * (r >> 2), quad_transpose(hi, lane), quad_transpose(lo, lane));
     };
 #pragma unroll
     for (int x = 0; x < PER; ++x) {
-        const int it = x * kStepThreads + threadIdx.x;
+        const int it = x * THREADS + threadIdx.x;
         if (it >= ITEMS) continue;
         int bi, bj;
         triangle(it / kWave, bi, bj);
-        // D rows 4 g + e, column r: symmetric, so row 16 j + r holds columns 16 i + 4 g ..
+        // rows 16 bi + 4 g .., column 16 bj + r: S is symmetric
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = s[x][e] * scale * scale;
-        put(S, 16 * bj + r, 16 * bi + 4 * g, v);
-        if (bi != bj) {
-            u32x2 hi, lo;
-            split4(v, hi, lo);
-            hi = quad_transpose(hi, lane);
-            lo = quad_transpose(lo, lane);
-            const int row = 16 * bi + 4 * g + (r & 3), col = 16 * bj + 4 * (r >> 2);
-            *reinterpret_cast<u32x2*>(S.hi + row * Pair<NP>::kPitch + col * 2) = hi;
-            *reinterpret_cast<u32x2*>(S.lo + row * Pair<NP>::kPitch + col * 2) = lo;
-        }
+        put(bj, bi, bi != bj, v, to_lds(S));
     }
     __syncthreads();
 
     int si = 0, sj = 0;
-    const bool mine = wave < blocks_of(SB);
+    const bool mine = wave < step_waves<NP>();
     if (mine) triangle(wave, si, sj);
     si = __builtin_amdgcn_readfirstlane(si);
     sj = __builtin_amdgcn_readfirstlane(sj);
 
     // lower super-block of A B: lane (r, g) holds columns 4 g .. of row r of each block
-    float v[WB][WB][4];
-    auto product = [&](auto&& frag_a, const Pair<NP>& B) __attribute__((always_inline)) {
+    typedef float Block[WB][WB][4];
+    auto product = [&](auto&& frag_a, const Pair<NP>& B, Block& v) __attribute__((always_inline)) {
         f32x4 main[WB][WB], corr[WB][WB];
 #pragma unroll
         for (int i = 0; i < WB; ++i)
@@ -236,45 +247,34 @@ __global__ __launch_bounds__(kStepThreads) void gram_steps_kernel(int n, int spl
                 for (int e = 0; e < 4; ++e)
                     v[i][j][e] = __builtin_fmaf(corr[i][j][e], 1.0f / kLoScale, main[i][j][e]);
     };
-    auto from = [&](const Pair<NP>& M) {
-        return [&M](int row, int chunk, f16x8& hi, f16x8& lo) __attribute__((always_inline)) {
-            hi = pair_frag<NP>(M.hi, row, chunk);
-            lo = pair_frag<NP>(M.lo, row, chunk);
+    auto from = [&](const Pair<NP>& D) {
+        return [&D](int row, int chunk, f16x8& hi, f16x8& lo) __attribute__((always_inline)) {
+            hi = pair_frag<NP>(D.hi, row, chunk);
+            lo = pair_frag<NP>(D.lo, row, chunk);
         };
     };
-    auto from_ws = [&](int row, int chunk, f16x8& hi, f16x8& lo) __attribute__((always_inline)) {
-        hi = *reinterpret_cast<const f16x8*>(qh + row * NP + chunk * 8);
-        lo = *reinterpret_cast<const f16x8*>(ql + row * NP + chunk * 8);
+    auto from_ws = [&](int which) {
+        const uint16_t* const q = qw + which * 2 * NP * NP;
+        return [q](int row, int chunk, f16x8& hi, f16x8& lo) __attribute__((always_inline)) {
+            hi = *reinterpret_cast<const f16x8*>(q + row * NP + chunk * 8);
+            lo = *reinterpret_cast<const f16x8*>(q + NP * NP + row * NP + chunk * 8);
+        };
     };
-    // store(row, col, hi, lo) of the wave's blocks and their mirror images
-    auto each = [&](auto&& store) __attribute__((always_inline)) {
+    auto each = [&](const Block& v, auto&& store) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < WB; ++i)
 #pragma unroll
-            for (int j = 0; j < WB; ++j) {
-                const int bi = si * WB + i, bj = sj * WB + j;
-                u32x2 hi, lo;
-                split4(v[i][j], hi, lo);
-                store(16 * bi + r, 16 * bj + 4 * g, hi, lo);
-                if (si != sj) store(16 * bj + 4 * g + (r & 3), 16 * bi + 4 * (r >> 2), quad_transpose(hi, lane), quad_transpose(lo, lane));
-            }
-    };
-    auto to_lds = [](auto& M) {
-        return [&M](int row, int col, const u32x2& hi, const u32x2& lo) __attribute__((always_inline)) {
-            *reinterpret_cast<u32x2*>(M.hi + row * Pair<NP>::kPitch + col * 2) = hi;
-            *reinterpret_cast<u32x2*>(M.lo + row * Pair<NP>::kPitch + col * 2) = lo;
-        };
-    };
-    auto to_ws = [&](int row, int col, const u32x2& hi, const u32x2& lo) __attribute__((always_inline)) {
-        *reinterpret_cast<u32x2*>(qh + row * NP + col) = hi;
-        *reinterpret_cast<u32x2*>(ql + row * NP + col) = lo;
+            for (int j = 0; j < WB; ++j) put(si * WB + i, sj * WB + j, si != sj, v[i][j], store);
     };
 
     for (int it = 0; it < steps; ++it) {
         const float a = coef.v[it][0], b = coef.v[it][1], c = coef.v[it][2];
         const bool last = it + 1 == steps;
+        // the workspace's Q of step it is written to place (steps - 1 - it) % 2: the last to the first
+        const int q_to = (steps - 1 - it) & 1;
         if (mine) {
-            product(from(S), S);
+            Block v;
+            product(from(S), S, v);
 #pragma unroll
             for (int i = 0; i < WB; ++i)
 #pragma unroll
@@ -289,32 +289,39 @@ __global__ __launch_bounds__(kStepThreads) void gram_steps_kernel(int n, int spl
                         v[i][j][e] = __builtin_fmaf(c, v[i][j][e], __builtin_fmaf(b, sv, d));
                     }
                 }
-            each(to_lds(P));
-            if (it == 0) {
-                if constexpr (kQLds) each(to_lds(Ql));
-                if (!kQLds || last) each(to_ws);
+            each(v, to_lds(P));
+            if (it == 0) {                                   // Q = P
+                if constexpr (kSmall) {
+                    if (last) each(v, to_ws(0));
+                    else each(v, to_lds(M[3]));
+                } else {
+                    each(v, to_ws(q_to));
+                }
             }
         }
         __syncthreads();
-        if (it > 0) {                                        // Q <- Q P
-            if (mine) {
-                if constexpr (kQLds) product(from(Ql), P);
-                else product(from_ws, P);
+        Block t;
+        if (mine) {
+            if (it > 0) {                                    // Q <- Q P
+                Block v;
+                if constexpr (kSmall) {
+                    product(from(M[3 + ((it - 1) & 1)]), P, v);
+                    if (last) each(v, to_ws(0));
+                    else each(v, to_lds(M[3 + (it & 1)]));
+                } else {
+                    product(from_ws(q_to ^ 1), P, v);
+                    each(v, to_ws(q_to));
+                }
             }
-            __syncthreads();
-            if (mine) {
-                if constexpr (kQLds) each(to_lds(Ql));
-                if (!kQLds || last) each(to_ws);
-            }
+            if (!last) product(from(P), S, t);               // S <- P S P
         }
         if (last) break;
-        if (mine) product(from(P), S);                       // S <- P S P
+        if constexpr (!kSmall) __syncthreads();
+        if (mine) each(t, to_lds(T));
         __syncthreads();
-        if (mine) each(to_lds(S));
-        __syncthreads();
-        if (mine) product(from(S), P);
-        __syncthreads();
-        if (mine) each(to_lds(S));
+        if (mine) product(from(T), P, t);
+        if constexpr (!kSmall) __syncthreads();
+        if (mine) each(t, to_lds(S));
         __syncthreads();
     }
 }
@@ -322,8 +329,7 @@ __global__ __launch_bounds__(kStepThreads) void gram_steps_kernel(int n, int spl
 // Q X_0: a wave takes 16 positions of the longer side at a time.
 template <int NP, bool BF16, bool MOM>
 __global__ __launch_bounds__(kGramThreads) void gram_apply_kernel(Source src, int n, int m, int tall, int vec, int run,
-                                                                  const uint16_t* __restrict__ q_hi,
-                                                                  const uint16_t* __restrict__ q_lo,
+                                                                  const uint16_t* __restrict__ q_ws, int q_stride,
                                                                   const float* __restrict__ scales,
                                                                   uint16_t* __restrict__ out) {
     constexpr int KS = NP / 32;
@@ -331,8 +337,8 @@ __global__ __launch_bounds__(kGramThreads) void gram_apply_kernel(Source src, in
     const int lane = threadIdx.x % kWave;
     const int wave = static_cast<int>(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
     const int r = lane & 15, g = lane >> 4;
-    const uint16_t* qh = q_hi + static_cast<size_t>(blockIdx.y) * NP * NP;
-    const uint16_t* ql = q_lo + static_cast<size_t>(blockIdx.y) * NP * NP;
+    const uint16_t* qh = q_ws + static_cast<size_t>(blockIdx.y) * q_stride;
+    const uint16_t* ql = qh + NP * NP;
     for (int i = threadIdx.x; i < NP * NP / 8; i += kGramThreads) {
         const int row = i / (NP / 8), c = i % (NP / 8);
         *reinterpret_cast<u32x4*>(Q.hi + row * Pair<NP>::kPitch + c * 16) = *reinterpret_cast<const u32x4*>(qh + i * 8);
@@ -412,7 +418,7 @@ __global__ __launch_bounds__(kGramThreads) void gram_apply_kernel(Source src, in
 }
 
 struct GramPlan {
-    int n, m, NB, NP, splits, run, items;
+    int n, m, NB, NP, splits, run, items, q_values;
     bool reduce;
 };
 
@@ -423,6 +429,7 @@ GramPlan gram_plan(int batch, int rows, int cols) {
     p.NB = p.n <= 16 ? 1 : p.n <= 32 ? 2 : p.n <= 64 ? 4 : 8;
     p.NP = p.NB < 2 ? 32 : 16 * p.NB;
     p.items = blocks_of(p.NB) * kWave;
+    p.q_values = (p.NP == 128 ? 4 : 2) * p.NP * p.NP;        // of a matrix: high and low halves, twice at 128 rows
     // runs of at least 64 positions (one step of the four waves); about two
     // workgroups a CU over the batch, and no more parts than one workgroup sums soon
     int splits = (512 + batch - 1) / batch;
@@ -443,7 +450,7 @@ size_t gram_form_bytes(int batch, int rows, int cols) {
     const GramPlan p = gram_plan(batch, rows, cols);
     const size_t b = batch;
     return align_up(b * p.splits * p.items * 16) + align_up(p.reduce ? b * p.items * 16 : 0) +
-           2 * align_up(b * p.NP * p.NP * 2) + align_up(b * 4);
+           align_up(b * p.q_values * 2) + align_up(b * 4);
 }
 
 cap_status gram_form_launch(int batch, int rows, int cols, const void* g, bool bf16, float* momentum, float mu,
@@ -456,10 +463,8 @@ cap_status gram_form_launch(int batch, int rows, int cols, const void* g, bool b
     at += align_up(b * p.splits * p.items * 16);
     f32x4* sum = reinterpret_cast<f32x4*>(at);
     at += align_up(p.reduce ? b * p.items * 16 : 0);
-    uint16_t* qh = reinterpret_cast<uint16_t*>(at);
-    at += align_up(b * p.NP * p.NP * 2);
-    uint16_t* ql = reinterpret_cast<uint16_t*>(at);
-    at += align_up(b * p.NP * p.NP * 2);
+    uint16_t* q = reinterpret_cast<uint16_t*>(at);
+    at += align_up(b * p.q_values * 2);
     float* scale = reinterpret_cast<float*>(at);
     const Source src{g, momentum, mu, nesterov, bf16 ? 1 : 0};
     const int tall = rows > cols, vec = vector_rows(src, cols);
@@ -476,9 +481,9 @@ cap_status gram_form_launch(int batch, int rows, int cols, const void* g, bool b
         if (p.reduce)
             gram_reduce_kernel<<<dim3((p.items + kGramThreads - 1) / kGramThreads, batch), kGramThreads, 0, stream>>>(
                 p.items, p.splits, part, sum);
-        gram_steps_kernel<NP, NB><<<batch, kStepThreads, 0, stream>>>(p.n, p.reduce ? 1 : p.splits, steps, coef, eps,
-                                                                   p.reduce ? sum : part, qh, ql, scale);
-        gram_apply_kernel<NP, bf, mo><<<agrid, kGramThreads, 0, stream>>>(src, p.n, p.m, tall, vec, arun, qh, ql, scale, o);
+        gram_steps_kernel<NP, NB><<<batch, step_threads<NP>(), 0, stream>>>(p.n, p.reduce ? 1 : p.splits, steps, coef, eps,
+                                                                           p.reduce ? sum : part, q, scale);
+        gram_apply_kernel<NP, bf, mo><<<agrid, kGramThreads, 0, stream>>>(src, p.n, p.m, tall, vec, arun, q, p.q_values, scale, o);
     };
     auto by_type = [&](auto NBc, auto NPc) {
         if (bf16 && momentum) go(NBc, NPc, std::true_type{}, std::true_type{});
