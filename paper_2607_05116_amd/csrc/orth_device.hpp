@@ -47,12 +47,12 @@ __device__ __forceinline__ void split4_rtz(const float (&v)[4], u32x2& hi, u32x2
 __device__ __forceinline__ u32x2 quad_transpose(const u32x2& v, int lane) {
     const uint32_t p0 = __builtin_amdgcn_update_dpp(0, v[0], 0xB1, 0xF, 0xF, false);       // lane ^ 1
     const uint32_t p1 = __builtin_amdgcn_update_dpp(0, v[1], 0xB1, 0xF, 0xF, false);
-    const bool odd = lane & 1;
-    const uint32_t x0 = odd ? (p0 >> 16) | (v[0] & 0xFFFF0000u) : (v[0] & 0xFFFFu) | (p0 << 16);
-    const uint32_t x1 = odd ? (p1 >> 16) | (v[1] & 0xFFFF0000u) : (v[1] & 0xFFFFu) | (p1 << 16);
-    const bool up = lane & 2;
-    const uint32_t y = __builtin_amdgcn_update_dpp(0, up ? x0 : x1, 0x4E, 0xF, 0xF, false);   // lane ^ 2
-    return up ? u32x2{y, x1} : u32x2{x0, y};
+    // even lanes: the low halves of their own and the partner's pair; odd: the high ones
+    const uint32_t pick = 0x05040100u ^ ((0u - (lane & 1)) & (0x05040100u ^ 0x03020706u));
+    const uint32_t x0 = __builtin_amdgcn_perm(p0, v[0], pick), x1 = __builtin_amdgcn_perm(p1, v[1], pick);
+    const uint32_t up = 0u - ((lane >> 1) & 1);
+    const uint32_t y = __builtin_amdgcn_update_dpp(0, x1 ^ (up & (x0 ^ x1)), 0x4E, 0xF, 0xF, false);   // lane ^ 2
+    return u32x2{x0 ^ (up & (x0 ^ y)), y ^ (up & (x1 ^ y))};
 }
 
 // Block (i, j), j <= i, of the t-th block on or below the diagonal.

@@ -4,31 +4,43 @@
 //
 //   U  = G                                   (cap_orthogonalise)
 //   M <- mu M + G,  U = G + mu M  or  M      (cap_muon_update)
-//   X0 = U / (|U|_F + eps);   S = X X^T;   X <- a X + (b S + c S S) X,  steps times
+//   X0 = U / (|U|_F + eps);   S = X X^T;   X <- (a I + b S + c S S) X,  steps times
 //
 // X is held with the shorter side n as its rows ([n][m], transposed on the way in
-// and out when the matrix has more rows than columns), so S is n x n and a step
-// costs 3 n^2 m + n^3 multiply-adds with both symmetric products (S and S S)
-// computed on and below the diagonal and mirrored.
+// and out when the matrix has more rows than columns), so S is n x n.
+//
+// Steps go in groups of one or two: the first two and the last two are pairs, the
+// others single.  A pair needs X once, since S of its second step is P S P with P =
+// a I + b S + c S S (polynomials of one symmetric matrix commute):
+//   S (n^2 m), then n x n products:  R = P - p I;   T = P S;   S' = T P;  R' = P' - p' I;
+//   Q = P P';   X <- Q X (2 n^2 m).
+// All n x n products are symmetric: tiles on and below the diagonal, mirrored.  Five
+// steps take 9 n^2 m + 11 n^3 multiply-adds, single steps 15 n^2 m + 5 n^3, and X is
+// read and written three times instead of five.
 //
 // Every product is an MFMA product of fp16 values with fp32 sums whose operands
-// are both contiguous along the contraction: S from rows of X; S S from rows of S
-// (it is symmetric); the last from rows of b S + c S S and rows of X^T, of which a
-// second copy is kept.  fp16, not bf16: |X|_2 <= 1.3 at every step, so the range
-// is known, and the steps amplify what rounding adds to small singular values;
-// its 11 bits leave 1 to 2e-3 of the result's norm where bf16 leaves 1 to 3e-2.
-// X itself is carried to 22 bits (a second fp16 with the rounding error, scaled by
-// 2^11), because a X passes its rounding on undamped: rounding X to fp16 at each
-// step doubles the error on square or decaying spectra.
+// are both contiguous along the contraction: S from rows of X, the n x n ones from
+// rows of symmetric matrices, the last from rows of Q and rows of X^T, of which a
+// second copy is kept.  What is rounded to fp16, and why that is enough:
+//   * fp16, not bf16: the singular values stay below 1.3, so the range is known, and
+//     steps amplify what rounding adds to small singular values (by a each).
+//   * S, P, T and Q are carried as a multiple of I and the rest (S = s I + D, with s
+//     their mean diagonal, in fp32), and only the rest is rounded: with m >> n, or once
+//     the singular values are near 1, it is several times smaller.
+//   * X is carried to 22 bits (a second fp16 with its rounding error, scaled by 2^11)
+//     where it is multiplied by the multiple of I, which passes its error on undamped.
+// Together 3e-4 to 1.3e-3 of the result's norm on square, wide, low-rank and 1/i spectra,
+// 2.5e-3 where they fall by e^-12; bf16 products leave 1e-2 to 1e-1.  A pair in the middle
+// or three steps in one group lose more (up to 3e-3 and 2e-2): the noise of S' grows by
+// a^2 with each step taken on it.
+//
+// Matrices of at most 128 rows or columns take the Gram form (orth_gram.hip).
 #include "orth_device.hpp"
 
 namespace cap {
 namespace {
 
 constexpr int kPad = 128;                  // n and m in the workspace are multiples of this
-constexpr int kT = 128;                    // tile of the products
-constexpr int kThreads = 256;              // four waves of 64 x 64
-constexpr int kTileStageB = 2 * kT * kRowB;
 constexpr int kNormThreads = 256;
 constexpr int kMaxNormParts = 256;
 // Up to this many rows (or columns) the Gram form (orth_gram.hip) is taken.
@@ -36,9 +48,12 @@ constexpr int kGramRows = 128;
 constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
 
 struct OrthWs {
-    uint16_t *xh, *xl, *xt[2], *s, *p;
-    float* norm;                           // [batch][parts] sums of squares
-    int n, m, np, mp, parts;
+    uint16_t *xh, *xl, *xt[2];             // X [n][m]: fp16 and its scaled error; X^T [m][n], in turn
+    uint16_t* sq[3];                       // n x n
+    float* norm;                           // [batch][parts] sums of squares of U
+    float* trace;                          // [batch][trace_cap] parts of the next trace
+    float* center;                         // [batch][2] s of the group's first and second step
+    int n, m, np, mp, parts, trace_cap;
 };
 
 int up_to(int v, int q) { return (v + q - 1) / q * q; }
@@ -60,24 +75,31 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
         return q;
     };
     const size_t x = 2 * batch * np * mp, q = 2 * batch * np * np;
-    char* v[6];
+    // tiles of 256 may read 128 rows past a matrix (never used): of the next one, or of
+    // what follows here; each kind of matrix is followed by one at least as large
+    char* v[7];
+    for (int i = 4; i < 7; ++i) v[i] = take(q);
     for (int i = 0; i < 4; ++i) v[i] = take(x);
-    for (int i = 4; i < 6; ++i) v[i] = take(q);
+    take(static_cast<size_t>(kPad) * mp * 2);
     const int parts = norm_parts(rows, cols);
     char* f = take(static_cast<size_t>(batch) * parts * 4);
+    const size_t cap = (np / 128) * (mp / 128);
+    char* t = take(static_cast<size_t>(batch) * cap * 4);
+    char* c = take(static_cast<size_t>(batch) * 8);
     if (w) {
         w->xh = reinterpret_cast<uint16_t*>(v[0]);
         w->xl = reinterpret_cast<uint16_t*>(v[1]);
-        w->xt[0] = reinterpret_cast<uint16_t*>(v[2]);
-        w->xt[1] = reinterpret_cast<uint16_t*>(v[3]);
-        w->s = reinterpret_cast<uint16_t*>(v[4]);
-        w->p = reinterpret_cast<uint16_t*>(v[5]);
+        for (int i = 0; i < 2; ++i) w->xt[i] = reinterpret_cast<uint16_t*>(v[2 + i]);
+        for (int i = 0; i < 3; ++i) w->sq[i] = reinterpret_cast<uint16_t*>(v[4 + i]);
         w->norm = reinterpret_cast<float*>(f);
+        w->trace = reinterpret_cast<float*>(t);
+        w->center = reinterpret_cast<float*>(c);
         w->n = n;
         w->m = m;
         w->np = static_cast<int>(np);
         w->mp = static_cast<int>(mp);
         w->parts = parts;
+        w->trace_cap = static_cast<int>(cap);
     }
     return at;
 }
@@ -119,7 +141,12 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
         for (int i = threadIdx.x; i < w.parts; i += kWave) t += w.norm[static_cast<size_t>(batch) * w.parts + i];
 #pragma unroll
         for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
-        if (threadIdx.x == 0) scale_s = 1.0f / (sqrtf(t) + eps);
+        if (threadIdx.x == 0) {
+            const float scale = 1.0f / (sqrtf(t) + eps);
+            scale_s = scale;
+            // the trace of S_0
+            if (blockIdx.x == 0 && blockIdx.y == 0) w.trace[static_cast<size_t>(batch) * w.trace_cap] = t * scale * scale;
+        }
     }
     __syncthreads();
     const float scale = scale_s;
@@ -153,50 +180,304 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
 }
 
 // ------------------------------------------------------------------ products
-// kGram: S = X X^T; kPoly: P = b S + c S S; kApply: X <- a X + P X (X, its error
-// and X^T); kFinal: the same to the bf16 result, in the orientation it is wanted.
-enum Product { kGram, kPoly, kApply, kFinal };
+// kGram:  D = X X^T - s I, s = its trace / n
+// kSym:   one of the group's n x n products (Sym)
+// kApply: X <- p X + Q X: X, its error, X^T and the parts of |X|^2
+// kFinal: the same to the bf16 result, in the orientation it is wanted
+enum Product { kGram, kSym, kApply, kFinal };
+
+// The n x n products of a group, with p = a + b s + c s^2 of the first step's
+// coefficients and s, p' of the second's:
+//   kSymFirst:  R  = (b + 2 c s) D + c D D               (P = p I + R)
+//   kSymMix:    T  = p D + s R + R D                     (P S = p s I + T), parts of tr(P S P)
+//   kSymNext:   D' = p T + p s R + T R + (p^2 s - s') I  (P S P = s' I + D')
+//   kSymSecond: R' = kSymFirst of the second step
+//   kSymJoin:   Q  = p R' + p' R + R R'                  (P P' = p p' I + Q)
+enum Sym { kSymFirst, kSymMix, kSymNext, kSymSecond, kSymJoin };
 
 struct ProductArgs {
     OrthWs w;
-    int from;                              // X^T buffer that holds X
-    float a, b, c;
+    const uint16_t *A, *B;                 // rows of the left operand; rows (of the transpose) of the right
+    uint16_t* D;                           // kSym, kGram: result; kApply: X^T
+    int sym, traces;                       // kSym: which; kGram, kSymNext: parts of the trace
+    float coef[2][3];                      // of the group's steps
+    int pair;
     uint16_t* out;
-    int rows, cols;
+    int rows, cols, batch;
 };
 
+struct Scalars {
+    float ab, a, b, i;                     // of A B, A, B and I
+    float s1;                              // kSymNext: s'
+    float p, ps;                           // kSymMix: the multiples of I in P and T
+};
+
+// Sum of `count` parts by the whole workgroup, in a fixed order.
+template <int THREADS>
+__device__ __forceinline__ float sum_parts(const float* parts, int count, float* red) {
+    float t = 0.0f;
+    for (int i = threadIdx.x; i < count; i += THREADS) t += parts[i];
+#pragma unroll
+    for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
+    __syncthreads();
+    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = t;
+    __syncthreads();
+    t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < THREADS / kWave; ++i) t += red[i];
+    return t;
+}
+
+__device__ __forceinline__ float poly(const float (&c)[3], float s) { return __builtin_fmaf(__builtin_fmaf(c[2], s, c[1]), s, c[0]); }
+
+// The scalars of a product of matrix `batch`; kGram and kSymNext find their s from the
+// parts and (tile 0 of the matrix) keep it for the products after them.
+template <Product MODE, int THREADS>
+__device__ __forceinline__ Scalars scalars(const ProductArgs& q, int batch, bool first_tile, float* red) {
+    Scalars c{};
+    float* center = q.w.center + 2 * static_cast<size_t>(batch);
+    const float* parts = q.w.trace + static_cast<size_t>(batch) * q.w.trace_cap;
+    c.ab = 1.0f;
+    if constexpr (MODE == kGram) {
+        const float s = sum_parts<THREADS>(parts, q.traces, red) / static_cast<float>(q.w.n);
+        if (first_tile && threadIdx.x == 0) center[0] = s;
+        c.i = -s;
+    } else {
+        const float s = center[0];
+        const float p = poly(q.coef[0], s);
+        if constexpr (MODE == kSym) {
+            if (q.sym == kSymFirst) {
+                c.ab = q.coef[0][2];
+                c.a = __builtin_fmaf(2.0f * q.coef[0][2], s, q.coef[0][1]);
+            } else if (q.sym == kSymMix) {
+                c.a = s;
+                c.b = p;
+                c.p = p;
+                c.ps = p * s;
+            } else if (q.sym == kSymNext) {
+                c.s1 = sum_parts<THREADS>(parts, q.traces, red) / static_cast<float>(q.w.n);
+                if (first_tile && threadIdx.x == 0) center[1] = c.s1;
+                c.a = p;
+                c.b = p * s;
+                c.i = p * p * s - c.s1;
+            } else if (q.sym == kSymSecond) {
+                c.ab = q.coef[1][2];
+                c.a = __builtin_fmaf(2.0f * q.coef[1][2], center[1], q.coef[1][1]);
+            } else {
+                c.a = poly(q.coef[1], center[1]);
+                c.b = p;
+            }
+        } else {
+            c.a = q.pair ? p * poly(q.coef[1], center[1]) : p;
+        }
+    }
+    return c;
+}
+
+// LDS row of an operand's tile that holds its row v (0 .. 31) of a pair of 16-row
+// blocks, the other way round: LDS row 16 i + r holds row 8 (r / 4) + 4 i + r % 4, so
+// that after a transpose within the quads a lane's values of both blocks are eight
+// consecutive rows.
+__device__ __forceinline__ int paired_row(int v) {
+    return (v & ~31) | ((v & 12) << 1) | ((v >> 2) & 4) | (v & 3);
+}
+
+// Results of a wave's 64 x 16 NJ block at (row0, col0) of the matrix.  Lane (r, g)
+// holds columns 4 g .. + 3 of each 16 x 16 block, of row paired_row.  Two adjacent
+// blocks trade halves (permlane16_swap), so that a lane reads and writes 8 consecutive
+// columns: columns 8 (g / 2) .. of block g % 2.
+template <Product MODE, int NJ>
+__device__ __forceinline__ float store_wave(const ProductArgs& q, const Scalars& c, f32x4 (&acc)[4][NJ], int batch, int row0,
+                                            int col0, bool mirror, int lane) {
+    const OrthWs& w = q.w;
+    const int r = lane & 15, g = lane >> 4;
+    constexpr bool kSquare = MODE == kGram || MODE == kSym;
+    const size_t pitch = kSquare ? w.np : w.mp;
+    const size_t xb = static_cast<size_t>(batch) * w.np * w.mp, sb = static_cast<size_t>(batch) * w.np * w.np;
+    const size_t base = kSquare ? sb : xb;
+    const bool use_a = MODE == kSym, use_b = MODE == kSym && c.b != 0.0f;
+    float sum = 0.0f;
+    // 8 consecutive columns of a row: the lane's halves of two blocks
+    auto load_pair = [&](const uint16_t* p, size_t at, u32x2& x, u32x2& y) __attribute__((always_inline)) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(p + at);
+        const auto s0 = __builtin_amdgcn_permlane16_swap(v[0], v[2], false, false);
+        const auto s1 = __builtin_amdgcn_permlane16_swap(v[1], v[3], false, false);
+        x = u32x2{s0[0], s1[0]};
+        y = u32x2{s0[1], s1[1]};
+    };
+    auto join_pair = [&](const u32x2& x, const u32x2& y) __attribute__((always_inline)) {
+        const auto s0 = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false);
+        const auto s1 = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
+        return u32x4{s0[0], s1[0], s0[1], s1[1]};
+    };
+#pragma unroll
+    for (int ip = 0; ip < 2; ++ip)
+#pragma unroll
+        for (int pr = 0; pr < NJ / 2; ++pr) {
+            u32x2 t[2][2];                                         // [row block][column block], transposed
+#pragma unroll
+            for (int ii = 0; ii < 2; ++ii) {
+                const int row = row0 + 32 * ip + 8 * (r >> 2) + 4 * ii + (r & 3);
+                const int c8 = col0 + 32 * pr + 16 * (g & 1) + 8 * (g >> 1);
+                const size_t at = base + static_cast<size_t>(row) * pitch + c8;
+                float v[2][4];
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[b][e] = acc[2 * ip + ii][2 * pr + b][e];
+                u32x2 hi[2], lo[2];
+                if constexpr (kSquare) {
+                    u32x2 ea[2], eb[2];
+                    if (use_a) load_pair(q.A, at, ea[0], ea[1]);
+                    if (use_b) load_pair(q.B, at, eb[0], eb[1]);
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int col = col0 + 32 * pr + 16 * b + 4 * g + e;
+                            const bool diag = row == col && row < w.n;
+                            float x = c.ab * v[b][e];
+                            if (use_a) x = __builtin_fmaf(c.a, f16_at(ea[b], e), x);
+                            if (use_b) x = __builtin_fmaf(c.b, f16_at(eb[b], e), x);
+                            if (diag) x += c.i;
+                            if constexpr (MODE == kSym)
+                                if (q.sym == kSymMix)                  // P and T whole
+                                    sum = __builtin_fmaf(diag ? x + c.ps : x, f16_at(ea[b], e) + (diag ? c.p : 0.0f), sum);
+                            v[b][e] = x;
+                        }
+                        hi[b] = u32x2{pack_f16x2(v[b][0], v[b][1]), pack_f16x2(v[b][2], v[b][3])};
+                    }
+                    *reinterpret_cast<u32x4*>(q.D + at) = join_pair(hi[0], hi[1]);
+                    if (mirror) {
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) t[ii][b] = quad_transpose(hi[b], lane);
+                    }
+                } else {
+                    u32x2 xh[2], xl[2];
+                    load_pair(w.xh, at, xh[0], xh[1]);
+                    load_pair(w.xl, at, xl[0], xl[1]);
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float x = __builtin_fmaf(f16_at(xl[b], e), 1.0f / kLoScale, f16_at(xh[b], e));
+                            v[b][e] = __builtin_fmaf(c.a, x, v[b][e]);
+                        }
+                        if constexpr (MODE == kApply) {
+                            split4(v[b], hi[b], lo[b]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) sum = __builtin_fmaf(v[b][e], v[b][e], sum);
+                            t[ii][b] = quad_transpose(hi[b], lane);
+                        } else {
+                            hi[b] = u32x2{pack_bf16x2_rne(v[b][0], v[b][1]), pack_bf16x2_rne(v[b][2], v[b][3])};
+                            if (q.rows > q.cols) t[ii][b] = quad_transpose(hi[b], lane);
+                        }
+                    }
+                    if constexpr (MODE == kApply) {
+                        *reinterpret_cast<u32x4*>(w.xh + at) = join_pair(hi[0], hi[1]);
+                        *reinterpret_cast<u32x4*>(w.xl + at) = join_pair(lo[0], lo[1]);
+                    } else if (q.rows <= q.cols) {
+                        const u32x4 y = join_pair(hi[0], hi[1]);
+                        if (row < q.rows) {
+                            uint16_t* o = q.out + (static_cast<size_t>(batch) * q.rows + row) * q.cols + c8;
+                            if (c8 + 7 < q.cols && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+                                *reinterpret_cast<u32x4*>(o) = y;
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    if (c8 + e < q.cols) o[e] = static_cast<uint16_t>(y[e >> 1] >> (16 * (e & 1)));
+                            }
+                        }
+                    }
+                }
+            }
+            // transposed: row col0 + .. + 4 g + r % 4, eight columns
+            const int tc = row0 + 32 * ip + 8 * (r >> 2);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int tr = col0 + 32 * pr + 16 * b + 4 * g + (r & 3);
+                const u32x4 y = {t[0][b][0], t[0][b][1], t[1][b][0], t[1][b][1]};
+                if constexpr (kSquare) {
+                    if (mirror) *reinterpret_cast<u32x4*>(q.D + sb + static_cast<size_t>(tr) * w.np + tc) = y;
+                } else if constexpr (MODE == kApply) {
+                    *reinterpret_cast<u32x4*>(q.D + xb + static_cast<size_t>(tr) * w.np + tc) = y;
+                } else if (q.rows > q.cols && tr < q.rows) {
+                    uint16_t* o = q.out + (static_cast<size_t>(batch) * q.rows + tr) * q.cols + tc;
+                    if (tc + 7 < q.cols && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+                        *reinterpret_cast<u32x4*>(o) = y;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (tc + e < q.cols) o[e] = static_cast<uint16_t>(y[e >> 1] >> (16 * (e & 1)));
+                    }
+                }
+            }
+        }
+    return sum;
+}
+
+// This tile's part of a trace (off the diagonal it stands for two tiles).
+template <int THREADS>
+__device__ __forceinline__ void store_part(const ProductArgs& q, int batch, int tile, float sum, float* red) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+    __syncthreads();
+    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float t = 0.0f;
+        for (int i = 0; i < THREADS / kWave; ++i) t += red[i];
+        q.w.trace[static_cast<size_t>(batch) * q.w.trace_cap + tile] = t;
+    }
+}
+
 template <Product MODE>
-__global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs q) {
+__device__ __forceinline__ void decode_tile(const ProductArgs& q, int t, int tile_rows, int& ti, int& tj) {
+    if constexpr (MODE == kGram || MODE == kSym) {
+        triangle(t, ti, tj);
+    } else {
+        const int tm = (q.w.np + tile_rows - 1) / tile_rows;
+        ti = t % tm;
+        tj = t / tm;
+    }
+}
+
+// ---- tiles of 128 x 128: four waves of 64 x 64, two workgroups a CU
+constexpr int kT = 128;
+constexpr int kThreads = 256;
+constexpr int kTileStageB = 2 * kT * kRowB;
+
+template <Product MODE>
+__global__ __launch_bounds__(kThreads, 2) void product128_kernel(ProductArgs q) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kTileStageB];
+    __shared__ float red[kThreads / kWave];
     const OrthWs& w = q.w;
     const int lane = threadIdx.x % kWave;
     const int wave = static_cast<int>(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
     const int wm = wave >> 1, wn = wave & 1;
-    const size_t xb = static_cast<size_t>(blockIdx.y) * w.np * w.mp, sb = static_cast<size_t>(blockIdx.y) * w.np * w.np;
+    const int batch = blockIdx.y;
     int ti, tj;
-    if constexpr (MODE == kGram || MODE == kPoly) {
-        triangle(blockIdx.x, ti, tj);
-    } else {
-        const int tm = w.np / kT;
-        ti = blockIdx.x % tm;
-        tj = blockIdx.x / tm;
-    }
+    decode_tile<MODE>(q, blockIdx.x, kT, ti, tj);
+    const size_t xb = static_cast<size_t>(batch) * w.np * w.mp, sb = static_cast<size_t>(batch) * w.np * w.np;
     const int K = MODE == kGram ? w.mp : w.np;
-    const uint16_t* A = MODE == kGram ? w.xh + xb : MODE == kPoly ? w.s + sb : w.p + sb;
-    const uint16_t* B = MODE == kGram ? w.xh + xb : MODE == kPoly ? w.s + sb : w.xt[q.from] + xb;
+    const uint16_t* A = q.A + (MODE == kGram ? xb : sb);
+    const uint16_t* B = q.B + (MODE == kSym ? sb : xb);
     const uint32_t pitch = static_cast<uint32_t>(K) * 2u;
     const LaneMap lm = lane_map(lane);
     const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
     // wave w brings rows 32 w .. + 31 of both operands, eight at a time
     const char* pa = reinterpret_cast<const char*>(A + (static_cast<size_t>(ti) * kT + wave * 32) * K);
     const char* pb = reinterpret_cast<const char*>(B + (static_cast<size_t>(tj) * kT + wave * 32) * K);
-    uint32_t off[4];
+    uint32_t a_off[4], b_off[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) off[i] = (i * 8 + lm.ld_row) * pitch + lm.col_b[i & 1];
+    for (int i = 0; i < 4; ++i) {
+        a_off[i] = paired_row(i * 8 + lm.ld_row) * pitch + lm.col_b[i & 1];
+        b_off[i] = (i * 8 + lm.ld_row) * pitch + lm.col_b[i & 1];
+    }
     auto issue = [&](int buf) __attribute__((always_inline)) {
         const uint32_t at = lds_base + buf * kTileStageB + wave * 32 * kRowB;
-        static_for<4>([&](auto I) { lds_dma16(pa, off[I.value], at + I.value * 1024); });
-        static_for<4>([&](auto I) { lds_dma16(pb, off[I.value], at + kT * kRowB + I.value * 1024); });
+        static_for<4>([&](auto I) { lds_dma16(pa, a_off[I.value], at + I.value * 1024); });
+        static_for<4>([&](auto I) { lds_dma16(pb, b_off[I.value], at + kT * kRowB + I.value * 1024); });
         pa += kRowB;
         pb += kRowB;
     };
@@ -232,66 +513,117 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs q) {
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j], a[i], acc[i][j], 0, 0, 0);
         }
     }
-    // lane (r, g) holds columns 4 g .. + 3 of row r of each 16 x 16 block
-    const int r = lm.fr_row, g = lane >> 4;
+    const Scalars c = scalars<MODE, kThreads>(q, batch, blockIdx.x == 0, red);
+    const float sum = store_wave<MODE, 4>(q, c, acc, batch, ti * kT + wm * 64, tj * kT + wn * 64, ti != tj, lane);
+    if (MODE == kApply || (MODE == kSym && q.sym == kSymMix))
+        store_part<kThreads>(q, batch, blockIdx.x, MODE == kSym && ti != tj ? 2.0f * sum : sum, red);
+}
+
+// ---- tiles of 256 x 256: the K loop of mfma_tile.hpp, persistent, one workgroup a CU
+template <Product MODE>
+__global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs q, int tiles) {
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * kStageBytes];
+    __shared__ float red[kNW];
+    const OrthWs& w = q.w;
+    const int lane = threadIdx.x % kWave;
+    const int wave = static_cast<int>(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
+    const bool loader = wave < kNL;
+    const int wm = wave / kWavesN, wn = wave % kWavesN;
+    const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
+    const uint32_t a_lds = lds_base + wave * kALd * 1024;
+    const uint32_t b_lds = lds_base + (kBM + (wave >> 1) * kWN + (wave & 1) * 16) * kRowB;
+    const int K = MODE == kGram ? w.mp : w.np;
+    const int KT = K / kStageK;
+    const size_t xb = static_cast<size_t>(w.np) * w.mp, sb = static_cast<size_t>(w.np) * w.np;
+    const int total = tiles * q.batch;
+    // block b runs on XCD b % 8: each XCD gets a run of tiles, mostly of one matrix
+    const int G = gridDim.x;
+    int tile = G % 8 == 0 ? (blockIdx.x % 8) * (G / 8) + blockIdx.x / 8 : blockIdx.x;
+    int batch = 0, t = 0, ti = 0, tj = 0;
+    Loads ld;
+    auto start_tile = [&](int x) __attribute__((always_inline)) {
+        batch = __builtin_amdgcn_readfirstlane(x / tiles);
+        t = x - batch * tiles;
+        decode_tile<MODE>(q, t, kBM, ti, tj);
+        ti = __builtin_amdgcn_readfirstlane(ti);
+        tj = __builtin_amdgcn_readfirstlane(tj);
+        if (!loader) return;
+        const LaneMap lm = lane_map(opaque(lane));
+        const uint32_t pitch = static_cast<uint32_t>(K) * 2u;
+        const uint16_t* A = q.A + batch * (MODE == kGram ? xb : sb) + static_cast<size_t>(ti) * kBM * K;
+        const uint16_t* B = q.B + batch * (MODE == kSym ? sb : xb) +
+                            (static_cast<size_t>(tj) * kBN + (wave >> 1) * kWN + (wave & 1) * 16) * K;
+        ld.a = reinterpret_cast<const char*>(A);
+        ld.a_on = ti * kBM + wave / kWavesN * kWM < w.np;
+        ld.b0 = reinterpret_cast<const char*>(B);
+        ld.b1 = ld.b0 + static_cast<size_t>(32) * pitch;
+        ld.c0 = ld.b0 + static_cast<size_t>(64) * pitch;
+        ld.c1 = ld.b0 + static_cast<size_t>(96) * pitch;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2; ++i) ld.b_off[i] = (i * kRowsPerLoad + lm.ld_row) * pitch + lm.col_b[i];
+        // (a loader whose own rows lie past the end loads none: its rows come after them)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int row = ti * kT + wm * 64 + i * 16 + r, col = tj * kT + wn * 64 + j * 16 + 4 * g;
-            const int trow = ti * kT + wm * 64 + i * 16 + 4 * (r >> 2), tcol = col + (r & 3);    // after quad_transpose
-            float v[4];
+        for (int i = 0; i < kALd; ++i)
+            ld.a_off[i] = static_cast<uint32_t>(paired_row(wave * kALd * kRowsPerLoad + i * kRowsPerLoad + lm.ld_row)) * pitch +
+                          lm.col_b[i & 1];
+        load_half0(ld, ld.a_on, a_lds, b_lds, 0);
+        load_half1(ld, b_lds, 0);
+    };
+    if (tile < total) start_tile(tile);
+    while (tile < total) {
+        f32x4 acc[kMI][kNJ];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e];
-            if constexpr (MODE == kGram || MODE == kPoly) {
-                if constexpr (MODE == kPoly) {
-                    const u32x2 s = *reinterpret_cast<const u32x2*>(w.s + sb + static_cast<size_t>(row) * w.np + col);
+        for (int i = 0; i < kMI; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        v[e] = __builtin_fmaf(q.c, v[e], q.b * f16_at(s, e));
-                }
-                uint16_t* out = MODE == kGram ? w.s : w.p;
-                const u32x2 h = {pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3])};
-                *reinterpret_cast<u32x2*>(out + sb + static_cast<size_t>(row) * w.np + col) = h;
-                if (ti != tj)
-                    *reinterpret_cast<u32x2*>(out + sb + static_cast<size_t>(tcol) * w.np + trow) = quad_transpose(h, lane);
-            } else {
-                const size_t at = xb + static_cast<size_t>(row) * w.mp + col;
-                const u32x2 h = *reinterpret_cast<const u32x2*>(w.xh + at), l = *reinterpret_cast<const u32x2*>(w.xl + at);
+            for (int j = 0; j < kNJ; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = __builtin_fmaf(f16_at(l, e), 1.0f / kLoScale, f16_at(h, e));
-                    v[e] = __builtin_fmaf(q.a, x, v[e]);
-                }
-                if constexpr (MODE == kApply) {
-                    u32x2 hi, lo;
-                    split4(v, hi, lo);
-                    *reinterpret_cast<u32x2*>(w.xh + at) = hi;
-                    *reinterpret_cast<u32x2*>(w.xl + at) = lo;
-                    *reinterpret_cast<u32x2*>(w.xt[q.from ^ 1] + xb + static_cast<size_t>(tcol) * w.np + trow) =
-                        quad_transpose(hi, lane);
-                } else {
-                    u32x2 y = {pack_bf16x2_rne(v[0], v[1]), pack_bf16x2_rne(v[2], v[3])};
-                    uint16_t* out = q.out + static_cast<size_t>(blockIdx.y) * q.rows * q.cols;
-                    int orow = row, ocol = col;
-                    if (q.rows > q.cols) {
-                        y = quad_transpose(y, lane);
-                        orow = tcol;
-                        ocol = trow;
-                    }
-                    if (orow < q.rows) {
-                        uint16_t* o = out + static_cast<size_t>(orow) * q.cols + ocol;
-                        if (ocol + 3 < q.cols && (reinterpret_cast<uintptr_t>(o) & 7) == 0) {
-                            *reinterpret_cast<u32x2*>(o) = y;
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (ocol + e < q.cols) o[e] = static_cast<uint16_t>(y[e >> 1] >> (16 * (e & 1)));
-                        }
-                    }
-                }
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
+        const int cb = batch, ct = t, ci = ti, cj = tj;
+        const int next = tile + G;
+        // in the last stage buffer 0 is free: the next tile's stage 0 lands during the
+        // rest of that stage and the results' way out
+        auto hook = [&](auto step) {
+            if constexpr (decltype(step)::value == kLast) {
+                if (next < total) start_tile(next);
             }
-        }
+        };
+        const bool active = ci * kBM + wm * kWM < w.np;
+        run_k_loop<f16x8>(KT, lds, wm, wn, lane, loader, active, acc, ld, a_lds, b_lds, hook, hook);
+        const Scalars c = scalars<MODE, kNW * kWave>(q, cb, ct == 0, red);
+        float sum = 0.0f;
+        if (active && cj * kBN + wn * kWN < (MODE == kGram || MODE == kSym ? w.np : w.mp))
+            sum = store_wave<MODE, kNJ>(q, c, acc, cb, ci * kBM + wm * kWM, cj * kBN + wn * kWN, ci != cj, opaque(lane));
+        if (MODE == kApply || (MODE == kSym && q.sym == kSymMix))
+            store_part<kNW * kWave>(q, cb, ct, MODE == kSym && ci != cj ? 2.0f * sum : sum, red);
+        tile = next;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+// Which tiles a product runs on: 256 x 256 (one workgroup a CU) or 128 x 128 (two).
+bool wide_tiles(int big, int small, int batch) {
+    const long long cus = device_cu_count();
+    const long long rounds256 = (static_cast<long long>(big) * batch + cus - 1) / cus;
+    const long long rounds128 = (static_cast<long long>(small) * batch + 2 * cus - 1) / (2 * cus);
+    return rounds256 * 24 <= rounds128 * 16;
+}
+
+template <Product MODE>
+void launch_product(const ProductArgs& q, hipStream_t stream) {
+    const OrthWs& w = q.w;
+    constexpr bool square = MODE == kGram || MODE == kSym;
+    auto tiles = [&](int t) {
+        const int r = (w.np + t - 1) / t, c = ((square ? w.np : w.mp) + t - 1) / t;
+        return square ? r * (r + 1) / 2 : r * c;
+    };
+    const int big = tiles(kBM);
+    if (wide_tiles(big, tiles(kT), q.batch)) {
+        const long long total = static_cast<long long>(big) * q.batch;
+        const int cus = device_cu_count();
+        product256_kernel<MODE><<<total < cus ? static_cast<int>(total) : cus, kNW * kWave, 0, stream>>>(q, big);
+    } else {
+        product128_kernel<MODE><<<dim3(tiles(kT), q.batch), kThreads, 0, stream>>>(q);
+    }
 }
 
 }  // namespace
@@ -317,6 +649,7 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
     q.out = static_cast<uint16_t*>(out);
     q.rows = rows;
     q.cols = cols;
+    q.batch = batch;
     const size_t size = static_cast<size_t>(rows) * cols;
     const bool tall = rows > cols;
     const dim3 ngrid(w.parts, batch);
@@ -331,17 +664,45 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
     else if (momentum) begin(std::false_type{}, std::true_type{});
     else begin(std::false_type{}, std::false_type{});
     CAP_LAUNCH_CHECK();
-    const int tn = w.np / kT, tm = w.mp / kT;
-    const dim3 tri(tn * (tn + 1) / 2, batch), all(tn * tm, batch);
-    for (int i = 0; i < steps; ++i) {
-        q.from = i & 1;
-        q.a = sc.v[i][0];
-        q.b = sc.v[i][1];
-        q.c = sc.v[i][2];
-        product_kernel<kGram><<<tri, kThreads, 0, stream>>>(q);
-        product_kernel<kPoly><<<tri, kThreads, 0, stream>>>(q);
-        if (i + 1 < steps) product_kernel<kApply><<<all, kThreads, 0, stream>>>(q);
-        else product_kernel<kFinal><<<all, kThreads, 0, stream>>>(q);
+    auto tri_tiles = [&](int side) { return side * (side + 1) / 2; };
+    const int t256 = (w.np + kBM - 1) / kBM, t128 = w.np / kT;
+    const int sym_tiles = wide_tiles(tri_tiles(t256), tri_tiles(t128), batch) ? tri_tiles(t256) : tri_tiles(t128);
+    const int a256 = t256 * ((w.mp + kBN - 1) / kBN), a128 = t128 * (w.mp / kT);
+    const int apply_tiles = wide_tiles(a256, a128, batch) ? a256 : a128;
+    int from = 0, traces = 1;
+    auto sym = [&](int which, uint16_t* A, uint16_t* B, uint16_t* D) {
+        q.sym = which;
+        q.A = A;
+        q.B = B;
+        q.D = D;
+        q.traces = sym_tiles;
+        launch_product<kSym>(q, stream);
+    };
+    for (int i = 0; i < steps;) {
+        q.pair = (i == 0 && steps >= 4) || i == steps - 2;
+        for (int h = 0; h < 2; ++h)
+            for (int j = 0; j < 3; ++j) q.coef[h][j] = sc.v[q.pair ? i + h : i][j];
+        q.A = q.B = w.xh;
+        q.D = w.sq[0];
+        q.traces = traces;
+        launch_product<kGram>(q, stream);                          // D
+        sym(kSymFirst, w.sq[0], w.sq[0], w.sq[1]);                   // R
+        uint16_t* Q = w.sq[1];
+        if (q.pair) {
+            sym(kSymMix, w.sq[1], w.sq[0], w.sq[2]);                  // T
+            sym(kSymNext, w.sq[2], w.sq[1], w.sq[0]);                 // D'
+            sym(kSymSecond, w.sq[0], w.sq[0], w.sq[2]);               // R'
+            sym(kSymJoin, w.sq[1], w.sq[2], w.sq[0]);                 // Q
+            Q = w.sq[0];
+        }
+        q.A = Q;
+        q.B = w.xt[from];
+        q.D = w.xt[from ^ 1];
+        i += q.pair ? 2 : 1;
+        if (i < steps) launch_product<kApply>(q, stream);
+        else launch_product<kFinal>(q, stream);
+        from ^= 1;
+        traces = apply_tiles;
     }
     CAP_LAUNCH_CHECK();
     return CAP_OK;

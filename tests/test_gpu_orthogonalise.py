@@ -82,6 +82,22 @@ def test_spectra(kind, r, c):
     _near(_run(torch.from_numpy(host).cuda()), [R.orth64(m) for m in host])
 
 
+@pytest.mark.parametrize("b,r,c", [(40, 640, 900), (40, 900, 640), (3, 1920, 2300), (24, 1024, 1024)])
+def test_many_tiles(b, r, c):
+    """Enough tiles for the large form of the products, with sides that end within a tile (reference: the same steps
+    in 64 bits on the GPU)."""
+    g = torch.randn((b, r, c), generator=torch.Generator("cuda").manual_seed(b + r), device="cuda")
+    x = g.double()
+    x = x / (x.square().sum((1, 2), keepdim=True).sqrt() + 1e-7)
+    x = x.transpose(1, 2).contiguous() if r > c else x
+    for _ in range(5):
+        s = torch.matmul(x, x.transpose(1, 2).contiguous())
+        x = R.QUINTIC[0] * x + torch.matmul(R.QUINTIC[1] * s + R.QUINTIC[2] * torch.matmul(s, s), x)
+    x = x.transpose(1, 2) if r > c else x
+    err = ((_run(g).double() - x).square().sum((1, 2)) / x.square().sum((1, 2))).sqrt()
+    assert err.max().item() <= TOL, err.max().item()
+
+
 @pytest.mark.parametrize("nesterov", [False, True])
 @pytest.mark.parametrize("b,r,c", [(1, 5, 3), (3, 96, 200), (2, 300, 130), (1, 1024, 520)])
 def test_muon_steps(b, r, c, nesterov):
