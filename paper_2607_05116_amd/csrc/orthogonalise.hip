@@ -53,15 +53,28 @@ struct OrthWs {
     float* norm;                           // [batch][parts] sums of squares of U
     float* trace;                          // [batch][trace_cap] parts of the next trace
     float* center;                         // [batch][2] s of the group's first and second step
-    int n, m, np, mp, parts, trace_cap;
+    int n, m, np, mp;                      // sides, and as padded with zeros
+    int xp, sp;                            // row pitch of X, and of X^T and the n x n matrices
+    int parts, trace_cap;
 };
 
 int up_to(int v, int q) { return (v + q - 1) / q * q; }
 
+// Row pitch of a padded side: an odd number of 256-byte units.  Consecutive rows then
+// lie in different memory channels; with 4096-byte rows (n = 2048) the 16 rows that an
+// instruction of the results' way out touches share one, and a product of n x n
+// matrices took 214 us where it takes PITCHED (8 matrices).
+int pitch_of(int padded) { return (padded / 128 % 2) ? padded : padded + 128; }
+
+// Parts of a matrix for its norm, of at least 8192 values: four steps of a workgroup.
+size_t norm_per_part(int rows, int cols) {
+    const size_t size = static_cast<size_t>(rows) * cols;
+    const size_t per = (size + kMaxNormParts - 1) / kMaxNormParts;
+    return per < 8192 ? 8192 : (per + 3) / 4 * 4;
+}
 int norm_parts(int rows, int cols) {
-    const long long per = 64 * 1024;       // values per block
-    const long long want = (static_cast<long long>(rows) * cols + per - 1) / per;
-    return static_cast<int>(want < kMaxNormParts ? want : kMaxNormParts);
+    const size_t per = norm_per_part(rows, cols);
+    return static_cast<int>((static_cast<size_t>(rows) * cols + per - 1) / per);
 }
 
 size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
@@ -74,13 +87,14 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
         at += (bytes + 255) & ~size_t(255);
         return q;
     };
-    const size_t x = 2 * batch * np * mp, q = 2 * batch * np * np;
+    const size_t xp = pitch_of(static_cast<int>(mp)), sp = pitch_of(static_cast<int>(np));
+    const size_t x = 2 * batch * np * xp, xt = 2 * batch * mp * sp, q = 2 * batch * np * sp;
     // tiles of 256 may read 128 rows past a matrix (never used): of the next one, or of
     // what follows here; each kind of matrix is followed by one at least as large
     char* v[7];
     for (int i = 4; i < 7; ++i) v[i] = take(q);
-    for (int i = 0; i < 4; ++i) v[i] = take(x);
-    take(static_cast<size_t>(kPad) * mp * 2);
+    for (int i = 0; i < 4; ++i) v[i] = take(i < 2 ? x : xt);
+    take(static_cast<size_t>(kPad) * (xp > sp ? xp : sp) * 2);
     const int parts = norm_parts(rows, cols);
     char* f = take(static_cast<size_t>(batch) * parts * 4);
     const size_t cap = (np / 128) * (mp / 128);
@@ -98,6 +112,8 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
         w->m = m;
         w->np = static_cast<int>(np);
         w->mp = static_cast<int>(mp);
+        w->xp = static_cast<int>(xp);
+        w->sp = static_cast<int>(sp);
         w->parts = parts;
         w->trace_cap = static_cast<int>(cap);
     }
@@ -107,16 +123,24 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
 // ------------------------------------------------------------------ norm and momentum
 // Sum of squares of U over this block's part of its matrix; writes the momentum.
 template <bool BF16, bool MOM>
-__global__ __launch_bounds__(kNormThreads) void norm_kernel(Source src, size_t size, int parts,
+__global__ __launch_bounds__(kNormThreads) void norm_kernel(Source src, size_t size, size_t per, int parts, int vec,
                                                             float* __restrict__ norm) {
     __shared__ float red[kNormThreads / kWave];
     const size_t base = blockIdx.y * size;
-    const size_t per = (size + parts - 1) / parts;
     const size_t a = blockIdx.x * per, b = a + per < size ? a + per : size;
     float sum = 0.0f;
-    for (size_t i = a + threadIdx.x; i < b; i += kNormThreads) {
-        const float u = load_u<BF16, MOM, true>(src, base + i);
-        sum = __builtin_fmaf(u, u, sum);
+    if (vec) {                                               // per and size are multiples of 4
+#pragma unroll 4
+        for (size_t i = a + 4 * threadIdx.x; i < b; i += 4 * kNormThreads) {
+            const f32x4 u = load_u4<BF16, MOM, true>(src, base + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = __builtin_fmaf(u[e], u[e], sum);
+        }
+    } else {
+        for (size_t i = a + threadIdx.x; i < b; i += kNormThreads) {
+            const float u = load_u<BF16, MOM, true>(src, base + i);
+            sum = __builtin_fmaf(u, u, sum);
+        }
     }
 #pragma unroll
     for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
@@ -129,13 +153,33 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(Source src, size_t s
     }
 }
 
-// X0 in both orientations, padded with zeros: 64 x 64 tiles of U through LDS.
+// X0 in both orientations, padded with zeros: 64 x 64 tiles of U through LDS, four
+// values a thread at a time.
 template <bool BF16, bool MOM>
-__global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int cols, float eps, OrthWs w) {
+__global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int cols, int vec, float eps, OrthWs w) {
     __shared__ float tile[64][65];
     __shared__ float scale_s;
     const bool tall = rows > cols;
     const int batch = blockIdx.z;
+    const size_t base = static_cast<size_t>(batch) * rows * cols;
+    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;      // in the matrix as given
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    f32x4 u[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        const int row = r0 + 16 * x + ty, col = c0 + 4 * tx;
+        u[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (row < rows) {
+            const size_t i = base + static_cast<size_t>(row) * cols + col;
+            if (vec) {
+                if (col < cols) u[x] = load_u4<BF16, MOM, false>(src, i);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col + e < cols) u[x][e] = load_u<BF16, MOM, false>(src, i + e);
+            }
+        }
+    }
     if (threadIdx.x < kWave) {
         float t = 0.0f;
         for (int i = threadIdx.x; i < w.parts; i += kWave) t += w.norm[static_cast<size_t>(batch) * w.parts + i];
@@ -150,66 +194,68 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
     }
     __syncthreads();
     const float scale = scale_s;
-    const size_t base = static_cast<size_t>(batch) * rows * cols;
-    const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;      // in the matrix as given
-    const int tx = threadIdx.x % 64, ty = threadIdx.x / 64;
-    for (int r = ty; r < 64; r += 4) {
-        float u = 0.0f;
-        if (r0 + r < rows && c0 + tx < cols) {
-            const size_t i = base + static_cast<size_t>(r0 + r) * cols + c0 + tx;
-            u = load_u<BF16, MOM, false>(src, i);
+    const size_t xb = static_cast<size_t>(batch) * w.np * w.xp, tb = static_cast<size_t>(batch) * w.mp * w.sp;
+    // as given, [rows][cols] is X of a wide matrix and X^T of a tall one
+    uint16_t* const nat_hi = tall ? w.xt[0] : w.xh;
+    uint16_t* const tra_hi = tall ? w.xh : w.xt[0];
+    const size_t nat_pitch = tall ? w.sp : w.xp, tra_pitch = tall ? w.xp : w.sp;
+    const size_t nat_base = tall ? tb : xb, tra_base = tall ? xb : tb;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = u[x][e] * scale;
+            tile[16 * x + ty][4 * tx + e] = v[e];
         }
-        tile[r][tx] = u * scale;
+        u32x2 hi, lo;
+        split4(v, hi, lo);
+        const size_t at = nat_base + static_cast<size_t>(r0 + 16 * x + ty) * nat_pitch + c0 + 4 * tx;
+        *reinterpret_cast<u32x2*>(nat_hi + at) = hi;
+        if (!tall) *reinterpret_cast<u32x2*>(w.xl + at) = lo;
     }
     __syncthreads();
-    const size_t xb = static_cast<size_t>(batch) * w.np * w.mp;
-    // as given: [rows][cols] goes to X (wide) or to X^T (tall)
-    for (int r = ty; r < 64; r += 4) {
-        const float v = tile[r][tx], u = tile[tx][r];
-        const _Float16 hv = static_cast<_Float16>(v), hu = static_cast<_Float16>(u);
-        const int ra = r0 + r, ca = c0 + tx;                   // element v
-        const int rb = c0 + r, cb = r0 + tx;                   // element u, transposed
-        const float x = tall ? u : v;
-        const _Float16 h = tall ? hu : hv;
-        const size_t nat = tall ? xb + static_cast<size_t>(rb) * w.mp + cb : xb + static_cast<size_t>(ra) * w.mp + ca;
-        const size_t tra = tall ? xb + static_cast<size_t>(ra) * w.np + ca : xb + static_cast<size_t>(rb) * w.np + cb;
-        w.xh[nat] = __builtin_bit_cast(uint16_t, h);
-        w.xl[nat] = __builtin_bit_cast(uint16_t, static_cast<_Float16>((x - static_cast<float>(h)) * kLoScale));
-        w.xt[0][tra] = __builtin_bit_cast(uint16_t, tall ? hv : hu);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = tile[4 * tx + e][16 * x + ty];
+        u32x2 hi, lo;
+        split4(v, hi, lo);
+        const size_t at = tra_base + static_cast<size_t>(c0 + 16 * x + ty) * tra_pitch + r0 + 4 * tx;
+        *reinterpret_cast<u32x2*>(tra_hi + at) = hi;
+        if (tall) *reinterpret_cast<u32x2*>(w.xl + at) = lo;
     }
 }
 
 // ------------------------------------------------------------------ products
-// kGram:  D = X X^T - s I, s = its trace / n
-// kSym:   one of the group's n x n products (Sym)
-// kApply: X <- p X + Q X: X, its error, X^T and the parts of |X|^2
-// kFinal: the same to the bf16 result, in the orientation it is wanted
-enum Product { kGram, kSym, kApply, kFinal };
-
-// The n x n products of a group, with p = a + b s + c s^2 of the first step's
-// coefficients and s, p' of the second's:
-//   kSymFirst:  R  = (b + 2 c s) D + c D D               (P = p I + R)
-//   kSymMix:    T  = p D + s R + R D                     (P S = p s I + T), parts of tr(P S P)
-//   kSymNext:   D' = p T + p s R + T R + (p^2 s - s') I  (P S P = s' I + D')
-//   kSymSecond: R' = kSymFirst of the second step
-//   kSymJoin:   Q  = p R' + p' R + R R'                  (P P' = p p' I + Q)
-enum Sym { kSymFirst, kSymMix, kSymNext, kSymSecond, kSymJoin };
+// The products of a group, with p = a + b s + c s^2 of the first step's coefficients and
+// s, p' of the second's and s':
+//   kGram   D  = X X^T - s I                      s = |X|^2 / n
+//   kSym1   R  = (b + 2 c s) D + c D D            P = p I + R
+//   kMix    T  = s R + p D + R D                  P S = p s I + T; parts of tr(P S P)
+//   kSym2   D' = p T + p s R + T R + (p^2 s - s') I       P S P = s' I + D'
+//   kSym1   R' of the second step
+//   kSym2   Q  = p' R + p R' + R R'               P P' = p p' I + Q
+//   kApply  X <- p X + Q X: X, its error, X^T and the parts of |X|^2
+//   kFinal  the same to the bf16 result, in the orientation it is wanted
+enum Product { kGram, kSym1, kMix, kSym2, kApply, kFinal };
+constexpr bool is_square(Product m) { return m == kGram || m == kSym1 || m == kMix || m == kSym2; }
 
 struct ProductArgs {
     OrthWs w;
     const uint16_t *A, *B;                 // rows of the left operand; rows (of the transpose) of the right
-    uint16_t* D;                           // kSym, kGram: result; kApply: X^T
-    int sym, traces;                       // kSym: which; kGram, kSymNext: parts of the trace
+    uint16_t* D;                           // result; kApply: X^T
+    int second, pair;                      // kSym1: of the second step; kSym2: Q; the group has two steps
+    int traces;                            // kGram, kSym2 (D'): parts of the trace
     float coef[2][3];                      // of the group's steps
-    int pair;
     uint16_t* out;
     int rows, cols, batch;
 };
 
 struct Scalars {
-    float ab, a, b, i;                     // of A B, A, B and I
-    float s1;                              // kSymNext: s'
-    float p, ps;                           // kSymMix: the multiples of I in P and T
+    float ab, a, b, i;                     // of A B, A (kApply: X), B and I
+    float p, ps;                           // kMix: the multiples of I in P and T
 };
 
 // Sum of `count` parts by the whole workgroup, in a fixed order.
@@ -230,7 +276,7 @@ __device__ __forceinline__ float sum_parts(const float* parts, int count, float*
 
 __device__ __forceinline__ float poly(const float (&c)[3], float s) { return __builtin_fmaf(__builtin_fmaf(c[2], s, c[1]), s, c[0]); }
 
-// The scalars of a product of matrix `batch`; kGram and kSymNext find their s from the
+// The scalars of a product of matrix `batch`; kGram and kSym2 (D') find their s from the
 // parts and (tile 0 of the matrix) keep it for the products after them.
 template <Product MODE, int THREADS>
 __device__ __forceinline__ Scalars scalars(const ProductArgs& q, int batch, bool first_tile, float* red) {
@@ -242,34 +288,33 @@ __device__ __forceinline__ Scalars scalars(const ProductArgs& q, int batch, bool
         const float s = sum_parts<THREADS>(parts, q.traces, red) / static_cast<float>(q.w.n);
         if (first_tile && threadIdx.x == 0) center[0] = s;
         c.i = -s;
-    } else {
-        const float s = center[0];
-        const float p = poly(q.coef[0], s);
-        if constexpr (MODE == kSym) {
-            if (q.sym == kSymFirst) {
-                c.ab = q.coef[0][2];
-                c.a = __builtin_fmaf(2.0f * q.coef[0][2], s, q.coef[0][1]);
-            } else if (q.sym == kSymMix) {
-                c.a = s;
-                c.b = p;
-                c.p = p;
-                c.ps = p * s;
-            } else if (q.sym == kSymNext) {
-                c.s1 = sum_parts<THREADS>(parts, q.traces, red) / static_cast<float>(q.w.n);
-                if (first_tile && threadIdx.x == 0) center[1] = c.s1;
-                c.a = p;
-                c.b = p * s;
-                c.i = p * p * s - c.s1;
-            } else if (q.sym == kSymSecond) {
-                c.ab = q.coef[1][2];
-                c.a = __builtin_fmaf(2.0f * q.coef[1][2], center[1], q.coef[1][1]);
-            } else {
-                c.a = poly(q.coef[1], center[1]);
-                c.b = p;
-            }
+        return c;
+    }
+    const float s = center[0];
+    const float p = poly(q.coef[0], s);
+    if constexpr (MODE == kSym1) {
+        const float x = q.second ? center[1] : s;
+        const float(&f)[3] = q.coef[q.second];
+        c.ab = f[2];
+        c.a = __builtin_fmaf(2.0f * f[2], x, f[1]);
+    } else if constexpr (MODE == kMix) {
+        c.a = s;
+        c.b = p;
+        c.p = p;
+        c.ps = p * s;
+    } else if constexpr (MODE == kSym2) {
+        if (q.second) {
+            c.a = poly(q.coef[1], center[1]);
+            c.b = p;
         } else {
-            c.a = q.pair ? p * poly(q.coef[1], center[1]) : p;
+            const float s1 = sum_parts<THREADS>(parts, q.traces, red) / static_cast<float>(q.w.n);
+            if (first_tile && threadIdx.x == 0) center[1] = s1;
+            c.a = p;
+            c.b = p * s;
+            c.i = p * p * s - s1;
         }
+    } else {
+        c.a = q.pair ? p * poly(q.coef[1], center[1]) : p;
     }
     return c;
 }
@@ -282,137 +327,157 @@ __device__ __forceinline__ int paired_row(int v) {
     return (v & ~31) | ((v & 12) << 1) | ((v >> 2) & 4) | (v & 3);
 }
 
+// 16 bytes at a scalar base and a lane's 32-bit offset, in global memory.
+typedef __attribute__((address_space(1))) char global_char;
+typedef __attribute__((address_space(1))) u32x4 global_u32x4;
+__device__ __forceinline__ global_u32x4* lane_ptr(const void* base, uint32_t off) {
+    return reinterpret_cast<global_u32x4*>(reinterpret_cast<global_char*>(reinterpret_cast<uint64_t>(uniform_ptr(base))) + off);
+}
+
 // Results of a wave's 64 x 16 NJ block at (row0, col0) of the matrix.  Lane (r, g)
 // holds columns 4 g .. + 3 of each 16 x 16 block, of row paired_row.  Two adjacent
 // blocks trade halves (permlane16_swap), so that a lane reads and writes 8 consecutive
-// columns: columns 8 (g / 2) .. of block g % 2.
+// columns: columns 8 (g / 2) .. of block g % 2.  They go out in steps of two row blocks
+// and two column blocks; what a step adds to (A and B, or X and its error) is loaded
+// kAhead steps before, since the loads' way is as long as several steps.  The steps are
+// kept apart (sched_barrier): mixed, they need more registers than there are.
+// Addresses are a scalar base for the step and a 32-bit lane offset.
 template <Product MODE, int NJ>
 __device__ __forceinline__ float store_wave(const ProductArgs& q, const Scalars& c, f32x4 (&acc)[4][NJ], int batch, int row0,
                                             int col0, bool mirror, int lane) {
     const OrthWs& w = q.w;
     const int r = lane & 15, g = lane >> 4;
-    constexpr bool kSquare = MODE == kGram || MODE == kSym;
-    const size_t pitch = kSquare ? w.np : w.mp;
-    const size_t xb = static_cast<size_t>(batch) * w.np * w.mp, sb = static_cast<size_t>(batch) * w.np * w.np;
-    const size_t base = kSquare ? sb : xb;
-    const bool use_a = MODE == kSym, use_b = MODE == kSym && c.b != 0.0f;
-    float sum = 0.0f;
-    // 8 consecutive columns of a row: the lane's halves of two blocks
-    auto load_pair = [&](const uint16_t* p, size_t at, u32x2& x, u32x2& y) __attribute__((always_inline)) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(p + at);
+    constexpr bool kSquare = is_square(MODE);
+    constexpr int kIn = MODE == kGram ? 0 : MODE == kSym1 ? 1 : 2;     // matrices the results add to
+    constexpr int kSteps = NJ, kAhead = 2;
+    const int pitch = kSquare ? w.sp : w.xp;
+    const size_t at0 = (static_cast<size_t>(batch) * w.np + row0) * pitch + col0;
+    const size_t t0 = (static_cast<size_t>(batch) * (kSquare ? w.np : w.mp) + col0) * w.sp + row0;
+    const uint32_t lane_at = 2u * ((8 * (r >> 2) + (r & 3)) * pitch + 16 * (g & 1) + 8 * (g >> 1));
+    const uint32_t lane_t = 2u * ((4 * g + (r & 3)) * w.sp + 8 * (r >> 2));
+    auto step_of = [&](const uint16_t* p, int x, int ii) __attribute__((always_inline)) {
+        const int ip = x / (NJ / 2), pr = x % (NJ / 2);
+        return lane_ptr(p + at0 + static_cast<size_t>(32 * ip + 4 * ii) * pitch + 32 * pr, lane_at);
+    };
+    auto put = [&](uint16_t* p, int x, int ii, const u32x4& v) __attribute__((always_inline)) {
+        *step_of(p, x, ii) = v;
+    };
+    // 8 consecutive columns of a row <-> the lane's halves of two blocks
+    auto halves = [](const u32x4& v, u32x2& x, u32x2& y) __attribute__((always_inline)) {
         const auto s0 = __builtin_amdgcn_permlane16_swap(v[0], v[2], false, false);
         const auto s1 = __builtin_amdgcn_permlane16_swap(v[1], v[3], false, false);
         x = u32x2{s0[0], s1[0]};
         y = u32x2{s0[1], s1[1]};
     };
-    auto join_pair = [&](const u32x2& x, const u32x2& y) __attribute__((always_inline)) {
+    auto join = [](const u32x2& x, const u32x2& y) __attribute__((always_inline)) {
         const auto s0 = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false);
         const auto s1 = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
         return u32x4{s0[0], s1[0], s0[1], s1[1]};
     };
+    auto bf16_out = [&](int row, int col, const u32x4& y) __attribute__((always_inline)) {
+        if (row >= q.rows) return;
+        uint16_t* o = q.out + (static_cast<size_t>(batch) * q.rows + row) * q.cols + col;
+        if (col + 7 < q.cols && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+            *reinterpret_cast<u32x4*>(o) = y;
+        } else {
 #pragma unroll
-    for (int ip = 0; ip < 2; ++ip)
+            for (int e = 0; e < 8; ++e)
+                if (col + e < q.cols) o[e] = static_cast<uint16_t>(y[e >> 1] >> (16 * (e & 1)));
+        }
+    };
+    const uint16_t* const p0 = kSquare ? q.A : w.xh;
+    const uint16_t* const p1 = kSquare ? q.B : w.xl;
+    u32x4 in[kAhead + 1][2][2];
+    auto fetch = [&](auto X) __attribute__((always_inline)) {
+        constexpr int x = decltype(X)::value;
 #pragma unroll
-        for (int pr = 0; pr < NJ / 2; ++pr) {
-            u32x2 t[2][2];                                         // [row block][column block], transposed
+        for (int ii = 0; ii < 2; ++ii) {
+            if constexpr (kIn > 0) in[x % (kAhead + 1)][ii][0] = *step_of(p0, x, ii);
+            if constexpr (kIn > 1) in[x % (kAhead + 1)][ii][1] = *step_of(p1, x, ii);
+        }
+    };
+    float sum = 0.0f;
+    static_for<kAhead>([&](auto X) { fetch(X); });
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<kSteps>([&](auto X) __attribute__((always_inline)) {
+        constexpr int x = decltype(X)::value, ip = x / (NJ / 2), pr = x % (NJ / 2);
+        if constexpr (x + kAhead < kSteps) fetch(std::integral_constant<int, x + kAhead>{});
+        u32x2 t[2][2];                                             // [row block][column block], transposed
 #pragma unroll
-            for (int ii = 0; ii < 2; ++ii) {
-                const int row = row0 + 32 * ip + 8 * (r >> 2) + 4 * ii + (r & 3);
-                const int c8 = col0 + 32 * pr + 16 * (g & 1) + 8 * (g >> 1);
-                const size_t at = base + static_cast<size_t>(row) * pitch + c8;
-                float v[2][4];
+        for (int ii = 0; ii < 2; ++ii) {
+            const int row = row0 + 32 * ip + 8 * (r >> 2) + 4 * ii + (r & 3);
+            float v[2][4];
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[b][e] = acc[2 * ip + ii][2 * pr + b][e];
-                u32x2 hi[2], lo[2];
-                if constexpr (kSquare) {
-                    u32x2 ea[2], eb[2];
-                    if (use_a) load_pair(q.A, at, ea[0], ea[1]);
-                    if (use_b) load_pair(q.B, at, eb[0], eb[1]);
+                for (int e = 0; e < 4; ++e) v[b][e] = acc[2 * ip + ii][2 * pr + b][e];
+            u32x2 hi[2], lo[2], i0[2], i1[2];
+            if constexpr (kIn > 0) halves(in[x % (kAhead + 1)][ii][0], i0[0], i0[1]);
+            if constexpr (kIn > 1) halves(in[x % (kAhead + 1)][ii][1], i1[0], i1[1]);
+            if constexpr (kSquare) {
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) {
+                for (int b = 0; b < 2; ++b) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int col = col0 + 32 * pr + 16 * b + 4 * g + e;
-                            const bool diag = row == col && row < w.n;
-                            float x = c.ab * v[b][e];
-                            if (use_a) x = __builtin_fmaf(c.a, f16_at(ea[b], e), x);
-                            if (use_b) x = __builtin_fmaf(c.b, f16_at(eb[b], e), x);
-                            if (diag) x += c.i;
-                            if constexpr (MODE == kSym)
-                                if (q.sym == kSymMix)                  // P and T whole
-                                    sum = __builtin_fmaf(diag ? x + c.ps : x, f16_at(ea[b], e) + (diag ? c.p : 0.0f), sum);
-                            v[b][e] = x;
-                        }
-                        hi[b] = u32x2{pack_f16x2(v[b][0], v[b][1]), pack_f16x2(v[b][2], v[b][3])};
+                    for (int e = 0; e < 4; ++e) {
+                        float y = MODE == kSym1 ? c.ab * v[b][e] : v[b][e];
+                        if constexpr (kIn > 0) y = __builtin_fmaf(c.a, f16_at(i0[b], e), y);
+                        if constexpr (kIn > 1) y = __builtin_fmaf(c.b, f16_at(i1[b], e), y);
+                        if constexpr (MODE == kMix) sum = __builtin_fmaf(y, f16_at(i0[b], e), sum);
+                        v[b][e] = y;
                     }
-                    *reinterpret_cast<u32x4*>(q.D + at) = join_pair(hi[0], hi[1]);
-                    if (mirror) {
+                    if (!mirror) {                                 // a tile on the diagonal
+                        const int d = row - (col0 + 32 * pr + 16 * b + 4 * g);
 #pragma unroll
-                        for (int b = 0; b < 2; ++b) t[ii][b] = quad_transpose(hi[b], lane);
+                        for (int e = 0; e < 4; ++e)
+                            if (d == e && row < w.n) {
+                                // tr(T P): T = T' + ps I, P = R + p I
+                                if constexpr (MODE == kMix)
+                                    sum += __builtin_fmaf(c.ps, f16_at(i0[b], e), c.p * (v[b][e] + c.ps));
+                                v[b][e] += c.i;
+                            }
                     }
-                } else {
-                    u32x2 xh[2], xl[2];
-                    load_pair(w.xh, at, xh[0], xh[1]);
-                    load_pair(w.xl, at, xl[0], xl[1]);
+                    hi[b] = u32x2{pack_f16x2(v[b][0], v[b][1]), pack_f16x2(v[b][2], v[b][3])};
+                }
+                put(q.D, x, ii, join(hi[0], hi[1]));
+            } else {
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) {
+                for (int b = 0; b < 2; ++b) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float x = __builtin_fmaf(f16_at(xl[b], e), 1.0f / kLoScale, f16_at(xh[b], e));
-                            v[b][e] = __builtin_fmaf(c.a, x, v[b][e]);
-                        }
-                        if constexpr (MODE == kApply) {
-                            split4(v[b], hi[b], lo[b]);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) sum = __builtin_fmaf(v[b][e], v[b][e], sum);
-                            t[ii][b] = quad_transpose(hi[b], lane);
-                        } else {
-                            hi[b] = u32x2{pack_bf16x2_rne(v[b][0], v[b][1]), pack_bf16x2_rne(v[b][2], v[b][3])};
-                            if (q.rows > q.cols) t[ii][b] = quad_transpose(hi[b], lane);
-                        }
+                    for (int e = 0; e < 4; ++e) {
+                        const float xv = __builtin_fmaf(f16_at(i1[b], e), 1.0f / kLoScale, f16_at(i0[b], e));
+                        v[b][e] = __builtin_fmaf(c.a, xv, v[b][e]);
                     }
                     if constexpr (MODE == kApply) {
-                        *reinterpret_cast<u32x4*>(w.xh + at) = join_pair(hi[0], hi[1]);
-                        *reinterpret_cast<u32x4*>(w.xl + at) = join_pair(lo[0], lo[1]);
-                    } else if (q.rows <= q.cols) {
-                        const u32x4 y = join_pair(hi[0], hi[1]);
-                        if (row < q.rows) {
-                            uint16_t* o = q.out + (static_cast<size_t>(batch) * q.rows + row) * q.cols + c8;
-                            if (c8 + 7 < q.cols && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-                                *reinterpret_cast<u32x4*>(o) = y;
-                            } else {
+                        split4(v[b], hi[b], lo[b]);
 #pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    if (c8 + e < q.cols) o[e] = static_cast<uint16_t>(y[e >> 1] >> (16 * (e & 1)));
-                            }
-                        }
+                        for (int e = 0; e < 4; ++e) sum = __builtin_fmaf(v[b][e], v[b][e], sum);
+                    } else {
+                        hi[b] = u32x2{pack_bf16x2_rne(v[b][0], v[b][1]), pack_bf16x2_rne(v[b][2], v[b][3])};
                     }
+                }
+                if constexpr (MODE == kApply) {
+                    put(w.xh, x, ii, join(hi[0], hi[1]));
+                    put(w.xl, x, ii, join(lo[0], lo[1]));
+                } else if (q.rows <= q.cols) {
+                    bf16_out(row, col0 + 32 * pr + 16 * (g & 1) + 8 * (g >> 1), join(hi[0], hi[1]));
                 }
             }
-            // transposed: row col0 + .. + 4 g + r % 4, eight columns
-            const int tc = row0 + 32 * ip + 8 * (r >> 2);
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int tr = col0 + 32 * pr + 16 * b + 4 * g + (r & 3);
-                const u32x4 y = {t[0][b][0], t[0][b][1], t[1][b][0], t[1][b][1]};
-                if constexpr (kSquare) {
-                    if (mirror) *reinterpret_cast<u32x4*>(q.D + sb + static_cast<size_t>(tr) * w.np + tc) = y;
-                } else if constexpr (MODE == kApply) {
-                    *reinterpret_cast<u32x4*>(q.D + xb + static_cast<size_t>(tr) * w.np + tc) = y;
-                } else if (q.rows > q.cols && tr < q.rows) {
-                    uint16_t* o = q.out + (static_cast<size_t>(batch) * q.rows + tr) * q.cols + tc;
-                    if (tc + 7 < q.cols && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-                        *reinterpret_cast<u32x4*>(o) = y;
-                    } else {
+            for (int b = 0; b < 2; ++b) t[ii][b] = quad_transpose(hi[b], lane);
+        }
+        // transposed: row col0 + .. + 4 g + r % 4, eight columns
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (tc + e < q.cols) o[e] = static_cast<uint16_t>(y[e >> 1] >> (16 * (e & 1)));
-                    }
-                }
+        for (int b = 0; b < 2; ++b) {
+            const u32x4 y = {t[0][b][0], t[0][b][1], t[1][b][0], t[1][b][1]};
+            if constexpr (MODE == kFinal) {
+                if (q.rows > q.cols)
+                    bf16_out(col0 + 32 * pr + 16 * b + 4 * g + (r & 3), row0 + 32 * ip + 8 * (r >> 2), y);
+            } else if (MODE == kApply || mirror) {
+                *lane_ptr(q.D + t0 + static_cast<size_t>(32 * pr + 16 * b) * w.sp + 32 * ip, lane_t) = y;
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+    });
     return sum;
 }
 
@@ -433,7 +498,7 @@ __device__ __forceinline__ void store_part(const ProductArgs& q, int batch, int 
 
 template <Product MODE>
 __device__ __forceinline__ void decode_tile(const ProductArgs& q, int t, int tile_rows, int& ti, int& tj) {
-    if constexpr (MODE == kGram || MODE == kSym) {
+    if constexpr (is_square(MODE)) {
         triangle(t, ti, tj);
     } else {
         const int tm = (q.w.np + tile_rows - 1) / tile_rows;
@@ -458,16 +523,15 @@ __global__ __launch_bounds__(kThreads, 2) void product128_kernel(ProductArgs q) 
     const int batch = blockIdx.y;
     int ti, tj;
     decode_tile<MODE>(q, blockIdx.x, kT, ti, tj);
-    const size_t xb = static_cast<size_t>(batch) * w.np * w.mp, sb = static_cast<size_t>(batch) * w.np * w.np;
-    const int K = MODE == kGram ? w.mp : w.np;
-    const uint16_t* A = q.A + (MODE == kGram ? xb : sb);
-    const uint16_t* B = q.B + (MODE == kSym ? sb : xb);
-    const uint32_t pitch = static_cast<uint32_t>(K) * 2u;
+    const int K = MODE == kGram ? w.mp : w.np, ld = MODE == kGram ? w.xp : w.sp;
+    const uint16_t* A = q.A + static_cast<size_t>(batch) * w.np * ld;
+    const uint16_t* B = q.B + static_cast<size_t>(batch) * (is_square(MODE) ? w.np : w.mp) * ld;
+    const uint32_t pitch = static_cast<uint32_t>(ld) * 2u;
     const LaneMap lm = lane_map(lane);
     const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
     // wave w brings rows 32 w .. + 31 of both operands, eight at a time
-    const char* pa = reinterpret_cast<const char*>(A + (static_cast<size_t>(ti) * kT + wave * 32) * K);
-    const char* pb = reinterpret_cast<const char*>(B + (static_cast<size_t>(tj) * kT + wave * 32) * K);
+    const char* pa = reinterpret_cast<const char*>(A + (static_cast<size_t>(ti) * kT + wave * 32) * ld);
+    const char* pb = reinterpret_cast<const char*>(B + (static_cast<size_t>(tj) * kT + wave * 32) * ld);
     uint32_t a_off[4], b_off[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -515,8 +579,8 @@ __global__ __launch_bounds__(kThreads, 2) void product128_kernel(ProductArgs q) 
     }
     const Scalars c = scalars<MODE, kThreads>(q, batch, blockIdx.x == 0, red);
     const float sum = store_wave<MODE, 4>(q, c, acc, batch, ti * kT + wm * 64, tj * kT + wn * 64, ti != tj, lane);
-    if (MODE == kApply || (MODE == kSym && q.sym == kSymMix))
-        store_part<kThreads>(q, batch, blockIdx.x, MODE == kSym && ti != tj ? 2.0f * sum : sum, red);
+    if constexpr (MODE == kApply || MODE == kMix)
+        store_part<kThreads>(q, batch, blockIdx.x, MODE == kMix && ti != tj ? 2.0f * sum : sum, red);
 }
 
 // ---- tiles of 256 x 256: the K loop of mfma_tile.hpp, persistent, one workgroup a CU
@@ -532,9 +596,7 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
     const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
     const uint32_t a_lds = lds_base + wave * kALd * 1024;
     const uint32_t b_lds = lds_base + (kBM + (wave >> 1) * kWN + (wave & 1) * 16) * kRowB;
-    const int K = MODE == kGram ? w.mp : w.np;
-    const int KT = K / kStageK;
-    const size_t xb = static_cast<size_t>(w.np) * w.mp, sb = static_cast<size_t>(w.np) * w.np;
+    const int KT = (MODE == kGram ? w.mp : w.np) / kStageK, lead = MODE == kGram ? w.xp : w.sp;
     const int total = tiles * q.batch;
     // block b runs on XCD b % 8: each XCD gets a run of tiles, mostly of one matrix
     const int G = gridDim.x;
@@ -549,10 +611,10 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
         tj = __builtin_amdgcn_readfirstlane(tj);
         if (!loader) return;
         const LaneMap lm = lane_map(opaque(lane));
-        const uint32_t pitch = static_cast<uint32_t>(K) * 2u;
-        const uint16_t* A = q.A + batch * (MODE == kGram ? xb : sb) + static_cast<size_t>(ti) * kBM * K;
-        const uint16_t* B = q.B + batch * (MODE == kSym ? sb : xb) +
-                            (static_cast<size_t>(tj) * kBN + (wave >> 1) * kWN + (wave & 1) * 16) * K;
+        const uint32_t pitch = static_cast<uint32_t>(lead) * 2u;
+        const size_t b_rows = is_square(MODE) ? w.np : w.mp;
+        const uint16_t* A = q.A + (static_cast<size_t>(batch) * w.np + static_cast<size_t>(ti) * kBM) * lead;
+        const uint16_t* B = q.B + (batch * b_rows + static_cast<size_t>(tj) * kBN + (wave >> 1) * kWN + (wave & 1) * 16) * lead;
         ld.a = reinterpret_cast<const char*>(A);
         ld.a_on = ti * kBM + wave / kWavesN * kWM < w.np;
         ld.b0 = reinterpret_cast<const char*>(B);
@@ -591,10 +653,10 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
         run_k_loop<f16x8>(KT, lds, wm, wn, lane, loader, active, acc, ld, a_lds, b_lds, hook, hook);
         const Scalars c = scalars<MODE, kNW * kWave>(q, cb, ct == 0, red);
         float sum = 0.0f;
-        if (active && cj * kBN + wn * kWN < (MODE == kGram || MODE == kSym ? w.np : w.mp))
+        if (active && cj * kBN + wn * kWN < (is_square(MODE) ? w.np : w.mp))
             sum = store_wave<MODE, kNJ>(q, c, acc, cb, ci * kBM + wm * kWM, cj * kBN + wn * kWN, ci != cj, opaque(lane));
-        if (MODE == kApply || (MODE == kSym && q.sym == kSymMix))
-            store_part<kNW * kWave>(q, cb, ct, MODE == kSym && ci != cj ? 2.0f * sum : sum, red);
+        if constexpr (MODE == kApply || MODE == kMix)
+            store_part<kNW * kWave>(q, cb, ct, MODE == kMix && ci != cj ? 2.0f * sum : sum, red);
         tile = next;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -611,7 +673,7 @@ bool wide_tiles(int big, int small, int batch) {
 template <Product MODE>
 void launch_product(const ProductArgs& q, hipStream_t stream) {
     const OrthWs& w = q.w;
-    constexpr bool square = MODE == kGram || MODE == kSym;
+    constexpr bool square = is_square(MODE);
     auto tiles = [&](int t) {
         const int r = (w.np + t - 1) / t, c = ((square ? w.np : w.mp) + t - 1) / t;
         return square ? r * (r + 1) / 2 : r * c;
@@ -656,8 +718,9 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
     const dim3 sgrid((tall ? w.np : w.mp) / 64, (tall ? w.mp : w.np) / 64, batch);
     auto begin = [&](auto BF, auto MOM) {
         constexpr bool bf = decltype(BF)::value, mo = decltype(MOM)::value;
-        norm_kernel<bf, mo><<<ngrid, kNormThreads, 0, stream>>>(src, size, w.parts, w.norm);
-        start_kernel<bf, mo><<<sgrid, 256, 0, stream>>>(src, rows, cols, eps, w);
+        norm_kernel<bf, mo><<<ngrid, kNormThreads, 0, stream>>>(src, size, norm_per_part(rows, cols), w.parts,
+                                                               vector_rows(src, size % 4 == 0 ? 4 : 1), w.norm);
+        start_kernel<bf, mo><<<sgrid, 256, 0, stream>>>(src, rows, cols, vector_rows(src, cols), eps, w);
     };
     if (bf16 && momentum) begin(std::true_type{}, std::true_type{});
     else if (bf16) begin(std::true_type{}, std::false_type{});
@@ -670,34 +733,35 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
     const int a256 = t256 * ((w.mp + kBN - 1) / kBN), a128 = t128 * (w.mp / kT);
     const int apply_tiles = wide_tiles(a256, a128, batch) ? a256 : a128;
     int from = 0, traces = 1;
-    auto sym = [&](int which, uint16_t* A, uint16_t* B, uint16_t* D) {
-        q.sym = which;
+    auto set = [&](uint16_t* A, uint16_t* B, uint16_t* D, int second, int parts) {
         q.A = A;
         q.B = B;
         q.D = D;
-        q.traces = sym_tiles;
-        launch_product<kSym>(q, stream);
+        q.second = second;
+        q.traces = parts;
     };
     for (int i = 0; i < steps;) {
         q.pair = (i == 0 && steps >= 4) || i == steps - 2;
         for (int h = 0; h < 2; ++h)
             for (int j = 0; j < 3; ++j) q.coef[h][j] = sc.v[q.pair ? i + h : i][j];
-        q.A = q.B = w.xh;
-        q.D = w.sq[0];
-        q.traces = traces;
+        uint16_t *s0 = w.sq[0], *s1 = w.sq[1], *s2 = w.sq[2];
+        set(w.xh, w.xh, s0, 0, traces);
         launch_product<kGram>(q, stream);                          // D
-        sym(kSymFirst, w.sq[0], w.sq[0], w.sq[1]);                   // R
-        uint16_t* Q = w.sq[1];
+        set(s0, s0, s1, 0, 0);
+        launch_product<kSym1>(q, stream);                          // R
+        uint16_t* Q = s1;
         if (q.pair) {
-            sym(kSymMix, w.sq[1], w.sq[0], w.sq[2]);                  // T
-            sym(kSymNext, w.sq[2], w.sq[1], w.sq[0]);                 // D'
-            sym(kSymSecond, w.sq[0], w.sq[0], w.sq[2]);               // R'
-            sym(kSymJoin, w.sq[1], w.sq[2], w.sq[0]);                 // Q
-            Q = w.sq[0];
+            set(s1, s0, s2, 0, 0);
+            launch_product<kMix>(q, stream);                       // T
+            set(s2, s1, s0, 0, sym_tiles);
+            launch_product<kSym2>(q, stream);                      // D'
+            set(s0, s0, s2, 1, 0);
+            launch_product<kSym1>(q, stream);                      // R'
+            set(s1, s2, s0, 1, 0);
+            launch_product<kSym2>(q, stream);                      // Q
+            Q = s0;
         }
-        q.A = Q;
-        q.B = w.xt[from];
-        q.D = w.xt[from ^ 1];
+        set(Q, w.xt[from], w.xt[from ^ 1], 0, 0);
         i += q.pair ? 2 : 1;
         if (i < steps) launch_product<kApply>(q, stream);
         else launch_product<kFinal>(q, stream);
