@@ -37,10 +37,13 @@
 // Matrices of at most 128 rows or columns take the Gram form (orth_gram.hip).
 #include "orth_device.hpp"
 
+#include <algorithm>
+
 namespace cap {
 namespace {
 
 constexpr int kPad = 128;                  // n and m in the workspace are multiples of this
+constexpr int kT = 128;                    // the smaller tile
 constexpr int kNormThreads = 256;
 constexpr int kMaxNormParts = 256;
 // Up to this many rows (or columns) the Gram form (orth_gram.hip) is taken.
@@ -53,6 +56,7 @@ struct OrthWs {
     float* norm;                           // [batch][parts] sums of squares of U
     float* trace;                          // [batch][trace_cap] parts of the next trace
     float* center;                         // [batch][2] s of the group's first and second step
+    f32x4* sums;                           // parts of Gram tiles
     int n, m, np, mp;                      // sides, and as padded with zeros
     int xp, sp;                            // row pitch of X, and of X^T and the n x n matrices
     int parts, trace_cap;
@@ -75,6 +79,44 @@ size_t norm_per_part(int rows, int cols) {
 int norm_parts(int rows, int cols) {
     const size_t per = norm_per_part(rows, cols);
     return static_cast<int>((static_cast<size_t>(rows) * cols + per - 1) / per);
+}
+
+// How a product runs: tiles of 256 x 256 (one workgroup a CU) or 128 x 128 (two), and
+// for the Gram product which of its tiles are computed in parts along K.
+struct ProductPlan {
+    int side, tiles;                       // of one matrix
+    int whole, split;                      // tiles of all matrices computed whole; parts of each of the others
+    size_t sums;                           // bytes of the parts' sums
+};
+ProductPlan plan_product(bool square, bool gram, int np, int mp, int batch) {
+    const int cus = device_cu_count();
+    auto count = [&](int t) {
+        const int r = (np + t - 1) / t, c = ((square ? np : mp) + t - 1) / t;
+        return square ? r * (r + 1) / 2 : r * c;
+    };
+    auto rounds = [&](long long tiles, int slots) { return (tiles * batch + slots - 1) / slots; };
+    ProductPlan p{};
+    const bool wide = rounds(count(kBM), cus) * 24 <= rounds(count(kT), 2 * cus) * 16;
+    p.side = wide ? kBM : kT;
+    p.tiles = count(p.side);
+    const long long total = static_cast<long long>(p.tiles) * batch;
+    p.whole = static_cast<int>(total);
+    p.split = 1;
+    if (gram) {
+        const int slots = wide ? cus : 2 * cus;
+        const int rest = static_cast<int>(total % slots), KT = mp / kStageK;
+        const int split = rest ? std::min(std::min(slots / rest, 16), KT / 4) : 1;
+        const size_t bytes = static_cast<size_t>(p.side) * p.side * 4;
+        // stages saved (about 1.4 us each) against the sums' way out and in at 4 MB / us and a launch
+        const double saved = 1.4 * KT * (1.0 - 1.0 / split);
+        const double cost = 5.0 + 2.0 * rest * split * bytes / 4e6;
+        if (split > 1 && saved > cost) {
+            p.whole = static_cast<int>(total - rest);
+            p.split = split;
+            p.sums = rest * split * bytes;
+        }
+    }
+    return p;
 }
 
 size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
@@ -100,7 +142,9 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
     const size_t cap = (np / 128) * (mp / 128);
     char* t = take(static_cast<size_t>(batch) * cap * 4);
     char* c = take(static_cast<size_t>(batch) * 8);
+    char* sums = take(plan_product(true, true, static_cast<int>(np), static_cast<int>(mp), batch).sums);
     if (w) {
+        w->sums = reinterpret_cast<f32x4*>(sums);
         w->xh = reinterpret_cast<uint16_t*>(v[0]);
         w->xl = reinterpret_cast<uint16_t*>(v[1]);
         for (int i = 0; i < 2; ++i) w->xt[i] = reinterpret_cast<uint16_t*>(v[2 + i]);
@@ -249,6 +293,7 @@ struct ProductArgs {
     int second, pair;                      // kSym1: of the second step; kSym2: Q; the group has two steps
     int traces;                            // kGram, kSym2 (D'): parts of the trace
     float coef[2][3];                      // of the group's steps
+    int whole, split;                      // kGram: tiles (of all matrices) computed whole, parts of each of the others
     uint16_t* out;
     int rows, cols, batch;
 };
@@ -334,47 +379,53 @@ __device__ __forceinline__ global_u32x4* lane_ptr(const void* base, uint32_t off
     return reinterpret_cast<global_u32x4*>(reinterpret_cast<global_char*>(reinterpret_cast<uint64_t>(uniform_ptr(base))) + off);
 }
 
-// Results of a wave's 64 x 16 NJ block at (row0, col0) of the matrix.  Lane (r, g)
-// holds columns 4 g .. + 3 of each 16 x 16 block, of row paired_row.  Two adjacent
-// blocks trade halves (permlane16_swap), so that a lane reads and writes 8 consecutive
-// columns: columns 8 (g / 2) .. of block g % 2.  They go out in steps of two row blocks
-// and two column blocks; what a step adds to (A and B, or X and its error) is loaded
-// kAhead steps before, since the loads' way is as long as several steps.  The steps are
-// kept apart (sched_barrier): mixed, they need more registers than there are.
+// Results leave a wave in steps of 32 x 32 values: two row blocks and two column
+// blocks, at (row0, col0) of the matrix.  Lane (r, g) holds columns 4 g .. + 3 of each 16
+// x 16 block, of row paired_row.  Two adjacent blocks trade halves (permlane16_swap), so
+// that a lane reads and writes 8 consecutive columns: columns 8 (g / 2) .. of block g % 2.
 // Addresses are a scalar base for the step and a 32-bit lane offset.
-template <Product MODE, int NJ>
-__device__ __forceinline__ float store_wave(const ProductArgs& q, const Scalars& c, f32x4 (&acc)[4][NJ], int batch, int row0,
-                                            int col0, bool mirror, int lane) {
-    const OrthWs& w = q.w;
-    const int r = lane & 15, g = lane >> 4;
-    constexpr bool kSquare = is_square(MODE);
-    constexpr int kIn = MODE == kGram ? 0 : MODE == kSym1 ? 1 : 2;     // matrices the results add to
-    constexpr int kSteps = NJ, kAhead = 2;
-    const int pitch = kSquare ? w.sp : w.xp;
-    const size_t at0 = (static_cast<size_t>(batch) * w.np + row0) * pitch + col0;
-    const size_t t0 = (static_cast<size_t>(batch) * (kSquare ? w.np : w.mp) + col0) * w.sp + row0;
-    const uint32_t lane_at = 2u * ((8 * (r >> 2) + (r & 3)) * pitch + 16 * (g & 1) + 8 * (g >> 1));
-    const uint32_t lane_t = 2u * ((4 * g + (r & 3)) * w.sp + 8 * (r >> 2));
-    auto step_of = [&](const uint16_t* p, int x, int ii) __attribute__((always_inline)) {
-        const int ip = x / (NJ / 2), pr = x % (NJ / 2);
-        return lane_ptr(p + at0 + static_cast<size_t>(32 * ip + 4 * ii) * pitch + 32 * pr, lane_at);
-    };
-    auto put = [&](uint16_t* p, int x, int ii, const u32x4& v) __attribute__((always_inline)) {
-        *step_of(p, x, ii) = v;
-    };
+template <Product MODE>
+struct Out {
+    static constexpr bool kSquare = is_square(MODE);
+    static constexpr int kIn = MODE == kGram ? 0 : MODE == kSym1 ? 1 : 2;     // matrices the results add to
+    const ProductArgs& q;
+    const Scalars& c;
+    int batch, lane, pitch;
+    bool mirror;
+    uint32_t lane_at, lane_t;
+    const uint16_t *p0, *p1;
+
+    __device__ __forceinline__ Out(const ProductArgs& q_, const Scalars& c_, int batch_, bool mirror_, int lane_)
+        : q(q_), c(c_), batch(batch_), lane(lane_), pitch(kSquare ? q_.w.sp : q_.w.xp), mirror(mirror_) {
+        const int r = lane & 15, g = lane >> 4;
+        lane_at = 2u * ((8 * (r >> 2) + (r & 3)) * pitch + 16 * (g & 1) + 8 * (g >> 1));
+        lane_t = 2u * ((4 * g + (r & 3)) * q.w.sp + 8 * (r >> 2));
+        p0 = kSquare ? q.A : q.w.xh;
+        p1 = kSquare ? q.B : q.w.xl;
+    }
+    __device__ __forceinline__ global_u32x4* at(const uint16_t* p, int row0, int col0, int ii) const {
+        return lane_ptr(p + (static_cast<size_t>(batch) * q.w.np + row0 + 4 * ii) * pitch + col0, lane_at);
+    }
+    __device__ __forceinline__ void fetch(u32x4 (&in)[2][2], int row0, int col0) const {
+#pragma unroll
+        for (int ii = 0; ii < 2; ++ii) {
+            if constexpr (kIn > 0) in[ii][0] = *at(p0, row0, col0, ii);
+            if constexpr (kIn > 1) in[ii][1] = *at(p1, row0, col0, ii);
+        }
+    }
     // 8 consecutive columns of a row <-> the lane's halves of two blocks
-    auto halves = [](const u32x4& v, u32x2& x, u32x2& y) __attribute__((always_inline)) {
+    static __device__ __forceinline__ void halves(const u32x4& v, u32x2& x, u32x2& y) {
         const auto s0 = __builtin_amdgcn_permlane16_swap(v[0], v[2], false, false);
         const auto s1 = __builtin_amdgcn_permlane16_swap(v[1], v[3], false, false);
         x = u32x2{s0[0], s1[0]};
         y = u32x2{s0[1], s1[1]};
-    };
-    auto join = [](const u32x2& x, const u32x2& y) __attribute__((always_inline)) {
+    }
+    static __device__ __forceinline__ u32x4 join(const u32x2& x, const u32x2& y) {
         const auto s0 = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false);
         const auto s1 = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
         return u32x4{s0[0], s1[0], s0[1], s1[1]};
-    };
-    auto bf16_out = [&](int row, int col, const u32x4& y) __attribute__((always_inline)) {
+    }
+    __device__ __forceinline__ void bf16_out(int row, int col, const u32x4& y) const {
         if (row >= q.rows) return;
         uint16_t* o = q.out + (static_cast<size_t>(batch) * q.rows + row) * q.cols + col;
         if (col + 7 < q.cols && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
@@ -384,36 +435,25 @@ __device__ __forceinline__ float store_wave(const ProductArgs& q, const Scalars&
             for (int e = 0; e < 8; ++e)
                 if (col + e < q.cols) o[e] = static_cast<uint16_t>(y[e >> 1] >> (16 * (e & 1)));
         }
-    };
-    const uint16_t* const p0 = kSquare ? q.A : w.xh;
-    const uint16_t* const p1 = kSquare ? q.B : w.xl;
-    u32x4 in[kAhead + 1][2][2];
-    auto fetch = [&](auto X) __attribute__((always_inline)) {
-        constexpr int x = decltype(X)::value;
+    }
+
+    // One step: acc[row block][column block], what fetch() brought; returns its part of
+    // a trace.
+    __device__ __forceinline__ float store(const f32x4 (&acc)[2][2], const u32x4 (&in)[2][2], int row0, int col0) const {
+        const int r = lane & 15, g = lane >> 4;
+        float sum = 0.0f;
+        u32x2 t[2][2];                                             // transposed
 #pragma unroll
         for (int ii = 0; ii < 2; ++ii) {
-            if constexpr (kIn > 0) in[x % (kAhead + 1)][ii][0] = *step_of(p0, x, ii);
-            if constexpr (kIn > 1) in[x % (kAhead + 1)][ii][1] = *step_of(p1, x, ii);
-        }
-    };
-    float sum = 0.0f;
-    static_for<kAhead>([&](auto X) { fetch(X); });
-    __builtin_amdgcn_sched_barrier(0);
-    static_for<kSteps>([&](auto X) __attribute__((always_inline)) {
-        constexpr int x = decltype(X)::value, ip = x / (NJ / 2), pr = x % (NJ / 2);
-        if constexpr (x + kAhead < kSteps) fetch(std::integral_constant<int, x + kAhead>{});
-        u32x2 t[2][2];                                             // [row block][column block], transposed
-#pragma unroll
-        for (int ii = 0; ii < 2; ++ii) {
-            const int row = row0 + 32 * ip + 8 * (r >> 2) + 4 * ii + (r & 3);
+            const int row = row0 + 8 * (r >> 2) + 4 * ii + (r & 3);
             float v[2][4];
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[b][e] = acc[2 * ip + ii][2 * pr + b][e];
+                for (int e = 0; e < 4; ++e) v[b][e] = acc[ii][b][e];
             u32x2 hi[2], lo[2], i0[2], i1[2];
-            if constexpr (kIn > 0) halves(in[x % (kAhead + 1)][ii][0], i0[0], i0[1]);
-            if constexpr (kIn > 1) halves(in[x % (kAhead + 1)][ii][1], i1[0], i1[1]);
+            if constexpr (kIn > 0) halves(in[ii][0], i0[0], i0[1]);
+            if constexpr (kIn > 1) halves(in[ii][1], i1[0], i1[1]);
             if constexpr (kSquare) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
@@ -426,10 +466,10 @@ __device__ __forceinline__ float store_wave(const ProductArgs& q, const Scalars&
                         v[b][e] = y;
                     }
                     if (!mirror) {                                 // a tile on the diagonal
-                        const int d = row - (col0 + 32 * pr + 16 * b + 4 * g);
+                        const int d = row - (col0 + 16 * b + 4 * g);
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (d == e && row < w.n) {
+                            if (d == e && row < q.w.n) {
                                 // tr(T P): T = T' + ps I, P = R + p I
                                 if constexpr (MODE == kMix)
                                     sum += __builtin_fmaf(c.ps, f16_at(i0[b], e), c.p * (v[b][e] + c.ps));
@@ -438,14 +478,14 @@ __device__ __forceinline__ float store_wave(const ProductArgs& q, const Scalars&
                     }
                     hi[b] = u32x2{pack_f16x2(v[b][0], v[b][1]), pack_f16x2(v[b][2], v[b][3])};
                 }
-                put(q.D, x, ii, join(hi[0], hi[1]));
+                *at(q.D, row0, col0, ii) = join(hi[0], hi[1]);
             } else {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float xv = __builtin_fmaf(f16_at(i1[b], e), 1.0f / kLoScale, f16_at(i0[b], e));
-                        v[b][e] = __builtin_fmaf(c.a, xv, v[b][e]);
+                        const float x = __builtin_fmaf(f16_at(i1[b], e), 1.0f / kLoScale, f16_at(i0[b], e));
+                        v[b][e] = __builtin_fmaf(c.a, x, v[b][e]);
                     }
                     if constexpr (MODE == kApply) {
                         split4(v[b], hi[b], lo[b]);
@@ -456,10 +496,10 @@ __device__ __forceinline__ float store_wave(const ProductArgs& q, const Scalars&
                     }
                 }
                 if constexpr (MODE == kApply) {
-                    put(w.xh, x, ii, join(hi[0], hi[1]));
-                    put(w.xl, x, ii, join(lo[0], lo[1]));
+                    *at(q.w.xh, row0, col0, ii) = join(hi[0], hi[1]);
+                    *at(q.w.xl, row0, col0, ii) = join(lo[0], lo[1]);
                 } else if (q.rows <= q.cols) {
-                    bf16_out(row, col0 + 32 * pr + 16 * (g & 1) + 8 * (g >> 1), join(hi[0], hi[1]));
+                    bf16_out(row, col0 + 16 * (g & 1) + 8 * (g >> 1), join(hi[0], hi[1]));
                 }
             }
 #pragma unroll
@@ -470,15 +510,51 @@ __device__ __forceinline__ float store_wave(const ProductArgs& q, const Scalars&
         for (int b = 0; b < 2; ++b) {
             const u32x4 y = {t[0][b][0], t[0][b][1], t[1][b][0], t[1][b][1]};
             if constexpr (MODE == kFinal) {
-                if (q.rows > q.cols)
-                    bf16_out(col0 + 32 * pr + 16 * b + 4 * g + (r & 3), row0 + 32 * ip + 8 * (r >> 2), y);
+                if (q.rows > q.cols) bf16_out(col0 + 16 * b + 4 * g + (r & 3), row0 + 8 * (r >> 2), y);
             } else if (MODE == kApply || mirror) {
-                *lane_ptr(q.D + t0 + static_cast<size_t>(32 * pr + 16 * b) * w.sp + 32 * ip, lane_t) = y;
+                const size_t rows = kSquare ? q.w.np : q.w.mp;
+                *lane_ptr(q.D + (batch * rows + col0 + 16 * b) * q.w.sp + row0, lane_t) = y;
             }
         }
+        return sum;
+    }
+};
+
+// All results of a wave's 64 x 16 NJ block.  What a step adds to is loaded kAhead steps
+// before, since the loads' way is as long as several steps.  The steps are kept apart
+// (sched_barrier): mixed, they need more registers than there are.
+template <Product MODE, int NJ>
+__device__ __forceinline__ float store_wave(const ProductArgs& q, const Scalars& c, f32x4 (&acc)[4][NJ], int batch, int row0,
+                                            int col0, bool mirror, int lane) {
+    constexpr int kSteps = NJ, kAhead = 2;
+    const Out<MODE> out(q, c, batch, mirror, lane);
+    u32x4 in[kAhead + 1][2][2];
+    auto fetch = [&](auto X) __attribute__((always_inline)) {
+        constexpr int x = decltype(X)::value;
+        out.fetch(in[x % (kAhead + 1)], row0 + 32 * (x / (NJ / 2)), col0 + 32 * (x % (NJ / 2)));
+    };
+    float sum = 0.0f;
+    static_for<kAhead>([&](auto X) { fetch(X); });
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<kSteps>([&](auto X) __attribute__((always_inline)) {
+        constexpr int x = decltype(X)::value, ip = x / (NJ / 2), pr = x % (NJ / 2);
+        if constexpr (x + kAhead < kSteps) fetch(std::integral_constant<int, x + kAhead>{});
+        const f32x4 v[2][2] = {{acc[2 * ip][2 * pr], acc[2 * ip][2 * pr + 1]},
+                               {acc[2 * ip + 1][2 * pr], acc[2 * ip + 1][2 * pr + 1]}};
+        sum += out.store(v, in[x % (kAhead + 1)], row0 + 32 * ip, col0 + 32 * pr);
         __builtin_amdgcn_sched_barrier(0);
     });
     return sum;
+}
+
+// The fp32 sums of a part of a product, as a wave holds them: [step][block][lane].
+template <int NJ>
+__device__ __forceinline__ void store_sums(f32x4* dst, const f32x4 (&acc)[4][NJ], int lane) {
+    static_for<NJ>([&](auto X) __attribute__((always_inline)) {
+        constexpr int x = decltype(X)::value, ip = x / (NJ / 2), pr = x % (NJ / 2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dst[(4 * x + e) * kWave + lane] = acc[2 * ip + e / 2][2 * pr + e % 2];
+    });
 }
 
 // This tile's part of a trace (off the diagonal it stands for two tiles).
@@ -496,6 +572,27 @@ __device__ __forceinline__ void store_part(const ProductArgs& q, int batch, int 
     }
 }
 
+// The u-th unit of a product's tiles (of all matrices, the matrix outermost): whole
+// tiles, then parts along K of the rest.  Parts are runs of an even number of stages.
+struct Unit {
+    int tile, part;                        // part -1: whole
+    int kt0, kt1;                          // stages
+};
+template <Product MODE>
+__device__ __forceinline__ Unit unit_of(const ProductArgs& q, int u, int KT) {
+    Unit x{u, -1, 0, KT};
+    if constexpr (MODE == kGram) {
+        if (u >= q.whole) {
+            const int v = u - q.whole, t = v / q.split, p = v - t * q.split;
+            x.tile = q.whole + t;
+            x.part = v;
+            x.kt0 = (KT / 2) * p / q.split * 2;
+            x.kt1 = (KT / 2) * (p + 1) / q.split * 2;
+        }
+    }
+    return x;
+}
+
 template <Product MODE>
 __device__ __forceinline__ void decode_tile(const ProductArgs& q, int t, int tile_rows, int& ti, int& tj) {
     if constexpr (is_square(MODE)) {
@@ -508,30 +605,30 @@ __device__ __forceinline__ void decode_tile(const ProductArgs& q, int t, int til
 }
 
 // ---- tiles of 128 x 128: four waves of 64 x 64, two workgroups a CU
-constexpr int kT = 128;
 constexpr int kThreads = 256;
 constexpr int kTileStageB = 2 * kT * kRowB;
 
 template <Product MODE>
-__global__ __launch_bounds__(kThreads, 2) void product128_kernel(ProductArgs q) {
+__global__ __launch_bounds__(kThreads, 2) void product128_kernel(ProductArgs q, int tiles) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kTileStageB];
     __shared__ float red[kThreads / kWave];
     const OrthWs& w = q.w;
     const int lane = threadIdx.x % kWave;
     const int wave = static_cast<int>(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
     const int wm = wave >> 1, wn = wave & 1;
-    const int batch = blockIdx.y;
-    int ti, tj;
-    decode_tile<MODE>(q, blockIdx.x, kT, ti, tj);
     const int K = MODE == kGram ? w.mp : w.np, ld = MODE == kGram ? w.xp : w.sp;
+    const Unit u = unit_of<MODE>(q, blockIdx.x, K / kStageK);
+    const int batch = u.tile / tiles, t = u.tile - batch * tiles;
+    int ti, tj;
+    decode_tile<MODE>(q, t, kT, ti, tj);
     const uint16_t* A = q.A + static_cast<size_t>(batch) * w.np * ld;
     const uint16_t* B = q.B + static_cast<size_t>(batch) * (is_square(MODE) ? w.np : w.mp) * ld;
     const uint32_t pitch = static_cast<uint32_t>(ld) * 2u;
     const LaneMap lm = lane_map(lane);
     const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
     // wave w brings rows 32 w .. + 31 of both operands, eight at a time
-    const char* pa = reinterpret_cast<const char*>(A + (static_cast<size_t>(ti) * kT + wave * 32) * ld);
-    const char* pb = reinterpret_cast<const char*>(B + (static_cast<size_t>(tj) * kT + wave * 32) * ld);
+    const char* pa = reinterpret_cast<const char*>(A + (static_cast<size_t>(ti) * kT + wave * 32) * ld + u.kt0 * kStageK);
+    const char* pb = reinterpret_cast<const char*>(B + (static_cast<size_t>(tj) * kT + wave * 32) * ld + u.kt0 * kStageK);
     uint32_t a_off[4], b_off[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -552,7 +649,7 @@ __global__ __launch_bounds__(kThreads, 2) void product128_kernel(ProductArgs q) 
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
-    const int KT = K / kStageK;
+    const int KT = u.kt1 - u.kt0;
     const int pc[2] = {(lm.fr_kc ^ lm.fr_swz) << 4, ((lm.fr_kc ^ lm.fr_swz) << 4) ^ 64};
     issue(0);
     for (int kt = 0; kt < KT; ++kt) {
@@ -577,15 +674,19 @@ __global__ __launch_bounds__(kThreads, 2) void product128_kernel(ProductArgs q) 
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j], a[i], acc[i][j], 0, 0, 0);
         }
     }
-    const Scalars c = scalars<MODE, kThreads>(q, batch, blockIdx.x == 0, red);
+    if (MODE == kGram && u.part >= 0) {
+        store_sums<4>(q.w.sums + (static_cast<size_t>(u.part) * 4 + wave) * 16 * kWave, acc, lane);
+        return;
+    }
+    const Scalars c = scalars<MODE, kThreads>(q, batch, t == 0, red);
     const float sum = store_wave<MODE, 4>(q, c, acc, batch, ti * kT + wm * 64, tj * kT + wn * 64, ti != tj, lane);
     if constexpr (MODE == kApply || MODE == kMix)
-        store_part<kThreads>(q, batch, blockIdx.x, MODE == kMix && ti != tj ? 2.0f * sum : sum, red);
+        store_part<kThreads>(q, batch, t, MODE == kMix && ti != tj ? 2.0f * sum : sum, red);
 }
 
 // ---- tiles of 256 x 256: the K loop of mfma_tile.hpp, persistent, one workgroup a CU
 template <Product MODE>
-__global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs q, int tiles) {
+__global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs q, int tiles, int units) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * kStageBytes];
     __shared__ float red[kNW];
     const OrthWs& w = q.w;
@@ -597,15 +698,17 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
     const uint32_t a_lds = lds_base + wave * kALd * 1024;
     const uint32_t b_lds = lds_base + (kBM + (wave >> 1) * kWN + (wave & 1) * 16) * kRowB;
     const int KT = (MODE == kGram ? w.mp : w.np) / kStageK, lead = MODE == kGram ? w.xp : w.sp;
-    const int total = tiles * q.batch;
     // block b runs on XCD b % 8: each XCD gets a run of tiles, mostly of one matrix
     const int G = gridDim.x;
     int tile = G % 8 == 0 ? (blockIdx.x % 8) * (G / 8) + blockIdx.x / 8 : blockIdx.x;
-    int batch = 0, t = 0, ti = 0, tj = 0;
+    int batch = 0, t = 0, ti = 0, tj = 0, part = -1, stages = KT;
     Loads ld;
     auto start_tile = [&](int x) __attribute__((always_inline)) {
-        batch = __builtin_amdgcn_readfirstlane(x / tiles);
-        t = x - batch * tiles;
+        const Unit u = unit_of<MODE>(q, x, KT);
+        part = __builtin_amdgcn_readfirstlane(u.part);
+        stages = __builtin_amdgcn_readfirstlane(u.kt1 - u.kt0);
+        batch = __builtin_amdgcn_readfirstlane(u.tile / tiles);
+        t = __builtin_amdgcn_readfirstlane(u.tile) - batch * tiles;
         decode_tile<MODE>(q, t, kBM, ti, tj);
         ti = __builtin_amdgcn_readfirstlane(ti);
         tj = __builtin_amdgcn_readfirstlane(tj);
@@ -615,9 +718,10 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
         const size_t b_rows = is_square(MODE) ? w.np : w.mp;
         const uint16_t* A = q.A + (static_cast<size_t>(batch) * w.np + static_cast<size_t>(ti) * kBM) * lead;
         const uint16_t* B = q.B + (batch * b_rows + static_cast<size_t>(tj) * kBN + (wave >> 1) * kWN + (wave & 1) * 16) * lead;
-        ld.a = reinterpret_cast<const char*>(A);
+        const int k0 = MODE == kGram ? u.kt0 * kStageK : 0;
+        ld.a = reinterpret_cast<const char*>(A + k0);
         ld.a_on = ti * kBM + wave / kWavesN * kWM < w.np;
-        ld.b0 = reinterpret_cast<const char*>(B);
+        ld.b0 = reinterpret_cast<const char*>(B + k0);
         ld.b1 = ld.b0 + static_cast<size_t>(32) * pitch;
         ld.c0 = ld.b0 + static_cast<size_t>(64) * pitch;
         ld.c1 = ld.b0 + static_cast<size_t>(96) * pitch;
@@ -631,8 +735,8 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
         load_half0(ld, ld.a_on, a_lds, b_lds, 0);
         load_half1(ld, b_lds, 0);
     };
-    if (tile < total) start_tile(tile);
-    while (tile < total) {
+    if (tile < units) start_tile(tile);
+    while (tile < units) {
         f32x4 acc[kMI][kNJ];
 #pragma unroll
         for (int i = 0; i < kMI; ++i)
@@ -640,17 +744,22 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
             for (int j = 0; j < kNJ; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
-        const int cb = batch, ct = t, ci = ti, cj = tj;
+        const int cb = batch, ct = t, ci = ti, cj = tj, cp = part, ck = MODE == kGram ? stages : KT;
         const int next = tile + G;
         // in the last stage buffer 0 is free: the next tile's stage 0 lands during the
         // rest of that stage and the results' way out
         auto hook = [&](auto step) {
             if constexpr (decltype(step)::value == kLast) {
-                if (next < total) start_tile(next);
+                if (next < units) start_tile(next);
             }
         };
         const bool active = ci * kBM + wm * kWM < w.np;
-        run_k_loop<f16x8>(KT, lds, wm, wn, lane, loader, active, acc, ld, a_lds, b_lds, hook, hook);
+        run_k_loop<f16x8>(ck, lds, wm, wn, lane, loader, active, acc, ld, a_lds, b_lds, hook, hook);
+        if (MODE == kGram && cp >= 0) {
+            store_sums<kNJ>(q.w.sums + (static_cast<size_t>(cp) * kNW + wave) * 32 * kWave, acc, lane);
+            tile = next;
+            continue;
+        }
         const Scalars c = scalars<MODE, kNW * kWave>(q, cb, ct == 0, red);
         float sum = 0.0f;
         if (active && cj * kBN + wn * kWN < (is_square(MODE) ? w.np : w.mp))
@@ -662,29 +771,47 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
-// Which tiles a product runs on: 256 x 256 (one workgroup a CU) or 128 x 128 (two).
-bool wide_tiles(int big, int small, int batch) {
-    const long long cus = device_cu_count();
-    const long long rounds256 = (static_cast<long long>(big) * batch + cus - 1) / cus;
-    const long long rounds128 = (static_cast<long long>(small) * batch + 2 * cus - 1) / (2 * cus);
-    return rounds256 * 24 <= rounds128 * 16;
+// Joins the parts of the Gram tiles computed in parts: one wave for a step of a wave of
+// the tile.
+template <int NJ>
+__global__ __launch_bounds__(kWave) void gram_join_kernel(ProductArgs q, int tiles) {
+    constexpr int kWavesTile = NJ == 8 ? kNW : 4, kSide = NJ == 8 ? kBM : kT, kAcross = 2;
+    __shared__ float red[1];
+    const int lane = threadIdx.x;
+    const int wave = blockIdx.x / NJ, x = blockIdx.x % NJ;
+    const int tile = q.whole + blockIdx.y, batch = tile / tiles, t = tile - batch * tiles;
+    int ti, tj;
+    triangle(t, ti, tj);
+    const int row0 = ti * kSide + wave / kAcross * 64 + 32 * (x / (NJ / 2));
+    const int col0 = tj * kSide + wave % kAcross * 16 * NJ + 32 * (x % (NJ / 2));
+    const Scalars c = scalars<kGram, kWave>(q, batch, t == 0 && blockIdx.x == 0, red);
+    if (row0 >= q.w.np || col0 >= q.w.np) return;
+    f32x4 acc[2][2] = {};
+    const f32x4* p = q.w.sums + (static_cast<size_t>(blockIdx.y) * q.split * kWavesTile + wave) * 4 * NJ * kWave + 4 * x * kWave + lane;
+#pragma unroll 4
+    for (int i = 0; i < q.split; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e / 2][e % 2] += p[e * kWave];
+        p += static_cast<size_t>(kWavesTile) * 4 * NJ * kWave;
+    }
+    const Out<kGram> out(q, c, batch, ti != tj, lane);
+    const u32x4 none[2][2] = {};
+    out.store(acc, none, row0, col0);
 }
 
 template <Product MODE>
-void launch_product(const ProductArgs& q, hipStream_t stream) {
-    const OrthWs& w = q.w;
-    constexpr bool square = is_square(MODE);
-    auto tiles = [&](int t) {
-        const int r = (w.np + t - 1) / t, c = ((square ? w.np : w.mp) + t - 1) / t;
-        return square ? r * (r + 1) / 2 : r * c;
-    };
-    const int big = tiles(kBM);
-    if (wide_tiles(big, tiles(kT), q.batch)) {
-        const long long total = static_cast<long long>(big) * q.batch;
+void launch_product(const ProductArgs& args, const ProductPlan& p, hipStream_t stream) {
+    ProductArgs q = args;
+    q.whole = p.whole;
+    q.split = p.split;
+    const int rest = p.tiles * q.batch - p.whole, units = p.whole + rest * p.split;
+    if (p.side == kBM) {
         const int cus = device_cu_count();
-        product256_kernel<MODE><<<total < cus ? static_cast<int>(total) : cus, kNW * kWave, 0, stream>>>(q, big);
+        product256_kernel<MODE><<<units < cus ? units : cus, kNW * kWave, 0, stream>>>(q, p.tiles, units);
+        if (rest) gram_join_kernel<8><<<dim3(kNW * 8, rest), kWave, 0, stream>>>(q, p.tiles);
     } else {
-        product128_kernel<MODE><<<dim3(tiles(kT), q.batch), kThreads, 0, stream>>>(q);
+        product128_kernel<MODE><<<units, kThreads, 0, stream>>>(q, p.tiles);
+        if (rest) gram_join_kernel<4><<<dim3(4 * 4, rest), kWave, 0, stream>>>(q, p.tiles);
     }
 }
 
@@ -727,11 +854,8 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
     else if (momentum) begin(std::false_type{}, std::true_type{});
     else begin(std::false_type{}, std::false_type{});
     CAP_LAUNCH_CHECK();
-    auto tri_tiles = [&](int side) { return side * (side + 1) / 2; };
-    const int t256 = (w.np + kBM - 1) / kBM, t128 = w.np / kT;
-    const int sym_tiles = wide_tiles(tri_tiles(t256), tri_tiles(t128), batch) ? tri_tiles(t256) : tri_tiles(t128);
-    const int a256 = t256 * ((w.mp + kBN - 1) / kBN), a128 = t128 * (w.mp / kT);
-    const int apply_tiles = wide_tiles(a256, a128, batch) ? a256 : a128;
+    const ProductPlan gram = plan_product(true, true, w.np, w.mp, batch), sym = plan_product(true, false, w.np, w.mp, batch),
+                      apply = plan_product(false, false, w.np, w.mp, batch);
     int from = 0, traces = 1;
     auto set = [&](uint16_t* A, uint16_t* B, uint16_t* D, int second, int parts) {
         q.A = A;
@@ -746,27 +870,27 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
             for (int j = 0; j < 3; ++j) q.coef[h][j] = sc.v[q.pair ? i + h : i][j];
         uint16_t *s0 = w.sq[0], *s1 = w.sq[1], *s2 = w.sq[2];
         set(w.xh, w.xh, s0, 0, traces);
-        launch_product<kGram>(q, stream);                          // D
+        launch_product<kGram>(q, gram, stream);                          // D
         set(s0, s0, s1, 0, 0);
-        launch_product<kSym1>(q, stream);                          // R
+        launch_product<kSym1>(q, sym, stream);                          // R
         uint16_t* Q = s1;
         if (q.pair) {
             set(s1, s0, s2, 0, 0);
-            launch_product<kMix>(q, stream);                       // T
-            set(s2, s1, s0, 0, sym_tiles);
-            launch_product<kSym2>(q, stream);                      // D'
+            launch_product<kMix>(q, sym, stream);                       // T
+            set(s2, s1, s0, 0, sym.tiles);
+            launch_product<kSym2>(q, sym, stream);                      // D'
             set(s0, s0, s2, 1, 0);
-            launch_product<kSym1>(q, stream);                      // R'
+            launch_product<kSym1>(q, sym, stream);                      // R'
             set(s1, s2, s0, 1, 0);
-            launch_product<kSym2>(q, stream);                      // Q
+            launch_product<kSym2>(q, sym, stream);                      // Q
             Q = s0;
         }
         set(Q, w.xt[from], w.xt[from ^ 1], 0, 0);
         i += q.pair ? 2 : 1;
-        if (i < steps) launch_product<kApply>(q, stream);
-        else launch_product<kFinal>(q, stream);
+        if (i < steps) launch_product<kApply>(q, apply, stream);
+        else launch_product<kFinal>(q, apply, stream);
         from ^= 1;
-        traces = apply_tiles;
+        traces = apply.tiles;
     }
     CAP_LAUNCH_CHECK();
     return CAP_OK;
