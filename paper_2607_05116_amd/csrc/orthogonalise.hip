@@ -56,7 +56,7 @@ struct OrthWs {
     float* norm;                           // [batch][parts] sums of squares of U
     float* trace;                          // [batch][trace_cap] parts of the next trace
     float* center;                         // [batch][2] s of the group's first and second step
-    f32x4* sums;                           // parts of Gram tiles
+    f32x4* sums;                           // of the tiles computed in parts
     int n, m, np, mp;                      // sides, and as padded with zeros
     int xp, sp;                            // row pitch of X, and of X^T and the n x n matrices
     int parts, trace_cap;
@@ -81,14 +81,16 @@ int norm_parts(int rows, int cols) {
     return static_cast<int>((static_cast<size_t>(rows) * cols + per - 1) / per);
 }
 
-// How a product runs: tiles of 256 x 256 (one workgroup a CU) or 128 x 128 (two), and
-// for the Gram product which of its tiles are computed in parts along K.
+// How a product runs: tiles of 256 x 256 (one workgroup a CU) or 128 x 128 (two).  Tiles
+// of a symmetric product that do not fill a round of the chip are computed in parts along
+// K, whose fp32 sums a second kernel joins.
 struct ProductPlan {
     int side, tiles;                       // of one matrix
     int whole, split;                      // tiles of all matrices computed whole; parts of each of the others
+    int traces;                            // places of a trace's parts, of one matrix
     size_t sums;                           // bytes of the parts' sums
 };
-ProductPlan plan_product(bool square, bool gram, int np, int mp, int batch) {
+ProductPlan plan_product(bool square, int np, int mp, int K, int batch) {
     const int cus = device_cu_count();
     auto count = [&](int t) {
         const int r = (np + t - 1) / t, c = ((square ? np : mp) + t - 1) / t;
@@ -99,24 +101,38 @@ ProductPlan plan_product(bool square, bool gram, int np, int mp, int batch) {
     const bool wide = rounds(count(kBM), cus) * 24 <= rounds(count(kT), 2 * cus) * 16;
     p.side = wide ? kBM : kT;
     p.tiles = count(p.side);
+    p.traces = p.tiles * (wide ? (square ? kNW * 8 : kNW) : (square ? 16 : 4));
     const long long total = static_cast<long long>(p.tiles) * batch;
     p.whole = static_cast<int>(total);
     p.split = 1;
-    if (gram) {
-        const int slots = wide ? cus : 2 * cus;
-        const int rest = static_cast<int>(total % slots), KT = mp / kStageK;
-        const int split = rest ? std::min(std::min(slots / rest, 16), KT / 4) : 1;
-        const size_t bytes = static_cast<size_t>(p.side) * p.side * 4;
-        // stages saved (about 1.4 us each) against the sums' way out and in at 4 MB / us and a launch
-        const double saved = 1.4 * KT * (1.0 - 1.0 / split);
-        const double cost = 5.0 + 2.0 * rest * split * bytes / 4e6;
-        if (split > 1 && saved > cost) {
+    if (square) {
+        // us: stages of about 1.4 against the sums' way out and in at 4 MB a us and a launch
+        const int slots = wide ? cus : 2 * cus, KT = K / kStageK;
+        const int rest = static_cast<int>(total % slots);
+        const double tile_us = static_cast<double>(p.side) * p.side * 4 / 4e6;
+        double best = 1.4 * KT;
+        for (int split = 2; split <= 16 && split * rest <= slots && split <= KT / 2; ++split) {
+            const double t = 1.4 * ((KT / 2 + split - 1) / split * 2) + 4.0 + 2.0 * rest * split * tile_us;
+            if (t < 0.95 * best) {
+                best = t;
+                p.split = split;
+            }
+        }
+        if (rest && p.split > 1) {
             p.whole = static_cast<int>(total - rest);
-            p.split = split;
-            p.sums = rest * split * bytes;
+            p.sums = static_cast<size_t>(rest) * p.split * p.side * p.side * 4;
+        } else {
+            p.split = 1;
         }
     }
     return p;
+}
+struct Plans {
+    ProductPlan gram, sym, apply;
+};
+Plans plan_all(int np, int mp, int batch) {
+    return Plans{plan_product(true, np, mp, mp, batch), plan_product(true, np, mp, np, batch),
+                 plan_product(false, np, mp, np, batch)};
 }
 
 size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
@@ -139,10 +155,11 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
     take(static_cast<size_t>(kPad) * (xp > sp ? xp : sp) * 2);
     const int parts = norm_parts(rows, cols);
     char* f = take(static_cast<size_t>(batch) * parts * 4);
-    const size_t cap = (np / 128) * (mp / 128);
+    const Plans plans = plan_all(static_cast<int>(np), static_cast<int>(mp), batch);
+    const size_t cap = std::max(plans.sym.traces, plans.apply.traces);
     char* t = take(static_cast<size_t>(batch) * cap * 4);
     char* c = take(static_cast<size_t>(batch) * 8);
-    char* sums = take(plan_product(true, true, static_cast<int>(np), static_cast<int>(mp), batch).sums);
+    char* sums = take(std::max(plans.gram.sums, plans.sym.sums));
     if (w) {
         w->sums = reinterpret_cast<f32x4*>(sums);
         w->xh = reinterpret_cast<uint16_t*>(v[0]);
@@ -293,7 +310,7 @@ struct ProductArgs {
     int second, pair;                      // kSym1: of the second step; kSym2: Q; the group has two steps
     int traces;                            // kGram, kSym2 (D'): parts of the trace
     float coef[2][3];                      // of the group's steps
-    int whole, split;                      // kGram: tiles (of all matrices) computed whole, parts of each of the others
+    int whole, split;                      // tiles (of all matrices) computed whole, parts of each of the others
     uint16_t* out;
     int rows, cols, batch;
 };
@@ -557,18 +574,18 @@ __device__ __forceinline__ void store_sums(f32x4* dst, const f32x4 (&acc)[4][NJ]
     });
 }
 
-// This tile's part of a trace (off the diagonal it stands for two tiles).
-template <int THREADS>
-__device__ __forceinline__ void store_part(const ProductArgs& q, int batch, int tile, float sum, float* red) {
+// A wave's part of a trace.  In the n x n products each step of each wave has a place
+// (a tile computed in parts is joined step by step); whoever sums several writes the
+// others 0.  Off the diagonal a tile stands for two.
+template <Product MODE, int NJ>
+__device__ __forceinline__ void store_trace(const ProductArgs& q, int batch, int place, float sum, int lane) {
 #pragma unroll
     for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-    __syncthreads();
-    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        float t = 0.0f;
-        for (int i = 0; i < THREADS / kWave; ++i) t += red[i];
-        q.w.trace[static_cast<size_t>(batch) * q.w.trace_cap + tile] = t;
+    float* p = q.w.trace + static_cast<size_t>(batch) * q.w.trace_cap;
+    if constexpr (MODE == kApply) {
+        if (lane == 0) p[place] = sum;
+    } else {
+        if (lane < NJ) p[place * NJ + lane] = lane == 0 ? sum : 0.0f;
     }
 }
 
@@ -581,7 +598,7 @@ struct Unit {
 template <Product MODE>
 __device__ __forceinline__ Unit unit_of(const ProductArgs& q, int u, int KT) {
     Unit x{u, -1, 0, KT};
-    if constexpr (MODE == kGram) {
+    if constexpr (is_square(MODE)) {
         if (u >= q.whole) {
             const int v = u - q.whole, t = v / q.split, p = v - t * q.split;
             x.tile = q.whole + t;
@@ -674,14 +691,14 @@ __global__ __launch_bounds__(kThreads, 2) void product128_kernel(ProductArgs q, 
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j], a[i], acc[i][j], 0, 0, 0);
         }
     }
-    if (MODE == kGram && u.part >= 0) {
+    if (is_square(MODE) && u.part >= 0) {
         store_sums<4>(q.w.sums + (static_cast<size_t>(u.part) * 4 + wave) * 16 * kWave, acc, lane);
         return;
     }
     const Scalars c = scalars<MODE, kThreads>(q, batch, t == 0, red);
     const float sum = store_wave<MODE, 4>(q, c, acc, batch, ti * kT + wm * 64, tj * kT + wn * 64, ti != tj, lane);
     if constexpr (MODE == kApply || MODE == kMix)
-        store_part<kThreads>(q, batch, t, MODE == kMix && ti != tj ? 2.0f * sum : sum, red);
+        store_trace<MODE, 4>(q, batch, t * 4 + wave, MODE == kMix && ti != tj ? 2.0f * sum : sum, lane);
 }
 
 // ---- tiles of 256 x 256: the K loop of mfma_tile.hpp, persistent, one workgroup a CU
@@ -718,7 +735,7 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
         const size_t b_rows = is_square(MODE) ? w.np : w.mp;
         const uint16_t* A = q.A + (static_cast<size_t>(batch) * w.np + static_cast<size_t>(ti) * kBM) * lead;
         const uint16_t* B = q.B + (batch * b_rows + static_cast<size_t>(tj) * kBN + (wave >> 1) * kWN + (wave & 1) * 16) * lead;
-        const int k0 = MODE == kGram ? u.kt0 * kStageK : 0;
+        const int k0 = is_square(MODE) ? u.kt0 * kStageK : 0;
         ld.a = reinterpret_cast<const char*>(A + k0);
         ld.a_on = ti * kBM + wave / kWavesN * kWM < w.np;
         ld.b0 = reinterpret_cast<const char*>(B + k0);
@@ -744,7 +761,7 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
             for (int j = 0; j < kNJ; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
-        const int cb = batch, ct = t, ci = ti, cj = tj, cp = part, ck = MODE == kGram ? stages : KT;
+        const int cb = batch, ct = t, ci = ti, cj = tj, cp = part, ck = is_square(MODE) ? stages : KT;
         const int next = tile + G;
         // in the last stage buffer 0 is free: the next tile's stage 0 lands during the
         // rest of that stage and the results' way out
@@ -755,7 +772,7 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
         };
         const bool active = ci * kBM + wm * kWM < w.np;
         run_k_loop<f16x8>(ck, lds, wm, wn, lane, loader, active, acc, ld, a_lds, b_lds, hook, hook);
-        if (MODE == kGram && cp >= 0) {
+        if (is_square(MODE) && cp >= 0) {
             store_sums<kNJ>(q.w.sums + (static_cast<size_t>(cp) * kNW + wave) * 32 * kWave, acc, lane);
             tile = next;
             continue;
@@ -765,16 +782,16 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
         if (active && cj * kBN + wn * kWN < (is_square(MODE) ? w.np : w.mp))
             sum = store_wave<MODE, kNJ>(q, c, acc, cb, ci * kBM + wm * kWM, cj * kBN + wn * kWN, ci != cj, opaque(lane));
         if constexpr (MODE == kApply || MODE == kMix)
-            store_part<kNW * kWave>(q, cb, ct, MODE == kMix && ci != cj ? 2.0f * sum : sum, red);
+            store_trace<MODE, kNJ>(q, cb, ct * kNW + wave, MODE == kMix && ci != cj ? 2.0f * sum : sum, lane);
         tile = next;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
-// Joins the parts of the Gram tiles computed in parts: one wave for a step of a wave of
-// the tile.
-template <int NJ>
-__global__ __launch_bounds__(kWave) void gram_join_kernel(ProductArgs q, int tiles) {
+// Joins the parts of the tiles computed in parts: one wave for a step of a wave of the
+// tile.
+template <Product MODE, int NJ>
+__global__ __launch_bounds__(kWave) void join_kernel(ProductArgs q, int tiles) {
     constexpr int kWavesTile = NJ == 8 ? kNW : 4, kSide = NJ == 8 ? kBM : kT, kAcross = 2;
     __shared__ float red[1];
     const int lane = threadIdx.x;
@@ -784,19 +801,28 @@ __global__ __launch_bounds__(kWave) void gram_join_kernel(ProductArgs q, int til
     triangle(t, ti, tj);
     const int row0 = ti * kSide + wave / kAcross * 64 + 32 * (x / (NJ / 2));
     const int col0 = tj * kSide + wave % kAcross * 16 * NJ + 32 * (x % (NJ / 2));
-    const Scalars c = scalars<kGram, kWave>(q, batch, t == 0 && blockIdx.x == 0, red);
-    if (row0 >= q.w.np || col0 >= q.w.np) return;
-    f32x4 acc[2][2] = {};
-    const f32x4* p = q.w.sums + (static_cast<size_t>(blockIdx.y) * q.split * kWavesTile + wave) * 4 * NJ * kWave + 4 * x * kWave + lane;
+    const Scalars c = scalars<MODE, kWave>(q, batch, t == 0 && blockIdx.x == 0, red);
+    float sum = 0.0f;
+    if (row0 < q.w.np && col0 < q.w.np) {
+        const Out<MODE> out(q, c, batch, ti != tj, lane);
+        u32x4 in[2][2] = {};
+        out.fetch(in, row0, col0);
+        f32x4 acc[2][2] = {};
+        const f32x4* p = q.w.sums + (static_cast<size_t>(blockIdx.y) * q.split * kWavesTile + wave) * 4 * NJ * kWave + 4 * x * kWave + lane;
 #pragma unroll 4
-    for (int i = 0; i < q.split; ++i) {
+        for (int i = 0; i < q.split; ++i) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e / 2][e % 2] += p[e * kWave];
-        p += static_cast<size_t>(kWavesTile) * 4 * NJ * kWave;
+            for (int e = 0; e < 4; ++e) acc[e / 2][e % 2] += p[e * kWave];
+            p += static_cast<size_t>(kWavesTile) * 4 * NJ * kWave;
+        }
+        sum = out.store(acc, in, row0, col0);
     }
-    const Out<kGram> out(q, c, batch, ti != tj, lane);
-    const u32x4 none[2][2] = {};
-    out.store(acc, none, row0, col0);
+    if constexpr (MODE == kMix) {
+#pragma unroll
+        for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+        if (lane == 0)
+            q.w.trace[static_cast<size_t>(batch) * q.w.trace_cap + (t * kWavesTile + wave) * NJ + x] = ti != tj ? 2.0f * sum : sum;
+    }
 }
 
 template <Product MODE>
@@ -808,10 +834,12 @@ void launch_product(const ProductArgs& args, const ProductPlan& p, hipStream_t s
     if (p.side == kBM) {
         const int cus = device_cu_count();
         product256_kernel<MODE><<<units < cus ? units : cus, kNW * kWave, 0, stream>>>(q, p.tiles, units);
-        if (rest) gram_join_kernel<8><<<dim3(kNW * 8, rest), kWave, 0, stream>>>(q, p.tiles);
+        if constexpr (is_square(MODE))
+            if (rest) join_kernel<MODE, 8><<<dim3(kNW * 8, rest), kWave, 0, stream>>>(q, p.tiles);
     } else {
         product128_kernel<MODE><<<units, kThreads, 0, stream>>>(q, p.tiles);
-        if (rest) gram_join_kernel<4><<<dim3(4 * 4, rest), kWave, 0, stream>>>(q, p.tiles);
+        if constexpr (is_square(MODE))
+            if (rest) join_kernel<MODE, 4><<<dim3(4 * 4, rest), kWave, 0, stream>>>(q, p.tiles);
     }
 }
 
@@ -854,8 +882,7 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
     else if (momentum) begin(std::false_type{}, std::true_type{});
     else begin(std::false_type{}, std::false_type{});
     CAP_LAUNCH_CHECK();
-    const ProductPlan gram = plan_product(true, true, w.np, w.mp, batch), sym = plan_product(true, false, w.np, w.mp, batch),
-                      apply = plan_product(false, false, w.np, w.mp, batch);
+    const auto [gram, sym, apply] = plan_all(w.np, w.mp, batch);
     int from = 0, traces = 1;
     auto set = [&](uint16_t* A, uint16_t* B, uint16_t* D, int second, int parts) {
         q.A = A;
@@ -877,7 +904,7 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
         if (q.pair) {
             set(s1, s0, s2, 0, 0);
             launch_product<kMix>(q, sym, stream);                       // T
-            set(s2, s1, s0, 0, sym.tiles);
+            set(s2, s1, s0, 0, sym.traces);
             launch_product<kSym2>(q, sym, stream);                      // D'
             set(s0, s0, s2, 1, 0);
             launch_product<kSym1>(q, sym, stream);                      // R'
@@ -890,7 +917,7 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
         if (i < steps) launch_product<kApply>(q, apply, stream);
         else launch_product<kFinal>(q, apply, stream);
         from ^= 1;
-        traces = apply.tiles;
+        traces = apply.traces;
     }
     CAP_LAUNCH_CHECK();
     return CAP_OK;
