@@ -43,7 +43,19 @@ namespace cap {
 namespace {
 
 constexpr int kPad = 128;                  // n and m in the workspace are multiples of this
-constexpr int kT = 128;                    // the smaller tile
+
+// Tiles of the products, a workgroup's: ROWS x COLS in WM x WN waves.
+template <int ROWS_, int COLS_, int WM_, int WN_>
+struct Shape {
+    static constexpr int ROWS = ROWS_, COLS = COLS_, WM = WM_, WN = WN_, WAVES = WM * WN;
+    static constexpr int WR = ROWS / WM, WC = COLS / WN;     // of a wave
+    static constexpr int MI = WR / 16, NJ = WC / 16;         // 16 x 16 blocks of a wave
+    static constexpr int STEPS = (MI / 2) * (NJ / 2);        // its results' way out (Out)
+    static constexpr int BLOCK = ROWS < 128 ? ROWS : 128;    // symmetric products: left out or mirrored by blocks
+};
+using Big = Shape<256, 256, 4, 2>;
+using Mid = Shape<128, 256, 2, 4>;
+using Small = Shape<64, 64, 2, 2>;
 constexpr int kNormThreads = 256;
 constexpr int kMaxNormParts = 256;
 // Up to this many rows (or columns) the Gram form (orth_gram.hip) is taken.
@@ -81,51 +93,60 @@ int norm_parts(int rows, int cols) {
     return static_cast<int>((static_cast<size_t>(rows) * cols + per - 1) / per);
 }
 
-// How a product runs: tiles of 256 x 256 (one workgroup a CU) or 128 x 128 (two).  Tiles
-// of a symmetric product that do not fill a round of the chip are computed in parts along
-// K, whose fp32 sums a second kernel joins.
+// How a product runs.  Tiles of a symmetric product that do not fill a round of the chip
+// may be computed in parts along K, whose fp32 sums a second kernel joins.
 struct ProductPlan {
-    int side, tiles;                       // of one matrix
+    int shape, tiles;                      // 0 Big, 1 Mid, 2 Small; tiles of one matrix
     int whole, split;                      // tiles of all matrices computed whole; parts of each of the others
+    int grid;
     int traces;                            // places of a trace's parts, of one matrix
     size_t sums;                           // bytes of the parts' sums
 };
+
+// Tiles of a matrix: all of them, or those with a block on or below the diagonal.
+template <typename S>
+int count_tiles(bool square, int np, int mp) {
+    const int r = (np + S::ROWS - 1) / S::ROWS, c = ((square ? np : mp) + S::COLS - 1) / S::COLS;
+    if (!square) return r * c;
+    if (S::ROWS == S::COLS) return r * (r + 1) / 2;
+    return r / 2 * (r / 2 + 1) + (r % 2 ? r / 2 + 1 : 0);
+}
+
+// The rule: the estimated time of each shape, whole or with its last round in `split`
+// parts, from what a stage of K = 64 and the way in and out of a tile take (us, measured
+// on 2 to 576 tiles of K = 256 to 7168).
 ProductPlan plan_product(bool square, int np, int mp, int K, int batch) {
-    const int cus = device_cu_count();
-    auto count = [&](int t) {
-        const int r = (np + t - 1) / t, c = ((square ? np : mp) + t - 1) / t;
-        return square ? r * (r + 1) / 2 : r * c;
-    };
-    auto rounds = [&](long long tiles, int slots) { return (tiles * batch + slots - 1) / slots; };
-    ProductPlan p{};
-    const bool wide = rounds(count(kBM), cus) * 24 <= rounds(count(kT), 2 * cus) * 16;
-    p.side = wide ? kBM : kT;
-    p.tiles = count(p.side);
-    p.traces = p.tiles * (wide ? (square ? kNW * 8 : kNW) : (square ? 16 : 4));
-    const long long total = static_cast<long long>(p.tiles) * batch;
-    p.whole = static_cast<int>(total);
-    p.split = 1;
-    if (square) {
-        // us: stages of about 1.4 against the sums' way out and in at 4 MB a us and a launch
-        const int slots = wide ? cus : 2 * cus, KT = K / kStageK;
+    const int cus = device_cu_count(), KT = K / kStageK;
+    ProductPlan best{};
+    double best_us = 0.0;
+    auto consider = [&](auto shape, int id, int per_cu, double stage, double fixed) {
+        using S = decltype(shape);
+        const int tiles = count_tiles<S>(square, np, mp), slots = per_cu * cus;
+        const long long total = static_cast<long long>(tiles) * batch;
+        const long long rounds = total / slots;
         const int rest = static_cast<int>(total % slots);
-        const double tile_us = static_cast<double>(p.side) * p.side * 4 / 4e6;
-        double best = 1.4 * KT;
-        for (int split = 2; split <= 16 && split * rest <= slots && split <= KT / 2; ++split) {
-            const double t = 1.4 * ((KT / 2 + split - 1) / split * 2) + 4.0 + 2.0 * rest * split * tile_us;
-            if (t < 0.95 * best) {
-                best = t;
-                p.split = split;
-            }
+        const double tile_us = S::ROWS * S::COLS * 4 / 4e6;  // a part's sums one way, 4 MB a us
+        for (int split = 1; split <= (square && rest ? 16 : 1); ++split) {
+            if (split > 1 && (split * rest > slots || split > KT / 2)) break;
+            double us = rounds * (KT * stage + fixed);
+            if (rest && split == 1) us += KT * stage + fixed;
+            if (split > 1) us += (KT / 2 + split - 1) / split * 2 * stage + fixed + 5.0 + 2.0 * rest * split * tile_us;
+            if (best_us > 0.0 && us >= best_us) continue;
+            best_us = us;
+            best.shape = id;
+            best.tiles = tiles;
+            best.whole = static_cast<int>(split > 1 ? total - rest : total);
+            best.split = split;
+            const long long units = best.whole + (split > 1 ? static_cast<long long>(rest) * split : 0);
+            best.grid = static_cast<int>(std::min<long long>(units, slots));
+            best.traces = tiles * S::WAVES * (square ? S::STEPS : 1);
+            best.sums = split > 1 ? static_cast<size_t>(rest) * split * S::ROWS * S::COLS * 4 : 0;
         }
-        if (rest && p.split > 1) {
-            p.whole = static_cast<int>(total - rest);
-            p.sums = static_cast<size_t>(rest) * p.split * p.side * p.side * 4;
-        } else {
-            p.split = 1;
-        }
-    }
-    return p;
+    };
+    consider(Big{}, 0, 1, 1.42, square ? 10.0 : 22.0);
+    consider(Mid{}, 1, 1, 1.05, square ? 7.0 : 12.0);
+    consider(Small{}, 2, 2, 0.5, 4.0);
+    return best;
 }
 struct Plans {
     ProductPlan gram, sym, apply;
@@ -339,16 +360,16 @@ __device__ __forceinline__ float sum_parts(const float* parts, int count, float*
 __device__ __forceinline__ float poly(const float (&c)[3], float s) { return __builtin_fmaf(__builtin_fmaf(c[2], s, c[1]), s, c[0]); }
 
 // The scalars of a product of matrix `batch`; kGram and kSym2 (D') find their s from the
-// parts and (tile 0 of the matrix) keep it for the products after them.
-template <Product MODE, int THREADS>
+// parts and (tile 0 of the matrix) keep it for the products after them.  KNOWN: it is kept.
+template <Product MODE, int THREADS, bool KNOWN = false>
 __device__ __forceinline__ Scalars scalars(const ProductArgs& q, int batch, bool first_tile, float* red) {
     Scalars c{};
     float* center = q.w.center + 2 * static_cast<size_t>(batch);
     const float* parts = q.w.trace + static_cast<size_t>(batch) * q.w.trace_cap;
     c.ab = 1.0f;
     if constexpr (MODE == kGram) {
-        const float s = sum_parts<THREADS>(parts, q.traces, red) / static_cast<float>(q.w.n);
-        if (first_tile && threadIdx.x == 0) center[0] = s;
+        const float s = KNOWN ? center[0] : sum_parts<THREADS>(parts, q.traces, red) / static_cast<float>(q.w.n);
+        if (!KNOWN && first_tile && threadIdx.x == 0) center[0] = s;
         c.i = -s;
         return c;
     }
@@ -369,8 +390,8 @@ __device__ __forceinline__ Scalars scalars(const ProductArgs& q, int batch, bool
             c.a = poly(q.coef[1], center[1]);
             c.b = p;
         } else {
-            const float s1 = sum_parts<THREADS>(parts, q.traces, red) / static_cast<float>(q.w.n);
-            if (first_tile && threadIdx.x == 0) center[1] = s1;
+            const float s1 = KNOWN ? center[1] : sum_parts<THREADS>(parts, q.traces, red) / static_cast<float>(q.w.n);
+            if (!KNOWN && first_tile && threadIdx.x == 0) center[1] = s1;
             c.a = p;
             c.b = p * s;
             c.i = p * p * s - s1;
@@ -537,25 +558,25 @@ struct Out {
     }
 };
 
-// All results of a wave's 64 x 16 NJ block.  What a step adds to is loaded kAhead steps
+// All results of a wave at (row0, col0).  What a step adds to is loaded kAhead steps
 // before, since the loads' way is as long as several steps.  The steps are kept apart
 // (sched_barrier): mixed, they need more registers than there are.
-template <Product MODE, int NJ>
-__device__ __forceinline__ float store_wave(const ProductArgs& q, const Scalars& c, f32x4 (&acc)[4][NJ], int batch, int row0,
-                                            int col0, bool mirror, int lane) {
-    constexpr int kSteps = NJ, kAhead = 2;
+template <Product MODE, typename S>
+__device__ __forceinline__ float store_wave(const ProductArgs& q, const Scalars& c, f32x4 (&acc)[S::MI][S::NJ], int batch,
+                                            int row0, int col0, bool mirror, int lane) {
+    constexpr int kAcross = S::NJ / 2, kAhead = S::STEPS < 2 ? S::STEPS : 2;
     const Out<MODE> out(q, c, batch, mirror, lane);
     u32x4 in[kAhead + 1][2][2];
     auto fetch = [&](auto X) __attribute__((always_inline)) {
         constexpr int x = decltype(X)::value;
-        out.fetch(in[x % (kAhead + 1)], row0 + 32 * (x / (NJ / 2)), col0 + 32 * (x % (NJ / 2)));
+        out.fetch(in[x % (kAhead + 1)], row0 + 32 * (x / kAcross), col0 + 32 * (x % kAcross));
     };
     float sum = 0.0f;
     static_for<kAhead>([&](auto X) { fetch(X); });
     __builtin_amdgcn_sched_barrier(0);
-    static_for<kSteps>([&](auto X) __attribute__((always_inline)) {
-        constexpr int x = decltype(X)::value, ip = x / (NJ / 2), pr = x % (NJ / 2);
-        if constexpr (x + kAhead < kSteps) fetch(std::integral_constant<int, x + kAhead>{});
+    static_for<S::STEPS>([&](auto X) __attribute__((always_inline)) {
+        constexpr int x = decltype(X)::value, ip = x / kAcross, pr = x % kAcross;
+        if constexpr (x + kAhead < S::STEPS) fetch(std::integral_constant<int, x + kAhead>{});
         const f32x4 v[2][2] = {{acc[2 * ip][2 * pr], acc[2 * ip][2 * pr + 1]},
                                {acc[2 * ip + 1][2 * pr], acc[2 * ip + 1][2 * pr + 1]}};
         sum += out.store(v, in[x % (kAhead + 1)], row0 + 32 * ip, col0 + 32 * pr);
@@ -565,10 +586,12 @@ __device__ __forceinline__ float store_wave(const ProductArgs& q, const Scalars&
 }
 
 // The fp32 sums of a part of a product, as a wave holds them: [step][block][lane].
-template <int NJ>
-__device__ __forceinline__ void store_sums(f32x4* dst, const f32x4 (&acc)[4][NJ], int lane) {
-    static_for<NJ>([&](auto X) __attribute__((always_inline)) {
-        constexpr int x = decltype(X)::value, ip = x / (NJ / 2), pr = x % (NJ / 2);
+template <typename S>
+__device__ __forceinline__ void store_sums(const OrthWs& w, int part, int wave, const f32x4 (&acc)[S::MI][S::NJ], int lane) {
+    constexpr int kAcross = S::NJ / 2;
+    f32x4* dst = w.sums + (static_cast<size_t>(part) * S::WAVES + wave) * S::STEPS * 4 * kWave;
+    static_for<S::STEPS>([&](auto X) __attribute__((always_inline)) {
+        constexpr int x = decltype(X)::value, ip = x / kAcross, pr = x % kAcross;
 #pragma unroll
         for (int e = 0; e < 4; ++e) dst[(4 * x + e) * kWave + lane] = acc[2 * ip + e / 2][2 * pr + e % 2];
     });
@@ -577,15 +600,16 @@ __device__ __forceinline__ void store_sums(f32x4* dst, const f32x4 (&acc)[4][NJ]
 // A wave's part of a trace.  In the n x n products each step of each wave has a place
 // (a tile computed in parts is joined step by step); whoever sums several writes the
 // others 0.  Off the diagonal a tile stands for two.
-template <Product MODE, int NJ>
-__device__ __forceinline__ void store_trace(const ProductArgs& q, int batch, int place, float sum, int lane) {
+template <Product MODE, typename S>
+__device__ __forceinline__ void store_trace(const ProductArgs& q, int batch, int t, int wave, float sum, int lane) {
 #pragma unroll
     for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
     float* p = q.w.trace + static_cast<size_t>(batch) * q.w.trace_cap;
+    const int place = t * S::WAVES + wave;
     if constexpr (MODE == kApply) {
         if (lane == 0) p[place] = sum;
     } else {
-        if (lane < NJ) p[place * NJ + lane] = lane == 0 ? sum : 0.0f;
+        if (lane < S::STEPS) p[place * S::STEPS + lane] = lane == 0 ? sum : 0.0f;
     }
 }
 
@@ -610,100 +634,177 @@ __device__ __forceinline__ Unit unit_of(const ProductArgs& q, int u, int KT) {
     return x;
 }
 
-template <Product MODE>
-__device__ __forceinline__ void decode_tile(const ProductArgs& q, int t, int tile_rows, int& ti, int& tj) {
-    if constexpr (is_square(MODE)) {
-        triangle(t, ti, tj);
-    } else {
-        const int tm = (q.w.np + tile_rows - 1) / tile_rows;
+// Tile t of a matrix: of all, or of those on and below the diagonal.
+template <Product MODE, typename S>
+__device__ __forceinline__ void decode_tile(const ProductArgs& q, int t, int& ti, int& tj) {
+    if constexpr (!is_square(MODE)) {
+        const int tm = (q.w.np + S::ROWS - 1) / S::ROWS;
         ti = t % tm;
         tj = t / tm;
+    } else if constexpr (S::ROWS == S::COLS) {
+        triangle(t, ti, tj);
+    } else {                                                 // row tiles 2 p and 2 p + 1 have p + 1 each
+        static_assert(S::COLS == 2 * S::ROWS, "row tiles in pairs");
+        int p = static_cast<int>((sqrtf(4.0f * static_cast<float>(t) + 1.0f) - 1.0f) * 0.5f);
+        while (p * (p + 1) > t) --p;
+        while ((p + 1) * (p + 2) <= t) ++p;
+        const int rest = t - p * (p + 1), second = rest > p;
+        ti = 2 * p + second;
+        tj = rest - second * (p + 1);
     }
 }
 
-// ---- tiles of 128 x 128: four waves of 64 x 64, two workgroups a CU
-constexpr int kThreads = 256;
-constexpr int kTileStageB = 2 * kT * kRowB;
+// What becomes of a wave's block at (row0, col0): in a symmetric product the blocks above
+// the diagonal are left out, those below it mirrored.
+template <Product MODE, typename S>
+struct Place {
+    bool store, mirror;
+    __device__ __forceinline__ Place(const OrthWs& w, int row0, int col0) {
+        const int r = row0 / S::BLOCK, c = col0 / S::BLOCK;
+        if constexpr (is_square(MODE)) {
+            store = row0 < w.np && col0 < w.np && c <= r;
+            mirror = c < r;
+        } else {
+            store = row0 < w.np && col0 < w.mp;
+            mirror = true;
+        }
+    }
+};
 
-template <Product MODE>
-__global__ __launch_bounds__(kThreads, 2) void product128_kernel(ProductArgs q, int tiles) {
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kTileStageB];
-    __shared__ float red[kThreads / kWave];
+// ---- Mid and Small: a ring of K = 64 stages that runs on across the tiles of a workgroup,
+// all but one of them in flight
+template <typename S>
+struct Ring {
+    static constexpr int kStages = S::ROWS == 64 ? 4 : 3;                     // 64 or 144 KB
+    static constexpr int kStageB = (S::ROWS + S::COLS) * kRowB;
+    static constexpr int kA = S::ROWS / kRowsPerLoad / S::WAVES, kB = S::COLS / kRowsPerLoad / S::WAVES;   // loads of a wave
+    static constexpr int kPerCu = S::ROWS == 64 ? 2 : 1;
+};
+
+template <Product MODE, typename S>
+__global__ __launch_bounds__(S::WAVES * kWave, Ring<S>::kPerCu) void product_ring_kernel(ProductArgs q, int tiles, int units) {
+    using R = Ring<S>;
+    constexpr int THREADS = S::WAVES * kWave;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[R::kStages * R::kStageB];
+    __shared__ float red[S::WAVES];
     const OrthWs& w = q.w;
     const int lane = threadIdx.x % kWave;
     const int wave = static_cast<int>(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
-    const int wm = wave >> 1, wn = wave & 1;
-    const int K = MODE == kGram ? w.mp : w.np, ld = MODE == kGram ? w.xp : w.sp;
-    const Unit u = unit_of<MODE>(q, blockIdx.x, K / kStageK);
-    const int batch = u.tile / tiles, t = u.tile - batch * tiles;
-    int ti, tj;
-    decode_tile<MODE>(q, t, kT, ti, tj);
-    const uint16_t* A = q.A + static_cast<size_t>(batch) * w.np * ld;
-    const uint16_t* B = q.B + static_cast<size_t>(batch) * (is_square(MODE) ? w.np : w.mp) * ld;
-    const uint32_t pitch = static_cast<uint32_t>(ld) * 2u;
-    const LaneMap lm = lane_map(lane);
+    const int wm = wave / S::WN, wn = wave % S::WN;
     const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
-    // wave w brings rows 32 w .. + 31 of both operands, eight at a time
-    const char* pa = reinterpret_cast<const char*>(A + (static_cast<size_t>(ti) * kT + wave * 32) * ld + u.kt0 * kStageK);
-    const char* pb = reinterpret_cast<const char*>(B + (static_cast<size_t>(tj) * kT + wave * 32) * ld + u.kt0 * kStageK);
-    uint32_t a_off[4], b_off[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        a_off[i] = paired_row(i * 8 + lm.ld_row) * pitch + lm.col_b[i & 1];
-        b_off[i] = (i * 8 + lm.ld_row) * pitch + lm.col_b[i & 1];
-    }
-    auto issue = [&](int buf) __attribute__((always_inline)) {
-        const uint32_t at = lds_base + buf * kTileStageB + wave * 32 * kRowB;
-        static_for<4>([&](auto I) { lds_dma16(pa, a_off[I.value], at + I.value * 1024); });
-        static_for<4>([&](auto I) { lds_dma16(pb, b_off[I.value], at + kT * kRowB + I.value * 1024); });
-        pa += kRowB;
-        pb += kRowB;
+    const int KT = (MODE == kGram ? w.mp : w.np) / kStageK, lead = MODE == kGram ? w.xp : w.sp;
+    const uint32_t pitch = static_cast<uint32_t>(lead) * 2u;
+    const LaneMap lm = lane_map(lane);
+    const int G = gridDim.x;
+    int unit = G % 8 == 0 ? (blockIdx.x % 8) * (G / 8) + blockIdx.x / 8 : blockIdx.x;
+    if (unit >= units) return;
+
+    struct Tile { int batch, t, ti, tj, part, kt0, stages; };
+    auto decode = [&](int x) __attribute__((always_inline)) {
+        const Unit u = unit_of<MODE>(q, x, KT);
+        Tile T;
+        T.part = __builtin_amdgcn_readfirstlane(u.part);
+        T.kt0 = __builtin_amdgcn_readfirstlane(u.kt0);
+        T.stages = __builtin_amdgcn_readfirstlane(u.kt1 - u.kt0);
+        T.batch = __builtin_amdgcn_readfirstlane(u.tile / tiles);
+        T.t = __builtin_amdgcn_readfirstlane(u.tile) - T.batch * tiles;
+        int ti, tj;
+        decode_tile<MODE, S>(q, T.t, ti, tj);
+        T.ti = __builtin_amdgcn_readfirstlane(ti);
+        T.tj = __builtin_amdgcn_readfirstlane(tj);
+        return T;
     };
-    f32x4 acc[4][4];
+    // the load cursor, all but one stage ahead: a wave brings kA (kB) runs of eight rows
+    uint32_t a_off[R::kA], b_off[R::kB];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < R::kA; ++i)
+        a_off[i] = paired_row((wave * R::kA + i) * kRowsPerLoad + lm.ld_row) * pitch + lm.col_b[(wave * R::kA + i) & 1];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
-    const int KT = u.kt1 - u.kt0;
-    const int pc[2] = {(lm.fr_kc ^ lm.fr_swz) << 4, ((lm.fr_kc ^ lm.fr_swz) << 4) ^ 64};
-    issue(0);
-    for (int kt = 0; kt < KT; ++kt) {
-        const int buf = kt & 1;
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the stage before has been read
-        wait_vm<0>();                                            // this wave's part of the stage has landed
-        block_barrier();
-        if (kt + 1 < KT) issue(buf ^ 1);
-        const uint8_t* la = lds + buf * kTileStageB + (wm * 64 + lm.fr_row) * kRowB;
-        const uint8_t* lb = lds + buf * kTileStageB + (kT + wn * 64 + lm.fr_row) * kRowB;
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            f16x8 a[4], b[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] = frag_at<f16x8>(la + i * 16 * kRowB + pc[ks]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) b[j] = frag_at<f16x8>(lb + j * 16 * kRowB + pc[ks]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j], a[i], acc[i][j], 0, 0, 0);
+    for (int i = 0; i < R::kB; ++i)
+        b_off[i] = ((wave * R::kB + i) * kRowsPerLoad + lm.ld_row) * pitch + lm.col_b[(wave * R::kB + i) & 1];
+    const char *pa = nullptr, *pb = nullptr;
+    int it_unit = unit, it_left = 0, it_buf = 0;
+    auto cursor = [&]() __attribute__((always_inline)) {
+        const Tile T = decode(it_unit);
+        const size_t b_rows = is_square(MODE) ? w.np : w.mp;
+        pa = reinterpret_cast<const char*>(q.A + (static_cast<size_t>(T.batch) * w.np + T.ti * S::ROWS) * lead + T.kt0 * kStageK);
+        pb = reinterpret_cast<const char*>(q.B + (T.batch * b_rows + T.tj * S::COLS) * lead + T.kt0 * kStageK);
+        it_left = T.stages;
+    };
+    auto issue = [&]() __attribute__((always_inline)) {
+        const uint32_t at = lds_base + it_buf * R::kStageB;
+        static_for<R::kA>([&](auto I) { lds_dma16(pa, a_off[I.value], at + (wave * R::kA + I.value) * 1024); });
+        static_for<R::kB>(
+            [&](auto I) { lds_dma16(pb, b_off[I.value], at + S::ROWS * kRowB + (wave * R::kB + I.value) * 1024); });
+        it_buf = it_buf + 1 == R::kStages ? 0 : it_buf + 1;
+        if (--it_left > 0) {
+            pa += kRowB;
+            pb += kRowB;
+        } else if (it_unit + G < units) {
+            it_unit += G;
+            cursor();
+        } else {
+            it_left = 1;                   // past the end: the last stage again, so that the counts of loads in flight hold
         }
+    };
+    cursor();
+#pragma unroll 1
+    for (int i = 0; i < R::kStages - 1; ++i) issue();
+    int buf = 0;
+    const int pc[2] = {(lm.fr_kc ^ lm.fr_swz) << 4, ((lm.fr_kc ^ lm.fr_swz) << 4) ^ 64};
+    for (; unit < units; unit += G) {
+        const Tile T = decode(unit);
+        const int row0 = T.ti * S::ROWS + wm * S::WR, col0 = T.tj * S::COLS + wn * S::WC;
+        const Place<MODE, S> place(w, row0, col0);
+        f32x4 acc[S::MI][S::NJ];
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+            for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
+        for (int kt = 0; kt < T.stages; ++kt) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the stage before has been read
+            wait_vm<(R::kStages - 2) * (R::kA + R::kB)>();                                 // this wave's part of this one has landed
+            block_barrier();
+            issue();                                                 // into the buffer of the stage before
+            const uint8_t* la = lds + buf * R::kStageB + (wm * S::WR + lm.fr_row) * kRowB;
+            const uint8_t* lb = lds + buf * R::kStageB + (S::ROWS + wn * S::WC + lm.fr_row) * kRowB;
+            buf = buf + 1 == R::kStages ? 0 : buf + 1;
+            if (!place.store) continue;                              // wave-uniform
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                f16x8 a[S::MI], b[S::NJ];
+#pragma unroll
+                for (int i = 0; i < S::MI; ++i) a[i] = frag_at<f16x8>(la + i * 16 * kRowB + pc[ks]);
+#pragma unroll
+                for (int j = 0; j < S::NJ; ++j) b[j] = frag_at<f16x8>(lb + j * 16 * kRowB + pc[ks]);
+#pragma unroll
+                for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < S::NJ; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j], a[i], acc[i][j], 0, 0, 0);
+            }
+        }
+        if (is_square(MODE) && T.part >= 0) {
+            store_sums<S>(w, T.part, wave, acc, lane);
+            if (T.t == 0 && T.kt0 == 0) scalars<MODE, THREADS>(q, T.batch, true, red);
+            continue;
+        }
+        const Scalars c = scalars<MODE, THREADS>(q, T.batch, T.t == 0, red);
+        float sum = 0.0f;
+        if (place.store) sum = store_wave<MODE, S>(q, c, acc, T.batch, row0, col0, place.mirror, lane);
+        if constexpr (MODE == kApply || MODE == kMix)
+            store_trace<MODE, S>(q, T.batch, T.t, wave, MODE == kMix && place.mirror ? 2.0f * sum : sum, lane);
     }
-    if (is_square(MODE) && u.part >= 0) {
-        store_sums<4>(q.w.sums + (static_cast<size_t>(u.part) * 4 + wave) * 16 * kWave, acc, lane);
-        return;
-    }
-    const Scalars c = scalars<MODE, kThreads>(q, batch, t == 0, red);
-    const float sum = store_wave<MODE, 4>(q, c, acc, batch, ti * kT + wm * 64, tj * kT + wn * 64, ti != tj, lane);
-    if constexpr (MODE == kApply || MODE == kMix)
-        store_trace<MODE, 4>(q, batch, t * 4 + wave, MODE == kMix && ti != tj ? 2.0f * sum : sum, lane);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
-// ---- tiles of 256 x 256: the K loop of mfma_tile.hpp, persistent, one workgroup a CU
+// ---- Big: the K loop of mfma_tile.hpp
+static_assert(Big::ROWS == kBM && Big::COLS == kBN && Big::WM == kWavesM && Big::WN == kWavesN, "the K loop's tile");
+
 template <Product MODE>
-__global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs q, int tiles, int units) {
+__global__ __launch_bounds__(kNW * kWave, 1) void product_big_kernel(ProductArgs q, int tiles, int units) {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * kStageBytes];
     __shared__ float red[kNW];
     const OrthWs& w = q.w;
@@ -719,14 +820,16 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
     const int G = gridDim.x;
     int tile = G % 8 == 0 ? (blockIdx.x % 8) * (G / 8) + blockIdx.x / 8 : blockIdx.x;
     int batch = 0, t = 0, ti = 0, tj = 0, part = -1, stages = KT;
+    bool first = true;
     Loads ld;
     auto start_tile = [&](int x) __attribute__((always_inline)) {
         const Unit u = unit_of<MODE>(q, x, KT);
         part = __builtin_amdgcn_readfirstlane(u.part);
+        first = u.kt0 == 0;
         stages = __builtin_amdgcn_readfirstlane(u.kt1 - u.kt0);
         batch = __builtin_amdgcn_readfirstlane(u.tile / tiles);
         t = __builtin_amdgcn_readfirstlane(u.tile) - batch * tiles;
-        decode_tile<MODE>(q, t, kBM, ti, tj);
+        decode_tile<MODE, Big>(q, t, ti, tj);
         ti = __builtin_amdgcn_readfirstlane(ti);
         tj = __builtin_amdgcn_readfirstlane(tj);
         if (!loader) return;
@@ -761,6 +864,7 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
             for (int j = 0; j < kNJ; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
+        const bool cfirst = first;
         const int cb = batch, ct = t, ci = ti, cj = tj, cp = part, ck = is_square(MODE) ? stages : KT;
         const int next = tile + G;
         // in the last stage buffer 0 is free: the next tile's stage 0 lands during the
@@ -773,16 +877,18 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
         const bool active = ci * kBM + wm * kWM < w.np;
         run_k_loop<f16x8>(ck, lds, wm, wn, lane, loader, active, acc, ld, a_lds, b_lds, hook, hook);
         if (is_square(MODE) && cp >= 0) {
-            store_sums<kNJ>(q.w.sums + (static_cast<size_t>(cp) * kNW + wave) * 32 * kWave, acc, lane);
+            store_sums<Big>(w, cp, wave, acc, lane);
+            if (ct == 0 && cfirst) scalars<MODE, kNW * kWave>(q, cb, true, red);
             tile = next;
             continue;
         }
         const Scalars c = scalars<MODE, kNW * kWave>(q, cb, ct == 0, red);
+        const int row0 = ci * kBM + wm * kWM, col0 = cj * kBN + wn * kWN;
+        const Place<MODE, Big> place(w, row0, col0);
         float sum = 0.0f;
-        if (active && cj * kBN + wn * kWN < (is_square(MODE) ? w.np : w.mp))
-            sum = store_wave<MODE, kNJ>(q, c, acc, cb, ci * kBM + wm * kWM, cj * kBN + wn * kWN, ci != cj, opaque(lane));
+        if (place.store) sum = store_wave<MODE, Big>(q, c, acc, cb, row0, col0, place.mirror, opaque(lane));
         if constexpr (MODE == kApply || MODE == kMix)
-            store_trace<MODE, kNJ>(q, cb, ct * kNW + wave, MODE == kMix && ci != cj ? 2.0f * sum : sum, lane);
+            store_trace<MODE, Big>(q, cb, ct, wave, MODE == kMix && place.mirror ? 2.0f * sum : sum, lane);
         tile = next;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -790,30 +896,29 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product256_kernel(ProductArgs 
 
 // Joins the parts of the tiles computed in parts: one wave for a step of a wave of the
 // tile.
-template <Product MODE, int NJ>
+template <Product MODE, typename S>
 __global__ __launch_bounds__(kWave) void join_kernel(ProductArgs q, int tiles) {
-    constexpr int kWavesTile = NJ == 8 ? kNW : 4, kSide = NJ == 8 ? kBM : kT, kAcross = 2;
-    __shared__ float red[1];
     const int lane = threadIdx.x;
-    const int wave = blockIdx.x / NJ, x = blockIdx.x % NJ;
+    const int wave = blockIdx.x / S::STEPS, x = blockIdx.x % S::STEPS;
     const int tile = q.whole + blockIdx.y, batch = tile / tiles, t = tile - batch * tiles;
     int ti, tj;
-    triangle(t, ti, tj);
-    const int row0 = ti * kSide + wave / kAcross * 64 + 32 * (x / (NJ / 2));
-    const int col0 = tj * kSide + wave % kAcross * 16 * NJ + 32 * (x % (NJ / 2));
-    const Scalars c = scalars<MODE, kWave>(q, batch, t == 0 && blockIdx.x == 0, red);
+    decode_tile<MODE, S>(q, t, ti, tj);
+    const int row0 = ti * S::ROWS + wave / S::WN * S::WR + 32 * (x / (S::NJ / 2));
+    const int col0 = tj * S::COLS + wave % S::WN * S::WC + 32 * (x % (S::NJ / 2));
+    const Scalars c = scalars<MODE, kWave, true>(q, batch, false, nullptr);
+    const Place<MODE, S> place(q.w, row0, col0);
     float sum = 0.0f;
-    if (row0 < q.w.np && col0 < q.w.np) {
-        const Out<MODE> out(q, c, batch, ti != tj, lane);
+    if (place.store) {
+        const Out<MODE> out(q, c, batch, place.mirror, lane);
         u32x4 in[2][2] = {};
         out.fetch(in, row0, col0);
         f32x4 acc[2][2] = {};
-        const f32x4* p = q.w.sums + (static_cast<size_t>(blockIdx.y) * q.split * kWavesTile + wave) * 4 * NJ * kWave + 4 * x * kWave + lane;
+        const f32x4* p = q.w.sums + ((static_cast<size_t>(blockIdx.y) * q.split * S::WAVES + wave) * S::STEPS + x) * 4 * kWave + lane;
 #pragma unroll 4
         for (int i = 0; i < q.split; ++i) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e / 2][e % 2] += p[e * kWave];
-            p += static_cast<size_t>(kWavesTile) * 4 * NJ * kWave;
+            p += static_cast<size_t>(S::WAVES) * S::STEPS * 4 * kWave;
         }
         sum = out.store(acc, in, row0, col0);
     }
@@ -821,7 +926,7 @@ __global__ __launch_bounds__(kWave) void join_kernel(ProductArgs q, int tiles) {
 #pragma unroll
         for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
         if (lane == 0)
-            q.w.trace[static_cast<size_t>(batch) * q.w.trace_cap + (t * kWavesTile + wave) * NJ + x] = ti != tj ? 2.0f * sum : sum;
+            q.w.trace[static_cast<size_t>(batch) * q.w.trace_cap + (t * S::WAVES + wave) * S::STEPS + x] = place.mirror ? 2.0f * sum : sum;
     }
 }
 
@@ -831,15 +936,20 @@ void launch_product(const ProductArgs& args, const ProductPlan& p, hipStream_t s
     q.whole = p.whole;
     q.split = p.split;
     const int rest = p.tiles * q.batch - p.whole, units = p.whole + rest * p.split;
-    if (p.side == kBM) {
-        const int cus = device_cu_count();
-        product256_kernel<MODE><<<units < cus ? units : cus, kNW * kWave, 0, stream>>>(q, p.tiles, units);
+    auto join = [&](auto shape) {
+        using S = decltype(shape);
         if constexpr (is_square(MODE))
-            if (rest) join_kernel<MODE, 8><<<dim3(kNW * 8, rest), kWave, 0, stream>>>(q, p.tiles);
+            if (rest) join_kernel<MODE, S><<<dim3(S::WAVES * S::STEPS, rest), kWave, 0, stream>>>(q, p.tiles);
+    };
+    if (p.shape == 0) {
+        product_big_kernel<MODE><<<p.grid, Big::WAVES * kWave, 0, stream>>>(q, p.tiles, units);
+        join(Big{});
+    } else if (p.shape == 1) {
+        product_ring_kernel<MODE, Mid><<<p.grid, Mid::WAVES * kWave, 0, stream>>>(q, p.tiles, units);
+        join(Mid{});
     } else {
-        product128_kernel<MODE><<<units, kThreads, 0, stream>>>(q, p.tiles);
-        if constexpr (is_square(MODE))
-            if (rest) join_kernel<MODE, 4><<<dim3(4 * 4, rest), kWave, 0, stream>>>(q, p.tiles);
+        product_ring_kernel<MODE, Small><<<p.grid, Small::WAVES * kWave, 0, stream>>>(q, p.tiles, units);
+        join(Small{});
     }
 }
 
