@@ -27,8 +27,8 @@
 //   * S, P, T and Q are carried as a multiple of I and the rest (S = s I + D, with s
 //     their mean diagonal, in fp32), and only the rest is rounded: with m >> n, or once
 //     the singular values are near 1, it is several times smaller.
-//   * X is carried to 22 bits (a second fp16 with its rounding error, scaled by 2^11)
-//     where it is multiplied by the multiple of I, which passes its error on undamped.
+//   * X is carried to 15 bits (fp16 and its rounding error in fp8) where it is multiplied
+//     by the multiple of I, which passes its error on undamped.
 // Together 3e-4 to 1.3e-3 of the result's norm on square, wide, low-rank and 1/i spectra,
 // 2.5e-3 where they fall by e^-12; bf16 products leave 1e-2 to 1e-1.  A pair in the middle
 // or three steps in one group lose more (up to 3e-3 and 2e-2): the noise of S' grows by
@@ -63,7 +63,8 @@ constexpr int kGramRows = 128;
 constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
 
 struct OrthWs {
-    uint16_t *xh, *xl, *xt[2];             // X [n][m]: fp16 and its scaled error; X^T [m][n], in turn
+    uint16_t *xh, *xt[2];                  // X [n][m] in fp16; X^T [m][n], in turn
+    uint8_t* xl;                           // the scaled error of X in fp16, in fp8
     uint16_t* sq[3];                       // n x n
     float* norm;                           // [batch][parts] sums of squares of U
     float* trace;                          // [batch][trace_cap] parts of the next trace
@@ -172,7 +173,7 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
     // what follows here; each kind of matrix is followed by one at least as large
     char* v[7];
     for (int i = 4; i < 7; ++i) v[i] = take(q);
-    for (int i = 0; i < 4; ++i) v[i] = take(i < 2 ? x : xt);
+    for (int i = 0; i < 4; ++i) v[i] = take(i == 0 ? x : i == 1 ? x / 2 : xt);
     take(static_cast<size_t>(kPad) * (xp > sp ? xp : sp) * 2);
     const int parts = norm_parts(rows, cols);
     char* f = take(static_cast<size_t>(batch) * parts * 4);
@@ -184,7 +185,7 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
     if (w) {
         w->sums = reinterpret_cast<f32x4*>(sums);
         w->xh = reinterpret_cast<uint16_t*>(v[0]);
-        w->xl = reinterpret_cast<uint16_t*>(v[1]);
+        w->xl = reinterpret_cast<uint8_t*>(v[1]);
         for (int i = 0; i < 2; ++i) w->xt[i] = reinterpret_cast<uint16_t*>(v[2 + i]);
         for (int i = 0; i < 3; ++i) w->sq[i] = reinterpret_cast<uint16_t*>(v[4 + i]);
         w->norm = reinterpret_cast<float*>(f);
@@ -200,6 +201,28 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
         w->trace_cap = static_cast<int>(cap);
     }
     return at;
+}
+
+// ------------------------------------------------------------------ X in two parts
+// x = fp16 + fp8 2^-18 (e4m3): the error of a value of fp16 is below its 2^-11, so the
+// second part is below 2^7 |x|, a normal fp8 down to |x| = 2^-13; four more bits of x there.
+// Larger than 448 (|x| > 3.5, which steps of other coefficients may reach) it saturates.
+constexpr float kErrScale = 262144.0f;
+__device__ __forceinline__ void split_x(const float (&v)[4], u32x2& hi, uint32_t& err) {
+    hi = u32x2{pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3])};
+    float d[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        d[e] = __builtin_amdgcn_fmed3f((v[e] - f16_at(hi, e)) * kErrScale, -448.0f, 448.0f);
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(d[0], d[1], 0, false);
+    err = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(d[2], d[3], lo, true));
+}
+__device__ __forceinline__ void join_x(const u32x2& hi, uint32_t err, float (&v)[4]) {
+    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(err), false);
+    const auto b = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(err), true);
+    const float d[4] = {a[0], a[1], b[0], b[1]};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(d[e], 1.0f / kErrScale, f16_at(hi, e));
 }
 
 // ------------------------------------------------------------------ norm and momentum
@@ -290,11 +313,12 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
             v[e] = u[x][e] * scale;
             tile[16 * x + ty][4 * tx + e] = v[e];
         }
-        u32x2 hi, lo;
-        split4(v, hi, lo);
+        u32x2 hi;
+        uint32_t err;
+        split_x(v, hi, err);
         const size_t at = nat_base + static_cast<size_t>(r0 + 16 * x + ty) * nat_pitch + c0 + 4 * tx;
         *reinterpret_cast<u32x2*>(nat_hi + at) = hi;
-        if (!tall) *reinterpret_cast<u32x2*>(w.xl + at) = lo;
+        if (!tall) *reinterpret_cast<uint32_t*>(w.xl + at) = err;
     }
     __syncthreads();
 #pragma unroll
@@ -302,11 +326,12 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = tile[4 * tx + e][16 * x + ty];
-        u32x2 hi, lo;
-        split4(v, hi, lo);
+        u32x2 hi;
+        uint32_t err;
+        split_x(v, hi, err);
         const size_t at = tra_base + static_cast<size_t>(c0 + 16 * x + ty) * tra_pitch + r0 + 4 * tx;
         *reinterpret_cast<u32x2*>(tra_hi + at) = hi;
-        if (tall) *reinterpret_cast<u32x2*>(w.xl + at) = lo;
+        if (tall) *reinterpret_cast<uint32_t*>(w.xl + at) = err;
     }
 }
 
@@ -410,12 +435,20 @@ __device__ __forceinline__ int paired_row(int v) {
     return (v & ~31) | ((v & 12) << 1) | ((v >> 2) & 4) | (v & 3);
 }
 
-// 16 bytes at a scalar base and a lane's 32-bit offset, in global memory.
+// A vector at a scalar base and a lane's 32-bit offset, in global memory.
 typedef __attribute__((address_space(1))) char global_char;
-typedef __attribute__((address_space(1))) u32x4 global_u32x4;
-__device__ __forceinline__ global_u32x4* lane_ptr(const void* base, uint32_t off) {
-    return reinterpret_cast<global_u32x4*>(reinterpret_cast<global_char*>(reinterpret_cast<uint64_t>(uniform_ptr(base))) + off);
+template <typename V = u32x4>
+__device__ __forceinline__ __attribute__((address_space(1))) V* lane_ptr(const void* base, uint32_t off) {
+    return reinterpret_cast<__attribute__((address_space(1))) V*>(
+        reinterpret_cast<global_char*>(reinterpret_cast<uint64_t>(uniform_ptr(base))) + off);
 }
+
+// What a step of the results adds to: 8 columns a lane of two rows, of A and B or of X and
+// its error.
+struct Added {
+    u32x4 first[2], second[2];
+    u32x2 err[2];
+};
 
 // Results leave a wave in steps of 32 x 32 values: two row blocks and two column
 // blocks, at (row0, col0) of the matrix.  Lane (r, g) holds columns 4 g .. + 3 of each 16
@@ -431,7 +464,7 @@ struct Out {
     int batch, lane, pitch;
     bool mirror;
     uint32_t lane_at, lane_t;
-    const uint16_t *p0, *p1;
+    const uint16_t* p0;
 
     __device__ __forceinline__ Out(const ProductArgs& q_, const Scalars& c_, int batch_, bool mirror_, int lane_)
         : q(q_), c(c_), batch(batch_), lane(lane_), pitch(kSquare ? q_.w.sp : q_.w.xp), mirror(mirror_) {
@@ -439,16 +472,19 @@ struct Out {
         lane_at = 2u * ((8 * (r >> 2) + (r & 3)) * pitch + 16 * (g & 1) + 8 * (g >> 1));
         lane_t = 2u * ((4 * g + (r & 3)) * q.w.sp + 8 * (r >> 2));
         p0 = kSquare ? q.A : q.w.xh;
-        p1 = kSquare ? q.B : q.w.xl;
     }
-    __device__ __forceinline__ global_u32x4* at(const uint16_t* p, int row0, int col0, int ii) const {
+    __device__ __forceinline__ auto at(const uint16_t* p, int row0, int col0, int ii) const {
         return lane_ptr(p + (static_cast<size_t>(batch) * q.w.np + row0 + 4 * ii) * pitch + col0, lane_at);
     }
-    __device__ __forceinline__ void fetch(u32x4 (&in)[2][2], int row0, int col0) const {
+    __device__ __forceinline__ auto err_at(int row0, int col0, int ii) const {
+        return lane_ptr<u32x2>(q.w.xl + (static_cast<size_t>(batch) * q.w.np + row0 + 4 * ii) * pitch + col0, lane_at / 2);
+    }
+    __device__ __forceinline__ void fetch(Added& in, int row0, int col0) const {
 #pragma unroll
         for (int ii = 0; ii < 2; ++ii) {
-            if constexpr (kIn > 0) in[ii][0] = *at(p0, row0, col0, ii);
-            if constexpr (kIn > 1) in[ii][1] = *at(p1, row0, col0, ii);
+            if constexpr (kIn > 0) in.first[ii] = *at(p0, row0, col0, ii);
+            if constexpr (kIn > 1 && kSquare) in.second[ii] = *at(q.B, row0, col0, ii);
+            if constexpr (!kSquare) in.err[ii] = *err_at(row0, col0, ii);
         }
     }
     // 8 consecutive columns of a row <-> the lane's halves of two blocks
@@ -477,7 +513,7 @@ struct Out {
 
     // One step: acc[row block][column block], what fetch() brought; returns its part of
     // a trace.
-    __device__ __forceinline__ float store(const f32x4 (&acc)[2][2], const u32x4 (&in)[2][2], int row0, int col0) const {
+    __device__ __forceinline__ float store(const f32x4 (&acc)[2][2], const Added& in, int row0, int col0) const {
         const int r = lane & 15, g = lane >> 4;
         float sum = 0.0f;
         u32x2 t[2][2];                                             // transposed
@@ -489,9 +525,9 @@ struct Out {
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[b][e] = acc[ii][b][e];
-            u32x2 hi[2], lo[2], i0[2], i1[2];
-            if constexpr (kIn > 0) halves(in[ii][0], i0[0], i0[1]);
-            if constexpr (kIn > 1) halves(in[ii][1], i1[0], i1[1]);
+            u32x2 hi[2], i0[2], i1[2];
+            if constexpr (kIn > 0) halves(in.first[ii], i0[0], i0[1]);
+            if constexpr (kIn > 1 && kSquare) halves(in.second[ii], i1[0], i1[1]);
             if constexpr (kSquare) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
@@ -518,15 +554,16 @@ struct Out {
                 }
                 *at(q.D, row0, col0, ii) = join(hi[0], hi[1]);
             } else {
+                const auto ie = __builtin_amdgcn_permlane16_swap(in.err[ii][0], in.err[ii][1], false, false);
+                uint32_t err[2];
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
+                    float x[4];
+                    join_x(i0[b], ie[b], x);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float x = __builtin_fmaf(f16_at(i1[b], e), 1.0f / kLoScale, f16_at(i0[b], e));
-                        v[b][e] = __builtin_fmaf(c.a, x, v[b][e]);
-                    }
+                    for (int e = 0; e < 4; ++e) v[b][e] = __builtin_fmaf(c.a, x[e], v[b][e]);
                     if constexpr (MODE == kApply) {
-                        split4(v[b], hi[b], lo[b]);
+                        split_x(v[b], hi[b], err[b]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) sum = __builtin_fmaf(v[b][e], v[b][e], sum);
                     } else {
@@ -535,7 +572,8 @@ struct Out {
                 }
                 if constexpr (MODE == kApply) {
                     *at(q.w.xh, row0, col0, ii) = join(hi[0], hi[1]);
-                    *at(q.w.xl, row0, col0, ii) = join(lo[0], lo[1]);
+                    const auto oe = __builtin_amdgcn_permlane16_swap(err[0], err[1], false, false);
+                    *err_at(row0, col0, ii) = u32x2{oe[0], oe[1]};
                 } else if (q.rows <= q.cols) {
                     bf16_out(row, col0 + 16 * (g & 1) + 8 * (g >> 1), join(hi[0], hi[1]));
                 }
@@ -566,7 +604,7 @@ __device__ __forceinline__ float store_wave(const ProductArgs& q, const Scalars&
                                             int row0, int col0, bool mirror, int lane) {
     constexpr int kAcross = S::NJ / 2, kAhead = S::STEPS < 2 ? S::STEPS : 2;
     const Out<MODE> out(q, c, batch, mirror, lane);
-    u32x4 in[kAhead + 1][2][2];
+    Added in[kAhead + 1];
     auto fetch = [&](auto X) __attribute__((always_inline)) {
         constexpr int x = decltype(X)::value;
         out.fetch(in[x % (kAhead + 1)], row0 + 32 * (x / kAcross), col0 + 32 * (x % kAcross));
@@ -910,7 +948,7 @@ __global__ __launch_bounds__(kWave) void join_kernel(ProductArgs q, int tiles) {
     float sum = 0.0f;
     if (place.store) {
         const Out<MODE> out(q, c, batch, place.mirror, lane);
-        u32x4 in[2][2] = {};
+        Added in{};
         out.fetch(in, row0, col0);
         f32x4 acc[2][2] = {};
         const f32x4* p = q.w.sums + ((static_cast<size_t>(blockIdx.y) * q.split * S::WAVES + wave) * S::STEPS + x) * 4 * kWave + lane;
