@@ -225,6 +225,16 @@ __device__ __forceinline__ void join_x(const u32x2& hi, uint32_t err, float (&v)
     for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(d[e], 1.0f / kErrScale, f16_at(hi, e));
 }
 
+// The errors of X lie in blocks of 32 x 32, the bytes of a step of the results in the order
+// in which the lanes hold them: [4-row half][lane][8 columns].
+__device__ __forceinline__ size_t err_block(const OrthWs& w, int batch, int row0, int col0) {
+    return ((static_cast<size_t>(batch) * w.np + row0) * w.mp + 32 * static_cast<size_t>(col0));
+}
+__device__ __forceinline__ int err_place(int row, int col) {       // of element (row, col), col a multiple of 4
+    const int r = ((row >> 1) & 12) | (row & 3), g = ((col >> 4) & 1) | ((col >> 2) & 2);
+    return 512 * ((row >> 2) & 1) + 8 * (r + 16 * g) + (col & 7);
+}
+
 // ------------------------------------------------------------------ norm and momentum
 // Sum of squares of U over this block's part of its matrix; writes the momentum.
 template <bool BF16, bool MOM>
@@ -318,7 +328,9 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
         split_x(v, hi, err);
         const size_t at = nat_base + static_cast<size_t>(r0 + 16 * x + ty) * nat_pitch + c0 + 4 * tx;
         *reinterpret_cast<u32x2*>(nat_hi + at) = hi;
-        if (!tall) *reinterpret_cast<uint32_t*>(w.xl + at) = err;
+        const int row = r0 + 16 * x + ty, col = c0 + 4 * tx;
+        if (!tall)
+            *reinterpret_cast<uint32_t*>(w.xl + err_block(w, batch, row & ~31, col & ~31) + err_place(row & 31, col & 31)) = err;
     }
     __syncthreads();
 #pragma unroll
@@ -331,7 +343,9 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
         split_x(v, hi, err);
         const size_t at = tra_base + static_cast<size_t>(c0 + 16 * x + ty) * tra_pitch + r0 + 4 * tx;
         *reinterpret_cast<u32x2*>(tra_hi + at) = hi;
-        if (tall) *reinterpret_cast<uint32_t*>(w.xl + at) = err;
+        const int row = c0 + 16 * x + ty, col = r0 + 4 * tx;
+        if (tall)
+            *reinterpret_cast<uint32_t*>(w.xl + err_block(w, batch, row & ~31, col & ~31) + err_place(row & 31, col & 31)) = err;
     }
 }
 
@@ -455,6 +469,7 @@ struct Added {
 // x 16 block, of row paired_row.  Two adjacent blocks trade halves (permlane16_swap), so
 // that a lane reads and writes 8 consecutive columns: columns 8 (g / 2) .. of block g % 2.
 // Addresses are a scalar base for the step and a 32-bit lane offset.
+
 template <Product MODE>
 struct Out {
     static constexpr bool kSquare = is_square(MODE);
@@ -477,14 +492,27 @@ struct Out {
         return lane_ptr(p + (static_cast<size_t>(batch) * q.w.np + row0 + 4 * ii) * pitch + col0, lane_at);
     }
     __device__ __forceinline__ auto err_at(int row0, int col0, int ii) const {
-        return lane_ptr<u32x2>(q.w.xl + (static_cast<size_t>(batch) * q.w.np + row0 + 4 * ii) * pitch + col0, lane_at / 2);
+        return lane_ptr<u32x2>(q.w.xl + err_block(q.w, batch, row0, col0) + 512 * ii, 8u * lane);
     }
-    __device__ __forceinline__ void fetch(Added& in, int row0, int col0) const {
+    // What N steps side by side add to; steps that share lines of 128 bytes are loaded
+    // together, a row block at a time (apart, each line came twice: 460 -> PAIRED us for the
+    // last product of 8 x 2048 x 7168).
+    template <int N>
+    __device__ __forceinline__ void fetch(Added (&in)[N], int row0, int col0) const {
 #pragma unroll
         for (int ii = 0; ii < 2; ++ii) {
-            if constexpr (kIn > 0) in.first[ii] = *at(p0, row0, col0, ii);
-            if constexpr (kIn > 1 && kSquare) in.second[ii] = *at(q.B, row0, col0, ii);
-            if constexpr (!kSquare) in.err[ii] = *err_at(row0, col0, ii);
+            if constexpr (kIn > 0) {
+#pragma unroll
+                for (int x = 0; x < N; ++x) in[x].first[ii] = *at(p0, row0, col0 + 32 * x, ii);
+            }
+            if constexpr (kIn > 1 && kSquare) {
+#pragma unroll
+                for (int x = 0; x < N; ++x) in[x].second[ii] = *at(q.B, row0, col0 + 32 * x, ii);
+            }
+            if constexpr (!kSquare) {
+#pragma unroll
+                for (int x = 0; x < N; ++x) in[x].err[ii] = *err_at(row0, col0 + 32 * x, ii);
+            }
         }
     }
     // 8 consecutive columns of a row <-> the lane's halves of two blocks
@@ -596,28 +624,28 @@ struct Out {
     }
 };
 
-// All results of a wave at (row0, col0).  What a step adds to is loaded kAhead steps
+// All results of a wave at (row0, col0).  What a pair of steps adds to is loaded a pair
 // before, since the loads' way is as long as several steps.  The steps are kept apart
 // (sched_barrier): mixed, they need more registers than there are.
 template <Product MODE, typename S>
 __device__ __forceinline__ float store_wave(const ProductArgs& q, const Scalars& c, f32x4 (&acc)[S::MI][S::NJ], int batch,
                                             int row0, int col0, bool mirror, int lane) {
-    constexpr int kAcross = S::NJ / 2, kAhead = S::STEPS < 2 ? S::STEPS : 2;
+    constexpr int kAcross = S::NJ / 2, kPair = kAcross < 2 ? 1 : 2;           // steps that share lines
     const Out<MODE> out(q, c, batch, mirror, lane);
-    Added in[kAhead + 1];
+    Added in[2][kPair];
     auto fetch = [&](auto X) __attribute__((always_inline)) {
         constexpr int x = decltype(X)::value;
-        out.fetch(in[x % (kAhead + 1)], row0 + 32 * (x / kAcross), col0 + 32 * (x % kAcross));
+        out.fetch(in[x / kPair % 2], row0 + 32 * (x / kAcross), col0 + 32 * (x % kAcross));
     };
     float sum = 0.0f;
-    static_for<kAhead>([&](auto X) { fetch(X); });
+    fetch(std::integral_constant<int, 0>{});
     __builtin_amdgcn_sched_barrier(0);
     static_for<S::STEPS>([&](auto X) __attribute__((always_inline)) {
         constexpr int x = decltype(X)::value, ip = x / kAcross, pr = x % kAcross;
-        if constexpr (x + kAhead < S::STEPS) fetch(std::integral_constant<int, x + kAhead>{});
+        if constexpr (x % kPair == 0 && x + kPair < S::STEPS) fetch(std::integral_constant<int, x + kPair>{});
         const f32x4 v[2][2] = {{acc[2 * ip][2 * pr], acc[2 * ip][2 * pr + 1]},
                                {acc[2 * ip + 1][2 * pr], acc[2 * ip + 1][2 * pr + 1]}};
-        sum += out.store(v, in[x % (kAhead + 1)], row0 + 32 * ip, col0 + 32 * pr);
+        sum += out.store(v, in[x / kPair % 2][x % kPair], row0 + 32 * ip, col0 + 32 * pr);
         __builtin_amdgcn_sched_barrier(0);
     });
     return sum;
@@ -948,7 +976,7 @@ __global__ __launch_bounds__(kWave) void join_kernel(ProductArgs q, int tiles) {
     float sum = 0.0f;
     if (place.store) {
         const Out<MODE> out(q, c, batch, place.mirror, lane);
-        Added in{};
+        Added in[1];
         out.fetch(in, row0, col0);
         f32x4 acc[2][2] = {};
         const f32x4* p = q.w.sums + ((static_cast<size_t>(blockIdx.y) * q.split * S::WAVES + wave) * S::STEPS + x) * 4 * kWave + lane;
@@ -958,7 +986,7 @@ __global__ __launch_bounds__(kWave) void join_kernel(ProductArgs q, int tiles) {
             for (int e = 0; e < 4; ++e) acc[e / 2][e % 2] += p[e * kWave];
             p += static_cast<size_t>(S::WAVES) * S::STEPS * 4 * kWave;
         }
-        sum = out.store(acc, in, row0, col0);
+        sum = out.store(acc, in[0], row0, col0);
     }
     if constexpr (MODE == kMix) {
 #pragma unroll
