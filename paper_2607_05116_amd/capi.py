@@ -126,8 +126,15 @@ def _ptr(t) -> int | None:
     return t.data_ptr()
 
 
+# The current stream's handle without making a Stream object (0.2 us instead of 2.7), where torch offers it.
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int | None:
     if stream is None:
+        if _current_raw_stream is not None and _current_device is not None and torch.cuda.is_initialized():
+            return _current_raw_stream(_current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream

@@ -21,8 +21,9 @@
 // the tokens v and s only grow and one of them does at every piece, so slots are
 // distinct and there are at most waves + sequences of them, however the batch is
 // cut.  A block whose tokens all belong to one sequence joins its waves' rows in
-// LDS and leaves one piece.  The second kernel sums a sequence's pieces; the last
-// of its blocks sums the losses over the sequences.
+// LDS and leaves one piece.  A second kernel sums each sequence's pieces and a third the
+// losses over the sequences; one workgroup does both where the pieces are few, and
+// everything in one launch for a batch of at most 256 tokens.
 #include "cap_device.hpp"
 
 #include <type_traits>
@@ -98,25 +99,47 @@ __device__ __forceinline__ void row_exp(float (&v)[NV][4], float& top, float& to
     total = row_sum(s);
 }
 
-// Sequence of token t among sequences lo .. hi (it is known to be one of them):
-// the last whose offset is <= t, so an empty sequence never has a token.
-__device__ __forceinline__ int find_sequence(const int32_t* __restrict__ offs, int t, int lo, int hi) {
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (offs[mid] <= t) lo = mid; else hi = mid - 1;
-    }
-    return lo;
-}
+// The sequences that a block's tokens belong to: -1 before the first offset, S at or past
+// the last.  Found by the whole block (the offsets <= a token are counted); the offsets
+// from the first one's on are kept in LDS, so that a token's sequence is found there and
+// not by a chain of loads.
+constexpr int kSeqCache = 64;
+struct Sequences {
+    const int32_t* offs;
+    const int32_t* cache;
+    int S, first, last;
 
-// Sequences of tokens t0 and t1 (-1: before the first offset, S: at or past the
-// last), found by the whole block: the offsets <= t are counted.  Ends in a barrier.
-__device__ __forceinline__ void block_sequences(const int32_t* __restrict__ offs, int S, int t0, int t1, int* shared2,
-                                                int& s0, int& s1) {
-    if (!offs) {
-        s0 = s1 = 0;
-        return;
+    __device__ __forceinline__ int offset(int i) const {
+        const int c = i - first;
+        return c < kSeqCache ? cache[max(c, 0)] : offs[i];
     }
-    if (threadIdx.x < 2) shared2[threadIdx.x] = 0;
+    // sequence of token t, one of lo .. last: the last whose offset is <= t, so an empty
+    // sequence never has a token
+    __device__ __forceinline__ int of(int t, int lo) const {
+        if (first == last) return first;
+        lo = max(lo, first);
+        if (lo < 0) {
+            if (t < offs[0]) return -1;
+            lo = 0;
+        }
+        int hi = min(last, S);
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (offset(mid) <= t) lo = mid; else hi = mid - 1;
+        }
+        return lo;
+    }
+};
+struct SequencesLds {
+    int found[2];
+    int32_t cache[kSeqCache];
+};
+// Of tokens t0 and t1 and those between them.  Ends in a barrier.
+__device__ __forceinline__ Sequences block_sequences(const int32_t* __restrict__ offs, int S, int t0, int t1,
+                                                     SequencesLds& lds) {
+    Sequences q{offs, lds.cache, S, 0, 0};
+    if (!offs) return q;
+    if (threadIdx.x < 2) lds.found[threadIdx.x] = 0;
     __syncthreads();
     int n0 = 0, n1 = 0;
     for (int i = threadIdx.x; i <= S; i += blockDim.x) {
@@ -124,11 +147,16 @@ __device__ __forceinline__ void block_sequences(const int32_t* __restrict__ offs
         n0 += o <= t0;
         n1 += o <= t1;
     }
-    if (n0) atomicAdd(&shared2[0], n0);
-    if (n1) atomicAdd(&shared2[1], n1);
+    if (n0) atomicAdd(&lds.found[0], n0);
+    if (n1) atomicAdd(&lds.found[1], n1);
     __syncthreads();
-    s0 = __builtin_amdgcn_readfirstlane(shared2[0]) - 1;
-    s1 = max(s0, __builtin_amdgcn_readfirstlane(shared2[1]) - 1);
+    q.first = __builtin_amdgcn_readfirstlane(lds.found[0]) - 1;
+    q.last = max(q.first, __builtin_amdgcn_readfirstlane(lds.found[1]) - 1);
+    if (q.first != q.last) {
+        for (int i = threadIdx.x; i < kSeqCache; i += blockDim.x) lds.cache[i] = offs[min(max(q.first + i, 0), S)];
+        __syncthreads();
+    }
+    return q;
 }
 
 // LDS accesses of one wave stay in order; this keeps the compiler's order too.
@@ -139,23 +167,32 @@ struct LossWs {
     int32_t* csum;      // [pieces][EP] kept slots
     int32_t* nsum;      // [pieces] valid tokens
     float* zsum;        // [pieces] sums of lse^2
-    float* seq;         // [2][S] balance and z sums of each sequence
-    int32_t* done;      // finished blocks of the second kernel
-    int pieces, EP;
+    float* seq;         // [S][4] balance sums of each quarter of the experts, [S] z sums
+    int EP;
 };
 
-int loss_tokens_per_wave(int T) {
+// How a batch is cut: `per_wave` tokens a wave, `waves` waves a block.
+struct LossPlan {
+    int waves, per_wave, blocks;
+    bool one_launch, one_sum;
+};
+LossPlan loss_plan(int T, int S) {
+    LossPlan p;
+    p.one_launch = T <= 256 && S <= 64;
     // Four tokens at a time; a batch that fills the chip several times over takes
-    // 16 a wave, so that a partial row is left for 64 tokens.
-    return T >= 16384 ? 16 : T >= 4096 ? 8 : 4;
+    // 16 a wave, so that a piece is left for 64 tokens.
+    p.waves = p.one_launch ? 16 : kLossWaves;
+    p.per_wave = p.one_launch ? (T <= 64 ? 4 : 16) : T >= 16384 ? 16 : T >= 4096 ? 8 : 4;
+    p.blocks = T > 0 ? (T - 1) / (p.per_wave * p.waves) + 1 : 1;
+    p.one_sum = p.one_launch || (p.blocks <= 32 && S <= 64);
+    return p;
 }
 
 size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
 
 size_t loss_ws_layout(int T, int E, int S, void* base, LossWs* w) {
-    const int per_wave = loss_tokens_per_wave(T);
-    const int blocks = T > 0 ? (T - 1) / (per_wave * kLossWaves) + 1 : 0;
-    const size_t pieces = static_cast<size_t>(blocks) * kLossWaves + S;
+    const LossPlan plan = loss_plan(T, S);
+    const size_t pieces = static_cast<size_t>(plan.blocks) * plan.waves + S;
     const size_t EP = (E + 3) & ~3;
     size_t at = 0;
     char* p = static_cast<char*>(base);
@@ -168,47 +205,183 @@ size_t loss_ws_layout(int T, int E, int S, void* base, LossWs* w) {
     char* b = take(pieces * EP * 4);
     char* c = take(pieces * 4);
     char* d = take(pieces * 4);
-    char* e = take(static_cast<size_t>(S) * 8);
-    char* f = take(4);
+    char* e = take(static_cast<size_t>(S) * 20);
     if (w) {
         w->psum = reinterpret_cast<float*>(a);
         w->csum = reinterpret_cast<int32_t*>(b);
         w->nsum = reinterpret_cast<int32_t*>(c);
         w->zsum = reinterpret_cast<float*>(d);
         w->seq = reinterpret_cast<float*>(e);
-        w->done = reinterpret_cast<int32_t*>(f);
-        w->pieces = static_cast<int>(pieces);
         w->EP = static_cast<int>(EP);
     }
     return at;
 }
 
-template <int NV, bool VEC>
-__global__ __launch_bounds__(kLossThreads) void loss_pieces_kernel(
-    int T, int k, int E, const float* __restrict__ logits, const int32_t* __restrict__ idx,
-    const uint8_t* __restrict__ keep, const uint8_t* __restrict__ mask, const int32_t* __restrict__ offs, int S,
-    int per_wave, LossWs ws) {
-    __shared__ int hist[kLossWaves][kMaxE];
-    __shared__ float part[kLossWaves][kMaxE];
-    __shared__ int part_n[kLossWaves];
-    __shared__ float part_z[kLossWaves];
-    __shared__ int found[2];
+struct LossArgs {
+    int T, k, E, S, per_wave;
+    const float* logits;
+    const int32_t* idx;
+    const uint8_t *keep, *mask;
+    const int32_t* offs;
+    float balance_coef, z_coef;
+    int32_t* counts;
+    float* probs;
+    int32_t* tokens;
+    float* loss;
+    LossWs ws;
+};
+
+// add(slot) for the pieces of sequence s (tokens a .. b - 1) that worker `me` of `of` takes.
+// waves: of the blocks that left the pieces; 0: each piece is a wave's.
+template <typename Add>
+__device__ __forceinline__ void each_piece(const LossArgs& q, int waves, int s, int a, int b, int me, int of, Add&& add) {
+    if (a >= b) return;
+    if (waves == 0) {
+        for (int v = a / q.per_wave + me; v <= (b - 1) / q.per_wave; v += of) add(static_cast<size_t>(v) + s);
+        return;
+    }
+    const int per_block = q.per_wave * waves;
+    const int b0 = a / per_block, b1 = (b - 1) / per_block;
+    // token blocks that lie in the sequence whole left one piece
+    const int m0 = a == b0 * per_block ? b0 : b0 + 1;
+    const int m1 = b == min(q.T, (b1 + 1) * per_block) ? b1 : b1 - 1;
+#pragma unroll 4
+    for (int i = m0 + me; i <= m1; i += of) add(static_cast<size_t>(i) * waves + s);
+    // the waves of the others that have tokens of the sequence
+    auto edge = [&](int block) {
+        const int w0 = max(a / q.per_wave, block * waves);
+        const int w1 = min((b - 1) / q.per_wave, block * waves + waves - 1);
+        for (int v = w0 + me; v <= w1; v += of) add(static_cast<size_t>(v) + s);
+    };
+    if (m0 > b0) edge(b0);
+    if (m1 < b1 && (b1 > b0 || m0 == b0)) edge(b1);
+}
+
+__device__ __forceinline__ void sequence_range(const LossArgs& q, int s, int& a, int& b) {
+    a = q.offs ? max(0, min(q.offs[s], q.T)) : 0;
+    b = q.offs ? max(a, min(q.offs[s + 1], q.T)) : q.T;
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// The losses from their sums over the sequences.
+__device__ __forceinline__ void write_loss(const LossArgs& q, float bal, float zz, int present, int total) {
+    q.tokens[q.S] = present;
+    q.tokens[q.S + 1] = total;
+    bal = present > 0 ? bal / static_cast<float>(present) : 0.0f;
+    zz = total > 0 ? zz / static_cast<float>(total) : 0.0f;
+    // a loss that is switched off adds nothing, not 0 * inf (rows at the lowest value have an infinite lse^2)
+    q.loss[0] = (q.balance_coef != 0.0f ? q.balance_coef * bal : 0.0f) + (q.z_coef != 0.0f ? q.z_coef * zz : 0.0f);
+    q.loss[1] = bal;
+    q.loss[2] = zz;
+}
+
+// All sequences and the losses by one workgroup: a wave for every 16th sequence, lane l
+// holds columns 4 l .. + 3.  waves: as each_piece.
+__device__ __forceinline__ void sum_all(const LossArgs& q, int waves) {
+    __shared__ float bal_w[kSumWaves], z_w[kSumWaves];
+    __shared__ int present_w[kSumWaves], total_w[kSumWaves];
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    float bal = 0.0f, zz = 0.0f;
+    int present = 0, total = 0;
+    for (int s = wave; s < q.S; s += kSumWaves) {
+        int a, b;
+        sequence_range(q, s, a, b);
+        f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
+        int c[4] = {0, 0, 0, 0};
+        int n = 0;
+        float z = 0.0f;
+        each_piece(q, waves, s, a, b, 0, 1, [&](size_t slot) __attribute__((always_inline)) {
+            if (4 * lane < q.ws.EP) {
+                p += *reinterpret_cast<const f32x4*>(q.ws.psum + slot * q.ws.EP + 4 * lane);
+                const u32x4 v = *reinterpret_cast<const u32x4*>(q.ws.csum + slot * q.ws.EP + 4 * lane);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) c[i] += static_cast<int>(v[i]);
+            }
+            n += q.ws.nsum[slot];
+            z += q.ws.zsum[slot];
+        });
+        float term = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (4 * lane + i < q.E) {
+                const float mean = n > 0 ? p[i] / static_cast<float>(n) : 0.0f;
+                q.probs[static_cast<size_t>(s) * q.E + 4 * lane + i] = mean;
+                q.counts[static_cast<size_t>(s) * q.E + 4 * lane + i] = c[i];
+                term = __builtin_fmaf(static_cast<float>(c[i]), mean, term);
+            }
+        term = wave_sum(term);
+        if (n > 0) bal += term * (static_cast<float>(q.E) / static_cast<float>(q.k) / static_cast<float>(n));
+        zz += z;
+        present += n > 0;
+        total += n;
+        if (lane == 0) q.tokens[s] = n;
+    }
+    if (lane == 0) {
+        bal_w[wave] = bal;
+        z_w[wave] = zz;
+        present_w[wave] = present;
+        total_w[wave] = total;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kSumWaves; ++w) {
+            bal += bal_w[w];
+            zz += z_w[w];
+            present += present_w[w];
+            total += total_w[w];
+        }
+        write_loss(q, bal, zz, present, total);
+    }
+}
+
+// WAVES == 16: the whole batch in one workgroup, which then sums its pieces too.
+template <int NV, bool VEC, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave) void loss_pieces_kernel(LossArgs q) {
+    constexpr bool ALL = WAVES == kSumWaves;
+    __shared__ int hist[WAVES][64 * NV];
+    __shared__ float part[ALL ? 1 : WAVES][64 * NV];
+    __shared__ int part_n[WAVES];
+    __shared__ float part_z[WAVES];
+    __shared__ SequencesLds found;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const int g = lane / kRowLanes, j = lane % kRowLanes;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *ws.done = 0;
-    const int block_t0 = blockIdx.x * per_wave * kLossWaves;
-    const int block_t1 = min(T, block_t0 + per_wave * kLossWaves);
-    int s0, s1;
-    block_sequences(offs, S, block_t0, block_t1 - 1, found, s0, s1);
-    for (int i = lane; i < kMaxE; i += kWave) hist[wave][i] = 0;
+    const int T = q.T, k = q.k, E = q.E, S = q.S;
+    const LossWs& ws = q.ws;
+    const int block_t0 = blockIdx.x * q.per_wave * WAVES;
+    const int block_t1 = min(T, block_t0 + q.per_wave * WAVES);
+    for (int i = lane; i < 64 * NV; i += kWave) hist[wave][i] = 0;
+    const Sequences seq = block_sequences(q.offs, S, block_t0, block_t1 - 1, found);
     wave_fence();
 
-    const int wave_id = blockIdx.x * kLossWaves + wave;
-    const int a = min(block_t1, block_t0 + wave * per_wave), b = min(block_t1, a + per_wave);
+    const int wave_id = blockIdx.x * WAVES + wave;
+    const int a = min(block_t1, block_t0 + wave * q.per_wave), b = min(block_t1, a + q.per_wave);
     float sum[NV][4];
     float zsum = 0.0f;
     int n = 0;
 
+    // four tokens: their logits, and the expert of lane j's slot (-1: none)
+    struct Rows {
+        float v[NV][4];
+        int e;
+        bool valid;
+    };
+    auto load = [&](Rows& x, int t4, int to) __attribute__((always_inline)) {
+        const int t = t4 + g;
+        const bool in = t < to;
+        const size_t tc = in ? t : to - 1;
+        load_row<NV, VEC>(q.logits + tc * E, E, j, x.v);
+        x.e = -1;
+        if (in && j < k) {
+            x.e = q.idx[tc * k + j];
+            if (q.keep && !q.keep[tc * k + j]) x.e = -1;
+        }
+        x.valid = in && (!q.mask || q.mask[tc] != 0);
+    };
     auto tokens = [&](int from, int to) __attribute__((always_inline)) {
 #pragma unroll
         for (int c = 0; c < NV; ++c)
@@ -216,30 +389,23 @@ __global__ __launch_bounds__(kLossThreads) void loss_pieces_kernel(
             for (int i = 0; i < 4; ++i) sum[c][i] = 0.0f;
         zsum = 0.0f;
         n = 0;
+        Rows next;
+        if (from < to) load(next, from, to);
         for (int t4 = from; t4 < to; t4 += kTokPerStep) {
-            const int t = t4 + g;
-            const bool in = t < to;
-            const size_t tc = in ? t : to - 1;
-            float v[NV][4];
-            load_row<NV, VEC>(logits + tc * E, E, j, v);
-            int e = -1;
-            if (in && j < k) {
-                e = idx[tc * k + j];
-                if (keep && !keep[tc * k + j]) e = -1;
-            }
+            Rows x = next;
+            if (t4 + kTokPerStep < to) load(next, t4 + kTokPerStep, to);       // on their way during this step
             float top, total;
-            row_exp<NV>(v, top, total);
-            const bool valid = in && !(top == -INFINITY) && (!mask || mask[tc] != 0);
-            if (valid) {
+            row_exp<NV>(x.v, top, total);
+            if (x.valid && !(top == -INFINITY)) {
                 const float inv = 1.0f / total;
 #pragma unroll
                 for (int c = 0; c < NV; ++c)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[c][i] = __builtin_fmaf(v[c][i], inv, sum[c][i]);
+                    for (int i = 0; i < 4; ++i) sum[c][i] = __builtin_fmaf(x.v[c][i], inv, sum[c][i]);
                 const float lse = top + logf(total);
                 zsum = __builtin_fmaf(lse, lse, zsum);
                 n += 1;
-                if (static_cast<unsigned>(e) < static_cast<unsigned>(E)) atomicAdd(&hist[wave][e], 1);
+                if (static_cast<unsigned>(x.e) < static_cast<unsigned>(E)) atomicAdd(&hist[wave][x.e], 1);
             }
         }
         // over the wave's four rows
@@ -257,27 +423,26 @@ __global__ __launch_bounds__(kLossThreads) void loss_pieces_kernel(
         wave_fence();
     };
 
-    if (s0 == s1) {                                  // block-uniform: one piece
-        if (s0 < 0 || s0 >= S) return;
+    if (!ALL && seq.first == seq.last) {             // the block's tokens are of one sequence: one piece
+        if (seq.first < 0 || seq.first >= S) return;
         tokens(a, b);
         if (g == 0) {
 #pragma unroll
             for (int c = 0; c < NV; ++c)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) part[wave][64 * c + 4 * j + i] = sum[c][i];
+                *reinterpret_cast<f32x4*>(&part[wave][64 * c + 4 * j]) = f32x4{sum[c][0], sum[c][1], sum[c][2], sum[c][3]};
         }
         if (lane == 0) {
             part_n[wave] = n;
             part_z[wave] = zsum;
         }
         __syncthreads();
-        const size_t slot = static_cast<size_t>(blockIdx.x) * kLossWaves + s0;
+        const size_t slot = static_cast<size_t>(blockIdx.x) * WAVES + seq.first;
         const int e = threadIdx.x;
         if (e < ws.EP) {
             float p = 0.0f;
             int c = 0;
 #pragma unroll
-            for (int w = 0; w < kLossWaves; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 p += part[w][e];
                 c += hist[w][e];
             }
@@ -287,7 +452,7 @@ __global__ __launch_bounds__(kLossThreads) void loss_pieces_kernel(
         if (e == 0) {
             int m = 0;
             float z = 0.0f;
-            for (int w = 0; w < kLossWaves; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 m += part_n[w];
                 z += part_z[w];
             }
@@ -297,10 +462,11 @@ __global__ __launch_bounds__(kLossThreads) void loss_pieces_kernel(
         return;
     }
     int at = a;
-    int s = s0;
+    int s = seq.first;
     while (at < b) {                                 // the wave's sequences
-        s = s < 0 && at < offs[0] ? -1 : find_sequence(offs, at, max(s, 0), min(s1, S));
-        const int end = s >= S ? b : min(b, max(at + 1, offs[s + 1]));
+        s = seq.of(at, s);
+        // (one sequence: its offsets are not kept)
+        const int end = seq.first == seq.last || s >= S ? b : min(b, max(at + 1, seq.offset(s + 1)));
         if (s >= 0 && s < S) {
             tokens(at, end);
             const size_t slot = static_cast<size_t>(wave_id) + s;
@@ -325,142 +491,111 @@ __global__ __launch_bounds__(kLossThreads) void loss_pieces_kernel(
         }
         at = end;
     }
+    if constexpr (ALL) {
+        __syncthreads();
+        sum_all(q, 0);
+    }
 }
 
-// Sum of v over the block's 1024 threads, in a fixed order; every thread gets it.
-__device__ __forceinline__ float block_sum(float v, float* shared) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-    __syncthreads();
-    if (threadIdx.x % kWave == 0) shared[threadIdx.x / kWave] = v;
-    __syncthreads();
-    float r = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kSumWaves; ++w) r += shared[w];
-    return r;
-}
+__global__ __launch_bounds__(kSumThreads) void loss_sum_all_kernel(LossArgs q) { sum_all(q, kLossWaves); }
 
-// One block per sequence: wave w sums the pieces of token blocks w, w + 16, ..;
-// lane l holds columns 4 l .. + 3.
-__global__ __launch_bounds__(kSumThreads) void loss_sum_kernel(
-    int T, int k, int E, const int32_t* __restrict__ offs, int S, int per_wave, float balance_coef, float z_coef,
-    int32_t* __restrict__ counts, float* __restrict__ probs, int32_t* __restrict__ tokens, float* __restrict__ loss,
-    LossWs ws) {
-    __shared__ float psum[kSumWaves][kMaxE];
-    __shared__ int csum[kSumWaves][kMaxE];
-    __shared__ int nsum[kSumWaves];
-    __shared__ float zsum[kSumWaves];
-    __shared__ float red[kSumWaves];
-    __shared__ int last;
-    const int s = blockIdx.x;
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    const int per_block = per_wave * kLossWaves;
-    const int a = offs ? max(0, min(offs[s], T)) : 0;
-    const int b = offs ? max(a, min(offs[s + 1], T)) : T;
-
+// Sequence blockIdx.x, columns 64 blockIdx.y .. + 63: 16 groups of 16 lanes share the pieces.
+__global__ __launch_bounds__(256) void loss_sum_kernel(LossArgs q) {
+    __shared__ f32x4 psum[16][16];
+    __shared__ u32x4 csum[16][16];
+    __shared__ int nsum[16];
+    __shared__ float zsum[16];
+    const int s = blockIdx.x, quarter = blockIdx.y;
+    const int group = threadIdx.x / 16, j = threadIdx.x % 16;
+    const int col = 64 * quarter + 4 * j;
+    int a, b;
+    sequence_range(q, s, a, b);
     f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
-    int c[4] = {0, 0, 0, 0};
+    u32x4 c = {0, 0, 0, 0};
     int n = 0;
     float z = 0.0f;
-    auto add = [&](size_t slot) __attribute__((always_inline)) {
-        if (4 * lane < ws.EP) {
-            p += *reinterpret_cast<const f32x4*>(ws.psum + slot * ws.EP + 4 * lane);
-            const u32x4 q = *reinterpret_cast<const u32x4*>(ws.csum + slot * ws.EP + 4 * lane);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) c[i] += static_cast<int>(q[i]);
+    each_piece(q, kLossWaves, s, a, b, group, 16, [&](size_t slot) __attribute__((always_inline)) {
+        if (col < q.ws.EP) {
+            p += *reinterpret_cast<const f32x4*>(q.ws.psum + slot * q.ws.EP + col);
+            c += *reinterpret_cast<const u32x4*>(q.ws.csum + slot * q.ws.EP + col);
         }
-        n += ws.nsum[slot];
-        z += ws.zsum[slot];
-    };
-    if (a < b) {
-        const int b0 = a / per_block, b1 = (b - 1) / per_block;
-        // token blocks that lie in the sequence whole left one piece
-        const int m0 = a == b0 * per_block ? b0 : b0 + 1;
-        const int m1 = b == min(T, (b1 + 1) * per_block) ? b1 : b1 - 1;
-#pragma unroll 4
-        for (int i = m0 + wave; i <= m1; i += kSumWaves) add(static_cast<size_t>(i) * kLossWaves + s);
-        // the waves of the others that have tokens of the sequence
-        auto edge = [&](int block) {
-            const int w0 = max(a / per_wave, block * kLossWaves);
-            const int w1 = min((b - 1) / per_wave, block * kLossWaves + kLossWaves - 1);
-            for (int v = w0; v <= w1; ++v) add(static_cast<size_t>(v) + s);
-        };
-        if (wave == 0 && m0 > b0) edge(b0);
-        if (wave == 1 && m1 < b1 && (b1 > b0 || m0 == b0)) edge(b1);
-    }
-    *reinterpret_cast<f32x4*>(&psum[wave][4 * lane]) = p;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) csum[wave][4 * lane + i] = c[i];
-    if (lane == 0) {
-        nsum[wave] = n;
-        zsum[wave] = z;
+        n += q.ws.nsum[slot];
+        z += q.ws.zsum[slot];
+    });
+    psum[group][j] = p;
+    csum[group][j] = c;
+    if (j == 0) {
+        nsum[group] = n;
+        zsum[group] = z;
     }
     __syncthreads();
     int nt = 0;
     float zt = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kSumWaves; ++w) {
+    for (int w = 0; w < 16; ++w) {
         nt += nsum[w];
         zt += zsum[w];
     }
-    const float inv_n = nt > 0 ? 1.0f / static_cast<float>(nt) : 0.0f;
+    // thread e of the first 64: column 64 quarter + e
     float term = 0.0f;
-    const int e = threadIdx.x;
-    if (e < E) {
+    if (threadIdx.x < 64) {
+        const int e = 64 * quarter + threadIdx.x;
         float ps = 0.0f;
         int cs = 0;
 #pragma unroll
-        for (int w = 0; w < kSumWaves; ++w) {
-            ps += psum[w][e];
-            cs += csum[w][e];
+        for (int w = 0; w < 16; ++w) {
+            ps += psum[w][threadIdx.x / 4][threadIdx.x % 4];
+            cs += static_cast<int>(csum[w][threadIdx.x / 4][threadIdx.x % 4]);
         }
-        ps = nt > 0 ? ps / static_cast<float>(nt) : 0.0f;
-        const size_t at = static_cast<size_t>(s) * E + e;
-        probs[at] = ps;
-        counts[at] = cs;
-        term = static_cast<float>(cs) * ps;
+        if (e < q.E) {
+            ps = nt > 0 ? ps / static_cast<float>(nt) : 0.0f;
+            q.probs[static_cast<size_t>(s) * q.E + e] = ps;
+            q.counts[static_cast<size_t>(s) * q.E + e] = cs;
+            term = static_cast<float>(cs) * ps;
+        }
+        term = wave_sum(term);
+        if (threadIdx.x == 0) {
+            q.ws.seq[4 * static_cast<size_t>(s) + quarter] =
+                nt > 0 ? term * (static_cast<float>(q.E) / static_cast<float>(q.k) / static_cast<float>(nt)) : 0.0f;
+            if (quarter == 0) {
+                q.ws.seq[4 * static_cast<size_t>(q.S) + s] = zt;
+                q.tokens[s] = nt;
+            }
+        }
     }
-    const float dot = block_sum(term, red);
-    if (threadIdx.x == 0) {
-        const float scale = static_cast<float>(E) / static_cast<float>(k) * inv_n;
-        __hip_atomic_store(&ws.seq[s], dot * scale, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(&ws.seq[S + s], zt, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(&tokens[s], nt, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        last = __hip_atomic_fetch_add(ws.done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == S - 1;
-    }
-    __syncthreads();
-    if (!last) return;
-    // the last block: sums over the sequences
+}
+
+// The losses: sums over the sequences.
+__global__ __launch_bounds__(256) void loss_final_kernel(LossArgs q, int quarters) {
+    __shared__ float bal_w[4], z_w[4];
+    __shared__ int present_w[4], total_w[4];
     float bal = 0.0f, zz = 0.0f;
     int present = 0, total = 0;
-    for (int i = threadIdx.x; i < S; i += kSumThreads) {
-        bal += __hip_atomic_load(&ws.seq[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        zz += __hip_atomic_load(&ws.seq[S + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        const int m = __hip_atomic_load(&tokens[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int s = threadIdx.x; s < q.S; s += 256) {
+        for (int x = 0; x < quarters; ++x) bal += q.ws.seq[4 * static_cast<size_t>(s) + x];
+        zz += q.ws.seq[4 * static_cast<size_t>(q.S) + s];
+        const int m = q.tokens[s];
         present += m > 0;
         total += m;
     }
-    bal = block_sum(bal, red);
-    zz = block_sum(zz, red);
-    // token totals as whole numbers
-    __shared__ int ints[2];
-    if (threadIdx.x < 2) ints[threadIdx.x] = 0;
-    __syncthreads();
-    if (present) atomicAdd(&ints[0], present);
-    if (total) atomicAdd(&ints[1], total);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        present = ints[0];
-        total = ints[1];
-        tokens[S] = present;
-        tokens[S + 1] = total;
-        bal = present > 0 ? bal / static_cast<float>(present) : 0.0f;
-        zz = total > 0 ? zz / static_cast<float>(total) : 0.0f;
-        // a loss that is switched off adds nothing, not 0 * inf (rows at the lowest value have an infinite lse^2)
-        loss[0] = (balance_coef != 0.0f ? balance_coef * bal : 0.0f) + (z_coef != 0.0f ? z_coef * zz : 0.0f);
-        loss[1] = bal;
-        loss[2] = zz;
+    bal = wave_sum(bal);
+    zz = wave_sum(zz);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        present += __shfl_xor(present, o);
+        total += __shfl_xor(total, o);
     }
+    if (threadIdx.x % kWave == 0) {
+        bal_w[threadIdx.x / kWave] = bal;
+        z_w[threadIdx.x / kWave] = zz;
+        present_w[threadIdx.x / kWave] = present;
+        total_w[threadIdx.x / kWave] = total;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0)
+        write_loss(q, (bal_w[0] + bal_w[1]) + (bal_w[2] + bal_w[3]), (z_w[0] + z_w[1]) + (z_w[2] + z_w[3]),
+                   present_w[0] + present_w[1] + present_w[2] + present_w[3],
+                   total_w[0] + total_w[1] + total_w[2] + total_w[3]);
 }
 
 // Gradient of the logits: each wave four tokens at a time, `steps` times.  The
@@ -473,13 +608,12 @@ __global__ __launch_bounds__(kLossThreads) void router_grad_kernel(
     const int32_t* __restrict__ tokens, float balance_coef, float z_coef, const float* __restrict__ d_loss, int steps,
     void* __restrict__ out) {
     __shared__ __attribute__((aligned(16))) float gates[kLossThreads / kRowLanes][64 * NV];
-    __shared__ int found[2];
+    __shared__ SequencesLds found;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const int row = threadIdx.x / kRowLanes, g = lane / kRowLanes, j = lane % kRowLanes;
     const int per_block = kLossWaves * kTokPerStep * steps;
     const int block_t0 = blockIdx.x * per_block;
-    int s0, s1;
-    block_sequences(offs, S, block_t0, min(T, block_t0 + per_block) - 1, found, s0, s1);
+    const Sequences seq = block_sequences(offs, S, block_t0, min(T, block_t0 + per_block) - 1, found);
 #pragma unroll
     for (int c = 0; c < NV; ++c)
         *reinterpret_cast<f32x4*>(&gates[row][64 * c + 4 * j]) = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -507,7 +641,7 @@ __global__ __launch_bounds__(kLossThreads) void router_grad_kernel(
                 dw = d_w[tt * k + j];
             }
         }
-        const int s = s0 == s1 ? s0 : (offs[0] > t ? -1 : find_sequence(offs, t, max(s0, 0), min(s1, S)));
+        const int s = seq.of(t, seq.first);
         const bool inside = s >= 0 && s < S;
         float top, total;
         row_exp<NV>(v, top, total);
@@ -598,26 +732,29 @@ cap_status balance_loss_launch(int T, int k, int E, const float* logits, const i
                                const uint8_t* mask, const int32_t* offs, int S, float balance_coef, float z_coef,
                                int32_t* counts, float* probs, int32_t* tokens, float* loss, void* workspace,
                                hipStream_t stream) {
-    LossWs ws;
-    loss_ws_layout(T, E, S, workspace, &ws);
-    const int per_wave = loss_tokens_per_wave(T);
-    const int blocks = T > 0 ? (T - 1) / (per_wave * kLossWaves) + 1 : 1;
+    const LossPlan plan = loss_plan(T, S);
+    LossArgs q{T, k, E, S, plan.per_wave, logits, idx, keep, mask, offs, balance_coef, z_coef, counts, probs, tokens, loss, {}};
+    loss_ws_layout(T, E, S, workspace, &q.ws);
     const bool vec = E % 4 == 0 && aligned(logits, 16);
     auto launch = [&](auto NV) {
         constexpr int nv = decltype(NV)::value;
-        if (vec)
-            loss_pieces_kernel<nv, true><<<blocks, kLossThreads, 0, stream>>>(T, k, E, logits, idx, keep, mask, offs, S,
-                                                                             per_wave, ws);
-        else
-            loss_pieces_kernel<nv, false><<<blocks, kLossThreads, 0, stream>>>(T, k, E, logits, idx, keep, mask, offs,
-                                                                              S, per_wave, ws);
+        constexpr int all = kSumWaves, few = kLossWaves;
+        if (plan.one_launch && vec) loss_pieces_kernel<nv, true, all><<<1, kSumThreads, 0, stream>>>(q);
+        else if (plan.one_launch) loss_pieces_kernel<nv, false, all><<<1, kSumThreads, 0, stream>>>(q);
+        else if (vec) loss_pieces_kernel<nv, true, few><<<plan.blocks, kLossThreads, 0, stream>>>(q);
+        else loss_pieces_kernel<nv, false, few><<<plan.blocks, kLossThreads, 0, stream>>>(q);
     };
     if (E <= 64) launch(std::integral_constant<int, 1>{});
     else if (E <= 128) launch(std::integral_constant<int, 2>{});
     else launch(std::integral_constant<int, 4>{});
-    CAP_LAUNCH_CHECK();
-    loss_sum_kernel<<<S, kSumThreads, 0, stream>>>(T, k, E, offs, S, per_wave, balance_coef, z_coef, counts, probs,
-                                                   tokens, loss, ws);
+    if (plan.one_launch) {
+    } else if (plan.one_sum) {
+        loss_sum_all_kernel<<<1, kSumThreads, 0, stream>>>(q);
+    } else {
+        const int quarters = (E + 63) / 64;
+        loss_sum_kernel<<<dim3(S, quarters), 256, 0, stream>>>(q);
+        loss_final_kernel<<<1, 256, 0, stream>>>(q, quarters);
+    }
     CAP_LAUNCH_CHECK();
     return CAP_OK;
 }
