@@ -33,8 +33,10 @@ namespace {
 
 constexpr int kRowLanes = 16;                        // lanes that hold one token's row
 constexpr int kTokPerStep = kWave / kRowLanes;       // tokens of a wave at a time
-constexpr int kLossWaves = 4;                        // waves per block, both directions
+constexpr int kLossWaves = 8;                        // waves of a block of the loss, of the gradient
 constexpr int kLossThreads = kLossWaves * kWave;
+constexpr int kGradWaves = 4;
+constexpr int kGradThreads = kGradWaves * kWave;
 constexpr int kSumThreads = 1024;
 constexpr int kSumWaves = kSumThreads / kWave;
 
@@ -180,11 +182,11 @@ LossPlan loss_plan(int T, int S) {
     LossPlan p;
     p.one_launch = T <= 256 && S <= 64;
     // Four tokens at a time; a batch that fills the chip several times over takes
-    // 16 a wave, so that a piece is left for 64 tokens.
+    // 16 a wave, so that a piece is left for 128 tokens.
     p.waves = p.one_launch ? 16 : kLossWaves;
-    p.per_wave = p.one_launch ? (T <= 64 ? 4 : 16) : T >= 16384 ? 16 : T >= 4096 ? 8 : 4;
+    p.per_wave = p.one_launch ? (T <= 64 ? 4 : 16) : T >= 16384 ? 16 : 4;
     p.blocks = T > 0 ? (T - 1) / (p.per_wave * p.waves) + 1 : 1;
-    p.one_sum = p.one_launch || (p.blocks <= 32 && S <= 64);
+    p.one_sum = p.one_launch || (p.blocks <= 16 && S <= 64);
     return p;
 }
 
@@ -355,33 +357,34 @@ __global__ __launch_bounds__(WAVES * kWave) void loss_pieces_kernel(LossArgs q) 
     const int block_t0 = blockIdx.x * q.per_wave * WAVES;
     const int block_t1 = min(T, block_t0 + q.per_wave * WAVES);
     for (int i = lane; i < 64 * NV; i += kWave) hist[wave][i] = 0;
-    const Sequences seq = block_sequences(q.offs, S, block_t0, block_t1 - 1, found);
-    wave_fence();
-
     const int wave_id = blockIdx.x * WAVES + wave;
     const int a = min(block_t1, block_t0 + wave * q.per_wave), b = min(block_t1, a + q.per_wave);
-    float sum[NV][4];
-    float zsum = 0.0f;
-    int n = 0;
-
     // four tokens: their logits, and the expert of lane j's slot (-1: none)
     struct Rows {
         float v[NV][4];
         int e;
         bool valid;
     };
-    auto load = [&](Rows& x, int t4, int to) __attribute__((always_inline)) {
+    auto load = [&](Rows& x, int t4) __attribute__((always_inline)) {
         const int t = t4 + g;
-        const bool in = t < to;
-        const size_t tc = in ? t : to - 1;
+        const size_t tc = min(t, b - 1);
         load_row<NV, VEC>(q.logits + tc * E, E, j, x.v);
         x.e = -1;
-        if (in && j < k) {
+        if (j < k) {
             x.e = q.idx[tc * k + j];
             if (q.keep && !q.keep[tc * k + j]) x.e = -1;
         }
-        x.valid = in && (!q.mask || q.mask[tc] != 0);
+        x.valid = !q.mask || q.mask[tc] != 0;
     };
+    // the first are on their way while the block finds its sequences
+    Rows next;
+    if (a < b) load(next, a);
+    const Sequences seq = block_sequences(q.offs, S, block_t0, block_t1 - 1, found);
+    wave_fence();
+    float sum[NV][4];
+    float zsum = 0.0f;
+    int n = 0;
+
     auto tokens = [&](int from, int to) __attribute__((always_inline)) {
 #pragma unroll
         for (int c = 0; c < NV; ++c)
@@ -389,14 +392,13 @@ __global__ __launch_bounds__(WAVES * kWave) void loss_pieces_kernel(LossArgs q) 
             for (int i = 0; i < 4; ++i) sum[c][i] = 0.0f;
         zsum = 0.0f;
         n = 0;
-        Rows next;
-        if (from < to) load(next, from, to);
+        if (from > a && from < to) load(next, from);
         for (int t4 = from; t4 < to; t4 += kTokPerStep) {
             Rows x = next;
-            if (t4 + kTokPerStep < to) load(next, t4 + kTokPerStep, to);       // on their way during this step
+            if (t4 + kTokPerStep < to) load(next, t4 + kTokPerStep);           // on their way during this step
             float top, total;
             row_exp<NV>(x.v, top, total);
-            if (x.valid && !(top == -INFINITY)) {
+            if (t4 + g < to && x.valid && !(top == -INFINITY)) {
                 const float inv = 1.0f / total;
 #pragma unroll
                 for (int c = 0; c < NV; ++c)
@@ -499,12 +501,14 @@ __global__ __launch_bounds__(WAVES * kWave) void loss_pieces_kernel(LossArgs q) 
 
 __global__ __launch_bounds__(kSumThreads) void loss_sum_all_kernel(LossArgs q) { sum_all(q, kLossWaves); }
 
-// Sequence blockIdx.x, columns 64 blockIdx.y .. + 63: 16 groups of 16 lanes share the pieces.
-__global__ __launch_bounds__(256) void loss_sum_kernel(LossArgs q) {
-    __shared__ f32x4 psum[16][16];
-    __shared__ u32x4 csum[16][16];
-    __shared__ int nsum[16];
-    __shared__ float zsum[16];
+// Sequence blockIdx.x, columns 64 blockIdx.y .. + 63: GROUPS groups of 16 lanes share the
+// pieces.
+template <int GROUPS>
+__global__ __launch_bounds__(GROUPS * 16) void loss_sum_kernel(LossArgs q) {
+    __shared__ f32x4 psum[GROUPS][16];
+    __shared__ u32x4 csum[GROUPS][16];
+    __shared__ int nsum[GROUPS];
+    __shared__ float zsum[GROUPS];
     const int s = blockIdx.x, quarter = blockIdx.y;
     const int group = threadIdx.x / 16, j = threadIdx.x % 16;
     const int col = 64 * quarter + 4 * j;
@@ -514,7 +518,7 @@ __global__ __launch_bounds__(256) void loss_sum_kernel(LossArgs q) {
     u32x4 c = {0, 0, 0, 0};
     int n = 0;
     float z = 0.0f;
-    each_piece(q, kLossWaves, s, a, b, group, 16, [&](size_t slot) __attribute__((always_inline)) {
+    each_piece(q, kLossWaves, s, a, b, group, GROUPS, [&](size_t slot) __attribute__((always_inline)) {
         if (col < q.ws.EP) {
             p += *reinterpret_cast<const f32x4*>(q.ws.psum + slot * q.ws.EP + col);
             c += *reinterpret_cast<const u32x4*>(q.ws.csum + slot * q.ws.EP + col);
@@ -529,23 +533,18 @@ __global__ __launch_bounds__(256) void loss_sum_kernel(LossArgs q) {
         zsum[group] = z;
     }
     __syncthreads();
-    int nt = 0;
-    float zt = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-        nt += nsum[w];
-        zt += zsum[w];
-    }
-    // thread e of the first 64: column 64 quarter + e
+    // thread e of the first wave: column 64 quarter + e
     float term = 0.0f;
     if (threadIdx.x < 64) {
         const int e = 64 * quarter + threadIdx.x;
-        float ps = 0.0f;
-        int cs = 0;
-#pragma unroll
-        for (int w = 0; w < 16; ++w) {
+        float ps = 0.0f, zt = 0.0f;
+        int cs = 0, nt = 0;
+#pragma unroll 16
+        for (int w = 0; w < GROUPS; ++w) {
             ps += psum[w][threadIdx.x / 4][threadIdx.x % 4];
             cs += static_cast<int>(csum[w][threadIdx.x / 4][threadIdx.x % 4]);
+            nt += nsum[w];
+            zt += zsum[w];
         }
         if (e < q.E) {
             ps = nt > 0 ? ps / static_cast<float>(nt) : 0.0f;
@@ -601,51 +600,70 @@ __global__ __launch_bounds__(256) void loss_final_kernel(LossArgs q, int quarter
 // Gradient of the logits: each wave four tokens at a time, `steps` times.  The
 // gates' part goes from the slots' lanes to the columns' lanes through a row of LDS.
 template <int NV, bool VEC, bool BF16>
-__global__ __launch_bounds__(kLossThreads) void router_grad_kernel(
+__global__ __launch_bounds__(kGradThreads) void router_grad_kernel(
     int T, int k, int E, const float* __restrict__ logits, const int32_t* __restrict__ idx,
     const uint8_t* __restrict__ keep, const float* __restrict__ w, const float* __restrict__ d_w,
     const uint8_t* __restrict__ mask, const int32_t* __restrict__ offs, int S, const int32_t* __restrict__ counts,
     const int32_t* __restrict__ tokens, float balance_coef, float z_coef, const float* __restrict__ d_loss, int steps,
     void* __restrict__ out) {
-    __shared__ __attribute__((aligned(16))) float gates[kLossThreads / kRowLanes][64 * NV];
+    __shared__ __attribute__((aligned(16))) float gates[kGradThreads / kRowLanes][64 * NV];
     __shared__ SequencesLds found;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const int row = threadIdx.x / kRowLanes, g = lane / kRowLanes, j = lane % kRowLanes;
-    const int per_block = kLossWaves * kTokPerStep * steps;
+    const int per_block = kGradWaves * kTokPerStep * steps;
     const int block_t0 = blockIdx.x * per_block;
+    // four tokens: their logits and lane j's slot (expert -1: none)
+    struct Rows {
+        float v[NV][4];
+        int e;
+        float w, dw;
+        bool masked;
+    };
+    auto load = [&](Rows& x, int t) __attribute__((always_inline)) {
+        const size_t tt = t;
+        load_row<NV, VEC>(logits + tt * E, E, j, x.v);
+        x.e = -1;
+        x.w = x.dw = 0.0f;
+        if (d_w && j < k) {
+            x.e = idx[tt * k + j];
+            if ((keep && !keep[tt * k + j]) || static_cast<unsigned>(x.e) >= static_cast<unsigned>(E)) x.e = -1;
+            const float a = w[tt * k + j], b = d_w[tt * k + j];
+            if (x.e >= 0) {
+                x.w = a;
+                x.dw = b;
+            }
+        }
+        x.masked = mask && mask[tt] == 0;
+    };
+    const int t_first = block_t0 + wave * kTokPerStep + g;
+    Rows next;
+    if (t_first < T) load(next, t_first);                // on their way while the block finds its sequences
+    const float up = d_loss ? *d_loss : 1.0f;
+    const int present = tokens[S], total_tokens = tokens[S + 1];
     const Sequences seq = block_sequences(offs, S, block_t0, min(T, block_t0 + per_block) - 1, found);
 #pragma unroll
     for (int c = 0; c < NV; ++c)
         *reinterpret_cast<f32x4*>(&gates[row][64 * c + 4 * j]) = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     wave_fence();
-    const float up = d_loss ? *d_loss : 1.0f;
-    const int present = tokens[S], total_tokens = tokens[S + 1];
     const float bal = present > 0 ? up * balance_coef * static_cast<float>(E) / static_cast<float>(k) /
                                         static_cast<float>(present)
                                   : 0.0f;
     const float zed = total_tokens > 0 ? up * 2.0f * z_coef / static_cast<float>(total_tokens) : 0.0f;
 
     for (int i = 0; i < steps; ++i) {
-        const int t = block_t0 + (i * kLossWaves + wave) * kTokPerStep + g;
-        if (t >= T) continue;                            // whole 16-lane rows
+        const int t = t_first + i * kGradWaves * kTokPerStep;
+        if (t >= T) break;                               // whole 16-lane rows
         const size_t tt = t;
-        float v[NV][4];
-        load_row<NV, VEC>(logits + tt * E, E, j, v);
-        int e = -1;
-        float ws = 0.0f, dw = 0.0f;
-        if (d_w && j < k) {
-            e = idx[tt * k + j];
-            if ((keep && !keep[tt * k + j]) || static_cast<unsigned>(e) >= static_cast<unsigned>(E)) e = -1;
-            if (e >= 0) {
-                ws = w[tt * k + j];
-                dw = d_w[tt * k + j];
-            }
-        }
+        Rows x = next;
+        if (i + 1 < steps && t + kGradWaves * kTokPerStep < T) load(next, t + kGradWaves * kTokPerStep);
+        float(&v)[NV][4] = x.v;
+        const int e = x.e;
+        const float ws = x.w, dw = x.dw;
         const int s = seq.of(t, seq.first);
         const bool inside = s >= 0 && s < S;
         float top, total;
         row_exp<NV>(v, top, total);
-        const bool valid = inside && !(top == -INFINITY) && (!mask || mask[t] != 0);
+        const bool valid = inside && !(top == -INFINITY) && !x.masked;
         const float inv = 1.0f / total;
         const float lse = top + logf(total);
         const int ns = inside ? tokens[s] : 0;
@@ -659,7 +677,7 @@ __global__ __launch_bounds__(kLossThreads) void router_grad_kernel(
                 u32x4 q = {0, 0, 0, 0};
                 if (inside && col < E) q = *reinterpret_cast<const u32x4*>(counts + static_cast<size_t>(s) * E + col);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) cc[c][x] = cs * static_cast<float>(static_cast<int>(q[x]));
+                for (int i4 = 0; i4 < 4; ++i4) cc[c][i4] = cs * static_cast<float>(static_cast<int>(q[i4]));
             } else {
 #pragma unroll
                 for (int x = 0; x < 4; ++x)
@@ -752,7 +770,9 @@ cap_status balance_loss_launch(int T, int k, int E, const float* logits, const i
         loss_sum_all_kernel<<<1, kSumThreads, 0, stream>>>(q);
     } else {
         const int quarters = (E + 63) / 64;
-        loss_sum_kernel<<<dim3(S, quarters), 256, 0, stream>>>(q);
+        // more groups where a sequence has more pieces than 16 groups take soon
+        if (plan.blocks > 8 * S) loss_sum_kernel<64><<<dim3(S, quarters), 1024, 0, stream>>>(q);
+        else loss_sum_kernel<16><<<dim3(S, quarters), 256, 0, stream>>>(q);
         loss_final_kernel<<<1, 256, 0, stream>>>(q, quarters);
     }
     CAP_LAUNCH_CHECK();
@@ -764,13 +784,13 @@ cap_status router_grad_launch(int T, int k, int E, const float* logits, const in
                               const int32_t* counts, const int32_t* tokens, float balance_coef, float z_coef,
                               const float* d_loss, cap_dtype dtype, void* d_logits, hipStream_t stream) {
     const int steps = T >= 16384 ? 2 : 1;
-    const int per_block = kLossWaves * kTokPerStep * steps;
+    const int per_block = kGradWaves * kTokPerStep * steps;
     const int blocks = (T - 1) / per_block + 1;
     const bool bf16 = dtype == CAP_DTYPE_BF16;
     const bool vec = E % 4 == 0 && aligned(logits, 16) && aligned(counts, 16) && aligned(d_logits, bf16 ? 8 : 16);
     auto launch = [&](auto NV, auto VEC, auto BF) {
         router_grad_kernel<decltype(NV)::value, decltype(VEC)::value, decltype(BF)::value>
-            <<<blocks, kLossThreads, 0, stream>>>(T, k, E, logits, idx, keep, w, d_w, mask, offs, S, counts, tokens,
+            <<<blocks, kGradThreads, 0, stream>>>(T, k, E, logits, idx, keep, w, d_w, mask, offs, S, counts, tokens,
                                                   balance_coef, z_coef, d_loss, steps, d_logits);
     };
     auto by_type = [&](auto NV) {
