@@ -133,30 +133,49 @@ struct Sequences {
     }
 };
 struct SequencesLds {
-    int found[2];
+    int found[2][16];                                // by wave
     int32_t cache[kSeqCache];
 };
+// A barrier for LDS alone: __syncthreads would wait for the rows on their way too.
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// This thread's first offset, to be asked for before the rows (loads return in order).
+__device__ __forceinline__ int first_offset(const int32_t* __restrict__ offs, int S) {
+    return offs && static_cast<int>(threadIdx.x) <= S ? offs[threadIdx.x] : INT32_MAX;
+}
+
 // Of tokens t0 and t1 and those between them.  Ends in a barrier.
-__device__ __forceinline__ Sequences block_sequences(const int32_t* __restrict__ offs, int S, int t0, int t1,
+__device__ __forceinline__ Sequences block_sequences(const int32_t* __restrict__ offs, int S, int t0, int t1, int mine,
                                                      SequencesLds& lds) {
     Sequences q{offs, lds.cache, S, 0, 0};
     if (!offs) return q;
-    if (threadIdx.x < 2) lds.found[threadIdx.x] = 0;
-    __syncthreads();
+    // counted by ballots (LDS atomics on one word took 5 us for 211 sequences)
     int n0 = 0, n1 = 0;
-    for (int i = threadIdx.x; i <= S; i += blockDim.x) {
-        const int o = offs[i];
-        n0 += o <= t0;
-        n1 += o <= t1;
+    for (int i = threadIdx.x; i - static_cast<int>(threadIdx.x) <= S; i += blockDim.x) {
+        const int o = i == static_cast<int>(threadIdx.x) ? mine : i <= S ? offs[i] : INT32_MAX;
+        n0 += __popcll(__ballot(i <= S && o <= t0));
+        n1 += __popcll(__ballot(i <= S && o <= t1));
     }
-    if (n0) atomicAdd(&lds.found[0], n0);
-    if (n1) atomicAdd(&lds.found[1], n1);
-    __syncthreads();
-    q.first = __builtin_amdgcn_readfirstlane(lds.found[0]) - 1;
-    q.last = max(q.first, __builtin_amdgcn_readfirstlane(lds.found[1]) - 1);
+    const int wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+    if (threadIdx.x % kWave == 0) {
+        lds.found[0][wave] = n0;
+        lds.found[1][wave] = n1;
+    }
+    lds_barrier();
+    n0 = n1 = 0;
+    for (int w = 0; w < waves; ++w) {
+        n0 += lds.found[0][w];
+        n1 += lds.found[1][w];
+    }
+    q.first = __builtin_amdgcn_readfirstlane(n0) - 1;
+    q.last = max(q.first, __builtin_amdgcn_readfirstlane(n1) - 1);
     if (q.first != q.last) {
         for (int i = threadIdx.x; i < kSeqCache; i += blockDim.x) lds.cache[i] = offs[min(max(q.first + i, 0), S)];
-        __syncthreads();
+        lds_barrier();
     }
     return q;
 }
@@ -346,7 +365,8 @@ template <int NV, bool VEC, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave) void loss_pieces_kernel(LossArgs q) {
     constexpr bool ALL = WAVES == kSumWaves;
     __shared__ int hist[WAVES][64 * NV];
-    __shared__ float part[ALL ? 1 : WAVES][64 * NV];
+    __shared__ __attribute__((aligned(16))) float part[WAVES][64 * NV];
+    __shared__ float term_w[WAVES];
     __shared__ int part_n[WAVES];
     __shared__ float part_z[WAVES];
     __shared__ SequencesLds found;
@@ -377,9 +397,10 @@ __global__ __launch_bounds__(WAVES * kWave) void loss_pieces_kernel(LossArgs q) 
         x.valid = !q.mask || q.mask[tc] != 0;
     };
     // the first are on their way while the block finds its sequences
+    const int mine = first_offset(q.offs, S);
     Rows next;
     if (a < b) load(next, a);
-    const Sequences seq = block_sequences(q.offs, S, block_t0, block_t1 - 1, found);
+    const Sequences seq = block_sequences(q.offs, S, block_t0, block_t1 - 1, mine, found);
     wave_fence();
     float sum[NV][4];
     float zsum = 0.0f;
@@ -425,9 +446,16 @@ __global__ __launch_bounds__(WAVES * kWave) void loss_pieces_kernel(LossArgs q) 
         wave_fence();
     };
 
-    if (!ALL && seq.first == seq.last) {             // the block's tokens are of one sequence: one piece
-        if (seq.first < 0 || seq.first >= S) return;
-        tokens(a, b);
+    if (ALL ? S == 1 : seq.first == seq.last) {      // the block's tokens are of one sequence
+        if (ALL) {
+            // (of the sequence's own range: tokens may lie outside it)
+            int lo = 0, hi = T;
+            sequence_range(q, 0, lo, hi);
+            tokens(max(a, lo), max(min(b, hi), max(a, lo)));
+        } else {
+            if (seq.first < 0 || seq.first >= S) return;
+            tokens(a, b);
+        }
         if (g == 0) {
 #pragma unroll
             for (int c = 0; c < NV; ++c)
@@ -438,28 +466,50 @@ __global__ __launch_bounds__(WAVES * kWave) void loss_pieces_kernel(LossArgs q) 
             part_z[wave] = zsum;
         }
         __syncthreads();
-        const size_t slot = static_cast<size_t>(blockIdx.x) * WAVES + seq.first;
         const int e = threadIdx.x;
-        if (e < ws.EP) {
-            float p = 0.0f;
-            int c = 0;
+        float p = 0.0f, z = 0.0f;
+        int c = 0, m = 0;
+        if (e < 64 * NV) {
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
                 p += part[w][e];
                 c += hist[w][e];
             }
-            ws.psum[slot * ws.EP + e] = p;
-            ws.csum[slot * ws.EP + e] = c;
         }
-        if (e == 0) {
-            int m = 0;
-            float z = 0.0f;
+        if (ALL || e == 0) {
             for (int w = 0; w < WAVES; ++w) {
                 m += part_n[w];
                 z += part_z[w];
             }
-            ws.nsum[slot] = m;
-            ws.zsum[slot] = z;
+        }
+        if constexpr (!ALL) {                        // one piece
+            const size_t slot = static_cast<size_t>(blockIdx.x) * WAVES + seq.first;
+            if (e < ws.EP) {
+                ws.psum[slot * ws.EP + e] = p;
+                ws.csum[slot * ws.EP + e] = c;
+            }
+            if (e == 0) {
+                ws.nsum[slot] = m;
+                ws.zsum[slot] = z;
+            }
+        } else {                                     // the result
+            float term = 0.0f;
+            if (e < E) {
+                p = m > 0 ? p / static_cast<float>(m) : 0.0f;
+                q.probs[e] = p;
+                q.counts[e] = c;
+                term = static_cast<float>(c) * p;
+            }
+            term = wave_sum(term);
+            if (lane == 0) term_w[wave] = term;
+            __syncthreads();
+            if (e == 0) {
+                term = 0.0f;
+                for (int w = 0; w < WAVES; ++w) term += term_w[w];
+                q.tokens[0] = m;
+                write_loss(q, m > 0 ? term * (static_cast<float>(E) / static_cast<float>(k) / static_cast<float>(m)) : 0.0f, z,
+                           m > 0, m);
+            }
         }
         return;
     }
@@ -636,11 +686,12 @@ __global__ __launch_bounds__(kGradThreads) void router_grad_kernel(
         x.masked = mask && mask[tt] == 0;
     };
     const int t_first = block_t0 + wave * kTokPerStep + g;
-    Rows next;
-    if (t_first < T) load(next, t_first);                // on their way while the block finds its sequences
+    const int mine = first_offset(offs, S);
     const float up = d_loss ? *d_loss : 1.0f;
     const int present = tokens[S], total_tokens = tokens[S + 1];
-    const Sequences seq = block_sequences(offs, S, block_t0, min(T, block_t0 + per_block) - 1, found);
+    Rows next;
+    if (t_first < T) load(next, t_first);                // on their way while the block finds its sequences
+    const Sequences seq = block_sequences(offs, S, block_t0, min(T, block_t0 + per_block) - 1, mine, found);
 #pragma unroll
     for (int c = 0; c < NV; ++c)
         *reinterpret_cast<f32x4*>(&gates[row][64 * c + 4 * j]) = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
