@@ -45,13 +45,13 @@ __device__ __forceinline__ void split4_rtz(const float (&v)[4], u32x2& hi, u32x2
 // 4 x 4 transpose of 16-bit values within each quad of lanes: lane r holds four
 // columns of row r; afterwards lane r holds four rows of column r % 4.
 __device__ __forceinline__ u32x2 quad_transpose(const u32x2& v, int lane) {
-    const uint32_t p0 = __builtin_amdgcn_update_dpp(0, v[0], 0xB1, 0xF, 0xF, false);       // lane ^ 1
-    const uint32_t p1 = __builtin_amdgcn_update_dpp(0, v[1], 0xB1, 0xF, 0xF, false);
+    const uint32_t p0 = __builtin_amdgcn_mov_dpp(v[0], 0xB1, 0xF, 0xF, true);              // lane ^ 1
+    const uint32_t p1 = __builtin_amdgcn_mov_dpp(v[1], 0xB1, 0xF, 0xF, true);
     // even lanes: the low halves of their own and the partner's pair; odd: the high ones
     const uint32_t pick = 0x05040100u ^ ((0u - (lane & 1)) & (0x05040100u ^ 0x03020706u));
     const uint32_t x0 = __builtin_amdgcn_perm(p0, v[0], pick), x1 = __builtin_amdgcn_perm(p1, v[1], pick);
     const uint32_t up = 0u - ((lane >> 1) & 1);
-    const uint32_t y = __builtin_amdgcn_update_dpp(0, x1 ^ (up & (x0 ^ x1)), 0x4E, 0xF, 0xF, false);   // lane ^ 2
+    const uint32_t y = __builtin_amdgcn_mov_dpp(x1 ^ (up & (x0 ^ x1)), 0x4E, 0xF, 0xF, true);   // lane ^ 2
     return u32x2{x0 ^ (up & (x0 ^ y)), y ^ (up & (x1 ^ y))};
 }
 
@@ -76,6 +76,55 @@ template <bool BF16>
 __device__ __forceinline__ float load_g(const void* g, size_t i) {
     if constexpr (BF16) return bf16_to_f32(static_cast<const uint16_t*>(g)[i]);
     else return static_cast<const float*>(g)[i];
+}
+// Raw values of four consecutive elements (the gradient's, the momentum's) and U from
+// them, apart so that loads can be under way while something else is computed.  vec: 16-byte
+// (fp32) and 8-byte (bf16) aligned; step: distance of the elements; n: how many there are.
+struct Raw4 {
+    f32x4 g, m;
+};
+template <bool BF16, bool MOM>
+__device__ __forceinline__ void load_raw(const Source& s, size_t i, size_t step, int n, bool vec, Raw4& x) {
+    x.g = x.m = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (vec) {
+        if (n <= 0) return;
+        if constexpr (BF16) {
+            const u32x2 v = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(s.g) + i);
+            x.g = f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u), __uint_as_float(v[1] << 16),
+                        __uint_as_float(v[1] & 0xFFFF0000u)};
+        } else {
+            x.g = *reinterpret_cast<const f32x4*>(static_cast<const float*>(s.g) + i);
+        }
+        if constexpr (MOM) x.m = *reinterpret_cast<const f32x4*>(s.mom + i);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < n) {
+                x.g[e] = load_g<BF16>(s.g, i + e * step);
+                if constexpr (MOM) x.m[e] = s.mom[i + e * step];
+            }
+    }
+}
+template <bool MOM, bool FIRST>
+__device__ __forceinline__ f32x4 finish_u(const Source& s, size_t i, size_t step, int n, bool vec, const Raw4& x) {
+    if constexpr (!MOM) return x.g;
+    f32x4 m = x.m;
+    if constexpr (FIRST) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[e] = __builtin_fmaf(s.mu, m[e], x.g[e]);
+        if (vec) {
+            if (n > 0) *reinterpret_cast<f32x4*>(s.mom + i) = m;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < n) s.mom[i + e * step] = m[e];
+        }
+    }
+    if (s.nesterov) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[e] = __builtin_fmaf(s.mu, m[e], x.g[e]);
+    }
+    return m;
 }
 template <bool BF16, bool MOM, bool FIRST>
 __device__ __forceinline__ float load_u(const Source& s, size_t i) {

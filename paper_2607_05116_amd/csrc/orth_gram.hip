@@ -46,24 +46,34 @@ __global__ __launch_bounds__(kGramThreads) void gram_partial_kernel(Source src, 
     f32x4 acc[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k0 = blockIdx.x * run + wave * 16; k0 < k_end; k0 += kGramWaves * 16) {
-        const int k = k0 + 4 * kq;                           // this lane's four positions along the longer side
+    // this lane's four positions along the longer side, of row 16 i + r
+    const bool rows_vec = !tall && vec;
+    const size_t step = tall ? n : 1;
+    auto place = [&](int k, int i) __attribute__((always_inline)) {
+        return base + (tall ? static_cast<size_t>(k) * n + 16 * i + r : static_cast<size_t>(16 * i + r) * m + k);
+    };
+    Raw4 raw[NB];
+    auto load = [&](int k) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+            load_raw<BF16, MOM>(src, place(k, i), step, 16 * i + r < n ? k_end - k : 0, rows_vec, raw[i]);
+    };
+    int k = blockIdx.x * run + wave * 16 + 4 * kq;
+    // the next positions are on their way during the products (with 128 rows there are no
+    // registers for them)
+    constexpr bool kAhead = NB < 8;
+    if (kAhead && k - 4 * kq < k_end) load(k);
+    for (; k - 4 * kq < k_end; k += kGramWaves * 16) {
         f32x4 u[NB];
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
-            const int row = 16 * i + r;
-            u[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            if (row >= n) continue;
-            if (!tall && vec) {
-                if (k < k_end) u[i] = load_u4<BF16, MOM, true>(src, base + static_cast<size_t>(row) * m + k);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (k + e < k_end)
-                        u[i][e] = load_u<BF16, MOM, true>(
-                            src, base + (tall ? static_cast<size_t>(k + e) * n + row : static_cast<size_t>(row) * m + k + e));
-            }
+            const int count = 16 * i + r < n ? k_end - k : 0;
+            Raw4 x;
+            if constexpr (kAhead) x = raw[i];
+            else load_raw<BF16, MOM>(src, place(k, i), step, count, rows_vec, x);
+            u[i] = finish_u<MOM, true>(src, place(k, i), step, count, rows_vec, x);
         }
+        if (kAhead && k - 4 * kq + kGramWaves * 16 < k_end) load(k + kGramWaves * 16);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -348,38 +358,42 @@ __global__ __launch_bounds__(kGramThreads) void gram_apply_kernel(Source src, in
     const size_t base = static_cast<size_t>(blockIdx.y) * n * m;
     const int end = min(m, static_cast<int>(blockIdx.x + 1) * run);
     __syncthreads();
-    for (int c0 = blockIdx.x * run + wave * 16; c0 < end; c0 += kGramWaves * 16) {
+    // position c0 + r of the longer side, values 32 ks + 8 g + 4 h .. of the shorter
+    const bool rows_vec = tall && vec;
+    const size_t step = tall ? 1 : m;
+    Raw4 raw[KS][2];
+    auto place = [&](int c, int k) __attribute__((always_inline)) {
+        return base + (tall ? static_cast<size_t>(c) * n + k : static_cast<size_t>(k) * m + c);
+    };
+    auto load = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = ks * 32 + g * 8 + 4 * h;
+                load_raw<BF16, MOM>(src, place(c, k), step, c < end ? n - k : 0, rows_vec, raw[ks][h]);
+            }
+    };
+    int c0 = blockIdx.x * run + wave * 16;
+    if (c0 < end) load(c0 + r);
+    for (; c0 < end; c0 += kGramWaves * 16) {
         f16x8 vh[KS], vl[KS];
         const int c = c0 + r;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            float u[8];
-            const int k0 = ks * 32 + g * 8;
-            if (tall && vec) {
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    f32x4 q = {0.0f, 0.0f, 0.0f, 0.0f};
-                    if (c < end && k0 + 4 * h < n) q = load_u4<BF16, MOM, false>(src, base + static_cast<size_t>(c) * n + k0 + 4 * h);
+            for (int h = 0; h < 2; ++h) {
+                const f32x4 u = finish_u<MOM, false>(src, 0, step, 0, rows_vec, raw[ks][h]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) u[4 * h + e] = q[e];
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    u[e] = 0.0f;
-                    if (c < end && k0 + e < n)
-                        u[e] = load_u<BF16, MOM, false>(
-                            src, base + (tall ? static_cast<size_t>(c) * n + k0 + e : static_cast<size_t>(k0 + e) * m + c));
+                for (int e = 0; e < 4; ++e) {
+                    const float x = u[e] * scale;
+                    const _Float16 hi = static_cast<_Float16>(x);
+                    vh[ks][4 * h + e] = hi;
+                    vl[ks][4 * h + e] = static_cast<_Float16>((x - static_cast<float>(hi)) * kLoScale);
                 }
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float x = u[e] * scale;
-                const _Float16 hi = static_cast<_Float16>(x);
-                vh[ks][e] = hi;
-                vl[ks][e] = static_cast<_Float16>((x - static_cast<float>(hi)) * kLoScale);
-            }
-        }
+        // the next are on their way during the products
+        if (c0 + kGramWaves * 16 < end) load(c + kGramWaves * 16);
 #pragma unroll 2
         for (int i = 0; i < NP / 16; ++i) {
             if (i * 16 >= n) break;
@@ -433,7 +447,10 @@ GramPlan gram_plan(int batch, int rows, int cols) {
     // runs of at least 64 positions (one step of the four waves); about two
     // workgroups a CU over the batch, and no more parts than one workgroup sums soon
     int splits = (512 + batch - 1) / batch;
-    if (splits > kMaxSplits) splits = kMaxSplits;
+    // (the steps' kernel sums eight runs while one load is on its way: few of them up to 64
+    // rows, whose runs are short work; with 128 rows many, behind a kernel of their own)
+    const int most_splits = p.NB == 8 ? kMaxSplits : p.m > 2048 ? 32 : 16;
+    if (splits > most_splits) splits = most_splits;
     const int most = (p.m + 63) / 64;
     if (splits > most) splits = most;
     p.run = ((p.m + splits - 1) / splits + 63) / 64 * 64;
@@ -469,9 +486,9 @@ cap_status gram_form_launch(int batch, int rows, int cols, const void* g, bool b
     const Source src{g, momentum, mu, nesterov, bf16 ? 1 : 0};
     const int tall = rows > cols, vec = vector_rows(src, cols);
     uint16_t* o = static_cast<uint16_t*>(out);
-    // the applying kernel: a workgroup loads Q once for its run
+    // the applying kernel: a workgroup loads Q once for its run; about two workgroups a CU
     int arun = 64;
-    while (arun < p.m && static_cast<size_t>((p.m + arun - 1) / arun) * batch > 1024) arun += 64;
+    while (arun < p.m && static_cast<size_t>((p.m + arun - 1) / arun) * batch > 512) arun += 64;
     const dim3 agrid((p.m + arun - 1) / arun, batch);
 
     auto go = [&](auto NBc, auto NPc, auto BF, auto MO) {

@@ -705,8 +705,8 @@ __global__ __launch_bounds__(kGradThreads) void router_grad_kernel(
         const int t = t_first + i * kGradWaves * kTokPerStep;
         if (t >= T) break;                               // whole 16-lane rows
         const size_t tt = t;
-        Rows x = next;
-        if (i + 1 < steps && t + kGradWaves * kTokPerStep < T) load(next, t + kGradWaves * kTokPerStep);
+        if (i > 0) load(next, t);
+        Rows& x = next;
         float(&v)[NV][4] = x.v;
         const int e = x.e;
         const float ws = x.w, dw = x.dw;
