@@ -199,7 +199,7 @@ struct LossPlan {
 };
 LossPlan loss_plan(int T, int S) {
     LossPlan p;
-    p.one_launch = T <= 256 && S <= 64;
+    p.one_launch = S == 1 ? T <= 256 : T <= 64 && S <= 64;
     // Four tokens at a time; a batch that fills the chip several times over takes
     // 16 a wave, so that a piece is left for 128 tokens.
     p.waves = p.one_launch ? 16 : kLossWaves;
@@ -406,6 +406,21 @@ __global__ __launch_bounds__(WAVES * kWave) void loss_pieces_kernel(LossArgs q) 
     float zsum = 0.0f;
     int n = 0;
 
+    auto over_rows = [&]() __attribute__((always_inline)) {
+        // over the wave's four rows
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                sum[c][i] += __shfl_xor(sum[c][i], 16);
+                sum[c][i] += __shfl_xor(sum[c][i], 32);
+            }
+        zsum += __shfl_xor(zsum, 16);
+        zsum += __shfl_xor(zsum, 32);
+        n += __shfl_xor(n, 16);
+        n += __shfl_xor(n, 32);
+        wave_fence();
+    };
     auto tokens = [&](int from, int to) __attribute__((always_inline)) {
 #pragma unroll
         for (int c = 0; c < NV; ++c)
@@ -431,19 +446,31 @@ __global__ __launch_bounds__(WAVES * kWave) void loss_pieces_kernel(LossArgs q) 
                 if (static_cast<unsigned>(x.e) < static_cast<unsigned>(E)) atomicAdd(&hist[wave][x.e], 1);
             }
         }
-        // over the wave's four rows
+        over_rows();
+    };
+    // a wave of one step that holds several sequences: its rows once, then each sequence's
+    // tokens among them
+    auto step_once = [&](Rows& x, float& lse2) __attribute__((always_inline)) {
+        float top, total;
+        row_exp<NV>(x.v, top, total);
+        x.valid = a + g < b && x.valid && !(top == -INFINITY);
+        const float inv = 1.0f / total, lse = top + logf(total);
+        lse2 = lse * lse;
 #pragma unroll
         for (int c = 0; c < NV; ++c)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sum[c][i] += __shfl_xor(sum[c][i], 16);
-                sum[c][i] += __shfl_xor(sum[c][i], 32);
-            }
-        zsum += __shfl_xor(zsum, 16);
-        zsum += __shfl_xor(zsum, 32);
-        n += __shfl_xor(n, 16);
-        n += __shfl_xor(n, 32);
-        wave_fence();
+            for (int i = 0; i < 4; ++i) x.v[c][i] *= inv;
+    };
+    auto some = [&](const Rows& x, float lse2, int from, int to) __attribute__((always_inline)) {
+        const bool mine = x.valid && a + g >= from && a + g < to;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[c][i] = mine ? x.v[c][i] : 0.0f;
+        zsum = mine ? lse2 : 0.0f;
+        n = mine;
+        if (mine && static_cast<unsigned>(x.e) < static_cast<unsigned>(E)) atomicAdd(&hist[wave][x.e], 1);
+        over_rows();
     };
 
     if (ALL ? S == 1 : seq.first == seq.last) {      // the block's tokens are of one sequence
@@ -515,12 +542,16 @@ __global__ __launch_bounds__(WAVES * kWave) void loss_pieces_kernel(LossArgs q) 
     }
     int at = a;
     int s = seq.first;
+    const bool once = q.per_wave == kTokPerStep && seq.first != seq.last;
+    float lse2 = 0.0f;
+    if (once && a < b) step_once(next, lse2);
     while (at < b) {                                 // the wave's sequences
         s = seq.of(at, s);
         // (one sequence: its offsets are not kept)
         const int end = seq.first == seq.last || s >= S ? b : min(b, max(at + 1, seq.offset(s + 1)));
         if (s >= 0 && s < S) {
-            tokens(at, end);
+            if (once) some(next, lse2, at, end);
+            else tokens(at, end);
             const size_t slot = static_cast<size_t>(wave_id) + s;
             if (g == 0) {
 #pragma unroll
