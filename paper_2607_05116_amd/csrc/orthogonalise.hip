@@ -71,17 +71,10 @@ struct OrthWs {
     float* center;                         // [batch][2] s of the group's first and second step
     f32x4* sums;                           // of the tiles computed in parts
     int n, m, np, mp;                      // sides, and as padded with zeros
-    int xp, sp;                            // row pitch of X, and of X^T and the n x n matrices
     int parts, trace_cap;
 };
 
 int up_to(int v, int q) { return (v + q - 1) / q * q; }
-
-// Row pitch of a padded side: an odd number of 256-byte units.  Consecutive rows then
-// lie in different memory channels; with 4096-byte rows (n = 2048) the 16 rows that an
-// instruction of the results' way out touches share one, and a product of n x n
-// matrices took 214 us where it takes PITCHED (8 matrices).
-int pitch_of(int padded) { return (padded / 128 % 2) ? padded : padded + 128; }
 
 // Parts of a matrix for its norm, of at least 8192 values: four steps of a workgroup.
 size_t norm_per_part(int rows, int cols) {
@@ -167,14 +160,13 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
         at += (bytes + 255) & ~size_t(255);
         return q;
     };
-    const size_t xp = pitch_of(static_cast<int>(mp)), sp = pitch_of(static_cast<int>(np));
-    const size_t x = 2 * batch * np * xp, xt = 2 * batch * mp * sp, q = 2 * batch * np * sp;
+    const size_t x = 2 * batch * np * mp, q = 2 * batch * np * np;
     // tiles of 256 may read 128 rows past a matrix (never used): of the next one, or of
     // what follows here; each kind of matrix is followed by one at least as large
     char* v[7];
     for (int i = 4; i < 7; ++i) v[i] = take(q);
-    for (int i = 0; i < 4; ++i) v[i] = take(i == 0 ? x : i == 1 ? x / 2 : xt);
-    take(static_cast<size_t>(kPad) * (xp > sp ? xp : sp) * 2);
+    for (int i = 0; i < 4; ++i) v[i] = take(i == 1 ? x / 2 : x);
+    take(static_cast<size_t>(kPad) * mp * 2);
     const int parts = norm_parts(rows, cols);
     char* f = take(static_cast<size_t>(batch) * parts * 4);
     const Plans plans = plan_all(static_cast<int>(np), static_cast<int>(mp), batch);
@@ -195,8 +187,6 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
         w->m = m;
         w->np = static_cast<int>(np);
         w->mp = static_cast<int>(mp);
-        w->xp = static_cast<int>(xp);
-        w->sp = static_cast<int>(sp);
         w->parts = parts;
         w->trace_cap = static_cast<int>(cap);
     }
@@ -309,12 +299,11 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
     }
     __syncthreads();
     const float scale = scale_s;
-    const size_t xb = static_cast<size_t>(batch) * w.np * w.xp, tb = static_cast<size_t>(batch) * w.mp * w.sp;
+    const size_t x0 = static_cast<size_t>(batch) * w.np * w.mp;
     // as given, [rows][cols] is X of a wide matrix and X^T of a tall one
     uint16_t* const nat_hi = tall ? w.xt[0] : w.xh;
     uint16_t* const tra_hi = tall ? w.xh : w.xt[0];
-    const size_t nat_pitch = tall ? w.sp : w.xp, tra_pitch = tall ? w.xp : w.sp;
-    const size_t nat_base = tall ? tb : xb, tra_base = tall ? xb : tb;
+    const size_t nat_pitch = tall ? w.np : w.mp, tra_pitch = tall ? w.mp : w.np;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
         float v[4];
@@ -326,7 +315,7 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
         u32x2 hi;
         uint32_t err;
         split_x(v, hi, err);
-        const size_t at = nat_base + static_cast<size_t>(r0 + 16 * x + ty) * nat_pitch + c0 + 4 * tx;
+        const size_t at = x0 + static_cast<size_t>(r0 + 16 * x + ty) * nat_pitch + c0 + 4 * tx;
         *reinterpret_cast<u32x2*>(nat_hi + at) = hi;
         const int row = r0 + 16 * x + ty, col = c0 + 4 * tx;
         if (!tall)
@@ -341,7 +330,7 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
         u32x2 hi;
         uint32_t err;
         split_x(v, hi, err);
-        const size_t at = tra_base + static_cast<size_t>(c0 + 16 * x + ty) * tra_pitch + r0 + 4 * tx;
+        const size_t at = x0 + static_cast<size_t>(c0 + 16 * x + ty) * tra_pitch + r0 + 4 * tx;
         *reinterpret_cast<u32x2*>(tra_hi + at) = hi;
         const int row = c0 + 16 * x + ty, col = r0 + 4 * tx;
         if (tall)
@@ -482,10 +471,10 @@ struct Out {
     const uint16_t* p0;
 
     __device__ __forceinline__ Out(const ProductArgs& q_, const Scalars& c_, int batch_, bool mirror_, int lane_)
-        : q(q_), c(c_), batch(batch_), lane(lane_), pitch(kSquare ? q_.w.sp : q_.w.xp), mirror(mirror_) {
+        : q(q_), c(c_), batch(batch_), lane(lane_), pitch(kSquare ? q_.w.np : q_.w.mp), mirror(mirror_) {
         const int r = lane & 15, g = lane >> 4;
         lane_at = 2u * ((8 * (r >> 2) + (r & 3)) * pitch + 16 * (g & 1) + 8 * (g >> 1));
-        lane_t = 2u * ((4 * g + (r & 3)) * q.w.sp + 8 * (r >> 2));
+        lane_t = 2u * ((4 * g + (r & 3)) * q.w.np + 8 * (r >> 2));
         p0 = kSquare ? q.A : q.w.xh;
     }
     __device__ __forceinline__ auto at(const uint16_t* p, int row0, int col0, int ii) const {
@@ -495,8 +484,8 @@ struct Out {
         return lane_ptr<u32x2>(q.w.xl + err_block(q.w, batch, row0, col0) + 512 * ii, 8u * lane);
     }
     // What N steps side by side add to; steps that share lines of 128 bytes are loaded
-    // together, a row block at a time (apart, each line came twice: 460 -> PAIRED us for the
-    // last product of 8 x 2048 x 7168).
+    // together, a row block at a time (apart, each line came twice: 467 -> 446 us for the last
+    // product of 8 x 2048 x 7168).
     template <int N>
     __device__ __forceinline__ void fetch(Added (&in)[N], int row0, int col0) const {
 #pragma unroll
@@ -617,7 +606,7 @@ struct Out {
                 if (q.rows > q.cols) bf16_out(col0 + 16 * b + 4 * g + (r & 3), row0 + 8 * (r >> 2), y);
             } else if (MODE == kApply || mirror) {
                 const size_t rows = kSquare ? q.w.np : q.w.mp;
-                *lane_ptr(q.D + (batch * rows + col0 + 16 * b) * q.w.sp + row0, lane_t) = y;
+                *lane_ptr(q.D + (batch * rows + col0 + 16 * b) * q.w.np + row0, lane_t) = y;
             }
         }
         return sum;
@@ -758,7 +747,7 @@ __global__ __launch_bounds__(S::WAVES * kWave, Ring<S>::kPerCu) void product_rin
     const int wave = static_cast<int>(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
     const int wm = wave / S::WN, wn = wave % S::WN;
     const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
-    const int KT = (MODE == kGram ? w.mp : w.np) / kStageK, lead = MODE == kGram ? w.xp : w.sp;
+    const int KT = (MODE == kGram ? w.mp : w.np) / kStageK, lead = MODE == kGram ? w.mp : w.np;
     const uint32_t pitch = static_cast<uint32_t>(lead) * 2u;
     const LaneMap lm = lane_map(lane);
     const int G = gridDim.x;
@@ -881,7 +870,7 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product_big_kernel(ProductArgs
     const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
     const uint32_t a_lds = lds_base + wave * kALd * 1024;
     const uint32_t b_lds = lds_base + (kBM + (wave >> 1) * kWN + (wave & 1) * 16) * kRowB;
-    const int KT = (MODE == kGram ? w.mp : w.np) / kStageK, lead = MODE == kGram ? w.xp : w.sp;
+    const int KT = (MODE == kGram ? w.mp : w.np) / kStageK, lead = MODE == kGram ? w.mp : w.np;
     // block b runs on XCD b % 8: each XCD gets a run of tiles, mostly of one matrix
     const int G = gridDim.x;
     int tile = G % 8 == 0 ? (blockIdx.x % 8) * (G / 8) + blockIdx.x / 8 : blockIdx.x;
