@@ -123,8 +123,10 @@ __device__ __forceinline__ f16x8 pair_frag(const uint8_t* p, int row, int chunk)
 // The steps of one matrix, in one workgroup: a wave for each lower block (pair of
 // blocks a side at 128 rows) of the products.  Q P and P S of a step are one phase.  Up
 // to 64 rows S, P S, P and two Q are in LDS and a phase ends in one barrier; at 128
-// rows S and P take 139 of the 160 KB: P S replaces S behind a second barrier, and Q,
-// read once a step, is in the workspace.
+// rows S and P take 139 of the 160 KB: P S replaces S behind a second barrier, and Q
+// stays in the waves' registers, a block each, and passes through the place of S while
+// the next S waits in registers (through the workspace Q P took 18,000 of a step's
+// 33,000 cycles).
 template <int NP>
 constexpr int step_waves() { return blocks_of(NP == 128 ? 4 : NP / 16); }
 template <int NP>
@@ -147,27 +149,31 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
     const int lane = threadIdx.x % kWave;
     const int wave = static_cast<int>(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
     const int r = lane & 15, g = lane >> 4;
-    // the workspace's Q: two of them in turn, high and low halves; the result is the first
-    uint16_t* const qw = q_ws + static_cast<size_t>(blockIdx.x) * (kSmall ? 2 : 4) * NP * NP;
+    uint16_t* const qw = q_ws + static_cast<size_t>(blockIdx.x) * 2 * NP * NP;   // the result, high and low halves
 
     // S_0 = U U^T / |U|^2, with |U|^2 its trace
     constexpr int ITEMS = NT * kWave, PER = (ITEMS + THREADS - 1) / THREADS;
     f32x4 s[PER];
     float trace = 0.0f;
+    const f32x4* p[PER];
 #pragma unroll
     for (int x = 0; x < PER; ++x) {
         const int it = x * THREADS + threadIdx.x;
+        p[x] = part + static_cast<size_t>(blockIdx.x) * splits * ITEMS + (it < ITEMS ? it : ITEMS - 1);
         s[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (it < ITEMS) {
-            const f32x4* p = part + static_cast<size_t>(blockIdx.x) * splits * ITEMS + it;
+    }
 #pragma unroll 8
-            for (int k = 0; k < splits; ++k) s[x] += p[static_cast<size_t>(k) * ITEMS];
-            int bi, bj;
-            triangle(it / kWave, bi, bj);
+    for (int k = 0; k < splits; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (bi == bj && 4 * g + e == r) trace += s[x][e];
-        }
+        for (int x = 0; x < PER; ++x) s[x] += p[x][static_cast<size_t>(k) * ITEMS];
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+        const int it = x * THREADS + threadIdx.x;
+        int bi, bj;
+        triangle(it / kWave, bi, bj);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (it < ITEMS && bi == bj && 4 * g + e == r) trace += s[x][e];
     }
     if constexpr (16 * NB < NP)
         for (int i = threadIdx.x; i < static_cast<int>(sizeof(Pair<NP>)) / 16; i += THREADS)
@@ -188,12 +194,9 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
             *reinterpret_cast<u32x2*>(D.lo + row * Pair<NP>::kPitch + col * 2) = lo;
         };
     };
-    auto to_ws = [&](int which) {
-        uint16_t* const q = qw + which * 2 * NP * NP;
-        return [q](int row, int col, const u32x2& hi, const u32x2& lo) __attribute__((always_inline)) {
-            *reinterpret_cast<u32x2*>(q + row * NP + col) = hi;
-            *reinterpret_cast<u32x2*>(q + NP * NP + row * NP + col) = lo;
-        };
+    auto to_ws = [qw](int row, int col, const u32x2& hi, const u32x2& lo) __attribute__((always_inline)) {
+        *reinterpret_cast<u32x2*>(qw + row * NP + col) = hi;
+        *reinterpret_cast<u32x2*>(qw + NP * NP + row * NP + col) = lo;
     };
     // four values of row 16 bi + r, columns 16 bj + 4 g .., and their mirror image
     auto put = [&](int bi, int bj, bool mirror, const float (&v)[4], auto&& store) __attribute__((always_inline)) {
@@ -225,7 +228,7 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
 
     // lower super-block of A B: lane (r, g) holds columns 4 g .. of row r of each block
     typedef float Block[WB][WB][4];
-    auto product = [&](auto&& frag_a, const Pair<NP>& B, Block& v) __attribute__((always_inline)) {
+    auto product = [&](const Pair<NP>& A, const Pair<NP>& B, Block& v) __attribute__((always_inline)) {
         f32x4 main[WB][WB], corr[WB][WB];
 #pragma unroll
         for (int i = 0; i < WB; ++i)
@@ -236,7 +239,8 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
             f16x8 ah[WB], al[WB], bh[WB], bl[WB];
 #pragma unroll
             for (int i = 0; i < WB; ++i) {
-                frag_a((si * WB + i) * 16 + r, ks * 4 + g, ah[i], al[i]);
+                ah[i] = pair_frag<NP>(A.hi, (si * WB + i) * 16 + r, ks * 4 + g);
+                al[i] = pair_frag<NP>(A.lo, (si * WB + i) * 16 + r, ks * 4 + g);
                 bh[i] = pair_frag<NP>(B.hi, (sj * WB + i) * 16 + r, ks * 4 + g);
                 bl[i] = pair_frag<NP>(B.lo, (sj * WB + i) * 16 + r, ks * 4 + g);
             }
@@ -257,19 +261,6 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
                 for (int e = 0; e < 4; ++e)
                     v[i][j][e] = __builtin_fmaf(corr[i][j][e], 1.0f / kLoScale, main[i][j][e]);
     };
-    auto from = [&](const Pair<NP>& D) {
-        return [&D](int row, int chunk, f16x8& hi, f16x8& lo) __attribute__((always_inline)) {
-            hi = pair_frag<NP>(D.hi, row, chunk);
-            lo = pair_frag<NP>(D.lo, row, chunk);
-        };
-    };
-    auto from_ws = [&](int which) {
-        const uint16_t* const q = qw + which * 2 * NP * NP;
-        return [q](int row, int chunk, f16x8& hi, f16x8& lo) __attribute__((always_inline)) {
-            hi = *reinterpret_cast<const f16x8*>(q + row * NP + chunk * 8);
-            lo = *reinterpret_cast<const f16x8*>(q + NP * NP + row * NP + chunk * 8);
-        };
-    };
     auto each = [&](const Block& v, auto&& store) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < WB; ++i)
@@ -277,14 +268,21 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
             for (int j = 0; j < WB; ++j) put(si * WB + i, sj * WB + j, si != sj, v[i][j], store);
     };
 
+    Block q;                                                 // at 128 rows
+    auto copy = [](const Block& from, Block& to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < WB; ++i)
+#pragma unroll
+            for (int j = 0; j < WB; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) to[i][j][e] = from[i][j][e];
+    };
     for (int it = 0; it < steps; ++it) {
         const float a = coef.v[it][0], b = coef.v[it][1], c = coef.v[it][2];
         const bool last = it + 1 == steps;
-        // the workspace's Q of step it is written to place (steps - 1 - it) % 2: the last to the first
-        const int q_to = (steps - 1 - it) & 1;
         if (mine) {
             Block v;
-            product(from(S), S, v);
+            product(S, S, v);
 #pragma unroll
             for (int i = 0; i < WB; ++i)
 #pragma unroll
@@ -302,38 +300,54 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
             each(v, to_lds(P));
             if (it == 0) {                                   // Q = P
                 if constexpr (kSmall) {
-                    if (last) each(v, to_ws(0));
+                    if (last) each(v, to_ws);
                     else each(v, to_lds(M[3]));
                 } else {
-                    each(v, to_ws(q_to));
+                    copy(v, q);
                 }
             }
         }
         __syncthreads();
         Block t;
-        if (mine) {
-            if (it > 0) {                                    // Q <- Q P
-                Block v;
-                if constexpr (kSmall) {
-                    product(from(M[3 + ((it - 1) & 1)]), P, v);
-                    if (last) each(v, to_ws(0));
-                    else each(v, to_lds(M[3 + (it & 1)]));
-                } else {
-                    product(from_ws(q_to ^ 1), P, v);
-                    each(v, to_ws(q_to));
+        if constexpr (kSmall) {
+            if (mine) {
+                if (it > 0) {                                // Q <- Q P
+                    product(M[3 + ((it - 1) & 1)], P, t);
+                    if (last) each(t, to_ws);
+                    else each(t, to_lds(M[3 + (it & 1)]));
                 }
+                if (!last) product(P, S, t);                 // S <- P S P
             }
-            if (!last) product(from(P), S, t);               // S <- P S P
+            if (last) break;
+            if (mine) each(t, to_lds(T));
+            __syncthreads();
+            if (mine) {
+                product(T, P, t);
+                each(t, to_lds(S));
+            }
+            __syncthreads();
+        } else {
+            if (!last) {                                     // t = P S P
+                if (mine) product(P, S, t);
+                __syncthreads();
+                if (mine) each(t, to_lds(T));
+                __syncthreads();
+                if (mine) product(T, P, t);
+                __syncthreads();
+            }
+            if (it > 0) {                                    // Q <- Q P
+                if (mine) each(q, to_lds(T));
+                __syncthreads();
+                if (mine) product(T, P, q);
+                __syncthreads();
+            }
+            if (last) break;
+            if (mine) each(t, to_lds(S));
+            __syncthreads();
         }
-        if (last) break;
-        if constexpr (!kSmall) __syncthreads();
-        if (mine) each(t, to_lds(T));
-        __syncthreads();
-        if (mine) product(from(T), P, t);
-        if constexpr (!kSmall) __syncthreads();
-        if (mine) each(t, to_lds(S));
-        __syncthreads();
     }
+    if constexpr (!kSmall)
+        if (mine) each(q, to_ws);
 }
 
 // Q X_0: a wave takes 16 positions of the longer side at a time.
@@ -443,7 +457,7 @@ GramPlan gram_plan(int batch, int rows, int cols) {
     p.NB = p.n <= 16 ? 1 : p.n <= 32 ? 2 : p.n <= 64 ? 4 : 8;
     p.NP = p.NB < 2 ? 32 : 16 * p.NB;
     p.items = blocks_of(p.NB) * kWave;
-    p.q_values = (p.NP == 128 ? 4 : 2) * p.NP * p.NP;        // of a matrix: high and low halves, twice at 128 rows
+    p.q_values = 2 * p.NP * p.NP;                            // of a matrix: high and low halves
     // runs of at least 64 positions (one step of the four waves); about two
     // workgroups a CU over the batch, and no more parts than one workgroup sums soon
     int splits = (512 + batch - 1) / batch;
