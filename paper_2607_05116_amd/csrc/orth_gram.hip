@@ -363,15 +363,9 @@ __global__ __launch_bounds__(kGramThreads) void gram_apply_kernel(Source src, in
     const int r = lane & 15, g = lane >> 4;
     const uint16_t* qh = q_ws + static_cast<size_t>(blockIdx.y) * q_stride;
     const uint16_t* ql = qh + NP * NP;
-    for (int i = threadIdx.x; i < NP * NP / 8; i += kGramThreads) {
-        const int row = i / (NP / 8), c = i % (NP / 8);
-        *reinterpret_cast<u32x4*>(Q.hi + row * Pair<NP>::kPitch + c * 16) = *reinterpret_cast<const u32x4*>(qh + i * 8);
-        *reinterpret_cast<u32x4*>(Q.lo + row * Pair<NP>::kPitch + c * 16) = *reinterpret_cast<const u32x4*>(ql + i * 8);
-    }
     const float scale = scales[blockIdx.y];
     const size_t base = static_cast<size_t>(blockIdx.y) * n * m;
     const int end = min(m, static_cast<int>(blockIdx.x + 1) * run);
-    __syncthreads();
     // position c0 + r of the longer side, values 32 ks + 8 g + 4 h .. of the shorter
     const bool rows_vec = tall && vec;
     const size_t step = tall ? 1 : m;
@@ -390,6 +384,24 @@ __global__ __launch_bounds__(kGramThreads) void gram_apply_kernel(Source src, in
     };
     int c0 = blockIdx.x * run + wave * 16;
     if (c0 < end) load(c0 + r);
+    // all of Q on its way at once
+    constexpr int ITEMS = NP * NP / 8, PER = (ITEMS + kGramThreads - 1) / kGramThreads;
+    u32x4 q[PER][2];
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+        const int i = x * kGramThreads + threadIdx.x, at = (i < ITEMS ? i : 0) * 8;
+        q[x][0] = *reinterpret_cast<const u32x4*>(qh + at);
+        q[x][1] = *reinterpret_cast<const u32x4*>(ql + at);
+    }
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+        const int i = x * kGramThreads + threadIdx.x, row = i / (NP / 8), c = i % (NP / 8);
+        if (i < ITEMS) {
+            *reinterpret_cast<u32x4*>(Q.hi + row * Pair<NP>::kPitch + c * 16) = q[x][0];
+            *reinterpret_cast<u32x4*>(Q.lo + row * Pair<NP>::kPitch + c * 16) = q[x][1];
+        }
+    }
+    __syncthreads();
     for (; c0 < end; c0 += kGramWaves * 16) {
         f16x8 vh[KS], vl[KS];
         const int c = c0 + r;
