@@ -76,11 +76,13 @@ struct OrthWs {
 
 int up_to(int v, int q) { return (v + q - 1) / q * q; }
 
-// Parts of a matrix for its norm, of at least 8192 values: four steps of a workgroup.
+// Parts of a matrix for its norm, of at least 2048 values: two vectors a thread (eight
+// single values where the matrices are not aligned, for which a part of 8192 took 12 us on
+// 3 x 333 x 517 with momentum).
 size_t norm_per_part(int rows, int cols) {
     const size_t size = static_cast<size_t>(rows) * cols;
     const size_t per = (size + kMaxNormParts - 1) / kMaxNormParts;
-    return per < 8192 ? 8192 : (per + 3) / 4 * 4;
+    return per < 2048 ? 2048 : (per + 3) / 4 * 4;
 }
 int norm_parts(int rows, int cols) {
     const size_t per = norm_per_part(rows, cols);
