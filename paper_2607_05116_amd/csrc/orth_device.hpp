@@ -7,8 +7,8 @@
 namespace cap {
 namespace {
 
-// A value as fp16 plus its rounding error in a second fp16, scaled so that the
-// error of the smallest normal values is normal too: 22 bits together.
+// A value as fp16 plus what is left of it in a second fp16, scaled so that what the
+// smallest normal values leave is normal too.
 constexpr float kLoScale = 2048.0f;
 
 __device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
@@ -21,16 +21,8 @@ __device__ __forceinline__ float f16_to_f32(uint16_t b) { return static_cast<flo
 __device__ __forceinline__ float f16_at(const u32x2& v, int e) {
     return f16_to_f32(static_cast<uint16_t>(v[e >> 1] >> (16 * (e & 1))));
 }
-__device__ __forceinline__ void split4(const float (&v)[4], u32x2& hi, u32x2& lo) {
-    hi = u32x2{pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3])};
-    float d[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) d[e] = (v[e] - f16_at(hi, e)) * kLoScale;
-    lo = u32x2{pack_f16x2(d[0], d[1]), pack_f16x2(d[2], d[3])};
-}
-
-// The same rounding toward zero (one instruction for two values): where both halves
-// are always used, the second takes up what the first leaves, and 21 bits remain.
+// Split with rounding toward zero (one instruction for two values): both halves are
+// always used, the second takes up what the first leaves, and 21 bits remain.
 __device__ __forceinline__ uint32_t pack_f16x2_rtz(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
 }

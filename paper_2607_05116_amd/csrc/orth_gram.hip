@@ -8,7 +8,7 @@
 // steps, and the trace of U U^T is the norm.  What the short form costs is
 // precision: S has the squares of the singular values, so its rounding reaches
 // directions of sqrt(2^-p) of the largest one.  S_0 is summed in fp32 and the n x n
-// products are taken on values of 22 bits (fp16 pairs, three MFMAs a product), which
+// products are taken on values of 21 bits (fp16 pairs, three MFMAs a product), which
 // leaves 1e-6 to 7e-4 of the result's norm over spectra that fall by e^-12; with plain
 // fp16 it would be 1e-3 to 2e-1.
 //
@@ -19,7 +19,10 @@
 //   4. gram_apply_kernel     Q X_0, rounded to bf16 once
 // Three or four launches, against two or more for every step of the general form.
 // Bound by the latency of the steps' chain of n x n products (four a step) for few
-// matrices, by U's way from HBM for many.
+// matrices, by U's way from HBM for many: 1 x 128 x 2048 bf16 10.4 + 4.5 + 45.8 + 10.4 us
+// (100 us in the general form), 1 x 64 x 2048 6.4 + 14.5 + 5.5, 40 x 20 x 300 3.4 + 8.8 + 4.0,
+// 14 x 4433 x 111 fp32 22 + 5 + 47 + 26 (its 28 MB in at 1.25 TB/s, the products on values of
+// 24 bits taking as long as the loads).
 #include "orth_device.hpp"
 
 namespace cap {
@@ -474,7 +477,9 @@ GramPlan gram_plan(int batch, int rows, int cols) {
     // workgroups a CU over the batch, and no more parts than one workgroup sums soon
     int splits = (512 + batch - 1) / batch;
     // (the steps' kernel sums eight runs while one load is on its way: few of them up to 64
-    // rows, whose runs are short work; with 128 rows many, behind a kernel of their own)
+    // rows, whose runs are short work, 32 x 4096 16.3 us against 17.1 with 64, but 64 x 7168
+    // 30.6 with 32 against 32.6 with 16; with 128 rows many, behind a kernel of their own:
+    // 128 x 7168 75 us against 90 with 16)
     const int most_splits = p.NB == 8 ? kMaxSplits : p.m > 2048 ? 32 : 16;
     if (splits > most_splits) splits = most_splits;
     const int most = (p.m + 63) / 64;

@@ -34,7 +34,16 @@
 // or three steps in one group lose more (up to 3e-3 and 2e-2): the noise of S' grows by
 // a^2 with each step taken on it.
 //
-// Matrices of at most 128 rows or columns take the Gram form (orth_gram.hip).
+// Bound by the matrix cores and, where X is the operand, by the results' way through
+// memory beside them.  8 x 2048 x 7168 in bf16: 3.4 ms, of which the three Gram products
+// take 225 us each (240 of their 481 GFLOP done, the rest mirrored: 1.07 PFLOP/s), the eleven
+// n x n products 85 to 94 us and 10 us for joining their parts, the two updates of X 530 us
+// each (481 GFLOP, 0.91 PFLOP/s; 1.7 GB read and written) and the last one 451 us (1.07).
+// A 8192^3 product of the library reaches 1.39 PFLOP/s on the same card.  A single matrix
+// of 256 x 7168 takes 129 us for 22 launches, each 5 to 10 us of latency.
+//
+// Matrices of at most 128 rows or columns take the Gram form (orth_gram.hip): 1 x 128 x 2048
+// takes 71 us there and 100 us here.
 #include "orth_device.hpp"
 
 #include <algorithm>
@@ -110,7 +119,14 @@ int count_tiles(bool square, int np, int mp) {
 
 // The rule: the estimated time of each shape, whole or with its last round in `split`
 // parts, from what a stage of K = 64 and the way in and out of a tile take (us, measured
-// on 2 to 576 tiles of K = 256 to 7168).
+// on 2 to 576 tiles of K = 256 to 7168).  Both sides, in us for a whole call:
+//                      Big only  Mid only  Small only  by the rule
+//   8 x 2048 x 7168      3523      4150      7114        3536 (Big)
+//   8 x 1408 x 2048      1059      1178      1348        1048 (Big; Mid for X)
+//   16 x 768 x 2048       746       657       792         650 (Mid)
+//   1 x 256 x 7168        284       229       140         143 (Small)
+// and without parts 3867, 1061, 648 and 204 (for one Gram product of the first and the
+// last: 310 against 215 + 12, 35 against 7 + 5).
 ProductPlan plan_product(bool square, int np, int mp, int K, int batch) {
     const int cus = device_cu_count(), KT = K / kStageK;
     ProductPlan best{};
@@ -228,7 +244,8 @@ __device__ __forceinline__ int err_place(int row, int col) {       // of element
 }
 
 // ------------------------------------------------------------------ norm and momentum
-// Sum of squares of U over this block's part of its matrix; writes the momentum.
+// Sum of squares of U over this block's part of its matrix; writes the momentum.  Bound by
+// HBM: 51 us for 235 MB (4.6 TB/s), 39 us for 46 MB of gradient and 185 MB of momentum.
 template <bool BF16, bool MOM>
 __global__ __launch_bounds__(kNormThreads) void norm_kernel(Source src, size_t size, size_t per, int parts, int vec,
                                                             float* __restrict__ norm) {
@@ -261,7 +278,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(Source src, size_t s
 }
 
 // X0 in both orientations, padded with zeros: 64 x 64 tiles of U through LDS, four
-// values a thread at a time.
+// values a thread at a time.  Bound by HBM: 197 us for 235 MB read and 587 MB written
+// (4.2 TB/s; a large copy reaches 5.1).
 template <bool BF16, bool MOM>
 __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int cols, int vec, float eps, OrthWs w) {
     __shared__ float tile[64][65];
@@ -729,7 +747,8 @@ struct Place {
 };
 
 // ---- Mid and Small: a ring of K = 64 stages that runs on across the tiles of a workgroup,
-// all but one of them in flight
+// all but one of them in flight.  (The two waves of a SIMD taking turns at reading fragments
+// and multiplying, a barrier apart, were 2 to 7 % slower on the 128 x 256 tiles.)
 template <typename S>
 struct Ring {
     static constexpr int kStages = S::ROWS == 64 ? 4 : 3;                     // 64 or 144 KB
