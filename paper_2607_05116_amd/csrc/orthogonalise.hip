@@ -9,14 +9,14 @@
 // X is held with the shorter side n as its rows ([n][m], transposed on the way in
 // and out when the matrix has more rows than columns), so S is n x n.
 //
-// Steps go in groups of one or two: the first two and the last two are pairs, the
-// others single.  A pair needs X once, since S of its second step is P S P with P =
+// Steps go in groups of one or two: where it pays (Plans), the first two and the last two
+// are pairs, the others single.  A pair needs X once, since S of its second step is P S P with P =
 // a I + b S + c S S (polynomials of one symmetric matrix commute):
 //   S (n^2 m), then n x n products:  R = P - p I;   T = P S;   S' = T P;  R' = P' - p' I;
 //   Q = P P';   X <- Q X (2 n^2 m).
 // All n x n products are symmetric: tiles on and below the diagonal, mirrored.  Five
-// steps take 9 n^2 m + 11 n^3 multiply-adds, single steps 15 n^2 m + 5 n^3, and X is
-// read and written three times instead of five.
+// steps take 9 n^2 m + 11 n^3 multiply-adds in 17 products, single steps 15 n^2 m + 5 n^3
+// in 15, and X is read and written three times instead of five.
 //
 // Every product is an MFMA product of fp16 values with fp32 sums whose operands
 // are both contiguous along the contraction: S from rows of X, the n x n ones from
@@ -106,6 +106,7 @@ struct ProductPlan {
     int grid;
     int traces;                            // places of a trace's parts, of one matrix
     size_t sums;                           // bytes of the parts' sums
+    double us;                             // estimated
 };
 
 // Tiles of a matrix: all of them, or those with a block on or below the diagonal.
@@ -130,7 +131,6 @@ int count_tiles(bool square, int np, int mp) {
 ProductPlan plan_product(bool square, int np, int mp, int K, int batch) {
     const int cus = device_cu_count(), KT = K / kStageK;
     ProductPlan best{};
-    double best_us = 0.0;
     auto consider = [&](auto shape, int id, int per_cu, double stage, double fixed) {
         using S = decltype(shape);
         const int tiles = count_tiles<S>(square, np, mp), slots = per_cu * cus;
@@ -143,8 +143,8 @@ ProductPlan plan_product(bool square, int np, int mp, int K, int batch) {
             double us = rounds * (KT * stage + fixed);
             if (rest && split == 1) us += KT * stage + fixed;
             if (split > 1) us += (KT / 2 + split - 1) / split * 2 * stage + fixed + 5.0 + 2.0 * rest * split * tile_us;
-            if (best_us > 0.0 && us >= best_us) continue;
-            best_us = us;
+            if (best.us > 0.0 && us >= best.us) continue;
+            best.us = us;
             best.shape = id;
             best.tiles = tiles;
             best.whole = static_cast<int>(split > 1 ? total - rest : total);
@@ -157,15 +157,24 @@ ProductPlan plan_product(bool square, int np, int mp, int K, int batch) {
     };
     consider(Big{}, 0, 1, 1.42, square ? 10.0 : 22.0);
     consider(Mid{}, 1, 1, 1.05, square ? 7.0 : 12.0);
-    consider(Small{}, 2, 2, 0.5, 4.0);
+    consider(Small{}, 2, 2, 0.5, square ? 4.0 : 6.0);
     return best;
 }
+// A pair of steps takes one product of X less than two single ones, and one update of X,
+// for three n x n products more.  Both sides, in us for a whole call (pairs, single):
+//   256 x 7168       132  142       333 x 517, three      124  116
+//   512 x 4096       150  157       600 x 700             135  121
+//   1024 x 4096      221  235       1000 x 1000, two      193  171
+//   256 x 2048, 8    141  153       2048 x 2048           461  440
 struct Plans {
     ProductPlan gram, sym, apply;
+    bool pairs;
 };
 Plans plan_all(int np, int mp, int batch) {
-    return Plans{plan_product(true, np, mp, mp, batch), plan_product(true, np, mp, np, batch),
-                 plan_product(false, np, mp, np, batch)};
+    Plans p{plan_product(true, np, mp, mp, batch), plan_product(true, np, mp, np, batch),
+            plan_product(false, np, mp, np, batch), false};
+    p.pairs = 3.0 * p.sym.us < p.gram.us + p.apply.us;
+    return p;
 }
 
 size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
@@ -1068,7 +1077,7 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
     else if (momentum) begin(std::false_type{}, std::true_type{});
     else begin(std::false_type{}, std::false_type{});
     CAP_LAUNCH_CHECK();
-    const auto [gram, sym, apply] = plan_all(w.np, w.mp, batch);
+    const auto [gram, sym, apply, pairs] = plan_all(w.np, w.mp, batch);
     int from = 0, traces = 1;
     auto set = [&](uint16_t* A, uint16_t* B, uint16_t* D, int second, int parts) {
         q.A = A;
@@ -1078,7 +1087,7 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
         q.traces = parts;
     };
     for (int i = 0; i < steps;) {
-        q.pair = (i == 0 && steps >= 4) || i == steps - 2;
+        q.pair = pairs && ((i == 0 && steps >= 4) || i == steps - 2);
         for (int h = 0; h < 2; ++h)
             for (int j = 0; j < 3; ++j) q.coef[h][j] = sc.v[q.pair ? i + h : i][j];
         uint16_t *s0 = w.sq[0], *s1 = w.sq[1], *s2 = w.sq[2];
