@@ -146,7 +146,8 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
     constexpr bool kSmall = NP <= 64;
     constexpr int THREADS = step_threads<NP>();
     __shared__ __attribute__((aligned(16))) Pair<NP> M[kSmall ? 5 : 2];
-    __shared__ float red[THREADS / kWave];
+    __shared__ float red[THREADS / kWave], abc[3 * kMaxOrthSteps];
+    constexpr int kSumAhead = NP == 128 ? 4 : 16;            // runs on their way at once
     Pair<NP>&S = M[0], &P = M[1];
     Pair<NP>& T = M[kSmall ? 2 : 0];
     const int lane = threadIdx.x % kWave;
@@ -154,29 +155,46 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
     const int r = lane & 15, g = lane >> 4;
     uint16_t* const qw = q_ws + static_cast<size_t>(blockIdx.x) * 2 * NP * NP;   // the result, high and low halves
 
-    // S_0 = U U^T / |U|^2, with |U|^2 its trace
+    // S_0 = U U^T / |U|^2, with |U|^2 its trace.  What does not depend on the runs' sums (block
+    // numbers, coefficients) is found while they are on their way.
     constexpr int ITEMS = NT * kWave, PER = (ITEMS + THREADS - 1) / THREADS;
     f32x4 s[PER];
     float trace = 0.0f;
     const f32x4* p[PER];
+    int bi[PER], bj[PER];
 #pragma unroll
     for (int x = 0; x < PER; ++x) {
         const int it = x * THREADS + threadIdx.x;
         p[x] = part + static_cast<size_t>(blockIdx.x) * splits * ITEMS + (it < ITEMS ? it : ITEMS - 1);
         s[x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        triangle(it / kWave, bi[x], bj[x]);
     }
-#pragma unroll 8
-    for (int k = 0; k < splits; ++k)
+    int si = 0, sj = 0;
+    const bool mine = wave < step_waves<NP>();
+    if (mine) triangle(wave, si, sj);
+    si = __builtin_amdgcn_readfirstlane(si);
+    sj = __builtin_amdgcn_readfirstlane(sj);
+    if (threadIdx.x < 3 * kMaxOrthSteps) abc[threadIdx.x] = coef.v[threadIdx.x / 3][threadIdx.x % 3];
+    for (int k = 0; k < splits; k += kSumAhead) {
+        f32x4 v[kSumAhead][PER];
 #pragma unroll
-        for (int x = 0; x < PER; ++x) s[x] += p[x][static_cast<size_t>(k) * ITEMS];
+        for (int i = 0; i < kSumAhead; ++i)
+#pragma unroll
+            for (int x = 0; x < PER; ++x) {
+                v[i][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                if (k + i < splits) v[i][x] = p[x][static_cast<size_t>(k + i) * ITEMS];
+            }
+#pragma unroll
+        for (int i = 0; i < kSumAhead; ++i)
+#pragma unroll
+            for (int x = 0; x < PER; ++x) s[x] += v[i][x];
+    }
 #pragma unroll
     for (int x = 0; x < PER; ++x) {
         const int it = x * THREADS + threadIdx.x;
-        int bi, bj;
-        triangle(it / kWave, bi, bj);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (it < ITEMS && bi == bj && 4 * g + e == r) trace += s[x][e];
+            if (it < ITEMS && bi[x] == bj[x] && 4 * g + e == r) trace += s[x][e];
     }
     if constexpr (16 * NB < NP)
         for (int i = threadIdx.x; i < static_cast<int>(sizeof(Pair<NP>)) / 16; i += THREADS)
@@ -189,7 +207,6 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
 #pragma unroll
     for (int w = 0; w < THREADS / kWave; ++w) trace += red[w];
     const float scale = 1.0f / (sqrtf(trace) + eps);
-    if (threadIdx.x == 0) scale_out[blockIdx.x] = scale;
 
     auto to_lds = [](Pair<NP>& D) {
         return [&D](int row, int col, const u32x2& hi, const u32x2& lo) __attribute__((always_inline)) {
@@ -213,21 +230,13 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
     for (int x = 0; x < PER; ++x) {
         const int it = x * THREADS + threadIdx.x;
         if (it >= ITEMS) continue;
-        int bi, bj;
-        triangle(it / kWave, bi, bj);
         // rows 16 bi + 4 g .., column 16 bj + r: S is symmetric
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = s[x][e] * scale * scale;
-        put(bj, bi, bi != bj, v, to_lds(S));
+        put(bj[x], bi[x], bi[x] != bj[x], v, to_lds(S));
     }
     __syncthreads();
-
-    int si = 0, sj = 0;
-    const bool mine = wave < step_waves<NP>();
-    if (mine) triangle(wave, si, sj);
-    si = __builtin_amdgcn_readfirstlane(si);
-    sj = __builtin_amdgcn_readfirstlane(sj);
 
     // lower super-block of A B: lane (r, g) holds columns 4 g .. of row r of each block
     typedef float Block[WB][WB][4];
@@ -281,7 +290,7 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
                 for (int e = 0; e < 4; ++e) to[i][j][e] = from[i][j][e];
     };
     for (int it = 0; it < steps; ++it) {
-        const float a = coef.v[it][0], b = coef.v[it][1], c = coef.v[it][2];
+        const float a = abc[3 * it], b = abc[3 * it + 1], c = abc[3 * it + 2];
         const bool last = it + 1 == steps;
         if (mine) {
             Block v;
@@ -351,6 +360,7 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
     }
     if constexpr (!kSmall)
         if (mine) each(q, to_ws);
+    if (threadIdx.x == 0) scale_out[blockIdx.x] = scale;     // (at its place above the next barrier would wait for it)
 }
 
 // Q X_0: a wave takes 16 positions of the longer side at a time.
