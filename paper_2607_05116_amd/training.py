@@ -20,6 +20,7 @@ until its experts are evenly loaded.
 """
 from __future__ import annotations
 
+import contextlib
 import math
 
 import torch
@@ -31,6 +32,13 @@ _BF16 = torch.bfloat16
 
 def _workspace(nbytes: int, device) -> torch.Tensor:
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+
+
+def _on(stream):
+    """What follows, torch operations too, on the given stream (None: the current one)."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
 
 
 class Muon:
@@ -54,8 +62,7 @@ class Muon:
 
     def step(self, w: torch.Tensor, g: torch.Tensor, w_bf16: torch.Tensor | None = None, stream=None):
         """w (fp32, updated in place), g (fp32 or bf16): [batch][rows][cols], contiguous; w_bf16: a copy of the
-        weights to refresh (what the layer's kernels read).  stream: of the kernels; the weights' own update is on the
-        current stream."""
+        weights to refresh (what the layer's kernels read).  All of it on `stream` (None: the current one)."""
         if tuple(w.shape) != self.shape or tuple(g.shape) != self.shape:
             raise ValueError(f"weights {tuple(w.shape)} and gradient {tuple(g.shape)}, expected {self.shape}")
         if w.dtype != torch.float32 or g.dtype not in (torch.float32, _BF16):
@@ -63,13 +70,14 @@ class Muon:
         if not g.is_contiguous():
             raise ValueError("the gradient must be contiguous")
         dt = capi.CAP_DTYPE_BF16 if g.dtype == _BF16 else capi.CAP_DTYPE_F32
-        capi.cap_muon_update(dt, *self.shape, g, self.momentum, self.mu, self.nesterov, self.steps, None, self.eps,
-                             self.update, self.ws, stream=stream)
-        if self.weight_decay:
-            w.mul_(1.0 - self.lr * self.weight_decay)
-        w.add_(self.update, alpha=-self.lr * self.scale)
-        if w_bf16 is not None:
-            w_bf16.copy_(w)
+        with _on(stream):
+            capi.cap_muon_update(dt, *self.shape, g, self.momentum, self.mu, self.nesterov, self.steps, None, self.eps,
+                                 self.update, self.ws)
+            if self.weight_decay:
+                w.mul_(1.0 - self.lr * self.weight_decay)
+            w.add_(self.update, alpha=-self.lr * self.scale)
+            if w_bf16 is not None:
+                w_bf16.copy_(w)
 
 
 class RouterTrainer:
@@ -118,10 +126,11 @@ class RouterTrainer:
     def backward(self, x: torch.Tensor, d_gates=None, seq_offsets=None, token_mask=None, d_loss=None, stream=None):
         """d_logits and the weights' gradient, for the gradient d_gates at the gates (None: of the losses alone) and
         d_loss at their total (a device scalar; None: 1)."""
-        capi.cap_router_grad(self.T, self.k, self.E, self.logits, self.idx, self.keep, self.gates, d_gates, token_mask,
-                             seq_offsets, self.n_seq, self.counts, self.tokens, self.balance_coef, self.z_coef, d_loss,
-                             capi.CAP_DTYPE_BF16, self.d_logits, stream)
-        torch.mm(self.d_logits.t(), x, out=self.d_w[0])
+        with _on(stream):
+            capi.cap_router_grad(self.T, self.k, self.E, self.logits, self.idx, self.keep, self.gates, d_gates,
+                                 token_mask, seq_offsets, self.n_seq, self.counts, self.tokens, self.balance_coef,
+                                 self.z_coef, d_loss, capi.CAP_DTYPE_BF16, self.d_logits)
+            torch.mm(self.d_logits.t(), x, out=self.d_w[0])
 
     def step(self, x: torch.Tensor, d_gates=None, seq_offsets=None, token_mask=None):
         """One training step on the current stream."""

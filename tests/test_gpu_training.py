@@ -90,6 +90,24 @@ def test_captured_step_replays_the_eager_one():
         assert torch.equal(a.w, b.w) and torch.equal(a.loss, b.loss), i
 
 
+@pytest.mark.parametrize("handle", [False, True])
+def test_a_given_stream_takes_all_of_a_step(handle):
+    # the stream is busy when the calls are made: whatever ran on another would read what is not written yet
+    a, b = _trainer(), _trainer()
+    offs, x = torch.tensor(OFFSETS, dtype=torch.int32, device="cuda"), _batch(4)
+    a.step(x, None, offs)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream if handle else side
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+    b.forward(x, offs, stream=stream)
+    b.backward(x, None, offs, stream=stream)
+    b.opt.step(b.w, b.d_w, b.w_bf16, stream=stream)
+    torch.cuda.synchronize()
+    assert torch.equal(a.d_w, b.d_w) and torch.equal(a.w, b.w) and torch.equal(a.w_bf16, b.w_bf16)
+
+
 def test_muon_refuses():
     opt = Muon(2, 8, 16, 1e-3)
     w, g = torch.zeros((2, 8, 16), device="cuda"), torch.zeros((2, 16, 8), device="cuda")
