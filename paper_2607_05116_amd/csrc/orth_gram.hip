@@ -19,9 +19,9 @@
 //   4. gram_apply_kernel     Q X_0, rounded to bf16 once
 // Three or four launches, against two or more for every step of the general form.
 // Bound by the latency of the steps' chain of n x n products (four a step) for few
-// matrices, by U's way from HBM for many: 1 x 128 x 2048 bf16 10.4 + 4.5 + 45.8 + 10.4 us
-// (100 us in the general form), 1 x 64 x 2048 6.4 + 14.5 + 5.5, 40 x 20 x 300 3.4 + 8.8 + 4.0,
-// 14 x 4433 x 111 fp32 22 + 5 + 47 + 26 (its 28 MB in at 1.25 TB/s, the products on values of
+// matrices, by U's way from HBM for many: 1 x 128 x 2048 bf16 10.4 + 4.5 + 44.8 + 10.4 us
+// (100 us in the general form), 1 x 64 x 2048 6.4 + 14 + 5.5, 40 x 20 x 300 3.4 + 8 + 4.0,
+// 14 x 4433 x 111 fp32 22 + 5 + 46 + 26 (its 28 MB in at 1.25 TB/s, the products on values of
 // 24 bits taking as long as the loads).
 #include "orth_device.hpp"
 
