@@ -592,10 +592,11 @@ __global__ __launch_bounds__(WAVES * kWave) void loss_pieces_kernel(LossArgs q) 
 // pieces.  Latency: two loads after one another for every 4 x GROUPS pieces.
 template <int GROUPS>
 __global__ __launch_bounds__(GROUPS * 16) void loss_sum_kernel(LossArgs q) {
-    __shared__ f32x4 psum[GROUPS][16];
-    __shared__ u32x4 csum[GROUPS][16];
-    __shared__ int nsum[GROUPS];
-    __shared__ float zsum[GROUPS];
+    constexpr int WAVES = GROUPS / 4;
+    __shared__ f32x4 psum[WAVES][16];
+    __shared__ u32x4 csum[WAVES][16];
+    __shared__ int nsum[WAVES];
+    __shared__ float zsum[WAVES];
     const int s = blockIdx.x, quarter = blockIdx.y;
     const int group = threadIdx.x / 16, j = threadIdx.x % 16;
     const int col = 64 * quarter + 4 * j;
@@ -613,11 +614,25 @@ __global__ __launch_bounds__(GROUPS * 16) void loss_sum_kernel(LossArgs q) {
         n += q.ws.nsum[slot];
         z += q.ws.zsum[slot];
     });
-    psum[group][j] = p;
-    csum[group][j] = c;
-    if (j == 0) {
-        nsum[group] = n;
-        zsum[group] = z;
+    // the four groups of a wave, then the waves through LDS
+#pragma unroll
+    for (int o = 16; o < kWave; o <<= 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[i] += __shfl_xor(p[i], o);
+            c[i] += __shfl_xor(c[i], o);
+        }
+        n += __shfl_xor(n, o);
+        z += __shfl_xor(z, o);
+    }
+    const int wave = threadIdx.x / kWave;
+    if (threadIdx.x % kWave < 16) {
+        psum[wave][j] = p;
+        csum[wave][j] = c;
+        if (j == 0) {
+            nsum[wave] = n;
+            zsum[wave] = z;
+        }
     }
     __syncthreads();
     // thread e of the first wave: column 64 quarter + e
@@ -626,8 +641,8 @@ __global__ __launch_bounds__(GROUPS * 16) void loss_sum_kernel(LossArgs q) {
         const int e = 64 * quarter + threadIdx.x;
         float ps = 0.0f, zt = 0.0f;
         int cs = 0, nt = 0;
-#pragma unroll 16
-        for (int w = 0; w < GROUPS; ++w) {
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
             ps += psum[w][threadIdx.x / 4][threadIdx.x % 4];
             cs += static_cast<int>(csum[w][threadIdx.x / 4][threadIdx.x % 4]);
             nt += nsum[w];
