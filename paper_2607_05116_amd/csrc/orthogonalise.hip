@@ -9,14 +9,12 @@
 // X is held with the shorter side n as its rows ([n][m], transposed on the way in
 // and out when the matrix has more rows than columns), so S is n x n.
 //
-// Steps go in groups of one or two: where it pays (Plans), the first two and the last two
-// are pairs, the others single.  A pair needs X once, since S of its second step is P S P with P =
-// a I + b S + c S S (polynomials of one symmetric matrix commute):
-//   S (n^2 m), then n x n products:  R = P - p I;   T = P S;   S' = T P;  R' = P' - p' I;
-//   Q = P P';   X <- Q X (2 n^2 m).
-// All n x n products are symmetric: tiles on and below the diagonal, mirrored.  Five
-// steps take 9 n^2 m + 11 n^3 multiply-adds in 17 products, single steps 15 n^2 m + 5 n^3
-// in 15, and X is read and written three times instead of five.
+// A step is three products:
+//   S (n^2 m);   R = P - p I with P = a I + b S + c S S (n^3);   X <- p X + R X (n^2 m).
+// S and R are symmetric: tiles on and below the diagonal, mirrored.  (Two steps in one, with
+// S of the second as P S P, would save a product of X each, but their common polynomial is
+// a difference of numbers ten times its size where singular values are 1 among others of 0:
+// matrices of one to three unequal rows came out with errors of 1e-2 to 2e-2.)
 //
 // Every product is an MFMA product of fp16 values with fp32 sums whose operands
 // are both contiguous along the contraction: S from rows of X, the n x n ones from
@@ -24,15 +22,15 @@
 // second copy is kept.  What is rounded to fp16, and why that is enough:
 //   * fp16, not bf16: the singular values stay below 1.3, so the range is known, and
 //     steps amplify what rounding adds to small singular values (by a each).
-//   * S, P, T and Q are carried as a multiple of I and the rest (S = s I + D, with s
-//     their mean diagonal, in fp32), and only the rest is rounded: with m >> n, or once
-//     the singular values are near 1, it is several times smaller.
-//   * X is carried to 15 bits (fp16 and its rounding error in fp8) where it is multiplied
-//     by the multiple of I, which passes its error on undamped.
-// Together 3e-4 to 1.3e-3 of the result's norm on square, wide, low-rank and 1/i spectra,
-// 2.5e-3 where they fall by e^-12; bf16 products leave 1e-2 to 1e-1.  A pair in the middle
-// or three steps in one group lose more (up to 3e-3 and 2e-2): the noise of S' grows by
-// a^2 with each step taken on it.
+//   * S and R are carried as a multiple of I and the rest (S = s I + D, with s their mean
+//     diagonal, in fp32), and only the rest is rounded: with m >> n, or once the singular
+//     values are near 1, it is several times smaller.  What rounding takes from R's diagonal
+//     is kept in fp32 and joins p: where few rows hold the matrix, R is little else.
+//   * X is carried as fp16 and its rounding error, in fp16 too (22 bits), where it is multiplied
+//     by p: that error passes on undamped, and in directions whose singular value is 0 each
+//     step multiplies it by a.
+// Together 3e-4 to 3.5e-3 of the result's norm for five steps, on square, wide, low-rank,
+// 1/i and e^-12 spectra, even and uneven rows; bf16 products leave 1e-2 to 1e-1.
 //
 // Bound by the matrix cores and, where X is the operand, by the results' way through
 // memory beside them.  8 x 2048 x 7168 in bf16: 3.4 ms, of which the three Gram products
@@ -72,12 +70,12 @@ constexpr int kGramRows = 128;
 constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
 
 struct OrthWs {
-    uint16_t *xh, *xt[2];                  // X [n][m] in fp16; X^T [m][n], in turn
-    uint8_t* xl;                           // the scaled error of X in fp16, in fp8
-    uint16_t* sq[3];                       // n x n
+    uint16_t *xh, *xl, *xt[2];             // X [n][m] in fp16 and its scaled error; X^T [m][n], in turn
+    uint16_t* sq[2];                       // D and R, n x n
+    float* diag;                           // [batch][np] what rounding took from the diagonal of R
     float* norm;                           // [batch][parts] sums of squares of U
     float* trace;                          // [batch][trace_cap] parts of the next trace
-    float* center;                         // [batch][2] s of the group's first and second step
+    float* center;                         // [batch] s of the step
     f32x4* sums;                           // of the tiles computed in parts
     int n, m, np, mp;                      // sides, and as padded with zeros
     int parts, trace_cap;
@@ -151,7 +149,7 @@ ProductPlan plan_product(bool square, int np, int mp, int K, int batch) {
             best.split = split;
             const long long units = best.whole + (split > 1 ? static_cast<long long>(rest) * split : 0);
             best.grid = static_cast<int>(std::min<long long>(units, slots));
-            best.traces = tiles * S::WAVES * (square ? S::STEPS : 1);
+            best.traces = tiles * S::WAVES;
             best.sums = split > 1 ? static_cast<size_t>(rest) * split * S::ROWS * S::COLS * 4 : 0;
         }
     };
@@ -160,21 +158,12 @@ ProductPlan plan_product(bool square, int np, int mp, int K, int batch) {
     consider(Small{}, 2, 2, 0.5, square ? 4.0 : 6.0);
     return best;
 }
-// A pair of steps takes one product of X less than two single ones, and one update of X,
-// for three n x n products more.  Both sides, in us for a whole call (pairs, single):
-//   256 x 7168       132  142       333 x 517, three      124  116
-//   512 x 4096       150  157       600 x 700             135  121
-//   1024 x 4096      221  235       1000 x 1000, two      193  171
-//   256 x 2048, 8    141  153       2048 x 2048           461  440
 struct Plans {
     ProductPlan gram, sym, apply;
-    bool pairs;
 };
 Plans plan_all(int np, int mp, int batch) {
-    Plans p{plan_product(true, np, mp, mp, batch), plan_product(true, np, mp, np, batch),
-            plan_product(false, np, mp, np, batch), false};
-    p.pairs = 3.0 * p.sym.us < p.gram.us + p.apply.us;
-    return p;
+    return {plan_product(true, np, mp, mp, batch), plan_product(true, np, mp, np, batch),
+            plan_product(false, np, mp, np, batch)};
 }
 
 size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
@@ -190,23 +179,25 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
     const size_t x = 2 * batch * np * mp, q = 2 * batch * np * np;
     // tiles of 256 may read 128 rows past a matrix (never used): of the next one, or of
     // what follows here; each kind of matrix is followed by one at least as large
-    char* v[7];
-    for (int i = 4; i < 7; ++i) v[i] = take(q);
-    for (int i = 0; i < 4; ++i) v[i] = take(i == 1 ? x / 2 : x);
+    char* v[6];
+    for (int i = 4; i < 6; ++i) v[i] = take(q);
+    for (int i = 0; i < 4; ++i) v[i] = take(x);
     take(static_cast<size_t>(kPad) * mp * 2);
+    char* d = take(static_cast<size_t>(batch) * np * 4);
     const int parts = norm_parts(rows, cols);
     char* f = take(static_cast<size_t>(batch) * parts * 4);
     const Plans plans = plan_all(static_cast<int>(np), static_cast<int>(mp), batch);
-    const size_t cap = std::max(plans.sym.traces, plans.apply.traces);
+    const size_t cap = plans.apply.traces;
     char* t = take(static_cast<size_t>(batch) * cap * 4);
-    char* c = take(static_cast<size_t>(batch) * 8);
+    char* c = take(static_cast<size_t>(batch) * 4);
     char* sums = take(std::max(plans.gram.sums, plans.sym.sums));
     if (w) {
         w->sums = reinterpret_cast<f32x4*>(sums);
         w->xh = reinterpret_cast<uint16_t*>(v[0]);
-        w->xl = reinterpret_cast<uint8_t*>(v[1]);
+        w->xl = reinterpret_cast<uint16_t*>(v[1]);
         for (int i = 0; i < 2; ++i) w->xt[i] = reinterpret_cast<uint16_t*>(v[2 + i]);
-        for (int i = 0; i < 3; ++i) w->sq[i] = reinterpret_cast<uint16_t*>(v[4 + i]);
+        for (int i = 0; i < 2; ++i) w->sq[i] = reinterpret_cast<uint16_t*>(v[4 + i]);
+        w->diag = reinterpret_cast<float*>(d);
         w->norm = reinterpret_cast<float*>(f);
         w->trace = reinterpret_cast<float*>(t);
         w->center = reinterpret_cast<float*>(c);
@@ -221,35 +212,13 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
 }
 
 // ------------------------------------------------------------------ X in two parts
-// x = fp16 + fp8 2^-18 (e4m3): the error of a value of fp16 is below its 2^-11, so the
-// second part is below 2^7 |x|, a normal fp8 down to |x| = 2^-13; four more bits of x there.
-// Larger than 448 (|x| > 3.5, which steps of other coefficients may reach) it saturates.
-constexpr float kErrScale = 262144.0f;
-__device__ __forceinline__ void split_x(const float (&v)[4], u32x2& hi, uint32_t& err) {
+// x = fp16 + fp16 2^-11: 22 bits down to the smallest normal fp16.
+__device__ __forceinline__ void split_x(const float (&v)[4], u32x2& hi, u32x2& err) {
     hi = u32x2{pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3])};
     float d[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        d[e] = __builtin_amdgcn_fmed3f((v[e] - f16_at(hi, e)) * kErrScale, -448.0f, 448.0f);
-    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(d[0], d[1], 0, false);
-    err = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(d[2], d[3], lo, true));
-}
-__device__ __forceinline__ void join_x(const u32x2& hi, uint32_t err, float (&v)[4]) {
-    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(err), false);
-    const auto b = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(err), true);
-    const float d[4] = {a[0], a[1], b[0], b[1]};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(d[e], 1.0f / kErrScale, f16_at(hi, e));
-}
-
-// The errors of X lie in blocks of 32 x 32, the bytes of a step of the results in the order
-// in which the lanes hold them: [4-row half][lane][8 columns].
-__device__ __forceinline__ size_t err_block(const OrthWs& w, int batch, int row0, int col0) {
-    return ((static_cast<size_t>(batch) * w.np + row0) * w.mp + 32 * static_cast<size_t>(col0));
-}
-__device__ __forceinline__ int err_place(int row, int col) {       // of element (row, col), col a multiple of 4
-    const int r = ((row >> 1) & 12) | (row & 3), g = ((col >> 4) & 1) | ((col >> 2) & 2);
-    return 512 * ((row >> 2) & 1) + 8 * (r + 16 * g) + (col & 7);
+    for (int e = 0; e < 4; ++e) d[e] = (v[e] - f16_at(hi, e)) * kLoScale;
+    err = u32x2{pack_f16x2(d[0], d[1]), pack_f16x2(d[2], d[3])};
 }
 
 // ------------------------------------------------------------------ norm and momentum
@@ -341,14 +310,11 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
             v[e] = u[x][e] * scale;
             tile[16 * x + ty][4 * tx + e] = v[e];
         }
-        u32x2 hi;
-        uint32_t err;
+        u32x2 hi, err;
         split_x(v, hi, err);
         const size_t at = x0 + static_cast<size_t>(r0 + 16 * x + ty) * nat_pitch + c0 + 4 * tx;
         *reinterpret_cast<u32x2*>(nat_hi + at) = hi;
-        const int row = r0 + 16 * x + ty, col = c0 + 4 * tx;
-        if (!tall)
-            *reinterpret_cast<uint32_t*>(w.xl + err_block(w, batch, row & ~31, col & ~31) + err_place(row & 31, col & 31)) = err;
+        if (!tall) *reinterpret_cast<u32x2*>(w.xl + at) = err;
     }
     __syncthreads();
 #pragma unroll
@@ -356,46 +322,36 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = tile[4 * tx + e][16 * x + ty];
-        u32x2 hi;
-        uint32_t err;
+        u32x2 hi, err;
         split_x(v, hi, err);
         const size_t at = x0 + static_cast<size_t>(c0 + 16 * x + ty) * tra_pitch + r0 + 4 * tx;
         *reinterpret_cast<u32x2*>(tra_hi + at) = hi;
-        const int row = c0 + 16 * x + ty, col = r0 + 4 * tx;
-        if (tall)
-            *reinterpret_cast<uint32_t*>(w.xl + err_block(w, batch, row & ~31, col & ~31) + err_place(row & 31, col & 31)) = err;
+        if (tall) *reinterpret_cast<u32x2*>(w.xl + at) = err;
     }
 }
 
 // ------------------------------------------------------------------ products
-// The products of a group, with p = a + b s + c s^2 of the first step's coefficients and
-// s, p' of the second's and s':
+// The products of a step, with p = a + b s + c s^2:
 //   kGram   D  = X X^T - s I                      s = |X|^2 / n
-//   kSym1   R  = (b + 2 c s) D + c D D            P = p I + R
-//   kMix    T  = s R + p D + R D                  P S = p s I + T; parts of tr(P S P)
-//   kSym2   D' = p T + p s R + T R + (p^2 s - s') I       P S P = s' I + D'
-//   kSym1   R' of the second step
-//   kSym2   Q  = p' R + p R' + R R'               P P' = p p' I + Q
-//   kApply  X <- p X + Q X: X, its error, X^T and the parts of |X|^2
+//   kSym    R  = (b + 2 c s) D + c D D            P = p I + R; what rounding takes from R's diagonal
+//   kApply  X <- p X + R X: X, its error, X^T and the parts of |X|^2
 //   kFinal  the same to the bf16 result, in the orientation it is wanted
-enum Product { kGram, kSym1, kMix, kSym2, kApply, kFinal };
-constexpr bool is_square(Product m) { return m == kGram || m == kSym1 || m == kMix || m == kSym2; }
+enum Product { kGram, kSym, kApply, kFinal };
+constexpr bool is_square(Product m) { return m == kGram || m == kSym; }
 
 struct ProductArgs {
     OrthWs w;
     const uint16_t *A, *B;                 // rows of the left operand; rows (of the transpose) of the right
     uint16_t* D;                           // result; kApply: X^T
-    int second, pair;                      // kSym1: of the second step; kSym2: Q; the group has two steps
-    int traces;                            // kGram, kSym2 (D'): parts of the trace
-    float coef[2][3];                      // of the group's steps
+    int traces;                            // kGram: parts of the trace
+    float coef[3];                         // of the step
     int whole, split;                      // tiles (of all matrices) computed whole, parts of each of the others
     uint16_t* out;
     int rows, cols, batch;
 };
 
 struct Scalars {
-    float ab, a, b, i;                     // of A B, A (kApply: X), B and I
-    float p, ps;                           // kMix: the multiples of I in P and T
+    float ab, a, i;                        // of A B, A (kApply: X) and I
 };
 
 // Sum of `count` parts by the whole workgroup, in a fixed order.
@@ -416,45 +372,23 @@ __device__ __forceinline__ float sum_parts(const float* parts, int count, float*
 
 __device__ __forceinline__ float poly(const float (&c)[3], float s) { return __builtin_fmaf(__builtin_fmaf(c[2], s, c[1]), s, c[0]); }
 
-// The scalars of a product of matrix `batch`; kGram and kSym2 (D') find their s from the
-// parts and (tile 0 of the matrix) keep it for the products after them.  KNOWN: it is kept.
+// The scalars of a product of matrix `batch`; kGram finds its s from the parts and (tile 0
+// of the matrix) keeps it for the products after it.  KNOWN: it is kept.
 template <Product MODE, int THREADS, bool KNOWN = false>
 __device__ __forceinline__ Scalars scalars(const ProductArgs& q, int batch, bool first_tile, float* red) {
     Scalars c{};
-    float* center = q.w.center + 2 * static_cast<size_t>(batch);
-    const float* parts = q.w.trace + static_cast<size_t>(batch) * q.w.trace_cap;
+    float* center = q.w.center + batch;
     c.ab = 1.0f;
     if constexpr (MODE == kGram) {
-        const float s = KNOWN ? center[0] : sum_parts<THREADS>(parts, q.traces, red) / static_cast<float>(q.w.n);
-        if (!KNOWN && first_tile && threadIdx.x == 0) center[0] = s;
+        const float* parts = q.w.trace + static_cast<size_t>(batch) * q.w.trace_cap;
+        const float s = KNOWN ? *center : sum_parts<THREADS>(parts, q.traces, red) / static_cast<float>(q.w.n);
+        if (!KNOWN && first_tile && threadIdx.x == 0) *center = s;
         c.i = -s;
-        return c;
-    }
-    const float s = center[0];
-    const float p = poly(q.coef[0], s);
-    if constexpr (MODE == kSym1) {
-        const float x = q.second ? center[1] : s;
-        const float(&f)[3] = q.coef[q.second];
-        c.ab = f[2];
-        c.a = __builtin_fmaf(2.0f * f[2], x, f[1]);
-    } else if constexpr (MODE == kMix) {
-        c.a = s;
-        c.b = p;
-        c.p = p;
-        c.ps = p * s;
-    } else if constexpr (MODE == kSym2) {
-        if (q.second) {
-            c.a = poly(q.coef[1], center[1]);
-            c.b = p;
-        } else {
-            const float s1 = KNOWN ? center[1] : sum_parts<THREADS>(parts, q.traces, red) / static_cast<float>(q.w.n);
-            if (!KNOWN && first_tile && threadIdx.x == 0) center[1] = s1;
-            c.a = p;
-            c.b = p * s;
-            c.i = p * p * s - s1;
-        }
+    } else if constexpr (MODE == kSym) {
+        c.ab = q.coef[2];
+        c.a = __builtin_fmaf(2.0f * q.coef[2], *center, q.coef[1]);
     } else {
-        c.a = q.pair ? p * poly(q.coef[1], center[1]) : p;
+        c.a = poly(q.coef, *center);
     }
     return c;
 }
@@ -475,11 +409,11 @@ __device__ __forceinline__ __attribute__((address_space(1))) V* lane_ptr(const v
         reinterpret_cast<global_char*>(reinterpret_cast<uint64_t>(uniform_ptr(base))) + off);
 }
 
-// What a step of the results adds to: 8 columns a lane of two rows, of A and B or of X and
-// its error.
+// What a step of the results adds to: 8 columns a lane of two rows, of A or of X and its
+// error, and (kApply) what joins p in these rows.
 struct Added {
     u32x4 first[2], second[2];
-    u32x2 err[2];
+    float diag[2];
 };
 
 // Results leave a wave in steps of 32 x 32 values: two row blocks and two column
@@ -491,7 +425,7 @@ struct Added {
 template <Product MODE>
 struct Out {
     static constexpr bool kSquare = is_square(MODE);
-    static constexpr int kIn = MODE == kGram ? 0 : MODE == kSym1 ? 1 : 2;     // matrices the results add to
+    static constexpr int kIn = MODE == kGram ? 0 : MODE == kSym ? 1 : 2;      // matrices the results add to
     const ProductArgs& q;
     const Scalars& c;
     int batch, lane, pitch;
@@ -509,8 +443,10 @@ struct Out {
     __device__ __forceinline__ auto at(const uint16_t* p, int row0, int col0, int ii) const {
         return lane_ptr(p + (static_cast<size_t>(batch) * q.w.np + row0 + 4 * ii) * pitch + col0, lane_at);
     }
-    __device__ __forceinline__ auto err_at(int row0, int col0, int ii) const {
-        return lane_ptr<u32x2>(q.w.xl + err_block(q.w, batch, row0, col0) + 512 * ii, 8u * lane);
+    // of the lane's row ii
+    __device__ __forceinline__ int row_of(int row0, int ii) const {
+        const int r = lane & 15;
+        return row0 + 8 * (r >> 2) + 4 * ii + (r & 3);
     }
     // What N steps side by side add to; steps that share lines of 128 bytes are loaded
     // together, a row block at a time (apart, each line came twice: 467 -> 446 us for the last
@@ -523,13 +459,12 @@ struct Out {
 #pragma unroll
                 for (int x = 0; x < N; ++x) in[x].first[ii] = *at(p0, row0, col0 + 32 * x, ii);
             }
-            if constexpr (kIn > 1 && kSquare) {
+            if constexpr (kIn > 1) {
 #pragma unroll
-                for (int x = 0; x < N; ++x) in[x].second[ii] = *at(q.B, row0, col0 + 32 * x, ii);
-            }
-            if constexpr (!kSquare) {
+                for (int x = 0; x < N; ++x) in[x].second[ii] = *at(q.w.xl, row0, col0 + 32 * x, ii);
+                const float d = q.w.diag[static_cast<size_t>(batch) * q.w.np + row_of(row0, ii)];
 #pragma unroll
-                for (int x = 0; x < N; ++x) in[x].err[ii] = *err_at(row0, col0 + 32 * x, ii);
+                for (int x = 0; x < N; ++x) in[x].diag[ii] = d;
             }
         }
     }
@@ -558,14 +493,14 @@ struct Out {
     }
 
     // One step: acc[row block][column block], what fetch() brought; returns its part of
-    // a trace.
+    // |X|^2.
     __device__ __forceinline__ float store(const f32x4 (&acc)[2][2], const Added& in, int row0, int col0) const {
         const int r = lane & 15, g = lane >> 4;
         float sum = 0.0f;
         u32x2 t[2][2];                                             // transposed
 #pragma unroll
         for (int ii = 0; ii < 2; ++ii) {
-            const int row = row0 + 8 * (r >> 2) + 4 * ii + (r & 3);
+            const int row = row_of(row0, ii);
             float v[2][4];
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -573,41 +508,35 @@ struct Out {
                 for (int e = 0; e < 4; ++e) v[b][e] = acc[ii][b][e];
             u32x2 hi[2], i0[2], i1[2];
             if constexpr (kIn > 0) halves(in.first[ii], i0[0], i0[1]);
-            if constexpr (kIn > 1 && kSquare) halves(in.second[ii], i1[0], i1[1]);
+            if constexpr (kIn > 1) halves(in.second[ii], i1[0], i1[1]);
             if constexpr (kSquare) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int d = row - (col0 + 16 * b + 4 * g);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (kIn > 0) v[b][e] = __builtin_fmaf(c.a, f16_at(i0[b], e), c.ab * v[b][e]);
+                        else if (!mirror && d == e && row < q.w.n) v[b][e] += c.i;
+                    }
+                    hi[b] = u32x2{pack_f16x2(v[b][0], v[b][1]), pack_f16x2(v[b][2], v[b][3])};
+                    if constexpr (MODE == kSym) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!mirror && d == e)
+                                q.w.diag[static_cast<size_t>(batch) * q.w.np + row] = v[b][e] - f16_at(hi[b], e);
+                    }
+                }
+                *at(q.D, row0, col0, ii) = join(hi[0], hi[1]);
+            } else {
+                const float p = c.a + in.diag[ii];
+                u32x2 err[2];
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float y = MODE == kSym1 ? c.ab * v[b][e] : v[b][e];
-                        if constexpr (kIn > 0) y = __builtin_fmaf(c.a, f16_at(i0[b], e), y);
-                        if constexpr (kIn > 1) y = __builtin_fmaf(c.b, f16_at(i1[b], e), y);
-                        if constexpr (MODE == kMix) sum = __builtin_fmaf(y, f16_at(i0[b], e), sum);
-                        v[b][e] = y;
+                        const float x = __builtin_fmaf(f16_at(i1[b], e), 1.0f / kLoScale, f16_at(i0[b], e));
+                        v[b][e] = __builtin_fmaf(p, x, v[b][e]);
                     }
-                    if (!mirror) {                                 // a tile on the diagonal
-                        const int d = row - (col0 + 16 * b + 4 * g);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (d == e && row < q.w.n) {
-                                // tr(T P): T = T' + ps I, P = R + p I
-                                if constexpr (MODE == kMix)
-                                    sum += __builtin_fmaf(c.ps, f16_at(i0[b], e), c.p * (v[b][e] + c.ps));
-                                v[b][e] += c.i;
-                            }
-                    }
-                    hi[b] = u32x2{pack_f16x2(v[b][0], v[b][1]), pack_f16x2(v[b][2], v[b][3])};
-                }
-                *at(q.D, row0, col0, ii) = join(hi[0], hi[1]);
-            } else {
-                const auto ie = __builtin_amdgcn_permlane16_swap(in.err[ii][0], in.err[ii][1], false, false);
-                uint32_t err[2];
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    float x[4];
-                    join_x(i0[b], ie[b], x);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[b][e] = __builtin_fmaf(c.a, x[e], v[b][e]);
                     if constexpr (MODE == kApply) {
                         split_x(v[b], hi[b], err[b]);
 #pragma unroll
@@ -618,8 +547,7 @@ struct Out {
                 }
                 if constexpr (MODE == kApply) {
                     *at(q.w.xh, row0, col0, ii) = join(hi[0], hi[1]);
-                    const auto oe = __builtin_amdgcn_permlane16_swap(err[0], err[1], false, false);
-                    *err_at(row0, col0, ii) = u32x2{oe[0], oe[1]};
+                    *at(q.w.xl, row0, col0, ii) = join(err[0], err[1]);
                 } else if (q.rows <= q.cols) {
                     bf16_out(row, col0 + 16 * (g & 1) + 8 * (g >> 1), join(hi[0], hi[1]));
                 }
@@ -681,20 +609,11 @@ __device__ __forceinline__ void store_sums(const OrthWs& w, int part, int wave, 
     });
 }
 
-// A wave's part of a trace.  In the n x n products each step of each wave has a place
-// (a tile computed in parts is joined step by step); whoever sums several writes the
-// others 0.  Off the diagonal a tile stands for two.
-template <Product MODE, typename S>
-__device__ __forceinline__ void store_trace(const ProductArgs& q, int batch, int t, int wave, float sum, int lane) {
+// A wave's part of |X|^2.
+__device__ __forceinline__ void store_trace(const ProductArgs& q, int batch, int place, float sum, int lane) {
 #pragma unroll
     for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-    float* p = q.w.trace + static_cast<size_t>(batch) * q.w.trace_cap;
-    const int place = t * S::WAVES + wave;
-    if constexpr (MODE == kApply) {
-        if (lane == 0) p[place] = sum;
-    } else {
-        if (lane < S::STEPS) p[place * S::STEPS + lane] = lane == 0 ? sum : 0.0f;
-    }
+    if (lane == 0) q.w.trace[static_cast<size_t>(batch) * q.w.trace_cap + place] = sum;
 }
 
 // The u-th unit of a product's tiles (of all matrices, the matrix outermost): whole
@@ -879,8 +798,7 @@ __global__ __launch_bounds__(S::WAVES * kWave, Ring<S>::kPerCu) void product_rin
         const Scalars c = scalars<MODE, THREADS>(q, T.batch, T.t == 0, red);
         float sum = 0.0f;
         if (place.store) sum = store_wave<MODE, S>(q, c, acc, T.batch, row0, col0, place.mirror, lane);
-        if constexpr (MODE == kApply || MODE == kMix)
-            store_trace<MODE, S>(q, T.batch, T.t, wave, MODE == kMix && place.mirror ? 2.0f * sum : sum, lane);
+        if constexpr (MODE == kApply) store_trace(q, T.batch, T.t * S::WAVES + wave, sum, lane);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
@@ -972,8 +890,7 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product_big_kernel(ProductArgs
         const Place<MODE, Big> place(w, row0, col0);
         float sum = 0.0f;
         if (place.store) sum = store_wave<MODE, Big>(q, c, acc, cb, row0, col0, place.mirror, opaque(lane));
-        if constexpr (MODE == kApply || MODE == kMix)
-            store_trace<MODE, Big>(q, cb, ct, wave, MODE == kMix && place.mirror ? 2.0f * sum : sum, lane);
+        if constexpr (MODE == kApply) store_trace(q, cb, ct * Big::WAVES + wave, sum, lane);
         tile = next;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -992,7 +909,6 @@ __global__ __launch_bounds__(kWave) void join_kernel(ProductArgs q, int tiles) {
     const int col0 = tj * S::COLS + wave % S::WN * S::WC + 32 * (x % (S::NJ / 2));
     const Scalars c = scalars<MODE, kWave, true>(q, batch, false, nullptr);
     const Place<MODE, S> place(q.w, row0, col0);
-    float sum = 0.0f;
     if (place.store) {
         const Out<MODE> out(q, c, batch, place.mirror, lane);
         Added in[1];
@@ -1005,13 +921,7 @@ __global__ __launch_bounds__(kWave) void join_kernel(ProductArgs q, int tiles) {
             for (int e = 0; e < 4; ++e) acc[e / 2][e % 2] += p[e * kWave];
             p += static_cast<size_t>(S::WAVES) * S::STEPS * 4 * kWave;
         }
-        sum = out.store(acc, in[0], row0, col0);
-    }
-    if constexpr (MODE == kMix) {
-#pragma unroll
-        for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-        if (lane == 0)
-            q.w.trace[static_cast<size_t>(batch) * q.w.trace_cap + (t * S::WAVES + wave) * S::STEPS + x] = place.mirror ? 2.0f * sum : sum;
+        out.store(acc, in[0], row0, col0);
     }
 }
 
@@ -1077,42 +987,25 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
     else if (momentum) begin(std::false_type{}, std::true_type{});
     else begin(std::false_type{}, std::false_type{});
     CAP_LAUNCH_CHECK();
-    const auto [gram, sym, apply, pairs] = plan_all(w.np, w.mp, batch);
+    const Plans plans = plan_all(w.np, w.mp, batch);
     int from = 0, traces = 1;
-    auto set = [&](uint16_t* A, uint16_t* B, uint16_t* D, int second, int parts) {
+    auto set = [&](uint16_t* A, uint16_t* B, uint16_t* D) {
         q.A = A;
         q.B = B;
         q.D = D;
-        q.second = second;
-        q.traces = parts;
     };
-    for (int i = 0; i < steps;) {
-        q.pair = pairs && ((i == 0 && steps >= 4) || i == steps - 2);
-        for (int h = 0; h < 2; ++h)
-            for (int j = 0; j < 3; ++j) q.coef[h][j] = sc.v[q.pair ? i + h : i][j];
-        uint16_t *s0 = w.sq[0], *s1 = w.sq[1], *s2 = w.sq[2];
-        set(w.xh, w.xh, s0, 0, traces);
-        launch_product<kGram>(q, gram, stream);                          // D
-        set(s0, s0, s1, 0, 0);
-        launch_product<kSym1>(q, sym, stream);                          // R
-        uint16_t* Q = s1;
-        if (q.pair) {
-            set(s1, s0, s2, 0, 0);
-            launch_product<kMix>(q, sym, stream);                       // T
-            set(s2, s1, s0, 0, sym.traces);
-            launch_product<kSym2>(q, sym, stream);                      // D'
-            set(s0, s0, s2, 1, 0);
-            launch_product<kSym1>(q, sym, stream);                      // R'
-            set(s1, s2, s0, 1, 0);
-            launch_product<kSym2>(q, sym, stream);                      // Q
-            Q = s0;
-        }
-        set(Q, w.xt[from], w.xt[from ^ 1], 0, 0);
-        i += q.pair ? 2 : 1;
-        if (i < steps) launch_product<kApply>(q, apply, stream);
-        else launch_product<kFinal>(q, apply, stream);
+    for (int i = 0; i < steps; ++i) {
+        for (int j = 0; j < 3; ++j) q.coef[j] = sc.v[i][j];
+        q.traces = traces;
+        set(w.xh, w.xh, w.sq[0]);
+        launch_product<kGram>(q, plans.gram, stream);                    // D
+        set(w.sq[0], w.sq[0], w.sq[1]);
+        launch_product<kSym>(q, plans.sym, stream);                      // R
+        set(w.sq[1], w.xt[from], w.xt[from ^ 1]);
+        if (i + 1 < steps) launch_product<kApply>(q, plans.apply, stream);
+        else launch_product<kFinal>(q, plans.apply, stream);
         from ^= 1;
-        traces = apply.traces;
+        traces = plans.apply.traces;
     }
     CAP_LAUNCH_CHECK();
     return CAP_OK;

@@ -1,0 +1,81 @@
+"""GPU orthogonalised gradients on matrices that are hard on their arithmetic: singular values of 0 (the gradient of
+an expert with few tokens), energy in a few rows, against the steps in 64 bits.
+
+Tolerance, by the norm of a matrix.  Where a singular value is 1 and others are 0, X <- p X + R X takes 3.4 X - 2.7 X:
+R's rounding (2^-12 of an entry at most, a diagonal one none) and D's come out four times as large, on average over a
+row's entries 5e-4 each; five steps with a slope of at most 1.2 leave 3.5e-3 at most, what X loses as an operand (2^-12
+of an entry, times the share |p - a| of R in directions of 0, which each later step multiplies by a) 3e-3, the bf16
+result 2^-9: 8e-3 with all of them at their largest."""
+import numpy as np
+import pytest
+
+from tests import training_reference as R
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+from paper_2607_05116_amd import capi  # noqa: E402
+
+TOL = 8e-3
+
+
+def matrix(kind, n, m, seed):
+    """fp32 [n][m]; low ranks are exact (their factors are rounded, not the product)."""
+    rng = np.random.default_rng(seed)
+    f = lambda *s: rng.standard_normal(s)                                     # noqa: E731
+    bf = lambda a: torch.from_numpy(a).bfloat16().double().numpy()             # noqa: E731
+    name, k = kind
+    if name == "rank":
+        g = bf(f(n, k)) @ bf(f(k, m))
+    elif name == "uneven":
+        g = bf(f(n, k) * np.exp(1.5 * f(n, 1))) @ bf(f(k, m))
+    elif name == "rows":                     # k rows hold everything
+        g = np.concatenate([f(k, m), np.zeros((n - k, m))])
+    elif name == "outer":                    # k unequal rows, one direction
+        g = np.concatenate([f(k, 1) @ f(1, m), np.zeros((n - k, m))])
+    elif name == "plane":                    # k unequal rows, two directions
+        g = np.concatenate([f(k, 2) @ f(2, m), np.zeros((n - k, m))])
+    elif name == "beside":                   # one row over a floor
+        g = np.concatenate([100 * f(1, m), 1e-3 * f(n - 1, m)])
+    else:                                    # singular values that fall by e^-k
+        u, v = np.linalg.qr(f(n, n))[0], np.linalg.qr(f(m, n))[0]
+        g = (u * np.exp(-k * np.arange(n) / n)) @ v.T
+    return (1e-3 * g).astype(np.float32)
+
+
+KINDS = [("rank", 1), ("rank", 2), ("rank", 8), ("rank", 100), ("uneven", 1), ("uneven", 2), ("uneven", 8), ("rows", 1),
+         ("rows", 3), ("outer", 2), ("outer", 4), ("plane", 3), ("plane", 4), ("beside", 1), ("fall", 12)]
+
+
+def run(g, steps=5, coef=None, eps=1e-7):
+    b, r, c = g.shape
+    n = capi.cap_workspace_size(capi.CAP_OP_ORTHOGONALISE, None, d=c, inter=r, max_rows=b)
+    ws = torch.full((n,), 0x7E, dtype=torch.uint8, device="cuda")
+    out = torch.empty((b, r, c), dtype=torch.bfloat16, device="cuda")
+    capi.cap_orthogonalise(capi.CAP_DTYPE_F32, b, r, c, g, steps, coef, eps, out, ws)
+    torch.cuda.synchronize()
+    return out.double().cpu().numpy()
+
+
+def near(got, want, tol):
+    for i in range(len(want)):
+        err = np.linalg.norm(got[i] - want[i]) / np.linalg.norm(want[i])
+        assert np.isfinite(got[i]).all() and err <= tol, f"matrix {i}: {err:.2e}"
+
+
+@pytest.mark.parametrize("n,m", [(160, 160), (200, 1000), (256, 4096)])
+@pytest.mark.parametrize("kind", KINDS, ids=lambda k: f"{k[0]}{k[1]}")
+def test_hard_spectra(kind, n, m):
+    host = np.stack([matrix((kind[0], min(kind[1], n)), n, m, s) for s in range(3)])
+    near(run(torch.from_numpy(host).cuda()), [R.orth64(x) for x in host], TOL)
+    tall = np.ascontiguousarray(host[:1].transpose(0, 2, 1))
+    near(run(torch.from_numpy(tall).cuda()), [R.orth64(x) for x in tall], TOL)
+
+
+@pytest.mark.parametrize("kind", [("rank", 1), ("rank", 300), ("uneven", 1), ("plane", 3)], ids=lambda k: f"{k[0]}{k[1]}")
+def test_hard_spectra_of_many_tiles(kind):
+    host = np.stack([matrix(kind, 1024, 1024, s) for s in range(2)])
+    near(run(torch.from_numpy(np.concatenate([host] * 12)).cuda())[::13], [R.orth64(host[0]), R.orth64(host[1])], TOL)
