@@ -9,8 +9,8 @@
 // precision: S has the squares of the singular values, so its rounding reaches
 // directions of sqrt(2^-p) of the largest one.  S_0 is summed in fp32 and the n x n
 // products are taken on values of 21 bits (fp16 pairs, three MFMAs a product), which
-// leaves 1e-6 to 7e-4 of the result's norm over spectra that fall by e^-12; with plain
-// fp16 it would be 1e-3 to 2e-1.
+// leaves 1e-6 to 1e-3 of the result's norm over spectra that fall by e^-12 and low ranks;
+// with plain fp16 it would be 1e-3 to 2e-1.
 //
 //   1. gram_partial_kernel   lower blocks of U U^T over a run of the longer side, fp32
 //                            MFMAs straight from global memory; the momentum update
@@ -218,23 +218,38 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
         *reinterpret_cast<u32x2*>(qw + row * NP + col) = hi;
         *reinterpret_cast<u32x2*>(qw + NP * NP + row * NP + col) = lo;
     };
-    // four values of row 16 bi + r, columns 16 bj + 4 g .., and their mirror image
-    auto put = [&](int bi, int bj, bool mirror, const float (&v)[4], auto&& store) __attribute__((always_inline)) {
+    // four values of row 16 bi + r, columns 16 bj + 4 g .., bj <= bi, and their mirror image.
+    // What is stored is symmetric to the last bit: of a block on the diagonal the lower
+    // triangle, mirrored.  (P, S and Q commute only up to rounding; with both triangles of such
+    // blocks as computed, that difference grew with every step to 1e-1 of the result's norm on
+    // matrices of rank 1.)
+    auto put = [&](int bi, int bj, const float (&v)[4], auto&& store) __attribute__((always_inline)) {
         u32x2 hi, lo;
         split4_rtz(v, hi, lo);
-        store(16 * bi + r, 16 * bj + 4 * g, hi, lo);
-        if (mirror)
-            store(16 * bj + 4 * g + (r & 3), 16 * bi + 4 * (r >> 2), quad_transpose(hi, lane), quad_transpose(lo, lane));
+        const u32x2 th = quad_transpose(hi, lane), tl = quad_transpose(lo, lane);
+        const int below = bi != bj ? 1 : (r >> 2) - g;       // of the diagonal: this lane's 4 x 4 values
+        if (below == 0) {
+            const u32x2 own = {(r & 3) >= 1 ? ~0u : 0xFFFFu, (r & 3) == 3 ? ~0u : (r & 3) == 2 ? 0xFFFFu : 0u};
+            hi = (hi & own) | (th & ~own);
+            lo = (lo & own) | (tl & ~own);
+        }
+        if (below >= 0) store(16 * bi + r, 16 * bj + 4 * g, hi, lo);
+        if (below > 0) store(16 * bj + 4 * g + (r & 3), 16 * bi + 4 * (r >> 2), th, tl);
     };
 #pragma unroll
     for (int x = 0; x < PER; ++x) {
         const int it = x * THREADS + threadIdx.x;
         if (it >= ITEMS) continue;
-        // rows 16 bi + 4 g .., column 16 bj + r: S is symmetric
+        // row 16 bj + r, columns 16 bi + 4 g .. (S is symmetric, each sum the same both ways), and
+        // their mirror image
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = s[x][e] * scale * scale;
-        put(bj[x], bi[x], bi[x] != bj[x], v, to_lds(S));
+        u32x2 hi, lo;
+        split4_rtz(v, hi, lo);
+        to_lds(S)(16 * bj[x] + r, 16 * bi[x] + 4 * g, hi, lo);
+        if (bi[x] != bj[x])
+            to_lds(S)(16 * bi[x] + 4 * g + (r & 3), 16 * bj[x] + 4 * (r >> 2), quad_transpose(hi, lane), quad_transpose(lo, lane));
     }
     __syncthreads();
 
@@ -277,7 +292,8 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
 #pragma unroll
         for (int i = 0; i < WB; ++i)
 #pragma unroll
-            for (int j = 0; j < WB; ++j) put(si * WB + i, sj * WB + j, si != sj, v[i][j], store);
+            for (int j = 0; j < WB; ++j)
+                if (si * WB + i >= sj * WB + j) put(si * WB + i, sj * WB + j, v[i][j], store);
     };
 
     Block q;                                                 // at 128 rows
