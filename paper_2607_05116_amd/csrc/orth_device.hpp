@@ -11,15 +11,28 @@ namespace {
 // smallest normal values leave is normal too.
 constexpr float kLoScale = 2048.0f;
 
+// (The packed bits are opaque to the compiler.  From a product that is rounded to fp16 and
+// back it makes two conversions, one of the fp32 product and one that rounds once, and where
+// the first is a tie they differ: what was left over was then that of another value.)
 __device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
     typedef _Float16 h2 __attribute__((ext_vector_type(2)));
     const h2 v = {static_cast<_Float16>(a), static_cast<_Float16>(b)};
-    return __builtin_bit_cast(uint32_t, v);
+    uint32_t bits = __builtin_bit_cast(uint32_t, v);
+    asm("" : "+v"(bits));
+    return bits;
 }
 __device__ __forceinline__ float f16_to_f32(uint16_t b) { return static_cast<float>(__builtin_bit_cast(_Float16, b)); }
 // value e = 0..3 of four packed fp16
 __device__ __forceinline__ float f16_at(const u32x2& v, int e) {
     return f16_to_f32(static_cast<uint16_t>(v[e >> 1] >> (16 * (e & 1))));
+}
+// Split over both, to 22 bits.
+__device__ __forceinline__ void split4(const float (&v)[4], u32x2& hi, u32x2& lo) {
+    hi = u32x2{pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3])};
+    float d[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) d[e] = (v[e] - f16_at(hi, e)) * kLoScale;
+    lo = u32x2{pack_f16x2(d[0], d[1]), pack_f16x2(d[2], d[3])};
 }
 // Split with rounding toward zero (one instruction for two values): both halves are
 // always used, the second takes up what the first leaves, and 21 bits remain.

@@ -435,18 +435,17 @@ __global__ __launch_bounds__(kGramThreads) void gram_apply_kernel(Source src, in
         f16x8 vh[KS], vl[KS];
         const int c = c0 + r;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
+        for (int ks = 0; ks < KS; ++ks) {
+            u32x2 hi[2], lo[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const f32x4 u = finish_u<MOM, false>(src, 0, step, 0, rows_vec, raw[ks][h]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = u[e] * scale;
-                    const _Float16 hi = static_cast<_Float16>(x);
-                    vh[ks][4 * h + e] = hi;
-                    vl[ks][4 * h + e] = static_cast<_Float16>((x - static_cast<float>(hi)) * kLoScale);
-                }
+                const float x[4] = {u[0] * scale, u[1] * scale, u[2] * scale, u[3] * scale};
+                split4(x, hi[h], lo[h]);
             }
+            vh[ks] = __builtin_bit_cast(f16x8, u32x4{hi[0][0], hi[0][1], hi[1][0], hi[1][1]});
+            vl[ks] = __builtin_bit_cast(f16x8, u32x4{lo[0][0], lo[0][1], lo[1][0], lo[1][1]});
+        }
         // the next are on their way during the products
         if (c0 + kGramWaves * 16 < end) load(c + kGramWaves * 16);
 #pragma unroll 2

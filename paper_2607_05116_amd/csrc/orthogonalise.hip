@@ -211,16 +211,6 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
     return at;
 }
 
-// ------------------------------------------------------------------ X in two parts
-// x = fp16 + fp16 2^-11: 22 bits down to the smallest normal fp16.
-__device__ __forceinline__ void split_x(const float (&v)[4], u32x2& hi, u32x2& err) {
-    hi = u32x2{pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3])};
-    float d[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) d[e] = (v[e] - f16_at(hi, e)) * kLoScale;
-    err = u32x2{pack_f16x2(d[0], d[1]), pack_f16x2(d[2], d[3])};
-}
-
 // ------------------------------------------------------------------ norm and momentum
 // Sum of squares of U over this block's part of its matrix; writes the momentum.  Bound by
 // HBM: 51 us for 235 MB (4.6 TB/s), 39 us for 46 MB of gradient and 185 MB of momentum.
@@ -311,7 +301,7 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
             tile[16 * x + ty][4 * tx + e] = v[e];
         }
         u32x2 hi, err;
-        split_x(v, hi, err);
+        split4(v, hi, err);
         const size_t at = x0 + static_cast<size_t>(r0 + 16 * x + ty) * nat_pitch + c0 + 4 * tx;
         *reinterpret_cast<u32x2*>(nat_hi + at) = hi;
         if (!tall) *reinterpret_cast<u32x2*>(w.xl + at) = err;
@@ -323,7 +313,7 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = tile[4 * tx + e][16 * x + ty];
         u32x2 hi, err;
-        split_x(v, hi, err);
+        split4(v, hi, err);
         const size_t at = x0 + static_cast<size_t>(c0 + 16 * x + ty) * tra_pitch + r0 + 4 * tx;
         *reinterpret_cast<u32x2*>(tra_hi + at) = hi;
         if (tall) *reinterpret_cast<u32x2*>(w.xl + at) = err;
@@ -538,7 +528,7 @@ struct Out {
                         v[b][e] = __builtin_fmaf(p, x, v[b][e]);
                     }
                     if constexpr (MODE == kApply) {
-                        split_x(v[b], hi[b], err[b]);
+                        split4(v[b], hi[b], err[b]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) sum = __builtin_fmaf(v[b][e], v[b][e], sum);
                     } else {

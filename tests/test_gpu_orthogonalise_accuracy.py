@@ -81,7 +81,8 @@ def test_hard_spectra_of_many_tiles(kind):
     near(run(torch.from_numpy(np.concatenate([host] * 12)).cuda())[::13], [R.orth64(host[0]), R.orth64(host[1])], TOL)
 
 
-@pytest.mark.parametrize("n,m", [(1, 50), (8, 30), (16, 64), (64, 64), (64, 200), (128, 1500)])
+@pytest.mark.parametrize("n,m", [(1, 50), (8, 30), (16, 64), (33, 100), (64, 64), (64, 200), (100, 300), (128, 128),
+                                 (128, 1500)])
 @pytest.mark.parametrize("kind", KINDS, ids=lambda k: f"{k[0]}{k[1]}")
 def test_hard_spectra_of_few_rows(kind, n, m):
     host = np.stack([matrix((kind[0], min(kind[1], n)), n, m, s) for s in range(3)])
