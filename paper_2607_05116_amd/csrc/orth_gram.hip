@@ -206,7 +206,7 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
     trace = 0.0f;
 #pragma unroll
     for (int w = 0; w < THREADS / kWave; ++w) trace += red[w];
-    const float scale = 1.0f / (sqrtf(trace) + eps);
+    const float norm = sqrtf(trace), scale = 1.0f / (norm + eps);
 
     auto to_lds = [](Pair<NP>& D) {
         return [&D](int row, int col, const u32x2& hi, const u32x2& lo) __attribute__((always_inline)) {
@@ -376,7 +376,12 @@ __global__ __launch_bounds__(step_threads<NP>()) void gram_steps_kernel(int n, i
     }
     if constexpr (!kSmall)
         if (mine) each(q, to_ws);
-    if (threadIdx.x == 0) scale_out[blockIdx.x] = scale;     // (at its place above the next barrier would wait for it)
+    // X_0 = |X_0| U / |U|: the applying kernel splits values of U / |U| into fp16, however small
+    // an eps well above |U| makes X_0.  (At its place above the next barrier would wait for it.)
+    if (threadIdx.x == 0) {
+        scale_out[2 * blockIdx.x] = trace == 0.0f ? 0.0f : 1.0f / norm;
+        scale_out[2 * blockIdx.x + 1] = norm / (norm + eps);
+    }
 }
 
 // Q X_0: a wave takes 16 positions of the longer side at a time.
@@ -392,7 +397,7 @@ __global__ __launch_bounds__(kGramThreads) void gram_apply_kernel(Source src, in
     const int r = lane & 15, g = lane >> 4;
     const uint16_t* qh = q_ws + static_cast<size_t>(blockIdx.y) * q_stride;
     const uint16_t* ql = qh + NP * NP;
-    const float scale = scales[blockIdx.y];
+    const float scale = scales[2 * blockIdx.y], size = scales[2 * blockIdx.y + 1];
     const size_t base = static_cast<size_t>(blockIdx.y) * n * m;
     const int end = min(m, static_cast<int>(blockIdx.x + 1) * run);
     // position c0 + r of the longer side, values 32 ks + 8 g + 4 h .. of the shorter
@@ -467,7 +472,7 @@ __global__ __launch_bounds__(kGramThreads) void gram_apply_kernel(Source src, in
             }
             float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(corr[e], 1.0f / kLoScale, main[e]);
+            for (int e = 0; e < 4; ++e) v[e] = size * __builtin_fmaf(corr[e], 1.0f / kLoScale, main[e]);
             const u32x2 o = {pack_bf16x2_rne(v[0], v[1]), pack_bf16x2_rne(v[2], v[3])};
             // tall: row c, columns 16 i + 4 g ..; wide: row 16 i + r, columns c0 + 4 g ..
             const int row = tall ? c : i * 16 + r, col = tall ? i * 16 + 4 * g : c0 + 4 * g;
@@ -523,7 +528,7 @@ size_t gram_form_bytes(int batch, int rows, int cols) {
     const GramPlan p = gram_plan(batch, rows, cols);
     const size_t b = batch;
     return align_up(b * p.splits * p.items * 16) + align_up(p.reduce ? b * p.items * 16 : 0) +
-           align_up(b * p.q_values * 2) + align_up(b * 4);
+           align_up(b * p.q_values * 2) + align_up(b * 8);
 }
 
 cap_status gram_form_launch(int batch, int rows, int cols, const void* g, bool bf16, float* momentum, float mu,

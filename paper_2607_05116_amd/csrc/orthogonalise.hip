@@ -29,6 +29,10 @@
 //   * X is carried as fp16 and its rounding error, in fp16 too (22 bits), where it is multiplied
 //     by p: that error passes on undamped, and in directions whose singular value is 0 each
 //     step multiplies it by a.
+//   * What is carried is Y = X / u, with u a number of each matrix.  u = 2^-12 (values of X up
+//     to 16, and 20 bits of one down to 2^-16, which 65536 x 65536 values of equal size have)
+//     while X may have a norm of 1 or more; below, as an eps well above |U| makes it, u
+//     follows a bound of |X|, since with a fixed one X would leave the range of fp16.
 // Together 3e-4 to 3.5e-3 of the result's norm for five steps, on square, wide, low-rank,
 // 1/i and e^-12 spectra, even and uneven rows; bf16 products leave 1e-2 to 1e-1.
 //
@@ -70,12 +74,12 @@ constexpr int kGramRows = 128;
 constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
 
 struct OrthWs {
-    uint16_t *xh, *xl, *xt[2];             // X [n][m] in fp16 and its scaled error; X^T [m][n], in turn
+    uint16_t *xh, *xl, *xt[2];             // Y [n][m] in fp16 and its error; Y^T [m][n], in turn
     uint16_t* sq[2];                       // D and R, n x n
     float* diag;                           // [batch][np] what rounding took from the diagonal of R
     float* norm;                           // [batch][parts] sums of squares of U
     float* trace;                          // [batch][trace_cap] parts of the next trace
-    float* center;                         // [batch] s of the step
+    float* scal;                           // [batch][4] s of the step, |Y|^2, and the units u in turn
     f32x4* sums;                           // of the tiles computed in parts
     int n, m, np, mp;                      // sides, and as padded with zeros
     int parts, trace_cap;
@@ -189,7 +193,7 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
     const Plans plans = plan_all(static_cast<int>(np), static_cast<int>(mp), batch);
     const size_t cap = plans.apply.traces;
     char* t = take(static_cast<size_t>(batch) * cap * 4);
-    char* c = take(static_cast<size_t>(batch) * 4);
+    char* c = take(static_cast<size_t>(batch) * 16);
     char* sums = take(std::max(plans.gram.sums, plans.sym.sums));
     if (w) {
         w->sums = reinterpret_cast<f32x4*>(sums);
@@ -200,7 +204,7 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
         w->diag = reinterpret_cast<float*>(d);
         w->norm = reinterpret_cast<float*>(f);
         w->trace = reinterpret_cast<float*>(t);
-        w->center = reinterpret_cast<float*>(c);
+        w->scal = reinterpret_cast<float*>(c);
         w->n = n;
         w->m = m;
         w->np = static_cast<int>(np);
@@ -245,7 +249,17 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(Source src, size_t s
     }
 }
 
-// X0 in both orientations, padded with zeros: 64 x 64 tiles of U through LDS, four
+constexpr float kUnit = 4096.0f;           // 1 / u, unless X is small
+// y = fp16 + fp16, the second unscaled
+__device__ __forceinline__ void split_y(const float (&v)[4], u32x2& hi, u32x2& err) {
+    hi = u32x2{pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3])};
+    float d[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) d[e] = v[e] - f16_at(hi, e);
+    err = u32x2{pack_f16x2(d[0], d[1]), pack_f16x2(d[2], d[3])};
+}
+
+// Y0 in both orientations, padded with zeros: 64 x 64 tiles of U through LDS, four
 // values a thread at a time.  Bound by HBM: 197 us for 235 MB read and 587 MB written
 // (4.2 TB/s; a large copy reaches 5.1).
 template <bool BF16, bool MOM>
@@ -279,10 +293,12 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
 #pragma unroll
         for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
         if (threadIdx.x == 0) {
-            const float scale = 1.0f / (sqrtf(t) + eps);
+            const float norm = sqrtf(t), scale = t == 0.0f ? 0.0f : kUnit / norm;
             scale_s = scale;
-            // the trace of S_0
-            if (blockIdx.x == 0 && blockIdx.y == 0) w.trace[static_cast<size_t>(batch) * w.trace_cap] = t * scale * scale;
+            if (blockIdx.x == 0 && blockIdx.y == 0) {
+                w.trace[static_cast<size_t>(batch) * w.trace_cap] = t * scale * scale;
+                w.scal[4 * static_cast<size_t>(batch) + 2] = norm / (norm + eps) / kUnit;
+            }
         }
     }
     __syncthreads();
@@ -301,7 +317,7 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
             tile[16 * x + ty][4 * tx + e] = v[e];
         }
         u32x2 hi, err;
-        split4(v, hi, err);
+        split_y(v, hi, err);
         const size_t at = x0 + static_cast<size_t>(r0 + 16 * x + ty) * nat_pitch + c0 + 4 * tx;
         *reinterpret_cast<u32x2*>(nat_hi + at) = hi;
         if (!tall) *reinterpret_cast<u32x2*>(w.xl + at) = err;
@@ -313,7 +329,7 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = tile[4 * tx + e][16 * x + ty];
         u32x2 hi, err;
-        split4(v, hi, err);
+        split_y(v, hi, err);
         const size_t at = x0 + static_cast<size_t>(c0 + 16 * x + ty) * tra_pitch + r0 + 4 * tx;
         *reinterpret_cast<u32x2*>(tra_hi + at) = hi;
         if (tall) *reinterpret_cast<u32x2*>(w.xl + at) = err;
@@ -321,11 +337,11 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
 }
 
 // ------------------------------------------------------------------ products
-// The products of a step, with p = a + b s + c s^2:
-//   kGram   D  = X X^T - s I                      s = |X|^2 / n
+// The products of a step, with p = a + b s + c s^2 and X = u Y:
+//   kGram   D  = u^2 Y Y^T - s I                  s = u^2 |Y|^2 / n
 //   kSym    R  = (b + 2 c s) D + c D D            P = p I + R; what rounding takes from R's diagonal
-//   kApply  X <- p X + R X: X, its error, X^T and the parts of |X|^2
-//   kFinal  the same to the bf16 result, in the orientation it is wanted
+//   kApply  Y <- (u / u') (p Y + R Y): Y, its error, Y^T and the parts of |Y|^2
+//   kFinal  u (p Y + R Y) to the bf16 result, in the orientation it is wanted
 enum Product { kGram, kSym, kApply, kFinal };
 constexpr bool is_square(Product m) { return m == kGram || m == kSym; }
 
@@ -333,7 +349,8 @@ struct ProductArgs {
     OrthWs w;
     const uint16_t *A, *B;                 // rows of the left operand; rows (of the transpose) of the right
     uint16_t* D;                           // result; kApply: X^T
-    int traces;                            // kGram: parts of the trace
+    int traces;                            // kGram: parts of |Y|^2
+    int turn;                              // which of the two units is the step's
     float coef[3];                         // of the step
     int whole, split;                      // tiles (of all matrices) computed whole, parts of each of the others
     uint16_t* out;
@@ -341,7 +358,8 @@ struct ProductArgs {
 };
 
 struct Scalars {
-    float ab, a, i;                        // of A B, A (kApply: X) and I
+    float ab, a, i;                        // of A B, A (kApply: Y) and I
+    float out;                             // kApply, kFinal: of the sum
 };
 
 // Sum of `count` parts by the whole workgroup, in a fixed order.
@@ -363,22 +381,45 @@ __device__ __forceinline__ float sum_parts(const float* parts, int count, float*
 __device__ __forceinline__ float poly(const float (&c)[3], float s) { return __builtin_fmaf(__builtin_fmaf(c[2], s, c[1]), s, c[0]); }
 
 // The scalars of a product of matrix `batch`; kGram finds its s from the parts and (tile 0
-// of the matrix) keeps it for the products after it.  KNOWN: it is kept.
+// of the matrix) keeps it for the products after it; so does kApply with the next unit.
+// KNOWN: they are kept.
 template <Product MODE, int THREADS, bool KNOWN = false>
 __device__ __forceinline__ Scalars scalars(const ProductArgs& q, int batch, bool first_tile, float* red) {
     Scalars c{};
-    float* center = q.w.center + batch;
+    float* k = q.w.scal + 4 * static_cast<size_t>(batch);
     c.ab = 1.0f;
     if constexpr (MODE == kGram) {
         const float* parts = q.w.trace + static_cast<size_t>(batch) * q.w.trace_cap;
-        const float s = KNOWN ? *center : sum_parts<THREADS>(parts, q.traces, red) / static_cast<float>(q.w.n);
-        if (!KNOWN && first_tile && threadIdx.x == 0) *center = s;
+        const float t = KNOWN ? k[1] : sum_parts<THREADS>(parts, q.traces, red);
+        c.ab = k[2 + q.turn] * k[2 + q.turn];
+        const float s = c.ab * t / static_cast<float>(q.w.n);
+        if (!KNOWN && first_tile && threadIdx.x == 0) {
+            k[0] = s;
+            k[1] = t;
+        }
         c.i = -s;
     } else if constexpr (MODE == kSym) {
         c.ab = q.coef[2];
-        c.a = __builtin_fmaf(2.0f * q.coef[2], *center, q.coef[1]);
+        c.a = __builtin_fmaf(2.0f * q.coef[2], k[0], q.coef[1]);
     } else {
-        c.a = poly(q.coef, *center);
+        c.a = poly(q.coef, k[0]);
+        const float u = k[2 + q.turn];
+        c.out = u;
+        if constexpr (MODE == kApply) {
+            // |X'| <= u f, since every singular value's square is at most |X|^2
+            const float t = u * u * k[1];
+            const float f = __builtin_fmaf(__builtin_fmaf(fabsf(q.coef[2]), t, fabsf(q.coef[1])), t, fabsf(q.coef[0])) * sqrtf(k[1]);
+            float next = u;
+            c.out = 1.0f;
+            if (u * f >= 1.0f) {
+                next = 1.0f / kUnit;
+                c.out = u * kUnit;
+            } else if (f > 0.0f) {
+                next = u * f / kUnit;
+                c.out = kUnit / f;
+            }
+            if (first_tile && threadIdx.x == 0) k[2 + (q.turn ^ 1)] = next;
+        }
     }
     return c;
 }
@@ -483,7 +524,7 @@ struct Out {
     }
 
     // One step: acc[row block][column block], what fetch() brought; returns its part of
-    // |X|^2.
+    // |Y|^2.
     __device__ __forceinline__ float store(const f32x4 (&acc)[2][2], const Added& in, int row0, int col0) const {
         const int r = lane & 15, g = lane >> 4;
         float sum = 0.0f;
@@ -505,7 +546,8 @@ struct Out {
                     const int d = row - (col0 + 16 * b + 4 * g);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        if constexpr (kIn > 0) v[b][e] = __builtin_fmaf(c.a, f16_at(i0[b], e), c.ab * v[b][e]);
+                        v[b][e] *= c.ab;
+                        if constexpr (kIn > 0) v[b][e] = __builtin_fmaf(c.a, f16_at(i0[b], e), v[b][e]);
                         else if (!mirror && d == e && row < q.w.n) v[b][e] += c.i;
                     }
                     hi[b] = u32x2{pack_f16x2(v[b][0], v[b][1]), pack_f16x2(v[b][2], v[b][3])};
@@ -524,11 +566,11 @@ struct Out {
                 for (int b = 0; b < 2; ++b) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float x = __builtin_fmaf(f16_at(i1[b], e), 1.0f / kLoScale, f16_at(i0[b], e));
-                        v[b][e] = __builtin_fmaf(p, x, v[b][e]);
+                        const float y = f16_at(i0[b], e) + f16_at(i1[b], e);
+                        v[b][e] = c.out * __builtin_fmaf(p, y, v[b][e]);
                     }
                     if constexpr (MODE == kApply) {
-                        split4(v[b], hi[b], err[b]);
+                        split_y(v[b], hi[b], err[b]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) sum = __builtin_fmaf(v[b][e], v[b][e], sum);
                     } else {
@@ -599,7 +641,7 @@ __device__ __forceinline__ void store_sums(const OrthWs& w, int part, int wave, 
     });
 }
 
-// A wave's part of |X|^2.
+// A wave's part of |Y|^2.
 __device__ __forceinline__ void store_trace(const ProductArgs& q, int batch, int place, float sum, int lane) {
 #pragma unroll
     for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
@@ -987,6 +1029,7 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
     for (int i = 0; i < steps; ++i) {
         for (int j = 0; j < 3; ++j) q.coef[j] = sc.v[i][j];
         q.traces = traces;
+        q.turn = i & 1;
         set(w.xh, w.xh, w.sq[0]);
         launch_product<kGram>(q, plans.gram, stream);                    // D
         set(w.sq[0], w.sq[0], w.sq[1]);

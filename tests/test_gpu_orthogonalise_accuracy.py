@@ -89,3 +89,23 @@ def test_hard_spectra_of_few_rows(kind, n, m):
     near(run(torch.from_numpy(host).cuda()), [R.orth64(x) for x in host], TOL)
     tall = np.ascontiguousarray(host[:1].transpose(0, 2, 1))
     near(run(torch.from_numpy(tall).cuda()), [R.orth64(x) for x in tall], TOL)
+
+
+@pytest.mark.parametrize("n,m", [(16, 40), (64, 100), (128, 300), (160, 200), (256, 1024)])
+@pytest.mark.parametrize("size", [1.0, 1e-1, 1e-2, 1e-3, 1e-5, 1e-8, 1e-12])
+def test_eps_above_the_norm(n, m, size):
+    """|X0| = |U| / (|U| + eps) from 1 to 1e-12, for an ordinary matrix and one of rank 1."""
+    for kind in (("rank", n), ("rank", 1)):
+        host = matrix(kind, n, m, 5)[None]
+        norm = float(np.linalg.norm(host.astype(np.float64)))
+        eps = float(np.float32(norm * (1 / size - 1)))
+        near(run(torch.from_numpy(host).cuda(), eps=eps), [R.orth64(host[0], eps=eps)], TOL)
+
+
+def test_eps_of_each_matrix_of_a_batch():
+    """Matrices of one call that eps leaves at their size, makes small and makes zeros of."""
+    host = np.stack([matrix(("rank", 150), 150, 300, 6 + i) * np.float32(s) for i, s in enumerate((1e6, 1.0, 1e-6, 0.0))])
+    for steps in (1, 2, 5):
+        got = run(torch.from_numpy(host).cuda(), steps=steps, eps=1.0)
+        near(got[:3], [R.orth64(x, steps, eps=1.0) for x in host[:3]], TOL)
+        assert not got[3].any()
