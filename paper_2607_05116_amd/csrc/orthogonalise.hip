@@ -44,11 +44,12 @@
 // A 8192^3 product of the library reaches 1.39 PFLOP/s on the same card.  A single matrix
 // of 256 x 7168 takes 129 us for 22 launches, each 5 to 10 us of latency.
 //
-// Matrices of at most 128 rows or columns take the Gram form (orth_gram.hip): 1 x 128 x 2048
-// takes 70 us there and 100 us here.
+// Matrices of at most 128 rows or columns take the Gram form (orth_gram.hip), unless the
+// steps' gain is too large for it: 1 x 128 x 2048 takes 70 us there and 100 us here.
 #include "orth_device.hpp"
 
 #include <algorithm>
+#include <cmath>
 
 namespace cap {
 namespace {
@@ -73,8 +74,29 @@ constexpr int kMaxNormParts = 256;
 constexpr int kGramRows = 128;
 constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
 
+// What the steps may make of noise where the singular value is 0: each multiplies it by a.
+float steps_gain(const StepCoef& c, int steps) {
+    float now = 0.0f, most = 0.0f;
+    for (int i = 0; i < steps; ++i) {
+        now = std::fabs(c.v[i][0]) * std::max(now, 1.0f);
+        most = std::max(most, now);
+    }
+    return most;
+}
+// Up to this gain (five steps of the default have 485) the last product takes X in 11 bits and
+// the Gram form may be used.  Past it X's error, the lower 11 bits, is an operand too, and the
+// Gram form, whose S takes the gain squared, is left.  Both sides, six and eight steps of the
+// default, error by the norm after rounding to bf16 (1.7e-3):
+//   256 x 1024 of rank 128   11 bits 8.4e-3, 9.5e-2   both parts 1.9e-3, 2.1e-3
+//   64 x 200 of rank 1       Gram 2.8e-3, 8.4e3       here 1.8e-3, 2.4e-3
+// and in us for six: 16 x 768 x 2048 851, 1220; 1 x 256 x 7168 176, 182; 8 x 2048 x 7168 5440,
+// 9440 (no 256 x 256 tiles); in the Gram form and here: 1 x 128 x 2048 80, 127; 40 x 20 x 300
+// 17, 126.
+constexpr float kMostGain = 512.0f;
+
 struct OrthWs {
-    uint16_t *xh, *xl, *xt[2];             // Y [n][m] in fp16 and its error; Y^T [m][n], in turn
+    uint16_t *xh, *xl, *xt[2];             // Y [n][m] in fp16 and its error; Y^T [m][n] (its error beside
+                                           // it in rows of 2 n where that is an operand), in turn
     uint16_t* sq[2];                       // D and R, n x n
     float* diag;                           // [batch][np] what rounding took from the diagonal of R
     float* norm;                           // [batch][parts] sums of squares of U
@@ -130,7 +152,7 @@ int count_tiles(bool square, int np, int mp) {
 //   1 x 256 x 7168        284       229       140         143 (Small)
 // and without parts 3867, 1061, 648 and 204 (for one Gram product of the first and the
 // last: 310 against 215 + 12, 35 against 7 + 5).
-ProductPlan plan_product(bool square, int np, int mp, int K, int batch) {
+ProductPlan plan_product(bool square, int np, int mp, int K, int batch, bool big = true) {
     const int cus = device_cu_count(), KT = K / kStageK;
     ProductPlan best{};
     auto consider = [&](auto shape, int id, int per_cu, double stage, double fixed) {
@@ -157,17 +179,17 @@ ProductPlan plan_product(bool square, int np, int mp, int K, int batch) {
             best.sums = split > 1 ? static_cast<size_t>(rest) * split * S::ROWS * S::COLS * 4 : 0;
         }
     };
-    consider(Big{}, 0, 1, 1.42, square ? 10.0 : 22.0);
+    if (big) consider(Big{}, 0, 1, 1.42, square ? 10.0 : 22.0);
     consider(Mid{}, 1, 1, 1.05, square ? 7.0 : 12.0);
     consider(Small{}, 2, 2, 0.5, square ? 4.0 : 6.0);
     return best;
 }
 struct Plans {
-    ProductPlan gram, sym, apply;
+    ProductPlan gram, sym, apply, apply2;  // apply2: with X in two parts
 };
 Plans plan_all(int np, int mp, int batch) {
     return {plan_product(true, np, mp, mp, batch), plan_product(true, np, mp, np, batch),
-            plan_product(false, np, mp, np, batch)};
+            plan_product(false, np, mp, np, batch), plan_product(false, np, mp, 2 * np, batch, false)};
 }
 
 size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
@@ -185,13 +207,13 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
     // what follows here; each kind of matrix is followed by one at least as large
     char* v[6];
     for (int i = 4; i < 6; ++i) v[i] = take(q);
-    for (int i = 0; i < 4; ++i) v[i] = take(x);
-    take(static_cast<size_t>(kPad) * mp * 2);
+    for (int i = 0; i < 4; ++i) v[i] = take(i < 2 ? x : 2 * x);
+    take(static_cast<size_t>(kPad) * np * 4);
     char* d = take(static_cast<size_t>(batch) * np * 4);
     const int parts = norm_parts(rows, cols);
     char* f = take(static_cast<size_t>(batch) * parts * 4);
     const Plans plans = plan_all(static_cast<int>(np), static_cast<int>(mp), batch);
-    const size_t cap = plans.apply.traces;
+    const size_t cap = std::max(plans.apply.traces, plans.apply2.traces);
     char* t = take(static_cast<size_t>(batch) * cap * 4);
     char* c = take(static_cast<size_t>(batch) * 16);
     char* sums = take(std::max(plans.gram.sums, plans.sym.sums));
@@ -263,7 +285,7 @@ __device__ __forceinline__ void split_y(const float (&v)[4], u32x2& hi, u32x2& e
 // values a thread at a time.  Bound by HBM: 197 us for 235 MB read and 587 MB written
 // (4.2 TB/s; a large copy reaches 5.1).
 template <bool BF16, bool MOM>
-__global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int cols, int vec, float eps, OrthWs w) {
+__global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int cols, int vec, float eps, int two, OrthWs w) {
     __shared__ float tile[64][65];
     __shared__ float scale_s;
     const bool tall = rows > cols;
@@ -303,36 +325,36 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
     }
     __syncthreads();
     const float scale = scale_s;
-    const size_t x0 = static_cast<size_t>(batch) * w.np * w.mp;
     // as given, [rows][cols] is X of a wide matrix and X^T of a tall one
-    uint16_t* const nat_hi = tall ? w.xt[0] : w.xh;
-    uint16_t* const tra_hi = tall ? w.xh : w.xt[0];
-    const size_t nat_pitch = tall ? w.np : w.mp, tra_pitch = tall ? w.mp : w.np;
+    const size_t t_pitch = two ? 2 * w.np : w.np;
+    uint16_t* const x = w.xh + static_cast<size_t>(batch) * w.np * w.mp;
+    uint16_t* const x_err = w.xl + static_cast<size_t>(batch) * w.np * w.mp;
+    uint16_t* const xt = w.xt[0] + static_cast<size_t>(batch) * w.mp * t_pitch;
+    auto store = [&](const float (&v)[4], bool transposed, int row, int col) __attribute__((always_inline)) {
+        u32x2 hi, err;
+        split_y(v, hi, err);
+        const size_t at = static_cast<size_t>(row) * (transposed ? t_pitch : w.mp) + col;
+        *reinterpret_cast<u32x2*>((transposed ? xt : x) + at) = hi;
+        if (!transposed) *reinterpret_cast<u32x2*>(x_err + at) = err;
+        else if (two) *reinterpret_cast<u32x2*>(xt + w.np + at) = err;
+    };
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
+    for (int i = 0; i < 4; ++i) {
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            v[e] = u[x][e] * scale;
-            tile[16 * x + ty][4 * tx + e] = v[e];
+            v[e] = u[i][e] * scale;
+            tile[16 * i + ty][4 * tx + e] = v[e];
         }
-        u32x2 hi, err;
-        split_y(v, hi, err);
-        const size_t at = x0 + static_cast<size_t>(r0 + 16 * x + ty) * nat_pitch + c0 + 4 * tx;
-        *reinterpret_cast<u32x2*>(nat_hi + at) = hi;
-        if (!tall) *reinterpret_cast<u32x2*>(w.xl + at) = err;
+        store(v, tall, r0 + 16 * i + ty, c0 + 4 * tx);
     }
     __syncthreads();
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
+    for (int i = 0; i < 4; ++i) {
         float v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = tile[4 * tx + e][16 * x + ty];
-        u32x2 hi, err;
-        split_y(v, hi, err);
-        const size_t at = x0 + static_cast<size_t>(c0 + 16 * x + ty) * tra_pitch + r0 + 4 * tx;
-        *reinterpret_cast<u32x2*>(tra_hi + at) = hi;
-        if (tall) *reinterpret_cast<u32x2*>(w.xl + at) = err;
+        for (int e = 0; e < 4; ++e) v[e] = tile[4 * tx + e][16 * i + ty];
+        store(v, !tall, c0 + 16 * i + ty, r0 + 4 * tx);
     }
 }
 
@@ -342,8 +364,12 @@ __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int co
 //   kSym    R  = (b + 2 c s) D + c D D            P = p I + R; what rounding takes from R's diagonal
 //   kApply  Y <- (u / u') (p Y + R Y): Y, its error, Y^T and the parts of |Y|^2
 //   kFinal  u (p Y + R Y) to the bf16 result, in the orientation it is wanted
-enum Product { kGram, kSym, kApply, kFinal };
+//   kApply2, kFinal2  the same with Y in two parts: R [Y Y_err], along 2 n
+enum Product { kGram, kSym, kApply, kFinal, kApply2, kFinal2 };
 constexpr bool is_square(Product m) { return m == kGram || m == kSym; }
+constexpr bool is_two(Product m) { return m == kApply2 || m == kFinal2; }
+constexpr bool is_final(Product m) { return m == kFinal || m == kFinal2; }
+constexpr bool is_apply(Product m) { return m == kApply || m == kApply2; }
 
 struct ProductArgs {
     OrthWs w;
@@ -405,7 +431,7 @@ __device__ __forceinline__ Scalars scalars(const ProductArgs& q, int batch, bool
         c.a = poly(q.coef, k[0]);
         const float u = k[2 + q.turn];
         c.out = u;
-        if constexpr (MODE == kApply) {
+        if constexpr (is_apply(MODE)) {
             // |X'| <= u f, since every singular value's square is at most |X|^2
             const float t = u * u * k[1];
             const float f = __builtin_fmaf(__builtin_fmaf(fabsf(q.coef[2]), t, fabsf(q.coef[1])), t, fabsf(q.coef[0])) * sqrtf(k[1]);
@@ -468,12 +494,13 @@ struct Out {
         : q(q_), c(c_), batch(batch_), lane(lane_), pitch(kSquare ? q_.w.np : q_.w.mp), mirror(mirror_) {
         const int r = lane & 15, g = lane >> 4;
         lane_at = 2u * ((8 * (r >> 2) + (r & 3)) * pitch + 16 * (g & 1) + 8 * (g >> 1));
-        lane_t = 2u * ((4 * g + (r & 3)) * q.w.np + 8 * (r >> 2));
+        lane_t = 2u * ((4 * g + (r & 3)) * t_pitch() + 8 * (r >> 2));
         p0 = kSquare ? q.A : q.w.xh;
     }
     __device__ __forceinline__ auto at(const uint16_t* p, int row0, int col0, int ii) const {
         return lane_ptr(p + (static_cast<size_t>(batch) * q.w.np + row0 + 4 * ii) * pitch + col0, lane_at);
     }
+    __device__ __forceinline__ int t_pitch() const { return is_two(MODE) ? 2 * q.w.np : q.w.np; }
     // of the lane's row ii
     __device__ __forceinline__ int row_of(int row0, int ii) const {
         const int r = lane & 15;
@@ -528,7 +555,7 @@ struct Out {
     __device__ __forceinline__ float store(const f32x4 (&acc)[2][2], const Added& in, int row0, int col0) const {
         const int r = lane & 15, g = lane >> 4;
         float sum = 0.0f;
-        u32x2 t[2][2];                                             // transposed
+        u32x2 t[2][2], t_err[2][2];                                // transposed
 #pragma unroll
         for (int ii = 0; ii < 2; ++ii) {
             const int row = row_of(row0, ii);
@@ -569,15 +596,16 @@ struct Out {
                         const float y = f16_at(i0[b], e) + f16_at(i1[b], e);
                         v[b][e] = c.out * __builtin_fmaf(p, y, v[b][e]);
                     }
-                    if constexpr (MODE == kApply) {
+                    if constexpr (is_apply(MODE)) {
                         split_y(v[b], hi[b], err[b]);
+                        if constexpr (is_two(MODE)) t_err[ii][b] = quad_transpose(err[b], lane);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) sum = __builtin_fmaf(v[b][e], v[b][e], sum);
                     } else {
                         hi[b] = u32x2{pack_bf16x2_rne(v[b][0], v[b][1]), pack_bf16x2_rne(v[b][2], v[b][3])};
                     }
                 }
-                if constexpr (MODE == kApply) {
+                if constexpr (is_apply(MODE)) {
                     *at(q.w.xh, row0, col0, ii) = join(hi[0], hi[1]);
                     *at(q.w.xl, row0, col0, ii) = join(err[0], err[1]);
                 } else if (q.rows <= q.cols) {
@@ -591,11 +619,14 @@ struct Out {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const u32x4 y = {t[0][b][0], t[0][b][1], t[1][b][0], t[1][b][1]};
-            if constexpr (MODE == kFinal) {
+            if constexpr (is_final(MODE)) {
                 if (q.rows > q.cols) bf16_out(col0 + 16 * b + 4 * g + (r & 3), row0 + 8 * (r >> 2), y);
-            } else if (MODE == kApply || mirror) {
+            } else if (is_apply(MODE) || mirror) {
                 const size_t rows = kSquare ? q.w.np : q.w.mp;
-                *lane_ptr(q.D + (batch * rows + col0 + 16 * b) * q.w.np + row0, lane_t) = y;
+                uint16_t* const d = q.D + (batch * rows + col0 + 16 * b) * t_pitch() + row0;
+                *lane_ptr(d, lane_t) = y;
+                if constexpr (is_two(MODE))
+                    *lane_ptr(d + q.w.np, lane_t) = u32x4{t_err[0][b][0], t_err[0][b][1], t_err[1][b][0], t_err[1][b][1]};
             }
         }
         return sum;
@@ -728,7 +759,8 @@ __global__ __launch_bounds__(S::WAVES * kWave, Ring<S>::kPerCu) void product_rin
     const int wave = static_cast<int>(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
     const int wm = wave / S::WN, wn = wave % S::WN;
     const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
-    const int KT = (MODE == kGram ? w.mp : w.np) / kStageK, lead = MODE == kGram ? w.mp : w.np;
+    constexpr int kParts = is_two(MODE) ? 2 : 1;                     // of the right operand, along K
+    const int lead = MODE == kGram ? w.mp : w.np, KT = kParts * lead / kStageK;
     const uint32_t pitch = static_cast<uint32_t>(lead) * 2u;
     const LaneMap lm = lane_map(lane);
     const int G = gridDim.x;
@@ -757,14 +789,14 @@ __global__ __launch_bounds__(S::WAVES * kWave, Ring<S>::kPerCu) void product_rin
         a_off[i] = paired_row((wave * R::kA + i) * kRowsPerLoad + lm.ld_row) * pitch + lm.col_b[(wave * R::kA + i) & 1];
 #pragma unroll
     for (int i = 0; i < R::kB; ++i)
-        b_off[i] = ((wave * R::kB + i) * kRowsPerLoad + lm.ld_row) * pitch + lm.col_b[(wave * R::kB + i) & 1];
+        b_off[i] = ((wave * R::kB + i) * kRowsPerLoad + lm.ld_row) * kParts * pitch + lm.col_b[(wave * R::kB + i) & 1];
     const char *pa = nullptr, *pb = nullptr;
     int it_unit = unit, it_left = 0, it_buf = 0;
     auto cursor = [&]() __attribute__((always_inline)) {
         const Tile T = decode(it_unit);
         const size_t b_rows = is_square(MODE) ? w.np : w.mp;
         pa = reinterpret_cast<const char*>(q.A + (static_cast<size_t>(T.batch) * w.np + T.ti * S::ROWS) * lead + T.kt0 * kStageK);
-        pb = reinterpret_cast<const char*>(q.B + (T.batch * b_rows + T.tj * S::COLS) * lead + T.kt0 * kStageK);
+        pb = reinterpret_cast<const char*>(q.B + (T.batch * b_rows + T.tj * S::COLS) * kParts * lead + T.kt0 * kStageK);
         it_left = T.stages;
     };
     auto issue = [&]() __attribute__((always_inline)) {
@@ -776,6 +808,8 @@ __global__ __launch_bounds__(S::WAVES * kWave, Ring<S>::kPerCu) void product_rin
         if (--it_left > 0) {
             pa += kRowB;
             pb += kRowB;
+            if constexpr (is_two(MODE))
+                if (it_left == KT / 2) pa -= pitch;                  // the left operand again, for the second part
         } else if (it_unit + G < units) {
             it_unit += G;
             cursor();
@@ -830,7 +864,7 @@ __global__ __launch_bounds__(S::WAVES * kWave, Ring<S>::kPerCu) void product_rin
         const Scalars c = scalars<MODE, THREADS>(q, T.batch, T.t == 0, red);
         float sum = 0.0f;
         if (place.store) sum = store_wave<MODE, S>(q, c, acc, T.batch, row0, col0, place.mirror, lane);
-        if constexpr (MODE == kApply) store_trace(q, T.batch, T.t * S::WAVES + wave, sum, lane);
+        if constexpr (is_apply(MODE)) store_trace(q, T.batch, T.t * S::WAVES + wave, sum, lane);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
@@ -922,7 +956,7 @@ __global__ __launch_bounds__(kNW * kWave, 1) void product_big_kernel(ProductArgs
         const Place<MODE, Big> place(w, row0, col0);
         float sum = 0.0f;
         if (place.store) sum = store_wave<MODE, Big>(q, c, acc, cb, row0, col0, place.mirror, opaque(lane));
-        if constexpr (MODE == kApply) store_trace(q, cb, ct * Big::WAVES + wave, sum, lane);
+        if constexpr (is_apply(MODE)) store_trace(q, cb, ct * Big::WAVES + wave, sum, lane);
         tile = next;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -969,8 +1003,10 @@ void launch_product(const ProductArgs& args, const ProductPlan& p, hipStream_t s
             if (rest) join_kernel<MODE, S><<<dim3(S::WAVES * S::STEPS, rest), kWave, 0, stream>>>(q, p.tiles);
     };
     if (p.shape == 0) {
-        product_big_kernel<MODE><<<p.grid, Big::WAVES * kWave, 0, stream>>>(q, p.tiles, units);
-        join(Big{});
+        if constexpr (!is_two(MODE)) {
+            product_big_kernel<MODE><<<p.grid, Big::WAVES * kWave, 0, stream>>>(q, p.tiles, units);
+            join(Big{});
+        }
     } else if (p.shape == 1) {
         product_ring_kernel<MODE, Mid><<<p.grid, Mid::WAVES * kWave, 0, stream>>>(q, p.tiles, units);
         join(Mid{});
@@ -983,8 +1019,9 @@ void launch_product(const ProductArgs& args, const ProductPlan& p, hipStream_t s
 }  // namespace
 
 size_t orthogonalise_workspace_bytes(int batch, int rows, int cols) {
-    if ((rows < cols ? rows : cols) <= kGramRows) return gram_form_bytes(batch, rows, cols);
-    return orth_layout(batch, rows, cols, nullptr, nullptr);
+    // (the form goes by the coefficients too)
+    const size_t general = orth_layout(batch, rows, cols, nullptr, nullptr);
+    return (rows < cols ? rows : cols) <= kGramRows ? std::max(general, gram_form_bytes(batch, rows, cols)) : general;
 }
 
 cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, const void* g, float* momentum, float mu,
@@ -994,7 +1031,8 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
     for (int i = 0; i < kMaxOrthSteps; ++i)
         for (int j = 0; j < 3; ++j) sc.v[i][j] = coef && i < steps ? coef[3 * i + j] : kQuintic[j];
     const bool bf16 = dtype == CAP_DTYPE_BF16;
-    if ((rows < cols ? rows : cols) <= kGramRows)
+    const bool two = !(steps_gain(sc, steps) <= kMostGain);
+    if ((rows < cols ? rows : cols) <= kGramRows && !two)
         return gram_form_launch(batch, rows, cols, g, bf16, momentum, mu, nesterov, steps, sc, eps, out, workspace, stream);
     const Source src{g, momentum, mu, nesterov, bf16 ? 1 : 0};
     ProductArgs q{};
@@ -1012,7 +1050,7 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
         constexpr bool bf = decltype(BF)::value, mo = decltype(MOM)::value;
         norm_kernel<bf, mo><<<ngrid, kNormThreads, 0, stream>>>(src, size, norm_per_part(rows, cols), w.parts,
                                                                vector_rows(src, size % 4 == 0 ? 4 : 1), w.norm);
-        start_kernel<bf, mo><<<sgrid, 256, 0, stream>>>(src, rows, cols, vector_rows(src, cols), eps, w);
+        start_kernel<bf, mo><<<sgrid, 256, 0, stream>>>(src, rows, cols, vector_rows(src, cols), eps, two, w);
     };
     if (bf16 && momentum) begin(std::true_type{}, std::true_type{});
     else if (bf16) begin(std::true_type{}, std::false_type{});
@@ -1035,10 +1073,15 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
         set(w.sq[0], w.sq[0], w.sq[1]);
         launch_product<kSym>(q, plans.sym, stream);                      // R
         set(w.sq[1], w.xt[from], w.xt[from ^ 1]);
-        if (i + 1 < steps) launch_product<kApply>(q, plans.apply, stream);
-        else launch_product<kFinal>(q, plans.apply, stream);
+        if (two) {
+            if (i + 1 < steps) launch_product<kApply2>(q, plans.apply2, stream);
+            else launch_product<kFinal2>(q, plans.apply2, stream);
+        } else {
+            if (i + 1 < steps) launch_product<kApply>(q, plans.apply, stream);
+            else launch_product<kFinal>(q, plans.apply, stream);
+        }
         from ^= 1;
-        traces = plans.apply.traces;
+        traces = two ? plans.apply2.traces : plans.apply.traces;
     }
     CAP_LAUNCH_CHECK();
     return CAP_OK;

@@ -109,3 +109,35 @@ def test_eps_of_each_matrix_of_a_batch():
         got = run(torch.from_numpy(host).cuda(), steps=steps, eps=1.0)
         near(got[:3], [R.orth64(x, steps, eps=1.0) for x in host[:3]], TOL)
         assert not got[3].any()
+
+
+@pytest.mark.parametrize("n,m", [(1, 40), (16, 40), (64, 200), (128, 300), (200, 1000), (256, 1024)])
+@pytest.mark.parametrize("steps", [6, 7, 8, 10])
+def test_more_steps(n, m, steps):
+    """1e-3 of arithmetic for each step more than five, and rounding to 22 bits (2^-23) that all steps multiply by a
+    where a singular value is 0, of each step's X: 1.4 times the first one's."""
+    tol = TOL + 1e-3 * (steps - 5) + 1.5 * 2.0 ** -23 * R.QUINTIC[0] ** steps
+    for kind in KINDS:
+        host = matrix((kind[0], min(kind[1], n)), n, m, 11)[None]
+        near(run(torch.from_numpy(host).cuda(), steps), [R.orth64(host[0], steps)], tol)
+    host = matrix(("rank", n), n, m, 12)[None]                                # tall
+    tall = np.ascontiguousarray(host.transpose(0, 2, 1))
+    near(run(torch.from_numpy(tall).cuda(), steps), [R.orth64(tall[0], steps)], tol)
+
+
+def test_most_steps():
+    """Sixteen: rounding rules where a singular value is 0, in any precision; others are as accurate as ever."""
+    for n, m in ((100, 400), (200, 1000)):
+        host = np.stack([matrix(("rank", n), n, m, s) for s in (1, 2)])
+        near(run(torch.from_numpy(host).cuda(), 16), [R.orth64(x, 16) for x in host], TOL + 11e-3)
+        low = matrix(("rank", 3), n, m, 3)[None]
+        assert np.isfinite(run(torch.from_numpy(low).cuda(), 16)).all()
+
+
+def test_steep_coefficients():
+    """Four steps of the default and three that converge: a product of the a of 928; on both sides of 128 rows."""
+    coef = [R.QUINTIC] * 4 + [(1.875, -1.25, 0.375)] * 3
+    for n, m in ((64, 200), (128, 300), (200, 1000)):
+        for kind in (("rank", n), ("rank", 1), ("uneven", 2), ("fall", 12)):
+            host = matrix(kind, n, m, 4)[None]
+            near(run(torch.from_numpy(host).cuda(), 7, coef), [R.orth64(host[0], 7, coef)], TOL)
