@@ -582,9 +582,11 @@ cap_status cap_router_grad(int32_t T, int32_t k, int32_t E, const float *logits,
  * a, whatever the precision: from a product of the a of 2^15 on (nine steps of the
  * default), rounding of 2^-22 times that product shows in matrices of low rank, as it
  * does in sums of 32 bits.  Coefficients that let the singular values, or a step's
- * polynomial, pass about 3 lose accuracy and may overflow fp16.  A non-finite value
- * in a matrix gives NaN in that matrix alone; with eps > 0 a matrix of zeros gives
- * zeros.  0 <= rows, cols <= 65536, batch <= 65535,
+ * polynomial, pass about 3 lose accuracy and may overflow fp16.  |G|_F is a sum of
+ * squares in fp32, so it has to be 0 or from 1e-15 to 1e18: finite values whose squares
+ * overflow give NaN, and values whose squares underflow count as 0.  A non-finite
+ * value or such an overflow gives NaN in that matrix alone; with eps > 0 a matrix of
+ * zeros gives zeros.  0 <= rows, cols <= 65536, batch <= 65535,
  * 1 <= steps <= 16; nothing is done if one of the sizes is 0.  Workspace:
  * cap_workspace_size(CAP_OP_ORTHOGONALISE, NULL, cols, rows, batch, ...), 256-byte
  * aligned; its contents need no initialisation.

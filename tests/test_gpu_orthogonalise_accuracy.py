@@ -141,3 +141,16 @@ def test_steep_coefficients():
         for kind in (("rank", n), ("rank", 1), ("uneven", 2), ("fall", 12)):
             host = matrix(kind, n, m, 4)[None]
             near(run(torch.from_numpy(host).cuda(), 7, coef), [R.orth64(host[0], 7, coef)], TOL)
+
+
+@pytest.mark.parametrize("n,m", [(16, 40), (64, 100), (128, 300), (160, 200), (256, 1024)])
+def test_range_of_the_norm(n, m):
+    """|G| from 1e-15 to 1e18, eps = 0; beyond the range of fp32's squares NaN, and only in that matrix."""
+    one = matrix(("rank", n), n, m, 7)
+    one = (one / np.linalg.norm(one.astype(np.float64))).astype(np.float64)
+    host = np.stack([one * s for s in (1e-15, 1e-9, 1.0, 1e9, 1e18)]).astype(np.float32)
+    near(run(torch.from_numpy(host).cuda(), eps=0.0), [R.orth64(x, eps=0.0) for x in host], TOL)
+    host = np.stack([one, one * 1e25, one]).astype(np.float32)
+    got = run(torch.from_numpy(host).cuda())
+    assert np.isnan(got[1]).all()
+    near(got[::2], [R.orth64(host[0]), R.orth64(host[2])], TOL)
