@@ -38,7 +38,10 @@ def _on(stream):
     """What follows, torch operations too, on the given stream (None: the current one)."""
     if stream is None:
         return contextlib.nullcontext()
-    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
+    if not isinstance(stream, torch.cuda.Stream):
+        # (an ExternalStream of handle 0 is a new stream of torch's pool, not the default one)
+        stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
 
 
 class Muon:
