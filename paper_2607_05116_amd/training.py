@@ -89,6 +89,10 @@ class RouterTrainer:
     T tokens a step over R virtual ranks (T % R == 0), hidden size d (a multiple of 64), E experts (17 to 256), top k;
     expert_rank / expert_local: the placement that pruning goes by (int32 [E]); p its threshold.  n_seq: sequences
     of a batch (their offsets come with each step).
+
+    Tokens that a mask or the offsets leave out count nowhere, whatever their rows of x hold: with either given, a copy
+    of x with zeros in those rows is what the router and the weights' gradient read (a zero gradient times a row that
+    is not finite would be NaN in all of the weights).
     """
 
     def __init__(self, T: int, d: int, E: int, k: int, R: int, ranks_per_node: int, expert_rank, expert_local, w_gate,
@@ -114,31 +118,55 @@ class RouterTrainer:
         self.loss = torch.empty(3, dtype=torch.float32, device=dev)
         self.d_logits = torch.empty((T, E), dtype=_BF16, device=dev)
         self.d_w = torch.empty((1, E, d), dtype=_BF16, device=dev)
+        self.rows = torch.empty((T, d), dtype=_BF16, device=dev)
+        self.token = torch.arange(T, **i32)
+        self.counted, self.one_rule = (torch.empty(T, dtype=torch.bool, device=dev) for _ in range(2))
+        self.zero = torch.zeros((), dtype=_BF16, device=dev)
         self.ws = _workspace(capi.cap_workspace_size(capi.CAP_OP_BALANCE_LOSS, self.topo, max_rows=n_seq), dev)
         self.opt = Muon(1, E, d, lr, mu, device=device)
+
+    def _counted_rows(self, x: torch.Tensor, seq_offsets, token_mask) -> torch.Tensor:
+        """x, with zeros in the rows of tokens that a mask or the offsets leave out."""
+        if seq_offsets is None and token_mask is None:
+            return x
+        self.counted.fill_(True)
+        if seq_offsets is not None:
+            self.counted.logical_and_(torch.ge(self.token, seq_offsets[0], out=self.one_rule))
+            self.counted.logical_and_(torch.lt(self.token, seq_offsets[-1], out=self.one_rule))
+        if token_mask is not None:
+            self.counted.logical_and_(torch.ne(token_mask, 0, out=self.one_rule))
+        return torch.where(self.counted[:, None], x, self.zero, out=self.rows)
 
     def forward(self, x: torch.Tensor, seq_offsets=None, token_mask=None, stream=None):
         """Logits, routing, pruning and the losses of x (bf16 [T][d]); seq_offsets int32 [n_seq + 1] on the device
         (None: one sequence), token_mask uint8 [T] (0: padding)."""
+        with _on(stream):
+            self._forward(self._counted_rows(x, seq_offsets, token_mask), seq_offsets, token_mask)
+
+    def _forward(self, x, seq_offsets, token_mask):
         capi.cap_router_route_prune(self.topo, capi.CAP_DTYPE_BF16, self.d, x, self.w_bf16, self.p, self.idx,
-                                    self.gates, self.keep, self.mask, self.logits, stream)
+                                    self.gates, self.keep, self.mask, self.logits)
         capi.cap_balance_loss(self.T, self.k, self.E, self.logits, self.idx, self.keep, token_mask, seq_offsets,
                               self.n_seq, self.balance_coef, self.z_coef, self.counts, self.probs, self.tokens,
-                              self.loss, self.ws, stream=stream)
+                              self.loss, self.ws)
 
     def backward(self, x: torch.Tensor, d_gates=None, seq_offsets=None, token_mask=None, d_loss=None, stream=None):
         """d_logits and the weights' gradient, for the gradient d_gates at the gates (None: of the losses alone) and
         d_loss at their total (a device scalar; None: 1)."""
         with _on(stream):
-            capi.cap_router_grad(self.T, self.k, self.E, self.logits, self.idx, self.keep, self.gates, d_gates,
-                                 token_mask, seq_offsets, self.n_seq, self.counts, self.tokens, self.balance_coef,
-                                 self.z_coef, d_loss, capi.CAP_DTYPE_BF16, self.d_logits)
-            torch.mm(self.d_logits.t(), x, out=self.d_w[0])
+            self._backward(self._counted_rows(x, seq_offsets, token_mask), d_gates, seq_offsets, token_mask, d_loss)
+
+    def _backward(self, x, d_gates, seq_offsets, token_mask, d_loss):
+        capi.cap_router_grad(self.T, self.k, self.E, self.logits, self.idx, self.keep, self.gates, d_gates, token_mask,
+                             seq_offsets, self.n_seq, self.counts, self.tokens, self.balance_coef, self.z_coef, d_loss,
+                             capi.CAP_DTYPE_BF16, self.d_logits)
+        torch.mm(self.d_logits.t(), x, out=self.d_w[0])
 
     def step(self, x: torch.Tensor, d_gates=None, seq_offsets=None, token_mask=None):
         """One training step on the current stream."""
-        self.forward(x, seq_offsets, token_mask)
-        self.backward(x, d_gates, seq_offsets, token_mask)
+        x = self._counted_rows(x, seq_offsets, token_mask)
+        self._forward(x, seq_offsets, token_mask)
+        self._backward(x, d_gates, seq_offsets, token_mask, None)
         self.opt.step(self.w, self.d_w, self.w_bf16)
 
     def expert_loads(self) -> torch.Tensor:
