@@ -44,6 +44,22 @@ def _on(stream):
     return torch.cuda.stream(stream)
 
 
+def _check(name: str, t, shape, dtypes, device, optional: bool = True):
+    """Refuses what a kernel would misread: it goes by pointers and sizes alone."""
+    if t is None and optional:
+        return
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name}: a tensor is taken, got {type(t).__name__}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} is {list(t.shape)}, expected {list(shape)}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} is {t.dtype}; {' or '.join(str(d) for d in dtypes)} is taken")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
 class Muon:
     """Momentum and orthogonalised updates of `batch` matrices [rows][cols].
 
@@ -66,12 +82,13 @@ class Muon:
     def step(self, w: torch.Tensor, g: torch.Tensor, w_bf16: torch.Tensor | None = None, stream=None):
         """w (fp32, updated in place), g (fp32 or bf16): [batch][rows][cols], contiguous; w_bf16: a copy of the
         weights to refresh (what the layer's kernels read).  All of it on `stream` (None: the current one)."""
-        if tuple(w.shape) != self.shape or tuple(g.shape) != self.shape:
-            raise ValueError(f"weights {tuple(w.shape)} and gradient {tuple(g.shape)}, expected {self.shape}")
-        if w.dtype != torch.float32 or g.dtype not in (torch.float32, _BF16):
-            raise ValueError(f"weights {w.dtype} and gradient {g.dtype}: fp32, and fp32 or bf16, are taken")
-        if not g.is_contiguous():
-            raise ValueError("the gradient must be contiguous")
+        if tuple(w.shape) != self.shape:
+            raise ValueError(f"weights are {list(w.shape)}, expected {list(self.shape)}")
+        if w.dtype != torch.float32 or w.device != self.momentum.device:
+            raise ValueError(f"weights are {w.dtype} on {w.device}; fp32 on {self.momentum.device} is taken")
+        if w_bf16 is not None and tuple(w_bf16.shape) != self.shape:
+            raise ValueError(f"the weights' copy is {list(w_bf16.shape)}, expected {list(self.shape)}")
+        _check("the gradient", g, self.shape, (torch.float32, _BF16), self.momentum.device, optional=False)
         dt = capi.CAP_DTYPE_BF16 if g.dtype == _BF16 else capi.CAP_DTYPE_F32
         with _on(stream):
             capi.cap_muon_update(dt, *self.shape, g, self.momentum, self.mu, self.nesterov, self.steps, None, self.eps,
@@ -125,6 +142,15 @@ class RouterTrainer:
         self.ws = _workspace(capi.cap_workspace_size(capi.CAP_OP_BALANCE_LOSS, self.topo, max_rows=n_seq), dev)
         self.opt = Muon(1, E, d, lr, mu, device=device)
 
+    def _check_batch(self, x, seq_offsets, token_mask, d_gates=None, d_loss=None):
+        dev = self.w.device
+        _check("x", x, (self.T, self.d), (_BF16,), dev, optional=False)
+        _check("seq_offsets", seq_offsets, (self.n_seq + 1,), (torch.int32,), dev)
+        _check("token_mask", token_mask, (self.T,), (torch.uint8, torch.bool), dev)
+        _check("d_gates", d_gates, (self.T, self.k), (torch.float32,), dev)
+        if d_loss is not None:
+            _check("d_loss", d_loss.reshape(-1) if isinstance(d_loss, torch.Tensor) else d_loss, (1,), (torch.float32,), dev)
+
     def _counted_rows(self, x: torch.Tensor, seq_offsets, token_mask) -> torch.Tensor:
         """x, with zeros in the rows of tokens that a mask or the offsets leave out."""
         if seq_offsets is None and token_mask is None:
@@ -139,7 +165,8 @@ class RouterTrainer:
 
     def forward(self, x: torch.Tensor, seq_offsets=None, token_mask=None, stream=None):
         """Logits, routing, pruning and the losses of x (bf16 [T][d]); seq_offsets int32 [n_seq + 1] on the device
-        (None: one sequence), token_mask uint8 [T] (0: padding)."""
+        (None: one sequence), token_mask uint8 or bool [T] (0: padding)."""
+        self._check_batch(x, seq_offsets, token_mask)
         with _on(stream):
             self._forward(self._counted_rows(x, seq_offsets, token_mask), seq_offsets, token_mask)
 
@@ -153,6 +180,7 @@ class RouterTrainer:
     def backward(self, x: torch.Tensor, d_gates=None, seq_offsets=None, token_mask=None, d_loss=None, stream=None):
         """d_logits and the weights' gradient, for the gradient d_gates at the gates (None: of the losses alone) and
         d_loss at their total (a device scalar; None: 1)."""
+        self._check_batch(x, seq_offsets, token_mask, d_gates, d_loss)
         with _on(stream):
             self._backward(self._counted_rows(x, seq_offsets, token_mask), d_gates, seq_offsets, token_mask, d_loss)
 
@@ -164,6 +192,7 @@ class RouterTrainer:
 
     def step(self, x: torch.Tensor, d_gates=None, seq_offsets=None, token_mask=None):
         """One training step on the current stream."""
+        self._check_batch(x, seq_offsets, token_mask, d_gates)
         x = self._counted_rows(x, seq_offsets, token_mask)
         self._forward(x, seq_offsets, token_mask)
         self._backward(x, d_gates, seq_offsets, token_mask, None)
