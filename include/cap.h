@@ -537,7 +537,8 @@ cap_status cap_adjustment_spectrum(const uint32_t *coact, int32_t E, int32_t R, 
  *     balance = (sum over s of E / (k n_s) * sum over e of c_se p_se) / present,
  *     z       = (sum over valid t of lse_t^2) / N;  all 0 without a valid token.
  * Sums are fp32, in an order fixed by T and the offsets.  1 <= k <= 8, k <= E <=
- * 256, T >= 0, n_seq * E < 2^31.  Workspace: cap_workspace_size(
+ * 256, 0 <= T <= 2^31 - 4096, T * k < 2^31, 1 <= n_seq <= 2^30, n_seq * E < 2^31.
+ * Workspace: cap_workspace_size(
  * CAP_OP_BALANCE_LOSS, topo with this T and E, 0, 0, n_seq, ...), 256-byte aligned.
  */
 cap_status cap_balance_loss(int32_t T, int32_t k, int32_t E, const float *logits, const int32_t *idx,

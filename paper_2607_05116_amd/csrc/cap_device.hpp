@@ -12,6 +12,7 @@ constexpr int kWave = 64;
 constexpr int kMaxK = 8;
 constexpr int kMaxE = 256;
 constexpr int kMaxR = 64;
+constexpr int kMaxLossTokens = INT32_MAX - 4095, kMaxLossSequences = 1 << 30;   // of the router's training
 constexpr int kMaxOrthSide = 65536, kMaxOrthBatch = 65535, kMaxOrthSteps = 16;
 constexpr int kMaxDevices = 64;                       // per-device caches of host code
 constexpr size_t kLayoutScratchBytes = size_t(4) << 20;   // cap_dispatch_layout_static's workspace

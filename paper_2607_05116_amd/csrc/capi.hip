@@ -147,7 +147,9 @@ size_t cap_workspace_size(cap_op op, const cap_topology* topo, int32_t d, int32_
         case CAP_OP_ROUTE_LAYOUT:
             return topo_ok(topo) ? front_end_workspace_bytes(topo) : 0;
         case CAP_OP_BALANCE_LOSS:
-            if (!topo || topo->T < 0 || topo->E < 1 || topo->E > kMaxE || max_rows < 1) return 0;
+            if (!topo || topo->T < 0 || topo->T > kMaxLossTokens || topo->E < 1 || topo->E > kMaxE || max_rows < 1 ||
+                max_rows > kMaxLossSequences)
+                return 0;
             return balance_workspace_bytes(topo->T, topo->E, max_rows);
         case CAP_OP_ORTHOGONALISE:
             return orth_shape_ok(max_rows, inter, d) ? orthogonalise_workspace_bytes(max_rows, inter, d) : 0;
@@ -372,9 +374,10 @@ cap_status cap_adjustment_spectrum(const uint32_t* coact, int32_t E, int32_t R, 
 
 namespace {
 
+// (with room in 32 bits for a block past the last token, a grid past the last sequence)
 bool loss_shape_ok(int32_t T, int32_t k, int32_t E, int32_t n_seq) {
-    return T >= 0 && k >= 1 && k <= kMaxK && E >= 1 && E <= kMaxE && k <= E &&
-           static_cast<long long>(T) * k < (1ll << 31) && n_seq >= 1 &&
+    return T >= 0 && T <= kMaxLossTokens && k >= 1 && k <= kMaxK && E >= 1 && E <= kMaxE && k <= E &&
+           static_cast<long long>(T) * k < (1ll << 31) && n_seq >= 1 && n_seq <= kMaxLossSequences &&
            static_cast<long long>(n_seq) * E < (1ll << 31);
 }
 

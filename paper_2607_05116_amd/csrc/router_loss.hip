@@ -212,7 +212,8 @@ LossPlan loss_plan(int T, int S) {
     // wave, so that a piece is left for 128 tokens (32768 tokens of 256 experts 20 us
     // against 25 with four a wave; 8192 of 64 experts 16.5 against 13.8).
     p.waves = p.one_launch ? 16 : kLossWaves;
-    p.per_wave = p.one_launch ? (T <= 64 ? 4 : 16) : T >= 16384 ? 16 : 4;
+    // Past 2^29 tokens 64, for a launch of less than 2^32 threads.
+    p.per_wave = p.one_launch ? (T <= 64 ? 4 : 16) : T > 1 << 29 ? 64 : T >= 16384 ? 16 : 4;
     p.blocks = T > 0 ? (T - 1) / (p.per_wave * p.waves) + 1 : 1;
     return p;
 }
@@ -588,8 +589,9 @@ __global__ __launch_bounds__(WAVES * kWave) void loss_pieces_kernel(LossArgs q) 
     }
 }
 
-// Sequence blockIdx.x, columns 64 blockIdx.y .. + 63: GROUPS groups of 16 lanes share the
-// pieces.  Latency: two loads after one another for every 4 x GROUPS pieces.
+// Sequences blockIdx.x, + gridDim.x, .., columns 64 blockIdx.y .. + 63: GROUPS groups of 16
+// lanes share the pieces.  Latency: two loads after one another for every 4 x GROUPS pieces.
+constexpr int kSumBlocks = 1 << 20;                  // at most, for a launch of less than 2^32 threads
 template <int GROUPS>
 __global__ __launch_bounds__(GROUPS * 16) void loss_sum_kernel(LossArgs q) {
     constexpr int WAVES = GROUPS / 4;
@@ -597,72 +599,75 @@ __global__ __launch_bounds__(GROUPS * 16) void loss_sum_kernel(LossArgs q) {
     __shared__ u32x4 csum[WAVES][16];
     __shared__ int nsum[WAVES];
     __shared__ float zsum[WAVES];
-    const int s = blockIdx.x, quarter = blockIdx.y;
+    const int quarter = blockIdx.y;
     const int group = threadIdx.x / 16, j = threadIdx.x % 16;
     const int col = 64 * quarter + 4 * j;
-    int a, b;
-    sequence_range(q, s, a, b);
-    f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
-    u32x4 c = {0, 0, 0, 0};
-    int n = 0;
-    float z = 0.0f;
-    each_piece(q, kLossWaves, s, a, b, group, GROUPS, [&](size_t slot) __attribute__((always_inline)) {
-        if (col < q.ws.EP) {
-            p += *reinterpret_cast<const f32x4*>(q.ws.psum + slot * q.ws.EP + col);
-            c += *reinterpret_cast<const u32x4*>(q.ws.csum + slot * q.ws.EP + col);
-        }
-        n += q.ws.nsum[slot];
-        z += q.ws.zsum[slot];
-    });
-    // the four groups of a wave, then the waves through LDS
+    for (int s = blockIdx.x; s < q.S; s += gridDim.x) {
+        int a, b;
+        sequence_range(q, s, a, b);
+        f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
+        u32x4 c = {0, 0, 0, 0};
+        int n = 0;
+        float z = 0.0f;
+        each_piece(q, kLossWaves, s, a, b, group, GROUPS, [&](size_t slot) __attribute__((always_inline)) {
+            if (col < q.ws.EP) {
+                p += *reinterpret_cast<const f32x4*>(q.ws.psum + slot * q.ws.EP + col);
+                c += *reinterpret_cast<const u32x4*>(q.ws.csum + slot * q.ws.EP + col);
+            }
+            n += q.ws.nsum[slot];
+            z += q.ws.zsum[slot];
+        });
+        // the four groups of a wave, then the waves through LDS
 #pragma unroll
-    for (int o = 16; o < kWave; o <<= 1) {
+        for (int o = 16; o < kWave; o <<= 1) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            p[i] += __shfl_xor(p[i], o);
-            c[i] += __shfl_xor(c[i], o);
+            for (int i = 0; i < 4; ++i) {
+                p[i] += __shfl_xor(p[i], o);
+                c[i] += __shfl_xor(c[i], o);
+            }
+            n += __shfl_xor(n, o);
+            z += __shfl_xor(z, o);
         }
-        n += __shfl_xor(n, o);
-        z += __shfl_xor(z, o);
-    }
-    const int wave = threadIdx.x / kWave;
-    if (threadIdx.x % kWave < 16) {
-        psum[wave][j] = p;
-        csum[wave][j] = c;
-        if (j == 0) {
-            nsum[wave] = n;
-            zsum[wave] = z;
-        }
-    }
-    __syncthreads();
-    // thread e of the first wave: column 64 quarter + e
-    float term = 0.0f;
-    if (threadIdx.x < 64) {
-        const int e = 64 * quarter + threadIdx.x;
-        float ps = 0.0f, zt = 0.0f;
-        int cs = 0, nt = 0;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            ps += psum[w][threadIdx.x / 4][threadIdx.x % 4];
-            cs += static_cast<int>(csum[w][threadIdx.x / 4][threadIdx.x % 4]);
-            nt += nsum[w];
-            zt += zsum[w];
-        }
-        if (e < q.E) {
-            ps = nt > 0 ? ps / static_cast<float>(nt) : 0.0f;
-            q.probs[static_cast<size_t>(s) * q.E + e] = ps;
-            q.counts[static_cast<size_t>(s) * q.E + e] = cs;
-            term = static_cast<float>(cs) * ps;
-        }
-        term = wave_sum(term);
-        if (threadIdx.x == 0) {
-            q.ws.seq[4 * static_cast<size_t>(s) + quarter] =
-                nt > 0 ? term * (static_cast<float>(q.E) / static_cast<float>(q.k) / static_cast<float>(nt)) : 0.0f;
-            if (quarter == 0) {
-                q.ws.seq[4 * static_cast<size_t>(q.S) + s] = zt;
-                q.tokens[s] = nt;
+        const int wave = threadIdx.x / kWave;
+        if (threadIdx.x % kWave < 16) {
+            psum[wave][j] = p;
+            csum[wave][j] = c;
+            if (j == 0) {
+                nsum[wave] = n;
+                zsum[wave] = z;
             }
         }
+        __syncthreads();
+        // thread e of the first wave: column 64 quarter + e
+        float term = 0.0f;
+        if (threadIdx.x < 64) {
+            const int e = 64 * quarter + threadIdx.x;
+            float ps = 0.0f, zt = 0.0f;
+            int cs = 0, nt = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                ps += psum[w][threadIdx.x / 4][threadIdx.x % 4];
+                cs += static_cast<int>(csum[w][threadIdx.x / 4][threadIdx.x % 4]);
+                nt += nsum[w];
+                zt += zsum[w];
+            }
+            if (e < q.E) {
+                ps = nt > 0 ? ps / static_cast<float>(nt) : 0.0f;
+                q.probs[static_cast<size_t>(s) * q.E + e] = ps;
+                q.counts[static_cast<size_t>(s) * q.E + e] = cs;
+                term = static_cast<float>(cs) * ps;
+            }
+            term = wave_sum(term);
+            if (threadIdx.x == 0) {
+                q.ws.seq[4 * static_cast<size_t>(s) + quarter] =
+                    nt > 0 ? term * (static_cast<float>(q.E) / static_cast<float>(q.k) / static_cast<float>(nt)) : 0.0f;
+                if (quarter == 0) {
+                    q.ws.seq[4 * static_cast<size_t>(q.S) + s] = zt;
+                    q.tokens[s] = nt;
+                }
+            }
+        }
+        if (s + static_cast<int>(gridDim.x) < q.S) __syncthreads();          // the sums in LDS have been read
     }
 }
 
@@ -872,8 +877,9 @@ cap_status balance_loss_launch(int T, int k, int E, const float* logits, const i
         const int quarters = (E + 63) / 64;
         // more groups where a sequence has more pieces than 16 groups take soon (one sequence
         // of 8192 tokens 14 us against 20; 211 sequences of them 15 against 14)
-        if (plan.blocks > 8 * S) loss_sum_kernel<64><<<dim3(S, quarters), 1024, 0, stream>>>(q);
-        else loss_sum_kernel<16><<<dim3(S, quarters), 256, 0, stream>>>(q);
+        const dim3 grid(S < kSumBlocks ? S : kSumBlocks, quarters);
+        if (plan.blocks / 8 > S) loss_sum_kernel<64><<<grid, 1024, 0, stream>>>(q);
+        else loss_sum_kernel<16><<<grid, 256, 0, stream>>>(q);
         loss_final_kernel<<<1, 256, 0, stream>>>(q, quarters);
     }
     CAP_LAUNCH_CHECK();
@@ -884,8 +890,9 @@ cap_status router_grad_launch(int T, int k, int E, const float* logits, const in
                               const float* w, const float* d_w, const uint8_t* mask, const int32_t* offs, int S,
                               const int32_t* counts, const int32_t* tokens, float balance_coef, float z_coef,
                               const float* d_loss, cap_dtype dtype, void* d_logits, hipStream_t stream) {
-    // two steps a wave once the chip is full (32768 tokens 15.2 us against 15.9; 8192 7.6 against 6.4)
-    const int steps = T >= 16384 ? 2 : 1;
+    // two steps a wave once the chip is full (32768 tokens 15.2 us against 15.9; 8192 7.6 against
+    // 6.4); past 2^28 tokens 16, for a launch of less than 2^32 threads
+    const int steps = T > 1 << 28 ? 16 : T >= 16384 ? 2 : 1;
     const int per_block = kGradWaves * kTokPerStep * steps;
     const int blocks = (T - 1) / per_block + 1;
     const bool bf16 = dtype == CAP_DTYPE_BF16;

@@ -1,0 +1,60 @@
+"""GPU load-balance loss and router gradient at the largest numbers of tokens and of sequences that are accepted."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+from paper_2607_05116_amd import capi  # noqa: E402
+
+
+def _forward(x, idx, mask, offs, S, bc, zc):
+    T, E = x.shape
+    o = (torch.full((S, E), -7, dtype=torch.int32, device="cuda"), torch.full((S, E), 9.0, device="cuda"),
+         torch.full((S + 2,), -7, dtype=torch.int32, device="cuda"), torch.full((3,), 9.0, device="cuda"))
+    n = capi.cap_workspace_size(capi.CAP_OP_BALANCE_LOSS, capi.Topology(E=E, T=T), max_rows=S)
+    assert n > 0
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    capi.cap_balance_loss(T, idx.shape[1], E, x, idx, None, mask, offs, S, bc, zc, *o, ws)
+    torch.cuda.synchronize()
+    return o
+
+
+@pytest.mark.parametrize("T", [(1 << 28) + 17, (1 << 29) + 1, (1 << 30) + 77, 2 ** 31 - 4096])
+def test_many_tokens(T):
+    """One expert: P = 1, lse = the logit.  The last four tokens are a sequence, every token before them counts."""
+    x = torch.zeros((T, 1), device="cuda")
+    x[-4:, 0] = torch.tensor([1.0, 2.0, 3.0, 4.0], device="cuda")
+    idx = torch.zeros((T, 1), dtype=torch.int32, device="cuda")
+    offs = torch.tensor([0, T - 4, T], dtype=torch.int32, device="cuda")
+    counts, probs, tokens, loss = _forward(x, idx, None, offs, 2, 1.0, 1.0)
+    assert counts.flatten().tolist() == [T - 4, 4] and tokens.tolist() == [T - 4, 4, 2, T]
+    assert (probs - 1).abs().max().item() <= 1e-5
+    assert abs(loss[1].item() - 1) <= 1e-5 and abs(loss[2].item() - 30 / T) <= 1e-5 * 30 / T
+    d = torch.full((T, 1), 9.0, dtype=torch.bfloat16, device="cuda")
+    capi.cap_router_grad(T, 1, 1, x, idx, None, None, None, None, offs, 2, counts, tokens, 1.0, float(T) / 2, None,
+                         capi.CAP_DTYPE_BF16, d)
+    torch.cuda.synchronize()
+    assert d[-4:, 0].tolist() == [1.0, 2.0, 3.0, 4.0]                        # 2 z_coef lse / N
+    assert not d[:-4].any().item()
+
+
+@pytest.mark.parametrize("S", [(1 << 20) + 3, (1 << 24) + 5])
+def test_many_sequences(S):
+    """Two tokens each in the first and the last sequence, the others empty."""
+    g = torch.Generator("cuda").manual_seed(1)
+    x = torch.randn((4, 2), generator=g, device="cuda")
+    idx = torch.tensor([[0], [1], [1], [1]], dtype=torch.int32, device="cuda")
+    offs = torch.full((S + 1,), 2, dtype=torch.int32, device="cuda")
+    offs[0], offs[-1] = 0, 4
+    counts, probs, tokens, loss = _forward(x, idx, None, offs, S, 1.0, 1.0)
+    p = torch.softmax(x.double(), 1)
+    assert counts[0].tolist() == [1, 1] and counts[-1].tolist() == [0, 2] and counts.sum().item() == 4
+    assert torch.allclose(probs[0].double(), p[:2].mean(0), rtol=1e-5) and torch.allclose(probs[-1].double(), p[2:].mean(0), rtol=1e-5)
+    assert not probs[1:-1].any().item() and not tokens[1:S - 1].any().item()
+    assert tokens[[0, S - 1, S, S + 1]].tolist() == [2, 2, 2, 4]
+    balance = 0.5 * ((p[:2].mean(0)).sum() + 2 * p[2:, 1].mean())
+    z = torch.logsumexp(x.double(), 1).square().mean()
+    assert abs(loss[1].item() - balance.item()) <= 1e-5 and abs(loss[2].item() - z.item()) <= 1e-5
