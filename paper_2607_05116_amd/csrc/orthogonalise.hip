@@ -255,9 +255,13 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(Source src, size_t s
             for (int e = 0; e < 4; ++e) sum = __builtin_fmaf(u[e], u[e], sum);
         }
     } else {
-        for (size_t i = a + threadIdx.x; i < b; i += kNormThreads) {
-            const float u = load_u<BF16, MOM, true>(src, base + i);
-            sum = __builtin_fmaf(u, u, sum);
+        // (in the same order: an odd address changes no bit of the result)
+        for (size_t i = a + 4 * threadIdx.x; i < b; i += 4 * kNormThreads) {
+            float u[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] = i + e < b ? load_u<BF16, MOM, true>(src, base + i + e) : 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = __builtin_fmaf(u[e], u[e], sum);
         }
     }
 #pragma unroll

@@ -154,3 +154,15 @@ def test_range_of_the_norm(n, m):
     got = run(torch.from_numpy(host).cuda())
     assert np.isnan(got[1]).all()
     near(got[::2], [R.orth64(host[0]), R.orth64(host[2])], TOL)
+
+
+@pytest.mark.parametrize("n,m", [(160, 200), (300, 380), (131, 132)])
+def test_an_odd_address_changes_no_bit(n, m):
+    """Same inputs, same bits, also where the norm is summed without vector loads."""
+    host = matrix(("rank", n), n, m, 8)[None]
+    g = torch.from_numpy(host).cuda()
+    a = run(g)
+    for shift in (1, 2, 3):
+        buf = torch.zeros(g.numel() + shift, device="cuda")
+        buf[shift:] = g.flatten()
+        assert np.array_equal(a, run(buf[shift:].view(1, n, m))), shift
