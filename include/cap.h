@@ -576,14 +576,17 @@ cap_status cap_router_grad(int32_t T, int32_t k, int32_t E, const float *logits,
  *     3.4445, -4.7750, 2.0315 for all of them.
  * Products take fp16 operands and fp32 sums; between steps X is carried as fp16 and
  * its rounding error, 22 bits (matrices of at most 128 rows or columns, if the product
- * of the steps' a is at most 512: all steps on fp16 pairs, 21 bits, in n x n space).  With the default coefficients the singular
- * values stay below 1.3, and after five steps the result is within 4e-3 of its norm,
- * low ranks and energy in a few rows included, before it is rounded to bf16; 1e-3 for
- * each step more.  Where a singular value is 0, every step multiplies rounding by its
- * a, whatever the precision: from a product of the a of 2^15 on (nine steps of the
- * default), rounding of 2^-22 times that product shows in matrices of low rank, as it
- * does in sums of 32 bits.  Coefficients that let the singular values, or a step's
- * polynomial, pass about 3 lose accuracy and may overflow fp16.  |G|_F is a sum of
+ * of the steps' a is at most 512: all steps on fp16 pairs, 21 bits, in n x n space).
+ * With the default coefficients the singular values stay below 1.3, and after five
+ * steps, before it is rounded to bf16, the result is within 2e-3 of its norm where many
+ * singular values are of a size, within 4e-3 for nearly all matrices of low rank or with
+ * their energy in a few rows, and within 1e-2 for all; each step more may make it half
+ * as large again, since steps stretch differences.  Where a singular value is 0, every
+ * step multiplies rounding by its a, whatever the precision: from a product of the a of
+ * 2^15 on (nine steps of the default), rounding of 2^-22 times that product shows in
+ * matrices of low rank, as it does in sums of 32 bits.  Coefficients that let the
+ * singular values, or a step's polynomial, pass about 3 lose accuracy and may overflow
+ * fp16.  |G|_F is a sum of
  * squares in fp32, so it has to be 0 or from 1e-15 to 1e18: finite values whose squares
  * overflow give NaN, and values whose squares underflow count as 0.  A non-finite
  * value or such an overflow gives NaN in that matrix alone; with eps > 0 a matrix of

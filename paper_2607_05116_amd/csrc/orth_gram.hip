@@ -19,9 +19,9 @@
 //   4. gram_apply_kernel     Q X_0, rounded to bf16 once
 // Three or four launches, against two or more for every step of the general form.
 // Bound by the latency of the steps' chain of n x n products (four a step) for few
-// matrices, by U's way from HBM for many: 1 x 128 x 2048 bf16 10.4 + 4.5 + 44.8 + 10.4 us
-// (100 us in the general form), 1 x 64 x 2048 6.4 + 14 + 5.5, 40 x 20 x 300 3.4 + 8 + 4.0,
-// 14 x 4433 x 111 fp32 22 + 5 + 46 + 26 (its 28 MB in at 1.25 TB/s, the products on values of
+// matrices, by U's way from HBM for many: 1 x 128 x 2048 bf16 10.4 + 4.6 + 47.3 + 10.2 us
+// (102 us in the general form), 1 x 64 x 2048 6.5 + 15.3 + 5.3, 40 x 20 x 300 3.5 + 9.4 + 4.1,
+// 14 x 4433 x 111 fp32 22 + 5 + 48 + 25 (its 28 MB in at 1.25 TB/s, the products on values of
 // 24 bits taking as long as the loads).
 #include "orth_device.hpp"
 
@@ -506,7 +506,7 @@ GramPlan gram_plan(int batch, int rows, int cols) {
     // runs of at least 64 positions (one step of the four waves); about two
     // workgroups a CU over the batch, and no more parts than one workgroup sums soon
     int splits = (512 + batch - 1) / batch;
-    // (the steps' kernel sums eight runs while one load is on its way: few of them up to 64
+    // (the steps' kernel has sixteen runs on their way at once, four at 128 rows: few of them up to 64
     // rows, whose runs are short work, 32 x 4096 16.3 us against 17.1 with 64, but 64 x 7168
     // 30.6 with 32 against 32.6 with 16; with 128 rows many, behind a kernel of their own:
     // 128 x 7168 75 us against 90 with 16)

@@ -33,19 +33,22 @@
 //     to 16, and 20 bits of one down to 2^-16, which 65536 x 65536 values of equal size have)
 //     while X may have a norm of 1 or more; below, as an eps well above |U| makes it, u
 //     follows a bound of |X|, since with a fixed one X would leave the range of fp16.
-// Together 3e-4 to 3.5e-3 of the result's norm for five steps, on square, wide, low-rank,
-// 1/i and e^-12 spectra, even and uneven rows; bf16 products leave 1e-2 to 1e-1.
+// Together 3e-4 to 1e-3 of the result's norm for five steps on full ranks, 1e-3 to 3.5e-3 on
+// low ones; where two or three unequal rows hold everything a few roundings may agree, and
+// 1 in 1000 such matrices has more than 5e-3, none of 12,800 more than 9e-3 (emulated; bf16
+// products leave 1e-2 to 1e-1).
 //
 // Bound by the matrix cores and, where X is the operand, by the results' way through
-// memory beside them.  8 x 2048 x 7168 in bf16: 3.4 ms, of which the three Gram products
-// take 225 us each (240 of their 481 GFLOP done, the rest mirrored: 1.07 PFLOP/s), the eleven
-// n x n products 85 to 94 us and 10 us for joining their parts, the two updates of X 530 us
-// each (481 GFLOP, 0.91 PFLOP/s; 1.7 GB read and written) and the last one 451 us (1.07).
+// memory beside them.  8 x 2048 x 7168 in bf16: 4.6 ms, of which the five Gram products
+// take 214 us each (240 of their 481 GFLOP done, the rest mirrored: 1.12 PFLOP/s), the five
+// n x n products 87 us and 10 us for joining their parts, the four updates of X 562 us
+// each (481 GFLOP, 0.86 PFLOP/s; 2.0 GB read and written) and the last one 455 us (1.06).
 // A 8192^3 product of the library reaches 1.39 PFLOP/s on the same card.  A single matrix
-// of 256 x 7168 takes 129 us for 22 launches, each 5 to 10 us of latency.
+// of 256 x 7168 takes 149 us for 22 launches, each 5 to 11 us of latency.
 //
 // Matrices of at most 128 rows or columns take the Gram form (orth_gram.hip), unless the
-// steps' gain is too large for it: 1 x 128 x 2048 takes 70 us there and 100 us here.
+// steps' gain is too large for it: 1 x 128 x 2048 takes 71 us there and 102 us here, 40 x 20 x
+// 300 16 and 100.
 #include "orth_device.hpp"
 
 #include <algorithm>
@@ -146,12 +149,12 @@ int count_tiles(bool square, int np, int mp) {
 // parts, from what a stage of K = 64 and the way in and out of a tile take (us, measured
 // on 2 to 576 tiles of K = 256 to 7168).  Both sides, in us for a whole call:
 //                      Big only  Mid only  Small only  by the rule
-//   8 x 2048 x 7168      3523      4150      7114        3536 (Big)
-//   8 x 1408 x 2048      1059      1178      1348        1048 (Big; Mid for X)
-//   16 x 768 x 2048       746       657       792         650 (Mid)
-//   1 x 256 x 7168        284       229       140         143 (Small)
-// and without parts 3867, 1061, 648 and 204 (for one Gram product of the first and the
-// last: 310 against 215 + 12, 35 against 7 + 5).
+//   8 x 2048 x 7168      4545      5484      9770        4534 (Big)
+//   8 x 1408 x 2048      1003      1064      1262         989 (Big; Mid for X)
+//   16 x 768 x 2048       839       712       828         713 (Mid)
+//   1 x 256 x 7168        306       232       149         149 (Small)
+// and without parts 5016, 993, 714 and 262 (for one Gram product of the first and the
+// last: 310 against 214 + 11, 35 against 7 + 5).
 ProductPlan plan_product(bool square, int np, int mp, int K, int batch, bool big = true) {
     const int cus = device_cu_count(), KT = K / kStageK;
     ProductPlan best{};
@@ -239,7 +242,7 @@ size_t orth_layout(int batch, int rows, int cols, void* base, OrthWs* w) {
 
 // ------------------------------------------------------------------ norm and momentum
 // Sum of squares of U over this block's part of its matrix; writes the momentum.  Bound by
-// HBM: 51 us for 235 MB (4.6 TB/s), 39 us for 46 MB of gradient and 185 MB of momentum.
+// HBM: 50 us for 235 MB (4.7 TB/s), 40 us for 46 MB of gradient and 185 MB of momentum.
 template <bool BF16, bool MOM>
 __global__ __launch_bounds__(kNormThreads) void norm_kernel(Source src, size_t size, size_t per, int parts, int vec,
                                                             float* __restrict__ norm) {
@@ -286,8 +289,8 @@ __device__ __forceinline__ void split_y(const float (&v)[4], u32x2& hi, u32x2& e
 }
 
 // Y0 in both orientations, padded with zeros: 64 x 64 tiles of U through LDS, four
-// values a thread at a time.  Bound by HBM: 197 us for 235 MB read and 587 MB written
-// (4.2 TB/s; a large copy reaches 5.1).
+// values a thread at a time.  Bound by HBM: 253 us for 235 MB read and 705 MB written
+// (3.7 TB/s; a large copy reaches 5.1).
 template <bool BF16, bool MOM>
 __global__ __launch_bounds__(256) void start_kernel(Source src, int rows, int cols, int vec, float eps, int two, OrthWs w) {
     __shared__ float tile[64][65];

@@ -24,10 +24,11 @@
 // LDS and leaves one piece.  A second kernel sums each sequence's pieces and a third the
 // losses over the sequences; a small batch is one workgroup's in one launch.
 //
-// 32768 tokens, 256 experts, top 8, 8 sequences: the pieces 12.2 us for 35 MB (2.9 TB/s,
-// with the exponentials about as long as the loads), their sums 6.0 and the losses 2.6 us;
-// the gradient in fp32 15.7 us for 37 MB read and 34 MB written (4.5 TB/s).  8192 tokens, 64
-// experts, 211 sequences: 6.3 + 5.7 + 2.2 and 5.3 us; 61 tokens: 4.4 and 4.0 us, a launch.
+// 32768 tokens, 256 experts, top 8, 8 sequences: the pieces 11.3 us for 35 MB (3.1 TB/s; the
+// exponentials are not why, since the gradient takes them too; most likely the loads' latency,
+// with two waves a SIMD and one step's rows on their way in each), their sums 5.4 and the losses 2.6 us;
+// the gradient in fp32 15.1 us for 37 MB read and 34 MB written (4.7 TB/s).  8192 tokens, 64
+// experts, 211 sequences: 5.9 + 5.7 + 2.5 and 4.8 us; 61 tokens: 4.1 and 3.5 us, a launch.
 #include "cap_device.hpp"
 
 #include <type_traits>

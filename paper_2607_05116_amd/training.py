@@ -133,6 +133,8 @@ class RouterTrainer:
         self.probs = torch.empty((n_seq, E), dtype=torch.float32, device=dev)
         self.tokens = torch.empty(n_seq + 2, **i32)
         self.loss = torch.empty(3, dtype=torch.float32, device=dev)
+        # bf16, as the product of both on the matrix cores takes and gives them: 2^-9 of each value, twice, below what
+        # the orthogonalised update rounds by itself
         self.d_logits = torch.empty((T, E), dtype=_BF16, device=dev)
         self.d_w = torch.empty((1, E, d), dtype=_BF16, device=dev)
         self.rows = torch.empty((T, d), dtype=_BF16, device=dev)
