@@ -1,4 +1,6 @@
 """The calls of the GPU tests take every form of the orthogonalisation (host copy of its rules)."""
+import random
+
 import pytest
 
 from tests.orth_cases import CALLS, kinds
@@ -7,8 +9,21 @@ from tests.orth_forms import GRAM_ROWS, form, gain, workspace_bytes
 EVERY = {(p, s, "whole") for p in ("gram", "sym", "apply") for s in ("Big", "Mid", "Small")} | {
     ("two", "Mid", "whole"), ("two", "Small", "whole"),
     ("gram", "Big", "in parts"), ("gram", "Mid", "in parts"), ("gram", "Small", "in parts"),
-    ("gram", "Big", "the last round in parts"), ("gram", "Small", "the last round in parts"),
+    ("gram", "Big", "the last round in parts"), ("gram", "Mid", "the last round in parts"),
+    ("gram", "Small", "the last round in parts"), ("sym", "Mid", "in parts"),
     ("sym", "Big", "the last round in parts"), ("sym", "Small", "the last round in parts")}
+
+
+def test_no_other_form_is_reached():
+    """By 20,000 calls of up to 60 million values."""
+    rng, seen = random.Random(0), set()
+    for _ in range(20000):
+        b, n = rng.randint(1, 64), rng.randint(1, 24) * 128
+        m = max(n, rng.randint(1, 60) * 128)
+        if b * n * m <= 6e7:
+            f = form(b, n, m, rng.choice([5, 8]))
+            seen |= kinds(f) if f else set()
+    assert not seen - EVERY, seen - EVERY
 
 
 def test_the_calls_take_every_form():
