@@ -1023,24 +1023,17 @@ void launch_product(const ProductArgs& args, const ProductPlan& p, hipStream_t s
     }
 }
 
-}  // namespace
-
-size_t orthogonalise_workspace_bytes(int batch, int rows, int cols) {
-    // (the form goes by the coefficients too)
-    const size_t general = orth_layout(batch, rows, cols, nullptr, nullptr);
-    return (rows < cols ? rows : cols) <= kGramRows ? std::max(general, gram_form_bytes(batch, rows, cols)) : general;
+// Matrices of at most 128 rows or columns that the Gram form leaves are taken in parts of the
+// batch whose workspace stays below this (or one by one), since their sides are padded to 128.
+constexpr size_t kMostPadded = size_t(256) << 20;
+int batch_part(int batch, int rows, int cols) {
+    if ((rows < cols ? rows : cols) > kGramRows) return batch;
+    const size_t one = orth_layout(1, rows, cols, nullptr, nullptr);
+    return static_cast<int>(std::max<size_t>(1, std::min<size_t>(batch, kMostPadded / one)));
 }
 
-cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, const void* g, float* momentum, float mu,
-                                int nesterov, int steps, const float* coef, float eps, void* out, void* workspace,
-                                hipStream_t stream) {
-    StepCoef sc;
-    for (int i = 0; i < kMaxOrthSteps; ++i)
-        for (int j = 0; j < 3; ++j) sc.v[i][j] = coef && i < steps ? coef[3 * i + j] : kQuintic[j];
-    const bool bf16 = dtype == CAP_DTYPE_BF16;
-    const bool two = !(steps_gain(sc, steps) <= kMostGain);
-    if ((rows < cols ? rows : cols) <= kGramRows && !two)
-        return gram_form_launch(batch, rows, cols, g, bf16, momentum, mu, nesterov, steps, sc, eps, out, workspace, stream);
+void general_launch(bool bf16, int batch, int rows, int cols, const void* g, float* momentum, float mu, int nesterov, int steps,
+                    const StepCoef& sc, bool two, float eps, void* out, void* workspace, hipStream_t stream) {
     const Source src{g, momentum, mu, nesterov, bf16 ? 1 : 0};
     ProductArgs q{};
     orth_layout(batch, rows, cols, workspace, &q.w);
@@ -1063,7 +1056,6 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
     else if (bf16) begin(std::true_type{}, std::false_type{});
     else if (momentum) begin(std::false_type{}, std::true_type{});
     else begin(std::false_type{}, std::false_type{});
-    CAP_LAUNCH_CHECK();
     const Plans plans = plan_all(w.np, w.mp, batch);
     int from = 0, traces = 1;
     auto set = [&](uint16_t* A, uint16_t* B, uint16_t* D) {
@@ -1090,7 +1082,37 @@ cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, 
         from ^= 1;
         traces = two ? plans.apply2.traces : plans.apply.traces;
     }
-    CAP_LAUNCH_CHECK();
+}
+
+}  // namespace
+
+size_t orthogonalise_workspace_bytes(int batch, int rows, int cols) {
+    const int part = batch_part(batch, rows, cols);
+    size_t bytes = std::max(orth_layout(part, rows, cols, nullptr, nullptr),
+                            orth_layout(batch % part ? batch % part : part, rows, cols, nullptr, nullptr));
+    // (the form goes by the coefficients too)
+    if ((rows < cols ? rows : cols) <= kGramRows) bytes = std::max(bytes, gram_form_bytes(batch, rows, cols));
+    return bytes;
+}
+
+cap_status orthogonalise_launch(cap_dtype dtype, int batch, int rows, int cols, const void* g, float* momentum, float mu,
+                                int nesterov, int steps, const float* coef, float eps, void* out, void* workspace,
+                                hipStream_t stream) {
+    StepCoef sc;
+    for (int i = 0; i < kMaxOrthSteps; ++i)
+        for (int j = 0; j < 3; ++j) sc.v[i][j] = coef && i < steps ? coef[3 * i + j] : kQuintic[j];
+    const bool bf16 = dtype == CAP_DTYPE_BF16;
+    const bool two = !(steps_gain(sc, steps) <= kMostGain);
+    if ((rows < cols ? rows : cols) <= kGramRows && !two)
+        return gram_form_launch(batch, rows, cols, g, bf16, momentum, mu, nesterov, steps, sc, eps, out, workspace, stream);
+    const int part = batch_part(batch, rows, cols);
+    for (int from = 0; from < batch; from += part) {
+        const size_t at = static_cast<size_t>(from) * rows * cols;
+        general_launch(bf16, std::min(part, batch - from), rows, cols, static_cast<const char*>(g) + at * (bf16 ? 2 : 4),
+                       momentum ? momentum + at : nullptr, mu, nesterov, steps, sc, two, eps, static_cast<uint16_t*>(out) + at,
+                       workspace, stream);
+        CAP_LAUNCH_CHECK();
+    }
     return CAP_OK;
 }
 

@@ -167,3 +167,13 @@ def test_an_odd_address_changes_no_bit(n, m):
         buf = torch.zeros(g.numel() + shift, device="cuda")
         buf[shift:] = g.flatten()
         assert np.array_equal(a, run(buf[shift:].view(1, n, m))), shift
+
+
+@pytest.mark.parametrize("b,n,m", [(2500, 30, 60), (1025, 100, 128), (5, 20, 60000)])
+def test_more_steps_of_large_batches(b, n, m):
+    """Matrices that are taken in parts of the batch; the first, the last and some at every place between."""
+    g = torch.randn((b, n, m), generator=torch.Generator("cuda").manual_seed(n), device="cuda")
+    got = run(g, 6)
+    some = sorted({0, 1, b // 3, b // 2, b - 2, b - 1})
+    near(got[some], [R.orth64(x, 6) for x in g[some].cpu().numpy()], TOL + 1e-3)
+    assert np.isfinite(got).all() and (np.abs(got).sum((1, 2)) > 0).all()

@@ -26,3 +26,10 @@ def test_sizes(T, S, ok):
         assert _balance(T, S, BIG) == capi.CAP_ERR_INVALID_ARG
     size = capi.cap_workspace_size(capi.CAP_OP_BALANCE_LOSS, capi.Topology(E=1, T=T), max_rows=S)
     assert (size > 0) == ok
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(65535, 16, 16), (65535, 64, 100), (4096, 128, 128), (64, 16, 65536), (1, 1, 65536)])
+def test_workspace_of_small_matrices(batch, rows, cols):
+    """Not more than 400 MB beside 64 bytes a value: the padding of small matrices is not paid for a whole batch."""
+    got = capi.cap_workspace_size(capi.CAP_OP_ORTHOGONALISE, None, d=cols, inter=rows, max_rows=batch)
+    assert 0 < got <= (400 << 20) + 64 * batch * rows * cols
