@@ -12,7 +12,9 @@
  *   kept expert on the rank; expert co-activation counts (Sec. IV-B); the
  *   expert-level pruning baseline (Sec. II-D); the Adjustment Approach's
  *   placement spectrum (Sec. V).  For training: the load-balance loss of the
- *   routing with its gradient, and the orthogonalised update of weights.
+ *   routing with its gradient, and the orthogonalised update of weights.  Routing by
+ *   sigmoid or softmax scores with a bias and groups, and the experts' products in
+ *   8-bit floating point, stand beside the routing and the FFN.
  * Expert-parallel ranks are virtual: all of them live on the one GPU.
  *
  * Conventions for every call
@@ -53,6 +55,9 @@ typedef enum {
 
 typedef enum { CAP_DTYPE_F32 = 0, CAP_DTYPE_BF16 = 1 } cap_dtype;
 
+/* How cap_route_scores turns a token's logits into scores. */
+typedef enum { CAP_SCORE_SOFTMAX = 0, CAP_SCORE_SIGMOID = 1 } cap_score_kind;
+
 typedef enum {
     /* destination side: the expanded, expert-sorted rows one rank computes on
        (pack + all-to-all + expand collapsed into one gather on one GPU) */
@@ -83,7 +88,9 @@ typedef enum {
     CAP_OP_ADJUSTMENT = 6,
     CAP_OP_ROUTE_LAYOUT = 7,
     CAP_OP_BALANCE_LOSS = 8,
-    CAP_OP_ORTHOGONALISE = 9
+    CAP_OP_ORTHOGONALISE = 9,
+    CAP_OP_PRODUCT_FP8 = 10,
+    CAP_OP_EXPERT_FFN_FP8 = 11
 } cap_op;
 
 /*
@@ -172,6 +179,10 @@ int32_t cap_version(void);
  *   CAP_OP_ORTHOGONALISE: the products of cap_orthogonalise and cap_muon_update
  *                      (inter is rows, d is cols, max_rows is the batch; topo
  *                      unused, may be NULL).
+ *   CAP_OP_PRODUCT_FP8: partial sums of cap_product_fp8 (d is n, inter is kdim;
+ *                      topo unused).
+ *   CAP_OP_EXPERT_FFN_FP8: the intermediate H of cap_expert_ffn_fp8 in e4m3 with
+ *                      its scales, and partial sums (topo unused).
  *   Other ops need none.
  * Returns 0 for invalid arguments as well.
  */
@@ -607,6 +618,139 @@ cap_status cap_orthogonalise(cap_dtype dtype, int32_t batch, int32_t rows, int32
 cap_status cap_muon_update(cap_dtype dtype, int32_t batch, int32_t rows, int32_t cols, const void *g, float *momentum,
                            float mu, int32_t nesterov, int32_t steps, const float *coef, float eps, void *out, void *ws,
                            size_t ws_bytes, void *stream);
+
+/*
+ * Options of routing by scores.  Arrays are device pointers.
+ *   kind          softmax over the token's experts, or sigmoid of each logit.
+ *   n_groups      experts are cut into this many groups of E / n_groups neighbours
+ *                 (1: no groups); E % n_groups == 0, n_groups <= 64.
+ *   topk_groups   groups a token chooses from, 1 <= topk_groups <= n_groups, with
+ *                 k <= topk_groups * E / n_groups.
+ *   group_top     1 or 2: a group's score is that of its best expert, or the sum of
+ *                 its best two (bias included).
+ *   normalise     != 0: the gates of a token's kept slots sum to `scale`.
+ *   scale         finite, > 0.
+ *   bias[E]       (nullable) fp32, finite: added to scores for the choice of groups
+ *                 and experts only, never to gates.
+ *   token_mask[T] (nullable) 0 for padding tokens, which keep no slot.
+ */
+typedef struct {
+    int32_t kind;
+    int32_t n_groups;
+    int32_t topk_groups;
+    int32_t group_top;
+    int32_t normalise;
+    float scale;
+    const float *bias;
+    const uint8_t *token_mask;
+} cap_score_options;
+
+/*
+ * Top-k routing by scores, gates and communication-aware pruning (Eq. 1; Sec. VI,
+ * Eq. 6 and its greedy), for routers that score experts each by itself or over all,
+ * balance them by a bias and choose among groups.
+ *   logits[T][E]  fp32.  An expert whose logit is -inf or NaN is off, and so is every
+ *                 expert of a masked token; +inf is a precondition violation.
+ * With s_e the score (1 / (1 + e^-l), or the softmax over the experts that are on) and
+ * b_e the bias (0 without one):
+ *   1. the topk_groups groups with the largest score, ties by lower index; experts
+ *      that are off add nothing, and a group without one that is on comes last;
+ *   2. in them the k largest s_e + b_e, ties by lower expert; experts that are off come
+ *      after all others, by index (single experts without a bias are compared by their
+ *      logits, here and in step 1);
+ *   3. shares s_e / (sum over the chosen); devices are kept by a_d / cost_d as in
+ *      cap_route_prune, whose a_d here sums the device's shares, until the kept ones
+ *      reach 1 - p (p == 0: all of them);
+ *   4. w' = scale s_e / (normalise ? sum over the kept : 1) for kept slots, 0 for others.
+ * A slot whose expert is off is not kept (its idx is still an expert of its own).  All
+ * decisions are those of fp64 values, of which keys keep 44 bits: closer ones count as
+ * equal.  Scores below 1e-300 are 0; gates are rounded to fp32 once.
+ * Outputs as cap_route_prune: idx[T][k] in the order of step 2, w, keep, dst_mask.
+ * No workspace.
+ */
+cap_status cap_route_scores(const cap_topology *topo, const float *logits, const cap_score_options *options, float p,
+                            int32_t *idx, float *w, uint8_t *keep, uint64_t *dst_mask, void *stream);
+
+/*
+ * Gradient of the router logits through cap_route_scores' gates (Eq. 1).  The choice,
+ * the pruning and the bias have no gradient.
+ *   idx, keep, w   as cap_route_scores wrote them (keep NULL: every slot is kept);
+ *   d_w[T][k]      the gradient at the gates (not read for slots that are not kept);
+ *   d_add[T][E]    (nullable, fp32) a gradient that reaches the logits another way
+ *                  (cap_router_grad's, of the losses), added before the one rounding;
+ *   options        kind, normalise and scale are used.
+ * With g_s = w_s d_w_s and G their sum over the token's kept slots:
+ *   sigmoid:  d_logit of a kept slot's expert = (1 - s_e) (g_s - (normalise ? w_s G / scale : 0));
+ *   softmax, normalise:                         g_s - w_s G / scale;
+ *   softmax, not:  (g_s for a kept slot's expert) - P_e G for every expert that is on.
+ * d_logits[T][E] (fp32 or bf16) is d_add (or 0) elsewhere.  logits may be NULL for
+ * softmax with normalise.  Slots whose idx is outside [0, E) are skipped.  0 <= T,
+ * T * k < 2^31, 1 <= k <= 8, k <= E <= 256.  No workspace.
+ */
+cap_status cap_route_scores_grad(int32_t T, int32_t k, int32_t E, const float *logits, const int32_t *idx,
+                                 const uint8_t *keep, const float *w, const float *d_w,
+                                 const cap_score_options *options, const float *d_add, cap_dtype dtype,
+                                 void *d_logits, void *stream);
+
+/*
+ * Quantisation to 8-bit floating point (OCP e4m3), with a scale for each block of
+ * block_rows x 128 values of a matrix.
+ *   x[batch][rows][cols]   fp32 or bf16, 16-byte aligned; cols % 128 == 0.
+ *   block_rows             1 (activations) or 128 (weights; the last block may have
+ *                          fewer rows).
+ *   q[batch][rows][cols]   e4m3 codes, 8-byte aligned;
+ *   scale[batch][ceil(rows / block_rows)][cols / 128]  fp32: the least power of two,
+ *                          at least 2^-126, with which the block's largest magnitude
+ *                          is at most 448.
+ * q is x / scale (exact) rounded to nearest even.  NaN and infinities become NaN codes
+ * and take no part in the scale.  Sizes may be 0; batch * rows * cols < 2^37 and, for
+ * blocks of 128 rows, fewer than 2^24 blocks.  No workspace.
+ */
+cap_status cap_quantise_fp8(cap_dtype dtype, int32_t batch, int32_t rows, int32_t cols, int32_t block_rows,
+                            const void *x, void *q, float *scale, void *stream);
+
+/*
+ * Products of expert-sorted rows with their expert's weights in 8-bit floating point
+ * (a plain product with E_loc = 1 and row_offsets = {0, rows}):
+ *   y[i][j] = sum over blocks b of K  x_scale[r][b] w_scale[l][j / 128][b]
+ *             (sum over k in b of x[r][k] w[l][j][k]),
+ *   for the rows i of expert l, r = row_src ? row_src[i] : i.
+ *   x[x_rows][kdim]        e4m3 codes, 16-byte aligned; x_scale[x_rows][kdim / 128] fp32.
+ *   row_src[max_rows]      (nullable) as cap_expert_ffn_gather: entries outside
+ *                          [0, x_rows) are clamped into it.  NULL needs x_rows >= max_rows.
+ *   row_offsets[E_loc + 1], max_rows   as cap_expert_ffn; rows of y past them are not written.
+ *   w[E_loc][n][kdim]      e4m3 codes, 16-byte aligned;
+ *   w_scale[E_loc][ceil(n / 128)][kdim / 128] fp32, any values.
+ *   y[max_rows][n]         fp32 or bf16 (out_dtype).
+ * Sums are fp32.  With a bf16 result the matrix cores' 8-bit instructions are used,
+ * which drop, within each eight neighbours along K, what is below 2^-13 of the largest
+ * product (about 1.4e-5 of y on normal values, 1 / 280 of a bf16 result's step); with
+ * an fp32 result their bf16 instructions, in which products are exact.  kdim % 128 == 0, 128 <= kdim <= 2^15; 1 <= n; E_loc <= 256;
+ * x_rows * kdim and n * kdim < 2^32.  Workspace: cap_workspace_size(CAP_OP_PRODUCT_FP8,
+ * NULL, n, kdim, max_rows, ...), 256-byte aligned (may be NULL if that is 0).
+ */
+cap_status cap_product_fp8(cap_dtype out_dtype, int32_t E_loc, int32_t n, int32_t kdim, int32_t max_rows,
+                           const void *x, const float *x_scale, int32_t x_rows, const int32_t *row_src,
+                           const int32_t *row_offsets, const void *w, const float *w_scale, void *y, void *ws,
+                           size_t ws_bytes, void *stream);
+
+/*
+ * cap_expert_ffn (row_src NULL) or cap_expert_ffn_gather in 8-bit floating point (Eq. 1
+ * Expert_i): y = W2 q(silu(W1 x) * (W3 x)), where q quantises each row of H from fp32
+ * as cap_quantise_fp8 does (blocks of 1 x 128); products as cap_product_fp8.
+ *   x[x_rows][d], x_scale[x_rows][d / 128]  quantised once per token;
+ *   w1, w3 [E_loc][inter][d], s1, s3 [E_loc][inter / 128][d / 128];
+ *   w2 [E_loc][d][inter], s2 [E_loc][d / 128][inter / 128];  y[max_rows][d] bf16.
+ * d % 128 == 0, inter % 128 == 0, d, inter <= 2^15; other limits as cap_product_fp8
+ * (x_rows * d and max_rows * inter < 2^32).  Workspace: cap_workspace_size(
+ * CAP_OP_EXPERT_FFN_FP8, NULL, d, inter, max_rows, ...), 256-byte aligned; its contents
+ * need no initialisation.
+ */
+cap_status cap_expert_ffn_fp8(int32_t E_loc, int32_t d, int32_t inter, int32_t max_rows, const void *x,
+                              const float *x_scale, int32_t x_rows, const int32_t *row_src,
+                              const int32_t *row_offsets, const void *w1, const float *s1, const void *w3,
+                              const float *s3, const void *w2, const float *s2, void *y, void *ws, size_t ws_bytes,
+                              void *stream);
 
 #ifdef __cplusplus
 }

@@ -9,6 +9,7 @@ Function names follow the C ABI: cap_route_prune, cap_route_prune_naive, cap_rou
 cap_dispatch_layout,
 cap_permute, cap_row_plan, cap_expert_ffn, cap_expert_ffn_gather, cap_expert_ffn_ex, cap_expert_ffn_combine,
 cap_combine, cap_coactivation, cap_balance_loss, cap_router_grad, cap_orthogonalise, cap_muon_update,
+cap_route_scores, cap_route_scores_grad, cap_quantise_fp8, cap_product_fp8, cap_expert_ffn_fp8,
 cap_workspace_size, cap_status_string, cap_version.
 """
 from __future__ import annotations
@@ -23,11 +24,12 @@ LIB_PATH = os.path.join(_HERE, "libcap.so")
 
 CAP_OK, CAP_ERR_INVALID_ARG, CAP_ERR_UNSUPPORTED, CAP_ERR_WORKSPACE, CAP_ERR_HIP = 0, -1, -2, -3, -4
 CAP_DTYPE_F32, CAP_DTYPE_BF16 = 0, 1
+CAP_SCORE_SOFTMAX, CAP_SCORE_SIGMOID = 0, 1
 CAP_PERMUTE_EXPERT_GATHER, CAP_PERMUTE_SEND_PACK, CAP_PERMUTE_ROW_SOURCE = 0, 1, 2
 CAP_COMBINE_DEST_REDUCE, CAP_COMBINE_SRC_REDUCE, CAP_COMBINE_DEST_REDUCE_MULTI = 0, 1, 2
 (CAP_OP_ROUTE_PRUNE, CAP_OP_DISPATCH_LAYOUT, CAP_OP_PERMUTE, CAP_OP_EXPERT_FFN,
  CAP_OP_COMBINE, CAP_OP_COACTIVATION, CAP_OP_ADJUSTMENT, CAP_OP_ROUTE_LAYOUT, CAP_OP_BALANCE_LOSS,
- CAP_OP_ORTHOGONALISE) = range(10)
+ CAP_OP_ORTHOGONALISE, CAP_OP_PRODUCT_FP8, CAP_OP_EXPERT_FFN_FP8) = range(12)
 
 EXPORTS = ["cap_status_string", "cap_version", "cap_workspace_size", "cap_route_prune", "cap_route_prune_naive",
            "cap_router_route_prune",
@@ -35,7 +37,8 @@ EXPORTS = ["cap_status_string", "cap_version", "cap_workspace_size", "cap_route_
            "cap_combine", "cap_coactivation", "cap_dispatch_layout_static",
            "cap_dispatch_layout_static_max_bytes", "cap_adjustment_spectrum", "cap_route_layout",
            "cap_row_plan", "cap_expert_ffn_combine", "cap_balance_loss", "cap_router_grad", "cap_orthogonalise",
-           "cap_muon_update"]
+           "cap_muon_update", "cap_route_scores", "cap_route_scores_grad", "cap_quantise_fp8", "cap_product_fp8",
+           "cap_expert_ffn_fp8"]
 
 
 class CapError(RuntimeError):
@@ -54,6 +57,12 @@ class Topology(ctypes.Structure):
 class FfnOptions(ctypes.Structure):
     _fields_ = [("wait_errors", ctypes.c_void_p), ("max_workgroups", ctypes.c_int32),
                 ("spin_limit", ctypes.c_int32), ("force_wait_timeout", ctypes.c_int32)]
+
+
+class ScoreOptions(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("topk_groups", ctypes.c_int32),
+                ("group_top", ctypes.c_int32), ("normalise", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("bias", ctypes.c_void_p), ("token_mask", ctypes.c_void_p)]
 
 
 class Layout(ctypes.Structure):
@@ -102,6 +111,14 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "cap_orthogonalise": ([ctypes.c_int, i32, i32, i32, vp, i32, vp, f32, vp, vp, sz, vp], ctypes.c_int),
         "cap_muon_update": ([ctypes.c_int, i32, i32, i32, vp, vp, f32, i32, i32, vp, f32, vp, vp, sz, vp],
                             ctypes.c_int),
+        "cap_route_scores": ([P(Topology), vp, P(ScoreOptions), f32, vp, vp, vp, vp, vp], ctypes.c_int),
+        "cap_route_scores_grad": ([i32, i32, i32, vp, vp, vp, vp, vp, P(ScoreOptions), vp, ctypes.c_int, vp, vp],
+                                  ctypes.c_int),
+        "cap_quantise_fp8": ([ctypes.c_int, i32, i32, i32, i32, vp, vp, vp, vp], ctypes.c_int),
+        "cap_product_fp8": ([ctypes.c_int, i32, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp],
+                            ctypes.c_int),
+        "cap_expert_ffn_fp8": ([i32, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+                               ctypes.c_int),
         "cap_adjustment_spectrum": ([vp, i32, i32, i32, f32, vp, vp, i32, vp, vp, vp, vp, sz, vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
@@ -326,3 +343,48 @@ def cap_muon_update(dtype, batch, rows, cols, g, momentum, mu, nesterov, steps, 
     _check("cap_muon_update", _lib.cap_muon_update(
         dtype, batch, rows, cols, _ptr(g), _ptr(momentum), mu, int(bool(nesterov)), steps, _coefficients(coef, steps),
         eps, _ptr(out), _ptr(ws), nbytes, _stream(stream)))
+
+
+def make_score_options(kind, n_groups=1, topk_groups=1, group_top=1, normalise=True, scale=1.0, bias=None,
+                       token_mask=None) -> ScoreOptions:
+    """bias: fp32 device tensor [E]; token_mask: uint8 or bool device tensor [T] (both kept alive by the caller)."""
+    return ScoreOptions(int(kind), int(n_groups), int(topk_groups), int(group_top), int(bool(normalise)), float(scale),
+                        _ptr(bias), _ptr(token_mask))
+
+
+def cap_route_scores(topo, logits, options: ScoreOptions, p, idx, w, keep, dst_mask, stream=None):
+    _check("cap_route_scores", _lib.cap_route_scores(
+        ctypes.byref(topo), _ptr(logits), ctypes.byref(options), p, _ptr(idx), _ptr(w), _ptr(keep), _ptr(dst_mask),
+        _stream(stream)))
+
+
+def cap_route_scores_grad(T, k, E, logits, idx, keep, w, d_w, options: ScoreOptions, d_add, dtype, d_logits,
+                          stream=None):
+    _check("cap_route_scores_grad", _lib.cap_route_scores_grad(
+        T, k, E, _ptr(logits), _ptr(idx), _ptr(keep), _ptr(w), _ptr(d_w), ctypes.byref(options), _ptr(d_add), dtype,
+        _ptr(d_logits), _stream(stream)))
+
+
+def cap_quantise_fp8(dtype, batch, rows, cols, block_rows, x, q, scale, stream=None):
+    _check("cap_quantise_fp8", _lib.cap_quantise_fp8(
+        dtype, batch, rows, cols, block_rows, _ptr(x), _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def _bytes(ws) -> int:
+    return ws.numel() * ws.element_size() if ws is not None else 0
+
+
+def cap_product_fp8(out_dtype, E_loc, n, kdim, max_rows, x, x_scale, x_rows, row_src, row_offsets, w, w_scale, y, ws,
+                    ws_bytes=None, stream=None):
+    nbytes = ws_bytes if ws_bytes is not None else _bytes(ws)
+    _check("cap_product_fp8", _lib.cap_product_fp8(
+        out_dtype, E_loc, n, kdim, max_rows, _ptr(x), _ptr(x_scale), x_rows, _ptr(row_src), _ptr(row_offsets), _ptr(w),
+        _ptr(w_scale), _ptr(y), _ptr(ws), nbytes, _stream(stream)))
+
+
+def cap_expert_ffn_fp8(E_loc, d, inter, max_rows, x, x_scale, x_rows, row_src, row_offsets, w1, s1, w3, s3, w2, s2, y,
+                       ws, ws_bytes=None, stream=None):
+    nbytes = ws_bytes if ws_bytes is not None else _bytes(ws)
+    _check("cap_expert_ffn_fp8", _lib.cap_expert_ffn_fp8(
+        E_loc, d, inter, max_rows, _ptr(x), _ptr(x_scale), x_rows, _ptr(row_src), _ptr(row_offsets), _ptr(w1), _ptr(s1),
+        _ptr(w3), _ptr(s3), _ptr(w2), _ptr(s2), _ptr(y), _ptr(ws), nbytes, _stream(stream)))

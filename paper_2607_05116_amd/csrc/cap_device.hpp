@@ -14,6 +14,9 @@ constexpr int kMaxE = 256;
 constexpr int kMaxR = 64;
 constexpr int kMaxLossTokens = INT32_MAX - 4095, kMaxLossSequences = 1 << 30;   // of the router's training
 constexpr int kMaxOrthSide = 65536, kMaxOrthBatch = 65535, kMaxOrthSteps = 16;
+constexpr int kMaxScoreGroups = 64;                   // groups of cap_route_scores: one bit each
+constexpr int kF8Block = 128;                         // values that share a scale in 8-bit floating point
+constexpr int kF8MaxK = 1 << 15, kF8MaxStages = kF8MaxK / kF8Block;   // K of the products in 8 bits
 constexpr int kMaxDevices = 64;                       // per-device caches of host code
 constexpr size_t kLayoutScratchBytes = size_t(4) << 20;   // cap_dispatch_layout_static's workspace
 

@@ -46,6 +46,19 @@ cap_status router_grad_launch(int, int, int, const float*, const int32_t*, const
 size_t orthogonalise_workspace_bytes(int, int, int);
 cap_status orthogonalise_launch(cap_dtype, int, int, int, const void*, float*, float, int, int, const float*, float,
                                 void*, void*, hipStream_t);
+cap_status route_scores_launch(const cap_topology*, const float*, const cap_score_options*, float, int32_t*, float*,
+                               uint8_t*, uint64_t*, hipStream_t);
+cap_status route_scores_grad_launch(int, int, int, const float*, const int32_t*, const uint8_t*, const float*,
+                                    const float*, const cap_score_options*, const float*, cap_dtype, void*,
+                                    hipStream_t);
+cap_status quantise_fp8_launch(cap_dtype, int, int, int, int, const void*, void*, float*, hipStream_t);
+size_t product_fp8_workspace_bytes(int, int, int);
+size_t ffn_fp8_workspace_bytes(int, int, int);
+cap_status product_fp8_launch(cap_dtype, int, int, int, int, const void*, const float*, int, const int32_t*,
+                              const int32_t*, const void*, const float*, void*, void*, hipStream_t);
+cap_status expert_ffn_fp8_launch(int, int, int, int, const void*, const float*, int, const int32_t*, const int32_t*,
+                                 const void*, const float*, const void*, const float*, const void*, const float*,
+                                 void*, void*, hipStream_t);
 cap_status coactivation_launch(int, int, int, const int32_t*, const uint8_t*, uint32_t*, int, void*,
                                hipStream_t);
 
@@ -109,6 +122,16 @@ bool orth_shape_ok(int batch, int rows, int cols) {
            cols <= kMaxOrthSide;
 }
 
+// Sizes of the products in 8 bits: whole scale blocks along K, and row offsets (in
+// bytes, within an expert's weights or the rows) of 32 bits.
+bool f8_k_ok(int k) { return k >= kF8Block && k <= kF8MaxK && k % kF8Block == 0; }
+bool f8_product_ok(int n, int k, long long max_rows) {
+    return n >= 1 && f8_k_ok(k) && max_rows >= 0 && static_cast<long long>(n) * k < (1ll << 32);
+}
+bool f8_ffn_ok(int d, int inter, long long max_rows) {
+    return f8_k_ok(d) && f8_k_ok(inter) && max_rows >= 0 && max_rows * inter < (1ll << 32);
+}
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
@@ -153,6 +176,10 @@ size_t cap_workspace_size(cap_op op, const cap_topology* topo, int32_t d, int32_
             return balance_workspace_bytes(topo->T, topo->E, max_rows);
         case CAP_OP_ORTHOGONALISE:
             return orth_shape_ok(max_rows, inter, d) ? orthogonalise_workspace_bytes(max_rows, inter, d) : 0;
+        case CAP_OP_PRODUCT_FP8:
+            return f8_product_ok(d, inter, max_rows) ? product_fp8_workspace_bytes(d, inter, max_rows) : 0;
+        case CAP_OP_EXPERT_FFN_FP8:
+            return f8_ffn_ok(d, inter, max_rows) ? ffn_fp8_workspace_bytes(d, inter, max_rows) : 0;
         case CAP_OP_ADJUSTMENT:
             if (!topo || topo->E < 1 || topo->E > kMaxE) return 0;
             return adjustment_workspace_bytes(topo->E);
@@ -460,6 +487,124 @@ cap_status cap_muon_update(cap_dtype dtype, int32_t batch, int32_t rows, int32_t
     if (!momentum || !aligned4(momentum)) return CAP_ERR_INVALID_ARG;
     return orthogonalise_launch(dtype, batch, rows, cols, g, momentum, mu, nesterov != 0, steps, coef, eps, out, ws,
                                 as_stream(stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+cap_status score_options_check(const cap_score_options* o, int E, int k) {
+    if (!o) return CAP_ERR_INVALID_ARG;
+    if (o->kind != CAP_SCORE_SOFTMAX && o->kind != CAP_SCORE_SIGMOID) return CAP_ERR_UNSUPPORTED;
+    if (!(o->scale > 0.0f) || !(o->scale < INFINITY)) return CAP_ERR_INVALID_ARG;
+    if (o->n_groups < 1 || o->n_groups > kMaxScoreGroups || E % o->n_groups != 0) return CAP_ERR_INVALID_ARG;
+    if (o->topk_groups < 1 || o->topk_groups > o->n_groups || k > o->topk_groups * (E / o->n_groups))
+        return CAP_ERR_INVALID_ARG;
+    if (o->group_top != 1 && o->group_top != 2) return CAP_ERR_INVALID_ARG;
+    return CAP_OK;
+}
+
+// What the products in 8 bits ask of rows, offsets and alignment.
+cap_status f8_rows_check(int32_t E_loc, int32_t k, int32_t max_rows, const void* x, const float* x_scale,
+                         int32_t x_rows, const int32_t* row_src, const int32_t* row_offsets) {
+    if (E_loc < 1 || E_loc > kMaxE || max_rows < 0 || !row_offsets || !aligned4(row_offsets)) return CAP_ERR_INVALID_ARG;
+    if (max_rows == 0) return CAP_OK;
+    if (!x || !x_scale || x_rows < 1 || (!row_src && x_rows < max_rows)) return CAP_ERR_INVALID_ARG;
+    if (!aligned16(x) || !aligned4(x_scale) || !aligned4(row_src)) return CAP_ERR_INVALID_ARG;
+    if (static_cast<long long>(x_rows) * k >= (1ll << 32)) return CAP_ERR_UNSUPPORTED;
+    return CAP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cap_status cap_route_scores(const cap_topology* topo, const float* logits, const cap_score_options* options, float p,
+                            int32_t* idx, float* w, uint8_t* keep, uint64_t* dst_mask, void* stream) {
+    if (!topo_ok(topo) || !logits || !idx || !w || !keep || !dst_mask) return CAP_ERR_INVALID_ARG;
+    if (!(p >= 0.0f) || !(p < 1.0f)) return CAP_ERR_INVALID_ARG;
+    const cap_status st = score_options_check(options, topo->E, topo->k);
+    if (st != CAP_OK) return st;
+    if (!aligned4(logits) || !aligned4(options->bias) || !aligned4(idx) || !aligned4(w) ||
+        (reinterpret_cast<uintptr_t>(dst_mask) & 7) != 0)
+        return CAP_ERR_INVALID_ARG;
+    return route_scores_launch(topo, logits, options, p, idx, w, keep, dst_mask, as_stream(stream));
+}
+
+cap_status cap_route_scores_grad(int32_t T, int32_t k, int32_t E, const float* logits, const int32_t* idx,
+                                 const uint8_t* keep, const float* w, const float* d_w,
+                                 const cap_score_options* options, const float* d_add, cap_dtype dtype,
+                                 void* d_logits, void* stream) {
+    if (!options) return CAP_ERR_INVALID_ARG;
+    if (T < 0 || k < 1 || k > kMaxK || E < k || E > kMaxE || static_cast<long long>(T) * k >= (1ll << 31))
+        return CAP_ERR_INVALID_ARG;
+    if (options->kind != CAP_SCORE_SOFTMAX && options->kind != CAP_SCORE_SIGMOID) return CAP_ERR_UNSUPPORTED;
+    if (dtype != CAP_DTYPE_BF16 && dtype != CAP_DTYPE_F32) return CAP_ERR_UNSUPPORTED;
+    if (!(options->scale > 0.0f) || !(options->scale < INFINITY)) return CAP_ERR_INVALID_ARG;
+    if (T == 0) return CAP_OK;
+    const bool reads_logits = options->kind == CAP_SCORE_SIGMOID || options->normalise == 0;
+    if ((reads_logits && !logits) || !idx || !w || !d_w || !d_logits) return CAP_ERR_INVALID_ARG;
+    if (!aligned4(logits) || !aligned4(idx) || !aligned4(w) || !aligned4(d_w) || !aligned4(d_add) ||
+        (reinterpret_cast<uintptr_t>(d_logits) & (dtype == CAP_DTYPE_BF16 ? 1 : 3)) != 0)
+        return CAP_ERR_INVALID_ARG;
+    return route_scores_grad_launch(T, k, E, logits, idx, keep, w, d_w, options, d_add, dtype, d_logits,
+                                    as_stream(stream));
+}
+
+cap_status cap_quantise_fp8(cap_dtype dtype, int32_t batch, int32_t rows, int32_t cols, int32_t block_rows,
+                            const void* x, void* q, float* scale, void* stream) {
+    if (batch < 0 || rows < 0 || cols < 0 || (block_rows != 1 && block_rows != kF8Block)) return CAP_ERR_INVALID_ARG;
+    if (dtype != CAP_DTYPE_BF16 && dtype != CAP_DTYPE_F32) return CAP_ERR_UNSUPPORTED;
+    if (cols % kF8Block != 0) return CAP_ERR_UNSUPPORTED;
+    if (batch == 0 || rows == 0 || cols == 0) return CAP_OK;
+    if (!x || !q || !scale || !aligned16(x) || (reinterpret_cast<uintptr_t>(q) & 7) != 0 || !aligned4(scale))
+        return CAP_ERR_INVALID_ARG;
+    // batch * rows < 2^62, so these products do not overflow
+    const long long all_rows = static_cast<long long>(batch) * rows;
+    const long long blocks = static_cast<long long>(batch) * ((rows - 1) / kF8Block + 1);
+    if (all_rows > (1ll << 37) / cols || (all_rows == (1ll << 37) / cols && (1ll << 37) % cols == 0) ||
+        (block_rows == kF8Block && blocks >= (1ll << 24) / (cols / kF8Block)))
+        return CAP_ERR_UNSUPPORTED;
+    return quantise_fp8_launch(dtype, batch, rows, cols, block_rows, x, q, scale, as_stream(stream));
+}
+
+cap_status cap_product_fp8(cap_dtype out_dtype, int32_t E_loc, int32_t n, int32_t kdim, int32_t max_rows,
+                           const void* x, const float* x_scale, int32_t x_rows, const int32_t* row_src,
+                           const int32_t* row_offsets, const void* w, const float* w_scale, void* y, void* ws,
+                           size_t ws_bytes, void* stream) {
+    if (n < 1 || kdim < 1) return CAP_ERR_INVALID_ARG;
+    if (out_dtype != CAP_DTYPE_BF16 && out_dtype != CAP_DTYPE_F32) return CAP_ERR_UNSUPPORTED;
+    const cap_status st = f8_rows_check(E_loc, kdim, max_rows, x, x_scale, x_rows, row_src, row_offsets);
+    if (st != CAP_OK) return st;
+    if (!f8_product_ok(n, kdim, max_rows)) return CAP_ERR_UNSUPPORTED;
+    if (max_rows == 0) return CAP_OK;
+    if (!w || !w_scale || !y || !aligned16(w) || !aligned4(w_scale) ||
+        (reinterpret_cast<uintptr_t>(y) & (out_dtype == CAP_DTYPE_BF16 ? 1 : 3)) != 0)
+        return CAP_ERR_INVALID_ARG;
+    const size_t need = product_fp8_workspace_bytes(n, kdim, max_rows);
+    if (need && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 255) != 0)) return CAP_ERR_WORKSPACE;
+    return product_fp8_launch(out_dtype, E_loc, n, kdim, max_rows, x, x_scale, x_rows, row_src, row_offsets, w, w_scale,
+                              y, ws, as_stream(stream));
+}
+
+cap_status cap_expert_ffn_fp8(int32_t E_loc, int32_t d, int32_t inter, int32_t max_rows, const void* x,
+                              const float* x_scale, int32_t x_rows, const int32_t* row_src,
+                              const int32_t* row_offsets, const void* w1, const float* s1, const void* w3,
+                              const float* s3, const void* w2, const float* s2, void* y, void* ws, size_t ws_bytes,
+                              void* stream) {
+    if (d < 1 || inter < 1) return CAP_ERR_INVALID_ARG;
+    const cap_status st = f8_rows_check(E_loc, d, max_rows, x, x_scale, x_rows, row_src, row_offsets);
+    if (st != CAP_OK) return st;
+    if (!f8_ffn_ok(d, inter, max_rows)) return CAP_ERR_UNSUPPORTED;
+    if (max_rows == 0) return CAP_OK;
+    if (!w1 || !s1 || !w3 || !s3 || !w2 || !s2 || !y) return CAP_ERR_INVALID_ARG;
+    if (!aligned16(w1) || !aligned16(w3) || !aligned16(w2) || !aligned16(y) || !aligned4(s1) || !aligned4(s3) ||
+        !aligned4(s2))
+        return CAP_ERR_INVALID_ARG;
+    if (!ws || ws_bytes < ffn_fp8_workspace_bytes(d, inter, max_rows) || (reinterpret_cast<uintptr_t>(ws) & 255) != 0)
+        return CAP_ERR_WORKSPACE;
+    return expert_ffn_fp8_launch(E_loc, d, inter, max_rows, x, x_scale, x_rows, row_src, row_offsets, w1, s1, w3, s3,
+                                 w2, s2, y, ws, as_stream(stream));
 }
 
 }  // extern "C"

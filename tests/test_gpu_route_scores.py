@@ -1,0 +1,238 @@
+"""cap_route_scores and cap_route_scores_grad against the definition in 64 bits (scores_reference)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import scores_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+SIGMOID = dict(kind="sigmoid", normalise=True, scale=2.5)
+PLAIN = dict(kind="softmax", normalise=False)
+COST = 5.0
+
+
+@pytest.fixture(scope="module")
+def capi():
+    from paper_2607_05116_amd import capi as c
+    return c
+
+
+def _dev(a):
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def _options(capi, opt, bias=None, mask=None):
+    kind = capi.CAP_SCORE_SIGMOID if opt["kind"] == "sigmoid" else capi.CAP_SCORE_SOFTMAX
+    rest = {k: v for k, v in opt.items() if k != "kind"}
+    return capi.make_score_options(kind, bias=bias, token_mask=mask, **rest)
+
+
+def _route(capi, logits, k, R, node, p, opt, bias=None, token_mask=None, rank=None, stream=None):
+    T, E = logits.shape
+    rank = np.arange(E, dtype=np.int32) // (E // R) if rank is None else rank
+    local = np.zeros(E, np.int32)
+    for r in range(R):
+        local[rank == r] = np.arange((rank == r).sum())
+    er, el, b, m = _dev(rank), _dev(local), _dev(bias), _dev(token_mask)
+    topo = capi.make_topology(E, R, node, T, k, er, el, COST)
+    out = [torch.full((T + 1, k), -7, dtype=torch.int32, device="cuda"), torch.full((T + 1, k), -7.0, device="cuda"),
+           torch.full((T + 1, k), 77, dtype=torch.uint8, device="cuda"),
+           torch.full((T + 1,), -7, dtype=torch.int64, device="cuda")]
+    capi.cap_route_scores(topo, _dev(logits), _options(capi, opt, b, m), p, *out, stream)
+    torch.cuda.synchronize()
+    assert (out[0][T] == -7).all() and (out[1][T] == -7).all() and (out[2][T] == 77).all() and out[3][T] == -7
+    idx, w, keep, mask = (v[:T].cpu().numpy() for v in out)
+    return idx, w, keep, mask.view(np.uint64), rank
+
+
+def _check(capi, logits, k, R, node, p, opt, bias=None, token_mask=None, rank=None):
+    idx, w, keep, mask, rank = _route(capi, logits, k, R, node, p, opt, bias, token_mask, rank)
+    r_idx, r_w, r_keep, r_mask, close = ref.route(logits, k, rank, R, node, p, COST, bias=bias, token_mask=token_mask, **opt)
+    assert np.array_equal(idx, r_idx)
+    sure = ~close
+    assert np.array_equal(keep[sure], r_keep[sure]) and np.array_equal(mask[sure], r_mask[sure])
+    # one rounding to fp32 (2^-24, of at least the least normal number), and the 64-bit exponentials'
+    assert np.all(np.abs(w - r_w)[sure] <= 2.0 ** -24 * np.abs(r_w[sure]) * (1 + 1e-6) + 2.0 ** -149)
+    return close.mean()
+
+
+CASES = [
+    # E, k, R, tokens a rank, node, p, options
+    (256, 8, 32, 3, 8, 0.1, dict(SIGMOID, n_groups=8, topk_groups=4, group_top=2), True),
+    (256, 8, 1, 1, 1, 0.0, dict(SIGMOID, n_groups=8, topk_groups=4, group_top=2), True),
+    (256, 8, 8, 9, 4, 0.3, dict(SIGMOID, n_groups=8, topk_groups=3, group_top=1), False),
+    (256, 6, 8, 9, 8, 0.1, dict(SIGMOID, n_groups=2, topk_groups=1, group_top=2), True),
+    (256, 3, 4, 17, 4, 0.2, dict(PLAIN, n_groups=4, topk_groups=1, group_top=1), False),
+    (256, 2, 4, 17, 4, 0.2, dict(PLAIN, n_groups=16, topk_groups=5, group_top=2), True),
+    (128, 8, 8, 13, 8, 0.1, dict(kind="softmax", normalise=True), False),
+    (128, 4, 8, 13, 8, 0.1, dict(SIGMOID, n_groups=4, topk_groups=2, group_top=2), True),
+    (128, 5, 8, 13, 8, 0.1, dict(SIGMOID, n_groups=32, topk_groups=3, group_top=2), False),
+    (64, 6, 8, 40, 8, 0.0, PLAIN, False),
+    (64, 8, 64, 2, 8, 0.3, dict(SIGMOID, n_groups=2, topk_groups=1, group_top=1), True),
+    (64, 1, 8, 5, 4, 0.5, dict(SIGMOID, n_groups=64, topk_groups=1, group_top=2), True),
+    (96, 8, 4, 11, 2, 0.1, dict(SIGMOID, n_groups=12, topk_groups=2, group_top=2), True),
+    (40, 7, 8, 7, 4, 0.1, dict(kind="softmax", normalise=True, scale=0.5, n_groups=8, topk_groups=2), True),
+    (24, 3, 3, 21, 3, 0.4, dict(SIGMOID, n_groups=3, topk_groups=2, group_top=2), False),
+    (16, 2, 4, 64, 4, 0.1, SIGMOID, True),
+    (7, 7, 7, 9, 7, 0.1, dict(kind="softmax", normalise=False, scale=3.0), True),
+    (2, 2, 1, 30, 1, 0.1, dict(SIGMOID, n_groups=2, topk_groups=2, group_top=2), True),
+    (1, 1, 1, 5, 1, 0.1, SIGMOID, False),
+    (255, 8, 5, 13, 5, 0.1, dict(SIGMOID, n_groups=5, topk_groups=2, group_top=2), True),
+]
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_route(capi, case):
+    E, k, R, each, node, p, opt, biased = CASES[case]
+    rng = np.random.default_rng(case)
+    logits = (2.0 * rng.standard_normal((R * each, E))).astype(np.float32)
+    bias = (0.3 * rng.standard_normal(E)).astype(np.float32) if biased else None
+    assert _check(capi, logits, k, R, node, p, opt, bias) < 0.05
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_experts_off_and_tokens_masked(capi, case):
+    """Rows with -inf and NaN logits, rows with nothing on, masked rows that hold anything, a scattered placement."""
+    E, k, R, each, node, p, opt, biased = CASES[case]
+    rng = np.random.default_rng(100 + case)
+    T = R * each
+    logits = (2.0 * rng.standard_normal((T, E))).astype(np.float32)
+    logits[rng.random((T, E)) < 0.5] = -math.inf
+    logits[rng.random((T, E)) < 0.05] = math.nan
+    logits[rng.random(T) < 0.2] = -math.inf
+    token_mask = (rng.random(T) < 0.8).astype(np.uint8)
+    logits[token_mask == 0] = rng.choice(np.array([math.nan, math.inf, -math.inf, 3e38], np.float32), (int((token_mask == 0).sum()), E))
+    bias = (0.3 * rng.standard_normal(E)).astype(np.float32) if biased else None
+    rank = rng.permutation(np.arange(E, dtype=np.int32) // (E // R)).astype(np.int32)
+    # one expert on, or devices of equal share: closeness is common here, so only most tokens need be decided
+    _check(capi, logits, k, R, node, p, opt, bias, token_mask, rank)
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_ties_go_to_the_lower_index(capi, case):
+    """Logits from a few values: experts, and groups, of equal scores."""
+    E, k, R, each, node, p, opt, biased = CASES[case]
+    rng = np.random.default_rng(200 + case)
+    logits = rng.choice(np.array([-1.0, -0.0, 0.0, 0.5, 2.0], np.float32), (R * each, E))
+    bias = np.full(E, 0.125, np.float32) if biased else None
+    _check(capi, logits, k, R, node, 0.0, opt, bias)
+
+
+@pytest.mark.parametrize("opt", [dict(SIGMOID, n_groups=8, topk_groups=4, group_top=2), PLAIN, dict(kind="softmax", normalise=True)])
+def test_extreme_logits(capi, opt):
+    """Logits whose scores underflow or saturate, far beyond what fp32 scores tell apart."""
+    rng = np.random.default_rng(5)
+    logits = np.concatenate([rng.uniform(-40, -20, (16, 64)), rng.uniform(-300, 300, (16, 64)), rng.uniform(-3e38, -1e4, (16, 64)),
+                             rng.uniform(-1e-30, 1e-30, (16, 64))]).astype(np.float32)
+    if opt["kind"] == "sigmoid":
+        logits = np.minimum(logits, 30)            # above, different logits have one score in 64 bits
+        logits[32:48] = rng.uniform(-690, -600, (16, 64))
+    _check(capi, logits, 8, 8, 8, 0.1, opt)
+
+
+def test_scores_below_64_bits(capi):
+    """No score is left: gates are 0, the slots stay (nothing tells the devices apart)."""
+    logits = np.full((8, 32), -1e30, np.float32)
+    idx, w, keep, mask, _ = _route(capi, logits, 4, 8, 8, 0.1, SIGMOID)
+    assert np.array_equal(idx, np.tile(np.arange(4), (8, 1))) and (w == 0).all() and keep.all() and (mask == 1).all()
+
+
+def test_same_as_route_prune(capi):
+    """With its scores and no groups, the choice of cap_route_prune, and its gates to fp32 rounding."""
+    rng = np.random.default_rng(6)
+    T, E, k, R = 512, 128, 8, 8
+    logits = rng.standard_normal((T, E)).astype(np.float32)
+    idx, w, keep, mask, rank = _route(capi, logits, k, R, 4, 0.1, dict(kind="softmax", normalise=True))
+    er, el = _dev(rank), _dev(np.arange(E, dtype=np.int32) % (E // R))
+    topo = capi.make_topology(E, R, 4, T, k, er, el, COST)
+    i2, w2 = torch.empty((T, k), dtype=torch.int32, device="cuda"), torch.empty((T, k), device="cuda")
+    k2, m2 = torch.empty((T, k), dtype=torch.uint8, device="cuda"), torch.empty(T, dtype=torch.int64, device="cuda")
+    capi.cap_route_prune(topo, _dev(logits), 0.1, i2, w2, k2, m2)
+    assert np.array_equal(idx, i2.cpu().numpy())
+    same = (keep == k2.cpu().numpy()).all(1)       # its shares are fp32: at a border it may keep one device more or less
+    assert same.mean() > 0.99
+    # its fp32 exponentials are within 2 ulp, its sums of eight within 8, its two divisions within 1
+    assert np.all(np.abs(w - w2.cpu().numpy())[same] <= 12 * 2.0 ** -23 * w[same])
+
+
+def test_other_stream(capi):
+    rng = np.random.default_rng(7)
+    logits = rng.standard_normal((64, 256)).astype(np.float32)
+    opt = dict(SIGMOID, n_groups=8, topk_groups=4, group_top=2)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        a = _route(capi, logits, 8, 32, 8, 0.1, opt)
+    b = _route(capi, logits, 8, 32, 8, 0.1, opt)
+    assert all(np.array_equal(x, y) for x, y in zip(a, b))
+
+
+# ------------------------------------------------------------------ gradient
+def _grad(capi, logits, idx, keep, w, d_w, opt, d_add, bf16):
+    T, E = logits.shape
+    out = torch.full((T + 1, E), 9.0, device="cuda", dtype=torch.bfloat16 if bf16 else torch.float32)
+    dt = capi.CAP_DTYPE_BF16 if bf16 else capi.CAP_DTYPE_F32
+    capi.cap_route_scores_grad(T, idx.shape[1], E, _dev(logits), _dev(idx), _dev(keep), _dev(w), _dev(d_w),
+                               _options(capi, opt), _dev(d_add), dt, out)
+    torch.cuda.synchronize()
+    assert (out[T] == 9.0).all()
+    return out[:T].float().cpu().numpy()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("opt", [SIGMOID, dict(kind="sigmoid", normalise=False, scale=2.5), dict(kind="softmax", normalise=True, scale=0.5),
+                                 PLAIN, dict(kind="softmax", normalise=False, scale=2.5)])
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (3, 7, 3), (130, 16, 2), (33, 33, 8), (70, 64, 6), (5, 100, 4), (66, 256, 8)])
+def test_grad(capi, T, E, k, opt, add, bf16):
+    rng = np.random.default_rng(T + E + k)
+    logits = (2.0 * rng.standard_normal((T, E))).astype(np.float32)
+    logits[rng.random((T, E)) < 0.1] = -math.inf
+    idx = np.stack([rng.permutation(E)[:k] for _ in range(T)]).astype(np.int32)
+    on = np.take_along_axis(logits, idx, 1) > -math.inf
+    keep = (on & (rng.random((T, k)) < 0.8)).astype(np.uint8)
+    keep[rng.random(T) < 0.1] = 0
+    w64 = ref.gates(logits.astype(np.float64), idx, keep, opt["kind"], opt["normalise"], opt.get("scale", 1.0))
+    w = w64.astype(np.float32)
+    d_w = rng.standard_normal((T, k)).astype(np.float32)
+    hidden = d_w.copy()
+    hidden[keep == 0] = math.nan                   # not read
+    d_add = rng.standard_normal((T, E)).astype(np.float32) if add else None
+    got = _grad(capi, logits, idx, keep, w, hidden, opt, d_add, bf16)
+    want = ref.grad(logits.astype(np.float64), idx, keep, d_w.astype(np.float64), opt["kind"], opt["normalise"], opt.get("scale", 1.0))
+    if add:
+        want = want + d_add
+    # fp32 arithmetic: w's rounding, a product, up to 8 additions of the sum, two more products, a difference, and 1 - s
+    # or the softmax's 2 log2(E) + 6 roundings, each of 2^-24 of the terms' magnitudes
+    terms = np.abs(w64 * d_w * keep)
+    size = np.zeros((T, E))
+    np.put_along_axis(size, idx, terms + np.abs(w64) / opt.get("scale", 1.0) * terms.sum(1, keepdims=True), 1)
+    if opt["kind"] == "softmax" and not opt["normalise"]:
+        size += terms.sum(1, keepdims=True)
+    bound = 32 * 2.0 ** -24 * size + 2.0 ** -24 * np.abs(want) + (2.0 ** -8 * np.abs(want) if bf16 else 0.0) + 1e-37
+    # the reference's own rounding: where the softmax is normalised its quotient rule subtracts a sum over the slots that is
+    # 0, of at most eight terms s ds that add up to at most 2 sum |w d_w| in size: 8 2^-53 of that, times s <= 1
+    bound = bound + 2.0 ** -49 * terms.sum(1, keepdims=True)
+    if add:
+        bound = bound + 2.0 ** -24 * np.abs(d_add)
+    assert np.all(np.abs(got - want) <= bound)
+
+
+def test_grad_of_masked_rows_and_bad_indices(capi):
+    """Rows with no kept slot give zeros whatever they hold; an index outside the experts is skipped."""
+    T, E, k = 9, 48, 4
+    logits = np.full((T, E), math.nan, np.float32)
+    idx = np.tile(np.arange(k, dtype=np.int32), (T, 1))
+    keep, nan = np.zeros((T, k), np.uint8), np.full((T, k), math.nan, np.float32)
+    for opt in (SIGMOID, PLAIN):
+        assert (_grad(capi, logits, idx, keep, nan, nan, opt, None, False) == 0).all()
+    logits = np.zeros((T, E), np.float32)
+    idx[:, 1], idx[:, 2] = -1, E
+    ones = np.ones((T, k), np.float32)
+    got = _grad(capi, logits, idx, np.ones((T, k), np.uint8), ones, ones, dict(SIGMOID, normalise=False), None, False)
+    want = np.zeros((T, E), np.float32)
+    want[:, [0, 3]] = 0.5
+    assert np.array_equal(got, want)
