@@ -148,6 +148,12 @@ __device__ __forceinline__ bool find_tile(const F8Args& a, int NT, Tile& out) {
     return false;
 }
 
+// Barrier that publishes LDS writes and leaves direct loads under way.
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    block_barrier();
+}
+
 // A tile's way out: y, or H with its scales.  `lds` (the stages) is free but for reads
 // of the last stage that other waves may still make.
 template <int BM, int BN, int NWM, int NWN, typename OUT>
@@ -155,7 +161,7 @@ __device__ __forceinline__ void finish_tile(const F8Args& a, const Tile& tile, i
                                             f32x4 (&acc)[BM / NWM / 16][BN / NWN / 16], uint8_t* lds) {
     constexpr bool kSwiglu = std::is_same<OUT, uint8_t>::value;
     constexpr int NW = NWM * NWN, WM = BM / NWM, WN = BN / NWN, MI = WM / 16, NJ = WN / 16;
-    const int NB = (a.N + 127) / 128, fr_row = lane & 15;
+    const int fr_row = lane & 15;
     const int q4 = (lane >> 4) * 4;                    // the lane's four outputs within a block of 16
     if constexpr (!kSwiglu) {
         OUT* const out = static_cast<OUT*>(a.out);
@@ -190,7 +196,7 @@ __device__ __forceinline__ void finish_tile(const F8Args& a, const Tile& tile, i
         float* const row_max = reinterpret_cast<float*>(lds);                    // [NWN][BM]
         uint8_t* const codes = lds + NWN * BM * 4;                               // [BM][kPitch]
         constexpr int kPitch = 128 + 16;
-        static_assert(NWN * BM * 4 + BM * kPitch <= 2 * (BM + BN) * 128, "epilogue in the stages");
+        static_assert(NWN * BM * 4 + BM * kPitch <= (BM + BN) * 128, "epilogue in one stage");
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -200,8 +206,7 @@ __device__ __forceinline__ void finish_tile(const F8Args& a, const Tile& tile, i
                     const float g = acc[i][j][v];
                     acc[i][j][v] = g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * acc[i][j + NJ / 2][v];
                 }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        block_barrier();                               // the last stage is read
+        lds_barrier();                                 // the last stage is read
         uint32_t m[MI];
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
@@ -220,7 +225,7 @@ __device__ __forceinline__ void finish_tile(const F8Args& a, const Tile& tile, i
             }
             if (lane < 16) row_max[wn * BM + wm * WM + 16 * i + lane] = __uint_as_float(m[i]);
         }
-        __syncthreads();
+        lds_barrier();
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int r = wm * WM + 16 * i + fr_row;
@@ -241,7 +246,7 @@ __device__ __forceinline__ void finish_tile(const F8Args& a, const Tile& tile, i
             if (wn == 0 && lane < 16 && tile.m0 + r < tile.end)
                 a.out_scale[tile.nt * a.scale_pitch + tile.m0 + r] = f8_scale(ex);
         }
-        __syncthreads();
+        lds_barrier();
         uint8_t* const out = static_cast<uint8_t*>(a.out);
         for (int c = threadIdx.x; c < BM * 8; c += 64 * NW) {
             const int r = c >> 3;
@@ -379,165 +384,188 @@ __global__ __launch_bounds__(64 * NWM * NWN) void f8_tile_kernel(const F8Args a)
 }
 
 // ------------------------------------------------------------------ wide tiles
-// 256 x 256 in the four quarters a stage of mfma_tile.hpp's K loop (its barriers, loads
-// and fragment reads, with 128 8-bit values in a stage row instead of 64 of 16 bits: a
-// quarter is 4 x 2 MFMAs of K = 128).  What differs: a group of two MFMAs (A block g,
-// both B blocks) leaves its sums in one of two register sets, and the FMAs that scale
-// and add those of the one before run meanwhile.  Activation scales come with a stage's
-// B quarters 0, 1, from [KT][rows] in the rows' order: 256 bytes a wave (read in place,
-// [rows][KT], they are 256 cache lines a stage, half as many as its operands: 5 to 9 % of
-// the time); the weights' are in LDS for the tile.
-// KT may be odd: the stages sit in buffers so that the last is in buffer 1.
-struct WideScales {
-    const char* src;             // of the wave's 64 rows, at the stage to be loaded next
-    size_t step;                 // bytes from stage to stage
-    uint32_t off, dst;           // the lane's four bytes; LDS of the wave's rows
-    const float* sx;             // LDS: [2][256], at the wave's rows and the lane's row of 16
-    const float* sw;             // LDS: scales of the wave's weights; SwiGLU: W1's, W3's KT further
-};
+// 256 x 256, eight waves of 64 x 128, in the four quarters a stage of mfma_tile.hpp's K
+// loop (its barriers a and c, LDS layout and fragment reads, with 128 8-bit values in a
+// stage row instead of 64 of 16 bits: a quarter is 4 x 2 MFMAs of K = 128).  What differs:
+//   - The FMAs that scale and add an MFMA's sums follow two MFMAs later, so that they never
+//     wait for it (right after the next one they did, for 28 cycles of every 64).
+//   - All waves load: each 32 rows of A and 8 of each quarter of B a stage.
+//   - Activation scales come with a stage's B quarters 0, 1, from [KT][rows] in the rows'
+//     order: 256 bytes a wave (read in place, [rows][KT], they are 256 cache lines a stage,
+//     half as many as its operands: 5 to 9 % of the time); the weights' are in LDS.
+//   - KT may be odd: stage kt sits in buffer (kt + KT) % 2, so the last is in buffer 1.
+constexpr int kALdF8 = kBM / kRowsPerLoad / kNW;       // direct loads of A per wave and stage
+static_assert(kALdF8 == 4 && kNW == 8, "32 rows of A, 8 of each B quarter");
 
-template <bool SWIGLU, bool LOADER, bool ACTIVE>
-__device__ __forceinline__ void f8_k_loop(int KT, const uint8_t* lds, int wm, int wn, int lane, f32x4 (&acc)[kMI][kNJ],
-                                          Loads& ld, WideScales& sc, uint32_t a_lds, uint32_t b_lds) {
-    constexpr bool LOAD_A = LOADER && ACTIVE;
-    constexpr int kA = LOAD_A ? kALd : 0, kS = LOAD_A ? 1 : 0;      // loads of A and of scales a stage
+struct WideLoads {
+    const char *a, *b[4], *s;    // at the stage to be loaded next (b: one for each quarter)
+    size_t s_step;               // bytes of the scales from stage to stage
+    uint32_t a_off[kALdF8], b_off, s_off;      // the lane's
+    uint32_t a_lds, b_lds, s_lds;              // in buffer 0
+};
+// Direct loads and waits of a stage that may lie past the last (left: stages from it to the
+// last, < 1 past it): left out by a branch
+// inside the statement, so that the loop's body stays one block for the compiler (with
+// branches of its own it spilled hundreds of registers; a copy of the body for the last
+// stages cost more in the instruction cache).
+__device__ __forceinline__ void lds_dma16_if(int left, const void* base, uint32_t off, uint32_t lds_addr) {
+    uint64_t b;
+    asm volatile("s_cmp_lt_i32 %4, 1\n\ts_cbranch_scc1 .Lskip%=\n\ts_mov_b64 %0, %2\n\t"
+                 "global_load_lds_dwordx4 %1, %0\n.Lskip%=:"
+                 : "=&s"(b)
+                 : "v"(off), "s"(uniform_ptr(base)), "{m0}"(__builtin_amdgcn_readfirstlane(lds_addr)), "s"(__builtin_amdgcn_readfirstlane(left))
+                 : "memory", "scc");
+}
+__device__ __forceinline__ void lds_dma4_if(int left, const void* base, uint32_t off, uint32_t lds_addr) {
+    uint64_t b;
+    asm volatile("s_cmp_lt_i32 %4, 1\n\ts_cbranch_scc1 .Lskip%=\n\ts_mov_b64 %0, %2\n\t"
+                 "global_load_lds_dword %1, %0\n.Lskip%=:"
+                 : "=&s"(b)
+                 : "v"(off), "s"(uniform_ptr(base)), "{m0}"(__builtin_amdgcn_readfirstlane(lds_addr)), "s"(__builtin_amdgcn_readfirstlane(left))
+                 : "memory", "scc");
+}
+// At most N loads under way if the stage is there, else at most M < N.
+template <int N, int M>
+__device__ __forceinline__ void wait_vm_if(int left) {
+    asm volatile("s_cmp_gt_i32 %0, 0\n\ts_cbranch_scc1 .Lmore%=\n\ts_waitcnt vmcnt(%2)\n.Lmore%=:\n\ts_waitcnt vmcnt(%1)"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane(left)), "n"(N), "n"(M)
+                 : "memory", "scc");
+}
+template <int I>
+__device__ __forceinline__ void wide_a(const WideLoads& l, int left, uint32_t buf) {
+    lds_dma16_if(left, l.a, l.a_off[I], l.a_lds + buf * kStageBytes + I * 1024);
+}
+template <int Q>
+__device__ __forceinline__ void wide_b(WideLoads& l, int left, uint32_t buf) {
+    lds_dma16_if(left, l.b[Q], l.b_off, l.b_lds + buf * kStageBytes + Q * 32 * kRowB);
+    l.b[Q] += kRowB;
+}
+__device__ __forceinline__ void wide_s(WideLoads& l, int left, uint32_t buf) {
+    lds_dma4_if(left, l.s, l.s_off, l.s_lds + buf * kBM * 4);
+    l.s += l.s_step;
+}
+
+// sx: LDS [2][256], at the wave's rows and the lane's row of 16; sw: LDS, the scales of the
+// wave's weights (SwiGLU: W1's, W3's KT further).  The caller has issued stage 0, whole.
+template <bool SWIGLU, bool ACTIVE>
+__device__ __forceinline__ void f8_k_loop(int KT, const uint8_t* lds, const float* sx, const float* sw, int wm, int wn,
+                                          int lane, f32x4 (&acc)[kMI][kNJ], WideLoads& ld) {
     i32x8 a[kMI], b0[2], b1[2];
-    f32x4 d[2] = {};
-    float s[kMI], pf = 0.0f;
+    f32x4 d[4] = {};
+    float s[kMI] = {}, fac[4] = {};
+    uint32_t buf = KT & 1;                             // of stage kt
     const LaneMap lm = lane_map(opaque(lane));
-    const int pc0 = (lm.fr_kc ^ lm.fr_swz) << 4, pc1 = pc0 ^ 64;
-    const uint8_t* const la = lds + (wm * kWM + lm.fr_row) * kRowB;
-    const uint8_t* const lb = lds + (kBM + wn * kWN + lm.fr_row) * kRowB;
-    auto read_a = [&](int buf, auto In) {
+    const int pc0 = (lm.fr_kc ^ lm.fr_swz) << 4;
+    // LDS offsets of the wave's fragments in the buffer that is read (chunks pc0, pc0 ^ 64)
+    uint32_t la0 = (wm * kWM + lm.fr_row) * kRowB + pc0 + buf * kStageBytes, la1 = la0 ^ 64;
+    uint32_t lb0 = (kBM + wn * kWN + lm.fr_row) * kRowB + pc0 + buf * kStageBytes, lb1 = lb0 ^ 64;
+    auto read_a = [&](auto In) {
         constexpr int i = decltype(In)::value;
-        const uint8_t* p = la + buf * kStageBytes + i * 16 * kRowB;
-        a[i] = frag8(p + pc0, p + pc1);
+        a[i] = frag8(lds + la0 + i * 16 * kRowB, lds + la1 + i * 16 * kRowB);
     };
-    auto read_b = [&](i32x8 (&b)[2], int buf, int q, auto Jn) {
-        constexpr int j = decltype(Jn)::value;
-        const uint8_t* p = lb + buf * kStageBytes + (2 * q + j) * 16 * kRowB;
-        b[j] = frag8(p + pc0, p + pc1);
+    auto read_b = [&](i32x8 (&b)[2], auto Qn, auto Jn) {
+        constexpr int at = (2 * decltype(Qn)::value + decltype(Jn)::value) * 16 * kRowB;
+        b[decltype(Jn)::value] = frag8(lds + lb0 + at, lds + lb1 + at);
     };
-    auto read_s = [&](int buf, int kt, bool up) {
-        const float w = sc.sw[up ? KT + kt : kt];
+    auto read_s = [&](int kt, bool up) {
+        const float w = sw[up ? KT + kt : kt];
 #pragma unroll
-        for (int i = 0; i < kMI; ++i) s[i] = sc.sx[buf * kBM + 16 * i] * w;
+        for (int i = 0; i < kMI; ++i) s[i] = sx[buf * kBM + 16 * i] * w;
     };
-    // group g of quarter q; the sums of the MFMA before each are scaled and added while it runs
+    // MFMA m = 8 q + 2 g + jj of the stage (A block g, B block 2 q + jj), then the scaling of
+    // MFMA m - 2 (of the stage before for m = 0, 1)
+    auto add = [&](auto Mn) {
+        constexpr int m = decltype(Mn)::value, i = (m >> 1) & 3, j = 2 * (m >> 3) + (m & 1);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(d[m & 3][v], fac[m & 3], acc[i][j][v]);
+    };
     auto group = [&](i32x8 (&b)[2], auto Qn, auto Gn) {
         constexpr int q = decltype(Qn)::value, g = decltype(Gn)::value;
-        constexpr int pg = g ? g - 1 : 3, pq = g ? q : (q + 3) % 4;
-        d[0] = block_sum<false>(b[0], a[g]);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) acc[pg][2 * pq + 1][v] = __builtin_fmaf(d[1][v], pf, acc[pg][2 * pq + 1][v]);
-        __builtin_amdgcn_sched_barrier(0);
-        d[1] = block_sum<false>(b[1], a[g]);
-        __builtin_amdgcn_sched_barrier(0);
-        pf = s[g];
-#pragma unroll
-        for (int v = 0; v < 4; ++v) acc[g][2 * q][v] = __builtin_fmaf(d[0][v], pf, acc[g][2 * q][v]);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    auto load_s = [&](int buf) {
-        if constexpr (LOAD_A) {
-            lds_dma4(sc.src, sc.off, sc.dst + buf * kBM * 4);
-            sc.src += sc.step;
-        }
+        static_for<2>([&](auto J) {
+            constexpr int m = 8 * q + 2 * g + J.value;
+            d[m & 3] = block_sum<false>(b[J.value], a[g]);
+            fac[m & 3] = s[g];
+            __builtin_amdgcn_sched_barrier(0);
+            add(std::integral_constant<int, (m + 30) % 32>{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
     };
     auto N0 = std::integral_constant<int, 0>{};
     auto N1 = std::integral_constant<int, 1>{};
     auto N2 = std::integral_constant<int, 2>{};
     auto N3 = std::integral_constant<int, 3>{};
-    const int first = KT & 1;
-    load_s(first);
-    if constexpr (LOADER) {
-        load_half0(ld, LOAD_A, a_lds, b_lds, first);
-        load_half1(ld, b_lds, first);
-        wait_vm<0>();
-    }
-    block_barrier();                                   // the first stage is visible
-    if constexpr (LOADER) {
-        if (KT > 1) {
-            load_s(first ^ 1);
-            load_half0(ld, LOAD_A, a_lds, b_lds, first ^ 1);
-        }
+    wait_vm<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    block_barrier();                                   // stage 0 and the weights' scales are visible; the other buffer is free
+    {
+        const int more = KT - 1;
+        static_for<kALdF8>([&](auto I) { wide_a<I.value>(ld, more, buf ^ 1); });
+        ld.a += kRowB;
+        wide_s(ld, more, buf ^ 1);
+        wide_b<0>(ld, more, buf ^ 1);
+        wide_b<1>(ld, more, buf ^ 1);
     }
     if constexpr (ACTIVE) {
-        static_for<2>([&](auto N) { read_b(b0, first, 0, N); });
-        static_for<2>([&](auto N) { read_a(first, N); });
+        static_for<2>([&](auto N) { read_b(b0, N0, N); });
+        static_for<2>([&](auto N) { read_a(N); });
     }
-    int kt = 0;
-    auto stage = [&](auto BUF, auto STEP) {
-        constexpr int buf = decltype(BUF)::value;
-        constexpr KStep step = decltype(STEP)::value;
-        constexpr bool next1 = step != kLast, next2 = next1 && step != kLast2;   // stages kt + 1, kt + 2 exist
-        if constexpr (ACTIVE) read_s(buf, kt, false);
+    for (int kt = 0; kt < KT; ++kt) {
+        const int next1 = KT - kt - 1, next2 = next1 - 1;      // stages from kt + 1, kt + 2 on
+        if constexpr (ACTIVE) read_s(kt, false);
         static_for<4>([&](auto G) {                                            // quarter 0
             if constexpr (ACTIVE) {
-                if constexpr (G.value < 2) read_a(buf, std::integral_constant<int, 2 + G.value>{});
-                else read_b(b1, buf, 1, std::integral_constant<int, G.value - 2>{});
+                if constexpr (G.value < 2) read_a(std::integral_constant<int, 2 + G.value>{});
+                else read_b(b1, N1, std::integral_constant<int, G.value - 2>{});
                 group(b0, N0, G);
             }
-            if constexpr (LOADER && next1) load_b<1, G.value>(ld, b_lds, buf ^ 1);
+            if constexpr (G.value < 2) wide_b<2 + G.value>(ld, next1, buf ^ 1);
             __builtin_amdgcn_sched_barrier(0);
         });
-        if constexpr (LOADER && next1) step_half1(ld);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // A, quarters 0 and 1 read
-        if constexpr (LOADER) wait_vm<next1 ? kA + kS + 8 : 0>();   // quarters 2, 3 of stage kt landed
+        wait_vm_if<kALdF8 + 5, 0>(next1);                        // quarters 2, 3 of stage kt landed
         block_barrier();                                         // barrier a
         static_for<4>([&](auto G) {                                            // quarter 1
             if constexpr (ACTIVE) {
-                if constexpr (G.value < 2) read_b(b0, buf, 2, G);
+                if constexpr (G.value < 2) read_b(b0, N2, G);
                 group(b1, N1, G);
             }
-            if constexpr (LOAD_A && next2) load_a<G.value>(ld, a_lds, buf);
+            if constexpr (G.value % 2 == 1) wide_a<G.value / 2>(ld, next2, buf);
             __builtin_amdgcn_sched_barrier(0);
         });
-        if constexpr (ACTIVE && SWIGLU) read_s(buf, kt, true);
+        if constexpr (ACTIVE && SWIGLU) read_s(kt, true);
         static_for<4>([&](auto G) {                                            // quarter 2
             if constexpr (ACTIVE) {
-                if constexpr (G.value < 2) read_b(b1, buf, 3, G);
+                if constexpr (G.value < 2) read_b(b1, N3, G);
                 group(b0, N2, G);
             }
-            if constexpr (LOAD_A && next2) load_a<4 + G.value>(ld, a_lds, buf);
+            if constexpr (G.value % 2 == 1) wide_a<2 + G.value / 2>(ld, next2, buf);
             __builtin_amdgcn_sched_barrier(0);
         });
+        ld.a += kRowB;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // quarters 2, 3 and the scales read
-        if constexpr (LOADER && next1) wait_vm<next2 ? kA + 4 : 4>();   // A, quarters 0, 1, scales of stage kt + 1 landed
+        wait_vm_if<kALdF8 + 2, 2>(next2);                        // A, quarters 0, 1, scales of stage kt + 1 landed
         block_barrier();                                         // barrier c
+        la0 ^= kStageBytes;
+        la1 ^= kStageBytes;
+        lb0 ^= kStageBytes;
+        lb1 ^= kStageBytes;
         static_for<4>([&](auto G) {                                            // quarter 3
             if constexpr (ACTIVE) {
-                if constexpr (next1) {
-                    if constexpr (G.value < 2) read_b(b0, buf ^ 1, 0, G);
-                    else read_a(buf ^ 1, std::integral_constant<int, G.value - 2>{});
-                }
+                // (after the last stage what is read here is not used)
+                if constexpr (G.value < 2) read_b(b0, N0, G);
+                else read_a(std::integral_constant<int, G.value - 2>{});
                 group(b1, N3, G);
             }
-            if constexpr (LOADER && next2) load_b<0, G.value>(ld, b_lds, buf);
+            if constexpr (G.value == 0) wide_s(ld, next2, buf);
+            else if constexpr (G.value < 3) wide_b<G.value - 1>(ld, next2, buf);
             __builtin_amdgcn_sched_barrier(0);
         });
-        if constexpr (LOADER && next2) {
-            load_s(buf);
-            step_half0(ld);
-        }
-        ++kt;
-    };
-    auto M = std::integral_constant<KStep, kMiddle>{};
-    if (KT == 1) {
-        stage(N1, std::integral_constant<KStep, kLast>{});
-    } else {
-        if (first) stage(N1, M);
-        while (kt + 2 < KT) {
-            stage(N0, M);
-            stage(N1, M);
-        }
-        stage(N0, std::integral_constant<KStep, kLast2>{});
-        stage(N1, std::integral_constant<KStep, kLast>{});
+        buf ^= 1;
     }
     if constexpr (ACTIVE) {
-#pragma unroll
-        for (int v = 0; v < 4; ++v) acc[3][7][v] = __builtin_fmaf(d[1][v], pf, acc[3][7][v]);
+        add(std::integral_constant<int, 30>{});
+        add(std::integral_constant<int, 31>{});
     }
 }
 
@@ -574,93 +602,152 @@ __device__ __forceinline__ void store_wide(const F8Args& a, const Tile& tile, in
     }
 }
 
-// N % 16 == 0: a loader's 16 weight rows of a quarter are all there or all past the end
-// (then those of the last 16 outputs are loaded, and nothing of them stored).
+// Tiles of the wide kernel: experts' row tiles and rows, once a workgroup.
+struct WideTable {
+    int upto[kMaxE];             // row tiles of the experts up to and with e
+    int start[kMaxE], end[kMaxE];
+};
+__device__ __forceinline__ int fill_table(const F8Args& a, WideTable& t, int lane, bool writes) {
+    int before = 0;
+    for (int c = 0; c < a.E_loc; c += 64) {
+        int lo = 0, n = 0;
+        if (c + lane < a.E_loc) expert_rows(a, c + lane, lo, n);
+        int upto = (n + kBM - 1) / kBM;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int o = __shfl_up(upto, d);
+            upto += lane >= d ? o : 0;
+        }
+        if (writes && c + lane < a.E_loc) {
+            t.upto[c + lane] = before + upto;
+            t.start[c + lane] = lo;
+            t.end[c + lane] = lo + n;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return before;
+}
+// Tile `id`: groups of four row tiles of an expert go through all column tiles together
+// (the workgroups of an XCD then meet on their operands in its L2).
+__device__ __forceinline__ Tile tile_at(const WideTable& t, int E_loc, int NT, int id, int lane) {
+    int e = 0;
+    for (int c = 0; c < E_loc; c += 64)
+        e += __popcll(__ballot(c + lane < E_loc && t.upto[c + lane < E_loc ? c + lane : 0] * NT <= id));
+    const int first = e ? __builtin_amdgcn_readfirstlane(t.upto[e - 1]) : 0;
+    const int mt = __builtin_amdgcn_readfirstlane(t.upto[e]) - first;
+    const int start = __builtin_amdgcn_readfirstlane(t.start[e]);
+    const int local = id - first * NT;
+    const int g = local / (4 * NT);
+    const int gm = mt - 4 * g < 4 ? mt - 4 * g : 4;
+    const int r = local - g * 4 * NT;
+    Tile out;
+    out.e = e;
+    out.nt = r / gm;
+    out.m0 = start + (4 * g + r % gm) * kBM;
+    out.end = __builtin_amdgcn_readfirstlane(t.end[e]);
+    return out;
+}
+
+// N % 8 == 0: the 8 weight rows of a load are all there or all past the end (then those of
+// the last 8 outputs are loaded, and nothing of them stored).  A workgroup goes through
+// the tiles of its XCD's run; the next tile's first stage and weight scales are on their
+// way while a tile's results go out through the other buffer.
 template <typename OUT>
 __global__ __launch_bounds__(512) void f8_wide_kernel(const F8Args a) {
     constexpr bool kSwiglu = std::is_same<OUT, uint8_t>::value;
     constexpr int kCols = kSwiglu ? kBN / 2 : kBN;
     __shared__ __align__(16) uint8_t lds[2 * kStageBytes];
     __shared__ float lds_sx[2 * kBM];
-    __shared__ float lds_sw[2 * kF8MaxStages];
+    __shared__ float lds_sw[2][2 * kF8MaxStages];
+    __shared__ WideTable table;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / kWavesN, wn = wave % kWavesN;
-    const int KT = a.KT, K = KT * 128, NT = (a.N + kCols - 1) / kCols;
-    Tile tile;
-    if (!find_tile<kBM>(a, NT, tile)) return;
-    const int n0 = tile.nt * kCols, NB = (a.N + 127) / 128;
-    {
-        const size_t first = (static_cast<size_t>(tile.e) * NB + n0 / 128) * KT;
-        for (int i = threadIdx.x; i < KT; i += 512) {
-            lds_sw[i] = a.s1[first + i];
-            lds_sw[KT + i] = kSwiglu ? a.s3[first + i] : a.s1[(n0 / 128 + 1 < NB ? first + KT : first) + i];
-        }
-    }
-    const bool loader = wave < kNL, active = tile.m0 + wm * kWM < tile.end;
-    Loads ld = {};
-    WideScales sc = {};
+    const int KT = a.KT, K = KT * 128, NT = (a.N + kCols - 1) / kCols, NB = (a.N + 127) / 128, first = KT & 1;
+    const int total = __builtin_amdgcn_readfirstlane(fill_table(a, table, lane, wave == 0)) * NT;
+    const int per = (total + 7) / 8, xcd = blockIdx.x % 8, step = gridDim.x / 8;
+    const int last = (xcd + 1) * per < total ? (xcd + 1) * per : total;
+    int id = xcd * per + blockIdx.x / 8;
+    if (id >= last) return;
+    __syncthreads();
+
     const LaneMap lm = lane_map(lane);
-    if (loader) {
-        ld.a_on = tile.m0 + wave / kWavesN * kWM < tile.end;
+    const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
+    const int col = wave >> 2, sub = wave & 3;         // B: wave column and eighths of a quarter's 32 rows
+    WideLoads ld = {};
+    ld.s_step = a.sx_block * 4;
+    ld.s_off = lane * 4;
+    ld.a_lds = lds_base + wave * kALdF8 * 1024;
+    ld.b_lds = lds_base + (kBM + col * kWN + sub * kRowsPerLoad) * kRowB;
+    ld.s_lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds_sx)) + (wave >> 1) * kWM * 4;
+    ld.b_off = lm.ld_row * K + (sub & 1 ? lm.col_b[1] : lm.col_b[0]);
+    const float* const sx = lds_sx + wm * kWM + lm.fr_row;
+    // a tile's operands, its first stage, and the weights' scales
+    auto begin = [&](const Tile& tile, float* sw) {
+        const int n0 = tile.nt * kCols;
         const size_t expert = static_cast<size_t>(tile.e) * a.N;
-        const int c = wave >> 1, h = (wave & 1) * 16;
         auto rows_at = [&](const uint8_t* w, int n) {
-            n = n < a.N ? n : a.N - 16;
+            n = n < a.N ? n : a.N - kRowsPerLoad;
             return reinterpret_cast<const char*>(w + (expert + n) * K);
         };
-        if constexpr (kSwiglu) {                       // 64 of W1, then 64 of W3, for each of the two wave columns
-            const int n = n0 + 64 * c + h;
-            ld.b0 = rows_at(a.w1, n);
-            ld.b1 = rows_at(a.w1, n + 32);
-            ld.c0 = rows_at(a.w3, n);
-            ld.c1 = rows_at(a.w3, n + 32);
-        } else {
-            const int n = n0 + 128 * c + h;
-            ld.b0 = rows_at(a.w1, n);
-            ld.b1 = rows_at(a.w1, n + 32);
-            ld.c0 = rows_at(a.w1, n + 64);
-            ld.c1 = rows_at(a.w1, n + 96);
-        }
-        auto source_row = [&](int r) {                 // rows past the end repeat the last
-            int row = tile.m0 + r;
+        const int n = n0 + (kSwiglu ? 64 : 128) * col + sub * kRowsPerLoad;
+        ld.b[0] = rows_at(a.w1, n);
+        ld.b[1] = rows_at(a.w1, n + 32);
+        ld.b[2] = rows_at(kSwiglu ? a.w3 : a.w1, kSwiglu ? n : n + 64);
+        ld.b[3] = rows_at(kSwiglu ? a.w3 : a.w1, kSwiglu ? n + 32 : n + 96);
+        ld.a = reinterpret_cast<const char*>(a.x);
+        ld.s = reinterpret_cast<const char*>(a.sx + tile.m0 + (wave >> 1) * kWM);
+#pragma unroll
+        for (int i = 0; i < kALdF8; ++i) {
+            int row = tile.m0 + wave * 8 * kALdF8 + i * kRowsPerLoad + lm.ld_row;     // rows past the end repeat the last
             row = row < tile.end ? row : tile.end - 1;
             if (a.row_src) {
                 row = a.row_src[row];
                 row = row < 0 ? 0 : row < a.x_rows ? row : a.x_rows - 1;
             }
-            return static_cast<uint32_t>(row);
-        };
-        ld.a = reinterpret_cast<const char*>(a.x);
+            ld.a_off[i] = static_cast<uint32_t>(row) * K + lm.col_b[i & 1];
+        }
+        const size_t at = (static_cast<size_t>(tile.e) * NB + n0 / 128) * KT;
+        float w0 = 0.0f, w1 = 0.0f;
+        if (static_cast<int>(threadIdx.x) < KT) {
+            w0 = a.s1[at + threadIdx.x];
+            w1 = kSwiglu ? a.s3[at + threadIdx.x] : a.s1[(n0 / 128 + 1 < NB ? at + KT : at) + threadIdx.x];
+        }
+        static_for<kALdF8>([&](auto I) { wide_a<I.value>(ld, 1, first); });
+        ld.a += kRowB;
+        wide_s(ld, 1, first);
+        static_for<4>([&](auto Q) { wide_b<Q.value>(ld, 1, first); });
+        if (static_cast<int>(threadIdx.x) < KT) {
+            sw[threadIdx.x] = w0;
+            sw[KT + threadIdx.x] = w1;
+        }
+    };
+    Tile tile = tile_at(table, a.E_loc, NT, id, lane);
+    int set = 0;
+    begin(tile, lds_sw[0]);
+    while (true) {
+        const float* const sw = lds_sw[set] + (kSwiglu ? 0 : wn * KT);
+        f32x4 acc[kMI][kNJ];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) ld.b_off[i] = (i * kRowsPerLoad + lm.ld_row) * K + lm.col_b[i];
+        for (int i = 0; i < kMI; ++i)
 #pragma unroll
-        for (int i = 0; i < kALd; ++i)
-            ld.a_off[i] = source_row(wave * kWM + i * kRowsPerLoad + lm.ld_row) * K + lm.col_b[i & 1];
-        sc.src = reinterpret_cast<const char*>(a.sx + tile.m0 + wave * kWM);
-        sc.step = a.sx_block * 4;
-        sc.off = lane * 4;
-        sc.dst = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds_sx)) + wave * kWM * 4;
+            for (int j = 0; j < kNJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (tile.m0 + wm * kWM < tile.end) f8_k_loop<kSwiglu, true>(KT, lds, sx, sw, wm, wn, lane, acc, ld);
+        else f8_k_loop<kSwiglu, false>(KT, lds, sx, sw, wm, wn, lane, acc, ld);
+        id += step;
+        const bool more = id < last;
+        const Tile done = tile;
+        if (more) {
+            tile = tile_at(table, a.E_loc, NT, id, lane);
+            set ^= 1;
+            begin(tile, lds_sw[set]);
+        }
+        uint8_t* const out_lds = lds + (first ^ 1) * kStageBytes;
+        if constexpr (kSwiglu)
+            finish_tile<kBM, kBN, kWavesM, kWavesN, OUT>(a, done, done.nt * kCols, wm, wn, lane, acc, out_lds);
+        else
+            store_wide(a, done, done.nt * kCols, wm, wn, wave, lane, acc, out_lds);
+        if (!more) return;
     }
-    sc.sx = lds_sx + wm * kWM + lm.fr_row;
-    sc.sw = lds_sw + (kSwiglu ? 0 : wn * KT);
-    const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
-    const uint32_t a_lds = lds_base + wave * kALd * 1024;
-    const uint32_t b_lds = lds_base + (kBM + (wave >> 1) * kWN + (wave & 1) * 16) * kRowB;
-    f32x4 acc[kMI][kNJ];
-#pragma unroll
-    for (int i = 0; i < kMI; ++i)
-#pragma unroll
-        for (int j = 0; j < kNJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    __syncthreads();                                   // the weights' scales; no load of the loop is under way yet
-    if (loader) {
-        if (active) f8_k_loop<kSwiglu, true, true>(KT, lds, wm, wn, lane, acc, ld, sc, a_lds, b_lds);
-        else f8_k_loop<kSwiglu, true, false>(KT, lds, wm, wn, lane, acc, ld, sc, a_lds, b_lds);
-    } else {
-        if (active) f8_k_loop<kSwiglu, false, true>(KT, lds, wm, wn, lane, acc, ld, sc, a_lds, b_lds);
-        else f8_k_loop<kSwiglu, false, false>(KT, lds, wm, wn, lane, acc, ld, sc, a_lds, b_lds);
-    }
-    if constexpr (kSwiglu) finish_tile<kBM, kBN, kWavesM, kWavesN, OUT>(a, tile, n0, wm, wn, lane, acc, lds);
-    else store_wide(a, tile, n0, wm, wn, wave, lane, acc, lds);
 }
 
 template <int BM, int BN, int NWM, int NWN, typename OUT>
@@ -699,8 +786,10 @@ template <typename OUT>
 cap_status launch_wide(F8Args a, float* scales, hipStream_t st) {
     constexpr int cols = std::is_same<OUT, uint8_t>::value ? kBN / 2 : kBN;
     const long long rows = a.max_rows / kBM + (a.E_loc < a.max_rows ? a.E_loc : a.max_rows);
-    const long long blocks = (rows * ((a.N + cols - 1) / cols) + 7) / 8 * 8;
-    if (blocks * 512 >= (1ll << 32)) return CAP_ERR_UNSUPPORTED;
+    const long long tiles = rows * ((a.N + cols - 1) / cols);
+    if (tiles >= (1ll << 31)) return CAP_ERR_UNSUPPORTED;
+    const long long cus = (device_cu_count() + 7) / 8 * 8;             // one workgroup a CU
+    const long long blocks = tiles < cus ? (tiles + 7) / 8 * 8 : cus;
     if (a.sx_row != 1) {
         const size_t pitch = f8_scale_pitch(a.max_rows);
         f8_gather_scales_kernel<<<(a.max_rows + 63) / 64, 256, 0, st>>>(a, scales, pitch);
@@ -729,7 +818,7 @@ namespace {
 
 cap_status product(cap_dtype out_dtype, const F8Args& a, float* scales, hipStream_t st) {
     if (out_dtype == CAP_DTYPE_F32) return launch_tiles<128, 128, 2, 2, float>(a, st);
-    if (wide_rows(a.max_rows) && a.N % 16 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15) == 0)
+    if (wide_rows(a.max_rows) && a.N % 8 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15) == 0)
         return launch_wide<uint16_t>(a, scales, st);
     return launch_tiles<128, 128, 2, 2, uint16_t>(a, st);
 }

@@ -219,6 +219,49 @@ def test_offsets_past_31_bits(capi):
     assert ((y.double() - want).abs() <= 400 * 2.0 ** -24 * want).all()
 
 
+# ------------------------------------------------------------------ wide tiles (many rows)
+WIDE_SHAPES = [([5000, 0, 3300], 264, 128, 0), ([8192], 1000, 256, 700), ([1, 257, 8000, 3], 520, 384, 0), ([130] * 64, 256, 640, 300),
+               ([8500], 8, 1408, 0), ([4100, 4100], 1003, 128, 0)]
+
+
+def _want_rows(p, rows):
+    """_want of some rows only."""
+    e = np.searchsorted(p["offsets"], rows, side="right") - 1
+    y, off = [], []
+    for r, ex in zip(rows, e):
+        at = p["src"][r] if p["src"] is not None else r
+        q = dict(counts=[1], n=p["n"], kdim=p["kdim"], src=None, x=p["x"][at:at + 1], sx=p["sx"][at:at + 1], w=p["w"][ex:ex + 1],
+                 sw=p["sw"][ex:ex + 1], offsets=np.array([0, 1], np.int32))
+        a, b = _want(q, True)
+        y.append(a[0])
+        off.append(b[0])
+    return np.array(y), np.array(off)
+
+
+def _sample(rng, counts, n):
+    """Rows at the experts' and the tiles' ends, and some others."""
+    ends = np.cumsum([0] + counts)
+    rows = [r for a, b in zip(ends[:-1], ends[1:]) for r in (a, a + 63, a + 64, a + 255, a + 256, b - 1) if a <= r < b]
+    return np.unique(np.concatenate([rows, rng.integers(0, ends[-1], n)]))
+
+
+@pytest.mark.parametrize("shape", range(len(WIDE_SHAPES)))
+def test_wide_product(capi, shape):
+    counts, n, kdim, x_rows = WIDE_SHAPES[shape]
+    rng = np.random.default_rng(80 + shape)
+    p = _problem(rng, counts, n, kdim, x_rows)
+    y = _run(capi, p, True)
+    rows = _sample(rng, counts, 60)
+    want, off = _want_rows(p, rows)
+    assert np.all(np.abs(y[rows] - want) <= off)
+    # every row against the kernel of few rows, within both bounds: one code path cannot be off alone
+    z = torch.from_numpy(y)
+    f32 = torch.from_numpy(_run(capi, p, False))
+    assert ((z - f32).norm() <= 3e-3 * f32.norm()).item() and ((z - f32).abs().amax(1) <= 0.02 * f32.abs().amax(1) + 1e-6).all()
+    more = _run(capi, p, True, len(y) + 700)
+    assert np.array_equal(more[:len(y)], y) and (more[len(y):] == -7.0).all()
+
+
 # ------------------------------------------------------------------ feed-forward
 def _ffn_want(p):
     """y in 64 bits with H rounded where the kernel rounds it, and how far the kernel may be off."""
@@ -309,3 +352,19 @@ def test_ffn_nan_stays_in_its_row(capi):
     hit = np.zeros(len(y), bool)
     hit[[2, 100]] = True
     assert np.isnan(y[hit]).all() and np.array_equal(y[~hit], clean[~hit])
+
+
+@pytest.mark.parametrize("counts,d,inter,x_rows", [([5000, 0, 3300], 256, 128, 0), ([3, 8300], 384, 640, 1000), ([8192], 128, 256, 0)])
+def test_wide_ffn(capi, counts, d, inter, x_rows):
+    rng = np.random.default_rng(90 + d)
+    p = _ffn_problem(rng, counts, d, inter, x_rows)
+    y = _ffn(capi, p)
+    for r in _sample(rng, counts, 25):
+        e = int(np.searchsorted(p["offsets"], r, side="right") - 1)
+        at = p["src"][r] if p["src"] is not None else r
+        q = dict(p, counts=[1], src=None, x=p["x"][at:at + 1], sx=p["sx"][at:at + 1], offsets=np.array([0, 1], np.int32),
+                 **{k: p[k][e:e + 1] for k in ("w", "sw", "w3", "sw3", "w2", "sw2")})
+        want, off = _ffn_want(q)
+        assert np.all(np.abs(y[r] - want[0]) <= off[0]), r
+    z = _ffn(capi, p, len(y) + 300)
+    assert np.array_equal(z[:len(y)], y) and (z[len(y):] == -7.0).all()
