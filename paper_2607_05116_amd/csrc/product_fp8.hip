@@ -21,6 +21,9 @@
 #include "mfma_tile.hpp"
 
 namespace cap {
+
+cap_status quantise_fp8_launch(cap_dtype, int, int, int, int, const void*, void*, float*, hipStream_t);
+
 namespace {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -761,6 +764,208 @@ cap_status launch_tiles(const F8Args& a, hipStream_t st) {
     return CAP_OK;
 }
 
+// ------------------------------------------------------------------ few rows
+// Up to some tens of rows an expert: every weight is read once for little arithmetic, and
+// its way from memory is all that counts.  A workgroup takes 16 I rows of an expert and 16 J
+// of its outputs (within one scale block); its eight waves share the blocks of K among
+// them, load their weights straight into the MFMA's registers, a block ahead, and join
+// their sums in LDS in the waves' order.  SwiGLU: four waves take W1 and four W3, and H
+// leaves in fp32: quantising it takes 128 of its columns, and workgroups of so many leave
+// half of the compute units without one.
+template <int BM>
+__device__ __forceinline__ bool find_rows(const F8Args& a, int NT, Tile& out) {
+    const int lane = threadIdx.x & 63, id = blockIdx.x;
+    int lo[kMaxE / 64], n[kMaxE / 64];
+    const int base = a.offsets[0];
+#pragma unroll
+    for (int c = 0; c < kMaxE / 64; ++c) {             // all on their way together; experts past the last are empty
+        const int e = 64 * c + lane;
+        lo[c] = a.offsets[e < a.E_loc ? e : a.E_loc];
+        n[c] = a.offsets[e < a.E_loc ? e + 1 : a.E_loc];
+    }
+#pragma unroll
+    for (int c = 0; c < kMaxE / 64; ++c) {
+        auto within = [&](int v) { return v < 0 ? 0 : v > a.max_rows ? a.max_rows : v; };
+        lo[c] = within(lo[c] - base);
+        const int hi = within(n[c] - base);
+        n[c] = hi > lo[c] ? hi - lo[c] : 0;
+    }
+    int before = 0;
+#pragma unroll
+    for (int c = 0; c < kMaxE / 64; ++c) {
+        if (64 * c >= a.E_loc) break;
+        const int m = (n[c] + BM - 1) / BM;
+        int upto = m;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int o = __shfl_up(upto, d);
+            upto += lane >= d ? o : 0;
+        }
+        const uint64_t hit = __ballot(id < before + upto * NT);
+        if (hit) {
+            const int l = __ffsll(static_cast<unsigned long long>(hit)) - 1;
+            const int mt = __builtin_amdgcn_readlane(m, l);
+            const int local = id - before - (__builtin_amdgcn_readlane(upto, l) - mt) * NT;
+            const int start = __builtin_amdgcn_readlane(lo[c], l);
+            out.e = 64 * c + l;
+            out.nt = local / mt;                       // an output block's row tiles side by side: its weights meet in a cache
+            out.m0 = start + (local % mt) * BM;
+            out.end = start + __builtin_amdgcn_readlane(n[c], l);
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63) * NT;
+    }
+    return false;
+}
+
+template <int I, int J>
+struct FewStage {
+    i32x4 w[J][2], x[I][2];
+    float sx[I], sw;
+};
+
+template <int I, int J, typename OUT, bool kSwiglu>
+__global__ __launch_bounds__(512) void f8_few_kernel(const F8Args a) {
+    constexpr bool kPrecise = std::is_same<OUT, float>::value && !kSwiglu;
+    constexpr int kParts = kSwiglu ? 4 : 8;            // waves that share K
+    constexpr int kCols = 16 * J, kRows = 16 * I;
+    constexpr int kPitch = kCols + 4;                  // of a row of sums in LDS
+    __shared__ __align__(16) float sums[8][kRows][kPitch];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int part = wave % kParts;
+    const bool up = kSwiglu && wave >= kParts;
+    const int KT = a.KT, NT = (a.N + kCols - 1) / kCols, NB = (a.N + 127) / 128;
+    const size_t K = static_cast<size_t>(KT) * 128;
+    Tile tile;
+    if (!find_rows<kRows>(a, NT, tile)) return;
+    const int n0 = tile.nt * kCols, r16 = lane & 15, g = lane >> 4;
+    const uint8_t* const w = (up ? a.w3 : a.w1) + static_cast<size_t>(tile.e) * a.N * K;
+    const float* const sw = (up ? a.s3 : a.s1) + (static_cast<size_t>(tile.e) * NB + n0 / 128) * KT;
+    uint32_t w_off[J], x_off[I];
+    size_t s_off[I];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const int n = n0 + 16 * j + r16;
+        w_off[j] = static_cast<uint32_t>(n < a.N ? n : a.N - 1) * static_cast<uint32_t>(K) + 16 * g;
+    }
+    FewStage<I, J> st[2];
+    auto load_w = [&](FewStage<I, J>& s, int kt) {
+        const uint8_t* const p = w + static_cast<size_t>(kt) * 128;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) s.w[j][h] = *reinterpret_cast<const i32x4*>(p + w_off[j] + 64 * h);
+        s.sw = sw[kt];
+    };
+    auto load_x = [&](FewStage<I, J>& s, int kt) {
+        const uint8_t* const p = a.x + static_cast<size_t>(kt) * 128;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) s.x[i][h] = *reinterpret_cast<const i32x4*>(p + x_off[i] + 64 * h);
+            s.sx[i] = a.sx[s_off[i] + kt * a.sx_block];
+        }
+    };
+    if (part < KT) load_w(st[0], part);                // before the rows' sources are known
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        int row = tile.m0 + 16 * i + r16;              // rows past the end repeat the last
+        row = row < tile.end ? row : tile.end - 1;
+        if (a.row_src) {
+            row = a.row_src[row];
+            row = row < 0 ? 0 : row < a.x_rows ? row : a.x_rows - 1;
+        }
+        x_off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(K) + 16 * g;
+        s_off[i] = row * a.sx_row;
+    }
+    f32x4 acc[I][J];
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    auto add = [&](const FewStage<I, J>& s) {
+        i32x8 xf[I];
+#pragma unroll
+        for (int i = 0; i < I; ++i) xf[i] = __builtin_shufflevector(s.x[i][0], s.x[i][1], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const i32x8 wf = __builtin_shufflevector(s.w[j][0], s.w[j][1], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                const f32x4 d = block_sum<kPrecise>(wf, xf[i]);
+                const float f = s.sx[i] * s.sw;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(d[v], f, acc[i][j][v]);
+            }
+        }
+    };
+    if (part < KT) load_x(st[0], part);
+    int kt = part;
+    for (; kt + kParts < KT; kt += 2 * kParts) {
+        load_w(st[1], kt + kParts);
+        load_x(st[1], kt + kParts);
+        add(st[0]);
+        if (kt + 2 * kParts < KT) {
+            load_w(st[0], kt + 2 * kParts);
+            load_x(st[0], kt + 2 * kParts);
+        }
+        add(st[1]);
+    }
+    if (kt < KT) add(st[0]);
+
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) *reinterpret_cast<f32x4*>(&sums[wave][16 * i + r16][16 * j + 4 * g]) = acc[i][j];
+    __syncthreads();
+    // four neighbouring outputs a thread
+    constexpr int kQuads = kRows * kCols / 4;
+    for (int t = threadIdx.x; t < (kQuads + 63) / 64 * 64; t += 512) {
+        const int r = t / (kCols / 4), c = t % (kCols / 4) * 4;
+        const int row = tile.m0 + r, n = n0 + c;
+        const bool there = t < kQuads && row < tile.end;
+        auto join = [&](int first) {
+            f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) v += *reinterpret_cast<const f32x4*>(&sums[first + p][t < kQuads ? r : 0][c]);
+            return v;
+        };
+        f32x4 v = join(0);
+        if constexpr (kSwiglu) {
+            const f32x4 u = join(kParts);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = v[i] * __builtin_amdgcn_rcpf(1.0f + __expf(-v[i])) * u[i];
+        }
+        {
+            if (!there || n >= a.N) continue;
+            OUT* const p = static_cast<OUT*>(a.out) + static_cast<size_t>(row) * a.N + n;
+            const bool whole = (a.N & 3) == 0 && (reinterpret_cast<uintptr_t>(a.out) & (4 * sizeof(OUT) - 1)) == 0;
+            if (whole) {
+                if constexpr (std::is_same<OUT, float>::value) *reinterpret_cast<f32x4*>(p) = v;
+                else *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2_rne(v[0], v[1]), pack_bf16x2_rne(v[2], v[3])};
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (n + i < a.N) {
+                        if constexpr (std::is_same<OUT, float>::value) p[i] = v[i];
+                        else p[i] = static_cast<uint16_t>(pack_bf16x2_rne(v[i], v[i]));
+                    }
+            }
+        }
+    }
+}
+
+template <int I, int J, typename OUT, bool SWIGLU = false>
+cap_status launch_few(const F8Args& a, hipStream_t st) {
+    constexpr int rows = 16 * I, cols = 16 * J;
+    const long long tiles = a.max_rows / rows + (a.E_loc < a.max_rows ? a.E_loc : a.max_rows);
+    const long long blocks = tiles * ((a.N + cols - 1) / cols);
+    if (blocks * 512 >= (1ll << 32)) return CAP_ERR_UNSUPPORTED;
+    f8_few_kernel<I, J, OUT, SWIGLU><<<static_cast<unsigned>(blocks), 512, 0, st>>>(a);
+    CAP_LAUNCH_CHECK();
+    return CAP_OK;
+}
+
 // Scales of the rows in expert-sorted order, [KT][pitch]; a lane takes a row.
 __global__ __launch_bounds__(256) void f8_gather_scales_kernel(const F8Args a, float* __restrict__ out, size_t pitch) {
     const int i = blockIdx.x * 64 + (threadIdx.x & 63);
@@ -778,9 +983,35 @@ __global__ __launch_bounds__(256) void f8_gather_scales_kernel(const F8Args a, f
 size_t f8_scale_pitch(int max_rows) { return (static_cast<size_t>(max_rows) + 2 * kBM - 1) / kBM * kBM; }
 size_t f8_scales_bytes(int k, int max_rows) { return f8_scale_pitch(max_rows) * (k / 128) * 4; }
 
-// Wide tiles: enough rows that their weights' passes through the tiles count for less
-// than the halves of tiles that stay empty.
-bool wide_rows(int max_rows) { return max_rows >= 8192; }
+// Which kernel a call takes goes by estimates of its time in microseconds, from its sizes
+// alone (max_rows for the rows, as if they fell about evenly; every kernel is right for any).
+// Measured, estimates in brackets: E = 8, n = 2048, kdim = 7168, 64 rows: few 21.5 (25), wide
+// 56 (61); 256 rows: 47 (47), 57 (61); n = 7168, kdim = 2048, 64 rows: 24.5 (25), 25.4 (28); 256
+// rows: 42 (42), 26 (28); E = 1, n = 1003, kdim = 2048, fp32, 16 rows: few 6.9 (4), tiles 24 (26).
+constexpr int kFewFfnRows = 8192;                      // the feed-forward's workspace has room for so many rows of H in fp32
+long long likely_tiles(const F8Args& a, int rows) {    // row tiles, experts' sizes differing by a factor of three
+    const long long some = a.E_loc < a.max_rows ? a.E_loc : a.max_rows, more = a.max_rows - 8ll * a.E_loc;
+    return some + (more > 0 ? more / rows : 0);
+}
+// Enough workgroups of 16 J outputs for three of four compute units.
+bool few_fill(const F8Args& a, int rows, int cols) {
+    return 4 * likely_tiles(a, rows) * ((a.N + cols - 1) / cols) >= 3 * device_cu_count();
+}
+// 32 rows a workgroup once most experts have more than 8 rows.
+bool few_take_32(const F8Args& a) { return a.max_rows > 8ll * a.E_loc && few_fill(a, 32, 64); }
+double weight_bytes(const F8Args& a) { return static_cast<double>(a.w3 ? 2 : 1) * a.N * a.KT * 128; }
+double few_time(const F8Args& a) {                     // the weights' way, again for each row tile
+    return 3.5 + static_cast<double>(likely_tiles(a, few_take_32(a) ? 32 : 16)) * weight_bytes(a) / 5.5e6;
+}
+// Tiles: a round of them takes so long a stage, but no less than the weights' way.
+double tiles_time(const F8Args& a, int rows, int cols, int at_once, double stage) {
+    const long long tiles = likely_tiles(a, rows) * ((a.N + cols - 1) / cols);
+    const double stages = stage * a.KT * static_cast<double>((tiles + at_once - 1) / at_once);
+    const double bytes = static_cast<double>(a.E_loc < a.max_rows ? a.E_loc : a.max_rows) * weight_bytes(a) / 5.0e6;
+    return 5.0 + (stages > bytes ? stages : bytes);
+}
+double wide_time(const F8Args& a) { return tiles_time(a, kBM, a.w3 ? kBN / 2 : kBN, device_cu_count(), 1.0); }
+double tile_time(const F8Args& a) { return tiles_time(a, 128, 128, 2 * device_cu_count(), 1.35); }
 
 template <typename OUT>
 cap_status launch_wide(F8Args a, float* scales, hipStream_t st) {
@@ -790,7 +1021,7 @@ cap_status launch_wide(F8Args a, float* scales, hipStream_t st) {
     if (tiles >= (1ll << 31)) return CAP_ERR_UNSUPPORTED;
     const long long cus = (device_cu_count() + 7) / 8 * 8;             // one workgroup a CU
     const long long blocks = tiles < cus ? (tiles + 7) / 8 * 8 : cus;
-    if (a.sx_row != 1) {
+    if (scales) {                                      // else a.sx is in the rows' order, whole tiles of them
         const size_t pitch = f8_scale_pitch(a.max_rows);
         f8_gather_scales_kernel<<<(a.max_rows + 63) / 64, 256, 0, st>>>(a, scales, pitch);
         a.sx = scales;
@@ -805,21 +1036,48 @@ cap_status launch_wide(F8Args a, float* scales, hipStream_t st) {
 }  // namespace
 
 size_t product_fp8_workspace_bytes(int, int kdim, int max_rows) {
-    return wide_rows(max_rows) ? f8_scales_bytes(kdim, max_rows) : 0;
+    return f8_scales_bytes(kdim, max_rows);
 }
 
-// H's codes, its scales, and the scales of x in the rows' order.
-size_t ffn_fp8_workspace_bytes(int d, int inter, int max_rows) {
-    const size_t codes = (static_cast<size_t>(max_rows) * inter + 255) & ~size_t(255);
-    return codes + f8_scales_bytes(inter, max_rows) + (wide_rows(max_rows) ? f8_scales_bytes(d, max_rows) : 0);
+// H's codes and its scales, [KT][rows], then scales in the rows' order (of x, or of H quantised
+// from fp32) and H in fp32, which few rows need.
+struct FfnSpace {
+    size_t codes, h_scales, scales, h, end;
+};
+FfnSpace ffn_space(int d, int inter, int max_rows) {
+    FfnSpace s;
+    s.codes = 0;
+    s.h_scales = (static_cast<size_t>(max_rows) * inter + 255) & ~size_t(255);
+    s.scales = s.h_scales + f8_scales_bytes(inter, max_rows);
+    s.h = s.scales + f8_scales_bytes(d > inter ? d : inter, max_rows);
+    s.end = s.h + (max_rows <= kFewFfnRows ? static_cast<size_t>(max_rows) * inter * 4 : 0);
+    return s;
 }
+size_t ffn_fp8_workspace_bytes(int d, int inter, int max_rows) { return ffn_space(d, inter, max_rows).end; }
 
 namespace {
 
+template <typename OUT, bool SWIGLU>
+cap_status launch_few_rows(const F8Args& a, hipStream_t st) {
+    if (few_take_32(a)) return launch_few<2, 4, OUT, SWIGLU>(a, st);
+    // the more outputs a workgroup, the fewer bytes of x it reads beside its weights; with W1
+    // and W3, a wave has twice the blocks of K (128 outputs: 78 us for 8 rows of 8 experts of
+    // d = 7168, inter = 2048 in 128 workgroups, 64: 47 us)
+    if constexpr (!SWIGLU)
+        if (likely_tiles(a, 16) * ((a.N + 127) / 128) >= device_cu_count()) return launch_few<1, 8, OUT, SWIGLU>(a, st);
+    if (few_fill(a, 16, 64)) return launch_few<1, 4, OUT, SWIGLU>(a, st);
+    return launch_few<1, 2, OUT, SWIGLU>(a, st);
+}
+
+// scales: room for those of the rows in their order; nullptr: a.sx holds them so.
 cap_status product(cap_dtype out_dtype, const F8Args& a, float* scales, hipStream_t st) {
-    if (out_dtype == CAP_DTYPE_F32) return launch_tiles<128, 128, 2, 2, float>(a, st);
-    if (wide_rows(a.max_rows) && a.N % 8 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15) == 0)
-        return launch_wide<uint16_t>(a, scales, st);
+    if (out_dtype == CAP_DTYPE_F32) {
+        if (few_time(a) < tile_time(a)) return launch_few_rows<float, false>(a, st);
+        return launch_tiles<128, 128, 2, 2, float>(a, st);
+    }
+    const bool wide = a.N % 8 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15) == 0;
+    if (few_time(a) < (wide ? wide_time(a) : tile_time(a))) return launch_few_rows<uint16_t, false>(a, st);
+    if (wide) return launch_wide<uint16_t>(a, scales, st);
     return launch_tiles<128, 128, 2, 2, uint16_t>(a, st);
 }
 
@@ -850,9 +1108,12 @@ cap_status expert_ffn_fp8_launch(int E_loc, int d, int inter, int max_rows, cons
                                  int x_rows, const int32_t* row_src, const int32_t* row_offsets, const void* w1,
                                  const float* s1, const void* w3, const float* s3, const void* w2, const float* s2,
                                  void* y, void* ws, hipStream_t st) {
-    uint8_t* const h = static_cast<uint8_t*>(ws);
-    float* const sh = reinterpret_cast<float*>(h + ((static_cast<size_t>(max_rows) * inter + 255) & ~size_t(255)));
-    float* const sxt = sh + f8_scales_bytes(inter, max_rows) / 4;
+    const FfnSpace space = ffn_space(d, inter, max_rows);
+    uint8_t* const at = static_cast<uint8_t*>(ws);
+    uint8_t* const codes = at + space.codes;
+    float* const h_scales = reinterpret_cast<float*>(at + space.h_scales);
+    float* const scales = reinterpret_cast<float*>(at + space.scales);
+    float* const h = reinterpret_cast<float*>(at + space.h);
     F8Args a = {};
     a.x = static_cast<const uint8_t*>(x);
     a.sx = x_scale;
@@ -864,28 +1125,38 @@ cap_status expert_ffn_fp8_launch(int E_loc, int d, int inter, int max_rows, cons
     a.w3 = static_cast<const uint8_t*>(w3);
     a.s1 = s1;
     a.s3 = s3;
-    a.out = h;
-    a.out_scale = sh;
+    a.out = codes;
+    a.out_scale = h_scales;
     a.scale_pitch = f8_scale_pitch(max_rows);
     a.x_rows = x_rows;
     a.E_loc = E_loc;
     a.max_rows = max_rows;
     a.N = inter;
     a.KT = d / 128;
-    const cap_status first = wide_rows(max_rows) ? launch_wide<uint8_t>(a, sxt, st) : launch_tiles<128, 256, 2, 4, uint8_t>(a, st);
-    if (first != CAP_OK) return first;
-    a.x = h;
-    a.sx = sh;
-    a.sx_row = 1;
-    a.sx_block = a.scale_pitch;
+    // few rows: H in fp32, then its codes (3 us, as the wide tiles' scales take)
+    const bool few = max_rows <= kFewFfnRows && few_time(a) < wide_time(a);
+    cap_status done;
+    if (few) {
+        a.out = h;
+        done = launch_few_rows<float, true>(a, st);
+        if (done == CAP_OK) done = quantise_fp8_launch(CAP_DTYPE_F32, 1, max_rows, inter, 1, h, codes, h_scales, st);
+    } else {
+        done = launch_wide<uint8_t>(a, scales, st);
+    }
+    if (done != CAP_OK) return done;
+    a.x = codes;
+    a.sx = h_scales;
+    a.sx_row = few ? inter / 128 : 1;
+    a.sx_block = few ? 1 : a.scale_pitch;
     a.row_src = nullptr;
     a.w1 = static_cast<const uint8_t*>(w2);
     a.s1 = s2;
+    a.w3 = nullptr;
     a.out = y;
     a.x_rows = max_rows;
     a.N = d;
     a.KT = inter / 128;
-    return product(CAP_DTYPE_BF16, a, nullptr, st);
+    return product(CAP_DTYPE_BF16, a, few ? scales : nullptr, st);
 }
 
 }  // namespace cap
