@@ -664,7 +664,8 @@ typedef struct {
  *   4. w' = scale s_e / (normalise ? sum over the kept : 1) for kept slots, 0 for others.
  * A slot whose expert is off is not kept (its idx is still an expert of its own).  All
  * decisions are those of fp64 values, of which keys keep 44 bits: closer ones count as
- * equal.  Scores below 1e-300 are 0; gates are rounded to fp32 once.
+ * equal.  Scores below 1e-300 are 0; gates are rounded to fp32 once (those of a softmax
+ * without normalise carry the error of its sum of fp32 exponentials, below 2^-20).
  * Outputs as cap_route_prune: idx[T][k] in the order of step 2, w, keep, dst_mask.
  * No workspace.
  */

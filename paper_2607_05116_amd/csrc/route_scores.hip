@@ -25,7 +25,7 @@
 namespace cap {
 namespace {
 
-constexpr int kQuadLanes = 4;               // lanes of a token
+constexpr int kQuadLanes = 4;
 constexpr uint32_t kOffHigh = 0xFFEFFFFFu;  // high word of an off expert's key: about the lowest double
 
 struct ScoreArgs {
@@ -121,6 +121,12 @@ __device__ __forceinline__ double group_total(double a, double b, int top) {
     return top > 1 && b > kNoKey ? a + b : a;
 }
 
+// Tokens up to which sixteen lanes take one.
+#ifndef FEWT
+#define FEWT 8192
+#endif
+constexpr int kFewTokens = FEWT;
+
 // Slots of the routing: s = 0 .. N - 1 as a compile-time loop.
 template <int N, int I = 0, typename F>
 __device__ __forceinline__ void each_slot(F&& f) {
@@ -130,218 +136,373 @@ __device__ __forceinline__ void each_slot(F&& f) {
     }
 }
 
-// Four lanes per token; lane h holds experts c * 16 + h * 4 + [0, 4), c < V / 4, and
-// owns slots h and h + 4.
-//   SCORE   keys are biased scores (else logits)
-//   GROUPS  0: one group (or all of them open); 1: groups of 16 * CPG experts, which
-//           are whole values of c; 2: any, through LDS (one wave per workgroup)
-template <int V, int KP, bool SCORE, bool VEC, int GROUPS, int CPG>
-__global__ __launch_bounds__(GROUPS == 2 ? 64 : 256) void route_scores_kernel(const ScoreArgs a) {
-    constexpr int kThreads = GROUPS == 2 ? 64 : 256;
-    constexpr int C = V / 4;
+// ------------------------------------------------------------------ exact choice
+// How far two biased scores v may lie apart, relative to 1 + |v|, and not be ordered for
+// certain by their fp32 values: twice their error, and twice that for a margin.  A sigmoid's
+// error is below 2^-22 (in units of 2^-24: 0.3 from the rounded argument, weighed with
+// s (1 - s) |x| < 0.23; 0.5 from the exponential's ulp, 1 from 1 + e, 2 from the reciprocal's
+// ulp), a softmax probability's 2^-20 of it (that of its sum, see below); the sum with the
+// bias rounds by 2^-24 |v|.
+constexpr float kUnsureSigmoid = 0x1p-20f, kUnsureSoftmax = 0x1p-18f;
+
+constexpr int kExactValues = kMaxE;
+struct ExactSpace {
+    double value[kExactValues];
+    int chosen[kMaxK];
+};
+
+// The choice of one token by the whole wave, on fp64 scores: for the few tokens that fp32
+// leaves unsure, and for ties.  Leaves expert | on << 16 of each slot in space.chosen.
+__device__ __forceinline__ void exact_choice(const ScoreArgs& a, int t, ExactSpace& space) {
+    const int lane = threadIdx.x & 63;
+    const float* row = a.logits + static_cast<size_t>(t) * a.E;
+    const bool counted = !a.token_mask || a.token_mask[t] != 0;
+    float x[4];
+    bool on[4];
+    float top_x = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int e = 4 * lane + i;
+        x[i] = e < a.E ? row[e] : -INFINITY;
+        on[i] = counted && x[i] > -INFINITY;
+        top_x = on[i] ? fmaxf(top_x, x[i]) : top_x;
+    }
+    double inv_sum = 1.0;
+    if (!a.sigmoid) {
+        for (int d = 1; d < 64; d *= 2) top_x = fmaxf(top_x, __shfl_xor(top_x, d));
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            sum += on[i] ? exp64(static_cast<double>(x[i]) - static_cast<double>(top_x)) : 0.0;
+        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+        inv_sum = sum > 0.0 ? 1.0 / sum : 0.0;
+    }
+    double key[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int e = 4 * lane + i;
+        double v = 0.0;
+        if (on[i])
+            v = a.sigmoid ? sigmoid64(x[i]) : exp64(static_cast<double>(x[i]) - static_cast<double>(top_x)) * inv_sum;
+        if (a.bias && e < a.E) v += static_cast<double>(a.bias[e]);
+        space.value[4 * lane + i] = on[i] ? words(high_word(v), low_word(v) & ~255u) : kNoKey;
+        const uint32_t tie = 255u - static_cast<uint32_t>(e);
+        const uint32_t hi = high_word(v), sign = static_cast<uint32_t>(static_cast<int32_t>(hi) >> 31);
+        // (without a bias, the choice within groups goes by the logits)
+        key[i] = !on[i] ? words(kOffHigh, ~tie) : a.bias ? words(hi, (low_word(v) & ~255u) | ((tie ^ sign) & 255u)) : logit_key(x[i], tie);
+        key[i] = e < a.E ? key[i] : kNoKey;
+    }
+    if (a.open_groups < a.groups) {
+        __builtin_amdgcn_wave_barrier();               // one wave: its LDS accesses stay in order
+        double b1 = kNoKey, b2 = kNoKey;
+        if (lane < a.groups)
+            for (int i = 0; i < a.group_size; ++i) best_two(b1, b2, space.value[lane * a.group_size + i]);
+        const double total = group_total(b1, b2, a.group_top);
+        int ahead = 0;
+        for (int o = 0; o < a.groups; ++o) {
+            const double other = __shfl(total, o);
+            ahead += (o < lane ? other >= total : other > total) ? 1 : 0;
+        }
+        const uint64_t open = __ballot(lane < a.groups && ahead < a.open_groups);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = 4 * lane + i;
+            key[i] = e < a.E && ((open >> small_quotient(e, a.group_size)) & 1ull) ? key[i] : kNoKey;
+        }
+    }
+    for (int s = 0; s < a.k; ++s) {
+        double best = __builtin_fmax(__builtin_fmax(key[0], key[1]), __builtin_fmax(key[2], key[3]));
+        for (int d = 1; d < 64; d *= 2) best = __builtin_fmax(best, __shfl_xor(best, d));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) key[i] = key[i] == best ? kNoKey : key[i];     // keys are distinct
+        if (lane == 0) space.chosen[s] = key_expert(best) | (high_word(best) != kOffHigh ? 1 << 16 : 0);
+    }
+    __builtin_amdgcn_wave_barrier();
+}
+
+// ------------------------------------------------------------------ routing
+// Joins over the L lanes of a token (4: a quad; 16: a DPP row).
+template <int L, typename F>
+__device__ __forceinline__ void over_lanes(F&& step) {
+    step(std::integral_constant<int, kDppXor1>{});
+    step(std::integral_constant<int, kDppXor2>{});
+    if constexpr (L == 16) {
+        step(std::integral_constant<int, kDppHalfMirror>{});
+        step(std::integral_constant<int, 0x140>{});    // row_mirror
+    }
+}
+template <int CTRL>
+__device__ __forceinline__ int dpp_swap_i32(int v) { return __builtin_amdgcn_mov_dpp(v, CTRL, 0xF, 0xF, true); }
+
+// L lanes per token; lane h holds experts c * 4 L + h * 4 + [0, 4), c < V / 4; the lanes h of
+// a quad own slots h and h + 4 (of 16 lanes, all quads work them out, and the first writes).
+//   SCORE   the choice goes by biased scores, first in fp32; tokens whose order that leaves
+//           unsure (about one of 2000) are chosen by exact_choice.  Else it goes by logits.
+//   GROUPS  0: one group (or all of them open); 1: groups of 16 * CPG experts, which are whole
+//           values of c (L = 4); 2: any, through LDS
+// What bounds it: instruction issue, most of it the selection network.  All scores in fp64
+// took 35.8 us for 32,768 tokens of 256 experts (one wave a SIMD, for the registers of 64 keys
+// a lane): keys are formed block by block now, and fp64 is left to the chosen slots.
+template <int L, int V, int KP, bool SCORE, bool VEC, int GROUPS, int CPG>
+__global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
+    constexpr int C = V / 4, kTokens = 256 / L;
     constexpr int NS = (KP + 3) / 4;
-    const int h = threadIdx.x & 3;
-    const int t = blockIdx.x * (kThreads / kQuadLanes) + (threadIdx.x >> 2);
+    __shared__ ExactSpace exact[SCORE ? 4 : 1];
+    const int h = threadIdx.x & (L - 1), hq = h & 3;
+    const int t = blockIdx.x * kTokens + threadIdx.x / L;
     const bool live = t < a.T;
     const int tc = live ? t : a.T - 1;
     const float* row = a.logits + static_cast<size_t>(tc) * a.E;
+    auto expert = [&](int j) { return (j >> 2) * (4 * L) + h * 4 + (j & 3); };
 
-    float x[V];
+    // v: what the choice goes by; -inf: off (NaN too: the comparison is false)
+    float v[V];
+    const bool counted = !a.token_mask || a.token_mask[tc] != 0;
+    auto load_row = [&]() {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        if constexpr (VEC) {
-            const f32x4 v = *reinterpret_cast<const f32x4*>(row + c * 16 + h * 4);
+        for (int c = 0; c < C; ++c) {
+            if constexpr (VEC) {
+                const f32x4 q = *reinterpret_cast<const f32x4*>(row + c * (4 * L) + h * 4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[c * 4 + i] = v[i];
-        } else {
+                for (int i = 0; i < 4; ++i) v[c * 4 + i] = q[i];
+            } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int e = c * 16 + h * 4 + i;
-                x[c * 4 + i] = e < a.E ? row[e] : -INFINITY;
+                for (int i = 0; i < 4; ++i) {
+                    const int e = expert(c * 4 + i);
+                    v[c * 4 + i] = e < a.E ? row[e] : -INFINITY;
+                }
             }
         }
-    }
-    const bool counted = !a.token_mask || a.token_mask[tc] != 0;
-    // off: -inf; NaN too (the comparison is false)
 #pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = (counted && x[j] > -INFINITY) ? x[j] : -INFINITY;
+        for (int j = 0; j < V; ++j) v[j] = (counted && v[j] > -INFINITY) ? v[j] : -INFINITY;
+    };
+    load_row();
 
-    // ---- softmax: the row's maximum and sum (in fp64 where keys take them)
+    // ---- softmax: the row's maximum, and the sum of fp32 exponentials in fp64.  With z = l -
+    // max, a term is off by 2^-23 (its ulp) and 2.5 |z| 2^-24 (z, log2 e and their product
+    // rounded); |z| is at most ln 256 on average under the softmax: the sum is within 2^-20.
+    constexpr float kLog2E = 1.44269504088896340736f;
     float top_x = 0.0f;
     double inv_sum = 1.0;
     const bool need_sum = !a.sigmoid && (SCORE || !a.normalise);
     if (need_sum) {
-        top_x = x[0];
+        top_x = v[0];
 #pragma unroll
-        for (int j = 1; j < V; ++j) top_x = fmaxf(top_x, x[j]);
-        top_x = fmaxf(top_x, dpp_swap_f32<kDppXor1>(top_x));
-        top_x = fmaxf(top_x, dpp_swap_f32<kDppXor2>(top_x));
+        for (int j = 1; j < V; ++j) top_x = fmaxf(top_x, v[j]);
+        over_lanes<L>([&](auto ctrl) { top_x = fmaxf(top_x, dpp_swap_f32<ctrl.value>(top_x)); });
         top_x = top_x > -INFINITY ? top_x : 0.0f;
         double sum = 0.0;
 #pragma unroll
         for (int j = 0; j < V; ++j)
-            sum += x[j] > -INFINITY ? exp64(static_cast<double>(x[j]) - static_cast<double>(top_x)) : 0.0;
-        sum += dpp_swap<kDppXor1>(sum);
-        sum += dpp_swap<kDppXor2>(sum);
+            sum += static_cast<double>(__builtin_amdgcn_exp2f((v[j] - top_x) * kLog2E));         // 2^-inf = 0
+        over_lanes<L>([&](auto ctrl) { sum += dpp_swap<ctrl.value>(sum); });
         inv_sum = sum > 0.0 ? 1.0 / sum : 0.0;
     }
-    auto score_of = [&](float l) {             // of an expert that is on
-        return a.sigmoid ? sigmoid64(l) : exp64(static_cast<double>(l) - static_cast<double>(top_x)) * inv_sum;
+    const float inv_sum32 = static_cast<float>(inv_sum);
+    if constexpr (SCORE) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float l = v[j];
+            float s = a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-l * kLog2E))
+                                : __builtin_amdgcn_exp2f((l - top_x) * kLog2E) * inv_sum32;
+            if (a.bias) s += a.bias[VEC || expert(j) < a.E ? expert(j) : 0];
+            v[j] = l > -INFINITY ? s : -INFINITY;
+        }
+    }
+
+    // ---- groups: experts of closed ones leave the choice (NaN)
+    bool unsure = false;
+    const float reach_of = a.sigmoid ? kUnsureSigmoid : kUnsureSoftmax;
+    // with scores: totals of two values, of magnitudes up to `size`, each unsure by itself
+    auto gap_unsure = [&](float lowest_open, float highest_closed, float size) {
+        return highest_closed > -INFINITY && lowest_open - highest_closed <= 2.0f * reach_of * (1.0f + size);
     };
-
-    // ---- keys
-    double keys[V];
+    if constexpr (GROUPS == 1) {
+        constexpr int G = C / CPG;
+        float total[G], size = 0.0f;
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+        for (int g = 0; g < G; ++g) {
+            float b1 = -INFINITY, b2 = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = c * 4 + i, e = c * 16 + h * 4 + i;
-            const bool on = x[j] > -INFINITY;
-            const uint32_t tie = 255u - static_cast<uint32_t>(e);
-            double key;
-            if constexpr (SCORE) {
-                double v = score_of(on ? x[j] : 0.0f);
-                if (a.bias) v += static_cast<double>(a.bias[VEC || e < a.E ? e : 0]);
-                const uint32_t hi = high_word(v), sign = static_cast<uint32_t>(static_cast<int32_t>(hi) >> 31);
-                key = words(hi, (low_word(v) & ~255u) | ((tie ^ sign) & 255u));
-            } else {
-                key = logit_key(x[j], tie);
+            for (int j = g * CPG * 4; j < (g + 1) * CPG * 4; ++j) {
+                b2 = fmaxf(b2, fminf(b1, v[j]));
+                b1 = fmaxf(b1, v[j]);
             }
-            key = on ? key : words(kOffHigh, ~tie);
-            keys[j] = (VEC || e < a.E) ? key : kNoKey;
+            over_lanes<L>([&](auto ctrl) {
+                const float p1 = dpp_swap_f32<ctrl.value>(b1), p2 = dpp_swap_f32<ctrl.value>(b2);
+                b2 = fmaxf(fminf(b1, p1), fmaxf(b2, p2));
+                b1 = fmaxf(b1, p1);
+            });
+            total[g] = a.group_top > 1 && b2 > -INFINITY ? b1 + b2 : b1;
+            size = b2 > -INFINITY ? fmaxf(size, fmaxf(fabsf(b1), fabsf(b2))) : b1 > -INFINITY ? fmaxf(size, fabsf(b1)) : size;
         }
-
-    // ---- groups: the experts of closed ones leave the choice
-    if constexpr (GROUPS != 0) {
-        // what a key stands for in its group's score
-        auto value_of = [&](double key) {
-            const uint32_t hi = high_word(key);
-            const double v = words(hi, SCORE ? low_word(key) & ~255u : 0u);
-            return hi == kOffHigh ? kNoKey : v;
-        };
+        uint32_t open = 0;
+        float lowest = INFINITY, highest = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            int ahead = 0;
+#pragma unroll
+            for (int o = 0; o < G; ++o)
+                if (o != g) ahead += (o < g ? total[o] >= total[g] : total[o] > total[g]) ? 1 : 0;
+            const bool is_open = ahead < a.open_groups;
+            open |= is_open ? 1u << g : 0u;
+            lowest = is_open ? fminf(lowest, total[g]) : lowest;
+            highest = is_open ? highest : fmaxf(highest, total[g]);
+        }
+        if (SCORE) {
+            unsure = gap_unsure(lowest, highest, size);
+            if (!a.bias) load_row();                   // within groups the choice goes by the logits
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = (open >> (j / (4 * CPG))) & 1u ? v[j] : NAN;
+    }
+    if constexpr (GROUPS == 2) {
+        // pitches are odd: a token's lanes, and the tokens, fall into different banks
+        constexpr int kPitch = L * V + 1;
+        __shared__ float value[kTokens * kPitch];
+        __shared__ float total[kTokens * (kMaxScoreGroups + 1)];
+        float* const mine = value + threadIdx.x / L * kPitch;
+        float* const sums = total + threadIdx.x / L * (kMaxScoreGroups + 1);
+#pragma unroll
+        for (int j = 0; j < V; ++j) mine[expert(j)] = v[j];
+        __syncthreads();
+        float size = 0.0f;
+        for (int g = h; g < a.groups; g += L) {
+            float b1 = -INFINITY, b2 = -INFINITY;
+            for (int i = 0; i < a.group_size; ++i) {
+                const float x = mine[g * a.group_size + i];
+                b2 = fmaxf(b2, fminf(b1, x));
+                b1 = fmaxf(b1, x);
+            }
+            sums[g] = a.group_top > 1 && b2 > -INFINITY ? b1 + b2 : b1;
+            size = b2 > -INFINITY ? fmaxf(size, fmaxf(fabsf(b1), fabsf(b2))) : b1 > -INFINITY ? fmaxf(size, fabsf(b1)) : size;
+        }
+        __syncthreads();
         uint64_t open = 0;
-        if constexpr (GROUPS == 1) {
-            constexpr int G = C / CPG;
-            double total[G];
+        float lowest = INFINITY, highest = -INFINITY;
+        for (int g = h; g < a.groups; g += L) {
+            const float s = sums[g];
+            int ahead = 0;
+            for (int o = 0; o < a.groups; ++o) ahead += (o < g ? sums[o] >= s : sums[o] > s) ? 1 : 0;
+            const bool is_open = ahead < a.open_groups;
+            open |= is_open ? 1ull << g : 0ull;
+            lowest = is_open ? fminf(lowest, s) : lowest;
+            highest = is_open ? highest : fmaxf(highest, s);
+        }
+        over_lanes<L>([&](auto ctrl) {
+            open |= dpp_swap_u64<ctrl.value>(open);
+            lowest = fminf(lowest, dpp_swap_f32<ctrl.value>(lowest));
+            highest = fmaxf(highest, dpp_swap_f32<ctrl.value>(highest));
+            size = fmaxf(size, dpp_swap_f32<ctrl.value>(size));
+        });
+        if (SCORE) {
+            unsure = gap_unsure(lowest, highest, size);
+            if (!a.bias) load_row();
+        }
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                double b1 = kNoKey, b2 = kNoKey;
-#pragma unroll
-                for (int j = g * CPG * 4; j < (g + 1) * CPG * 4; ++j) best_two(b1, b2, value_of(keys[j]));
-                auto join = [&](double p1, double p2) {
-                    b2 = __builtin_fmax(__builtin_fmin(b1, p1), __builtin_fmax(b2, p2));
-                    b1 = __builtin_fmax(b1, p1);
-                };
-                join(dpp_swap<kDppXor1>(b1), dpp_swap<kDppXor1>(b2));
-                join(dpp_swap<kDppXor2>(b1), dpp_swap<kDppXor2>(b2));
-                total[g] = group_total(b1, b2, a.group_top);
-            }
-            uint32_t bits = 0;
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                int ahead = 0;
-#pragma unroll
-                for (int o = 0; o < G; ++o)
-                    if (o != g) ahead += (o < g ? total[o] >= total[g] : total[o] > total[g]) ? 1 : 0;
-                bits |= ahead < a.open_groups ? 1u << g : 0u;
-            }
-            open = bits;
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    keys[c * 4 + i] = (bits >> (c / CPG)) & 1u ? keys[c * 4 + i] : kNoKey;
-        } else {
-            // 16 tokens a workgroup of one wave; pitches are odd, so a token's lanes and
-            // the tokens fall into different banks
-            constexpr int kPitch = 4 * V + 1;
-            __shared__ double value[16 * kPitch];
-            __shared__ double total[16 * 65];
-            double* mine = value + (threadIdx.x >> 2) * kPitch;
-            double* sums = total + (threadIdx.x >> 2) * 65;
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) mine[c * 16 + h * 4 + i] = value_of(keys[c * 4 + i]);
-            __syncthreads();
-            for (int g = h; g < a.groups; g += 4) {
-                double b1 = kNoKey, b2 = kNoKey;
-                for (int i = 0; i < a.group_size; ++i) best_two(b1, b2, mine[g * a.group_size + i]);
-                sums[g] = group_total(b1, b2, a.group_top);
-            }
-            __syncthreads();
-            for (int g = h; g < a.groups; g += 4) {
-                const double s = sums[g];
-                int ahead = 0;
-                for (int o = 0; o < a.groups; ++o) ahead += (o < g ? sums[o] >= s : sums[o] > s) ? 1 : 0;
-                open |= ahead < a.open_groups ? 1ull << g : 0ull;
-            }
-            open |= dpp_swap_u64<kDppXor1>(open);
-            open |= dpp_swap_u64<kDppXor2>(open);
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int e = c * 16 + h * 4 + i;
-                    const bool in = e < a.E && ((open >> small_quotient(e, a.group_size)) & 1ull);
-                    keys[c * 4 + i] = in ? keys[c * 4 + i] : kNoKey;
-                }
+        for (int j = 0; j < V; ++j) {
+            const int e = expert(j);
+            v[j] = e < a.E && ((open >> small_quotient(e, a.group_size)) & 1ull) ? v[j] : NAN;
         }
     }
 
-    // without a bias the choice within groups goes by the logits, which tell apart what
-    // scores of 64 bits may not (the row is read again: keeping it costs V registers)
-    const bool by_logit = !SCORE || (GROUPS != 0 && !a.bias);
-    if constexpr (SCORE && GROUPS != 0) {
-        if (!a.bias) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int e = (j / 4) * 16 + h * 4 + j % 4;
-                const float l = row[VEC || e < a.E ? e : 0];
-                const bool on = high_word(keys[j]) != kOffHigh && keys[j] > kNoKey;
-                keys[j] = on ? logit_key(l, 255u - static_cast<uint32_t>(e)) : keys[j];
-            }
-        }
-    }
-
-    // ---- the KP largest keys of the lane, then of the quad
+    // ---- the KP largest keys of the lane, then of the token's lanes
+    auto key_of = [&](int j) {
+        const uint32_t tie = 255u - static_cast<uint32_t>(expert(j));
+        double key = logit_key(v[j], tie);
+        key = v[j] > -INFINITY ? key : words(kOffHigh, ~tie);
+        return v[j] == v[j] && (VEC || expert(j) < a.E) ? key : kNoKey;
+    };
     double top[KP];
 #pragma unroll
-    for (int s = 0; s < KP; ++s) top[s] = s < V ? keys[s < V ? s : 0] : kNoKey;
+    for (int s = 0; s < KP; ++s) top[s] = s < V ? key_of(s < V ? s : 0) : kNoKey;
     sort_desc<KP>(top);
 #pragma unroll
     for (int b0 = KP; b0 < V; b0 += KP) {
         double blk[KP];
 #pragma unroll
-        for (int s = 0; s < KP; ++s) blk[s] = keys[b0 + s];
+        for (int s = 0; s < KP; ++s) blk[s] = key_of(b0 + s);
         sort_desc<KP>(blk);
         merge_top<KP>(top, blk);
     }
-    merge_with_partner<kDppXor1, KP>(top);
-    merge_with_partner<kDppXor2, KP>(top);
+    over_lanes<L>([&](auto ctrl) { merge_with_partner<ctrl.value, KP>(top); });
 
-    // ---- the lane's slots h + 4 u: expert, device, score
+    // ---- is the order sure?  Neighbours among the chosen lie far enough apart, and so does
+    // what comes next: no more than k values within reach of the last one
+    if constexpr (SCORE) {
+        if (GROUPS == 0 || a.bias) {
+            float last = -INFINITY;
+#pragma unroll
+            for (int s = 0; s < KP; ++s) {
+                const bool on = high_word(top[s]) != kOffHigh && top[s] > kNoKey;
+                const float x = key_logit(top[s]);
+                if (s + 1 < KP) {
+                    const bool next_on = high_word(top[s + 1 < KP ? s + 1 : s]) != kOffHigh && top[s + 1 < KP ? s + 1 : s] > kNoKey;
+                    unsure = unsure || (s + 1 < a.k && on && next_on && x - key_logit(top[s + 1 < KP ? s + 1 : s]) <= reach_of * (1.0f + fabsf(x)));
+                }
+                last = s + 1 == a.k && on ? x - reach_of * (1.0f + fabsf(x)) : last;
+            }
+            int reach = 0;
+#pragma unroll
+            for (int j = 0; j < V; ++j) reach += v[j] >= last ? 1 : 0;
+            over_lanes<L>([&](auto ctrl) { reach += dpp_swap_i32<ctrl.value>(reach); });
+            unsure = unsure || (last > -INFINITY && reach > a.k);
+        }
+    }
+
+    // ---- the lane's slots hq + 4 u
     bool has[NS], on[NS];
-    int my_e[NS], my_dev[NS];
-    double q[NS];
-    const float lead = key_logit(top[0]);                     // logit keys: the largest chosen logit
+    int my_e[NS];
 #pragma unroll
     for (int u = 0; u < NS; ++u) {
         double m = top[4 * u];
 #pragma unroll
-        for (int s = 1; s < kQuadLanes && 4 * u + s < KP; ++s) m = (h == s) ? top[4 * u + s] : m;
-        has[u] = h + 4 * u < a.k;
-        const int e = key_expert(m);
-        my_e[u] = e < a.E ? e : a.E - 1;
-        on[u] = has[u] && high_word(m) != kOffHigh;
-        my_dev[u] = has[u] ? a.expert_rank[my_e[u]] & 63 : -1;
-        double s = 0.0;
-        if (on[u]) {
-            const float l = by_logit ? key_logit(m) : row[my_e[u]];
-            // softmax that is normalised over the chosen: relative to the largest of them
-            s = a.sigmoid || need_sum ? score_of(l) : exp64(static_cast<double>(l) - static_cast<double>(lead));
+        for (int s = 1; s < kQuadLanes && 4 * u + s < KP; ++s) m = (hq == s) ? top[4 * u + s] : m;
+        has[u] = hq + 4 * u < a.k;
+        my_e[u] = key_expert(m);
+        on[u] = high_word(m) != kOffHigh;
+    }
+    if constexpr (SCORE) {
+        ExactSpace& space = exact[threadIdx.x >> 6];
+        uint64_t left = __ballot(unsure && live && h == 0);
+        while (left) {                                 // wave-uniform
+            const int l = __ffsll(static_cast<unsigned long long>(left)) - 1;
+            left &= left - 1;
+            exact_choice(a, __builtin_amdgcn_readlane(t, l), space);
+            const bool here = ((threadIdx.x & 63) ^ h) == l;
+#pragma unroll
+            for (int u = 0; u < NS; ++u) {
+                const int c = space.chosen[hq + 4 * u];
+                my_e[u] = here ? c & 0xFFFF : my_e[u];
+                on[u] = here ? (c >> 16) != 0 : on[u];
+            }
+            __builtin_amdgcn_wave_barrier();
         }
-        q[u] = s;
+    }
+
+    // ---- their devices and scores
+    int my_dev[NS];
+    double q[NS];
+    float my_l[NS];
+#pragma unroll
+    for (int u = 0; u < NS; ++u) {
+        my_e[u] = has[u] && my_e[u] < a.E ? my_e[u] : a.E - 1;
+        on[u] = on[u] && has[u];
+        my_dev[u] = has[u] ? a.expert_rank[my_e[u]] & 63 : -1;
+        my_l[u] = row[my_e[u]];
+    }
+    float lead = -INFINITY;                            // normalised over the chosen: relative to the largest of them
+#pragma unroll
+    for (int u = 0; u < NS; ++u) lead = on[u] ? fmaxf(lead, my_l[u]) : lead;
+    lead = fmaxf(lead, dpp_swap_f32<kDppXor1>(lead));
+    lead = fmaxf(lead, dpp_swap_f32<kDppXor2>(lead));
+    const float base = a.normalise ? lead : top_x;
+#pragma unroll
+    for (int u = 0; u < NS; ++u) {
+        const double s = a.sigmoid ? sigmoid64(my_l[u])
+                                   : exp64(static_cast<double>(my_l[u]) - static_cast<double>(base)) *
+                                         (a.normalise ? 1.0 : inv_sum);
+        q[u] = on[u] ? s : 0.0;
     }
     double qs[KP];
     int devs[KP];
@@ -375,7 +536,7 @@ __global__ __launch_bounds__(GROUPS == 2 ? 64 : 256) void route_scores_kernel(co
             for (int s = 0; s < KP; ++s) {
                 const bool same = on[u] && devs[s] == my_dev[u];
                 sh += same ? qs[s] : 0.0;
-                repeat = repeat || (same && s < h + 4 * u);
+                repeat = repeat || (same && s < hq + 4 * u);
             }
             share[u] = sh * inv;
             first[u] = on[u] && !repeat;
@@ -413,11 +574,11 @@ __global__ __launch_bounds__(GROUPS == 2 ? 64 : 256) void route_scores_kernel(co
     for (int s = 0; s < KP; ++s) kept_sum += devs[s] >= 0 && ((mask >> (devs[s] & 63)) & 1ull) ? qs[s] : 0.0;
     const double factor = static_cast<double>(a.scale) *
                           (a.normalise ? (kept_sum > 0.0 ? 1.0 / kept_sum : 0.0) : 1.0);
-    if (!live) return;
+    if (!live || h >= 4) return;
 #pragma unroll
     for (int u = 0; u < NS; ++u)
         if (has[u]) {
-            const size_t at = static_cast<size_t>(t) * a.k + h + 4 * u;
+            const size_t at = static_cast<size_t>(t) * a.k + hq + 4 * u;
             a.idx[at] = my_e[u];
             a.w[at] = kept[u] ? static_cast<float>(q[u] * factor) : 0.0f;
             a.keep[at] = kept[u] ? 1 : 0;
@@ -425,43 +586,42 @@ __global__ __launch_bounds__(GROUPS == 2 ? 64 : 256) void route_scores_kernel(co
     if (h == 0) a.mask[t] = mask;
 }
 
-template <int V, int KP, bool SCORE, bool VEC, int GROUPS, int CPG>
+template <int L, int V, int KP, bool SCORE, bool VEC, int GROUPS, int CPG = 1>
 void launch(const ScoreArgs& a, hipStream_t st) {
-    const int tokens = GROUPS == 2 ? 16 : 64;
-    route_scores_kernel<V, KP, SCORE, VEC, GROUPS, CPG>
-        <<<(a.T + tokens - 1) / tokens, GROUPS == 2 ? 64 : 256, 0, st>>>(a);
+    constexpr int tokens = 256 / L;
+    route_scores_kernel<L, V, KP, SCORE, VEC, GROUPS, CPG><<<(a.T + tokens - 1) / tokens, 256, 0, st>>>(a);
 }
 
-template <int V, int KP, bool SCORE>
+template <int L, int V, int KP, bool SCORE>
 void launch_groups(const ScoreArgs& a, bool vec, hipStream_t st) {
     if (a.open_groups >= a.groups) {
-        if (vec) launch<V, KP, SCORE, true, 0, 1>(a, st);
-        else launch<V, KP, SCORE, false, 0, 1>(a, st);
+        if (vec) launch<L, V, KP, SCORE, true, 0>(a, st);
+        else launch<L, V, KP, SCORE, false, 0>(a, st);
         return;
     }
-    if constexpr (V >= 16) {
-        if (vec && a.group_size % 16 == 0 && a.groups > 1) {
+    if constexpr (L == 4 && V >= 16) {
+        if (vec && a.group_size % 16 == 0) {
             const int cpg = a.group_size / 16;
-            if (cpg == 1) return launch<V, KP, SCORE, true, 1, 1>(a, st);
-            if constexpr (V >= 16) if (cpg == 2) return launch<V, KP, SCORE, true, 1, 2>(a, st);
-            if constexpr (V >= 32) if (cpg == 4) return launch<V, KP, SCORE, true, 1, 4>(a, st);
-            if constexpr (V >= 64) if (cpg == 8) return launch<V, KP, SCORE, true, 1, 8>(a, st);
+            if (cpg == 1) return launch<L, V, KP, SCORE, true, 1, 1>(a, st);
+            if constexpr (V >= 16) if (cpg == 2) return launch<L, V, KP, SCORE, true, 1, 2>(a, st);
+            if constexpr (V >= 32) if (cpg == 4) return launch<L, V, KP, SCORE, true, 1, 4>(a, st);
+            if constexpr (V >= 64) if (cpg == 8) return launch<L, V, KP, SCORE, true, 1, 8>(a, st);
         }
     }
-    launch<V, KP, SCORE, false, 2, 1>(a, st);
+    launch<L, V, KP, SCORE, false, 2>(a, st);
 }
 
-template <int V>
+template <int L, int V>
 void launch_keys(const ScoreArgs& a, bool vec, hipStream_t st) {
     // logits order experts and groups alike where nothing is added to scores
     const bool grouped = a.open_groups < a.groups;
     const bool score = a.bias || (grouped && a.group_top > 1 && a.group_size > 1);
     if (a.k <= 4) {
-        if (score) launch_groups<V, 4, true>(a, vec, st);
-        else launch_groups<V, 4, false>(a, vec, st);
+        if (score) launch_groups<L, V, 4, true>(a, vec, st);
+        else launch_groups<L, V, 4, false>(a, vec, st);
     } else {
-        if (score) launch_groups<V, 8, true>(a, vec, st);
-        else launch_groups<V, 8, false>(a, vec, st);
+        if (score) launch_groups<L, V, 8, true>(a, vec, st);
+        else launch_groups<L, V, 8, false>(a, vec, st);
     }
 }
 
@@ -601,15 +761,26 @@ cap_status route_scores_launch(const cap_topology* tp, const float* logits, cons
     a.scale = opt->scale;
     a.p = p;
     a.inter_node_cost = tp->inter_node_cost;
+    // sixteen lanes a token where four leave compute units without a wave
+    const bool few = a.T <= kFewTokens && a.E > 16;
+    const int lanes = few ? 16 : 4;
     int V = 4;
-    while (kQuadLanes * V < a.E) V *= 2;
-    const bool vec = a.E == kQuadLanes * V && (reinterpret_cast<uintptr_t>(logits) & 15) == 0;
-    switch (V) {
-        case 4: launch_keys<4>(a, vec, st); break;
-        case 8: launch_keys<8>(a, vec, st); break;
-        case 16: launch_keys<16>(a, vec, st); break;
-        case 32: launch_keys<32>(a, vec, st); break;
-        default: launch_keys<64>(a, vec, st); break;
+    while (lanes * V < a.E) V *= 2;
+    const bool vec = a.E == lanes * V && (reinterpret_cast<uintptr_t>(logits) & 15) == 0;
+    if (few) {
+        switch (V) {
+            case 4: launch_keys<16, 4>(a, vec, st); break;
+            case 8: launch_keys<16, 8>(a, vec, st); break;
+            default: launch_keys<16, 16>(a, vec, st); break;
+        }
+    } else {
+        switch (V) {
+            case 4: launch_keys<4, 4>(a, vec, st); break;
+            case 8: launch_keys<4, 8>(a, vec, st); break;
+            case 16: launch_keys<4, 16>(a, vec, st); break;
+            case 32: launch_keys<4, 32>(a, vec, st); break;
+            default: launch_keys<4, 64>(a, vec, st); break;
+        }
     }
     CAP_LAUNCH_CHECK();
     return CAP_OK;
