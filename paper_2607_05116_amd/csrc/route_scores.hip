@@ -26,7 +26,11 @@ namespace cap {
 namespace {
 
 constexpr int kQuadLanes = 4;
-constexpr uint32_t kOffHigh = 0xFFEFFFFFu;  // high word of an off expert's key: about the lowest double
+// High words of keys: that of an expert that is off is -inf's in fp32 (a finite double, as its
+// exponent has three bits more, below those of all finite logits), that of one of a closed
+// group a negative NaN's, below it.
+constexpr uint32_t kOffHigh = 0xFF800000u, kClosedHigh = 0xFFC00000u;
+__device__ __forceinline__ bool key_is_on(uint32_t high) { return high < kOffHigh; }
 
 struct ScoreArgs {
     const float* logits;
@@ -105,9 +109,9 @@ __device__ __forceinline__ uint32_t low_word(double v) {
     return static_cast<uint32_t>(static_cast<uint64_t>(__double_as_longlong(v)));
 }
 
-// Key of a logit (-0 as +0).
-__device__ __forceinline__ double logit_key(float l, uint32_t tie) {
-    const uint32_t hi = __float_as_uint(l + 0.0f);
+// Key of a value that is not -0.
+__device__ __forceinline__ double value_key(float v, uint32_t tie) {
+    const uint32_t hi = __float_as_uint(v);
     return words(hi, tie ^ static_cast<uint32_t>(static_cast<int32_t>(hi) >> 31));
 }
 
@@ -151,30 +155,48 @@ struct ExactSpace {
     int chosen[kMaxK];
 };
 
+// Joins over a wave: DPP within rows of 16 lanes, then the four rows' first lanes.
+__device__ __forceinline__ double lane_f64(double v, int l) {
+    const long long b = __double_as_longlong(v);
+    return words(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(b >> 32), l)),
+                 static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(b), l)));
+}
+template <typename F>
+__device__ __forceinline__ double over_wave(double v, F&& join) {
+    v = join(v, dpp_swap<kDppXor1>(v));
+    v = join(v, dpp_swap<kDppXor2>(v));
+    v = join(v, dpp_swap<kDppHalfMirror>(v));
+    v = join(v, dpp_swap<0x140>(v));                   // row_mirror
+    return join(join(lane_f64(v, 0), lane_f64(v, 16)), join(lane_f64(v, 32), lane_f64(v, 48)));
+}
+
 // The choice of one token by the whole wave, on fp64 scores: for the few tokens that fp32
 // leaves unsure, and for ties.  Leaves expert | on << 16 of each slot in space.chosen.
 __device__ __forceinline__ void exact_choice(const ScoreArgs& a, int t, ExactSpace& space) {
     const int lane = threadIdx.x & 63;
     const float* row = a.logits + static_cast<size_t>(t) * a.E;
     const bool counted = !a.token_mask || a.token_mask[t] != 0;
-    float x[4];
+    float x[4], b[4];
     bool on[4];
-    float top_x = -INFINITY;
+    double top_x = kNoKey;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int e = 4 * lane + i;
-        x[i] = e < a.E ? row[e] : -INFINITY;
-        on[i] = counted && x[i] > -INFINITY;
-        top_x = on[i] ? fmaxf(top_x, x[i]) : top_x;
+        const int e = 4 * lane + i < a.E ? 4 * lane + i : a.E - 1;
+        x[i] = row[e];
+        b[i] = a.bias ? a.bias[e] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        on[i] = 4 * lane + i < a.E && counted && x[i] > -INFINITY;
+        top_x = on[i] ? __builtin_fmax(top_x, static_cast<double>(x[i])) : top_x;
     }
     double inv_sum = 1.0;
     if (!a.sigmoid) {
-        for (int d = 1; d < 64; d *= 2) top_x = fmaxf(top_x, __shfl_xor(top_x, d));
+        top_x = over_wave(top_x, [](double p, double q) { return __builtin_fmax(p, q); });
         double sum = 0.0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            sum += on[i] ? exp64(static_cast<double>(x[i]) - static_cast<double>(top_x)) : 0.0;
-        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+        for (int i = 0; i < 4; ++i) sum += on[i] ? exp64(static_cast<double>(x[i]) - top_x) : 0.0;
+        sum = over_wave(sum, [](double p, double q) { return p + q; });
         inv_sum = sum > 0.0 ? 1.0 / sum : 0.0;
     }
     double key[4];
@@ -183,24 +205,25 @@ __device__ __forceinline__ void exact_choice(const ScoreArgs& a, int t, ExactSpa
         const int e = 4 * lane + i;
         double v = 0.0;
         if (on[i])
-            v = a.sigmoid ? sigmoid64(x[i]) : exp64(static_cast<double>(x[i]) - static_cast<double>(top_x)) * inv_sum;
-        if (a.bias && e < a.E) v += static_cast<double>(a.bias[e]);
+            v = a.sigmoid ? sigmoid64(x[i]) : exp64(static_cast<double>(x[i]) - top_x) * inv_sum;
+        v += static_cast<double>(b[i]);
         space.value[4 * lane + i] = on[i] ? words(high_word(v), low_word(v) & ~255u) : kNoKey;
         const uint32_t tie = 255u - static_cast<uint32_t>(e);
         const uint32_t hi = high_word(v), sign = static_cast<uint32_t>(static_cast<int32_t>(hi) >> 31);
         // (without a bias, the choice within groups goes by the logits)
-        key[i] = !on[i] ? words(kOffHigh, ~tie) : a.bias ? words(hi, (low_word(v) & ~255u) | ((tie ^ sign) & 255u)) : logit_key(x[i], tie);
+        key[i] = !on[i] ? words(kOffHigh, ~tie) : a.bias ? words(hi, (low_word(v) & ~255u) | ((tie ^ sign) & 255u)) : value_key(x[i] + 0.0f, tie);
         key[i] = e < a.E ? key[i] : kNoKey;
     }
     if (a.open_groups < a.groups) {
         __builtin_amdgcn_wave_barrier();               // one wave: its LDS accesses stay in order
         double b1 = kNoKey, b2 = kNoKey;
         if (lane < a.groups)
+#pragma unroll 8
             for (int i = 0; i < a.group_size; ++i) best_two(b1, b2, space.value[lane * a.group_size + i]);
         const double total = group_total(b1, b2, a.group_top);
         int ahead = 0;
         for (int o = 0; o < a.groups; ++o) {
-            const double other = __shfl(total, o);
+            const double other = lane_f64(total, o);
             ahead += (o < lane ? other >= total : other > total) ? 1 : 0;
         }
         const uint64_t open = __ballot(lane < a.groups && ahead < a.open_groups);
@@ -211,8 +234,8 @@ __device__ __forceinline__ void exact_choice(const ScoreArgs& a, int t, ExactSpa
         }
     }
     for (int s = 0; s < a.k; ++s) {
-        double best = __builtin_fmax(__builtin_fmax(key[0], key[1]), __builtin_fmax(key[2], key[3]));
-        for (int d = 1; d < 64; d *= 2) best = __builtin_fmax(best, __shfl_xor(best, d));
+        const double best = over_wave(__builtin_fmax(__builtin_fmax(key[0], key[1]), __builtin_fmax(key[2], key[3])),
+                                      [](double p, double q) { return __builtin_fmax(p, q); });
 #pragma unroll
         for (int i = 0; i < 4; ++i) key[i] = key[i] == best ? kNoKey : key[i];     // keys are distinct
         if (lane == 0) space.chosen[s] = key_expert(best) | (high_word(best) != kOffHigh ? 1 << 16 : 0);
@@ -255,7 +278,7 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
     const float* row = a.logits + static_cast<size_t>(tc) * a.E;
     auto expert = [&](int j) { return (j >> 2) * (4 * L) + h * 4 + (j & 3); };
 
-    // v: what the choice goes by; -inf: off (NaN too: the comparison is false)
+    // v: what the choice goes by, never -0; -inf: off (NaN too: the comparison is false)
     float v[V];
     const bool counted = !a.token_mask || a.token_mask[tc] != 0;
     auto load_row = [&]() {
@@ -274,7 +297,7 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
             }
         }
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = (counted && v[j] > -INFINITY) ? v[j] : -INFINITY;
+        for (int j = 0; j < V; ++j) v[j] = counted & (v[j] > -INFINITY) ? v[j] + 0.0f : -INFINITY;
     };
     load_row();
 
@@ -300,17 +323,28 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
     }
     const float inv_sum32 = static_cast<float>(inv_sum);
     if constexpr (SCORE) {
+        // (each branch for all values at once: one around every value would keep the loads apart)
+        if (a.sigmoid) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float l = v[j];
-            float s = a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-l * kLog2E))
-                                : __builtin_amdgcn_exp2f((l - top_x) * kLog2E) * inv_sum32;
-            if (a.bias) s += a.bias[VEC || expert(j) < a.E ? expert(j) : 0];
-            v[j] = l > -INFINITY ? s : -INFINITY;
+            for (int j = 0; j < V; ++j) {
+                const float p = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-v[j] * kLog2E));
+                v[j] = v[j] > -INFINITY ? p : -INFINITY;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float p = __builtin_amdgcn_exp2f((v[j] - top_x) * kLog2E) * inv_sum32;
+                v[j] = v[j] > -INFINITY ? p : -INFINITY;
+            }
+        }
+        if (a.bias) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] += a.bias[VEC || expert(j) < a.E ? expert(j) : 0];       // -inf stays
         }
     }
 
-    // ---- groups: experts of closed ones leave the choice (NaN)
+    // ---- groups: experts of closed ones leave the choice
+    const float closed = __uint_as_float(kClosedHigh);     // a NaN: no comparison holds for it
     bool unsure = false;
     const float reach_of = a.sigmoid ? kUnsureSigmoid : kUnsureSoftmax;
     // with scores: totals of two values, of magnitudes up to `size`, each unsure by itself
@@ -333,8 +367,9 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
                 b2 = fmaxf(fminf(b1, p1), fmaxf(b2, p2));
                 b1 = fmaxf(b1, p1);
             });
-            total[g] = a.group_top > 1 && b2 > -INFINITY ? b1 + b2 : b1;
-            size = b2 > -INFINITY ? fmaxf(size, fmaxf(fabsf(b1), fabsf(b2))) : b1 > -INFINITY ? fmaxf(size, fabsf(b1)) : size;
+            total[g] = (a.group_top > 1) & (b2 > -INFINITY) ? b1 + b2 : b1;
+            size = fmaxf(size, b1 > -INFINITY ? fabsf(b1) : 0.0f);
+            size = fmaxf(size, b2 > -INFINITY ? fabsf(b2) : 0.0f);
         }
         uint32_t open = 0;
         float lowest = INFINITY, highest = -INFINITY;
@@ -354,7 +389,7 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
             if (!a.bias) load_row();                   // within groups the choice goes by the logits
         }
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = (open >> (j / (4 * CPG))) & 1u ? v[j] : NAN;
+        for (int j = 0; j < V; ++j) v[j] = (open >> (j / (4 * CPG))) & 1u ? v[j] : closed;
     }
     if constexpr (GROUPS == 2) {
         // pitches are odd: a token's lanes, and the tokens, fall into different banks
@@ -374,8 +409,9 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
                 b2 = fmaxf(b2, fminf(b1, x));
                 b1 = fmaxf(b1, x);
             }
-            sums[g] = a.group_top > 1 && b2 > -INFINITY ? b1 + b2 : b1;
-            size = b2 > -INFINITY ? fmaxf(size, fmaxf(fabsf(b1), fabsf(b2))) : b1 > -INFINITY ? fmaxf(size, fabsf(b1)) : size;
+            sums[g] = (a.group_top > 1) & (b2 > -INFINITY) ? b1 + b2 : b1;
+            size = fmaxf(size, b1 > -INFINITY ? fabsf(b1) : 0.0f);
+            size = fmaxf(size, b2 > -INFINITY ? fabsf(b2) : 0.0f);
         }
         __syncthreads();
         uint64_t open = 0;
@@ -402,16 +438,14 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int e = expert(j);
-            v[j] = e < a.E && ((open >> small_quotient(e, a.group_size)) & 1ull) ? v[j] : NAN;
+            v[j] = e < a.E && ((open >> small_quotient(e, a.group_size)) & 1ull) ? v[j] : closed;
         }
     }
 
     // ---- the KP largest keys of the lane, then of the token's lanes
     auto key_of = [&](int j) {
-        const uint32_t tie = 255u - static_cast<uint32_t>(expert(j));
-        double key = logit_key(v[j], tie);
-        key = v[j] > -INFINITY ? key : words(kOffHigh, ~tie);
-        return v[j] == v[j] && (VEC || expert(j) < a.E) ? key : kNoKey;
+        const double key = value_key(v[j], 255u - static_cast<uint32_t>(expert(j)));
+        return VEC || expert(j) < a.E ? key : kNoKey;
     };
     double top[KP];
 #pragma unroll
@@ -434,19 +468,19 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
             float last = -INFINITY;
 #pragma unroll
             for (int s = 0; s < KP; ++s) {
-                const bool on = high_word(top[s]) != kOffHigh && top[s] > kNoKey;
+                const bool on = key_is_on(high_word(top[s]));
                 const float x = key_logit(top[s]);
                 if (s + 1 < KP) {
-                    const bool next_on = high_word(top[s + 1 < KP ? s + 1 : s]) != kOffHigh && top[s + 1 < KP ? s + 1 : s] > kNoKey;
-                    unsure = unsure || (s + 1 < a.k && on && next_on && x - key_logit(top[s + 1 < KP ? s + 1 : s]) <= reach_of * (1.0f + fabsf(x)));
+                    const bool next_on = key_is_on(high_word(top[s + 1 < KP ? s + 1 : s]));
+                    unsure |= (s + 1 < a.k) & on & next_on & (x - key_logit(top[s + 1 < KP ? s + 1 : s]) <= reach_of * (1.0f + fabsf(x)));
                 }
-                last = s + 1 == a.k && on ? x - reach_of * (1.0f + fabsf(x)) : last;
+                last = (s + 1 == a.k) & on ? x - reach_of * (1.0f + fabsf(x)) : last;
             }
             int reach = 0;
 #pragma unroll
             for (int j = 0; j < V; ++j) reach += v[j] >= last ? 1 : 0;
             over_lanes<L>([&](auto ctrl) { reach += dpp_swap_i32<ctrl.value>(reach); });
-            unsure = unsure || (last > -INFINITY && reach > a.k);
+            unsure |= (last > -INFINITY) & (reach > a.k);
         }
     }
 
@@ -460,7 +494,7 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
         for (int s = 1; s < kQuadLanes && 4 * u + s < KP; ++s) m = (hq == s) ? top[4 * u + s] : m;
         has[u] = hq + 4 * u < a.k;
         my_e[u] = key_expert(m);
-        on[u] = high_word(m) != kOffHigh;
+        on[u] = key_is_on(high_word(m));
     }
     if constexpr (SCORE) {
         ExactSpace& space = exact[threadIdx.x >> 6];
