@@ -630,7 +630,7 @@ cap_status cap_muon_update(cap_dtype dtype, int32_t batch, int32_t rows, int32_t
  *                 its best two (bias included).
  *   normalise     != 0: the gates of a token's kept slots sum to `scale`.
  *   scale         finite, > 0.
- *   bias[E]       (nullable) fp32, finite: added to scores for the choice of groups
+ *   bias[E]       (nullable) fp32, at most 1e30 in size: added to scores for the choice of groups
  *                 and experts only, never to gates.
  *   token_mask[T] (nullable) 0 for padding tokens, which keep no slot.
  */
@@ -649,8 +649,9 @@ typedef struct {
  * Top-k routing by scores, gates and communication-aware pruning (Eq. 1; Sec. VI,
  * Eq. 6 and its greedy), for routers that score experts each by itself or over all,
  * balance them by a bias and choose among groups.
- *   logits[T][E]  fp32.  An expert whose logit is -inf or NaN is off, and so is every
- *                 expert of a masked token; +inf is a precondition violation.
+ *   logits[T][E]  fp32.  An expert whose logit is not finite is off, and so is every
+ *                 expert of a masked token (finite logits are taken to be above the
+ *                 lowest of them, -3.4028235e38).
  * With s_e the score (1 / (1 + e^-l), or the softmax over the experts that are on) and
  * b_e the bias (0 without one):
  *   1. the topk_groups groups with the largest score, ties by lower index; experts

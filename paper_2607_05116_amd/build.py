@@ -40,6 +40,7 @@ FILE_FLAGS = {
     "route_prune.hip": ["-fno-honor-nans"],
     "router_route.hip": ["-fno-honor-nans"],
     "front_end.hip": ["-fno-honor-nans"],
+    "route_scores.hip": ["-fno-honor-nans"],     # asks the bits of a logit whether it is finite
 }
 
 

@@ -1,6 +1,7 @@
 // Routing by scores: sigmoid or softmax over a token's experts, a bias for balance,
 // groups of experts, top-k, gates, and the communication-aware pruning of Eq. 6
-// (Sec. VI) on the gates' shares; and the gradient of the logits through the gates.
+// (Sec. VI) on the gates' shares.  (Built without NaN semantics: whether a logit is finite
+// is asked of its bits.)
 //
 // Decisions (groups, experts, kept devices) are taken on values in 64 bits, so that
 // they are those of the real numbers for all but values within about 2^-43 of each
@@ -11,9 +12,9 @@
 // goes by the logits (the high word), and so do groups by their best expert; else the
 // key is the biased score in fp64, whose low 8 bits hold the expert
 // (255 - e, or e below zero, so that the larger double is the lower expert among
-// equal scores): 44 bits of the score are left.  An expert that is off (logit -inf
-// or NaN, or a masked token) has a key below all scores, one of a closed group
-// -infinity.
+// equal scores): 44 bits of the score are left.  An expert that is off (its logit is
+// not finite, or its token masked) has a key below all scores, one of a closed group
+// a key below that.
 #pragma clang fp contract(off)
 
 #include <math.h>
@@ -26,11 +27,14 @@ namespace cap {
 namespace {
 
 constexpr int kQuadLanes = 4;
-// High words of keys: that of an expert that is off is -inf's in fp32 (a finite double, as its
-// exponent has three bits more, below those of all finite logits), that of one of a closed
-// group a negative NaN's, below it.
-constexpr uint32_t kOffHigh = 0xFF800000u, kClosedHigh = 0xFFC00000u;
+// Values in the place of logits or scores: of an expert that is off (the lowest finite float:
+// the operator takes finite logits to lie above it), and of one of a closed group (-inf).  As
+// high words of keys both are finite doubles, whose exponent has three bits more, below all others.
+constexpr uint32_t kInfBits = 0x7F800000u;
+constexpr float kOff = -3.402823466e38f;
+constexpr uint32_t kOffHigh = 0xFF7FFFFFu, kClosedHigh = 0xFF800000u;
 __device__ __forceinline__ bool key_is_on(uint32_t high) { return high < kOffHigh; }
+__device__ __forceinline__ bool finite_bits(float v) { return (__float_as_uint(v) & kInfBits) != kInfBits; }
 
 struct ScoreArgs {
     const float* logits;
@@ -125,11 +129,10 @@ __device__ __forceinline__ double group_total(double a, double b, int top) {
     return top > 1 && b > kNoKey ? a + b : a;
 }
 
-// Tokens up to which sixteen lanes take one.
-#ifndef FEWT
-#define FEWT 8192
-#endif
-constexpr int kFewTokens = FEWT;
+// Tokens up to which eight lanes take one: more of them fill the chip, at the price of one join
+// more (tokens of 256 experts in 8 groups: 32 of them 8.0 us with eight lanes, 9.8 with four and
+// 10.1 with sixteen; 8,192 12.5, 14.2 and 17.4; 16,384 15.5, 14.8 and 24).
+constexpr int kTokens8 = 12288;
 
 // Slots of the routing: s = 0 .. N - 1 as a compile-time loop.
 template <int N, int I = 0, typename F>
@@ -187,7 +190,7 @@ __device__ __forceinline__ void exact_choice(const ScoreArgs& a, int t, ExactSpa
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        on[i] = 4 * lane + i < a.E && counted && x[i] > -INFINITY;
+        on[i] = 4 * lane + i < a.E && counted && finite_bits(x[i]) && x[i] > kOff;
         top_x = on[i] ? __builtin_fmax(top_x, static_cast<double>(x[i])) : top_x;
     }
     double inv_sum = 1.0;
@@ -244,25 +247,22 @@ __device__ __forceinline__ void exact_choice(const ScoreArgs& a, int t, ExactSpa
 }
 
 // ------------------------------------------------------------------ routing
-// Joins over the L lanes of a token (4: a quad; 16: a DPP row).
+// Joins over the L lanes of a token (4 or 8).
 template <int L, typename F>
 __device__ __forceinline__ void over_lanes(F&& step) {
     step(std::integral_constant<int, kDppXor1>{});
     step(std::integral_constant<int, kDppXor2>{});
-    if constexpr (L == 16) {
-        step(std::integral_constant<int, kDppHalfMirror>{});
-        step(std::integral_constant<int, 0x140>{});    // row_mirror
-    }
+    if constexpr (L == 8) step(std::integral_constant<int, kDppHalfMirror>{});
 }
 template <int CTRL>
 __device__ __forceinline__ int dpp_swap_i32(int v) { return __builtin_amdgcn_mov_dpp(v, CTRL, 0xF, 0xF, true); }
 
 // L lanes per token; lane h holds experts c * 4 L + h * 4 + [0, 4), c < V / 4; the lanes h of
-// a quad own slots h and h + 4 (of 16 lanes, all quads work them out, and the first writes).
+// a quad own slots h and h + 4 (of 8 lanes, both quads work them out, and the first writes).
 //   SCORE   the choice goes by biased scores, first in fp32; tokens whose order that leaves
 //           unsure (about one of 2000) are chosen by exact_choice.  Else it goes by logits.
-//   GROUPS  0: one group (or all of them open); 1: groups of 16 * CPG experts, which are whole
-//           values of c (L = 4); 2: any, through LDS
+//   GROUPS  0: one group (or all of them open); 1: groups of 4 L CPG experts, which are whole
+//           values of c; 2: any, through LDS
 // What bounds it: instruction issue, most of it the selection network.  All scores in fp64
 // took 35.8 us for 32,768 tokens of 256 experts (one wave a SIMD, for the registers of 64 keys
 // a lane): keys are formed block by block now, and fp64 is left to the chosen slots.
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
     const float* row = a.logits + static_cast<size_t>(tc) * a.E;
     auto expert = [&](int j) { return (j >> 2) * (4 * L) + h * 4 + (j & 3); };
 
-    // v: what the choice goes by, never -0; -inf: off (NaN too: the comparison is false)
+    // v: what the choice goes by, never -0
     float v[V];
     const bool counted = !a.token_mask || a.token_mask[tc] != 0;
     auto load_row = [&]() {
@@ -292,12 +292,12 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int e = expert(c * 4 + i);
-                    v[c * 4 + i] = e < a.E ? row[e] : -INFINITY;
+                    v[c * 4 + i] = e < a.E ? row[e] : kOff;
                 }
             }
         }
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = counted & (v[j] > -INFINITY) ? v[j] + 0.0f : -INFINITY;
+        for (int j = 0; j < V; ++j) v[j] = counted & finite_bits(v[j]) ? v[j] + 0.0f : kOff;
     };
     load_row();
 
@@ -313,11 +313,11 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
 #pragma unroll
         for (int j = 1; j < V; ++j) top_x = fmaxf(top_x, v[j]);
         over_lanes<L>([&](auto ctrl) { top_x = fmaxf(top_x, dpp_swap_f32<ctrl.value>(top_x)); });
-        top_x = top_x > -INFINITY ? top_x : 0.0f;
+        top_x = top_x > kOff ? top_x : 0.0f;
         double sum = 0.0;
 #pragma unroll
         for (int j = 0; j < V; ++j)
-            sum += static_cast<double>(__builtin_amdgcn_exp2f((v[j] - top_x) * kLog2E));         // 2^-inf = 0
+            sum += static_cast<double>(__builtin_amdgcn_exp2f((v[j] - top_x) * kLog2E));         // 0 if off
         over_lanes<L>([&](auto ctrl) { sum += dpp_swap<ctrl.value>(sum); });
         inv_sum = sum > 0.0 ? 1.0 / sum : 0.0;
     }
@@ -328,35 +328,35 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const float p = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-v[j] * kLog2E));
-                v[j] = v[j] > -INFINITY ? p : -INFINITY;
+                v[j] = v[j] > kOff ? p : kOff;
             }
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const float p = __builtin_amdgcn_exp2f((v[j] - top_x) * kLog2E) * inv_sum32;
-                v[j] = v[j] > -INFINITY ? p : -INFINITY;
+                v[j] = v[j] > kOff ? p : kOff;
             }
         }
         if (a.bias) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] += a.bias[VEC || expert(j) < a.E ? expert(j) : 0];       // -inf stays
+            for (int j = 0; j < V; ++j) v[j] += a.bias[VEC || expert(j) < a.E ? expert(j) : 0];       // kOff stays: |b| is below half its ulp
         }
     }
 
     // ---- groups: experts of closed ones leave the choice
-    const float closed = __uint_as_float(kClosedHigh);     // a NaN: no comparison holds for it
+    const float closed = -INFINITY;
     bool unsure = false;
     const float reach_of = a.sigmoid ? kUnsureSigmoid : kUnsureSoftmax;
     // with scores: totals of two values, of magnitudes up to `size`, each unsure by itself
     auto gap_unsure = [&](float lowest_open, float highest_closed, float size) {
-        return highest_closed > -INFINITY && lowest_open - highest_closed <= 2.0f * reach_of * (1.0f + size);
+        return (highest_closed > kOff) & lowest_open - highest_closed <= 2.0f * reach_of * (1.0f + size);
     };
     if constexpr (GROUPS == 1) {
         constexpr int G = C / CPG;
         float total[G], size = 0.0f;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            float b1 = -INFINITY, b2 = -INFINITY;
+            float b1 = kOff, b2 = kOff;
 #pragma unroll
             for (int j = g * CPG * 4; j < (g + 1) * CPG * 4; ++j) {
                 b2 = fmaxf(b2, fminf(b1, v[j]));
@@ -367,12 +367,12 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
                 b2 = fmaxf(fminf(b1, p1), fmaxf(b2, p2));
                 b1 = fmaxf(b1, p1);
             });
-            total[g] = (a.group_top > 1) & (b2 > -INFINITY) ? b1 + b2 : b1;
-            size = fmaxf(size, b1 > -INFINITY ? fabsf(b1) : 0.0f);
-            size = fmaxf(size, b2 > -INFINITY ? fabsf(b2) : 0.0f);
+            total[g] = (a.group_top > 1) & (b2 > kOff) ? b1 + b2 : b1;
+            size = fmaxf(size, b1 > kOff ? fabsf(b1) : 0.0f);
+            size = fmaxf(size, b2 > kOff ? fabsf(b2) : 0.0f);
         }
         uint32_t open = 0;
-        float lowest = INFINITY, highest = -INFINITY;
+        float lowest = INFINITY, highest = kOff;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             int ahead = 0;
@@ -403,19 +403,19 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
         __syncthreads();
         float size = 0.0f;
         for (int g = h; g < a.groups; g += L) {
-            float b1 = -INFINITY, b2 = -INFINITY;
+            float b1 = kOff, b2 = kOff;
             for (int i = 0; i < a.group_size; ++i) {
                 const float x = mine[g * a.group_size + i];
                 b2 = fmaxf(b2, fminf(b1, x));
                 b1 = fmaxf(b1, x);
             }
-            sums[g] = (a.group_top > 1) & (b2 > -INFINITY) ? b1 + b2 : b1;
-            size = fmaxf(size, b1 > -INFINITY ? fabsf(b1) : 0.0f);
-            size = fmaxf(size, b2 > -INFINITY ? fabsf(b2) : 0.0f);
+            sums[g] = (a.group_top > 1) & (b2 > kOff) ? b1 + b2 : b1;
+            size = fmaxf(size, b1 > kOff ? fabsf(b1) : 0.0f);
+            size = fmaxf(size, b2 > kOff ? fabsf(b2) : 0.0f);
         }
         __syncthreads();
         uint64_t open = 0;
-        float lowest = INFINITY, highest = -INFINITY;
+        float lowest = INFINITY, highest = kOff;
         for (int g = h; g < a.groups; g += L) {
             const float s = sums[g];
             int ahead = 0;
@@ -465,7 +465,7 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
     // what comes next: no more than k values within reach of the last one
     if constexpr (SCORE) {
         if (GROUPS == 0 || a.bias) {
-            float last = -INFINITY;
+            float last = INFINITY;
 #pragma unroll
             for (int s = 0; s < KP; ++s) {
                 const bool on = key_is_on(high_word(top[s]));
@@ -480,7 +480,7 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
 #pragma unroll
             for (int j = 0; j < V; ++j) reach += v[j] >= last ? 1 : 0;
             over_lanes<L>([&](auto ctrl) { reach += dpp_swap_i32<ctrl.value>(reach); });
-            unsure |= (last > -INFINITY) & (reach > a.k);
+            unsure |= (last < INFINITY) & (reach > a.k);
         }
     }
 
@@ -633,14 +633,12 @@ void launch_groups(const ScoreArgs& a, bool vec, hipStream_t st) {
         else launch<L, V, KP, SCORE, false, 0>(a, st);
         return;
     }
-    if constexpr (L == 4 && V >= 16) {
-        if (vec && a.group_size % 16 == 0) {
-            const int cpg = a.group_size / 16;
-            if (cpg == 1) return launch<L, V, KP, SCORE, true, 1, 1>(a, st);
-            if constexpr (V >= 16) if (cpg == 2) return launch<L, V, KP, SCORE, true, 1, 2>(a, st);
-            if constexpr (V >= 32) if (cpg == 4) return launch<L, V, KP, SCORE, true, 1, 4>(a, st);
-            if constexpr (V >= 64) if (cpg == 8) return launch<L, V, KP, SCORE, true, 1, 8>(a, st);
-        }
+    if (vec && a.group_size % (4 * L) == 0) {
+        const int cpg = a.group_size / (4 * L);
+        if constexpr (V >= 8) if (cpg == 1) return launch<L, V, KP, SCORE, true, 1, 1>(a, st);
+        if constexpr (V >= 16) if (cpg == 2) return launch<L, V, KP, SCORE, true, 1, 2>(a, st);
+        if constexpr (V >= 32) if (cpg == 4) return launch<L, V, KP, SCORE, true, 1, 4>(a, st);
+        if constexpr (V >= 64) if (cpg == 8) return launch<L, V, KP, SCORE, true, 1, 8>(a, st);
     }
     launch<L, V, KP, SCORE, false, 2>(a, st);
 }
@@ -657,114 +655,6 @@ void launch_keys(const ScoreArgs& a, bool vec, hipStream_t st) {
         if (score) launch_groups<L, V, 8, true>(a, vec, st);
         else launch_groups<L, V, 8, false>(a, vec, st);
     }
-}
-
-// ------------------------------------------------------------------ gradient
-struct ScoreGradArgs {
-    const float* logits;
-    const int32_t* idx;
-    const uint8_t* keep;
-    const float* w;
-    const float* d_w;
-    const float* d_add;
-    void* out;
-    int T, E, k, sigmoid, normalise;
-    float inv_scale;
-};
-
-__device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store_value(uint16_t* p, float v) {
-    // round to nearest even, once (a NaN stays one)
-    *p = static_cast<uint16_t>(pack_bf16x2_rne(v, v));
-}
-
-// L lanes per token (a power of two, at least 8), four experts a lane.  The slots'
-// gradients are worked out by the token's first k lanes and put in place through LDS.
-template <int L, typename OUT>
-__global__ __launch_bounds__(256) void route_scores_grad_kernel(const ScoreGradArgs a) {
-    constexpr int kTokens = 256 / L;
-    __shared__ float slot_row[kTokens][4 * L];
-    const int j = threadIdx.x & (L - 1), tl = threadIdx.x / L;
-    const long long t = static_cast<long long>(blockIdx.x) * kTokens + tl;
-    const bool live = t < a.T;
-    const bool full = !a.sigmoid && !a.normalise;        // the softmax's other experts have a gradient too
-    const size_t row = static_cast<size_t>(live ? t : 0) * a.E;
-
-    // the slot's part
-    float g = 0.0f, wk = 0.0f, one_less = 1.0f;
-    int e = -1;
-    if (live && j < a.k) {
-        const size_t at = static_cast<size_t>(t) * a.k + j;
-        const int ei = a.idx[at];
-        if ((!a.keep || a.keep[at]) && ei >= 0 && ei < a.E) {
-            e = ei;
-            wk = a.w[at];
-            g = wk * a.d_w[at];
-            if (a.sigmoid) one_less = 1.0f / (1.0f + expf(a.logits[row + ei]));   // 1 - s
-        }
-    }
-    float total = g;
-#pragma unroll
-    for (int d = 1; d < 8; d *= 2) total += __shfl_xor(total, d);      // within the first 8 lanes
-    total = __shfl(total, 0, L);                                       // to the token's lanes
-    const uint64_t any_kept = __ballot(e >= 0);
-    const int lane = threadIdx.x & 63;
-    const bool some = ((any_kept >> (lane & ~(L - 1))) & 0xFFull) != 0;
-    float slot = a.normalise ? g - wk * (total * a.inv_scale) : g;
-    slot *= one_less;
-
-    f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-    *reinterpret_cast<f32x4*>(&slot_row[tl][4 * j]) = zero;
-    __builtin_amdgcn_wave_barrier();                 // a token's lanes are of one wave, whose LDS accesses stay in order
-    if (e >= 0) slot_row[tl][e] = slot;
-    __builtin_amdgcn_wave_barrier();
-    f32x4 d = *reinterpret_cast<const f32x4*>(&slot_row[tl][4 * j]);
-
-    if (full) {
-        float x[4], top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int ei = 4 * j + i;
-            x[i] = live && ei < a.E ? a.logits[row + ei] : -INFINITY;
-            x[i] = x[i] > -INFINITY ? x[i] : -INFINITY;          // NaN is off
-            top = fmaxf(top, x[i]);
-        }
-#pragma unroll
-        for (int s = 1; s < L; s *= 2) top = fmaxf(top, __shfl_xor(top, s));
-        float p[4], sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            p[i] = x[i] > -INFINITY ? expf(x[i] - top) : 0.0f;
-            sum += p[i];
-        }
-#pragma unroll
-        for (int s = 1; s < L; s *= 2) sum += __shfl_xor(sum, s);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) d[i] -= some && sum > 0.0f ? total * (p[i] / sum) : 0.0f;
-    }
-    if (!live) return;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int ei = 4 * j + i;
-        if (ei < a.E) {
-            float v = d[i];
-            if (a.d_add) v += a.d_add[row + ei];
-            store_value(static_cast<OUT*>(a.out) + row + ei, v);
-        }
-    }
-}
-
-template <typename OUT>
-void launch_grad(const ScoreGradArgs& a, hipStream_t st) {
-    auto go = [&](auto lanes) {
-        constexpr int L = decltype(lanes)::value;
-        constexpr int tokens = 256 / L;
-        route_scores_grad_kernel<L, OUT><<<(a.T + tokens - 1) / tokens, 256, 0, st>>>(a);
-    };
-    if (a.E <= 32) go(std::integral_constant<int, 8>{});
-    else if (a.E <= 64) go(std::integral_constant<int, 16>{});
-    else if (a.E <= 128) go(std::integral_constant<int, 32>{});
-    else go(std::integral_constant<int, 64>{});
 }
 
 }  // namespace
@@ -795,50 +685,19 @@ cap_status route_scores_launch(const cap_topology* tp, const float* logits, cons
     a.scale = opt->scale;
     a.p = p;
     a.inter_node_cost = tp->inter_node_cost;
-    // sixteen lanes a token where four leave compute units without a wave
-    const bool few = a.T <= kFewTokens && a.E > 16;
-    const int lanes = few ? 16 : 4;
-    int V = 4;
-    while (lanes * V < a.E) V *= 2;
-    const bool vec = a.E == lanes * V && (reinterpret_cast<uintptr_t>(logits) & 15) == 0;
-    if (few) {
-        switch (V) {
-            case 4: launch_keys<16, 4>(a, vec, st); break;
-            case 8: launch_keys<16, 8>(a, vec, st); break;
-            default: launch_keys<16, 16>(a, vec, st); break;
-        }
-    } else {
-        switch (V) {
-            case 4: launch_keys<4, 4>(a, vec, st); break;
-            case 8: launch_keys<4, 8>(a, vec, st); break;
-            case 16: launch_keys<4, 16>(a, vec, st); break;
-            case 32: launch_keys<4, 32>(a, vec, st); break;
-            default: launch_keys<4, 64>(a, vec, st); break;
-        }
-    }
-    CAP_LAUNCH_CHECK();
-    return CAP_OK;
-}
-
-cap_status route_scores_grad_launch(int T, int k, int E, const float* logits, const int32_t* idx, const uint8_t* keep,
-                                    const float* w, const float* d_w, const cap_score_options* opt, const float* d_add,
-                                    cap_dtype dtype, void* d_logits, hipStream_t st) {
-    ScoreGradArgs a;
-    a.logits = logits;
-    a.idx = idx;
-    a.keep = keep;
-    a.w = w;
-    a.d_w = d_w;
-    a.d_add = d_add;
-    a.out = d_logits;
-    a.T = T;
-    a.E = E;
-    a.k = k;
-    a.sigmoid = opt->kind == CAP_SCORE_SIGMOID;
-    a.normalise = opt->normalise != 0;
-    a.inv_scale = 1.0f / opt->scale;
-    if (dtype == CAP_DTYPE_BF16) launch_grad<uint16_t>(a, st);
-    else launch_grad<float>(a, st);
+    auto go = [&](auto lanes) {
+        constexpr int L = decltype(lanes)::value;
+        int V = 4;
+        while (L * V < a.E) V *= 2;
+        const bool vec = a.E == L * V && (reinterpret_cast<uintptr_t>(logits) & 15) == 0;
+        if (V == 4) return launch_keys<L, 4>(a, vec, st);
+        if (V == 8) return launch_keys<L, 8>(a, vec, st);
+        if (V == 16) return launch_keys<L, 16>(a, vec, st);
+        if (V == 32) return launch_keys<L, 32>(a, vec, st);
+        if constexpr (L == 4) if (V == 64) return launch_keys<L, 64>(a, vec, st);
+    };
+    if (a.E > 16 && a.T <= kTokens8) go(std::integral_constant<int, 8>{});
+    else go(std::integral_constant<int, 4>{});
     CAP_LAUNCH_CHECK();
     return CAP_OK;
 }

@@ -32,7 +32,7 @@ def route(logits, k, expert_rank, R, node, p, cost, kind="softmax", n_groups=1, 
     target = 1.0 - float(np.float32(p))
     for t in range(T):
         row = logits[t]
-        on = row > -math.inf                       # NaN compares false
+        on = np.isfinite(row)
         if token_mask is not None and not token_mask[t]:
             on = np.zeros(E, bool)
         s = _scores(row, on, kind)
@@ -91,7 +91,7 @@ def gates(x, idx, keep, kind, normalise, scale):
     T, k = idx.shape
     w = np.zeros((T, k))
     for t in range(T):
-        s = _scores(x[t], x[t] > -math.inf, kind)
+        s = _scores(x[t], np.isfinite(x[t]), kind)
         q = np.where(keep[t] != 0, s[idx[t]], 0.0)
         total = q.sum() if normalise else 1.0
         w[t] = scale * q / total if total > 0 else 0.0
@@ -103,7 +103,7 @@ def grad(x, idx, keep, d_w, kind, normalise, scale):
     T, E = x.shape
     out = np.zeros((T, E))
     for t in range(T):
-        on = x[t] > -math.inf
+        on = np.isfinite(x[t])
         s = _scores(x[t], on, kind)
         kept = [j for j in range(idx.shape[1]) if keep[t, j]]
         ds = np.zeros(E)                           # gradient at the scores

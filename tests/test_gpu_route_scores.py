@@ -106,6 +106,7 @@ def test_experts_off_and_tokens_masked(capi, case):
     logits = (2.0 * rng.standard_normal((T, E))).astype(np.float32)
     logits[rng.random((T, E)) < 0.5] = -math.inf
     logits[rng.random((T, E)) < 0.05] = math.nan
+    logits[rng.random((T, E)) < 0.02] = math.inf
     logits[rng.random(T) < 0.2] = -math.inf
     token_mask = (rng.random(T) < 0.8).astype(np.uint8)
     logits[token_mask == 0] = rng.choice(np.array([math.nan, math.inf, -math.inf, 3e38], np.float32), (int((token_mask == 0).sum()), E))
