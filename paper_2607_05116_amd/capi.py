@@ -37,8 +37,9 @@ EXPORTS = ["cap_status_string", "cap_version", "cap_workspace_size", "cap_route_
            "cap_combine", "cap_coactivation", "cap_dispatch_layout_static",
            "cap_dispatch_layout_static_max_bytes", "cap_adjustment_spectrum", "cap_route_layout",
            "cap_row_plan", "cap_expert_ffn_combine", "cap_balance_loss", "cap_router_grad", "cap_orthogonalise",
-           "cap_muon_update", "cap_route_scores", "cap_route_scores_grad", "cap_quantise_fp8", "cap_product_fp8",
-           "cap_expert_ffn_fp8"]
+           "cap_muon_update", "cap_route_scores", "cap_route_scores_grad"]
+# the calls whose names end in a type
+EXPORTS_FP8 = ["cap_quantise_fp8", "cap_product_fp8", "cap_expert_ffn_fp8"]
 
 
 class CapError(RuntimeError):

@@ -7,6 +7,9 @@ layer (Sec. II-B/II-C; Sec. VI):
   expert_gather(rank) -> expert_ffn(rank) -> dest_reduce(rank)
   [shared experts on the source rank's tokens] -> src_reduce(rank)
 
+set_scores routes by sigmoid or softmax scores with a bias and groups instead; set_fp8
+runs the routed experts in 8-bit floating point (row_source -> quantise_x -> ffn_fp8).
+
 Every step runs in libcap.so's HIP kernels; this module only allocates and
 passes pointers.  All calls are asynchronous on the current stream.
 """
@@ -92,6 +95,9 @@ class DeviceLayer:
         self.fused_gather = True        # FFN reads x through row_src instead of a gathered copy
         # bf16: single-expert tokens' destination combine in the FFN's epilogue
         self.fused_combine = cfg.dtype == "bf16"
+        self.scores = None              # routing by scores instead of the logits' softmax (set_scores)
+        self.fp8 = False                # the routed experts in 8-bit floating point (set_fp8)
+        self.weights_fp8: dict[int, tuple] = {}
         # with a side stream: start the shared experts after the routing front
         # end (True) or with it (False)
         self.shared_after_front = False
@@ -107,6 +113,56 @@ class DeviceLayer:
     def set_rank_weights(self, rank: int, w1: np.ndarray, w3: np.ndarray, w2: np.ndarray):
         """w1, w3 [E_loc][inter][d], w2 [E_loc][d][inter] in local-slot order (storage type)."""
         self.weights[rank] = tuple(to_device_rows(w, self.cfg.dtype, self.dev) for w in (w1, w3, w2))
+        if rank in self.weights_fp8:
+            self.quantise_weights(rank)
+
+    def set_scores(self, kind: str | None = "sigmoid", n_groups: int = 1, topk_groups: int = 1, group_top: int = 1,
+                   normalise: bool = True, scale: float = 1.0, bias=None, token_mask=None):
+        """Route by scores (cap_route_scores): kind "sigmoid" or "softmax" (None: back to the softmax over the chosen
+        logits); bias fp32 [E], token_mask uint8 or bool [T] on the device, read at every step.  The front end then runs
+        as separate calls."""
+        if kind is None:
+            self.scores = None
+            return
+        if kind not in ("sigmoid", "softmax"):
+            raise ValueError(f"kind is {kind!r}; sigmoid or softmax is taken")
+        for name, t, n, dtypes in (("bias", bias, self.cfg.E, (torch.float32,)),
+                                   ("token_mask", token_mask, self.cfg.T, (torch.uint8, torch.bool))):
+            if t is None:
+                continue
+            if tuple(t.shape) != (n,) or t.dtype not in dtypes or t.device != self.logits.device or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous {dtypes[0]} [{n}] on {self.logits.device}, got {t.dtype} "
+                                 f"{list(t.shape)} on {t.device}")
+        self._score_inputs = (bias, token_mask)         # the options hold their addresses
+        self.scores = capi.make_score_options(
+            capi.CAP_SCORE_SIGMOID if kind == "sigmoid" else capi.CAP_SCORE_SOFTMAX, n_groups, topk_groups, group_top,
+            normalise, scale, bias, token_mask)
+
+    def set_fp8(self, on: bool = True):
+        """The routed experts in 8-bit floating point: their weights quantised in blocks of 128 x 128 (each rank's at its
+        first step, or by quantise_weights after they change), the tokens' rows at every step."""
+        cfg = self.cfg
+        if on and (cfg.dtype != "bf16" or self.d % 128 or cfg.inter % 128):
+            raise ValueError("8-bit experts take a bf16 layer with d and inter multiples of 128")
+        self.fp8 = on
+        if on and not hasattr(self, "x8"):
+            self.x8 = torch.empty((cfg.T, self.d), dtype=torch.float8_e4m3fn, device=self.dev)
+            self.x8_scale = torch.empty((cfg.T, self.d // 128), dtype=torch.float32, device=self.dev)
+            self.ws_fp8 = self._ws(capi.cap_workspace_size(capi.CAP_OP_EXPERT_FFN_FP8, None, self.d, cfg.inter,
+                                                           self.row_cap))
+
+    def quantise_weights(self, rank: int, stream=None):
+        """The rank's weights in e4m3 with their scales, from set_rank_weights' (buffers are kept)."""
+        if rank not in self.weights_fp8:
+            made = []
+            for w in self.weights[rank]:
+                E_loc, n, k = w.shape
+                made += [torch.empty((E_loc, n, k), dtype=torch.float8_e4m3fn, device=self.dev),
+                         torch.empty((E_loc, n // 128, k // 128), dtype=torch.float32, device=self.dev)]
+            self.weights_fp8[rank] = tuple(made)
+        q = self.weights_fp8[rank]
+        for i, w in enumerate(self.weights[rank]):
+            capi.cap_quantise_fp8(self.dt, *w.shape, 128, w, q[2 * i], q[2 * i + 1], stream)
 
     def set_placement(self, expert_rank, expert_local):
         """Replace the placement in place (the topology keeps pointing at the
@@ -125,6 +181,10 @@ class DeviceLayer:
 
     # ------------------------------------------------------------ steps
     def route(self, stream=None):
+        if self.scores is not None:
+            capi.cap_route_scores(self.topo, self.logits, self.scores, self.p, self.idx, self.w, self.keep, self.mask,
+                                  stream)
+            return
         fn = capi.cap_route_prune_naive if self.naive else capi.cap_route_prune
         fn(self.topo, self.logits, self.p, self.idx, self.w, self.keep, self.mask, stream)
 
@@ -192,6 +252,20 @@ class DeviceLayer:
                                     self.row_w, self.parts, self.recv_cap, self.ws_ffn, options=self.ffn_opts,
                                     stream=stream)
 
+    def quantise_x(self, stream=None):
+        """The tokens' rows in e4m3, once for all experts that read them."""
+        capi.cap_quantise_fp8(self.dt, 1, self.cfg.T, self.d, 1, self.x, self.x8, self.x8_scale, stream)
+
+    def ffn_fp8(self, rank: int, stream=None):
+        """ffn_gather in 8-bit floating point, from quantise_x's rows."""
+        if rank not in self.weights_fp8:
+            self.quantise_weights(rank, stream)
+        w1, s1, w3, s3, w2, s2 = self.weights_fp8[rank]
+        E_loc = self.cfg.E_loc
+        offs = self.lay_t["expert_offsets"][rank * E_loc:(rank + 1) * E_loc + 1]
+        capi.cap_expert_ffn_fp8(E_loc, self.d, self.cfg.inter, self.row_cap, self.x8, self.x8_scale, self.cfg.T,
+                                self.row_src, offs, w1, s1, w3, s3, w2, s2, self.Y, self.ws_fp8, stream=stream)
+
     def shared_ffn(self, rank: int, stream=None):
         if self.shared is None:
             return
@@ -219,14 +293,20 @@ class DeviceLayer:
                          self.shared_out if self.shared is not None else None, self.y,
                          self.y.shape[0], stream)
 
+    @property
+    def one_front(self) -> bool:
+        """The front end is the fused call (which routes by the logits' softmax with CAP pruning only)."""
+        return self.fused_front and not self.naive and self.scores is None
+
     def front(self, stream=None, side=None):
         """Routing front end over all virtual ranks' tokens: the fused
         three-launch front end (CAP pruning), or route, layout and
-        co-activation as separate calls (naive pruning, or fused_front off).
+        co-activation as separate calls (naive pruning, routing by scores, or
+        fused_front off).
         In the separate form, with a side stream the co-activation counts
         (which only feed placement) run there beside the layout; the main
         stream waits for them before returning control to later work."""
-        if self.fused_front and not self.naive:
+        if self.one_front:
             self.route_layout(True, stream)
             return
         if side is None:
@@ -251,16 +331,19 @@ class DeviceLayer:
         the source reduce waits for, when the shared experts ran on another
         stream; without it they run here, before the source reduce."""
         main = stream if stream is not None else torch.cuda.current_stream()
-        combine = self.fused_gather and self.fused_combine
+        combine = self.fused_gather and self.fused_combine and not self.fp8
         if combine:
             self.row_plan(rank, main)
-        elif self.fused_gather:
+        elif self.fused_gather or self.fp8:
             self.row_source(rank, main)
         else:
             self.gather(rank, main)
         if ffn_events is not None:
             ffn_events[0].record(main)
-        if combine:
+        if self.fp8:
+            self.quantise_x(main)
+            self.ffn_fp8(rank, main)
+        elif combine:
             self.ffn_combine(rank, main)
         elif self.fused_gather:
             self.ffn_gather(rank, main)
@@ -301,7 +384,7 @@ class DeviceLayer:
         is done; the main stream joins it before the source reduce, which adds
         the shared output.  ffn_events: as in rank_path."""
         main = stream if stream is not None else torch.cuda.current_stream()
-        if side is None or (self.fused_front and not self.naive):
+        if side is None or self.one_front:
             # the fused front end, then (beside it on the side stream, when
             # there is one) the shared experts, which read only x
             if side is not None:

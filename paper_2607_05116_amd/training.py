@@ -6,6 +6,9 @@ C-ABI calls in its order:
   router_route_prune (logits, routing, pruning) -> balance_loss -> router_grad
   -> the gradient of the router's weights -> muon_update -> the weights
 
+or, routing by scores (Scores), with route_scores after the first and
+route_scores_grad after the third.
+
 Muon is the optimizer for a batch of matrices of one shape (the experts' of a
 rank, or the router's): momentum, then the orthogonalised update.
 
@@ -100,6 +103,22 @@ class Muon:
                 w_bf16.copy_(w)
 
 
+class Scores:
+    """Routing by scores in a RouterTrainer (cap_route_scores; kind "sigmoid" or "softmax").
+
+    bias_speed: with it, the trainer keeps a bias [E] for the choice of experts, and after each step raises that of
+    experts with less than the mean load by so much and lowers the others': balance without a gradient.
+    """
+
+    def __init__(self, kind: str = "sigmoid", n_groups: int = 1, topk_groups: int = 1, group_top: int = 1,
+                 normalise: bool = True, scale: float = 1.0, bias_speed: float = 0.0):
+        if kind not in ("sigmoid", "softmax"):
+            raise ValueError(f"kind is {kind!r}; sigmoid or softmax is taken")
+        self.kind = capi.CAP_SCORE_SIGMOID if kind == "sigmoid" else capi.CAP_SCORE_SOFTMAX
+        self.n_groups, self.topk_groups, self.group_top = int(n_groups), int(topk_groups), int(group_top)
+        self.normalise, self.scale, self.bias_speed = bool(normalise), float(scale), float(bias_speed)
+
+
 class RouterTrainer:
     """Buffers and calls of one layer's router training.
 
@@ -110,11 +129,14 @@ class RouterTrainer:
     Tokens that a mask or the offsets leave out count nowhere, whatever their rows of x hold: with either given, a copy
     of x with zeros in those rows is what the router and the weights' gradient read (a zero gradient times a row that
     is not finite would be NaN in all of the weights).
+
+    scores: route by scores instead of the softmax over the chosen logits.  The gates' gradient is then that of the
+    scores; the balance and z losses stay those of the logits' softmax.
     """
 
     def __init__(self, T: int, d: int, E: int, k: int, R: int, ranks_per_node: int, expert_rank, expert_local, w_gate,
                  p: float = 0.0, n_seq: int = 1, balance_coef: float = 1e-2, z_coef: float = 1e-3, lr: float = 1e-3,
-                 mu: float = 0.95, device: str = "cuda"):
+                 mu: float = 0.95, device: str = "cuda", scores: Scores | None = None):
         self.T, self.d, self.E, self.k, self.n_seq, self.p = T, d, E, k, n_seq, float(p)
         self.balance_coef, self.z_coef = float(balance_coef), float(z_coef)
         dev = self.dev = torch.device(device)
@@ -143,6 +165,18 @@ class RouterTrainer:
         self.zero = torch.zeros((), dtype=_BF16, device=dev)
         self.ws = _workspace(capi.cap_workspace_size(capi.CAP_OP_BALANCE_LOSS, self.topo, max_rows=n_seq), dev)
         self.opt = Muon(1, E, d, lr, mu, device=device)
+        self.scores = scores
+        if scores is not None:
+            self.bias = torch.zeros(E, dtype=torch.float32, device=dev) if scores.bias_speed else None
+            self.d_losses = torch.empty((T, E), dtype=torch.float32, device=dev)
+            self.kept = torch.empty((T, k), dtype=torch.uint8, device=dev)
+            # (the mask's address changes from batch to batch; the backward pass does not read it)
+            self.options = self._score_options(None)
+
+    def _score_options(self, token_mask):
+        s = self.scores
+        return capi.make_score_options(s.kind, s.n_groups, s.topk_groups, s.group_top, s.normalise, s.scale, self.bias,
+                                       token_mask)
 
     def _check_batch(self, x, seq_offsets, token_mask, d_gates=None, d_loss=None):
         dev = self.w.device
@@ -175,6 +209,9 @@ class RouterTrainer:
     def _forward(self, x, seq_offsets, token_mask):
         capi.cap_router_route_prune(self.topo, capi.CAP_DTYPE_BF16, self.d, x, self.w_bf16, self.p, self.idx,
                                     self.gates, self.keep, self.mask, self.logits)
+        if self.scores is not None:                     # the same logits, chosen and weighed by scores
+            capi.cap_route_scores(self.topo, self.logits, self._score_options(token_mask), self.p, self.idx, self.gates,
+                                  self.keep, self.mask)
         capi.cap_balance_loss(self.T, self.k, self.E, self.logits, self.idx, self.keep, token_mask, seq_offsets,
                               self.n_seq, self.balance_coef, self.z_coef, self.counts, self.probs, self.tokens,
                               self.loss, self.ws)
@@ -187,9 +224,17 @@ class RouterTrainer:
             self._backward(self._counted_rows(x, seq_offsets, token_mask), d_gates, seq_offsets, token_mask, d_loss)
 
     def _backward(self, x, d_gates, seq_offsets, token_mask, d_loss):
-        capi.cap_router_grad(self.T, self.k, self.E, self.logits, self.idx, self.keep, self.gates, d_gates, token_mask,
-                             seq_offsets, self.n_seq, self.counts, self.tokens, self.balance_coef, self.z_coef, d_loss,
-                             capi.CAP_DTYPE_BF16, self.d_logits)
+        by_scores = self.scores is not None and d_gates is not None
+        capi.cap_router_grad(self.T, self.k, self.E, self.logits, self.idx, self.keep, self.gates,
+                             None if by_scores else d_gates, token_mask, seq_offsets, self.n_seq, self.counts, self.tokens,
+                             self.balance_coef, self.z_coef, d_loss,
+                             capi.CAP_DTYPE_F32 if by_scores else capi.CAP_DTYPE_BF16,
+                             self.d_losses if by_scores else self.d_logits)
+        if by_scores:
+            # a token that the offsets leave out is routed, but counts nowhere: no gradient of its gates
+            keep = self._counted_keep(seq_offsets)
+            capi.cap_route_scores_grad(self.T, self.k, self.E, self.logits, self.idx, keep, self.gates, d_gates,
+                                       self.options, self.d_losses, capi.CAP_DTYPE_BF16, self.d_logits)
         torch.mm(self.d_logits.t(), x, out=self.d_w[0])
 
     def step(self, x: torch.Tensor, d_gates=None, seq_offsets=None, token_mask=None):
@@ -199,6 +244,19 @@ class RouterTrainer:
         self._forward(x, seq_offsets, token_mask)
         self._backward(x, d_gates, seq_offsets, token_mask, None)
         self.opt.step(self.w, self.d_w, self.w_bf16)
+        if self.scores is not None and self.scores.bias_speed:
+            self._update_bias()
+
+    def _counted_keep(self, seq_offsets):
+        if seq_offsets is None:
+            return self.keep
+        torch.ge(self.token, seq_offsets[0], out=self.counted)
+        self.counted.logical_and_(torch.lt(self.token, seq_offsets[-1], out=self.one_rule))
+        return torch.mul(self.keep, self.counted[:, None], out=self.kept)
+
+    def _update_bias(self):
+        loads = self.counts.sum(0, dtype=torch.float32)
+        self.bias.add_(torch.sign(loads.mean() - loads), alpha=self.scores.bias_speed)
 
     def expert_loads(self) -> torch.Tensor:
         """Kept slots per expert of the last batch."""
