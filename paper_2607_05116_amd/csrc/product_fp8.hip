@@ -99,11 +99,33 @@ struct Tile {
     int e, m0, end, nt;          // expert, first row, end of the expert's rows, column tile
 };
 
+// Four neighbouring results of a row from column n on, those that are there.
+template <typename OUT>
+__device__ __forceinline__ void store4(const F8Args& a, OUT* out, int row, int n, const f32x4& v) {
+    if (n >= a.N) return;
+    OUT* const p = out + static_cast<size_t>(row) * a.N + n;
+    // rows of whole, aligned groups of four
+    if ((a.N & 3) == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(OUT) - 1)) == 0) {
+        if constexpr (std::is_same<OUT, float>::value) *reinterpret_cast<f32x4*>(p) = v;
+        else *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2_rne(v[0], v[1]), pack_bf16x2_rne(v[2], v[3])};
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        if (n + c < a.N) {
+            if constexpr (std::is_same<OUT, float>::value) p[c] = v[c];
+            else p[c] = static_cast<uint16_t>(pack_bf16x2_rne(v[c], v[c]));
+        }
+}
+
+// ------------------------------------------------------------------ tiles of 128 x 128
+constexpr int kTile = 128;
+
 // The tile of a workgroup; false for surplus ones.  Workgroups go to the XCDs in
 // turn: each XCD gets a contiguous run of tiles, in which groups of four row tiles
 // go through all column tiles together (their operands then meet in its L2).
-template <int BM>
 __device__ __forceinline__ bool find_tile(const F8Args& a, int NT, Tile& out) {
+    constexpr int BM = kTile;
     const int lane = threadIdx.x & 63;
     int total = 0;
     for (int c = 0; c < a.E_loc; c += 64) {
@@ -157,142 +179,27 @@ __device__ __forceinline__ void lds_barrier() {
     block_barrier();
 }
 
-// A tile's way out: y, or H with its scales.  `lds` (the stages) is free but for reads
-// of the last stage that other waves may still make.
-template <int BM, int BN, int NWM, int NWN, typename OUT>
-__device__ __forceinline__ void finish_tile(const F8Args& a, const Tile& tile, int n0, int wm, int wn, int lane,
-                                            f32x4 (&acc)[BM / NWM / 16][BN / NWN / 16], uint8_t* lds) {
-    constexpr bool kSwiglu = std::is_same<OUT, uint8_t>::value;
-    constexpr int NW = NWM * NWN, WM = BM / NWM, WN = BN / NWN, MI = WM / 16, NJ = WN / 16;
-    const int fr_row = lane & 15;
-    const int q4 = (lane >> 4) * 4;                    // the lane's four outputs within a block of 16
-    if constexpr (!kSwiglu) {
-        OUT* const out = static_cast<OUT*>(a.out);
-        // rows of whole, aligned groups of four
-        const bool whole = (a.N & 3) == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(OUT) - 1)) == 0;
-#pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            const int row = tile.m0 + wm * WM + 16 * i + fr_row;
-            if (row >= tile.end) continue;
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                const int n = n0 + wn * WN + 16 * j + q4;
-                OUT* const p = out + static_cast<size_t>(row) * a.N + n;
-                const f32x4 v = acc[i][j];
-                if (whole) {
-                    if (n < a.N) {
-                        if constexpr (std::is_same<OUT, float>::value) *reinterpret_cast<f32x4*>(p) = v;
-                        else *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2_rne(v[0], v[1]), pack_bf16x2_rne(v[2], v[3])};
-                    }
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        if (n + c < a.N) {
-                            if constexpr (std::is_same<OUT, float>::value) p[c] = v[c];
-                            else p[c] = static_cast<uint16_t>(pack_bf16x2_rne(v[c], v[c]));
-                        }
-                }
-            }
-        }
-    } else {
-        constexpr int HC = WN / 2;                     // H columns of a wave
-        float* const row_max = reinterpret_cast<float*>(lds);                    // [NWN][BM]
-        uint8_t* const codes = lds + NWN * BM * 4;                               // [BM][kPitch]
-        constexpr int kPitch = 128 + 16;
-        static_assert(NWN * BM * 4 + BM * kPitch <= (BM + BN) * 128, "epilogue in one stage");
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int j = 0; j < NJ / 2; ++j)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const float g = acc[i][j][v];
-                    acc[i][j][v] = g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * acc[i][j + NJ / 2][v];
-                }
-        lds_barrier();                                 // the last stage is read
-        uint32_t m[MI];
-#pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            m[i] = 0;
-#pragma unroll
-            for (int j = 0; j < NJ / 2; ++j)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const uint32_t b = finite_magnitude(acc[i][j][v]);
-                    m[i] = b > m[i] ? b : m[i];
-                }
-#pragma unroll
-            for (int d = 16; d < 64; d *= 2) {
-                const uint32_t o = static_cast<uint32_t>(__shfl_xor(static_cast<int>(m[i]), d));
-                m[i] = o > m[i] ? o : m[i];
-            }
-            if (lane < 16) row_max[wn * BM + wm * WM + 16 * i + lane] = __uint_as_float(m[i]);
-        }
-        lds_barrier();
-#pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            const int r = wm * WM + 16 * i + fr_row;
-            uint32_t top = 0;
-#pragma unroll
-            for (int c = 0; c < NWN; ++c) {
-                const uint32_t o = __float_as_uint(row_max[c * BM + r]);
-                top = o > top ? o : top;
-            }
-            const uint32_t ex = f8_scale_exponent(top);
-            const float inv = f8_inverse(ex);
-#pragma unroll
-            for (int j = 0; j < NJ / 2; ++j) {
-                const f32x4 v = acc[i][j];
-                *reinterpret_cast<uint32_t*>(codes + r * kPitch + wn * HC + 16 * j + q4) =
-                    f8_pack4(v[0], v[1], v[2], v[3], inv);
-            }
-            if (wn == 0 && lane < 16 && tile.m0 + r < tile.end)
-                a.out_scale[tile.nt * a.scale_pitch + tile.m0 + r] = f8_scale(ex);
-        }
-        lds_barrier();
-        uint8_t* const out = static_cast<uint8_t*>(a.out);
-        for (int c = threadIdx.x; c < BM * 8; c += 64 * NW) {
-            const int r = c >> 3;
-            if (tile.m0 + r < tile.end)
-                *reinterpret_cast<u32x4*>(out + static_cast<size_t>(tile.m0 + r) * a.N + n0 + (c & 7) * 16) =
-                    *reinterpret_cast<const u32x4*>(codes + r * kPitch + (c & 7) * 16);
-        }
-    }
-}
-
-// One tile of BM rows x BN weight rows; K in stages of 128, double buffered, one
-// barrier a stage.  OUT: uint16_t (bf16), float, or uint8_t: SwiGLU, whose BN weight
-// rows are 128 of W1 and the same 128 of W3, those of each wave half and half, and
-// whose result is quantised to e4m3 by rows.
-template <int BM, int BN, int NWM, int NWN, typename OUT>
-__global__ __launch_bounds__(64 * NWM * NWN) void f8_tile_kernel(const F8Args a) {
-    constexpr bool kSwiglu = std::is_same<OUT, uint8_t>::value;
-    constexpr int NW = NWM * NWN, WM = BM / NWM, WN = BN / NWN, MI = WM / 16, NJ = WN / 16;
-    constexpr int kChunksW = (BM + BN) / 8 / NW;        // 1 KiB loads of a wave per stage
-    constexpr int kStage = (BM + BN) * 128;
-    constexpr int kCols = kSwiglu ? BN / 2 : BN;        // outputs of the tile
-    static_assert((BM + BN) % (8 * NW) == 0 && BM % 64 == 0 && BM / 64 <= NW, "load split");
-    static_assert(kSwiglu ? BN == 256 : BN <= 256, "scale blocks of a tile");
+// One tile of 128 rows x 128 weight rows, four waves of 64 x 64; K in stages of 128, double
+// buffered, one barrier a stage.  For fp32 results, and for bf16 ones whose rows the wide
+// kernel cannot load or store (n % 8 or y's address).  OUT: uint16_t (bf16) or float.
+template <typename OUT>
+__global__ __launch_bounds__(256) void f8_tile_kernel(const F8Args a) {
+    constexpr int NW = 4, WM = 64, WN = 64, MI = WM / 16, NJ = WN / 16;
+    constexpr int kChunksW = 2 * kTile / 8 / NW;        // 1 KiB loads of a wave per stage
+    constexpr int kStage = 2 * kTile * 128;
     __shared__ __align__(16) uint8_t lds[2 * kStage];
-    __shared__ float lds_sx[2 * BM];
-    __shared__ float lds_sw[2 * kF8MaxStages];
+    __shared__ float lds_sx[2 * kTile];
+    __shared__ float lds_sw[kF8MaxStages];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave / NWN, wn = wave % NWN;
-    const int KT = a.KT, K = KT * 128, NT = (a.N + kCols - 1) / kCols;
+    const int wm = wave / 2, wn = wave % 2;
+    const int KT = a.KT, K = KT * 128, NT = (a.N + kTile - 1) / kTile;
     Tile tile;
-    if (!find_tile<BM>(a, NT, tile)) return;
-    const int n0 = tile.nt * kCols, NB = (a.N + 127) / 128;
+    if (!find_tile(a, NT, tile)) return;
+    const int n0 = tile.nt * kTile;
 
-    // the weights' scales of the tile: one row of blocks of W1 and of W3, or BN / 128 rows
-    {
-        const size_t first = (static_cast<size_t>(tile.e) * NB + n0 / 128) * KT;
-        for (int i = threadIdx.x; i < KT; i += 64 * NW) {
-            lds_sw[i] = a.s1[first + i];
-            if constexpr (kSwiglu) lds_sw[KT + i] = a.s3[first + i];
-            else if constexpr (BN > 128) lds_sw[KT + i] = a.s1[(n0 / 128 + 1 < NB ? first + KT : first) + i];
-        }
-    }
+    // the weights' scales of the tile: one row of blocks
+    for (int i = threadIdx.x; i < KT; i += 64 * NW) lds_sw[i] = a.s1[(static_cast<size_t>(tile.e) * NT + tile.nt) * KT + i];
 
     // direct loads: lane l of a load writes row l / 8 of its 8 rows, chunk l % 8
     const LaneMap lm = lane_map(lane);
@@ -311,33 +218,26 @@ __global__ __launch_bounds__(64 * NWM * NWN) void f8_tile_kernel(const F8Args a)
     for (int i = 0; i < kChunksW; ++i) {
         const int c = wave + NW * i;
         dst[i] = c * 1024;
-        if (c < BM / 8) {
+        if (c < kTile / 8) {
             base[i] = reinterpret_cast<const char*>(a.x);
             off[i] = static_cast<uint32_t>(source_row(8 * c + lm.ld_row)) * static_cast<uint32_t>(K) + lm.col_b[c & 1];
         } else {
-            const int b = 8 * (c - BM / 8) + lm.ld_row;               // row of the B tile
-            const size_t expert = static_cast<size_t>(tile.e) * a.N * K;
-            int n = b;
-            base[i] = reinterpret_cast<const char*>(a.w1 + expert);
-            if constexpr (kSwiglu) {
-                const int col = b / WN, in = b % WN;
-                n = col * (WN / 2) + in % (WN / 2);
-                if (in >= WN / 2) base[i] = reinterpret_cast<const char*>(a.w3 + expert);
-            }
-            n = n0 + n < a.N ? n0 + n : a.N - 1;
+            int n = n0 + 8 * (c - kTile / 8) + lm.ld_row;
+            n = n < a.N ? n : a.N - 1;
+            base[i] = reinterpret_cast<const char*>(a.w1 + static_cast<size_t>(tile.e) * a.N * K);
             off[i] = static_cast<uint32_t>(n) * static_cast<uint32_t>(K) + lm.col_b[c & 1];
         }
     }
     uint32_t sx_off = 0;
-    if (wave < BM / 64) sx_off = static_cast<uint32_t>(source_row(64 * wave + lane)) * static_cast<uint32_t>(a.sx_row) * 4u;
+    if (wave < kTile / 64) sx_off = static_cast<uint32_t>(source_row(64 * wave + lane)) * static_cast<uint32_t>(a.sx_row) * 4u;
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds));
     const uint32_t sx0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds_sx));
     auto issue = [&](int kt, int buf) {
 #pragma unroll
         for (int i = 0; i < kChunksW; ++i)
             lds_dma16(base[i] + static_cast<size_t>(kt) * 128, off[i], lds0 + buf * kStage + dst[i]);
-        if (wave < BM / 64)
-            lds_dma4(a.sx + kt * a.sx_block, sx_off, sx0 + buf * BM * 4 + wave * 256);
+        if (wave < kTile / 64)
+            lds_dma4(a.sx + kt * a.sx_block, sx_off, sx0 + buf * kTile * 4 + wave * 256);
     };
 
     f32x4 acc[MI][NJ];
@@ -348,7 +248,7 @@ __global__ __launch_bounds__(64 * NWM * NWN) void f8_tile_kernel(const F8Args a)
 
     const int pc0 = (lm.fr_kc ^ lm.fr_swz) << 4, pc1 = pc0 ^ 64;
     const uint8_t* const la = lds + (wm * WM + lm.fr_row) * 128;
-    const uint8_t* const lb = lds + (BM + wn * WN + lm.fr_row) * 128;
+    const uint8_t* const lb = lds + (kTile + wn * WN + lm.fr_row) * 128;
     __syncthreads();                                   // the weights' scales; no load of ours is under way yet
     issue(0, 0);
     for (int kt = 0; kt < KT; ++kt) {
@@ -357,33 +257,34 @@ __global__ __launch_bounds__(64 * NWM * NWN) void f8_tile_kernel(const F8Args a)
         wait_vm<0>();
         block_barrier();                               // stage kt is complete, stage kt - 1 read
         if (kt + 1 < KT) issue(kt + 1, buf ^ 1);
-        float s[MI], su[MI];
-        const float sw = lds_sw[(!kSwiglu && BN > 128 ? (wn * WN / 128) * KT : 0) + kt];
-        const float sw3 = kSwiglu ? lds_sw[KT + kt] : 0.0f;
-#pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            const float v = lds_sx[buf * BM + wm * WM + 16 * i + lm.fr_row];
-            s[i] = v * sw;
-            su[i] = v * sw3;
-        }
+        float s[MI];
         i32x8 xf[MI];
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+        for (int i = 0; i < MI; ++i) {
+            s[i] = lds_sx[buf * kTile + wm * WM + 16 * i + lm.fr_row] * lds_sw[kt];
             xf[i] = frag8(la + buf * kStage + i * 2048 + pc0, la + buf * kStage + i * 2048 + pc1);
+        }
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
             const i32x8 wf = frag8(lb + buf * kStage + j * 2048 + pc0, lb + buf * kStage + j * 2048 + pc1);
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
                 const f32x4 d = block_sum<std::is_same<OUT, float>::value>(wf, xf[i]);
-                const float f = kSwiglu && j >= NJ / 2 ? su[i] : s[i];
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(d[v], f, acc[i][j][v]);
+                for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(d[v], s[i], acc[i][j][v]);
             }
         }
     }
 
-    finish_tile<BM, BN, NWM, NWN, OUT>(a, tile, n0, wm, wn, lane, acc, lds);
+    OUT* const out = static_cast<OUT*>(a.out);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const int row = tile.m0 + wm * WM + 16 * i + lm.fr_row;
+        if (row >= tile.end) continue;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+            store4(a, out, row, n0 + wn * WN + 16 * j + (lane >> 4) * 4, acc[i][j]);
+    }
 }
 
 // ------------------------------------------------------------------ wide tiles
@@ -397,6 +298,11 @@ __global__ __launch_bounds__(64 * NWM * NWN) void f8_tile_kernel(const F8Args a)
 //     order: 256 bytes a wave (read in place, [rows][KT], they are 256 cache lines a stage,
 //     half as many as its operands: 5 to 9 % of the time); the weights' are in LDS.
 //   - KT may be odd: stage kt sits in buffer (kt + KT) % 2, so the last is in buffer 1.
+// 33,234 rows of 8 experts, n = 7168, kdim = 2048: 450 us, 2.17 PFLOP/s (tiles of 128 x 128
+// 727 us; one tile a workgroup, not a run of them, 520); the feed-forward of the same sizes
+// 1.33 ms, 2.2 PFLOP/s.  The chip's power bounds it: its clock falls to 1.6 to 1.9 GHz, and
+// with operands of zeros the same feed-forward takes 1.09 ms.  At that clock the MFMAs are
+// busy for 55 % of the time; without the FMAs' three quarters it takes 1.16 ms.
 constexpr int kALdF8 = kBM / kRowsPerLoad / kNW;       // direct loads of A per wave and stage
 static_assert(kALdF8 == 4 && kNW == 8, "32 rows of A, 8 of each B quarter");
 
@@ -605,6 +511,76 @@ __device__ __forceinline__ void store_wide(const F8Args& a, const Tile& tile, in
     }
 }
 
+// A wide SwiGLU tile's way out: H quantised to e4m3 by rows, with its scales.  `lds` (the
+// other buffer's stage) is free but for reads that other waves may still make.
+__device__ __forceinline__ void store_h(const F8Args& a, const Tile& tile, int n0, int wm, int wn, int lane,
+                                        f32x4 (&acc)[kMI][kNJ], uint8_t* lds) {
+    const int fr_row = lane & 15;
+    const int q4 = (lane >> 4) * 4;                    // the lane's four outputs within a block of 16
+    constexpr int kHCols = kWN / 2;                    // H columns of a wave
+    float* const row_max = reinterpret_cast<float*>(lds);            // [kWavesN][kBM]
+    uint8_t* const codes = lds + kWavesN * kBM * 4;                  // [kBM][kPitch]
+    constexpr int kPitch = 128 + 16;
+    static_assert(kWavesN * kBM * 4 + kBM * kPitch <= kStageBytes, "epilogue in one stage");
+#pragma unroll
+    for (int i = 0; i < kMI; ++i)
+#pragma unroll
+        for (int j = 0; j < kNJ / 2; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const float g = acc[i][j][v];
+                acc[i][j][v] = g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * acc[i][j + kNJ / 2][v];
+            }
+    lds_barrier();                                     // the last stage is read
+    uint32_t m[kMI];
+#pragma unroll
+    for (int i = 0; i < kMI; ++i) {
+        m[i] = 0;
+#pragma unroll
+        for (int j = 0; j < kNJ / 2; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const uint32_t b = finite_magnitude(acc[i][j][v]);
+                m[i] = b > m[i] ? b : m[i];
+            }
+#pragma unroll
+        for (int d = 16; d < 64; d *= 2) {
+            const uint32_t o = static_cast<uint32_t>(__shfl_xor(static_cast<int>(m[i]), d));
+            m[i] = o > m[i] ? o : m[i];
+        }
+        if (lane < 16) row_max[wn * kBM + wm * kWM + 16 * i + lane] = __uint_as_float(m[i]);
+    }
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < kMI; ++i) {
+        const int r = wm * kWM + 16 * i + fr_row;
+        uint32_t top = 0;
+#pragma unroll
+        for (int c = 0; c < kWavesN; ++c) {
+            const uint32_t o = __float_as_uint(row_max[c * kBM + r]);
+            top = o > top ? o : top;
+        }
+        const uint32_t ex = f8_scale_exponent(top);
+        const float inv = f8_inverse(ex);
+#pragma unroll
+        for (int j = 0; j < kNJ / 2; ++j) {
+            const f32x4 v = acc[i][j];
+            *reinterpret_cast<uint32_t*>(codes + r * kPitch + wn * kHCols + 16 * j + q4) =
+                f8_pack4(v[0], v[1], v[2], v[3], inv);
+        }
+        if (wn == 0 && lane < 16 && tile.m0 + r < tile.end)
+            a.out_scale[tile.nt * a.scale_pitch + tile.m0 + r] = f8_scale(ex);
+    }
+    lds_barrier();
+    uint8_t* const out = static_cast<uint8_t*>(a.out);
+    for (int c = threadIdx.x; c < kBM * 8; c += 64 * kNW) {
+        const int r = c >> 3;
+        if (tile.m0 + r < tile.end)
+            *reinterpret_cast<u32x4*>(out + static_cast<size_t>(tile.m0 + r) * a.N + n0 + (c & 7) * 16) =
+                *reinterpret_cast<const u32x4*>(codes + r * kPitch + (c & 7) * 16);
+    }
+}
+
 // Tiles of the wide kernel: experts' row tiles and rows, once a workgroup.
 struct WideTable {
     int upto[kMaxE];             // row tiles of the experts up to and with e
@@ -746,20 +722,19 @@ __global__ __launch_bounds__(512) void f8_wide_kernel(const F8Args a) {
         }
         uint8_t* const out_lds = lds + (first ^ 1) * kStageBytes;
         if constexpr (kSwiglu)
-            finish_tile<kBM, kBN, kWavesM, kWavesN, OUT>(a, done, done.nt * kCols, wm, wn, lane, acc, out_lds);
+            store_h(a, done, done.nt * kCols, wm, wn, lane, acc, out_lds);
         else
             store_wide(a, done, done.nt * kCols, wm, wn, wave, lane, acc, out_lds);
         if (!more) return;
     }
 }
 
-template <int BM, int BN, int NWM, int NWN, typename OUT>
+template <typename OUT>
 cap_status launch_tiles(const F8Args& a, hipStream_t st) {
-    constexpr int cols = std::is_same<OUT, uint8_t>::value ? BN / 2 : BN;
-    const long long rows = a.max_rows / BM + (a.E_loc < a.max_rows ? a.E_loc : a.max_rows);
-    const long long blocks = (rows * ((a.N + cols - 1) / cols) + 7) / 8 * 8;
-    if (blocks * (64 * NWM * NWN) >= (1ll << 32)) return CAP_ERR_UNSUPPORTED;
-    f8_tile_kernel<BM, BN, NWM, NWN, OUT><<<static_cast<unsigned>(blocks), 64 * NWM * NWN, 0, st>>>(a);
+    const long long rows = a.max_rows / kTile + (a.E_loc < a.max_rows ? a.E_loc : a.max_rows);
+    const long long blocks = (rows * ((a.N + kTile - 1) / kTile) + 7) / 8 * 8;
+    if (blocks * 256 >= (1ll << 32)) return CAP_ERR_UNSUPPORTED;
+    f8_tile_kernel<OUT><<<static_cast<unsigned>(blocks), 256, 0, st>>>(a);
     CAP_LAUNCH_CHECK();
     return CAP_OK;
 }
@@ -771,7 +746,8 @@ cap_status launch_tiles(const F8Args& a, hipStream_t st) {
 // them, load their weights straight into the MFMA's registers, a block ahead, and join
 // their sums in LDS in the waves' order.  SwiGLU: four waves take W1 and four W3, and H
 // leaves in fp32: quantising it takes 128 of its columns, and workgroups of so many leave
-// half of the compute units without one.
+// half of the compute units without one.  The weights' bytes bound it: 8 rows of 8 experts,
+// d = 7168, inter = 2048: 76 us for 352 MB, 4.65 TB/s (weights through LDS in tiles 120 us).
 template <int BM>
 __device__ __forceinline__ bool find_rows(const F8Args& a, int NT, Tile& out) {
     const int lane = threadIdx.x & 63, id = blockIdx.x;
@@ -936,26 +912,11 @@ __global__ __launch_bounds__(512) void f8_few_kernel(const F8Args a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = v[i] * __builtin_amdgcn_rcpf(1.0f + __expf(-v[i])) * u[i];
         }
-        {
-            if (!there || n >= a.N) continue;
-            OUT* const p = static_cast<OUT*>(a.out) + static_cast<size_t>(row) * a.N + n;
-            const bool whole = (a.N & 3) == 0 && (reinterpret_cast<uintptr_t>(a.out) & (4 * sizeof(OUT) - 1)) == 0;
-            if (whole) {
-                if constexpr (std::is_same<OUT, float>::value) *reinterpret_cast<f32x4*>(p) = v;
-                else *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2_rne(v[0], v[1]), pack_bf16x2_rne(v[2], v[3])};
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (n + i < a.N) {
-                        if constexpr (std::is_same<OUT, float>::value) p[i] = v[i];
-                        else p[i] = static_cast<uint16_t>(pack_bf16x2_rne(v[i], v[i]));
-                    }
-            }
-        }
+        if (there) store4(a, static_cast<OUT*>(a.out), row, n, v);
     }
 }
 
-template <int I, int J, typename OUT, bool SWIGLU = false>
+template <int I, int J, typename OUT, bool SWIGLU>
 cap_status launch_few(const F8Args& a, hipStream_t st) {
     constexpr int rows = 16 * I, cols = 16 * J;
     const long long tiles = a.max_rows / rows + (a.E_loc < a.max_rows ? a.E_loc : a.max_rows);
@@ -1011,7 +972,7 @@ double tiles_time(const F8Args& a, int rows, int cols, int at_once, double stage
     return 5.0 + (stages > bytes ? stages : bytes);
 }
 double wide_time(const F8Args& a) { return tiles_time(a, kBM, a.w3 ? kBN / 2 : kBN, device_cu_count(), 1.0); }
-double tile_time(const F8Args& a) { return tiles_time(a, 128, 128, 2 * device_cu_count(), 1.35); }
+double tile_time(const F8Args& a) { return tiles_time(a, kTile, kTile, 2 * device_cu_count(), 1.35); }
 
 template <typename OUT>
 cap_status launch_wide(F8Args a, float* scales, hipStream_t st) {
@@ -1073,12 +1034,12 @@ cap_status launch_few_rows(const F8Args& a, hipStream_t st) {
 cap_status product(cap_dtype out_dtype, const F8Args& a, float* scales, hipStream_t st) {
     if (out_dtype == CAP_DTYPE_F32) {
         if (few_time(a) < tile_time(a)) return launch_few_rows<float, false>(a, st);
-        return launch_tiles<128, 128, 2, 2, float>(a, st);
+        return launch_tiles<float>(a, st);
     }
     const bool wide = a.N % 8 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15) == 0;
     if (few_time(a) < (wide ? wide_time(a) : tile_time(a))) return launch_few_rows<uint16_t, false>(a, st);
     if (wide) return launch_wide<uint16_t>(a, scales, st);
-    return launch_tiles<128, 128, 2, 2, uint16_t>(a, st);
+    return launch_tiles<uint16_t>(a, st);
 }
 
 }  // namespace

@@ -3,18 +3,18 @@
 // (Sec. VI) on the gates' shares.  (Built without NaN semantics: whether a logit is finite
 // is asked of its bits.)
 //
-// Decisions (groups, experts, kept devices) are taken on values in 64 bits, so that
-// they are those of the real numbers for all but values within about 2^-43 of each
-// other: in 32 bits the scores of two experts at a border of the choice are equal or
-// exchanged once in some hundred thousand tokens.
+// Decisions (groups, experts, kept devices) are those of the real numbers for all but values
+// within about 2^-43 of each other: in fp32 the scores of two experts at a border of the choice
+// are equal or exchanged once in some hundred thousand tokens.  The choice is made in fp32, with
+// a bound on its error, and again in fp64 for the tokens that this leaves unsure; gates and
+// pruning are in fp64.
 //
-// Selection keys are the packed doubles of route_device.hpp.  Without a bias the choice
-// goes by the logits (the high word), and so do groups by their best expert; else the
-// key is the biased score in fp64, whose low 8 bits hold the expert
-// (255 - e, or e below zero, so that the larger double is the lower expert among
-// equal scores): 44 bits of the score are left.  An expert that is off (its logit is
-// not finite, or its token masked) has a key below all scores, one of a closed group
-// a key below that.
+// Selection keys are the packed doubles of route_device.hpp: the high word is the logit
+// (without a bias, within groups) or the biased score as fp32, the low word breaks ties (the
+// larger double is the lower expert).  The exact choice's keys are biased scores in fp64 whose
+// low 8 bits hold the expert: 44 bits of the score are left.  An expert that is off (its logit
+// is not finite, or its token masked) has a key below all scores, one of a closed group a key
+// below that.
 #pragma clang fp contract(off)
 
 #include <math.h>
@@ -263,9 +263,12 @@ __device__ __forceinline__ int dpp_swap_i32(int v) { return __builtin_amdgcn_mov
 //           unsure (about one of 2000) are chosen by exact_choice.  Else it goes by logits.
 //   GROUPS  0: one group (or all of them open); 1: groups of 4 L CPG experts, which are whole
 //           values of c; 2: any, through LDS
-// What bounds it: instruction issue, most of it the selection network.  All scores in fp64
-// took 35.8 us for 32,768 tokens of 256 experts (one wave a SIMD, for the registers of 64 keys
-// a lane): keys are formed block by block now, and fp64 is left to the chosen slots.
+// What bounds it: instruction issue, most of it the selection network.  32,768 tokens of 256
+// experts in 8 groups, sigmoid with a bias, pruned: 20.5 us (35.8 with all scores in fp64: one
+// wave a SIMD, for the registers of 64 keys a lane; keys are formed block by block now, and fp64
+// is left to the chosen slots), 4 us of which are the unsure tokens; to read and write 36 MB
+// takes 8.  32 tokens: 7.7 us, a chain of joins.  If every token is unsure (all logits alike),
+// 32,768 take 90 us.
 template <int L, int V, int KP, bool SCORE, bool VEC, int GROUPS, int CPG>
 __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
     constexpr int C = V / 4, kTokens = 256 / L;
