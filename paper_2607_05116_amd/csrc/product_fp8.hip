@@ -40,6 +40,7 @@ struct F8Args {
     float* out_scale;            // SwiGLU: [N / 128][scale_pitch]
     size_t sx_row, sx_block, scale_pitch;
     int x_rows, E_loc, max_rows, N, KT;
+    bool sx_in_order;            // wide: sx is [KT][sx_block] in the rows' order
 };
 
 // 4-byte form of lds_dma16: lane i's dword lands at LDS byte lds_addr + 4 i.
@@ -179,8 +180,8 @@ __device__ __forceinline__ void lds_barrier() {
     block_barrier();
 }
 
-// One tile of 128 rows x 128 weight rows, four waves of 64 x 64; K in stages of 128, double
-// buffered, one barrier a stage.  For fp32 results, and for bf16 ones whose rows the wide
+// One tile of 128 rows x 128 weight rows, four waves of 64 x 64; K in stages of 128, two of
+// them on their way: a stage's fragments are read at once, then its buffer is filled again.  For fp32 results, and for bf16 ones whose rows the wide
 // kernel cannot load or store (n % 8 or y's address).  OUT: uint16_t (bf16) or float.
 template <typename OUT>
 __global__ __launch_bounds__(256) void f8_tile_kernel(const F8Args a) {
@@ -203,6 +204,7 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(const F8Args a) {
 
     // direct loads: lane l of a load writes row l / 8 of its 8 rows, chunk l % 8
     const LaneMap lm = lane_map(lane);
+    const uint32_t col_b = wave & 1 ? lm.col_b[1] : lm.col_b[0];
     auto source_row = [&](int r) {               // tile row -> row of x; rows past the end repeat the last
         int row = tile.m0 + r;
         row = row < tile.end ? row : tile.end - 1;
@@ -220,12 +222,12 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(const F8Args a) {
         dst[i] = c * 1024;
         if (c < kTile / 8) {
             base[i] = reinterpret_cast<const char*>(a.x);
-            off[i] = static_cast<uint32_t>(source_row(8 * c + lm.ld_row)) * static_cast<uint32_t>(K) + lm.col_b[c & 1];
+            off[i] = static_cast<uint32_t>(source_row(8 * c + lm.ld_row)) * static_cast<uint32_t>(K) + col_b;
         } else {
             int n = n0 + 8 * (c - kTile / 8) + lm.ld_row;
             n = n < a.N ? n : a.N - 1;
             base[i] = reinterpret_cast<const char*>(a.w1 + static_cast<size_t>(tile.e) * a.N * K);
-            off[i] = static_cast<uint32_t>(n) * static_cast<uint32_t>(K) + lm.col_b[c & 1];
+            off[i] = static_cast<uint32_t>(n) * static_cast<uint32_t>(K) + col_b;
         }
     }
     uint32_t sx_off = 0;
@@ -251,39 +253,63 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(const F8Args a) {
     const uint8_t* const lb = lds + (kTile + wn * WN + lm.fr_row) * 128;
     __syncthreads();                                   // the weights' scales; no load of ours is under way yet
     issue(0, 0);
+    if (KT > 1) issue(1, 1);
     for (int kt = 0; kt < KT; ++kt) {
         const int buf = kt & 1;
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        wait_vm<0>();
-        block_barrier();                               // stage kt is complete, stage kt - 1 read
-        if (kt + 1 < KT) issue(kt + 1, buf ^ 1);
+        if (kt + 1 < KT) wait_vm<kChunksW>();          // stage kt has landed (the next, of as many loads or one more, may not have)
+        else wait_vm<0>();
+        block_barrier();
         float s[MI];
-        i32x8 xf[MI];
+        i32x8 xf[MI], wf[NJ];
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             s[i] = lds_sx[buf * kTile + wm * WM + 16 * i + lm.fr_row] * lds_sw[kt];
             xf[i] = frag8(la + buf * kStage + i * 2048 + pc0, la + buf * kStage + i * 2048 + pc1);
         }
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const i32x8 wf = frag8(lb + buf * kStage + j * 2048 + pc0, lb + buf * kStage + j * 2048 + pc1);
+        for (int j = 0; j < NJ; ++j) wf[j] = frag8(lb + buf * kStage + j * 2048 + pc0, lb + buf * kStage + j * 2048 + pc1);
+        lds_barrier();                                 // read by all waves
+        if (kt + 2 < KT) issue(kt + 2, buf);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
-                const f32x4 d = block_sum<std::is_same<OUT, float>::value>(wf, xf[i]);
+                const f32x4 d = block_sum<std::is_same<OUT, float>::value>(wf[j], xf[i]);
 #pragma unroll
                 for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(d[v], s[i], acc[i][j][v]);
             }
-        }
     }
 
+    // out by rows: a wave turns 16 of its rows at a time, in LDS of its own
+    constexpr int kPitch = WN + 4;
+    float* const mine = reinterpret_cast<float*>(lds) + wave * 16 * kPitch;
     OUT* const out = static_cast<OUT*>(a.out);
+    const int n = n0 + wn * WN;
+    const bool fours = (a.N & 3) == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(OUT) - 1)) == 0;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-        const int row = tile.m0 + wm * WM + 16 * i + lm.fr_row;
-        if (row >= tile.end) continue;
+        const int m = tile.m0 + wm * WM + 16 * i;
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
-            store4(a, out, row, n0 + wn * WN + 16 * j + (lane >> 4) * 4, acc[i][j]);
+            *reinterpret_cast<f32x4*>(mine + lm.fr_row * kPitch + 16 * j + (lane >> 4) * 4) = acc[i][j];
+        __builtin_amdgcn_wave_barrier();
+        if (fours) {
+#pragma unroll
+            for (int r = lane >> 4; r < 16; r += 4) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(mine + r * kPitch + 4 * (lane & 15));
+                if (m + r < tile.end) store4(a, out, m + r, n + 4 * (lane & 15), v);
+            }
+        } else if (n + lane < a.N) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float v = mine[r * kPitch + lane];
+                OUT* const p = out + static_cast<size_t>(m + r) * a.N + n + lane;
+                if (m + r >= tile.end) break;
+                if constexpr (std::is_same<OUT, float>::value) *p = v;
+                else *p = static_cast<uint16_t>(pack_bf16x2_rne(v, v));
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -294,9 +320,9 @@ __global__ __launch_bounds__(256) void f8_tile_kernel(const F8Args a) {
 //   - The FMAs that scale and add an MFMA's sums follow two MFMAs later, so that they never
 //     wait for it (right after the next one they did, for 28 cycles of every 64).
 //   - All waves load: each 32 rows of A and 8 of each quarter of B a stage.
-//   - Activation scales come with a stage's B quarters 0, 1, from [KT][rows] in the rows'
-//     order: 256 bytes a wave (read in place, [rows][KT], they are 256 cache lines a stage,
-//     half as many as its operands: 5 to 9 % of the time); the weights' are in LDS.
+//   - Activation scales come with a stage's B quarters 0, 1: in place ([rows][KT], 256 cache
+//     lines a stage, half as many as its operands), or, in long calls with long rows, from
+//     [KT][rows] in the rows' order, 256 bytes a wave; the weights' are in LDS.
 //   - KT may be odd: stage kt sits in buffer (kt + KT) % 2, so the last is in buffer 1.
 // 33,234 rows of 8 experts, n = 7168, kdim = 2048: 450 us, 2.17 PFLOP/s (tiles of 128 x 128
 // 727 us; one tile a workgroup, not a run of them, 520); the feed-forward of the same sizes
@@ -654,12 +680,20 @@ __global__ __launch_bounds__(512) void f8_wide_kernel(const F8Args a) {
     const int col = wave >> 2, sub = wave & 3;         // B: wave column and eighths of a quarter's 32 rows
     WideLoads ld = {};
     ld.s_step = a.sx_block * 4;
-    ld.s_off = lane * 4;
     ld.a_lds = lds_base + wave * kALdF8 * 1024;
     ld.b_lds = lds_base + (kBM + col * kWN + sub * kRowsPerLoad) * kRowB;
     ld.s_lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)lds_sx)) + (wave >> 1) * kWM * 4;
     ld.b_off = lm.ld_row * K + (sub & 1 ? lm.col_b[1] : lm.col_b[0]);
     const float* const sx = lds_sx + wm * kWM + lm.fr_row;
+    auto source_row = [&](const Tile& tile, int r) {   // rows past the end repeat the last
+        int row = tile.m0 + r;
+        row = row < tile.end ? row : tile.end - 1;
+        if (a.row_src) {
+            row = a.row_src[row];
+            row = row < 0 ? 0 : row < a.x_rows ? row : a.x_rows - 1;
+        }
+        return row;
+    };
     // a tile's operands, its first stage, and the weights' scales
     auto begin = [&](const Tile& tile, float* sw) {
         const int n0 = tile.nt * kCols;
@@ -674,17 +708,17 @@ __global__ __launch_bounds__(512) void f8_wide_kernel(const F8Args a) {
         ld.b[2] = rows_at(kSwiglu ? a.w3 : a.w1, kSwiglu ? n : n + 64);
         ld.b[3] = rows_at(kSwiglu ? a.w3 : a.w1, kSwiglu ? n + 32 : n + 96);
         ld.a = reinterpret_cast<const char*>(a.x);
-        ld.s = reinterpret_cast<const char*>(a.sx + tile.m0 + (wave >> 1) * kWM);
-#pragma unroll
-        for (int i = 0; i < kALdF8; ++i) {
-            int row = tile.m0 + wave * 8 * kALdF8 + i * kRowsPerLoad + lm.ld_row;     // rows past the end repeat the last
-            row = row < tile.end ? row : tile.end - 1;
-            if (a.row_src) {
-                row = a.row_src[row];
-                row = row < 0 ? 0 : row < a.x_rows ? row : a.x_rows - 1;
-            }
-            ld.a_off[i] = static_cast<uint32_t>(row) * K + lm.col_b[i & 1];
+        if (a.sx_in_order) {
+            ld.s = reinterpret_cast<const char*>(a.sx + tile.m0 + (wave >> 1) * kWM);
+            ld.s_off = lane * 4;
+        } else {
+            ld.s = reinterpret_cast<const char*>(a.sx);
+            ld.s_off = static_cast<uint32_t>(source_row(tile, (wave >> 1) * kWM + lane)) * KT * 4;
         }
+#pragma unroll
+        for (int i = 0; i < kALdF8; ++i)
+            ld.a_off[i] = static_cast<uint32_t>(source_row(tile, wave * 8 * kALdF8 + i * kRowsPerLoad + lm.ld_row)) * K +
+                          lm.col_b[i & 1];
         const size_t at = (static_cast<size_t>(tile.e) * NB + n0 / 128) * KT;
         float w0 = 0.0f, w1 = 0.0f;
         if (static_cast<int>(threadIdx.x) < KT) {
@@ -946,9 +980,10 @@ size_t f8_scales_bytes(int k, int max_rows) { return f8_scale_pitch(max_rows) * 
 
 // Which kernel a call takes goes by estimates of its time in microseconds, from its sizes
 // alone (max_rows for the rows, as if they fell about evenly; every kernel is right for any).
-// Measured, estimates in brackets: E = 8, n = 2048, kdim = 7168, 64 rows: few 21.5 (25), wide
-// 56 (61); 256 rows: 47 (47), 57 (61); n = 7168, kdim = 2048, 64 rows: 24.5 (25), 25.4 (28); 256
-// rows: 42 (42), 26 (28); E = 1, n = 1003, kdim = 2048, fp32, 16 rows: few 6.9 (4), tiles 24 (26).
+// Measured, estimates in brackets: E = 8, n = 2048, kdim = 7168, 64 rows: few 21.7 (27), wide 56
+// (61); 256 rows: 47 (50), 57 (61); n = 7168, kdim = 2048, 64 rows: few 24.5 (27), wide 22.9 (28);
+// 256 rows: 42 (50), 23.7 (28); E = 7, 6,126 rows, n = 267, kdim = 2304: few 36 (31), tiles 26.5
+// (26).
 constexpr int kFewFfnRows = 8192;                      // the feed-forward's workspace has room for so many rows of H in fp32
 long long likely_tiles(const F8Args& a, int rows) {    // row tiles, experts' sizes differing by a factor of three
     const long long some = a.E_loc < a.max_rows ? a.E_loc : a.max_rows, more = a.max_rows - 8ll * a.E_loc;
@@ -961,8 +996,10 @@ bool few_fill(const F8Args& a, int rows, int cols) {
 // 32 rows a workgroup once most experts have more than 8 rows.
 bool few_take_32(const F8Args& a) { return a.max_rows > 8ll * a.E_loc && few_fill(a, 32, 64); }
 double weight_bytes(const F8Args& a) { return static_cast<double>(a.w3 ? 2 : 1) * a.N * a.KT * 128; }
-double few_time(const F8Args& a) {                     // the weights' way, again for each row tile
-    return 3.5 + static_cast<double>(likely_tiles(a, few_take_32(a) ? 32 : 16)) * weight_bytes(a) / 5.5e6;
+double few_time(const F8Args& a) {                     // the weights' way, again for each row tile, and that of the rows (from nearer)
+    const int rows = few_take_32(a) ? 32 : 16;
+    const double row_bytes = static_cast<double>(rows) * a.KT * 128 * ((a.N + 63) / 64);
+    return 3.5 + static_cast<double>(likely_tiles(a, rows)) * (weight_bytes(a) + 0.5 * row_bytes) / 5.5e6;
 }
 // Tiles: a round of them takes so long a stage, but no less than the weights' way.
 double tiles_time(const F8Args& a, int rows, int cols, int at_once, double stage) {
@@ -972,8 +1009,12 @@ double tiles_time(const F8Args& a, int rows, int cols, int at_once, double stage
     return 5.0 + (stages > bytes ? stages : bytes);
 }
 double wide_time(const F8Args& a) { return tiles_time(a, kBM, a.w3 ? kBN / 2 : kBN, device_cu_count(), 1.0); }
-double tile_time(const F8Args& a) { return tiles_time(a, kTile, kTile, 2 * device_cu_count(), 1.35); }
+double tile_time(const F8Args& a) { return 1.5 + tiles_time(a, kTile, kTile, device_cu_count(), 1.1); }
 
+// From so many stages on a launch that puts the scales in order is worth its 5 us, if a row's
+// scales are more than a line of 128 bytes (d = 7168, 33,234 rows: the feed-forward 1.36 ms, in
+// place 1.40; the product of kdim = 2048 468 us, in place 459).
+constexpr int kStagesInOrder = 128;
 template <typename OUT>
 cap_status launch_wide(F8Args a, float* scales, hipStream_t st) {
     constexpr int cols = std::is_same<OUT, uint8_t>::value ? kBN / 2 : kBN;
@@ -982,12 +1023,13 @@ cap_status launch_wide(F8Args a, float* scales, hipStream_t st) {
     if (tiles >= (1ll << 31)) return CAP_ERR_UNSUPPORTED;
     const long long cus = (device_cu_count() + 7) / 8 * 8;             // one workgroup a CU
     const long long blocks = tiles < cus ? (tiles + 7) / 8 * 8 : cus;
-    if (scales) {                                      // else a.sx is in the rows' order, whole tiles of them
+    if (!a.sx_in_order && a.KT > 32 && (tiles + cus - 1) / cus * a.KT >= kStagesInOrder) {
         const size_t pitch = f8_scale_pitch(a.max_rows);
         f8_gather_scales_kernel<<<(a.max_rows + 63) / 64, 256, 0, st>>>(a, scales, pitch);
         a.sx = scales;
         a.sx_row = 1;
         a.sx_block = pitch;
+        a.sx_in_order = true;
     }
     f8_wide_kernel<OUT><<<static_cast<unsigned>(blocks), 512, 0, st>>>(a);
     CAP_LAUNCH_CHECK();
@@ -1030,7 +1072,7 @@ cap_status launch_few_rows(const F8Args& a, hipStream_t st) {
     return launch_few<1, 2, OUT, SWIGLU>(a, st);
 }
 
-// scales: room for those of the rows in their order; nullptr: a.sx holds them so.
+// scales: room for those of the rows in their order.
 cap_status product(cap_dtype out_dtype, const F8Args& a, float* scales, hipStream_t st) {
     if (out_dtype == CAP_DTYPE_F32) {
         if (few_time(a) < tile_time(a)) return launch_few_rows<float, false>(a, st);
@@ -1109,6 +1151,7 @@ cap_status expert_ffn_fp8_launch(int E_loc, int d, int inter, int max_rows, cons
     a.sx = h_scales;
     a.sx_row = few ? inter / 128 : 1;
     a.sx_block = few ? 1 : a.scale_pitch;
+    a.sx_in_order = !few;
     a.row_src = nullptr;
     a.w1 = static_cast<const uint8_t*>(w2);
     a.s1 = s2;
@@ -1117,7 +1160,7 @@ cap_status expert_ffn_fp8_launch(int E_loc, int d, int inter, int max_rows, cons
     a.x_rows = max_rows;
     a.N = d;
     a.KT = inter / 128;
-    return product(CAP_DTYPE_BF16, a, few ? scales : nullptr, st);
+    return product(CAP_DTYPE_BF16, a, scales, st);
 }
 
 }  // namespace cap
