@@ -179,10 +179,11 @@ int32_t cap_version(void);
  *   CAP_OP_ORTHOGONALISE: the products of cap_orthogonalise and cap_muon_update
  *                      (inter is rows, d is cols, max_rows is the batch; topo
  *                      unused, may be NULL).
- *   CAP_OP_PRODUCT_FP8: partial sums of cap_product_fp8 (d is n, inter is kdim;
- *                      topo unused).
+ *   CAP_OP_PRODUCT_FP8: cap_product_fp8's scales of x in the rows' order (d is n,
+ *                      inter is kdim; topo unused).
  *   CAP_OP_EXPERT_FFN_FP8: the intermediate H of cap_expert_ffn_fp8 in e4m3 with
- *                      its scales, and partial sums (topo unused).
+ *                      its scales (few rows: in fp32 too), and scales in the rows'
+ *                      order (topo unused).
  *   Other ops need none.
  * Returns 0 for invalid arguments as well.
  */
@@ -668,7 +669,7 @@ typedef struct {
  * equal.  Scores below 1e-300 are 0; gates are rounded to fp32 once (those of a softmax
  * without normalise carry the error of its sum of fp32 exponentials, below 2^-20).
  * Outputs as cap_route_prune: idx[T][k] in the order of step 2, w, keep, dst_mask.
- * No workspace.
+ * T < 2^29.  No workspace.
  */
 cap_status cap_route_scores(const cap_topology *topo, const float *logits, const cap_score_options *options, float p,
                             int32_t *idx, float *w, uint8_t *keep, uint64_t *dst_mask, void *stream);
@@ -687,7 +688,7 @@ cap_status cap_route_scores(const cap_topology *topo, const float *logits, const
  *   softmax, not:  (g_s for a kept slot's expert) - P_e G for every expert that is on.
  * d_logits[T][E] (fp32 or bf16) is d_add (or 0) elsewhere.  logits may be NULL for
  * softmax with normalise.  Slots whose idx is outside [0, E) are skipped.  0 <= T,
- * T * k < 2^31, 1 <= k <= 8, k <= E <= 256.  No workspace.
+ * T < 2^29, T * k < 2^31, 1 <= k <= 8, k <= E <= 256.  No workspace.
  */
 cap_status cap_route_scores_grad(int32_t T, int32_t k, int32_t E, const float *logits, const int32_t *idx,
                                  const uint8_t *keep, const float *w, const float *d_w,
@@ -727,7 +728,8 @@ cap_status cap_quantise_fp8(cap_dtype dtype, int32_t batch, int32_t rows, int32_
  * Sums are fp32.  With a bf16 result the matrix cores' 8-bit instructions are used,
  * which drop, within each eight neighbours along K, what is below 2^-13 of the largest
  * product (about 1.4e-5 of y on normal values, 1 / 280 of a bf16 result's step); with
- * an fp32 result their bf16 instructions, in which products are exact.  kdim % 128 == 0, 128 <= kdim <= 2^15; 1 <= n; E_loc <= 256;
+ * an fp32 result their bf16 instructions, in which products are exact.
+ * kdim % 128 == 0, 128 <= kdim <= 2^15; 1 <= n; E_loc <= 256; max_rows < 2^30;
  * x_rows * kdim and n * kdim < 2^32.  Workspace: cap_workspace_size(CAP_OP_PRODUCT_FP8,
  * NULL, n, kdim, max_rows, ...), 256-byte aligned (may be NULL if that is 0).
  */

@@ -122,11 +122,15 @@ bool orth_shape_ok(int batch, int rows, int cols) {
            cols <= kMaxOrthSide;
 }
 
+// Tokens routed by scores: threads of a launch (eight a token).
+constexpr int kMaxScoreTokens = 1 << 29;
+
 // Sizes of the products in 8 bits: whole scale blocks along K, and row offsets (in
 // bytes, within an expert's weights or the rows) of 32 bits.
+constexpr int kMaxF8Rows = 1 << 30;          // threads of a launch, and row numbers past the last tile
 bool f8_k_ok(int k) { return k >= kF8Block && k <= kF8MaxK && k % kF8Block == 0; }
 bool f8_product_ok(int n, int k, long long max_rows) {
-    return n >= 1 && f8_k_ok(k) && max_rows >= 0 && static_cast<long long>(n) * k < (1ll << 32);
+    return n >= 1 && f8_k_ok(k) && max_rows >= 0 && max_rows < kMaxF8Rows && static_cast<long long>(n) * k < (1ll << 32);
 }
 bool f8_ffn_ok(int d, int inter, long long max_rows) {
     return f8_k_ok(d) && f8_k_ok(inter) && max_rows >= 0 && max_rows * inter < (1ll << 32);
@@ -511,7 +515,7 @@ cap_status f8_rows_check(int32_t E_loc, int32_t k, int32_t max_rows, const void*
     if (max_rows == 0) return CAP_OK;
     if (!x || !x_scale || x_rows < 1 || (!row_src && x_rows < max_rows)) return CAP_ERR_INVALID_ARG;
     if (!aligned16(x) || !aligned4(x_scale) || !aligned4(row_src)) return CAP_ERR_INVALID_ARG;
-    if (static_cast<long long>(x_rows) * k >= (1ll << 32)) return CAP_ERR_UNSUPPORTED;
+    if (static_cast<long long>(x_rows) * k >= (1ll << 32) || max_rows >= kMaxF8Rows) return CAP_ERR_UNSUPPORTED;
     return CAP_OK;
 }
 
@@ -525,6 +529,7 @@ cap_status cap_route_scores(const cap_topology* topo, const float* logits, const
     if (!(p >= 0.0f) || !(p < 1.0f)) return CAP_ERR_INVALID_ARG;
     const cap_status st = score_options_check(options, topo->E, topo->k);
     if (st != CAP_OK) return st;
+    if (topo->T >= kMaxScoreTokens) return CAP_ERR_UNSUPPORTED;
     if (!aligned4(logits) || !aligned4(options->bias) || !aligned4(idx) || !aligned4(w) ||
         (reinterpret_cast<uintptr_t>(dst_mask) & 7) != 0)
         return CAP_ERR_INVALID_ARG;
@@ -541,6 +546,7 @@ cap_status cap_route_scores_grad(int32_t T, int32_t k, int32_t E, const float* l
     if (options->kind != CAP_SCORE_SOFTMAX && options->kind != CAP_SCORE_SIGMOID) return CAP_ERR_UNSUPPORTED;
     if (dtype != CAP_DTYPE_BF16 && dtype != CAP_DTYPE_F32) return CAP_ERR_UNSUPPORTED;
     if (!(options->scale > 0.0f) || !(options->scale < INFINITY)) return CAP_ERR_INVALID_ARG;
+    if (T >= kMaxScoreTokens) return CAP_ERR_UNSUPPORTED;
     if (T == 0) return CAP_OK;
     const bool reads_logits = options->kind == CAP_SCORE_SIGMOID || options->normalise == 0;
     if ((reads_logits && !logits) || !idx || !w || !d_w || !d_logits) return CAP_ERR_INVALID_ARG;

@@ -146,3 +146,16 @@ def test_ffn_workspace(capi):
     for over in (dict(ws=None), dict(ws=0x10080), dict(ws_bytes=need - 1)):
         assert _ffn(capi, **over) == capi.CAP_ERR_WORKSPACE
     assert _ffn(capi, max_rows=0, x=None, x_scale=None, x_rows=0, ws=None, w1=None, y=None) == capi.CAP_OK
+
+
+@pytest.mark.parametrize("T", [2 ** 29, 2 ** 31 - 8])
+def test_more_tokens_than_a_launch_has_threads_for(capi, T):
+    assert _route(capi, topo=dict(T=T, tokens_per_rank=T // 8, k=1)) == capi.CAP_ERR_UNSUPPORTED
+    assert _grad(capi, T=T, k=1) == capi.CAP_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("max_rows", [2 ** 30, 2 ** 31 - 1])
+@pytest.mark.parametrize("n", [1, 8])
+def test_more_rows_than_row_numbers_hold(capi, max_rows, n):
+    assert _product(capi, max_rows=max_rows, x_rows=1, row_src=0x7000, n=n, kdim=128) == capi.CAP_ERR_UNSUPPORTED
+    assert capi.cap_workspace_size(capi.CAP_OP_PRODUCT_FP8, None, n, 128, max_rows) == 0
