@@ -828,13 +828,21 @@ __device__ __forceinline__ bool find_rows(const F8Args& a, int NT, Tile& out) {
     return false;
 }
 
-template <int I, int J>
+template <int I, int J, bool H32>
 struct FewStage {
     i32x4 w[J][2], x[I][2];
     float sx[I], sw;
 };
+template <int I, int J>
+struct FewStage<I, J, true> {
+    i32x4 w[J][2];
+    f32x4 x[I][8];
+    float sw;
+};
 
-template <int I, int J, typename OUT, bool kSwiglu>
+// H32: the rows are H in fp32, quantised on their way to the MFMA, each block of 128 by the four
+// lanes that hold it (as the quantisation's kernel does, to the bit).
+template <int I, int J, typename OUT, bool kSwiglu, bool H32>
 __global__ __launch_bounds__(512) void f8_few_kernel(const F8Args a) {
     constexpr bool kPrecise = std::is_same<OUT, float>::value && !kSwiglu;
     constexpr int kParts = kSwiglu ? 4 : 8;            // waves that share K
@@ -858,8 +866,8 @@ __global__ __launch_bounds__(512) void f8_few_kernel(const F8Args a) {
         const int n = n0 + 16 * j + r16;
         w_off[j] = static_cast<uint32_t>(n < a.N ? n : a.N - 1) * static_cast<uint32_t>(K) + 16 * g;
     }
-    FewStage<I, J> st[2];
-    auto load_w = [&](FewStage<I, J>& s, int kt) {
+    FewStage<I, J, H32> st[2];
+    auto load_w = [&](FewStage<I, J, H32>& s, int kt) {
         const uint8_t* const p = w + static_cast<size_t>(kt) * 128;
 #pragma unroll
         for (int j = 0; j < J; ++j)
@@ -867,13 +875,19 @@ __global__ __launch_bounds__(512) void f8_few_kernel(const F8Args a) {
             for (int h = 0; h < 2; ++h) s.w[j][h] = *reinterpret_cast<const i32x4*>(p + w_off[j] + 64 * h);
         s.sw = sw[kt];
     };
-    auto load_x = [&](FewStage<I, J>& s, int kt) {
-        const uint8_t* const p = a.x + static_cast<size_t>(kt) * 128;
+    auto load_x = [&](FewStage<I, J, H32>& s, int kt) {
+        const uint8_t* const p = a.x + static_cast<size_t>(kt) * (H32 ? 512 : 128);
 #pragma unroll
         for (int i = 0; i < I; ++i) {
+            if constexpr (H32) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) s.x[i][h] = *reinterpret_cast<const i32x4*>(p + x_off[i] + 64 * h);
-            s.sx[i] = a.sx[s_off[i] + kt * a.sx_block];
+                for (int c = 0; c < 8; ++c)
+                    s.x[i][c] = *reinterpret_cast<const f32x4*>(p + x_off[i] + 256 * (c >> 2) + 16 * (c & 3));
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) s.x[i][h] = *reinterpret_cast<const i32x4*>(p + x_off[i] + 64 * h);
+                s.sx[i] = a.sx[s_off[i] + kt * a.sx_block];
+            }
         }
     };
     if (part < KT) load_w(st[0], part);                // before the rows' sources are known
@@ -885,7 +899,7 @@ __global__ __launch_bounds__(512) void f8_few_kernel(const F8Args a) {
             row = a.row_src[row];
             row = row < 0 ? 0 : row < a.x_rows ? row : a.x_rows - 1;
         }
-        x_off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(K) + 16 * g;
+        x_off[i] = (static_cast<uint32_t>(row) * static_cast<uint32_t>(K) + 16 * g) * (H32 ? 4 : 1);
         s_off[i] = row * a.sx_row;
     }
     f32x4 acc[I][J];
@@ -893,17 +907,43 @@ __global__ __launch_bounds__(512) void f8_few_kernel(const F8Args a) {
     for (int i = 0; i < I; ++i)
 #pragma unroll
         for (int j = 0; j < J; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    auto add = [&](const FewStage<I, J>& s) {
+    auto add = [&](const FewStage<I, J, H32>& s) {
         i32x8 xf[I];
+        float sx[I];
 #pragma unroll
-        for (int i = 0; i < I; ++i) xf[i] = __builtin_shufflevector(s.x[i][0], s.x[i][1], 0, 1, 2, 3, 4, 5, 6, 7);
+        for (int i = 0; i < I; ++i) {
+            if constexpr (H32) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const uint32_t b = finite_magnitude(s.x[i][c][v]);
+                        m = b > m ? b : m;
+                    }
+#pragma unroll
+                for (int d = 16; d < 64; d *= 2) {
+                    const uint32_t o = static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), d));
+                    m = o > m ? o : m;
+                }
+                const uint32_t ex = f8_scale_exponent(m);
+                const float inv = f8_inverse(ex);
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    xf[i][c] = static_cast<int>(f8_pack4(s.x[i][c][0], s.x[i][c][1], s.x[i][c][2], s.x[i][c][3], inv));
+                sx[i] = f8_scale(ex);
+            } else {
+                xf[i] = __builtin_shufflevector(s.x[i][0], s.x[i][1], 0, 1, 2, 3, 4, 5, 6, 7);
+                sx[i] = s.sx[i];
+            }
+        }
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const i32x8 wf = __builtin_shufflevector(s.w[j][0], s.w[j][1], 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
             for (int i = 0; i < I; ++i) {
                 const f32x4 d = block_sum<kPrecise>(wf, xf[i]);
-                const float f = s.sx[i] * s.sw;
+                const float f = sx[i] * s.sw;
 #pragma unroll
                 for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(d[v], f, acc[i][j][v]);
             }
@@ -950,13 +990,13 @@ __global__ __launch_bounds__(512) void f8_few_kernel(const F8Args a) {
     }
 }
 
-template <int I, int J, typename OUT, bool SWIGLU>
+template <int I, int J, typename OUT, bool SWIGLU, bool H32 = false>
 cap_status launch_few(const F8Args& a, hipStream_t st) {
     constexpr int rows = 16 * I, cols = 16 * J;
     const long long tiles = a.max_rows / rows + (a.E_loc < a.max_rows ? a.E_loc : a.max_rows);
     const long long blocks = tiles * ((a.N + cols - 1) / cols);
     if (blocks * 512 >= (1ll << 32)) return CAP_ERR_UNSUPPORTED;
-    f8_few_kernel<I, J, OUT, SWIGLU><<<static_cast<unsigned>(blocks), 512, 0, st>>>(a);
+    f8_few_kernel<I, J, OUT, SWIGLU, H32><<<static_cast<unsigned>(blocks), 512, 0, st>>>(a);
     CAP_LAUNCH_CHECK();
     return CAP_OK;
 }
@@ -1072,6 +1112,13 @@ cap_status launch_few_rows(const F8Args& a, hipStream_t st) {
     return launch_few<1, 2, OUT, SWIGLU>(a, st);
 }
 
+// y from H in fp32.
+constexpr double kH32Bytes = 8e6;
+cap_status launch_few_h32(const F8Args& a, hipStream_t st) {
+    if (few_fill(a, 16, 64)) return launch_few<1, 4, uint16_t, false, true>(a, st);
+    return launch_few<1, 2, uint16_t, false, true>(a, st);
+}
+
 // scales: room for those of the rows in their order.
 cap_status product(cap_dtype out_dtype, const F8Args& a, float* scales, hipStream_t st) {
     if (out_dtype == CAP_DTYPE_F32) {
@@ -1136,13 +1183,12 @@ cap_status expert_ffn_fp8_launch(int E_loc, int d, int inter, int max_rows, cons
     a.max_rows = max_rows;
     a.N = inter;
     a.KT = d / 128;
-    // few rows: H in fp32, then its codes (3 us, as the wide tiles' scales take)
+    // few rows: H in fp32, quantised by the product that reads it, or, for more rows, by itself
     const bool few = max_rows <= kFewFfnRows && few_time(a) < wide_time(a);
     cap_status done;
     if (few) {
         a.out = h;
         done = launch_few_rows<float, true>(a, st);
-        if (done == CAP_OK) done = quantise_fp8_launch(CAP_DTYPE_F32, 1, max_rows, inter, 1, h, codes, h_scales, st);
     } else {
         done = launch_wide<uint8_t>(a, scales, st);
     }
@@ -1160,6 +1206,17 @@ cap_status expert_ffn_fp8_launch(int E_loc, int d, int inter, int max_rows, cons
     a.x_rows = max_rows;
     a.N = d;
     a.KT = inter / 128;
+    if (few) {
+        // (the kernel that quantises by itself reads H again with every block of outputs: 10 rows of 13
+        // experts, d = 384, inter = 896 8.8 us instead of 10.3, but 8 rows of 8 experts, d = 7168,
+        // inter = 2048 75 instead of 71.4; of the cases timed it is ahead below 11 MB of weights)
+        if (!few_take_32(a) && static_cast<double>(likely_tiles(a, 16)) * weight_bytes(a) < kH32Bytes) {
+            a.x = reinterpret_cast<const uint8_t*>(h);
+            return launch_few_h32(a, st);
+        }
+        done = quantise_fp8_launch(CAP_DTYPE_F32, 1, max_rows, inter, 1, h, codes, h_scales, st);
+        if (done != CAP_OK) return done;
+    }
     return product(CAP_DTYPE_BF16, a, scales, st);
 }
 
