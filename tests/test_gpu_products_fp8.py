@@ -368,3 +368,49 @@ def test_wide_ffn(capi, counts, d, inter, x_rows):
         assert np.all(np.abs(y[r] - want[0]) <= off[0]), r
     z = _ffn(capi, p, len(y) + 300)
     assert np.array_equal(z[:len(y)], y) and (z[len(y):] == -7.0).all()
+
+
+# ------------------------------------------------------------------ few rows: each shape of workgroup
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("counts,n", [([1] * 8, 4099), ([1] * 8, 2056), ([1] * 8, 1003), ([3, 2], 100), ([10] * 7 + [33], 2056), ([17, 1], 40)])
+def test_few_rows(capi, counts, n, bf16):
+    p = _problem(np.random.default_rng(n), counts, n, 384, 9)
+    want, off = _want(p, bf16)
+    y = _run(capi, p, bf16)
+    assert np.all(np.abs(y - want) <= off)
+    assert np.array_equal(_run(capi, p, bf16), y)
+
+
+@pytest.mark.parametrize("counts,d,inter", [([1] * 8, 128, 1536), ([1] * 8, 1536, 128), ([1] * 8, 128, 768), ([2, 1], 256, 256), ([10] * 7 + [33], 128, 1536),
+                                            ([16, 17], 384, 1152), ([0, 0, 1], 128, 2048)])
+def test_few_rows_ffn(capi, counts, d, inter):
+    p = _ffn_problem(np.random.default_rng(d + inter), counts, d, inter, 9)
+    want, off = _ffn_want(p)
+    y = _ffn(capi, p)
+    assert np.all(np.abs(y - want) <= off)
+    assert np.array_equal(_ffn(capi, p, len(y) + 3)[:len(y)], y)
+
+
+@pytest.mark.parametrize("bad", [np.inf, np.nan])
+def test_few_rows_ffn_not_finite(capi, bad):
+    """A row of H that is not finite, quantised on its way to the second product: that row of y alone."""
+    p = _ffn_problem(np.random.default_rng(11), [4, 5], 256, 384)
+    clean = _ffn(capi, p)
+    p["sx"][6, 1] = bad
+    y = _ffn(capi, p)
+    assert np.isnan(y[6]).all() and np.array_equal(np.delete(y, 6, 0), np.delete(clean, 6, 0))
+
+
+def test_wide_product_of_long_rows(capi):
+    """Scales put in the rows' order first: many rows, each with more scales than a line holds."""
+    rng = np.random.default_rng(90)
+    counts = [300, 25000, 1, 14699]
+    p = _problem(rng, counts, 1544, 4224, 100)
+    y = _run(capi, p, True)
+    rows = _sample(rng, counts, 10)
+    want, off = _want_rows(p, rows)
+    assert np.all(np.abs(y[rows] - want) <= off)
+    # rows of one expert from the same row of x are alike
+    first = {}
+    for r in range(300, 25300):
+        assert np.array_equal(y[r], y[first.setdefault(p["src"][r], r)])
