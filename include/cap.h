@@ -677,7 +677,8 @@ cap_status cap_route_scores(const cap_topology *topo, const float *logits, const
 /*
  * Gradient of the router logits through cap_route_scores' gates (Eq. 1).  The choice,
  * the pruning and the bias have no gradient.
- *   idx, keep, w   as cap_route_scores wrote them (keep NULL: every slot is kept);
+ *   idx, keep, w   as cap_route_scores wrote them: the experts of a token's slots are
+ *                  distinct (keep NULL: every slot is kept);
  *   d_w[T][k]      the gradient at the gates (not read for slots that are not kept);
  *   d_add[T][E]    (nullable, fp32) a gradient that reaches the logits another way
  *                  (cap_router_grad's, of the losses), added before the one rounding;
