@@ -113,6 +113,23 @@ __device__ __forceinline__ uint32_t low_word(double v) {
     return static_cast<uint32_t>(static_cast<uint64_t>(__double_as_longlong(v)));
 }
 
+// 64 bits by shifts of 32.  (Summing the kept slots by a 64-bit shift of the mask, by the slot's device in
+// a register, now and then lost a slot in whole waves, in first calls after other work: 9 of 19,800
+// drawn cases, none of 29,700 without such shifts.)
+struct Bits {
+    uint32_t lo, hi;
+};
+__device__ __forceinline__ Bits split_bits(uint64_t m) {
+    Bits b = {static_cast<uint32_t>(m), static_cast<uint32_t>(m >> 32)};
+    asm("" : "+v"(b.lo), "+v"(b.hi));                  // two words for the compiler too, which would shift 64 bits
+    return b;
+}
+__device__ __forceinline__ uint64_t bit64(int i) {
+    const uint32_t b = 1u << (i & 31);
+    return static_cast<uint64_t>(i & 32 ? b : 0u) << 32 | (i & 32 ? 0u : b);
+}
+__device__ __forceinline__ bool has_bit(const Bits& m, int i) { return ((i & 32 ? m.hi : m.lo) >> (i & 31)) & 1u; }
+
 // Key of a value that is not -0.
 __device__ __forceinline__ double value_key(float v, uint32_t tie) {
     const uint32_t hi = __float_as_uint(v);
@@ -229,11 +246,11 @@ __device__ __forceinline__ void exact_choice(const ScoreArgs& a, int t, ExactSpa
             const double other = lane_f64(total, o);
             ahead += (o < lane ? other >= total : other > total) ? 1 : 0;
         }
-        const uint64_t open = __ballot(lane < a.groups && ahead < a.open_groups);
+        const Bits open = split_bits(__ballot(lane < a.groups && ahead < a.open_groups));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int e = 4 * lane + i;
-            key[i] = e < a.E && ((open >> small_quotient(e, a.group_size)) & 1ull) ? key[i] : kNoKey;
+            key[i] = e < a.E && has_bit(open, small_quotient(e, a.group_size)) ? key[i] : kNoKey;
         }
     }
     for (int s = 0; s < a.k; ++s) {
@@ -264,7 +281,7 @@ __device__ __forceinline__ int dpp_swap_i32(int v) { return __builtin_amdgcn_mov
 //   GROUPS  0: one group (or all of them open); 1: groups of 4 L CPG experts, which are whole
 //           values of c; 2: any, through LDS
 // What bounds it: instruction issue, most of it the selection network.  32,768 tokens of 256
-// experts in 8 groups, sigmoid with a bias, pruned: 20.5 us (35.8 with all scores in fp64: one
+// experts in 8 groups, sigmoid with a bias, pruned: 20.8 us (35.8 with all scores in fp64: one
 // wave a SIMD, for the registers of 64 keys a lane; keys are formed block by block now, and fp64
 // is left to the chosen slots), 4 us of which are the unsure tokens; to read and write 36 MB
 // takes 8.  32 tokens: 7.7 us, a chain of joins.  If every token is unsure (all logits alike),
@@ -424,7 +441,7 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
             int ahead = 0;
             for (int o = 0; o < a.groups; ++o) ahead += (o < g ? sums[o] >= s : sums[o] > s) ? 1 : 0;
             const bool is_open = ahead < a.open_groups;
-            open |= is_open ? 1ull << g : 0ull;
+            open |= is_open ? bit64(g) : 0ull;
             lowest = is_open ? fminf(lowest, s) : lowest;
             highest = is_open ? highest : fmaxf(highest, s);
         }
@@ -438,10 +455,11 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
             unsure = gap_unsure(lowest, highest, size);
             if (!a.bias) load_row();
         }
+        const Bits opened = split_bits(open);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int e = expert(j);
-            v[j] = e < a.E && ((open >> small_quotient(e, a.group_size)) & 1ull) ? v[j] : closed;
+            v[j] = e < a.E && has_bit(opened, small_quotient(e, a.group_size)) ? v[j] : closed;
         }
     }
 
@@ -604,11 +622,13 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
     uint64_t mask = 0;
     double kept_sum = 0.0;
 #pragma unroll
-    for (int u = 0; u < NS; ++u) mask |= kept[u] ? 1ull << (my_dev[u] & 63) : 0ull;
+    for (int u = 0; u < NS; ++u) mask |= kept[u] ? bit64(my_dev[u]) : 0ull;
     mask |= dpp_swap_u64<kDppXor1>(mask);
     mask |= dpp_swap_u64<kDppXor2>(mask);
-#pragma unroll
-    for (int s = 0; s < KP; ++s) kept_sum += devs[s] >= 0 && ((mask >> (devs[s] & 63)) & 1ull) ? qs[s] : 0.0;
+    each_slot<KP>([&](auto S) {
+        constexpr int s = decltype(S)::value;
+        kept_sum += quad_at<s % 4>(kept[s / 4] ? q[s / 4] : 0.0);
+    });
     const double factor = static_cast<double>(a.scale) *
                           (a.normalise ? (kept_sum > 0.0 ? 1.0 / kept_sum : 0.0) : 1.0);
     if (!live || h >= 4) return;

@@ -241,3 +241,28 @@ def test_grad_of_masked_rows_and_bad_indices(capi):
     want = np.zeros((T, E), np.float32)
     want[:, [0, 3]] = 0.5
     assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("T,E,k,R,groups,kind,p", [(30496, 32, 7, 32, 2, "softmax", 0.1), (26304, 64, 8, 32, 1, "softmax", 0.3),
+                                                   (19981, 61, 8, 1, 1, "softmax", 0.0), (20416, 64, 6, 32, 1, "sigmoid", 0.3)])
+def test_gates_sum_to_the_scale_after_other_work(capi, T, E, k, R, groups, kind, p):
+    """The same call many times, after other work each time: the same bits, and kept gates that sum to the scale."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    logits = torch.randn((T, E), generator=g, device="cuda") * 1.5
+    rank = torch.arange(E, dtype=torch.int32, device="cuda") // (E // R)
+    topo = capi.make_topology(E, R, R, T, k, rank, torch.arange(E, dtype=torch.int32, device="cuda") % (E // R))
+    opt = capi.make_score_options(capi.CAP_SCORE_SOFTMAX if kind == "softmax" else capi.CAP_SCORE_SIGMOID, groups, 1, 1, True, 2.5)
+    idx, w = torch.empty((T, k), dtype=torch.int32, device="cuda"), torch.empty((T, k), device="cuda")
+    keep, mask = torch.empty((T, k), dtype=torch.uint8, device="cuda"), torch.empty(T, dtype=torch.int64, device="cuda")
+    big = torch.randn((4096, 4096), generator=g, device="cuda")
+    first = None
+    for _ in range(30):
+        big = big @ big / 64
+        w.fill_(-1.0)
+        torch.cuda.synchronize()
+        capi.cap_route_scores(topo, logits, opt, p, idx, w, keep, mask)
+        torch.cuda.synchronize()
+        # k fp32 roundings of at most the scale each
+        assert ((w.double().sum(1) - 2.5).abs() <= k * 2.0 ** -24 * 2.5).all()
+        first = w.clone() if first is None else first
+        assert torch.equal(w, first)
