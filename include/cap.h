@@ -742,7 +742,9 @@ cap_status cap_product_fp8(cap_dtype out_dtype, int32_t E_loc, int32_t n, int32_
 /*
  * cap_expert_ffn (row_src NULL) or cap_expert_ffn_gather in 8-bit floating point (Eq. 1
  * Expert_i): y = W2 q(silu(W1 x) * (W3 x)), where q quantises each row of H from fp32
- * as cap_quantise_fp8 does (blocks of 1 x 128); products as cap_product_fp8.
+ * as cap_quantise_fp8 does (blocks of 1 x 128); products as cap_product_fp8 (for few
+ * rows those of H as with an fp32 result).  Which kernels run goes by max_rows, too: a
+ * value of H within its sum's error of a border between two codes may get either.
  *   x[x_rows][d], x_scale[x_rows][d / 128]  quantised once per token;
  *   w1, w3 [E_loc][inter][d], s1, s3 [E_loc][inter / 128][d / 128];
  *   w2 [E_loc][d][inter], s2 [E_loc][d / 128][inter / 128];  y[max_rows][d] bf16.

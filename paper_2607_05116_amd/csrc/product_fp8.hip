@@ -844,7 +844,7 @@ struct FewStage<I, J, true> {
 // lanes that hold it (as the quantisation's kernel does, to the bit).
 template <int I, int J, typename OUT, bool kSwiglu, bool H32>
 __global__ __launch_bounds__(512) void f8_few_kernel(const F8Args a) {
-    constexpr bool kPrecise = std::is_same<OUT, float>::value && !kSwiglu;
+    constexpr bool kPrecise = std::is_same<OUT, float>::value;         // H too: its error moves codes across a border
     constexpr int kParts = kSwiglu ? 4 : 8;            // waves that share K
     constexpr int kCols = 16 * J, kRows = 16 * I;
     constexpr int kPitch = kCols + 4;                  // of a row of sums in LDS
