@@ -128,7 +128,12 @@ __device__ __forceinline__ uint64_t bit64(int i) {
     const uint32_t b = 1u << (i & 31);
     return static_cast<uint64_t>(i & 32 ? b : 0u) << 32 | (i & 32 ? 0u : b);
 }
-__device__ __forceinline__ bool has_bit(const Bits& m, int i) { return ((i & 32 ? m.hi : m.lo) >> (i & 31)) & 1u; }
+// (A choice between the two words by a condition is one between their addresses for the compiler, which
+// then keeps them in memory: in LDS, at a place that it works out from the dispatch packet, which lies in host memory.)
+__device__ __forceinline__ bool has_bit(const Bits& m, int i) {
+    const uint32_t high = 0u - (static_cast<uint32_t>(i) >> 5 & 1u);
+    return ((m.hi & high) | (m.lo & ~high)) >> (i & 31) & 1u;
+}
 
 // Key of a value that is not -0.
 __device__ __forceinline__ double value_key(float v, uint32_t tie) {
