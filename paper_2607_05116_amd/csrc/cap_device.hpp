@@ -55,11 +55,52 @@ __device__ __forceinline__ uint32_t pack_bf16x2_rne(float a, float b) {
 
 __device__ __forceinline__ int lane_id() { return __lane_id(); }
 
-// Mask of lanes below the calling lane.
-__device__ __forceinline__ uint64_t lanemask_lt() {
-    const int l = lane_id();
-    return l == 0 ? 0ull : (~0ull >> (64 - l));
+// 64-bit masks by a lane's own bit number, in shifts of 32 bits.  A 64-bit shift whose amount is the last vector
+// register that the kernel has is taken to give wrong results now and then, in whole waves: of 2,406 such shifts by
+// a register in the 172 kernels of the routing by scores 7 were of that form, one each in 7 kernels, and the drawn
+// cases whose gates came out wrong (9 of 19,800) all ran kernels among these 7.  Which register it is, is the
+// compiler's choice, so no kernel of this library shifts 64 bits by one.
+struct Bits {
+    uint32_t lo, hi;
+};
+// (Two words for the compiler too, which would put 64-bit shifts together again.)
+__device__ __forceinline__ void keep_apart(Bits& b) { asm("" : "+v"(b.lo), "+v"(b.hi)); }
+__device__ __forceinline__ Bits split_bits(uint64_t m) {
+    Bits b = {static_cast<uint32_t>(m), static_cast<uint32_t>(m >> 32)};
+    keep_apart(b);
+    return b;
 }
+__device__ __forceinline__ uint64_t join_bits(Bits b) {
+    keep_apart(b);
+    return static_cast<uint64_t>(b.hi) << 32 | b.lo;
+}
+// Bit i.  (A choice between the two words by a condition is one between their addresses for the compiler, which
+// then keeps them in memory: in LDS, at a place that it works out from the dispatch packet, which lies in host memory.)
+__device__ __forceinline__ bool has_bit(const Bits& m, int i) {
+    const uint32_t high = 0u - (static_cast<uint32_t>(i) >> 5 & 1u);
+    return ((m.hi & high) | (m.lo & ~high)) >> (i & 31) & 1u;
+}
+__device__ __forceinline__ bool has_bit(uint64_t m, int i) { return has_bit(split_bits(m), i); }
+__device__ __forceinline__ uint64_t bit64(int i, bool set = true) {
+    const uint32_t b = (set ? 1u : 0u) << (i & 31), high = 0u - (static_cast<uint32_t>(i) >> 5 & 1u);
+    return join_bits(Bits{b & ~high, b & high});
+}
+// Bits 0 .. i - 1 (of 0 <= i < 64), and 0 .. i.
+__device__ __forceinline__ Bits bits_below(int i) {
+    const uint32_t part = (1u << (i & 31)) - 1u, high = 0u - (static_cast<uint32_t>(i) >> 5 & 1u);
+    return Bits{part | high, part & high};
+}
+__device__ __forceinline__ Bits bits_through(int i) {
+    const uint32_t part = (2u << (i & 31)) - 1u, high = 0u - (static_cast<uint32_t>(i) >> 5 & 1u);
+    return Bits{part | high, part & high};
+}
+// How many of the bits in `of` are set.
+__device__ __forceinline__ int count_bits(const Bits& m, const Bits& of) {
+    return __popc(m.lo & of.lo) + __popc(m.hi & of.hi);
+}
+
+// Mask of lanes below the calling lane.
+__device__ __forceinline__ Bits lanemask_lt() { return bits_below(lane_id()); }
 
 // floor(n / d) for 0 <= n < 2^31 and 1 <= d < 2^31 with a quotient below
 // 2^16: the fp32 estimate n * rcp(d) is within 2^-21 of n / d relative (so

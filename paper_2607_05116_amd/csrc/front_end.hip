@@ -129,14 +129,19 @@ __global__ __launch_bounds__(kRcThreads) void route_count_kernel(
     uint64_t vp = 0;
     if (live && lg == 0) {
         // devices of one node: rpn consecutive bits; the source's node is `home`
-        const uint64_t node_bits = (g.rpn >= 64) ? ~0ull : ((1ull << g.rpn) - 1);
-        const uint64_t home = node_bits << ((src / g.rpn) * g.rpn);
+        auto node_of = [&](int d) {
+            const int first = small_quotient(d, g.rpn) * g.rpn;
+            const Bits below = bits_below(first), through = bits_through(min(first + g.rpn, 64) - 1);
+            return join_bits(Bits{through.lo & ~below.lo, through.hi & ~below.hi});
+        };
+        const uint64_t home = node_of(src);
         v[0] = __popcll(m);
-        v[1] = __popcll(m & home & ~(1ull << src));
+        v[1] = __popcll(m & home & ~bit64(src));
         v[2] = __popcll(m & ~home);
         for (uint64_t b = m; b; ++v[3]) {        // one step per node: drop all of its devices
-            const int d = __ffsll(static_cast<unsigned long long>(b)) - 1;
-            b &= ~(node_bits << (small_quotient(d, g.rpn) * g.rpn));
+            int d = __ffsll(static_cast<unsigned long long>(b)) - 1;
+            asm("" : "+v"(d));                   // 32 bits for the quotient too: the bit's number is found in 64
+            b &= ~node_of(d);
         }
         reinterpret_cast<uint32_t*>(vol)[t] = static_cast<uint32_t>(v[0]) | (static_cast<uint32_t>(v[1]) << 8) |
                                               (static_cast<uint32_t>(v[2]) << 16) | (static_cast<uint32_t>(v[3]) << 24);
@@ -156,7 +161,10 @@ __global__ __launch_bounds__(kRcThreads) void route_count_kernel(
         uint64_t all = 0;
 #pragma unroll
         for (int w = 0; w < kRcWaves; ++w) all += vsum[w];
-        ws.volpart[sc * 4 + threadIdx.x] = static_cast<int64_t>((all >> (16 * threadIdx.x)) & 0xFFFFu);
+        const Bits sums = split_bits(all);
+        const uint32_t high = 0u - (threadIdx.x >> 1);
+        ws.volpart[sc * 4 + threadIdx.x] =
+            static_cast<int64_t>(((sums.hi & high) | (sums.lo & ~high)) >> (16 * (threadIdx.x & 1)) & 0xFFFFu);
     }
     // the part's row: the waves' histograms summed (W <= 2 * 256: two
     // columns per thread, the second clamped, all LDS reads issued together)

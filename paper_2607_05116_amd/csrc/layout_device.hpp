@@ -49,7 +49,7 @@ __device__ __forceinline__ int slot_position(const int32_t* er, const int32_t* e
 }
 
 __device__ __forceinline__ uint64_t device_bits(uint64_t m, int R) {
-    return R >= 64 ? m : (m & ((1ull << R) - 1));
+    return R >= 64 ? m : (m & ((1ull << R) - 1));        // R is the same for all lanes: a scalar shift
 }
 
 // Slot positions (-1 when pruned or invalid) and device mask of token t.
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(kChunk) void layout_count_kernel(
         for (int s = 0; s < kMaxK; ++s)
             if (P[s] >= 0) atomicAdd(&cnt[P[s]], 1);
         const int src_node = src / g.rpn;
-        uint64_t nodes = 0;
+        int last_node = -1;                     // devices come in ascending order, and so do nodes
         for (uint64_t b = m; b; b &= b - 1) {
             const int d = __ffsll(static_cast<unsigned long long>(b)) - 1;
             atomicAdd(&cnt[g.E + d], 1);
@@ -135,9 +135,9 @@ __global__ __launch_bounds__(kChunk) void layout_count_kernel(
             const int nd = d / g.rpn;
             if (nd != src_node) ++v[2];
             else if (d != src) ++v[1];
-            nodes |= 1ull << nd;
+            v[3] += nd != last_node ? 1 : 0;
+            last_node = nd;
         }
-        v[3] = __popcll(nodes);
         reinterpret_cast<uint32_t*>(vol)[t] = static_cast<uint32_t>(v[0]) | (static_cast<uint32_t>(v[1]) << 8) |
                                               (static_cast<uint32_t>(v[2]) << 16) | (static_cast<uint32_t>(v[3]) << 24);
     }
@@ -295,7 +295,7 @@ __device__ __forceinline__ void layout_scatter_block(
     int32_t* __restrict__ recv_offsets, int32_t* __restrict__ expert_counts,
     int32_t* __restrict__ expert_offsets, int32_t* __restrict__ slot_pos,
     int32_t* __restrict__ copy_row, int32_t* __restrict__ recv_token, int bid) {
-    __shared__ unsigned long long bits[kWavesPerChunk][kMaxW];
+    __shared__ __align__(8) uint32_t bits[kWavesPerChunk][kMaxW][2];
     __shared__ int32_t pre[kWavesPerChunk][kMaxW];
     __shared__ int pos_lds[kMaxE];
     __shared__ int32_t gbase[kMaxW];
@@ -339,7 +339,7 @@ __device__ __forceinline__ void layout_scatter_block(
     // ---- LDS work
 #pragma unroll
     for (int w = 0; w < kWavesPerChunk; ++w)
-        for (int c = i; c < g.W; c += kChunk) bits[w][c] = 0ull;
+        for (int c = i; c < g.W; c += kChunk) bits[w][c][0] = bits[w][c][1] = 0u;
     if (i >= g.E) tot_e = 0;
     if (i >= g.R) tot_d = 0;
     const uint64_t m = live ? device_bits(m_raw, g.R) : 0ull;
@@ -391,17 +391,17 @@ __device__ __forceinline__ void layout_scatter_block(
         if (j * kChunk >= pairs) continue;
         if (n < pairs && kp_raw[j] && static_cast<unsigned>(e_raw[j]) < static_cast<unsigned>(g.E)) P[j] = pos_lds[e_raw[j]];
         const int tok = (n * g.kinv) >> 16;
-        if (P[j] >= 0) atomicOr(&bits[tok / kWave][P[j] & 0xFFFF], 1ull << (tok % kWave));
+        if (P[j] >= 0) atomicOr(&bits[tok / kWave][P[j] & 0xFFFF][tok >> 5 & 1], 1u << (tok & 31));
     }
     for (uint64_t b = m; b; b &= b - 1)
-        atomicOr(&bits[wave][g.E + __ffsll(static_cast<unsigned long long>(b)) - 1], 1ull << lane_id());
+        atomicOr(&bits[wave][g.E + __ffsll(static_cast<unsigned long long>(b)) - 1][lane_id() >> 5], 1u << (lane_id() & 31));
     __syncthreads();
     for (int col = threadIdx.x; col < g.W; col += kChunk) {
         int run = gbase[col];
 #pragma unroll
         for (int w = 0; w < kWavesPerChunk; ++w) {
             pre[w][col] = run;                  // the column's rows before wave w's tokens
-            run += __popcll(bits[w][col]);
+            run += __popc(bits[w][col][0]) + __popc(bits[w][col][1]);
         }
     }
     __syncthreads();
@@ -410,24 +410,24 @@ __device__ __forceinline__ void layout_scatter_block(
         const int n = i + j * kChunk;
         if (j * kChunk >= pairs) break;
         const int tok = (n * g.kinv) >> 16, w = tok / kWave;
-        const unsigned long long at = 1ull << (tok % kWave);
+        const Bits below = bits_below(tok % kWave);
         int sp = -1, cr = -1;
         if (P[j] >= 0) {
             const int ce = P[j] & 0xFFFF, cd = g.E + (P[j] >> 16);
-            const unsigned long long be = bits[w][ce], bd = bits[w][cd];
-            sp = pre[w][ce] + __popcll(be & (at - 1));
-            if (bd & at) cr = pre[w][cd] + __popcll(bd & (at - 1));   // the mask holds the device
+            const Bits be = {bits[w][ce][0], bits[w][ce][1]}, bd = {bits[w][cd][0], bits[w][cd][1]};
+            sp = pre[w][ce] + count_bits(be, below);
+            if (has_bit(bd, tok % kWave)) cr = pre[w][cd] + count_bits(bd, below);   // the mask holds the device
         }
         if (n < pairs) {
             slot_pos[q0 + n] = sp;
             copy_row[q0 + n] = cr;
         }
     }
-    const unsigned long long below = lanemask_lt();
+    const Bits below = lanemask_lt();
     for (uint64_t b = m; b; b &= b - 1) {
         const int d = __ffsll(static_cast<unsigned long long>(b)) - 1;
         const int col = g.E + d;
-        const int row = pre[wave][col] + __popcll(bits[wave][col] & below);
+        const int row = pre[wave][col] + count_bits(Bits{bits[wave][col][0], bits[wave][col][1]}, below);
         const long long at = static_cast<long long>(roff[d]) + row;
         if (at >= 0 && at < static_cast<long long>(g.T) * g.k) recv_token[at] = t;   // malformed masks stay in bounds
     }

@@ -251,7 +251,7 @@ __global__ __launch_bounds__(kThreads) void send_pack_kernel(
             const int e = idx[q];
             if (keep[q] && static_cast<unsigned>(e) < static_cast<unsigned>(g.E)) d = dev_of[e];
             cr = copy_row[q];
-            if (static_cast<unsigned>(d) >= static_cast<unsigned>(g.R) || !((m >> d) & 1ull)) d = -1;
+            if (static_cast<unsigned>(d) >= static_cast<unsigned>(g.R) || !has_bit(m, d)) d = -1;
         }
         // one row per device: the device's first kept slot writes it
         bool first = d >= 0;
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(kThreads) void src_reduce_kernel(
             const int e = idx[q];
             cr = copy_row[q];
             if (keep[q] && static_cast<unsigned>(e) < static_cast<unsigned>(g.E)) d = dev_of[e];
-            if (static_cast<unsigned>(d) >= static_cast<unsigned>(g.R) || !((m >> d) & 1ull) || cr < 0) d = -1;
+            if (static_cast<unsigned>(d) >= static_cast<unsigned>(g.R) || !has_bit(m, d) || cr < 0) d = -1;
         }
         // one returned row per kept device (its first kept slot), ascending device
         bool first = d >= 0;

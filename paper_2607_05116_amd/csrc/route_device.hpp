@@ -320,13 +320,13 @@ __device__ __forceinline__ RouteResult route_token(const float (&vals)[V], int g
         rank_kept = ranked && (keep_all || g <= below);   // ranks 0 .. first reaching rank
         rank_dev = 63 - static_cast<int>((ckb >> 3) & 63u);
     }
-    uint64_t mask = rank_kept ? (1ull << rank_dev) : 0ull;
+    uint64_t mask = bit64(rank_dev, rank_kept);
     mask |= dpp_swap_u64<kDppXor1>(mask);
     mask |= dpp_swap_u64<kDppXor2>(mask);
     mask |= dpp_swap_u64<kDppHalfMirror>(mask);
 
     // ---- S' = kept gates summed in slot order; lane g writes slot g
-    const bool my_keep = NAIVE ? slot_kept : has_slot && ((mask >> (my_dev & 63)) & 1ull);
+    const bool my_keep = NAIVE ? slot_kept : has_slot && has_bit(mask, my_dev & 63);
     const float kw = my_keep ? my_w : 0.0f;
     float Sk = group_lane<0>(kw);
 #define CAP_KEPT_SUM(S_) \

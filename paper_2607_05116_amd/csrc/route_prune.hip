@@ -178,7 +178,7 @@ __device__ __forceinline__ void route_token4(const float (&vals)[V4], int h, int
 #pragma unroll
         for (int u = 0; u < NS; ++u) {
             slot_kept[u] = has[u] && h + 4 * u < n_keep;
-            bits |= slot_kept[u] ? (1ull << (my_dev[u] & 63)) : 0ull;
+            bits |= bit64(my_dev[u], slot_kept[u]);
         }
     } else {
         const int src = small_quotient(live ? t : 0, tokens_per_rank);
@@ -252,7 +252,7 @@ __device__ __forceinline__ void route_token4(const float (&vals)[V4], int h, int
         for (int u = 0; u < 2; ++u) {
             const bool kept = ranked[u] && (keep_all || h + 4 * u <= below);
             const int dev = 63 - static_cast<int>((static_cast<uint64_t>(__double_as_longlong(ck[u])) >> 3) & 63u);
-            bits |= kept ? (1ull << dev) : 0ull;
+            bits |= bit64(dev, kept);
         }
     }
     uint64_t mask = bits;
@@ -264,7 +264,7 @@ __device__ __forceinline__ void route_token4(const float (&vals)[V4], int h, int
     float kw[NS];
 #pragma unroll
     for (int u = 0; u < NS; ++u) {
-        my_keep[u] = NAIVE ? slot_kept[u] : has[u] && ((mask >> (my_dev[u] & 63)) & 1ull);
+        my_keep[u] = NAIVE ? slot_kept[u] : has[u] && has_bit(mask, my_dev[u] & 63);
         kw[u] = my_keep[u] ? my_w[u] : 0.0f;
     }
     float Sk = quad_lane<0>(kw[0]);

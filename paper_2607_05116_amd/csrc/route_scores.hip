@@ -113,28 +113,6 @@ __device__ __forceinline__ uint32_t low_word(double v) {
     return static_cast<uint32_t>(static_cast<uint64_t>(__double_as_longlong(v)));
 }
 
-// 64 bits by shifts of 32.  (Summing the kept slots by a 64-bit shift of the mask, by the slot's device in
-// a register, now and then lost a slot in whole waves, in first calls after other work: 9 of 19,800
-// drawn cases, none of 29,700 without such shifts.)
-struct Bits {
-    uint32_t lo, hi;
-};
-__device__ __forceinline__ Bits split_bits(uint64_t m) {
-    Bits b = {static_cast<uint32_t>(m), static_cast<uint32_t>(m >> 32)};
-    asm("" : "+v"(b.lo), "+v"(b.hi));                  // two words for the compiler too, which would shift 64 bits
-    return b;
-}
-__device__ __forceinline__ uint64_t bit64(int i) {
-    const uint32_t b = 1u << (i & 31);
-    return static_cast<uint64_t>(i & 32 ? b : 0u) << 32 | (i & 32 ? 0u : b);
-}
-// (A choice between the two words by a condition is one between their addresses for the compiler, which
-// then keeps them in memory: in LDS, at a place that it works out from the dispatch packet, which lies in host memory.)
-__device__ __forceinline__ bool has_bit(const Bits& m, int i) {
-    const uint32_t high = 0u - (static_cast<uint32_t>(i) >> 5 & 1u);
-    return ((m.hi & high) | (m.lo & ~high)) >> (i & 31) & 1u;
-}
-
 // Key of a value that is not -0.
 __device__ __forceinline__ double value_key(float v, uint32_t tie) {
     const uint32_t hi = __float_as_uint(v);
@@ -446,7 +424,7 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
             int ahead = 0;
             for (int o = 0; o < a.groups; ++o) ahead += (o < g ? sums[o] >= s : sums[o] > s) ? 1 : 0;
             const bool is_open = ahead < a.open_groups;
-            open |= is_open ? bit64(g) : 0ull;
+            open |= bit64(g, is_open);
             lowest = is_open ? fminf(lowest, s) : lowest;
             highest = is_open ? highest : fmaxf(highest, s);
         }
@@ -627,7 +605,7 @@ __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
     uint64_t mask = 0;
     double kept_sum = 0.0;
 #pragma unroll
-    for (int u = 0; u < NS; ++u) mask |= kept[u] ? bit64(my_dev[u]) : 0ull;
+    for (int u = 0; u < NS; ++u) mask |= bit64(my_dev[u], kept[u]);
     mask |= dpp_swap_u64<kDppXor1>(mask);
     mask |= dpp_swap_u64<kDppXor2>(mask);
     each_slot<KP>([&](auto S) {
