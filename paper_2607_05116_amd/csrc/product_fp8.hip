@@ -16,6 +16,7 @@
 #pragma clang fp contract(off)
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 
 #include "fp8_device.hpp"
 #include "mfma_tile.hpp"
@@ -990,12 +991,16 @@ __global__ __launch_bounds__(512) void f8_few_kernel(const F8Args a) {
     }
 }
 
+long long few_blocks(const F8Args& a, int rows, int cols) {
+    const long long tiles = a.max_rows / rows + (a.E_loc < a.max_rows ? a.E_loc : a.max_rows);
+    return tiles * ((a.N + cols - 1) / cols);
+}
+bool few_launches(long long blocks) { return blocks * 512 < (1ll << 32); }     // threads of a launch
+
 template <int I, int J, typename OUT, bool SWIGLU, bool H32 = false>
 cap_status launch_few(const F8Args& a, hipStream_t st) {
-    constexpr int rows = 16 * I, cols = 16 * J;
-    const long long tiles = a.max_rows / rows + (a.E_loc < a.max_rows ? a.E_loc : a.max_rows);
-    const long long blocks = tiles * ((a.N + cols - 1) / cols);
-    if (blocks * 512 >= (1ll << 32)) return CAP_ERR_UNSUPPORTED;
+    const long long blocks = few_blocks(a, 16 * I, 16 * J);
+    if (!few_launches(blocks)) return CAP_ERR_UNSUPPORTED;
     f8_few_kernel<I, J, OUT, SWIGLU, H32><<<static_cast<unsigned>(blocks), 512, 0, st>>>(a);
     CAP_LAUNCH_CHECK();
     return CAP_OK;
@@ -1035,9 +1040,28 @@ bool few_fill(const F8Args& a, int rows, int cols) {
 }
 // 32 rows a workgroup once most experts have more than 8 rows.
 bool few_take_32(const F8Args& a) { return a.max_rows > 8ll * a.E_loc && few_fill(a, 32, 64); }
+// Rows and outputs of a workgroup.
+struct FewForm {
+    int rows, cols;
+};
+FewForm few_form(const F8Args& a) {
+    if (few_take_32(a)) return {32, 64};
+    // the more outputs a workgroup, the fewer bytes of x it reads beside its weights; with W1
+    // and W3, a wave has twice the blocks of K (128 outputs: 78 us for 8 rows of 8 experts of
+    // d = 7168, inter = 2048 in 128 workgroups, 64: 47 us)
+    if (!a.w3 && likely_tiles(a, 16) * ((a.N + 127) / 128) >= device_cu_count()) return {16, 128};
+    if (few_fill(a, 16, 64)) return {16, 64};
+    // a compute unit has so much on its way at most: below half of them, 16 outputs each (8 rows of
+    // 6 experts, d = 6400, inter = 384 27.1 -> 21.5 us; 13 experts, 71 rows, d = 2176, in 156
+    // workgroups or 312: 17.5 or 18.7)
+    if (2 * likely_tiles(a, 16) * ((a.N + 31) / 32) < device_cu_count()) return {16, 16};
+    return {16, 32};
+}
 double weight_bytes(const F8Args& a) { return static_cast<double>(a.w3 ? 2 : 1) * a.N * a.KT * 128; }
 double few_time(const F8Args& a) {                     // the weights' way, again for each row tile, and that of the rows (from nearer)
-    const int rows = few_take_32(a) ? 32 : 16;
+    const FewForm f = few_form(a);
+    if (!few_launches(few_blocks(a, f.rows, f.cols))) return HUGE_VAL;
+    const int rows = f.rows;
     const double row_bytes = static_cast<double>(rows) * a.KT * 128 * ((a.N + 63) / 64);
     return 3.5 + static_cast<double>(likely_tiles(a, rows)) * (weight_bytes(a) + 0.5 * row_bytes) / 5.5e6;
 }
@@ -1063,9 +1087,10 @@ cap_status launch_wide(F8Args a, float* scales, hipStream_t st) {
     if (tiles >= (1ll << 31)) return CAP_ERR_UNSUPPORTED;
     const long long cus = (device_cu_count() + 7) / 8 * 8;             // one workgroup a CU
     const long long blocks = tiles < cus ? (tiles + 7) / 8 * 8 : cus;
-    if (!a.sx_in_order && a.KT > 32 && (tiles + cus - 1) / cus * a.KT >= kStagesInOrder) {
+    const long long ordering = (a.max_rows + 63) / 64;                 // workgroups that put the scales in order
+    if (!a.sx_in_order && a.KT > 32 && ordering * 256 < (1ll << 32) && (tiles + cus - 1) / cus * a.KT >= kStagesInOrder) {
         const size_t pitch = f8_scale_pitch(a.max_rows);
-        f8_gather_scales_kernel<<<(a.max_rows + 63) / 64, 256, 0, st>>>(a, scales, pitch);
+        f8_gather_scales_kernel<<<static_cast<unsigned>(ordering), 256, 0, st>>>(a, scales, pitch);
         a.sx = scales;
         a.sx_row = 1;
         a.sx_block = pitch;
@@ -1102,18 +1127,13 @@ namespace {
 
 template <typename OUT, bool SWIGLU>
 cap_status launch_few_rows(const F8Args& a, hipStream_t st) {
-    if (few_take_32(a)) return launch_few<2, 4, OUT, SWIGLU>(a, st);
-    // the more outputs a workgroup, the fewer bytes of x it reads beside its weights; with W1
-    // and W3, a wave has twice the blocks of K (128 outputs: 78 us for 8 rows of 8 experts of
-    // d = 7168, inter = 2048 in 128 workgroups, 64: 47 us)
+    const FewForm f = few_form(a);
+    if (f.rows == 32) return launch_few<2, 4, OUT, SWIGLU>(a, st);
     if constexpr (!SWIGLU)
-        if (likely_tiles(a, 16) * ((a.N + 127) / 128) >= device_cu_count()) return launch_few<1, 8, OUT, SWIGLU>(a, st);
-    if (few_fill(a, 16, 64)) return launch_few<1, 4, OUT, SWIGLU>(a, st);
-    // a compute unit has so much on its way at most: below half of them, 16 outputs each (8 rows of
-    // 6 experts, d = 6400, inter = 384 27.1 -> 21.5 us; 13 experts, 71 rows, d = 2176, in 156
-    // workgroups or 312: 17.5 or 18.7)
-    if (2 * likely_tiles(a, 16) * ((a.N + 31) / 32) < device_cu_count()) return launch_few<1, 1, OUT, SWIGLU>(a, st);
-    return launch_few<1, 2, OUT, SWIGLU>(a, st);
+        if (f.cols == 128) return launch_few<1, 8, OUT, SWIGLU>(a, st);
+    if (f.cols == 64) return launch_few<1, 4, OUT, SWIGLU>(a, st);
+    if (f.cols == 32) return launch_few<1, 2, OUT, SWIGLU>(a, st);
+    return launch_few<1, 1, OUT, SWIGLU>(a, st);
 }
 
 // y from H in fp32.
