@@ -120,7 +120,8 @@ class DeviceLayer:
                    normalise: bool = True, scale: float = 1.0, bias=None, token_mask=None):
         """Route by scores (cap_route_scores): kind "sigmoid" or "softmax" (None: back to the softmax over the chosen
         logits); bias fp32 [E], token_mask uint8 or bool [T] on the device, read at every step.  The front end then runs
-        as separate calls."""
+        as separate calls.  Pruning is by device: expert-level pruning (naive) and the fused call route_layout are
+        refused meanwhile."""
         if kind is None:
             self.scores = None
             return
@@ -181,21 +182,35 @@ class DeviceLayer:
 
     # ------------------------------------------------------------ steps
     def route(self, stream=None):
-        if self.scores is not None:
-            capi.cap_route_scores(self.topo, self.logits, self.scores, self.p, self.idx, self.w, self.keep, self.mask,
-                                  stream)
+        if self._by_scores():
+            self._route_scores(self.logits, stream)
             return
         fn = capi.cap_route_prune_naive if self.naive else capi.cap_route_prune
         fn(self.topo, self.logits, self.p, self.idx, self.w, self.keep, self.mask, stream)
 
+    def _by_scores(self) -> bool:
+        if self.scores is not None and self.naive:
+            raise ValueError("expert-level pruning (naive) goes by the chosen logits' softmax, not by scores")
+        return self.scores is not None
+
+    def _route_scores(self, logits, stream):
+        capi.cap_route_scores(self.topo, logits, self.scores, self.p, self.idx, self.w, self.keep, self.mask, stream)
+
     def router_route(self, w_gate: torch.Tensor, logits_out: torch.Tensor | None = None, stream=None):
-        """Router GEMM x W_g^T fused with top-k routing and pruning (bf16 x)."""
+        """Router GEMM x W_g^T fused with top-k routing and pruning (bf16 x); by scores, from the logits in logits_out
+        (fp32 [T][E], which that takes) in a second call."""
+        if self._by_scores() and logits_out is None:
+            raise ValueError("routing by scores reads the router's logits: give logits_out")
         capi.cap_router_route_prune(self.topo, self.dt, self.d, self.x, w_gate, self.p, self.idx, self.w,
                                     self.keep, self.mask, logits_out, stream)
+        if self.scores is not None:
+            self._route_scores(logits_out, stream)
 
     def route_layout(self, coactivation=True, stream=None):
         """Routing, pruning, layout and (optionally) co-activation counts in
-        the fused three-launch front end."""
+        the fused three-launch front end (by the chosen logits' softmax)."""
+        if self.scores is not None:
+            raise ValueError("the fused front end does not route by scores: route, layout and coactivation do")
         capi.cap_route_layout(self.topo, self.logits, self.p, self.idx, self.w, self.keep, self.mask, self.lay,
                               self.coact if coactivation else None, self.ws_front, stream=stream)
 
