@@ -1,4 +1,6 @@
 """A layer that routes by scores carries out its other options or refuses them (host only: no call goes through)."""
+import dataclasses
+
 import pytest
 import torch
 
@@ -58,10 +60,11 @@ def test_the_router_product_by_scores(calls):
 def test_the_router_product_and_scores_against_both_calls():
     from paper_2607_05116_amd.layer import DeviceLayer
     from workloads import generator as gen
-    layer = DeviceLayer(CFG, gen.logits(CFG), gen.activations(CFG), *gen.sequential_placement(CFG), 0.1)
+    cfg = dataclasses.replace(CFG, E=32)               # the router's product takes 17 experts at least
+    layer = DeviceLayer(cfg, gen.logits(cfg), gen.activations(cfg), *gen.sequential_placement(cfg), 0.1)
     g = torch.Generator(device="cuda").manual_seed(1)
-    w_gate = (torch.randn((CFG.E, CFG.d), generator=g, device="cuda") / 16).to(torch.bfloat16)
-    logits = torch.empty((CFG.T, CFG.E), device="cuda")
+    w_gate = (torch.randn((cfg.E, cfg.d), generator=g, device="cuda") / 16).to(torch.bfloat16)
+    logits = torch.empty((cfg.T, cfg.E), device="cuda")
     layer.router_route(w_gate, logits)
     layer.logits.copy_(logits)
     layer.set_scores("sigmoid", n_groups=4, topk_groups=2, group_top=2, scale=2.5)
