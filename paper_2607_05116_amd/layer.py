@@ -30,6 +30,13 @@ def to_device_rows(a: np.ndarray, dtype: str, device) -> torch.Tensor:
     return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(device)
 
 
+def _capturing(stream) -> bool:
+    if not isinstance(stream, torch.cuda.Stream):
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 class DeviceLayer:
     """Buffers and calls for one layer configuration.
 
@@ -113,8 +120,8 @@ class DeviceLayer:
     def set_rank_weights(self, rank: int, w1: np.ndarray, w3: np.ndarray, w2: np.ndarray):
         """w1, w3 [E_loc][inter][d], w2 [E_loc][d][inter] in local-slot order (storage type)."""
         self.weights[rank] = tuple(to_device_rows(w, self.cfg.dtype, self.dev) for w in (w1, w3, w2))
-        if rank in self.weights_fp8:
-            self.quantise_weights(rank)
+        if self.fp8 or rank in self.weights_fp8:
+            self._complete_fp8(rank)
 
     def set_scores(self, kind: str | None = "sigmoid", n_groups: int = 1, topk_groups: int = 1, group_top: int = 1,
                    normalise: bool = True, scale: float = 1.0, bias=None, token_mask=None):
@@ -140,8 +147,9 @@ class DeviceLayer:
             normalise, scale, bias, token_mask)
 
     def set_fp8(self, on: bool = True):
-        """The routed experts in 8-bit floating point: their weights quantised in blocks of 128 x 128 (each rank's at its
-        first step, or by quantise_weights after they change), the tokens' rows at every step."""
+        """The routed experts in 8-bit floating point: their weights quantised in blocks of 128 x 128 (here and in
+        set_rank_weights, which both wait for it; by quantise_weights after they change in place), the tokens' rows at
+        every step."""
         cfg = self.cfg
         if on and (cfg.dtype != "bf16" or self.d % 128 or cfg.inter % 128):
             raise ValueError("8-bit experts take a bf16 layer with d and inter multiples of 128")
@@ -151,10 +159,26 @@ class DeviceLayer:
             self.x8_scale = torch.empty((cfg.T, self.d // 128), dtype=torch.float32, device=self.dev)
             self.ws_fp8 = self._ws(capi.cap_workspace_size(capi.CAP_OP_EXPERT_FFN_FP8, None, self.d, cfg.inter,
                                                            self.row_cap))
+        if on:
+            for rank in self.weights:
+                if rank not in self.weights_fp8:
+                    self._complete_fp8(rank)
+
+    def _complete_fp8(self, rank: int):
+        """quantise_weights, complete for every stream, as the weights themselves are after set_rank_weights: what still
+        reads codes from before ends first."""
+        if self.dev.type != "cuda":                     # no kernel runs there
+            return
+        torch.cuda.synchronize(self.dev)
+        self.quantise_weights(rank)
+        torch.cuda.synchronize(self.dev)
 
     def quantise_weights(self, rank: int, stream=None):
-        """The rank's weights in e4m3 with their scales, from set_rank_weights' (buffers are kept)."""
+        """The rank's weights in e4m3 with their scales, from set_rank_weights' (buffers are kept), asynchronously on the
+        stream: other streams wait for it before they read them."""
         if rank not in self.weights_fp8:
+            if _capturing(stream):
+                raise RuntimeError(f"rank {rank} has no 8-bit weights yet: quantise them before a graph is captured")
             made = []
             for w in self.weights[rank]:
                 E_loc, n, k = w.shape
@@ -268,13 +292,15 @@ class DeviceLayer:
                                     stream=stream)
 
     def quantise_x(self, stream=None):
-        """The tokens' rows in e4m3, once for all experts that read them."""
+        """The tokens' rows in e4m3, for all experts of a rank (a step quantises them again for each rank it runs)."""
         capi.cap_quantise_fp8(self.dt, 1, self.cfg.T, self.d, 1, self.x, self.x8, self.x8_scale, stream)
 
     def ffn_fp8(self, rank: int, stream=None):
         """ffn_gather in 8-bit floating point, from quantise_x's rows."""
-        if rank not in self.weights_fp8:
-            self.quantise_weights(rank, stream)
+        if rank not in self.weights_fp8:                # its weights came another way than by set_rank_weights
+            if _capturing(stream):
+                raise RuntimeError(f"rank {rank} has no 8-bit weights yet: quantise them before a graph is captured")
+            self._complete_fp8(rank)
         w1, s1, w3, s3, w2, s2 = self.weights_fp8[rank]
         E_loc = self.cfg.E_loc
         offs = self.lay_t["expert_offsets"][rank * E_loc:(rank + 1) * E_loc + 1]
