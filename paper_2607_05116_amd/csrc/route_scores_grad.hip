@@ -24,7 +24,8 @@ struct ScoreGradArgs {
     const float* d_add;
     void* out;
     int T, E, k, sigmoid, normalise;
-    float inv_scale;
+    float inv_scale;             // 1 / scale in two factors, inv_scale 2^-scale_exponent: of the least scales it is infinite
+    int scale_exponent;
 };
 
 __device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(256) void route_scores_grad_kernel(const ScoreGradA
     float total = g;
 #pragma unroll
     for (int d = 1; d < 8; d *= 2) total += __shfl_xor(total, d);
-    const float slot = (a.normalise ? g - wk * (total * a.inv_scale) : g) * one_less;
+    const float slot = (a.normalise ? g - wk * __builtin_ldexpf(total * a.inv_scale, -a.scale_exponent) : g) * one_less;
     float(*const mine)[4 * L] = rows[wave];
     const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -185,7 +186,8 @@ cap_status route_scores_grad_launch(int T, int k, int E, const float* logits, co
     a.k = k;
     a.sigmoid = opt->kind == CAP_SCORE_SIGMOID;
     a.normalise = opt->normalise != 0;
-    a.inv_scale = 1.0f / opt->scale;
+    a.inv_scale = 0.5f / frexpf(opt->scale, &a.scale_exponent);
+    a.scale_exponent -= 1;
     if (dtype == CAP_DTYPE_BF16) launch_grad<uint16_t>(a, st);
     else launch_grad<float>(a, st);
     CAP_LAUNCH_CHECK();

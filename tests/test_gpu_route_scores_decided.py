@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 import scores_reference as ref
-from test_gpu_route_scores import CASES, COST, PLAIN, SIGMOID, _route, capi  # noqa: F401  (a fixture)
+from test_gpu_route_scores import CASES, COST, PLAIN, SIGMOID, _grad, _route, capi  # noqa: F401  (a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -99,3 +99,35 @@ def test_experts_off_and_tokens_masked(capi, case, p):  # noqa: F811
     bias = (0.3 * rng.standard_normal(E)).astype(np.float32) if biased else None
     rank = rng.permutation(np.arange(E, dtype=np.int32) // (E // R)).astype(np.int32)
     _all_decided(capi, logits, k, R, node, p_case if p is None else p, opt, bias, token_mask, rank)
+
+
+# ------------------------------------------------------------------ the gradient at any scale
+@pytest.mark.parametrize("scale", [1e-44, 1e-39, 2.0 ** -128, 2.0 ** -126, 1e-30, 2.5, 1e30, 2.0 ** 127, 3.4e38])
+@pytest.mark.parametrize("kind,normalise", [("sigmoid", True), ("sigmoid", False), ("softmax", True), ("softmax", False)])
+def test_gradient_at_the_ends_of_the_scales(capi, kind, normalise, scale):  # noqa: F811
+    """Finite scales above 0, whose inverse need not be a number of fp32."""
+    T, E, k = 40, 32, 4
+    rng = np.random.default_rng(11)
+    logits = (2.0 * rng.standard_normal((T, E))).astype(np.float32)
+    idx = np.stack([rng.permutation(E)[:k] for _ in range(T)]).astype(np.int32)
+    keep = (rng.random((T, k)) < 0.8).astype(np.uint8)
+    d_w = (rng.standard_normal((T, k)) / 64).astype(np.float32)
+    scale = float(np.float32(scale))
+    opt = dict(kind=kind, normalise=normalise, scale=scale)
+    w64 = ref.gates(logits.astype(np.float64), idx, keep, kind, normalise, scale)
+    got = _grad(capi, logits, idx, keep, w64.astype(np.float32), d_w, opt, None, False).astype(np.float64)
+    want = ref.grad(logits.astype(np.float64), idx, keep, d_w.astype(np.float64), kind, normalise, scale)
+    assert np.isfinite(got).all()
+    # what test_grad counts, and what is lost below the least normal number: a gate is off by 2^-150 there, and so is each
+    # product; the gates over the scale are at most 1 + 2^-150 / scale, the sum of four products over it that of |d_w|
+    terms = np.abs(w64 * d_w * keep)
+    least = 2.0 ** -149
+    share = np.abs(w64) / scale + least / scale
+    size, lost = np.zeros((T, E)), np.zeros((T, E))
+    np.put_along_axis(size, idx, terms + share * terms.sum(1, keepdims=True), 1)
+    rounding = least * (2.0 + np.abs(d_w))                       # of w d_w
+    np.put_along_axis(lost, idx, rounding + share * rounding.sum(1, keepdims=True) + least * (np.abs(d_w).sum(1, keepdims=True) + 2.0), 1)
+    if kind == "softmax" and not normalise:
+        size += terms.sum(1, keepdims=True)
+        lost += rounding.sum(1, keepdims=True) + 2 * least
+    assert np.all(np.abs(got - want) <= 32 * 2.0 ** -24 * size + 2.0 ** -24 * np.abs(want) + 4 * lost + 2.0 ** -49 * terms.sum(1, keepdims=True))
