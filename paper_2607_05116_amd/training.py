@@ -152,6 +152,7 @@ class RouterTrainer:
         self.mask = torch.empty(T, dtype=torch.int64, device=dev)
         self.logits = torch.empty((T, E), dtype=torch.float32, device=dev)
         self.counts = torch.empty((n_seq, E), **i32)
+        self.folded = torch.empty((max(n_seq // 2, 1), E), **i32)
         self.probs = torch.empty((n_seq, E), dtype=torch.float32, device=dev)
         self.tokens = torch.empty(n_seq + 2, **i32)
         self.loss = torch.empty(3, dtype=torch.float32, device=dev)
@@ -255,12 +256,22 @@ class RouterTrainer:
         return torch.mul(self.keep, self.counted[:, None], out=self.kept)
 
     def _update_bias(self):
-        loads = self.counts.sum(0, dtype=torch.float32)
-        self.bias.add_(torch.sign(loads.mean() - loads), alpha=self.scores.bias_speed)
+        # whole numbers: fp32 sums would lift or lower experts of just the mean load
+        loads = self.expert_loads()
+        self.bias.add_(torch.sign(loads.sum() - loads * self.E).to(torch.float32), alpha=self.scores.bias_speed)
 
     def expert_loads(self) -> torch.Tensor:
-        """Kept slots per expert of the last batch."""
-        return self.counts.sum(0)
+        """Kept slots per expert of the last batch (int64 [E])."""
+        # the sequences' counts are folded by halves: a library sum over many blocks clears its own memory by a call that
+        # goes wrong in replays of a captured graph after the first
+        rows, n = self.counts, self.n_seq
+        while n > 1:
+            half = n // 2
+            torch.add(rows[:half], rows[half:2 * half], out=self.folded[:half])
+            if n % 2:
+                self.folded[0].add_(rows[n - 1])
+            rows, n = self.folded, half
+        return rows[0].to(torch.int64)
 
 
 def _example(steps: int = 40):
