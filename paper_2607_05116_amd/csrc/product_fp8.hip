@@ -10,7 +10,11 @@
 // result on normal values, measured; what follows is fp32): far below a bf16 result's
 // rounding, but not an fp32 one's, so products with an fp32 result are taken on the
 // bf16 instructions, at half the rate: a code's value is a bf16 value, and those
-// products are exact.  The weights are the MFMA's first operand: a lane
+// products are exact.  H, whose codes an error of 1.4e-5 moves across a border once in some
+// thousands, is taken so for few rows (1 to 2 % of the time), but not for many: there exact
+// products take 2.60 ms instead of 1.36 for 33,234 rows of d = 7168, inter = 2048 (and 92 us
+// instead of 55 for 3,001 of d = 2048, inter = 1408), and y, in bf16, is then off by 0.00167 of
+// its norm against 64 bits instead of 0.0020 (0.0021).  The weights are the MFMA's first operand: a lane
 // then holds four consecutive outputs n of one row, one activation scale a lane and
 // block of rows, and the weights' scale is the same for a wave.
 #pragma clang fp contract(off)
@@ -183,7 +187,11 @@ __device__ __forceinline__ void lds_barrier() {
 
 // One tile of 128 rows x 128 weight rows, four waves of 64 x 64; K in stages of 128, two of
 // them on their way: a stage's fragments are read at once, then its buffer is filled again.  For fp32 results, and for bf16 ones whose rows the wide
-// kernel cannot load or store (n % 8 or y's address).  OUT: uint16_t (bf16) or float.
+// kernel cannot load or store (n % 8 or y's address).  OUT: uint16_t (bf16) or float.  33,234 rows
+// of 8 experts, kdim = 2048: n = 7165 in bf16 730 us (1.34 PFLOP/s, half of the 8-bit library
+// product's), n = 7168 in fp32 991 us (0.98, 0.7 of the bf16 library product's, whose instructions it
+// uses): a stage's LDS reads lie between two barriers before its first MFMA, and every wave converts
+// its own fragments.
 template <typename OUT>
 __global__ __launch_bounds__(256) void f8_tile_kernel(const F8Args a) {
     constexpr int NW = 4, WM = 64, WN = 64, MI = WM / 16, NJ = WN / 16;
@@ -782,7 +790,7 @@ cap_status launch_tiles(const F8Args& a, hipStream_t st) {
 // their sums in LDS in the waves' order.  SwiGLU: four waves take W1 and four W3, and H
 // leaves in fp32: quantising it takes 128 of its columns, and workgroups of so many leave
 // half of the compute units without one.  The weights' bytes bound it: 8 rows of 8 experts,
-// d = 7168, inter = 2048: 76 us for 352 MB, 4.65 TB/s (weights through LDS in tiles 120 us).
+// d = 7168, inter = 2048: 71 us for 352 MB, 4.95 TB/s (weights through LDS in tiles 120 us).
 template <int BM>
 __device__ __forceinline__ bool find_rows(const F8Args& a, int NT, Tile& out) {
     const int lane = threadIdx.x & 63, id = blockIdx.x;

@@ -2,8 +2,9 @@
 // fp8_device.hpp): blocks of 1 x 128 (rows of activations) or 128 x 128 (weights).
 //
 // Both read each value once and write each code once, so memory bounds them: 32,768 rows of
-// 7168 in bf16 126 us (5.6 TB/s of 712 MB), weights of 16 x 768 x 2048 in fp32 21.9 us (5.7
-// TB/s of 126 MB); a copy reaches 4.85 TB/s, writing alone 6.9.
+// 7168 in bf16 126 us (5.6 TB/s of 712 MB), weights of 16 x 768 x 2048 in fp32 26 us (4.8
+// TB/s of 126 MB; 21.8 us if they were read just before, and lie in the last-level cache); a copy
+// reaches 4.85 TB/s, writing alone 6.9.
 #include <hip/hip_runtime.h>
 
 #include "fp8_device.hpp"

@@ -129,9 +129,10 @@ __device__ __forceinline__ double group_total(double a, double b, int top) {
     return top > 1 && b > kNoKey ? a + b : a;
 }
 
-// Tokens up to which eight lanes take one: more of them fill the chip, at the price of one join
-// more (tokens of 256 experts in 8 groups: 32 of them 8.0 us with eight lanes, 9.8 with four and
-// 10.1 with sixteen; 8,192 12.5, 14.2 and 17.4; 16,384 15.5, 14.8 and 24).
+// Tokens up to which eight lanes take one, not four: they fill the chip sooner, at the price of
+// one join more.  us with eight and with four: 256 experts in 8 groups, 32 tokens 7.5 and 9.4,
+// 8,192 11.8 and 13.6, 12,288 14.3 and 13.5, 32,768 21.0 and 18.7; 96 experts in 12 groups
+// (through LDS) 9.2 and 13.0, 13.2 and 17.9, 13.2 and 18.0, 22.0 and 22.8.
 constexpr int kTokens8 = 12288;
 
 // Slots of the routing: s = 0 .. N - 1 as a compile-time loop.
@@ -263,12 +264,16 @@ __device__ __forceinline__ int dpp_swap_i32(int v) { return __builtin_amdgcn_mov
 //           unsure (about one of 2000) are chosen by exact_choice.  Else it goes by logits.
 //   GROUPS  0: one group (or all of them open); 1: groups of 4 L CPG experts, which are whole
 //           values of c; 2: any, through LDS
-// What bounds it: instruction issue, most of it the selection network.  32,768 tokens of 256
-// experts in 8 groups, sigmoid with a bias, pruned: 20.8 us (35.8 with all scores in fp64: one
-// wave a SIMD, for the registers of 64 keys a lane; keys are formed block by block now, and fp64
-// is left to the chosen slots), 4 us of which are the unsure tokens; to read and write 36 MB
-// takes 8.  32 tokens: 7.7 us, a chain of joins.  If every token is unsure (all logits alike),
-// 32,768 take 90 us.
+// What bounds it: instruction issue.  32,768 tokens of 256 experts in 8 groups, sigmoid with a
+// bias, pruned: 18.8 us (35.8 with all scores in fp64: one wave a SIMD, for the registers of 64
+// keys a lane; keys are formed block by block now, and fp64 is left to the chosen slots); to read
+// and write 36 MB takes 8.  A wave has 2,852 vector instructions.  The routing by the chosen
+// logits' softmax, whose selection network is the same and which takes 8.0 us for these logits, has
+// 1,314: the others are around the network, where every value is asked whether it is finite, scored,
+// biased, compared for its group, closed with it and counted if it is within reach of the last.
+// Unsure tokens cost under 0.2 us, but if every token is one (all logits alike), 32,768 take 90 us.
+// 32 tokens: 7.5 us, a chain of joins.  Through LDS (GROUPS 2), with loads of single values: 96
+// experts in 12 groups 22.8 us, 160 in 8 groups 43 us.
 template <int L, int V, int KP, bool SCORE, bool VEC, int GROUPS, int CPG>
 __global__ __launch_bounds__(256) void route_scores_kernel(const ScoreArgs a) {
     constexpr int C = V / 4, kTokens = 256 / L;
