@@ -128,7 +128,8 @@ class DeviceLayer:
         """Route by scores (cap_route_scores): kind "sigmoid" or "softmax" (None: back to the softmax over the chosen
         logits); bias fp32 [E], token_mask uint8 or bool [T] on the device, read at every step.  The front end then runs
         as separate calls.  Pruning is by device: expert-level pruning (naive) and the fused call route_layout are
-        refused meanwhile."""
+        refused meanwhile.  A captured step goes on reading the tensors that it was captured with: keep them, and write
+        into them to change what it reads."""
         if kind is None:
             self.scores = None
             return
